@@ -34,6 +34,8 @@
 
 #include "common.cuh"
 #include "quant_device.cuh"
+#include "tcgen05.cuh"
+#include "tensor_map.cuh"
 
 namespace fp4q {
 
@@ -139,11 +141,6 @@ constexpr int kTmemSfBase = 256;
 template <int KIND> struct SfCols { static constexpr int kStride = KIND == KIND_MXF4B16 ? 48 : 32; };
 static_assert(kTmemSfBase + 5 * SfCols<KIND_MXF4>::kStride <= kTmemCols && kTmemSfBase + 4 * SfCols<KIND_MXF4B16>::kStride <= kTmemCols,
               "tensor memory budget: 256 accumulator columns + one scale slot per ring stage");
-constexpr uint32_t kWaitLimit = 1u << 22;       // default number of polls after which a wait gives up (workspace word 2 overrides it)
-// Longest suspension of one suspending poll: without it the limit is the system's, and a number of polls bounds nothing.  With
-// 2^22 polls a wait gives up after about four seconds at the latest.
-constexpr uint32_t kSuspendNs = 1000;
-constexpr int kRelaxedNs = 64, kLazyNs = 256;   // back-off between polls of roles with slack
 // Developer diagnostic (off by default): -DFP4Q_TRACE makes CTA 0 add up clock64() intervals of its roles in
 // registers and leave them in the workspace's padding words (status[16 + 2*slot], 64-bit each).
 #ifdef FP4Q_TRACE
@@ -231,43 +228,6 @@ struct Tile {
 
 // ---------------------------------------------------------------------------------------- PTX helpers
 
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.b32 %0, 1, 0, p;\n}"
-                 : "=r"(ok) : "r"(bar), "r"(parity), "r"(kSuspendNs) : "memory");
-    return ok != 0;
-}
-
-// Non-blocking probe of a barrier phase (the try_wait form may suspend the thread for a while).
-__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}"
-                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-// One lane of a converged warp.
-__device__ __forceinline__ bool elect_one()
-{
-    uint32_t p;
-    asm volatile("{\n .reg .pred P;\n elect.sync _|P, 0xFFFFFFFF;\n selp.b32 %0, 1, 0, P;\n}" : "=r"(p));
-    return p != 0;
-}
 // Named barrier on which the MMA warp and the warp that watches a ring slot for it meet (64 threads).  Both sides use the waiting
 // form: with a non-waiting arrival a watcher that has given up, and only counts the remaining stages, could complete a barrier phase on
 // its own and leave the MMA warp without a partner.  It says so with its arrival; returns whether the stage may be used.
@@ -278,72 +238,6 @@ __device__ __forceinline__ bool named_meet(uint32_t id, bool usable)
     return r != 0u;
 }
 
-// Bounded wait.  Returns false when the limit ran out (the timeout is then recorded) or when another
-// role of this CTA has already given up, which it looks for after every suspension and after every 256th probe.  Every poll
-// of an mbarrier is a shared-memory transaction that competes with the tensor core's operand reads and with the other
-// roles' waits: a suspended thread makes one in kSuspendNs at most.
-template <int BACKOFF_NS, bool PROBE = false>
-__device__ __forceinline__ bool mbar_wait_impl(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t *status,
-                                               uint64_t limit, uint32_t where)
-{
-    for (uint64_t it = 1; ; it++) {
-        if (PROBE ? mbar_test_wait(bar, parity) : mbar_try_wait(bar, parity)) return true;
-        if (BACKOFF_NS > 0) __nanosleep(BACKOFF_NS);
-        if ((!PROBE || ((uint32_t)it & 255u) == 0u) && *abort_flag) return false;
-        if (it >= limit) break;   // after the first poll: a wait that need not wait does not wait for the limit's load either
-    }
-    *abort_flag = 1u;
-    if (atomicCAS(status, 0u, (uint32_t)FP4Q_ERR_TIMEOUT) == 0u) status[1] = where;
-    return false;
-}
-__device__ __noinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t *status, uint64_t limit,
-                                       uint32_t where)
-{
-    return mbar_wait_impl<0>(bar, parity, abort_flag, status, limit, where);
-}
-// For the end of an aborted launch, when the abort flag is set already: 256 polls, a third of a millisecond at most.
-__device__ __noinline__ void mbar_drain(uint32_t bar)
-{
-    for (int it = 0; it < 256 && !mbar_try_wait(bar, 0u); it++) __nanosleep(kLazyNs);
-}
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
-
-// The same load issued by either CTA of a pair: the bytes are counted on the barrier at this address in the
-// pair's leader CTA (cta_group::2 permits the barrier to live in the peer).
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t leader_bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(leader_bar) : "memory");
-}
-// shared::cluster address of this CTA's shared-memory location `addr` as seen in CTA `rank` of the cluster
-__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-// What such an arrival announces lies in this CTA's own shared memory or tensor memory and was made visible to the asynchronous proxy
-// or fenced before; the other CTA only issues the instructions that read it here.  Release at the default scope, this CTA, orders the
-// two, as an assumption about the hardware: that an SM has performed its own stores and the fence behind them before a later
-// arrival of the same thread leaves it.  PTX's memory model does not promise it; there, only release and acquire that both
-// reach the cluster order one CTA's writes before another's reads, and the waits on these barriers have the default scope too.
-// Were it wrong, a pair's MMAs would read scale images of the second CTA that are not written yet, or overwrite an accumulator that is
-// still being read: wrong results and no error.  Release at cluster scope for the images costs a product 0.45 to 0.6 us (forward
-// 2048 x 2048 x 2048 9.9 -> 10.4, 8192 x 2048 x 2048 20.5 -> 21.0, 16384 x 4096 x 4096 94.5 -> 95.2; 16 x 16 blocks there 116.8 -> 121.5).
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)
-{
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-__device__ __forceinline__ uint32_t cluster_ctarank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
 // The kernel's first barrier, which every warp passes at a place of its own: behind it the mbarriers of the CTA, or of both CTAs of
 // a pair, exist.  In a pair warps arrive ahead of time (warp 4, which initializes them, after its fence.mbarrier_init), so that the
 // way from one CTA to the other is under way while a role prepares what needs nobody else.  Only warp 1 arrives late: behind its
@@ -352,9 +246,6 @@ __device__ __forceinline__ uint32_t cluster_ctarank()
 // (2048 x 2048 x 2048 8.1 / 8.3 / 9.3 and 8.1 / 8.1 / 9.2), per-row kinds 1 to 1.5 % for small ones (16 x 16 blocks 8192 x 2048 x 2048 22.6 / 22.2 / 19.7 and
 // 22.9 / 22.4 / 20.0, MXFP8 there 29.8 and 30.2).  In one CTA nobody waits for the builders, which come late and have a barrier of
 // their own with warp 4.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 template <int CTAS, int BUILDERS, bool BUILDER = false>
 __device__ __forceinline__ void start_sync()
 {
@@ -363,31 +254,6 @@ __device__ __forceinline__ void start_sync()
     else asm volatile("bar.sync 13, %0;" ::"n"(kThreads - 32 * BUILDERS) : "memory");
 }
 
-// TMA stores out of shared memory (bulk async-group completion).
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, int32_t x, int32_t y, uint32_t src)
-{
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
-}
-__device__ __forceinline__ void tma_reduce_add_2d(const CUtensorMap *map, int32_t x, int32_t y, uint32_t src)
-{
-    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
-}
-__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read_all() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-
-__device__ __forceinline__ void tcgen05_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tcgen05_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-
-template <int CTAS>
-__device__ __forceinline__ void tcgen05_commit(uint32_t bar)
-{
-    if (CTAS == 1) {
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-    } else {   // arrives on the barrier at this offset in both CTAs of the pair
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                     ::"r"(bar), "h"((uint16_t)3) : "memory");
-    }
-}
 template <int CTAS>
 __device__ __forceinline__ void tcgen05_cp_32x128b_warpx4(uint32_t taddr, uint64_t sdesc)
 {
@@ -432,12 +298,6 @@ __device__ __forceinline__ void tcgen05_mma_block_scaled(uint32_t d_tmem, uint64
     }
 }
 
-// Shared-memory matrix descriptor, K-major operand tile stored as rows of 128 B with the 128-byte swizzle
-// (8-row groups 1024 B apart).
-__device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t addr)
-{
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
 // Descriptor of a replicated scale image: 8 rows of 16 B; the stride between 8-row groups is zero, so the 32 rows
 // tcgen05.cp reads are four passes over the same 128 bytes.
 __device__ __forceinline__ uint64_t smem_desc_scale_image_rep(uint32_t addr)
@@ -458,17 +318,6 @@ __device__ __forceinline__ uint32_t instr_desc(uint32_t a_sf_id, uint32_t b_sf_i
     return (b_sf_id << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(BN >> 3) << 17) | (1u << 23) |
            ((uint32_t)((BM * CTAS) >> 4) << 24) | (a_sf_id << 29);
 }
-
-#define FP4Q_TMEM_LD_X32(taddr, v)                                                                              \
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "                                                      \
-                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"                                      \
-                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"                     \
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), \
-                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]),      \
-                   "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]),    \
-                   "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]),    \
-                   "=r"(v[29]), "=r"(v[30]), "=r"(v[31])                                                         \
-                 : "r"(taddr))
 
 // ---------------------------------------------------------------------------------------- tile decoding
 
@@ -2142,37 +1991,6 @@ gemm_block_scaled_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_c
 
 // ---------------------------------------------------------------------------------------- host side
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiledFn encode_tiled_fn()
-{
-    static const EncodeTiledFn fn = [] {   // several threads may make their first product at the same time: all but one wait
-        void *ptr = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        const bool found = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) == cudaSuccess && qres == cudaDriverEntryPointSuccess;
-        return found ? reinterpret_cast<EncodeTiledFn>(ptr) : nullptr;
-    }();
-    return fn;
-}
-// The encoder wants a context on the calling thread, which the runtime binds with the thread's first call that needs one; a thread whose first
-// call is a product has made none.
-static bool encode_tiled(CUtensorMap *map, CUtensorMapDataType type, int rank, void *base, const cuuint64_t *dims, const cuuint64_t *strides,
-                         const cuuint32_t *box, CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion)
-{
-    const EncodeTiledFn fn = encode_tiled_fn();
-    if (!fn) return false;
-    const cuuint32_t estr[5] = {1u, 1u, 1u, 1u, 1u};
-    auto encode = [&] {
-        return fn(map, type, (cuuint32_t)rank, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, promotion, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    };
-    CUresult r = encode();
-    int dev;
-    if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess) r = encode();
-    return r == CUDA_SUCCESS;
-}
-
 // Operand tile map: a [rows, row_bytes] byte matrix with pitch ld_bytes, box = 128 B x box_rows, 128B swizzle.
 static bool make_operand_map(CUtensorMap *map, const void *base, int64_t rows, int64_t row_bytes, int64_t ld_bytes,
                              int box_rows)
@@ -2213,26 +2031,6 @@ struct Operand {
     int64_t rows, row_bytes, ld_bytes;
     ScaleView sf;
 };
-
-constexpr int kMaxDevices = 64;   // per-device host state (attributes set, SM counts, static workspace address); threads that find it unset all set the same
-
-static int current_device()
-{
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return -1;
-    return dev;
-}
-
-static int sm_count(int dev)
-{
-    static std::atomic<int> known[kMaxDevices];
-    int n = known[dev].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
-        known[dev].store(n, std::memory_order_relaxed);
-    }
-    return n;
-}
 
 // Most row tiles that pairs can have with grouped rows on multiples of 128: a group with an odd number has one alone.
 static int64_t paired_tiles(const GemmParams &p)
