@@ -54,7 +54,9 @@ typedef enum {
 
 /* FP4Q_OUT_PADDED, added to either type: the bytes from a row's last column up to the next multiple of 16 are padding that the
  * call may write (zeros; nothing is added to them that changes them).  It saves rows that end inside 16 bytes stores of their own. */
-typedef enum { FP4Q_OUT_BF16 = 0, FP4Q_OUT_F32 = 1, FP4Q_OUT_PADDED = 0x100 } fp4q_out;
+/* FP4Q_OUT_ZERO_REST, added to either type of fp4q_ragged_gemm_fwd / _dgrad: rows of the output that no group owns are written as zeros
+ * instead of being left alone. */
+typedef enum { FP4Q_OUT_BF16 = 0, FP4Q_OUT_F32 = 1, FP4Q_OUT_PADDED = 0x100, FP4Q_OUT_ZERO_REST = 0x200 } fp4q_out;
 
 /* fp4q_quantize2d flag: key the stochastic-rounding stream on the element's index in the
  * TRANSPOSED tensor (j*rows + i instead of i*cols + j), so that quantize(A^T) with this flag
@@ -377,6 +379,52 @@ fp4q_status fp4q_gemm_wgrad_b16(const fp4q_tensor *dY, const fp4q_tensor *X, voi
  */
 fp4q_status fp4q_gemm_fwd_static_workspace(const fp4q_tensor *X, const fp4q_tensor *W, void *Y, int64_t ldy,
                                            fp4q_out dt, uint32_t *status_out, void *stream);
+
+/*
+ * fp4q_ragged_gemm_fwd / _dgrad / _wgrad -- no counterpart in the paper's method; its runs are compared with BF16 ones: the three products
+ * of Section 3, "Application to linear layers", on BF16 operands, for groups of rows of any size (a mixture-of-experts layer without
+ * padding, or one kept out of FP4):
+ *   Y[T,N]  = X[T,K] W_g[N,K]^T,   dX[T,K] = dY[T,N] W_g[N,K],   dW_g[N,K] (+)= dY_g[.,N]^T X_g[.,K]
+ * Group g owns rows row_offsets[g] .. row_offsets[g+1]-1: here the offsets need not be multiples of anything (row_alignment 0 or 1 states
+ * nothing; 128 and 256 are accepted and state nothing either), row_offsets[0] may be above 0 and row_offsets[n_groups] below T.  Groups may be
+ * empty.  Rows that no group owns are not read, and not written either (but see FP4Q_OUT_ZERO_REST): what lies there stays there.  Offsets
+ * outside 0..T are held to it, and one that is below an earlier one counts as that one.  n_groups <= 4095 (FP4Q_ERR_UNSUPPORTED); g == NULL:
+ * one group of all rows.  w is the expert stack [w_rows = n_groups*N, K]; dW is such a stack; an empty group's dW is zero (or unchanged
+ * when accumulating).
+ * Any T, N and K, 0 included.  Operands are 16-byte aligned with leading dimensions in multiples of 8 elements; outputs are BF16 or FP32
+ * (dt; FP4Q_OUT_PADDED may be added and changes nothing), 16-byte aligned with rows of whole 16 bytes, and only their columns are
+ * written.  accumulate != 0 adds to dW (FP32 only).  FP32 accumulation; an FP32 output is the sum, rounded to nearest, of partial
+ * sums over 512 contraction elements each, so that the tensor cores' cut-off towards zero does not add up over a long contraction.
+ * A group's result does not depend on the other groups.  ws/ws_bytes/stream and the asynchronous FP4Q_ERR_TIMEOUT as for fp4q_gemm_fwd.
+ */
+fp4q_status fp4q_ragged_gemm_fwd(const void *x_bf16, int64_t T, int64_t K, int64_t ldx, const void *w_bf16, int64_t w_rows, int64_t ldw,
+                                 void *Y, int64_t ldy, fp4q_out dt, const fp4q_groups *g, void *ws, size_t ws_bytes, void *stream);
+fp4q_status fp4q_ragged_gemm_dgrad(const void *dy_bf16, int64_t T, int64_t N, int64_t ld_dy, const void *w_bf16, int64_t w_rows, int64_t K,
+                                   int64_t ldw, void *dX, int64_t ldx, fp4q_out dt, const fp4q_groups *g, void *ws, size_t ws_bytes, void *stream);
+fp4q_status fp4q_ragged_gemm_wgrad(const void *dy_bf16, int64_t T, int64_t N, int64_t ld_dy, const void *x_bf16, int64_t K, int64_t ldx,
+                                   void *dW, int64_t ldw, fp4q_out dt, int accumulate, const fp4q_groups *g, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * fp4q_newton_schulz -- no counterpart in the paper: the orthogonalised update of a weight matrix from its gradient, for the master weights
+ * that the quantizers read.  For each of `count` matrices [rows, cols], stacked as the grouped weight gradients leave them (matrix b
+ * starts at row b*rows):
+ *   momentum != NULL:  M = beta M + G (written back);  U = beta M + G if nesterov != 0, else M.    momentum == NULL:  U = G
+ *   X = U / (|U|_F + eps);   steps times, with (a, b, c) = coefficients[3s .. 3s+2] and A = X X^T:   X = a X + (b A + c A A) X
+ *   out = scale X, rounded to BF16
+ * (taken on the shorter side: for rows > cols the same polynomial is evaluated with A = X^T X).  g is BF16 or FP32 (g_type, a plain fp4q_out),
+ * momentum FP32 [count*rows, ld_m], out BF16; each with its leading dimension in elements, aligned to its element.  None of the three may
+ * overlap another.  coefficients is a HOST array, read during the call; steps 1 to 64.  (3.4445, -4.7750, 2.0315) five times is the usual choice.
+ * Coefficients that let a singular value exceed 10, or an eigenvalue of b A + c A A 100, are refused (FP4Q_ERR_UNSUPPORTED): the
+ * products' operands are FP16.  eps >= 0; a matrix U of zeros gives zeros if eps > 0.  A matrix that holds an infinity or NaN gives NaN
+ * and leaves the others as they are.  The iterate X is held in 22 bits and the sum of squares in 64-bit floating point.
+ * scratch: fp4q_newton_schulz_scratch_bytes() bytes of device memory, 256-byte aligned, any contents; calls that share it must not overlap
+ * on the GPU.  fp4q_newton_schulz_scratch_bytes returns 0 for sizes that the call refuses or that are empty.  Sides up to 2^20, up to
+ * 65535 matrices.  ws/ws_bytes/stream and the asynchronous FP4Q_ERR_TIMEOUT as for fp4q_gemm_fwd.
+ */
+size_t fp4q_newton_schulz_scratch_bytes(int64_t count, int64_t rows, int64_t cols);
+fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_t count, int64_t rows, int64_t cols, int64_t ld_g, float *momentum,
+                               int64_t ld_m, float beta, int nesterov, const float *coefficients, int32_t steps, float eps, float scale,
+                               void *out_bf16, int64_t ld_o, void *scratch, size_t scratch_bytes, void *ws, size_t ws_bytes, void *stream);
 
 const char *fp4q_status_string(fp4q_status s);
 

@@ -86,6 +86,45 @@ def fp4_linear(x: torch.Tensor, weight: torch.Tensor, seed: int = 0, tensor_id: 
     return y.reshape(*lead, weight.shape[0])
 
 
+class _RaggedLinearFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, row_offsets, ws):
+        e, n, k = weight.shape
+        xb, wb = _rows16(x), _rows16(weight.reshape(e * n, k))
+        ctx.save_for_backward(xb, wb, row_offsets)
+        ctx.ws, ctx.shape, ctx.x_dtype, ctx.w_dtype = ws, (e, n, k), x.dtype, weight.dtype
+        return binding.fp4q_ragged_gemm_fwd(xb, wb, row_offsets, ws=ws).contiguous()
+
+    @staticmethod
+    def backward(ctx, dy):
+        xb, wb, row_offsets = ctx.saved_tensors
+        dyb, dx, dw = _rows16(dy), None, None
+        if ctx.needs_input_grad[0]:
+            dx = binding.fp4q_ragged_gemm_dgrad(dyb, wb, row_offsets, ws=ctx.ws).to(ctx.x_dtype)
+        if ctx.needs_input_grad[1]:
+            out = binding.OUT_BF16 if ctx.w_dtype == torch.bfloat16 else binding.OUT_F32
+            dw = binding.fp4q_ragged_gemm_wgrad(dyb, xb, row_offsets, dt=out, ws=ctx.ws).to(ctx.w_dtype).reshape(ctx.shape)
+        return dx, dw, None, None
+
+
+def _rows16(t: torch.Tensor) -> torch.Tensor:
+    """t in BF16 and in rows that start on 16 bytes, as the products read them; t itself where it is so."""
+    t = t.to(torch.bfloat16)
+    rows, cols = t.shape
+    if (cols <= 1 or t.stride(1) == 1) and t.stride(0) % 8 == 0 and t.stride(0) >= cols and t.data_ptr() % 16 == 0:
+        return t
+    out = torch.empty((rows, (cols + 7) // 8 * 8), dtype=torch.bfloat16, device=t.device)[:, :cols]
+    return out.copy_(t)
+
+
+def ragged_linear(x: torch.Tensor, weight: torch.Tensor, row_offsets: torch.Tensor, ws=None) -> torch.Tensor:
+    """y_t = weight[g] x_t for the rows t of group g, in BF16: the expert layer as it is without FP4, on groups of any size.  x [T, K], weight
+    [E, N, K], row_offsets int64 [E+1], non-decreasing, all on one GPU; rows that no group owns give zeros and get no gradient."""
+    if ws is None:
+        ws = binding.alloc_workspace(x.device)
+    return _RaggedLinearFn.apply(x, weight, row_offsets, ws)
+
+
 class FP4Linear(torch.nn.Module):
     """Bias-free linear layer with an FP32 master weight and FP4 products.  Each backward pass draws fresh
     stochastic-rounding bits: the module counts its forward calls and uses the count as the Philox tensor id's

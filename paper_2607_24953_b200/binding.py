@@ -32,7 +32,8 @@ EXPORTS = ["fp4q_quantize2d", "fp4q_gemm_fwd", "fp4q_gemm_dgrad", "fp4q_gemm_wgr
            "fp4q_debug_withhold_load", "fp4q_quantize1d", "fp4q_quantize1d_t", "fp4q_gemm_fwd_act1d", "fp4q_gemm_wgrad_act1d",
            "fp4q_mxfp8_quantize1d_t", "fp4q_mxfp8_gemm", "fp4q_gemm_fwd_quantized", "fp4q_gemm_dgrad_quantized",
            "fp4q_gemm_fwd_b16", "fp4q_gemm_dgrad_b16", "fp4q_gemm_wgrad_b16", "fp4q_quantize2d_multi",
-           "fp4q_quantize2d_multi_f32"]
+           "fp4q_quantize2d_multi_f32", "fp4q_ragged_gemm_fwd", "fp4q_ragged_gemm_dgrad", "fp4q_ragged_gemm_wgrad",
+           "fp4q_newton_schulz", "fp4q_newton_schulz_scratch_bytes"]
 
 
 class Fp4qError(RuntimeError):
@@ -129,6 +130,17 @@ def lib() -> ctypes.CDLL:
         L.fp4q_gemm_dgrad_b16.argtypes = b16_args
         L.fp4q_gemm_wgrad_b16.restype = ci
         L.fp4q_gemm_wgrad_b16.argtypes = b16_args[:5] + [ci] + b16_args[5:]
+        L.fp4q_ragged_gemm_fwd.restype = ci
+        L.fp4q_ragged_gemm_fwd.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, i64, ci, ctypes.POINTER(_CGroups), vp, ctypes.c_size_t, vp]
+        L.fp4q_ragged_gemm_dgrad.restype = ci
+        L.fp4q_ragged_gemm_dgrad.argtypes = [vp, i64, i64, i64, vp, i64, i64, i64, vp, i64, ci, ctypes.POINTER(_CGroups), vp, ctypes.c_size_t, vp]
+        L.fp4q_ragged_gemm_wgrad.restype = ci
+        L.fp4q_ragged_gemm_wgrad.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, i64, ci, ci, ctypes.POINTER(_CGroups), vp, ctypes.c_size_t, vp]
+        L.fp4q_newton_schulz_scratch_bytes.restype = ctypes.c_size_t
+        L.fp4q_newton_schulz_scratch_bytes.argtypes = [i64, i64, i64]
+        L.fp4q_newton_schulz.restype = ci
+        L.fp4q_newton_schulz.argtypes = [vp, ci, i64, i64, i64, i64, vp, i64, ctypes.c_float, ci, ctypes.POINTER(ctypes.c_float), ctypes.c_int32, ctypes.c_float,
+                                         ctypes.c_float, vp, i64, vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -363,3 +375,37 @@ def fp4q_mxfp8_qk(xq, xs, wq_q, wq_s, wk_q, wk_s, T: int, K: int, N: int, dt: in
                   stream=None):
     """Q = X^ Wq^^T and K = X^ Wk^^T on MXFP8 operands from fp4q_mxfp8_quantize1d."""
     return _host().mxfp8_qk(xq, xs, wq_q, wq_s, wk_q, wk_s, T, K, N, dt, ws, _handle(stream))
+
+
+def fp4q_ragged_gemm_fwd(x: torch.Tensor, w: torch.Tensor, row_offsets=None, out=None, dt: int = OUT_BF16, ws=None, stream=None):
+    """Y[T,N] = X W_g^T for the rows of every group g, on BF16 operands: x [T, K], w the expert stack [E*N, K], row_offsets int64 [E+1] on the
+    device, any non-decreasing values (None: one group).  Rows that no group owns stay as they are in `out`; in an output that is
+    allocated here they are zero."""
+    return _host().ragged_gemm(_FWD, x, w, row_offsets, out, dt, False, ws, _handle(stream))
+
+
+def fp4q_ragged_gemm_dgrad(dY: torch.Tensor, w: torch.Tensor, row_offsets=None, out=None, dt: int = OUT_BF16, ws=None, stream=None):
+    """dX[T,K] = dY W_g for the rows of every group g; groups and rows that no group owns as in fp4q_ragged_gemm_fwd."""
+    return _host().ragged_gemm(_DGRAD, dY, w, row_offsets, out, dt, False, ws, _handle(stream))
+
+
+def fp4q_ragged_gemm_wgrad(dY: torch.Tensor, x: torch.Tensor, row_offsets=None, out=None, dt: int = OUT_F32, accumulate: bool = False, ws=None,
+                           stream=None):
+    """dW[E*N, K] (+)= dY^T X over the rows of every group; an empty group's is zero."""
+    return _host().ragged_gemm(_WGRAD, dY, x, row_offsets, out, dt, accumulate, ws, _handle(stream))
+
+
+NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+def alloc_newton_schulz_scratch(count: int, rows: int, cols: int, device) -> torch.Tensor:
+    """Scratch memory of fp4q_newton_schulz for `count` matrices [rows, cols]; calls that share it must not overlap on the GPU."""
+    return torch.empty(int(lib().fp4q_newton_schulz_scratch_bytes(count, rows, cols)), dtype=torch.uint8, device=device)
+
+
+def fp4q_newton_schulz(g: torch.Tensor, momentum=None, beta: float = 0.95, nesterov: bool = True, coefficients=NEWTON_SCHULZ, eps: float = 1e-7,
+                       scale: float = 1.0, out=None, scratch=None, ws=None, stream=None) -> torch.Tensor:
+    """The orthogonalised update of weights from their gradient g, BF16 or FP32 [rows, cols] or a stack [count, rows, cols]: with a momentum (FP32,
+    g's shape, updated in place) M = beta M + G and U = beta M + G (nesterov) or M, without one U = G; X = U / (|U| + eps), then one step
+    X = a X + (b A + c A A) X, A = X X^T, per triple of coefficients.  Returns scale X in BF16."""
+    return _host().newton_schulz(g, momentum, beta, nesterov, [v for triple in coefficients for v in triple], eps, scale, out, scratch, ws, _handle(stream))

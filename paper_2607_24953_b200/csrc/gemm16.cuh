@@ -1,0 +1,703 @@
+// Products of 16-bit matrices (BF16 or FP16) on the tensor cores of sm_100a, FP32 accumulation: C[M,N] = A B with either operand
+// stored along the contraction ("K-major") or across it ("MN-major"), for matrices cut into groups of rows that start anywhere, for
+// contractions cut the same way, for stacks of matrices and for symmetric results.  The entry points are in ragged_gemm.cu and
+// newton_schulz.cu.
+//
+// Persistent kernel, one CTA per SM, 12 warps.  A CTA has 128 rows of the accumulator; pairs (cta_group::2) share a tile of 256 rows and
+// each loads half of B's columns, which is what lets 32 KB of operands feed 2 x 256 x 256 x 64 operations per stage; single CTAs have tiles of
+// 128 x 128 or 128 x 64 for problems with few tiles or short groups.
+//   warp 0      TMA producer: a stage is 64 contraction elements, boxes of 128 bytes with the 128-byte swizzle
+//   warp 1      MMA issuer (in the leader of a pair): four tcgen05.mma of 16 contraction elements per stage
+//   warp 2      cut contractions: zeroes the rows of a group's last stage that lie behind the group
+//   warps 4-11  epilogue: a thread has a row of the tile; the accumulator is double-buffered in tensor memory
+// Every wait is bounded: when a limit is hit the CTA records FP4Q_ERR_TIMEOUT in the workspace, its roles stop and it leaves through the
+// normal exit, after its copies in flight have landed.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "tcgen05.cuh"
+#include "tensor_map.cuh"
+
+namespace fp4q {
+
+constexpr int kRows16 = 128;         // accumulator rows per CTA
+constexpr int kK16 = 64;             // contraction elements per stage: 128 bytes
+constexpr int kThreads16 = 384;
+constexpr int kRaster16 = 16;        // row tiles per rasterisation group: their A rows stay in L2 while the columns go by
+constexpr int kMaxGroups16 = 4095;   // boundaries and first tiles of this many groups lie in shared memory
+
+// TILES_ROWS: groups of A rows (and of output rows), a matrix B per group.  TILES_CUT: a product per group, contracted over its rows.
+// TILES_BATCH: a stack of products.  TILES_SYM: a stack of symmetric products; only tiles on and below the diagonal are computed.
+enum { TILES_ROWS = 0, TILES_CUT = 1, TILES_BATCH = 2, TILES_SYM = 3 };
+// EPI16_STORE: BF16 output.  EPI16_SUM: FP32 output.  The others are the three products of a Newton-Schulz step (newton_schulz.cu).
+// The tensor cores cut the sum of an accumulator and 16 products off to FP32, towards zero: the error grows with the contraction, by 1e-9 of
+// the result for every element (2e-5 at 16384; 8e-5 where all products are positive).  BF16 and FP16 outputs do not show it.  FP32
+// ones are sums, to nearest and in registers, of accumulators of 512 elements each.
+enum { EPI16_STORE = 0, EPI16_GRAM = 1, EPI16_POLY = 2, EPI16_UPDATE = 3, EPI16_SUM = 4 };
+constexpr int kSumStages = 8;        // stages that an accumulator takes with EPI16_SUM
+
+template <int CTAS, int BN>
+struct Cfg16 {
+    static_assert(CTAS == 1 || (CTAS == 2 && BN == 256), "tile shapes");
+    static constexpr int kBRows = BN / CTAS;
+    static constexpr int kABytes = kRows16 * 128, kBBytes = kBRows * 128;
+    static constexpr int kStages = BN == 64 ? 8 : 6;
+    static constexpr int kTmemCols = 2 * BN;
+    static constexpr int kOperands = kStages * (kABytes + kBBytes);
+    static constexpr int kTail = 512;                                       // barriers, tensor memory's address, abort flag
+    static constexpr int kTables = 2 * (kMaxGroups16 + 1) * 4;              // row groups and cut contractions only
+    static constexpr int smem(int tiles) { return 1024 + kOperands + kTail + (tiles <= TILES_CUT ? kTables : 0); }
+    static_assert(1024 + kOperands + kTail + kTables <= 227 * 1024, "shared memory budget");
+};
+
+struct Gemm16Params {
+    int32_t m, n, k;                 // output rows and columns and contraction length of one product (TILES_ROWS: m = all rows, TILES_CUT: k = all rows)
+    int32_t m_tiles, n_tiles;        // TILES_ROWS: m_tiles is found on the device
+    int32_t batch;                   // groups or matrices
+    int32_t bf16;                    // operand type: 0 = FP16, 1 = BF16
+    int32_t a_box;                   // rows of one copy of a K-major A operand: 128, or 32 for short groups
+    const int64_t *offsets;          // TILES_ROWS, TILES_CUT: batch + 1 boundaries; NULL: one group of all rows
+    int64_t total_rows;              // rows that the boundaries are held to
+    uint32_t *status;
+    // EPI16_STORE, EPI16_SUM
+    void *c;
+    int64_t ldc;
+    int32_t accumulate, wide, zero_rest;   // zero_rest: rows that no group owns are written as zeros
+    // EPI16_GRAM, _POLY, _UPDATE
+    float fa, fb, fc;                // the step's coefficients, with the iterates' scales
+    const __half *in0, *in1;         // POLY: A.  UPDATE: upper and lower parts of X
+    __half *out0, *out1;             // GRAM: A.  POLY: B.  UPDATE: upper and lower parts of the next X
+    int64_t pitch;                   // of in0, in1, out0, out1
+    __nv_bfloat16 *o;                // UPDATE, last step: the result instead
+    int64_t ld_o;
+    float o_scale;
+    int32_t o_vec;
+};
+
+// A tile as one CTA of it sees it.
+struct Tile16 {
+    int32_t batch, a_row, b_row, k0, k_len;    // where the operands start along M and N, where the contraction starts and how long it is
+    int32_t row, col, rows, rows_peer;         // first output row and column of this CTA's half, its valid rows and the other CTA's
+    bool mirror;                               // TILES_SYM: below the diagonal, so the transposed tile is written too
+};
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+// Of either CTA of a pair: the bytes are counted on the leader's barrier.
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t leader_bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(leader_bar) : "memory");
+}
+// Arrival on a barrier of either CTA of a pair that orders this thread's writes, to shared memory or tensor memory, before what the waiter does.
+__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void fence_cluster_acquire() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
+
+template <int CTAS>
+__device__ __forceinline__ void tcgen05_mma_f16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    if (CTAS == 2)
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                     ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                     ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// MN-major operand tile: chunks of 64 elements x 64 contraction rows (8 KB each), a row of a chunk 128 bytes with the 128-byte swizzle;
+// eight contraction rows make 1024 bytes.
+__device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t addr)
+{
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(8192 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+template <int CTAS, int BN>
+__device__ __forceinline__ uint32_t instr_desc16(bool bf16, bool a_mn, bool b_mn)
+{
+    const uint32_t type = bf16 ? 1u : 0u;
+    return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(BN >> 3) << 17) |
+           ((uint32_t)((kRows16 * CTAS) >> 4) << 24);
+}
+// A whole warp's wait: all lanes go on or none does.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t *status, uint64_t limit, uint32_t where)
+{
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, status, limit, where));
+}
+
+// ---------------------------------------------------------------------------------------- tiles
+
+// start[g], g = 0..n: the boundaries, held to [0, rows] and to rising order: whatever they are, no row outside the matrices is
+// touched and none belongs to two groups.  first[g]: row tiles before group g (TILES_ROWS).
+__device__ __forceinline__ int32_t group_rows(const int32_t *start, int g) { return start[g + 1] - start[g]; }
+
+__device__ __forceinline__ int find_group16(const int32_t *first, int n, int tile)   // the last g with first[g] <= tile; first[0] = 0
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= tile) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+template <int TILES, int CTAS, int BN>
+__device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int m_tiles, const int32_t *start, const int32_t *first, int rank)
+{
+    constexpr int kBM = kRows16 * CTAS, kBRows = Cfg16<CTAS, BN>::kBRows;
+    Tile16 t;
+    int mt, nt;
+    t.batch = 0;
+    t.mirror = false;
+    if (TILES == TILES_SYM) {
+        const int per = m_tiles * (m_tiles + 1) / 2;
+        t.batch = tile / per;
+        const int r = tile - t.batch * per;
+        mt = (int)((sqrtf(8.0f * (float)r + 1.0f) - 1.0f) * 0.5f);
+        while (mt * (mt + 1) / 2 > r) mt--;
+        while ((mt + 1) * (mt + 2) / 2 <= r) mt++;
+        nt = r - mt * (mt + 1) / 2;
+        t.mirror = mt != nt;
+    } else {
+        int r = tile;
+        if (TILES != TILES_ROWS) {
+            const int per = m_tiles * p.n_tiles;
+            t.batch = tile / per;
+            r = tile - t.batch * per;
+        }
+        const int per_group = kRaster16 * p.n_tiles, g = r / per_group, m0 = g * kRaster16, h = min(kRaster16, m_tiles - m0), rem = r - g * per_group;
+        nt = rem / h;
+        mt = m0 + rem - nt * h;
+    }
+    t.col = nt * BN;
+    t.b_row = t.col + rank * kBRows;
+    t.k0 = 0;
+    t.k_len = p.k;
+    int valid;   // rows of the whole tile
+    if (TILES == TILES_ROWS) {
+        t.batch = find_group16(first, p.batch, mt);
+        const int in = (mt - first[t.batch]) * kBM;
+        t.row = start[t.batch] + in;
+        valid = group_rows(start, t.batch) - in;
+    } else {
+        t.row = mt * kBM;
+        valid = p.m - t.row;
+    }
+    if (TILES == TILES_CUT) { t.k0 = start[t.batch]; t.k_len = group_rows(start, t.batch); }
+    t.row += rank * kRows16;
+    t.a_row = t.row;
+    t.rows = max(0, min(kRows16, valid - rank * kRows16));
+    t.rows_peer = CTAS == 2 ? max(0, min(kRows16, valid - (1 - rank) * kRows16)) : 0;
+    return t;
+}
+
+// ---------------------------------------------------------------------------------------- epilogues: 32 columns of a thread's row
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&b);
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi)
+{
+    const __half2 b = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&b);
+}
+__device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+__device__ __forceinline__ uint4 load_uint4(const void *p) { return *static_cast<const uint4 *>(p); }
+__device__ __forceinline__ void store_32_bytes(void *p, const uint32_t *w)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+
+// Row `row` (of all output rows), columns col .. col + 31, of which those below n exist.
+__device__ __forceinline__ void store_bf16(const Gemm16Params &p, int64_t row, int col, const float *v)
+{
+    const int left = p.n - col;
+    if (left <= 0) return;
+    __nv_bfloat16 *c = static_cast<__nv_bfloat16 *>(p.c) + row * p.ldc + col;
+    if (left >= 32) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 16) {
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) w[j] = pack_bf16(v[e + 2 * j], v[e + 2 * j + 1]);
+            if (p.wide) store_32_bytes(c + e, w);
+            else {
+                *reinterpret_cast<uint4 *>(c + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4 *>(c + e + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 32; e++)
+            if (e < left) c[e] = __float2bfloat16_rn(v[e]);
+    }
+}
+__device__ __forceinline__ void store_f32(const Gemm16Params &p, int64_t row, int col, float *v)
+{
+    const int left = p.n - col;
+    if (left <= 0) return;
+    float *c = static_cast<float *>(p.c) + row * p.ldc + col;
+    if (left >= 32) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+            float *w = v + e;
+            if (p.accumulate) {
+                const float4 a = *reinterpret_cast<const float4 *>(c + e), b = *reinterpret_cast<const float4 *>(c + e + 4);
+                w[0] += a.x; w[1] += a.y; w[2] += a.z; w[3] += a.w; w[4] += b.x; w[5] += b.y; w[6] += b.z; w[7] += b.w;
+            }
+            if (p.wide) store_32_bytes(c + e, reinterpret_cast<const uint32_t *>(w));
+            else {
+                *reinterpret_cast<float4 *>(c + e) = make_float4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<float4 *>(c + e + 4) = make_float4(w[4], w[5], w[6], w[7]);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 32; e++)
+            if (e < left) c[e] = p.accumulate ? c[e] + v[e] : v[e];
+    }
+}
+
+// The iterates' rows are padded to whole 32 bytes: a piece of eight columns is written if it starts inside the row.  What columns behind
+// the matrix hold is never read.
+template <int EPI>
+__device__ __forceinline__ void step16(const Gemm16Params &p, const Tile16 &t, int64_t base, int row, int col, const float *v)
+{
+    const int64_t at = base + (int64_t)row * p.pitch + col;
+#pragma unroll
+    for (int e = 0; e < 32; e += 8) {
+        if (col + e >= p.pitch) continue;
+        float w[8];
+        if (EPI == EPI16_GRAM) {
+#pragma unroll
+            for (int j = 0; j < 8; j++) w[j] = v[e + j] * p.fa;
+        }
+        if (EPI == EPI16_POLY) {
+            const uint4 a = load_uint4(p.in0 + at + e);
+            const float2 a0 = unpack_half(a.x), a1 = unpack_half(a.y), a2 = unpack_half(a.z), a3 = unpack_half(a.w);
+            const float x[8] = {a0.x, a0.y, a1.x, a1.y, a2.x, a2.y, a3.x, a3.y};
+#pragma unroll
+            for (int j = 0; j < 8; j++) w[j] = fmaf(p.fb, x[j], p.fc * v[e + j]);
+        }
+        if (EPI == EPI16_UPDATE) {
+            const uint4 a = load_uint4(p.in0 + at + e), b = load_uint4(p.in1 + at + e);
+            const uint32_t up[4] = {a.x, a.y, a.z, a.w}, lo[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const float2 x = unpack_half(up[j]), y = unpack_half(lo[j]);
+                w[2 * j] = fmaf(p.fa, x.x + y.x, p.fb * v[e + 2 * j]);
+                w[2 * j + 1] = fmaf(p.fa, x.y + y.y, p.fb * v[e + 2 * j + 1]);
+            }
+            if (p.o) {
+                __nv_bfloat16 *o = p.o + ((int64_t)t.batch * p.m + row) * p.ld_o + col + e;
+                if (p.o_vec && col + e + 8 <= p.n) {
+                    *reinterpret_cast<uint4 *>(o) = make_uint4(pack_bf16(w[0] * p.o_scale, w[1] * p.o_scale), pack_bf16(w[2] * p.o_scale, w[3] * p.o_scale),
+                                                               pack_bf16(w[4] * p.o_scale, w[5] * p.o_scale), pack_bf16(w[6] * p.o_scale, w[7] * p.o_scale));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; j++)
+                        if (col + e + j < p.n) o[j] = __float2bfloat16_rn(w[j] * p.o_scale);
+                }
+                continue;
+            }
+        }
+        uint32_t h[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) h[j] = pack_half(w[2 * j], w[2 * j + 1]);
+        *reinterpret_cast<uint4 *>(p.out0 + at + e) = make_uint4(h[0], h[1], h[2], h[3]);
+        if (EPI == EPI16_UPDATE) {
+            uint32_t l[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const float2 x = unpack_half(h[j]);
+                l[j] = pack_half(w[2 * j] - x.x, w[2 * j + 1] - x.y);
+            }
+            *reinterpret_cast<uint4 *>(p.out1 + at + e) = make_uint4(l[0], l[1], l[2], l[3]);
+        } else if (t.mirror) {
+            const __half *s = reinterpret_cast<const __half *>(h);
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (col + e + j < p.n) p.out0[base + (int64_t)(col + e + j) * p.pitch + row] = s[j];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------- kernel
+
+template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
+__global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Gemm16Params p)
+{
+    using C = Cfg16<CTAS, BN>;
+    constexpr int kStages = C::kStages;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t *smem_a = smem, *smem_b = smem + kStages * C::kABytes;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + C::kOperands);
+    // bars[0..7] full, [8..15] empty, [16..17] accumulator full, [18..19] accumulator empty, [20..27] a group's last stage has landed here,
+    // [28..35] (leader of a pair) it is ready in the other CTA
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 36);
+    volatile uint32_t *abort_flag = tmem_slot + 1;
+    int32_t *shared_tiles = reinterpret_cast<int32_t *>(tmem_slot + 2);
+    int32_t *start = reinterpret_cast<int32_t *>(smem + C::kOperands + C::kTail), *first = start + kMaxGroups16 + 1;
+    static_assert(kStages <= 8 && 36 * 8 + 16 <= C::kTail, "barriers");
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t bar_full = smem_u32(bars), bar_empty = smem_u32(bars + 8), bar_acc_full = smem_u32(bars + 16), bar_acc_empty = smem_u32(bars + 18),
+                   bar_cut = smem_u32(bars + 20), bar_peer = smem_u32(bars + 28);
+    const int rank = CTAS == 2 ? (int)cluster_ctarank() : 0;
+
+    if (warp == 4) {
+        mbar_init(smem_u32(bars + lane), lane >= 18 && lane < 20 ? 8 * CTAS : 1);
+        if (lane < 4) mbar_init(smem_u32(bars + 32 + lane), 1);
+        if (lane == 0) *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    } else if (warp == 1) {
+        if (CTAS == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+        tcgen05_fence_before();
+    } else if (warp == 0 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmA) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmB) : "memory");
+    }
+    __syncthreads();
+    if (CTAS == 2) { cluster_arrive(); cluster_wait(); }
+    tcgen05_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    wait_for_predecessor();   // from here on global memory is read and written
+
+    const uint32_t limit_word = load_global(p.status + 2), withhold = blockIdx.x == 0 ? load_global(p.status + 3) : 0u;
+    const uint64_t limit = limit_word != 0u ? limit_word : kWaitLimit;
+    int m_tiles = p.m_tiles;
+    if (TILES <= TILES_CUT) {
+        for (int g = threadIdx.x; g <= p.batch; g += kThreads16)
+            start[g] = !p.offsets ? (g == 0 ? 0 : (int32_t)p.total_rows) : (int32_t)max((int64_t)0, min(p.total_rows, load_global(p.offsets + g)));
+        __syncthreads();
+        if (warp == 4) {
+            const int per_lane = (p.batch + 32) / 32, g0 = min(lane * per_lane, p.batch + 1), g1 = min(g0 + per_lane, p.batch + 1);   // 32 runs of boundaries
+            int top = 0;
+            for (int g = g0; g < g1; g++) top = max(top, start[g]);
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int other = __shfl_up_sync(0xFFFFFFFFu, top, d);
+                if (lane >= d) top = max(top, other);
+            }
+            int before = __shfl_up_sync(0xFFFFFFFFu, top, 1);
+            if (lane == 0) before = 0;
+            for (int g = g0; g < g1; g++) start[g] = before = max(before, start[g]);   // boundaries that fall are lifted
+            __syncwarp();
+            if (TILES == TILES_ROWS) {   // row tiles of all groups before a group's
+                constexpr int kBM = kRows16 * CTAS;
+                const int last = min(g1, p.batch);
+                int sum = 0;
+                for (int g = g0; g < last; g++) sum += (group_rows(start, g) + kBM - 1) / kBM;
+                before = sum;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int other = __shfl_up_sync(0xFFFFFFFFu, before, d);
+                    if (lane >= d) before += other;
+                }
+                if (lane == 31) *shared_tiles = before;
+                before -= sum;
+                for (int g = g0; g < last; g++) {
+                    first[g] = before;
+                    before += (group_rows(start, g) + kBM - 1) / kBM;
+                }
+            }
+        }
+        __syncthreads();
+        if (TILES == TILES_ROWS) m_tiles = *shared_tiles;
+    }
+    const int tiles = TILES == TILES_ROWS ? m_tiles * p.n_tiles : TILES == TILES_SYM ? p.batch * (m_tiles * (m_tiles + 1) / 2) : p.batch * m_tiles * p.n_tiles;
+    const int tile0 = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer
+        uint32_t it = 0, loads = 0;
+        bool ok = true;
+        const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b);
+        for (int tile = tile0; ok && tile < tiles; tile += step) {
+            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
+            const int stages = (t.k_len + kK16 - 1) / kK16;
+            const int a_copies = A_MN ? 2 : (t.rows + p.a_box - 1) / p.a_box;
+            const int a_copies_peer = A_MN ? 2 : (t.rows_peer + p.a_box - 1) / p.a_box;
+            const uint32_t a_copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
+            for (int s = 0; s < stages; s++, it++) {
+                const uint32_t slot = it % kStages;
+                if (!warp_wait(bar_empty + 8 * slot, ((it / kStages) & 1u) ^ 1u, abort_flag, p.status, limit, 0x100u + slot)) { ok = false; break; }
+                const int k = t.k0 + s * kK16;
+                // A stage with rows behind its group's end lands on a barrier of its own in each CTA, where warp 2 waits for it.
+                const bool cut = TILES == TILES_CUT && t.k_len - s * kK16 < kK16;
+                if (elect_one()) {
+                    const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * slot;
+                    const bool lead_counts = CTAS == 2 && !cut;
+                    if (rank == 0 || cut)
+                        mbar_arrive_expect_tx(own_bar, (uint32_t)a_copies * a_copy_bytes + (uint32_t)C::kBBytes +
+                                                           (lead_counts ? (uint32_t)a_copies_peer * a_copy_bytes + (uint32_t)C::kBBytes : 0u));
+                    if (withhold == 0u || ++loads != withhold) {
+                        const uint32_t bar = lead_counts ? cluster_addr(own_bar, 0) : own_bar;
+                        const uint32_t a = a0 + slot * C::kABytes, b = b0 + slot * C::kBBytes;
+                        auto load = [&](uint32_t dst, const CUtensorMap *map, int x, int y, int z) {
+                            if (CTAS == 2 && lead_counts) tma_load_3d_pair(dst, map, x, y, z, bar);
+                            else tma_load_3d(dst, map, x, y, z, bar);
+                        };
+                        // TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack
+                        const int az = TILES <= TILES_CUT ? 0 : t.batch, bz = TILES == TILES_CUT ? 0 : t.batch;
+                        if (A_MN) {
+#pragma unroll
+                            for (int j = 0; j < 2; j++) load(a + j * 8192, &tmA, t.a_row + 64 * j, k, az);
+                        } else {
+                            for (int j = 0; j < a_copies; j++) load(a + j * a_copy_bytes, &tmA, k, t.a_row + j * p.a_box, az);
+                        }
+                        if (B_MN) {
+#pragma unroll
+                            for (int j = 0; j < C::kBRows / 64; j++) load(b + j * 8192, &tmB, t.b_row + 64 * j, k, bz);
+                        } else {
+                            load(b, &tmB, k, t.b_row, bz);
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        // The MMAs' last reports reach this CTA's barriers while it is still there.
+        for (uint32_t s = it < kStages ? 0u : it - kStages; ok && s < it; s++)
+            ok = warp_wait(bar_empty + 8 * (s % kStages), (s / kStages) & 1u, abort_flag, p.status, limit, 0x700u + s % kStages);
+    } else if (warp == 1 && rank == 0) {
+        // ------------------------------------------------------------------ MMA issuer
+        const uint32_t idesc = instr_desc16<CTAS, BN>(p.bf16 != 0, A_MN, B_MN);
+        uint32_t it = 0, n_acc = 0;
+        bool ok = true;
+        for (int tile = tile0; ok && tile < tiles; tile += step) {
+            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
+            const int stages = (t.k_len + kK16 - 1) / kK16;
+            uint32_t acc = 0;
+            for (int s = 0; s < stages; s++, it++) {
+                const bool opens = EPI == EPI16_SUM ? s % kSumStages == 0 : s == 0;
+                const bool closes = s == stages - 1 || (EPI == EPI16_SUM && s % kSumStages == kSumStages - 1);
+                if (opens) {
+                    acc = n_acc & 1u;
+                    if (!warp_wait(bar_acc_empty + 8 * acc, ((n_acc >> 1) & 1u) ^ 1u, abort_flag, p.status, limit, 0x200u)) { ok = false; break; }
+                    n_acc++;
+                    if (CTAS == 2) fence_cluster_acquire();
+                }
+                const uint32_t slot = it % kStages;
+                if (!warp_wait(bar_full + 8 * slot, (it / kStages) & 1u, abort_flag, p.status, limit, 0x300u + slot)) { ok = false; break; }
+                const int left = t.k_len - s * kK16;
+                if (TILES == TILES_CUT && CTAS == 2 && left < kK16) fence_cluster_acquire();
+                tcgen05_fence_after();
+                if (elect_one()) {
+                    const uint32_t a = smem_u32(smem_a) + slot * C::kABytes, b = smem_u32(smem_b) + slot * C::kBBytes;
+                    const uint64_t ad = A_MN ? smem_desc_mn_sw128(a) : smem_desc_sw128(a), bd = B_MN ? smem_desc_mn_sw128(b) : smem_desc_sw128(b);
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        if (16 * j < left)
+                            tcgen05_mma_f16<CTAS>(tmem + acc * BN, ad + (uint64_t)(j * (A_MN ? 2048 : 32) >> 4), bd + (uint64_t)(j * (B_MN ? 2048 : 32) >> 4), idesc, !opens || j > 0);
+                    tcgen05_commit<CTAS>(bar_empty + 8 * slot);
+                    if (closes) tcgen05_commit<CTAS>(bar_acc_full + 8 * acc);
+                }
+                __syncwarp();
+            }
+        }
+    } else if (warp == 2 && TILES == TILES_CUT) {
+        // ------------------------------------------------------------------ rows behind a group's end
+        // The last stage of a group holds rows of the next one, or whatever lies behind them.  Up to 15 of them meet an MMA: they are zeroed in
+        // both operands (in one, an infinity in the other would make NaN).  Then, and in a pair when the other CTA has done the same, the
+        // stage is full.  A slot is filled again only when the MMAs have read it, so its barriers are never a phase ahead.
+        uint32_t it = 0, phases = 0;
+        for (int tile = tile0; tile < tiles; tile += step) {
+            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
+            const int stages = (t.k_len + kK16 - 1) / kK16, left = t.k_len - (stages - 1) * kK16;
+            it += stages;
+            if (stages == 0 || left == kK16) continue;
+            const uint32_t slot = (it - 1) % kStages, parity = (phases >> slot) & 1u;
+            phases ^= 1u << slot;
+            if (!warp_wait(bar_cut + 8 * slot, parity, abort_flag, p.status, limit, 0x500u + slot)) break;
+            const int pieces = (((left + 15) & ~15) - left) * 8;
+            for (int c = 0; c < 2 + C::kBRows / 64; c++) {
+                uint8_t *chunk = c < 2 ? smem_a + slot * C::kABytes + c * 8192 : smem_b + slot * C::kBBytes + (c - 2) * 8192;
+                for (int i = lane; i < pieces; i += 32) *reinterpret_cast<uint4 *>(chunk + left * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (CTAS == 2 && rank == 0) {
+                if (!warp_wait(bar_peer + 8 * slot, parity, abort_flag, p.status, limit, 0x400u + slot)) break;
+                fence_cluster_acquire();
+            }
+            if (lane == 0) {
+                if (rank == 0) mbar_arrive(bar_full + 8 * slot);
+                else mbar_arrive_release_cluster(cluster_addr(bar_peer + 8 * slot, 0));
+            }
+            __syncwarp();
+        }
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ epilogue
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        uint32_t n_acc = 0;
+        for (int tile = tile0; tile < tiles; tile += step) {
+            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
+            const int in = 32 * quarter + lane;
+            const int chunks = EPI == EPI16_SUM ? (t.k_len + kSumStages * kK16 - 1) / (kSumStages * kK16) : t.k_len > 0;   // accumulators of the tile
+            const uint64_t acc_limit = limit * (uint64_t)(1 + (t.k_len >> 10));
+            const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
+            const int64_t row = (TILES == TILES_CUT ? (int64_t)t.batch * p.m : 0) + t.row + in;
+            // The accumulator may be overwritten as soon as all warps have it in registers.
+            auto release = [&](uint32_t acc) {
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    const uint32_t bar = bar_acc_empty + 8 * acc;
+                    if (CTAS == 2) mbar_arrive_release_cluster(cluster_addr(bar, 0));
+                    else mbar_arrive(bar);
+                }
+                __syncwarp();
+            };
+            if (EPI == EPI16_SUM) {
+                float sum[BN / 2];
+#pragma unroll
+                for (int e = 0; e < BN / 2; e++) sum[e] = 0.f;
+                bool ok = true;
+                for (int k = 0; k < chunks; k++, n_acc++) {
+                    const uint32_t acc = n_acc & 1u;
+                    if (!warp_wait(bar_acc_full + 8 * acc, (n_acc >> 1) & 1u, abort_flag, p.status, acc_limit, 0x600u)) { ok = false; break; }
+                    tcgen05_fence_after();
+#pragma unroll
+                    for (int c = 0; c < BN / 32; c++) {
+                        uint32_t v[16];
+                        FP4Q_TMEM_LD_X16(tmem + acc * BN + half * (BN / 2) + 16 * c + lanes, v);
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                        for (int e = 0; e < 16; e++) sum[16 * c + e] += __uint_as_float(v[e]);
+                    }
+                    release(acc);
+                }
+                if (!ok) break;
+                if (in < t.rows && (chunks > 0 || !p.accumulate)) {
+#pragma unroll
+                    for (int c = 0; c < BN / 64; c++) store_f32(p, row, t.col + half * (BN / 2) + 32 * c, sum + 32 * c);
+                }
+                __syncwarp();
+                continue;
+            }
+            const uint32_t acc = n_acc & 1u;
+            if (chunks > 0) {
+                if (!warp_wait(bar_acc_full + 8 * acc, (n_acc >> 1) & 1u, abort_flag, p.status, acc_limit, 0x600u)) break;
+                n_acc++;
+                tcgen05_fence_after();
+            }
+#pragma unroll 1
+            for (int c = 0; c < BN / 64; c++) {
+                const int col = half * (BN / 2) + 32 * c;
+                uint32_t v[32];
+                if (chunks > 0) {
+                    FP4Q_TMEM_LD_X32(tmem + acc * BN + col + lanes, v);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    if (c == BN / 64 - 1) release(acc);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; e++) v[e] = 0u;
+                }
+                if (in < t.rows) {
+                    if (EPI == EPI16_STORE) store_bf16(p, row, t.col + col, reinterpret_cast<const float *>(v));
+                    else step16<EPI>(p, t, (int64_t)t.batch * p.m * p.pitch, t.row + in, t.col + col, reinterpret_cast<const float *>(v));
+                }
+                __syncwarp();
+            }
+        }
+    }
+
+    if (TILES == TILES_ROWS && p.zero_rest && warp >= 4) {
+        constexpr int kElem = EPI == EPI16_SUM ? 4 : 2;
+        const int64_t head = start[0], rest = head + p.total_rows - start[p.batch];
+        const int pieces = p.n * kElem / 16;
+        for (int64_t i = blockIdx.x * 8 + warp - 4; i < rest; i += gridDim.x * 8) {
+            uint8_t *row = static_cast<uint8_t *>(p.c) + (i < head ? i : start[p.batch] + i - head) * p.ldc * kElem;
+            for (int e = lane; e < pieces; e += 32) reinterpret_cast<uint4 *>(row)[e] = make_uint4(0u, 0u, 0u, 0u);
+            for (int e = pieces * 8 + lane; e < p.n * kElem / 2; e += 32) reinterpret_cast<uint16_t *>(row)[e] = 0;
+        }
+    }
+
+    // Shared memory and tensor memory stay until all roles, of both CTAs of a pair, have done with them.  Where a wait has run out, copies and
+    // MMAs may still be under way: they take microseconds, a millisecond is left to them.
+    __syncwarp();
+    if (*abort_flag != 0u)
+        for (int i = 0; i < 64; i++) __nanosleep(16000);
+    tcgen05_fence_before();
+    __syncthreads();
+    if (CTAS == 2) { cluster_arrive(); cluster_wait(); }
+    if (warp == 1) {
+        tcgen05_fence_after();
+        if (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------------------------------- host side
+
+// What a launch reads of an operand: a stack of `batch` matrices [rows, cols] of 16-bit elements, `pitch` elements from row to row and `stride`
+// from matrix to matrix.
+struct Operand16 {
+    const void *base;
+    int64_t cols, rows, batch, pitch, stride;
+};
+inline bool make_map16(CUtensorMap *map, const Operand16 &o, int box_rows)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.batch};
+    const cuuint64_t strides[2] = {(cuuint64_t)o.pitch * 2, (cuuint64_t)o.stride * 2};
+    const cuuint32_t box[3] = {(cuuint32_t)kK16, (cuuint32_t)box_rows, 1u};
+    return encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void *>(o.base), dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+}
+
+// most_tiles: no fewer than the tiles there can be.
+template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
+fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Gemm16Params &p, int64_t most_tiles, cudaStream_t stream)
+{
+    using C = Cfg16<CTAS, BN>;
+    CUtensorMap tmA, tmB;
+    if (!make_map16(&tmA, a, A_MN ? kK16 : p.a_box)) return FP4Q_ERR_CUDA;
+    if (!make_map16(&tmB, b, B_MN ? kK16 : C::kBRows)) return FP4Q_ERR_CUDA;
+    const int dev = current_device();
+    if (dev < 0) return FP4Q_ERR_CUDA;
+    constexpr int kSmem = C::smem(TILES);
+    static std::atomic<bool> attr_set[kMaxDevices];   // the attribute is a property of (kernel, device)
+    if (!attr_set[dev].load(std::memory_order_relaxed)) {
+        if (cudaFuncSetAttribute(gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
+            cudaGetLastError();
+            return FP4Q_ERR_CUDA;
+        }
+        attr_set[dev].store(true, std::memory_order_relaxed);
+    }
+    const int64_t slots = sm_count(dev) / CTAS;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    cfg.gridDim = dim3((unsigned)(CTAS * (most_tiles < slots ? most_tiles : slots)));
+    cfg.blockDim = dim3(kThreads16);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
+    if (CTAS == 2) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = CTAS;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    return launched(cudaLaunchKernelEx(&cfg, gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES>, tmA, tmB, p));
+}
+
+}  // namespace fp4q

@@ -41,6 +41,11 @@ struct Entry {
     decltype(&fp4q_mxfp8_qk) mxfp8_qk;
     decltype(&fp4q_mxfp8_gemm) mxfp8_gemm;
     decltype(&fp4q_workspace_bytes) workspace_bytes;
+    decltype(&fp4q_ragged_gemm_fwd) ragged_gemm_fwd;
+    decltype(&fp4q_ragged_gemm_dgrad) ragged_gemm_dgrad;
+    decltype(&fp4q_ragged_gemm_wgrad) ragged_gemm_wgrad;
+    decltype(&fp4q_newton_schulz) newton_schulz;
+    decltype(&fp4q_newton_schulz_scratch_bytes) newton_schulz_scratch_bytes;
 } lib;
 
 PyObject *g_qtensor = nullptr, *g_fail = nullptr;   // binding.QTensor; binding._check
@@ -518,6 +523,123 @@ PyObject *mxfp8_qk(Args a, Py_ssize_t n)
     return PyTuple_Pack(2, q.p, k.p);
 }
 
+// A tensor that a kernel reads or writes beside `like`: on its device.
+void same_device(const at::Tensor &t, const at::Tensor &like, const char *name)
+{
+    if (t.device() == like.device()) return;
+    PyErr_Format(PyExc_ValueError, "%s must live on the same CUDA device as the other tensors", name);
+    throw PyError();
+}
+
+// which (0 fwd, 1 dgrad, 2 wgrad), a (x or dY), b (w or x), row_offsets | None, out | None, dt, accumulate, ws | None, stream
+PyObject *ragged_gemm(Args a, Py_ssize_t n)
+{
+    want(n, 9);
+    static const char *const names[3] = {"fp4q_ragged_gemm_fwd", "fp4q_ragged_gemm_dgrad", "fp4q_ragged_gemm_wgrad"};
+    static const char *const operands[3][2] = {{"x", "w"}, {"dY", "w"}, {"dY", "x"}};
+    const int which = as_int(a[0]), dt = as_int(a[5]), accumulate = as_bool(a[6]) ? 1 : 0;
+    const at::Tensor &x = as_matrix(a[1], operands[which][0], "operands must be 2-D BF16 tensors with contiguous rows");
+    const at::Tensor &y = as_matrix(a[2], operands[which][1], "operands must be 2-D BF16 tensors with contiguous rows");
+    same_device(y, x, operands[which][1]);
+    const Groups g(a[3], 1);
+    if (g.ptr) same_device(as_tensor(a[3]), x, "row_offsets");
+    if (g.ptr && g.g.n_groups < 1) value_error("row_offsets must hold at least two offsets");
+    const int64_t groups = g.ptr ? g.g.n_groups : 1;
+    if (which == 2 && x.size(0) != y.size(0)) value_error("dY and x must have the same number of rows");
+    if (which < 2 && y.size(0) % groups) value_error("w must hold the same number of rows for every group");
+    if (which < 2 && x.size(1) != (which ? y.size(0) / groups : y.size(1))) value_error("the operands' contraction lengths differ");
+    if (dt != FP4Q_OUT_BF16 && dt != FP4Q_OUT_F32) value_error("dt must be OUT_BF16 or OUT_F32");
+    const int64_t rows = which == 2 ? x.size(1) * groups : x.size(0), cols = which == 0 ? y.size(0) / groups : y.size(1);
+    const c10::cuda::CUDAGuard device(x.device());
+    const OnStream on(a[8], &x);
+    const bool ours = a[4] == Py_None;
+    const at::Tensor out = ours ? out_buffer(on, rows, cols, dt, x) : as_tensor(a[4]);
+    if (ours && accumulate) { Unlock u; out.zero_(); }
+    if (!ours) {
+        same_device(out, x, "out");
+        if (out.scalar_type() != (dt == FP4Q_OUT_BF16 ? at::kBFloat16 : at::kFloat) || out.dim() != 2 || out.size(0) != rows || out.size(1) != cols ||
+            (out.numel() && out.stride(1) != 1 && cols > 1))
+            value_error("out must be a 2-D tensor of the result's shape and of the type that dt names, with contiguous rows");
+    }
+    const at::Tensor ws = workspace(a[7], x);
+    const int64_t ld = out_pitch(out, cols);
+    const fp4q_out type = (fp4q_out)(ours && which < 2 ? dt | FP4Q_OUT_ZERO_REST : dt);   // fresh memory holds anything
+    const fp4q_status s =
+        which == 2   ? unlocked(lib.ragged_gemm_wgrad, x.data_ptr(), x.size(0), x.size(1), pitch(x), y.data_ptr(), y.size(1), pitch(y), out.data_ptr(), ld, type, accumulate,
+                                g.ptr, ws.data_ptr(), (size_t)ws.numel(), on.handle)
+        : which == 1 ? unlocked(lib.ragged_gemm_dgrad, x.data_ptr(), x.size(0), x.size(1), pitch(x), y.data_ptr(), y.size(0), y.size(1), pitch(y), out.data_ptr(), ld, type, g.ptr,
+                                ws.data_ptr(), (size_t)ws.numel(), on.handle)
+                     : unlocked(lib.ragged_gemm_fwd, x.data_ptr(), x.size(0), x.size(1), pitch(x), y.data_ptr(), y.size(0), pitch(y), out.data_ptr(), ld, type, g.ptr, ws.data_ptr(),
+                                (size_t)ws.numel(), on.handle);
+    check(s, names[which]);
+    return ours ? THPVariable_Wrap(out) : Py_NewRef(a[4]);
+}
+
+// A stack of matrices, or one: 3-D or 2-D, contiguous rows, matrices one behind the other in the rows' pitch.
+const at::Tensor &as_stack(const at::Tensor &t, const char *name)
+{
+    if (!t.is_cuda()) { PyErr_Format(PyExc_ValueError, "%s must live on a CUDA device (there is no CPU path)", name); throw PyError(); }
+    const bool dims = t.dim() == 2 || t.dim() == 3;
+    if (!dims || (t.numel() && ((t.size(-1) > 1 && t.stride(-1) != 1) || (t.dim() == 3 && t.size(0) > 1 && t.stride(0) != t.size(1) * t.stride(1))))) {
+        PyErr_Format(PyExc_ValueError, "%s must be a matrix or a stack of matrices [count, rows, cols] with contiguous rows, one matrix behind the other", name);
+        throw PyError();
+    }
+    return t;
+}
+int64_t stack_pitch(const at::Tensor &t) { return t.numel() && t.size(-2) * (t.dim() == 3 ? t.size(0) : 1) > 1 ? t.stride(-2) : t.size(-1); }
+
+// g, momentum | None, beta, nesterov, coefficients (a flat sequence of floats), eps, scale, out | None, scratch | None, ws | None, stream
+PyObject *newton_schulz(Args a, Py_ssize_t n)
+{
+    want(n, 11);
+    const at::Tensor &g = as_stack(as_tensor(a[0]), "g");
+    if (g.scalar_type() != at::kBFloat16 && g.scalar_type() != at::kFloat) value_error("g must be BF16 or FP32");
+    const bool ours = a[7] == Py_None;
+    at::Tensor m;
+    if (a[1] != Py_None) {
+        m = as_stack(as_tensor(a[1]), "momentum");
+        if (m.scalar_type() != at::kFloat || m.sizes() != g.sizes()) value_error("momentum must be FP32 and of g's shape");
+        same_device(m, g, "momentum");
+    }
+    const double beta = PyFloat_AsDouble(a[2]), eps = PyFloat_AsDouble(a[5]), scale = PyFloat_AsDouble(a[6]);
+    if (PyErr_Occurred()) throw PyError();
+    const int nesterov = as_bool(a[3]) ? 1 : 0;
+    Ref list(PySequence_Tuple(a[4]));
+    std::vector<float> c;
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(list.p); i++) {
+        c.push_back((float)PyFloat_AsDouble(PyTuple_GET_ITEM(list.p, i)));
+        if (PyErr_Occurred()) throw PyError();
+    }
+    if (c.empty() || c.size() % 3) value_error("coefficients must be triples, one for every step");
+    const int64_t count = g.dim() == 3 ? g.size(0) : 1, rows = g.size(-2), cols = g.size(-1);
+    const c10::cuda::CUDAGuard device(g.device());
+    const OnStream on(a[10], &g);
+    at::Tensor out, scratch;
+    {
+        Unlock u;
+        if (ours) out = on.returned(at::empty(g.sizes(), at::TensorOptions().dtype(at::kBFloat16).device(g.device())));
+        if (a[8] == Py_None)
+            scratch = at::empty({(int64_t)lib.newton_schulz_scratch_bytes(count, rows, cols)}, at::TensorOptions().dtype(at::kByte).device(g.device()));
+    }
+    if (!ours) {
+        out = as_stack(as_tensor(a[7]), "out");
+        if (out.scalar_type() != at::kBFloat16 || out.sizes() != g.sizes()) value_error("out must be BF16 and of g's shape");
+        same_device(out, g, "out");
+    }
+    if (a[8] != Py_None) {
+        scratch = as_tensor(a[8]);
+        same_device(scratch, g, "scratch");
+        if (!scratch.is_contiguous()) value_error("scratch must be contiguous");
+    }
+    const at::Tensor ws = workspace(a[9], g);
+    const float *coefficients = c.data();
+    check(unlocked(lib.newton_schulz, g.data_ptr(), g.scalar_type() == at::kFloat ? FP4Q_OUT_F32 : FP4Q_OUT_BF16, count, rows, cols, stack_pitch(g),
+                   m.defined() ? static_cast<float *>(m.data_ptr()) : nullptr, m.defined() ? stack_pitch(m) : 0, (float)beta, nesterov, coefficients, (int32_t)(c.size() / 3),
+                   (float)eps, (float)scale, out.data_ptr(), stack_pitch(out), scratch.data_ptr(), (size_t)scratch.nbytes(), ws.data_ptr(), (size_t)ws.numel(), on.handle),
+          "fp4q_newton_schulz");
+    return ours ? THPVariable_Wrap(out) : Py_NewRef(a[7]);
+}
+
 // ---- the straight-through layer of autograd.py as one native autograd node
 //
 // The layer's kernels run 20 to 90 us forward and backward at the sizes where layers are small; through a Python autograd
@@ -690,6 +812,11 @@ PyObject *init(Args a, Py_ssize_t n)
     set_entry(a[0], "fp4q_mxfp8_qk", lib.mxfp8_qk);
     set_entry(a[0], "fp4q_mxfp8_gemm", lib.mxfp8_gemm);
     set_entry(a[0], "fp4q_workspace_bytes", lib.workspace_bytes);
+    set_entry(a[0], "fp4q_ragged_gemm_fwd", lib.ragged_gemm_fwd);
+    set_entry(a[0], "fp4q_ragged_gemm_dgrad", lib.ragged_gemm_dgrad);
+    set_entry(a[0], "fp4q_ragged_gemm_wgrad", lib.ragged_gemm_wgrad);
+    set_entry(a[0], "fp4q_newton_schulz", lib.newton_schulz);
+    set_entry(a[0], "fp4q_newton_schulz_scratch_bytes", lib.newton_schulz_scratch_bytes);
     Py_XSETREF(g_qtensor, Py_NewRef(a[1]));
     Py_XSETREF(g_fail, Py_NewRef(a[2]));
     return Py_NewRef(Py_None);
@@ -724,6 +851,8 @@ PyMethodDef methods[] = {METHOD("init", init),
                          METHOD("mxfp8_gemm", mxfp8_gemm),
                          METHOD("mxfp8_qk", mxfp8_qk),
                          METHOD("linear", linear),
+                         METHOD("ragged_gemm", ragged_gemm),
+                         METHOD("newton_schulz", newton_schulz),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", "argument marshalling of binding.py", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

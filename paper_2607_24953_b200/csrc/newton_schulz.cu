@@ -1,0 +1,329 @@
+// Orthogonalised updates: momentum, normalisation and Newton-Schulz steps for a stack of weight gradients (include/fp4q.h).
+//
+//   X <- U / (|U| + eps);  per step, with A = X X^T on the shorter side:  X <- a X + (b A + c A A) X
+//
+// A step is three products: A = X X^T and P = b A + c A A are symmetric, so only the tiles on and below the diagonal are computed and
+// written to both places; X' = a X + P X reads X once more in its epilogue.  A matrix that is taller than wide keeps its layout: A = X^T X
+// and X' = a X + X P, with operands read across their rows.
+//
+// Precision.  The products' operands are FP16: values of X, A and P lie in a narrow range (singular values of at most about 1.3), so the
+// three bits that FP16 has more than BF16 cost nothing.  X itself is kept as a sum of two FP16 numbers (22 bits): what is rounded is only
+// the operand of the products.  The term a X carries directions of small singular values from step to step, multiplied by a = 3.4 each time,
+// and rounding X as a whole puts noise into those that a gradient does not have (rank 100, 768 x 2048: the update is off by 1.8e-2 with one
+// FP16 number and 1.4e-1 with a BF16 one, 7e-4 with the sum of two).  Scales: X 2^10, A and P 2^9, so that elements of large matrices
+// stay above FP16's smallest normal number and the largest singular values that the entry point admits below its largest.
+#include "gemm16.cuh"
+
+#include <cmath>
+
+using namespace fp4q;
+
+namespace {
+
+constexpr int kNsThreads = 256, kNsUnroll = 4, kNsMaxBlocks = 1024;
+constexpr float kScaleX = 1024.0f, kScaleA = 512.0f;
+constexpr int kMaxSteps = 64;
+
+struct MomentumParams {
+    const void *g;
+    float *m;                    // NULL: none
+    int64_t ld_g, ld_m;
+    int64_t rows;
+    int32_t cols, g_f32, vec_g, vec_m;
+    uint32_t units_row, units;   // units of four columns in a row and in a matrix
+    float beta;
+    int32_t nesterov;
+    double eps;
+    double *partial;             // [count, gridDim.x]
+    __half *up, *lo;             // normalised: upper and lower parts
+    int64_t pitch;
+};
+
+__device__ __forceinline__ float4 load_gradient(const MomentumParams &p, int64_t row, int col)
+{
+    const int64_t at = row * p.ld_g + col;
+    const int left = p.cols - col;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (p.g_f32) {
+        const float *g = static_cast<const float *>(p.g) + at;
+        if (p.vec_g && left >= 4) return *reinterpret_cast<const float4 *>(g);
+        v.x = g[0];
+        if (left > 1) v.y = g[1];
+        if (left > 2) v.z = g[2];
+        if (left > 3) v.w = g[3];
+    } else {
+        const __nv_bfloat16 *g = static_cast<const __nv_bfloat16 *>(p.g) + at;
+        if (p.vec_g && left >= 4) {
+            const uint2 w = *reinterpret_cast<const uint2 *>(g);
+            return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
+        }
+        v.x = __bfloat162float(g[0]);
+        if (left > 1) v.y = __bfloat162float(g[1]);
+        if (left > 2) v.z = __bfloat162float(g[2]);
+        if (left > 3) v.w = __bfloat162float(g[3]);
+    }
+    return v;
+}
+__device__ __forceinline__ float4 load_momentum(const MomentumParams &p, int64_t row, int col)
+{
+    const float *m = p.m + row * p.ld_m + col;
+    const int left = p.cols - col;
+    if (p.vec_m && left >= 4) return *reinterpret_cast<const float4 *>(m);
+    return make_float4(m[0], left > 1 ? m[1] : 0.f, left > 2 ? m[2] : 0.f, left > 3 ? m[3] : 0.f);
+}
+__device__ __forceinline__ void store_momentum(const MomentumParams &p, int64_t row, int col, float4 v)
+{
+    float *m = p.m + row * p.ld_m + col;
+    const int left = p.cols - col;
+    if (p.vec_m && left >= 4) { *reinterpret_cast<float4 *>(m) = v; return; }
+    m[0] = v.x;
+    if (left > 1) m[1] = v.y;
+    if (left > 2) m[2] = v.z;
+    if (left > 3) m[3] = v.w;
+}
+__device__ __forceinline__ float4 axpy(float a, float4 x, float4 y)
+{
+    return make_float4(fmaf(a, x.x, y.x), fmaf(a, x.y, y.y), fmaf(a, x.z, y.z), fmaf(a, x.w, y.w));
+}
+
+// The block's sum, in an order that depends on nothing but the block's size; every thread gets it.
+__device__ __forceinline__ double block_sum(double v)
+{
+    __shared__ double part[kNsThreads / 32];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double s = 0.0;
+#pragma unroll
+    for (int w = 0; w < kNsThreads / 32; w++) s += part[w];
+    return s;
+}
+
+// FINISH = false: the momentum, and each block's share of |U|^2.  FINISH = true: the norm, and X = U / (|U| + eps) in two halves.
+// The sum of squares is held in 64 bits: gradients of 1e-25 and 1e25 have squares that FP32 does not.
+template <bool FINISH>
+__global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumParams p)
+{
+    wait_for_predecessor();
+    const int64_t row0 = (int64_t)blockIdx.y * p.rows;
+    double sum = 0.0, inv = 0.0;
+    if (FINISH) {
+        for (int i = threadIdx.x; i < (int)gridDim.x; i += kNsThreads) sum += load_global(p.partial + (int64_t)blockIdx.y * gridDim.x + i);
+        inv = (double)kScaleX / (sqrt(block_sum(sum)) + p.eps);
+    }
+    const uint32_t step = gridDim.x * kNsThreads;
+    for (uint32_t base = blockIdx.x * kNsThreads + threadIdx.x; base < p.units; base += kNsUnroll * step) {
+        float4 g[kNsUnroll], m[kNsUnroll];
+        int64_t row[kNsUnroll];
+        int col[kNsUnroll];
+#pragma unroll
+        for (int j = 0; j < kNsUnroll; j++) {
+            const uint32_t u = base + j * step;
+            const uint32_t r = u / p.units_row;
+            row[j] = u < p.units ? row0 + r : -1;
+            col[j] = (int)(u - r * p.units_row) * 4;
+            g[j] = m[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (row[j] >= 0) {
+                if (!FINISH || !p.m || p.nesterov) g[j] = load_gradient(p, row[j], col[j]);
+                if (p.m) m[j] = load_momentum(p, row[j], col[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kNsUnroll; j++) {
+            if (row[j] < 0) continue;
+            float4 u = g[j];
+            if (p.m) {
+                if (!FINISH) {
+                    m[j] = axpy(p.beta, m[j], g[j]);
+                    store_momentum(p, row[j], col[j], m[j]);
+                }
+                u = p.nesterov ? axpy(p.beta, m[j], g[j]) : m[j];
+            }
+            if (!FINISH) {
+                sum += (double)u.x * u.x + (double)u.y * u.y;
+                sum += (double)u.z * u.z + (double)u.w * u.w;
+            } else {
+                const float x[4] = {(float)(u.x * inv), (float)(u.y * inv), (float)(u.z * inv), (float)(u.w * inv)};
+                uint32_t up[2], lo[2];
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    up[e] = pack_half(x[2 * e], x[2 * e + 1]);
+                    const float2 h = unpack_half(up[e]);
+                    lo[e] = pack_half(x[2 * e] - h.x, x[2 * e + 1] - h.y);
+                }
+                const int64_t at = row[j] * p.pitch + col[j];
+                *reinterpret_cast<uint2 *>(p.up + at) = make_uint2(up[0], up[1]);
+                *reinterpret_cast<uint2 *>(p.lo + at) = make_uint2(lo[0], lo[1]);
+            }
+        }
+    }
+    if (!FINISH) {
+        sum = block_sum(sum);
+        if (threadIdx.x == 0) p.partial[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
+    }
+}
+
+// Where things lie in the scratch memory.
+struct Scratch {
+    int64_t pitch_x, pitch_a, side;
+    size_t partial, x0, x1, lo, a, poly, bytes;
+    Scratch(int64_t count, int64_t rows, int64_t cols)
+    {
+        side = rows < cols ? rows : cols;
+        pitch_x = round_up(cols, 16);
+        pitch_a = round_up(side, 16);
+        const size_t x = (size_t)round_up(count * rows * pitch_x * 2, 256), s = (size_t)round_up(count * side * pitch_a * 2, 256);
+        partial = 0;
+        x0 = (size_t)round_up(count * kNsMaxBlocks * 8, 256);
+        x1 = x0 + x;
+        lo = x1 + x;
+        a = lo + x;
+        poly = a + s;
+        bytes = poly + s;
+    }
+};
+
+const int64_t kMaxSide = 1 << 20, kMaxCount = 65535;
+
+bool sizes_ok(int64_t count, int64_t rows, int64_t cols)
+{
+    return count <= kMaxCount && rows <= kMaxSide && cols <= kMaxSide && rows * ceil_div(cols, 4) < (1ll << 31) && count * rows <= 0x7FFFFFFF &&
+           count * rows * round_up(cols, 16) <= (1ll << 40) && count * ceil_div(rows, 128) * ceil_div(cols, 64) <= 0x7FFFFFFF - 4096;
+}
+
+// The largest singular value that X can have after each step, from at most 1, and the largest eigenvalue of b A + c A A: the polynomials
+// are sampled.  Whether FP16 holds all that they reach.
+bool steps_fit(const float *c, int32_t steps)
+{
+    double top = 1.0;
+    for (int32_t s = 0; s < steps; s++) {
+        double next = 0.0;
+        for (int i = 0; i <= 512; i++) {
+            const double x = top * i / 512, q = x * x, poly = c[3 * s + 1] * q + c[3 * s + 2] * q * q, y = std::fabs(x * (c[3 * s] + poly));
+            if (!(std::fabs(poly) <= 100.0) || !(y <= 10.0)) return false;
+            if (y > next) next = y;
+        }
+        top = next * 1.01;   // roundings
+        if (top < 1e-3) top = 1e-3;
+    }
+    return true;
+}
+
+template <int CTAS, int BN>
+struct Steps {
+    static constexpr int kBM = kRows16 * CTAS;
+    static fp4q_status gram(const Operand16 &x, bool tall, Gemm16Params p, cudaStream_t stream)
+    {
+        static_assert(kBM == BN, "symmetric products have square tiles");
+        p.m_tiles = p.n_tiles = (int32_t)ceil_div(p.n, BN);
+        const int64_t tiles = (int64_t)p.batch * p.m_tiles * (p.m_tiles + 1) / 2;
+        return tall ? launch_gemm16<CTAS, BN, true, true, EPI16_GRAM, TILES_SYM>(x, x, p, tiles, stream)
+                    : launch_gemm16<CTAS, BN, false, false, EPI16_GRAM, TILES_SYM>(x, x, p, tiles, stream);
+    }
+    static fp4q_status poly(const Operand16 &a, Gemm16Params p, cudaStream_t stream)
+    {
+        p.m_tiles = p.n_tiles = (int32_t)ceil_div(p.n, BN);
+        return launch_gemm16<CTAS, BN, false, false, EPI16_POLY, TILES_SYM>(a, a, p, (int64_t)p.batch * p.m_tiles * (p.m_tiles + 1) / 2, stream);
+    }
+    static fp4q_status update(const Operand16 &x, const Operand16 &poly, bool tall, Gemm16Params p, cudaStream_t stream)
+    {
+        p.m_tiles = (int32_t)ceil_div(p.m, kBM);
+        p.n_tiles = (int32_t)ceil_div(p.n, BN);
+        const int64_t tiles = (int64_t)p.batch * p.m_tiles * p.n_tiles;
+        return tall ? launch_gemm16<CTAS, BN, false, false, EPI16_UPDATE, TILES_BATCH>(x, poly, p, tiles, stream)
+                    : launch_gemm16<CTAS, BN, false, true, EPI16_UPDATE, TILES_BATCH>(poly, x, p, tiles, stream);
+    }
+};
+
+}  // namespace
+
+extern "C" size_t fp4q_newton_schulz_scratch_bytes(int64_t count, int64_t rows, int64_t cols)
+{
+    if (count <= 0 || rows <= 0 || cols <= 0 || !sizes_ok(count, rows, cols)) return 0;
+    return Scratch(count, rows, cols).bytes;
+}
+
+extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_t count, int64_t rows, int64_t cols, int64_t ld_g, float *momentum, int64_t ld_m,
+                                          float beta, int nesterov, const float *coefficients, int32_t steps, float eps, float scale, void *out_bf16,
+                                          int64_t ld_o, void *scratch, size_t scratch_bytes, void *ws, size_t ws_bytes, void *stream)
+{
+    if (count < 0 || rows < 0 || cols < 0 || ld_g < cols || ld_o < cols || (momentum && ld_m < cols)) return FP4Q_ERR_SHAPE;
+    if (g_type != FP4Q_OUT_BF16 && g_type != FP4Q_OUT_F32) return FP4Q_ERR_UNSUPPORTED;
+    if (!coefficients) return FP4Q_ERR_NULL;
+    if (steps < 1 || steps > kMaxSteps || !(eps >= 0.0f) || !steps_fit(coefficients, steps)) return FP4Q_ERR_UNSUPPORTED;
+    if (count == 0 || rows == 0 || cols == 0) return FP4Q_OK;
+    if (!sizes_ok(count, rows, cols)) return FP4Q_ERR_UNSUPPORTED;
+    if (!g || !out_bf16) return FP4Q_ERR_NULL;
+    const size_t g_bytes = g_type == FP4Q_OUT_F32 ? 4 : 2;
+    if (!aligned(g, g_bytes) || !aligned(momentum, 4) || !aligned(out_bf16, 2)) return FP4Q_ERR_ALIGN;
+    const Scratch at(count, rows, cols);
+    if (!ws || ws_bytes < sizeof(Workspace) || !scratch || scratch_bytes < at.bytes) return FP4Q_ERR_WORKSPACE;
+    if (!aligned(ws, 256) || !aligned(scratch, 256)) return FP4Q_ERR_ALIGN;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    uint8_t *base = static_cast<uint8_t *>(scratch);
+    __half *x[2] = {reinterpret_cast<__half *>(base + at.x0), reinterpret_cast<__half *>(base + at.x1)}, *lo = reinterpret_cast<__half *>(base + at.lo),
+           *a = reinterpret_cast<__half *>(base + at.a), *poly = reinterpret_cast<__half *>(base + at.poly);
+
+    MomentumParams q = {};
+    q.g = g; q.m = momentum; q.ld_g = ld_g; q.ld_m = ld_m; q.rows = rows; q.cols = (int32_t)cols;
+    q.g_f32 = g_type == FP4Q_OUT_F32;
+    q.vec_g = aligned(g, 4 * g_bytes) && ld_g % 4 == 0;
+    q.vec_m = momentum && aligned(momentum, 16) && ld_m % 4 == 0;
+    q.units_row = (uint32_t)ceil_div(cols, 4);
+    q.units = (uint32_t)(rows * q.units_row);
+    q.beta = beta; q.nesterov = nesterov != 0; q.eps = eps;
+    q.partial = reinterpret_cast<double *>(base + at.partial);
+    q.up = x[0]; q.lo = lo; q.pitch = at.pitch_x;
+    const int64_t want = ceil_div(q.units, kNsThreads * kNsUnroll), share = ceil_div(16 * 148, count);
+    const dim3 grid((unsigned)(want < share ? want : share < kNsMaxBlocks ? share : kNsMaxBlocks), (unsigned)count);
+    if (fp4q_status st = launched(launch_dependent(momentum_kernel<false>, grid, kNsThreads, s, q, true))) return st;
+    if (fp4q_status st = launched(launch_dependent(momentum_kernel<true>, grid, kNsThreads, s, q, true))) return st;
+
+    const bool tall = rows > cols;
+    const int64_t side = at.side;
+    Gemm16Params p = {};
+    p.batch = (int32_t)count;
+    p.a_box = 128;
+    p.status = static_cast<uint32_t *>(ws);
+    const Operand16 op_a = {a, side, side, count, at.pitch_a, side * at.pitch_a}, op_p = {poly, side, side, count, at.pitch_a, side * at.pitch_a};
+    // Pairs where their tiles fill the GPU; else smaller tiles.
+    const bool pairs = count * ceil_div(side, 256) * (ceil_div(side, 256) + 1) / 2 >= 74;
+    for (int32_t i = 0; i < steps; i++) {
+        const float *c = coefficients + 3 * i;
+        const Operand16 op_x = {x[i & 1], cols, rows, count, at.pitch_x, rows * at.pitch_x};
+        Gemm16Params gp = p;
+        gp.m = gp.n = (int32_t)side;
+        gp.k = (int32_t)(tall ? rows : cols);
+        gp.fa = kScaleA / (kScaleX * kScaleX);
+        gp.out0 = a;
+        gp.pitch = at.pitch_a;
+        Gemm16Params pp = gp;
+        pp.k = (int32_t)side;
+        pp.in0 = a;
+        pp.out0 = poly;
+        pp.fb = c[1];
+        pp.fc = c[2] / kScaleA;
+        Gemm16Params up = p;
+        up.m = (int32_t)rows;
+        up.n = (int32_t)cols;
+        up.k = (int32_t)side;
+        up.fa = c[0];
+        up.fb = 1.0f / kScaleA;
+        up.in0 = x[i & 1];
+        up.in1 = up.out1 = lo;
+        up.out0 = x[(i & 1) ^ 1];
+        up.pitch = at.pitch_x;
+        if (i == steps - 1) {
+            up.o = static_cast<__nv_bfloat16 *>(out_bf16);
+            up.ld_o = ld_o;
+            up.o_scale = scale / kScaleX;
+            up.o_vec = aligned(out_bf16, 16) && ld_o % 8 == 0;
+        }
+        fp4q_status st = pairs ? Steps<2, 256>::gram(op_x, tall, gp, s) : Steps<1, 128>::gram(op_x, tall, gp, s);
+        if (!st) st = pairs ? Steps<2, 256>::poly(op_a, pp, s) : Steps<1, 128>::poly(op_a, pp, s);
+        if (!st) st = pairs ? Steps<2, 256>::update(op_x, op_p, tall, up, s) : Steps<1, 128>::update(op_x, op_p, tall, up, s);
+        if (st) return st;
+    }
+    return FP4Q_OK;
+}

@@ -1,0 +1,173 @@
+// BF16 products of groups of rows that start anywhere: forward, input gradient, weight gradient (include/fp4q.h).  The kernel and its
+// variants are in gemm16.cuh; here are the arguments' checks and the choice of a variant.
+#include "gemm16.cuh"
+
+using namespace fp4q;
+
+namespace {
+
+const int kOutFlags = (int)FP4Q_OUT_PADDED | (int)FP4Q_OUT_ZERO_REST;
+const int64_t kMaxDim16 = 0x7FFFFFFF - 4096;
+
+struct Matrix16 {
+    const void *p;
+    int64_t rows, cols, ld;
+};
+
+fp4q_status check_groups16(const fp4q_groups *g)
+{
+    if (!g) return FP4Q_OK;
+    if (g->n_groups <= 0) return FP4Q_ERR_SHAPE;
+    if (g->row_alignment != 0 && g->row_alignment != 1 && g->row_alignment != 128 && g->row_alignment != 256) return FP4Q_ERR_UNSUPPORTED;
+    if (g->n_groups > kMaxGroups16) return FP4Q_ERR_UNSUPPORTED;
+    if (!g->row_offsets) return FP4Q_ERR_NULL;
+    return FP4Q_OK;
+}
+fp4q_status check_shape16(const Matrix16 &m)
+{
+    if (m.rows < 0 || m.cols < 0 || m.ld < m.cols) return FP4Q_ERR_SHAPE;
+    return m.rows > kMaxDim16 || m.cols > kMaxDim16 ? FP4Q_ERR_UNSUPPORTED : FP4Q_OK;
+}
+fp4q_status check_operand16(const Matrix16 &m)
+{
+    if (m.rows == 0 || m.cols == 0) return FP4Q_OK;
+    if (!m.p) return FP4Q_ERR_NULL;
+    return aligned(m.p, 16) && m.ld % 8 == 0 ? FP4Q_OK : FP4Q_ERR_ALIGN;
+}
+bool type_ok(fp4q_out dt)
+{
+    const int type = (int)dt & ~kOutFlags;
+    return type == FP4Q_OUT_BF16 || type == FP4Q_OUT_F32;
+}
+bool out_f32(fp4q_out dt) { return ((int)dt & ~kOutFlags) == FP4Q_OUT_F32; }
+fp4q_status check_output16(void *c, int64_t ldc, int64_t cols, fp4q_out dt, Gemm16Params &p)
+{
+    if (!c) return FP4Q_ERR_NULL;
+    if (ldc < cols) return FP4Q_ERR_SHAPE;
+    const int64_t bytes = out_f32(dt) ? 4 : 2;
+    if (!aligned(c, 16) || ldc * bytes % 16 != 0) return FP4Q_ERR_ALIGN;
+    p.c = c;
+    p.ldc = ldc;
+    p.zero_rest = ((int)dt & (int)FP4Q_OUT_ZERO_REST) != 0;
+    p.wide = aligned(c, 32) && ldc * bytes % 32 == 0;
+    return FP4Q_OK;
+}
+fp4q_status check_workspace(const void *ws, size_t ws_bytes)
+{
+    if (!ws || ws_bytes < sizeof(Workspace)) return FP4Q_ERR_WORKSPACE;
+    return aligned(ws, 256) ? FP4Q_OK : FP4Q_ERR_ALIGN;
+}
+Operand16 operand16(const Matrix16 &m, int64_t rows, int64_t batch) { return Operand16{m.p, m.cols, rows, batch, m.ld, rows * m.ld}; }
+
+template <int CTAS, int BN, bool A_MN, bool B_MN, int TILES>
+fp4q_status launch_store16(const Operand16 &a, const Operand16 &b, const Gemm16Params &p, fp4q_out dt, int64_t most_tiles, cudaStream_t stream)
+{
+    return out_f32(dt) ? launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_SUM, TILES>(a, b, p, most_tiles, stream)
+                       : launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_STORE, TILES>(a, b, p, most_tiles, stream);
+}
+
+// Rows of groups, T in all.
+template <bool B_MN>
+fp4q_status rows_product(const Operand16 &a, const Operand16 &b, Gemm16Params &p, fp4q_out dt, int64_t T, int64_t groups, cudaStream_t stream)
+{
+    const int64_t few = T < groups ? T : groups;   // groups that have rows, at most
+    if (T >= 192 * groups) {
+        p.n_tiles = (int32_t)ceil_div(p.n, 256);
+        p.a_box = 128;
+        return launch_store16<2, 256, false, B_MN, TILES_ROWS>(a, b, p, dt, (T / 256 + few) * p.n_tiles, stream);
+    }
+    p.a_box = T <= 64 * groups ? 32 : 128;
+    const int64_t row_tiles = T / 128 + few;
+    if (row_tiles * ceil_div(p.n, 128) >= 148) {
+        p.n_tiles = (int32_t)ceil_div(p.n, 128);
+        return launch_store16<1, 128, false, B_MN, TILES_ROWS>(a, b, p, dt, row_tiles * p.n_tiles, stream);
+    }
+    p.n_tiles = (int32_t)ceil_div(p.n, 64);
+    return launch_store16<1, 64, false, B_MN, TILES_ROWS>(a, b, p, dt, row_tiles * p.n_tiles, stream);
+}
+
+// which: 0 = Y = X W^T, 1 = dX = dY W.
+fp4q_status rows_call(int which, const Matrix16 &x, const Matrix16 &w, void *c, int64_t ldc, fp4q_out dt, const fp4q_groups *g, void *ws, size_t ws_bytes, void *stream)
+{
+    if (fp4q_status s = check_groups16(g)) return s;
+    if (!type_ok(dt)) return FP4Q_ERR_UNSUPPORTED;
+    if (fp4q_status s = check_shape16(x)) return s;
+    if (fp4q_status s = check_shape16(w)) return s;
+    const int64_t groups = g ? g->n_groups : 1;
+    if (w.rows % groups) return FP4Q_ERR_SHAPE;
+    const int64_t out_features = w.rows / groups, contraction = which ? out_features : w.cols, cols = which ? w.cols : out_features;
+    if (x.cols != contraction) return FP4Q_ERR_SHAPE;
+    if (x.rows == 0 || cols == 0) return FP4Q_OK;
+    Gemm16Params p = {};
+    if (fp4q_status s = check_output16(c, ldc, cols, dt, p)) return s;
+    if (fp4q_status s = check_operand16(x)) return s;
+    if (fp4q_status s = check_operand16(w)) return s;
+    if (fp4q_status s = check_workspace(ws, ws_bytes)) return s;
+    if ((x.rows / 128 + groups) * ceil_div(cols, 64) > kMaxDim16) return FP4Q_ERR_UNSUPPORTED;   // tiles are counted in 32 bits
+    p.m = (int32_t)x.rows;
+    p.n = (int32_t)cols;
+    p.k = (int32_t)contraction;
+    p.batch = (int32_t)groups;
+    p.bf16 = 1;
+    p.offsets = g ? g->row_offsets : nullptr;
+    p.total_rows = x.rows;
+    p.status = static_cast<uint32_t *>(ws);
+    // Without a contraction nothing is read: the maps describe some memory, the output's.
+    const Operand16 a = contraction ? operand16(x, x.rows, 1) : Operand16{c, 8, 1, 1, 8, 8};
+    const Operand16 b = contraction ? operand16(w, out_features, groups) : a;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return which ? rows_product<true>(a, b, p, dt, x.rows, groups, s) : rows_product<false>(a, b, p, dt, x.rows, groups, s);
+}
+
+}  // namespace
+
+extern "C" fp4q_status fp4q_ragged_gemm_fwd(const void *x, int64_t T, int64_t K, int64_t ldx, const void *w, int64_t w_rows, int64_t ldw, void *Y, int64_t ldy,
+                                            fp4q_out dt, const fp4q_groups *g, void *ws, size_t ws_bytes, void *stream)
+{
+    return rows_call(0, Matrix16{x, T, K, ldx}, Matrix16{w, w_rows, K, ldw}, Y, ldy, dt, g, ws, ws_bytes, stream);
+}
+
+extern "C" fp4q_status fp4q_ragged_gemm_dgrad(const void *dY, int64_t T, int64_t N, int64_t ld_dy, const void *w, int64_t w_rows, int64_t K, int64_t ldw, void *dX,
+                                              int64_t ldx, fp4q_out dt, const fp4q_groups *g, void *ws, size_t ws_bytes, void *stream)
+{
+    return rows_call(1, Matrix16{dY, T, N, ld_dy}, Matrix16{w, w_rows, K, ldw}, dX, ldx, dt, g, ws, ws_bytes, stream);
+}
+
+extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t N, int64_t ld_dy, const void *x, int64_t K, int64_t ldx, void *dW, int64_t ldw,
+                                              fp4q_out dt, int accumulate, const fp4q_groups *g, void *ws, size_t ws_bytes, void *stream)
+{
+    const Matrix16 d = {dY, T, N, ld_dy}, m = {x, T, K, ldx};
+    if (fp4q_status s = check_groups16(g)) return s;
+    if (!type_ok(dt)) return FP4Q_ERR_UNSUPPORTED;
+    if (fp4q_status s = check_shape16(d)) return s;
+    if (fp4q_status s = check_shape16(m)) return s;
+    const int64_t groups = g ? g->n_groups : 1;
+    if (N == 0 || K == 0) return FP4Q_OK;
+    Gemm16Params p = {};
+    if (fp4q_status s = check_output16(dW, ldw, K, dt, p)) return s;
+    if (accumulate && !out_f32(dt)) return FP4Q_ERR_UNSUPPORTED;
+    if (fp4q_status s = check_operand16(d)) return s;
+    if (fp4q_status s = check_operand16(m)) return s;
+    if (fp4q_status s = check_workspace(ws, ws_bytes)) return s;
+    if (groups * ceil_div(N, 128) * ceil_div(K, 128) > kMaxDim16) return FP4Q_ERR_UNSUPPORTED;
+    p.m = (int32_t)N;
+    p.n = (int32_t)K;
+    p.k = (int32_t)T;
+    p.batch = (int32_t)groups;
+    p.bf16 = 1;
+    p.a_box = 128;
+    p.offsets = g ? g->row_offsets : nullptr;
+    p.total_rows = T;
+    p.accumulate = accumulate != 0;
+    p.status = static_cast<uint32_t *>(ws);
+    const Operand16 a = T ? operand16(d, T, 1) : Operand16{dW, 8, 1, 1, 8, 8}, b = T ? operand16(m, T, 1) : a;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (groups * ceil_div(N, 256) * ceil_div(K, 256) >= 74) {
+        p.m_tiles = (int32_t)ceil_div(N, 256);
+        p.n_tiles = (int32_t)ceil_div(K, 256);
+        return launch_store16<2, 256, true, true, TILES_CUT>(a, b, p, dt, groups * p.m_tiles * p.n_tiles, s);
+    }
+    p.m_tiles = (int32_t)ceil_div(N, 128);
+    p.n_tiles = (int32_t)ceil_div(K, 128);
+    return launch_store16<1, 128, true, true, TILES_CUT>(a, b, p, dt, groups * p.m_tiles * p.n_tiles, s);
+}
