@@ -14,6 +14,7 @@
 // stay above FP16's smallest normal number and the largest singular values that the entry point admits below its largest.
 #include "gemm16.cuh"
 
+#include <algorithm>
 #include <cmath>
 
 using namespace fp4q;
@@ -276,7 +277,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     q.partial = reinterpret_cast<double *>(base + at.partial);
     q.up = x[0]; q.lo = lo; q.pitch = at.pitch_x;
     const int64_t want = ceil_div(q.units, kNsThreads * kNsUnroll), share = ceil_div(16 * 148, count);
-    const dim3 grid((unsigned)(want < share ? want : share < kNsMaxBlocks ? share : kNsMaxBlocks), (unsigned)count);
+    const dim3 grid((unsigned)std::min<int64_t>(std::min(want, share), kNsMaxBlocks), (unsigned)count);
     if (fp4q_status st = launched(launch_dependent(momentum_kernel<false>, grid, kNsThreads, s, q, true))) return st;
     if (fp4q_status st = launched(launch_dependent(momentum_kernel<true>, grid, kNsThreads, s, q, true))) return st;
 
