@@ -66,9 +66,10 @@ struct Gemm16Params {
     int64_t ldc;
     int32_t accumulate, wide, zero_rest;   // zero_rest: rows that no group owns are written as zeros
     // EPI16_GRAM, _POLY, _UPDATE
+    int32_t split;                   // operands are sums of two numbers: the products upper x upper, upper x lower and lower x upper are added up
     float fa, fb, fc;                // the step's coefficients, with the iterates' scales
-    const __half *in0, *in1;         // POLY: A.  UPDATE: upper and lower parts of X
-    __half *out0, *out1;             // GRAM: A.  POLY: B.  UPDATE: upper and lower parts of the next X
+    const __half *in0, *in1;         // POLY: A, upper and (split) lower parts.  UPDATE: those of X
+    __half *out0, *out1;             // GRAM: A.  POLY: P.  UPDATE: the next X.  Lower parts of A and P if split
     int64_t pitch;                   // of in0, in1, out0, out1
     __nv_bfloat16 *o;                // UPDATE, last step: the result instead
     int64_t ld_o;
@@ -281,11 +282,14 @@ __device__ __forceinline__ void step16(const Gemm16Params &p, const Tile16 &t, i
             for (int j = 0; j < 8; j++) w[j] = v[e + j] * p.fa;
         }
         if (EPI == EPI16_POLY) {
-            const uint4 a = load_uint4(p.in0 + at + e);
-            const float2 a0 = unpack_half(a.x), a1 = unpack_half(a.y), a2 = unpack_half(a.z), a3 = unpack_half(a.w);
-            const float x[8] = {a0.x, a0.y, a1.x, a1.y, a2.x, a2.y, a3.x, a3.y};
+            const uint4 a = load_uint4(p.in0 + at + e), b = p.split ? load_uint4(p.in1 + at + e) : make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t up[4] = {a.x, a.y, a.z, a.w}, lo[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-            for (int j = 0; j < 8; j++) w[j] = fmaf(p.fb, x[j], p.fc * v[e + j]);
+            for (int j = 0; j < 4; j++) {
+                const float2 x = unpack_half(up[j]), y = unpack_half(lo[j]);
+                w[2 * j] = fmaf(p.fb, x.x + y.x, p.fc * v[e + 2 * j]);
+                w[2 * j + 1] = fmaf(p.fb, x.y + y.y, p.fc * v[e + 2 * j + 1]);
+            }
         }
         if (EPI == EPI16_UPDATE) {
             const uint4 a = load_uint4(p.in0 + at + e), b = load_uint4(p.in1 + at + e);
@@ -313,19 +317,24 @@ __device__ __forceinline__ void step16(const Gemm16Params &p, const Tile16 &t, i
 #pragma unroll
         for (int j = 0; j < 4; j++) h[j] = pack_half(w[2 * j], w[2 * j + 1]);
         *reinterpret_cast<uint4 *>(p.out0 + at + e) = make_uint4(h[0], h[1], h[2], h[3]);
-        if (EPI == EPI16_UPDATE) {
-            uint32_t l[4];
+        uint32_t l[4];
+        if (EPI == EPI16_UPDATE || p.split) {
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 const float2 x = unpack_half(h[j]);
                 l[j] = pack_half(w[2 * j] - x.x, w[2 * j + 1] - x.y);
             }
             *reinterpret_cast<uint4 *>(p.out1 + at + e) = make_uint4(l[0], l[1], l[2], l[3]);
-        } else if (t.mirror) {
-            const __half *s = reinterpret_cast<const __half *>(h);
+        }
+        if (EPI != EPI16_UPDATE && t.mirror) {
+            const __half *s = reinterpret_cast<const __half *>(h), *r = reinterpret_cast<const __half *>(l);
 #pragma unroll
-            for (int j = 0; j < 8; j++)
-                if (col + e + j < p.n) p.out0[base + (int64_t)(col + e + j) * p.pitch + row] = s[j];
+            for (int j = 0; j < 8; j++) {
+                if (col + e + j >= p.n) continue;
+                const int64_t there = base + (int64_t)(col + e + j) * p.pitch + row;
+                p.out0[there] = s[j];
+                if (p.split) p.out1[there] = r[j];
+            }
         }
     }
 }
@@ -333,10 +342,12 @@ __device__ __forceinline__ void step16(const Gemm16Params &p, const Tile16 &t, i
 // ---------------------------------------------------------------------------------------- kernel
 
 template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
-__global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Gemm16Params p)
+__global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmA2,
+                                                               const __grid_constant__ CUtensorMap tmB2, const Gemm16Params p)
 {
     using C = Cfg16<CTAS, BN>;
     constexpr int kStages = C::kStages;
+    constexpr bool kSplits = EPI == EPI16_GRAM || EPI == EPI16_POLY || EPI == EPI16_UPDATE;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t *smem_a = smem, *smem_b = smem + kStages * C::kABytes;
@@ -430,14 +441,14 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b);
         for (int tile = tile0; ok && tile < tiles; tile += step) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
-            const int stages = (t.k_len + kK16 - 1) / kK16;
+            const int k_stages = (t.k_len + kK16 - 1) / kK16, stages = kSplits && p.split ? 3 * k_stages : k_stages;
             const int a_copies = A_MN ? 2 : (t.rows + p.a_box - 1) / p.a_box;
             const int a_copies_peer = A_MN ? 2 : (t.rows_peer + p.a_box - 1) / p.a_box;
             const uint32_t a_copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
             for (int s = 0; s < stages; s++, it++) {
                 const uint32_t slot = it % kStages;
                 if (!warp_wait(bar_empty + 8 * slot, ((it / kStages) & 1u) ^ 1u, abort_flag, p.status, limit, 0x100u + slot)) { ok = false; break; }
-                const int k = t.k0 + s * kK16;
+                const int pass = kSplits ? (s >= k_stages) + (s >= 2 * k_stages) : 0, k = t.k0 + (s - pass * k_stages) * kK16;
                 // A stage with rows behind its group's end lands on a barrier of its own in each CTA, where warp 2 waits for it.
                 const bool cut = TILES == TILES_CUT && t.k_len - s * kK16 < kK16;
                 if (elect_one()) {
@@ -454,18 +465,19 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                             else tma_load_3d(dst, map, x, y, z, bar);
                         };
                         // TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack
+                        const CUtensorMap *mapA = kSplits && pass == 2 ? &tmA2 : &tmA, *mapB = kSplits && pass == 1 ? &tmB2 : &tmB;
                         const int az = TILES <= TILES_CUT ? 0 : t.batch, bz = TILES == TILES_CUT ? 0 : t.batch;
                         if (A_MN) {
 #pragma unroll
-                            for (int j = 0; j < 2; j++) load(a + j * 8192, &tmA, t.a_row + 64 * j, k, az);
+                            for (int j = 0; j < 2; j++) load(a + j * 8192, mapA, t.a_row + 64 * j, k, az);
                         } else {
-                            for (int j = 0; j < a_copies; j++) load(a + j * a_copy_bytes, &tmA, k, t.a_row + j * p.a_box, az);
+                            for (int j = 0; j < a_copies; j++) load(a + j * a_copy_bytes, mapA, k, t.a_row + j * p.a_box, az);
                         }
                         if (B_MN) {
 #pragma unroll
-                            for (int j = 0; j < C::kBRows / 64; j++) load(b + j * 8192, &tmB, t.b_row + 64 * j, k, bz);
+                            for (int j = 0; j < C::kBRows / 64; j++) load(b + j * 8192, mapB, t.b_row + 64 * j, k, bz);
                         } else {
-                            load(b, &tmB, k, t.b_row, bz);
+                            load(b, mapB, k, t.b_row, bz);
                         }
                     }
                 }
@@ -482,7 +494,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         bool ok = true;
         for (int tile = tile0; ok && tile < tiles; tile += step) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
-            const int stages = (t.k_len + kK16 - 1) / kK16;
+            const int k_stages = (t.k_len + kK16 - 1) / kK16, stages = kSplits && p.split ? 3 * k_stages : k_stages;
             uint32_t acc = 0;
             for (int s = 0; s < stages; s++, it++) {
                 const bool opens = EPI == EPI16_SUM ? s % kSumStages == 0 : s == 0;
@@ -495,7 +507,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 }
                 const uint32_t slot = it % kStages;
                 if (!warp_wait(bar_full + 8 * slot, (it / kStages) & 1u, abort_flag, p.status, limit, 0x300u + slot)) { ok = false; break; }
-                const int left = t.k_len - s * kK16;
+                const int left = t.k_len - (kSplits ? s - ((s >= k_stages) + (s >= 2 * k_stages)) * k_stages : s) * kK16;
                 if (TILES == TILES_CUT && CTAS == 2 && left < kK16) fence_cluster_acquire();
                 tcgen05_fence_after();
                 if (elect_one()) {
@@ -550,7 +562,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
             const int in = 32 * quarter + lane;
             const int chunks = EPI == EPI16_SUM ? (t.k_len + kSumStages * kK16 - 1) / (kSumStages * kK16) : t.k_len > 0;   // accumulators of the tile
-            const uint64_t acc_limit = limit * (uint64_t)(1 + (t.k_len >> 10));
+            const uint64_t acc_limit = limit * (uint64_t)(1 + (t.k_len >> 8));
             const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
             const int64_t row = (TILES == TILES_CUT ? (int64_t)t.batch * p.m : 0) + t.row + in;
             // The accumulator may be overwritten as soon as all warps have it in registers.
@@ -660,14 +672,17 @@ inline bool make_map16(CUtensorMap *map, const Operand16 &o, int box_rows)
     return encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void *>(o.base), dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
-// most_tiles: no fewer than the tiles there can be.
+// a2, b2: the operands' lower parts (p.split).  most_tiles: no fewer than the tiles there can be.
 template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
-fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Gemm16Params &p, int64_t most_tiles, cudaStream_t stream)
+fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand16 &a2, const Operand16 &b2, const Gemm16Params &p, int64_t most_tiles, cudaStream_t stream)
 {
     using C = Cfg16<CTAS, BN>;
-    CUtensorMap tmA, tmB;
+    CUtensorMap tmA, tmB, tmA2, tmB2;
     if (!make_map16(&tmA, a, A_MN ? kK16 : p.a_box)) return FP4Q_ERR_CUDA;
     if (!make_map16(&tmB, b, B_MN ? kK16 : C::kBRows)) return FP4Q_ERR_CUDA;
+    tmA2 = tmA;
+    tmB2 = tmB;
+    if (p.split && (!make_map16(&tmA2, a2, A_MN ? kK16 : p.a_box) || !make_map16(&tmB2, b2, B_MN ? kK16 : C::kBRows))) return FP4Q_ERR_CUDA;
     const int dev = current_device();
     if (dev < 0) return FP4Q_ERR_CUDA;
     constexpr int kSmem = C::smem(TILES);
@@ -697,7 +712,7 @@ fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Gemm16Pa
         attr[1].val.clusterDim.z = 1;
         cfg.numAttrs = 2;
     }
-    return launched(cudaLaunchKernelEx(&cfg, gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES>, tmA, tmB, p));
+    return launched(cudaLaunchKernelEx(&cfg, gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES>, tmA, tmB, tmA2, tmB2, p));
 }
 
 }  // namespace fp4q

@@ -10,7 +10,9 @@
 // three bits that FP16 has more than BF16 cost nothing.  X itself is kept as a sum of two FP16 numbers (22 bits): what is rounded is only
 // the operand of the products.  The term a X carries directions of small singular values from step to step, multiplied by a = 3.4 each time,
 // and rounding X as a whole puts noise into those that a gradient does not have (rank 100, 768 x 2048: the update is off by 1.8e-2 with one
-// FP16 number and 1.4e-1 with a BF16 one, 7e-4 with the sum of two).  Scales: X 2^10, A and P 2^9, so that elements of large matrices
+// FP16 number and 1.4e-1 with a BF16 one, 7e-4 with the sum of two).  Matrices of a short side have few elements over which the roundings of
+// A, P and the products' X average out (1.5e-3 of the result at 777 x 1003, 2.0e-3 at 64 x 64, 3e-3 and more below 16) and little work:
+// there A and P are sums of two numbers as well, and the three products are made of three each (kSplitSide).  Scales: X 2^10, A and P 2^9, so that elements of large matrices
 // stay above FP16's smallest normal number and the largest singular values that the entry point admits below its largest.
 #include "gemm16.cuh"
 
@@ -24,6 +26,7 @@ namespace {
 constexpr int kNsThreads = 256, kNsUnroll = 4, kNsMaxBlocks = 1024;
 constexpr float kScaleX = 1024.0f, kScaleA = 512.0f;
 constexpr int kMaxSteps = 64;
+constexpr int64_t kSplitSide = 384;
 
 struct MomentumParams {
     const void *g;
@@ -168,20 +171,22 @@ __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumPara
 // Where things lie in the scratch memory.
 struct Scratch {
     int64_t pitch_x, pitch_a, side;
-    size_t partial, x0, x1, lo, a, poly, bytes;
+    bool split;
+    size_t partial, x[2], lo[2], a[2], poly[2], bytes;   // upper and lower parts; X and the next X: lower parts in one place unless they are operands
     Scratch(int64_t count, int64_t rows, int64_t cols)
     {
         side = rows < cols ? rows : cols;
         pitch_x = round_up(cols, 16);
         pitch_a = round_up(side, 16);
-        const size_t x = (size_t)round_up(count * rows * pitch_x * 2, 256), s = (size_t)round_up(count * side * pitch_a * 2, 256);
+        const size_t x_bytes = (size_t)round_up(count * rows * pitch_x * 2, 256), a_bytes = (size_t)round_up(count * side * pitch_a * 2, 256);
+        split = side <= kSplitSide;
         partial = 0;
-        x0 = (size_t)round_up(count * kNsMaxBlocks * 8, 256);
-        x1 = x0 + x;
-        lo = x1 + x;
-        a = lo + x;
-        poly = a + s;
-        bytes = poly + s;
+        bytes = (size_t)round_up(count * kNsMaxBlocks * 8, 256);
+        auto place = [&](size_t n) { const size_t at = bytes; bytes += n; return at; };
+        x[0] = place(x_bytes); x[1] = place(x_bytes);
+        lo[0] = place(x_bytes); lo[1] = split ? place(x_bytes) : lo[0];
+        a[0] = place(a_bytes); a[1] = split ? place(a_bytes) : a[0];
+        poly[0] = place(a_bytes); poly[1] = split ? place(a_bytes) : poly[0];
     }
 };
 
@@ -211,29 +216,36 @@ bool steps_fit(const float *c, int32_t steps)
     return true;
 }
 
+// Upper and lower parts of an operand.
+struct Parts {
+    Operand16 up, lo;
+    Parts(const void *u, const void *l, int64_t cols, int64_t rows, int64_t count, int64_t pitch)
+        : up{u, cols, rows, count, pitch, rows * pitch}, lo{l, cols, rows, count, pitch, rows * pitch} {}
+};
+
 template <int CTAS, int BN>
 struct Steps {
     static constexpr int kBM = kRows16 * CTAS;
-    static fp4q_status gram(const Operand16 &x, bool tall, Gemm16Params p, cudaStream_t stream)
+    static fp4q_status gram(const Parts &x, bool tall, Gemm16Params p, cudaStream_t stream)
     {
         static_assert(kBM == BN, "symmetric products have square tiles");
         p.m_tiles = p.n_tiles = (int32_t)ceil_div(p.n, BN);
         const int64_t tiles = (int64_t)p.batch * p.m_tiles * (p.m_tiles + 1) / 2;
-        return tall ? launch_gemm16<CTAS, BN, true, true, EPI16_GRAM, TILES_SYM>(x, x, p, tiles, stream)
-                    : launch_gemm16<CTAS, BN, false, false, EPI16_GRAM, TILES_SYM>(x, x, p, tiles, stream);
+        return tall ? launch_gemm16<CTAS, BN, true, true, EPI16_GRAM, TILES_SYM>(x.up, x.up, x.lo, x.lo, p, tiles, stream)
+                    : launch_gemm16<CTAS, BN, false, false, EPI16_GRAM, TILES_SYM>(x.up, x.up, x.lo, x.lo, p, tiles, stream);
     }
-    static fp4q_status poly(const Operand16 &a, Gemm16Params p, cudaStream_t stream)
+    static fp4q_status poly(const Parts &a, Gemm16Params p, cudaStream_t stream)
     {
         p.m_tiles = p.n_tiles = (int32_t)ceil_div(p.n, BN);
-        return launch_gemm16<CTAS, BN, false, false, EPI16_POLY, TILES_SYM>(a, a, p, (int64_t)p.batch * p.m_tiles * (p.m_tiles + 1) / 2, stream);
+        return launch_gemm16<CTAS, BN, false, false, EPI16_POLY, TILES_SYM>(a.up, a.up, a.lo, a.lo, p, (int64_t)p.batch * p.m_tiles * (p.m_tiles + 1) / 2, stream);
     }
-    static fp4q_status update(const Operand16 &x, const Operand16 &poly, bool tall, Gemm16Params p, cudaStream_t stream)
+    static fp4q_status update(const Parts &x, const Parts &poly, bool tall, Gemm16Params p, cudaStream_t stream)
     {
         p.m_tiles = (int32_t)ceil_div(p.m, kBM);
         p.n_tiles = (int32_t)ceil_div(p.n, BN);
         const int64_t tiles = (int64_t)p.batch * p.m_tiles * p.n_tiles;
-        return tall ? launch_gemm16<CTAS, BN, false, false, EPI16_UPDATE, TILES_BATCH>(x, poly, p, tiles, stream)
-                    : launch_gemm16<CTAS, BN, false, true, EPI16_UPDATE, TILES_BATCH>(poly, x, p, tiles, stream);
+        return tall ? launch_gemm16<CTAS, BN, false, false, EPI16_UPDATE, TILES_BATCH>(x.up, poly.up, x.lo, poly.lo, p, tiles, stream)
+                    : launch_gemm16<CTAS, BN, false, true, EPI16_UPDATE, TILES_BATCH>(poly.up, x.up, poly.lo, x.lo, p, tiles, stream);
     }
 };
 
@@ -263,8 +275,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     if (!aligned(ws, 256) || !aligned(scratch, 256)) return FP4Q_ERR_ALIGN;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     uint8_t *base = static_cast<uint8_t *>(scratch);
-    __half *x[2] = {reinterpret_cast<__half *>(base + at.x0), reinterpret_cast<__half *>(base + at.x1)}, *lo = reinterpret_cast<__half *>(base + at.lo),
-           *a = reinterpret_cast<__half *>(base + at.a), *poly = reinterpret_cast<__half *>(base + at.poly);
+    auto half_at = [&](size_t offset) { return reinterpret_cast<__half *>(base + offset); };
 
     MomentumParams q = {};
     q.g = g; q.m = momentum; q.ld_g = ld_g; q.ld_m = ld_m; q.rows = rows; q.cols = (int32_t)cols;
@@ -275,7 +286,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     q.units = (uint32_t)(rows * q.units_row);
     q.beta = beta; q.nesterov = nesterov != 0; q.eps = eps;
     q.partial = reinterpret_cast<double *>(base + at.partial);
-    q.up = x[0]; q.lo = lo; q.pitch = at.pitch_x;
+    q.up = half_at(at.x[0]); q.lo = half_at(at.lo[0]); q.pitch = at.pitch_x;
     const int64_t want = ceil_div(q.units, kNsThreads * kNsUnroll), share = ceil_div(16 * 148, count);
     const dim3 grid((unsigned)std::min<int64_t>(std::min(want, share), kNsMaxBlocks), (unsigned)count);
     if (fp4q_status st = launched(launch_dependent(momentum_kernel<false>, grid, kNsThreads, s, q, true))) return st;
@@ -287,22 +298,27 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     p.batch = (int32_t)count;
     p.a_box = 128;
     p.status = static_cast<uint32_t *>(ws);
-    const Operand16 op_a = {a, side, side, count, at.pitch_a, side * at.pitch_a}, op_p = {poly, side, side, count, at.pitch_a, side * at.pitch_a};
+    p.split = at.split;
+    const Parts part_a(half_at(at.a[0]), half_at(at.a[1]), side, side, count, at.pitch_a), part_p(half_at(at.poly[0]), half_at(at.poly[1]), side, side, count, at.pitch_a);
     // Pairs where their tiles fill the GPU; else smaller tiles.
     const bool pairs = count * ceil_div(side, 256) * (ceil_div(side, 256) + 1) / 2 >= 74;
     for (int32_t i = 0; i < steps; i++) {
         const float *c = coefficients + 3 * i;
-        const Operand16 op_x = {x[i & 1], cols, rows, count, at.pitch_x, rows * at.pitch_x};
+        const int now = i & 1, next = now ^ 1;
+        const Parts part_x(half_at(at.x[now]), half_at(at.lo[now]), cols, rows, count, at.pitch_x);
         Gemm16Params gp = p;
         gp.m = gp.n = (int32_t)side;
         gp.k = (int32_t)(tall ? rows : cols);
         gp.fa = kScaleA / (kScaleX * kScaleX);
-        gp.out0 = a;
+        gp.out0 = half_at(at.a[0]);
+        gp.out1 = half_at(at.a[1]);
         gp.pitch = at.pitch_a;
         Gemm16Params pp = gp;
         pp.k = (int32_t)side;
-        pp.in0 = a;
-        pp.out0 = poly;
+        pp.in0 = half_at(at.a[0]);
+        pp.in1 = half_at(at.a[1]);
+        pp.out0 = half_at(at.poly[0]);
+        pp.out1 = half_at(at.poly[1]);
         pp.fb = c[1];
         pp.fc = c[2] / kScaleA;
         Gemm16Params up = p;
@@ -311,9 +327,10 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
         up.k = (int32_t)side;
         up.fa = c[0];
         up.fb = 1.0f / kScaleA;
-        up.in0 = x[i & 1];
-        up.in1 = up.out1 = lo;
-        up.out0 = x[(i & 1) ^ 1];
+        up.in0 = half_at(at.x[now]);
+        up.in1 = half_at(at.lo[now]);
+        up.out0 = half_at(at.x[next]);
+        up.out1 = half_at(at.lo[next]);
         up.pitch = at.pitch_x;
         if (i == steps - 1) {
             up.o = static_cast<__nv_bfloat16 *>(out_bf16);
@@ -321,9 +338,9 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
             up.o_scale = scale / kScaleX;
             up.o_vec = aligned(out_bf16, 16) && ld_o % 8 == 0;
         }
-        fp4q_status st = pairs ? Steps<2, 256>::gram(op_x, tall, gp, s) : Steps<1, 128>::gram(op_x, tall, gp, s);
-        if (!st) st = pairs ? Steps<2, 256>::poly(op_a, pp, s) : Steps<1, 128>::poly(op_a, pp, s);
-        if (!st) st = pairs ? Steps<2, 256>::update(op_x, op_p, tall, up, s) : Steps<1, 128>::update(op_x, op_p, tall, up, s);
+        fp4q_status st = pairs ? Steps<2, 256>::gram(part_x, tall, gp, s) : Steps<1, 128>::gram(part_x, tall, gp, s);
+        if (!st) st = pairs ? Steps<2, 256>::poly(part_a, pp, s) : Steps<1, 128>::poly(part_a, pp, s);
+        if (!st) st = pairs ? Steps<2, 256>::update(part_x, part_p, tall, up, s) : Steps<1, 128>::update(part_x, part_p, tall, up, s);
         if (st) return st;
     }
     return FP4Q_OK;

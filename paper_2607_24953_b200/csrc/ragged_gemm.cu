@@ -62,8 +62,8 @@ Operand16 operand16(const Matrix16 &m, int64_t rows, int64_t batch) { return Ope
 template <int CTAS, int BN, bool A_MN, bool B_MN, int TILES>
 fp4q_status launch_store16(const Operand16 &a, const Operand16 &b, const Gemm16Params &p, fp4q_out dt, int64_t most_tiles, cudaStream_t stream)
 {
-    return out_f32(dt) ? launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_SUM, TILES>(a, b, p, most_tiles, stream)
-                       : launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_STORE, TILES>(a, b, p, most_tiles, stream);
+    return out_f32(dt) ? launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_SUM, TILES>(a, b, a, b, p, most_tiles, stream)
+                       : launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_STORE, TILES>(a, b, a, b, p, most_tiles, stream);
 }
 
 // Rows of groups, T in all.

@@ -131,7 +131,7 @@ def test_larger_ones_with_skewed_groups(op, T, n, k, e):
         rows = slice(0, None) if op == "wgrad" else slice(5, T)
         assert ((got - y).abs() <= bound(y, s, length, dt))[rows].all()
         if dt == b.OUT_F32:    # a sum of one sign, where the cut-off towards zero would add up: 512 elements' worth of it at most
-            z = call(op, a.abs(), w.abs(), offsets(values), None, dt).double()
+            z = call(op, rows16(a.abs()), rows16(w.abs()), offsets(values), None, dt).double()
             assert ((z - s).abs() <= bound(s, s, length, dt))[rows].all()
 
 
