@@ -6,8 +6,8 @@
 // Persistent kernel, one CTA per SM, 12 warps.  A CTA has 128 rows of the accumulator; pairs (cta_group::2) share a tile of 256 rows and
 // each loads half of B's columns, which is what lets 32 KB of operands feed 2 x 256 x 256 x 64 operations per stage; single CTAs have tiles of
 // 128 x 128 or 128 x 64 for problems with few tiles or short groups.
-//   warp 0      TMA producer: a stage is 64 contraction elements, boxes of 128 bytes with the 128-byte swizzle
-//   warp 1      MMA issuer (in the leader of a pair): four tcgen05.mma of 16 contraction elements per stage
+//   warp 0      TMA producer: a stage is 64 contraction elements (single CTAs: 128), boxes of 128 bytes with the 128-byte swizzle
+//   warp 1      MMA issuer (in the leader of a pair): four tcgen05.mma of 16 contraction elements per box
 //   warp 2      cut contractions: zeroes the rows of a group's last stage that lie behind the group
 //   warps 4-11  epilogue: a thread has a row of the tile; the accumulator is double-buffered in tensor memory
 // Every wait is bounded: when a limit is hit the CTA records FP4Q_ERR_TIMEOUT in the workspace, its roles stop and it leaves through the
@@ -23,7 +23,7 @@
 namespace fp4q {
 
 constexpr int kRows16 = 128;         // accumulator rows per CTA
-constexpr int kK16 = 64;             // contraction elements per stage: 128 bytes
+constexpr int kBox16 = 64;           // contraction elements of a box: 128 bytes
 constexpr int kThreads16 = 384;
 constexpr int kRaster16 = 16;        // row tiles per rasterisation group: their A rows stay in L2 while the columns go by
 constexpr int kMaxGroups16 = 4095;   // boundaries and first tiles of this many groups lie in shared memory
@@ -36,14 +36,20 @@ enum { TILES_ROWS = 0, TILES_CUT = 1, TILES_BATCH = 2, TILES_SYM = 3 };
 // the result for every element (2e-5 at 16384; 8e-5 where all products are positive).  BF16 and FP16 outputs do not show it.  FP32
 // ones are sums, to nearest and in registers, of accumulators of 512 elements each.
 enum { EPI16_STORE = 0, EPI16_GRAM = 1, EPI16_POLY = 2, EPI16_UPDATE = 3, EPI16_SUM = 4 };
-constexpr int kSumStages = 8;        // stages that an accumulator takes with EPI16_SUM
+constexpr int kSumElems = 512;
 
 template <int CTAS, int BN>
 struct Cfg16 {
     static_assert(CTAS == 1 || (CTAS == 2 && BN == 256), "tile shapes");
     static constexpr int kBRows = BN / CTAS;
-    static constexpr int kABytes = kRows16 * 128, kBBytes = kBRows * 128;
-    static constexpr int kStages = BN == 64 ? 8 : 6;
+    // A stage of a pair is one box deep: 512 cycles of MMAs.  The tiles of single CTAs take a quarter or half of that, less than a round of
+    // the issuer's (the wait for the next stage, a shared-memory access, queues behind the MMAs just issued: about 600 cycles, measured
+    // with one box), so their stages are two boxes deep.
+    static constexpr int kBoxes = CTAS == 2 ? 1 : 2;
+    static constexpr int kK = kBoxes * kBox16;                              // contraction elements per stage
+    static constexpr int kABox = kRows16 * 128, kBBox = kBRows * 128;
+    static constexpr int kABytes = kBoxes * kABox, kBBytes = kBoxes * kBBox;
+    static constexpr int kStages = CTAS == 2 ? 6 : BN == 64 ? 4 : 3;
     static constexpr int kTmemCols = 2 * BN;
     static constexpr int kOperands = kStages * (kABytes + kBBytes);
     static constexpr int kTail = 512;                                       // barriers, tensor memory's address, abort flag
@@ -61,6 +67,7 @@ struct Gemm16Params {
     const int64_t *offsets;          // TILES_ROWS, TILES_CUT: batch + 1 boundaries; NULL: one group of all rows
     int64_t total_rows;              // rows that the boundaries are held to
     uint32_t *status;
+    int32_t admit;                   // the next kernel may set up beside this one (it is one of the same call)
     // EPI16_STORE, EPI16_SUM
     void *c;
     int64_t ldc;
@@ -125,11 +132,44 @@ __device__ __forceinline__ uint32_t instr_desc16(bool bf16, bool a_mn, bool b_mn
     return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(BN >> 3) << 17) |
            ((uint32_t)((kRows16 * CTAS) >> 4) << 24);
 }
-// A whole warp's wait: all lanes go on or none does.
+// A whole warp's bounded wait: all lanes go on or none does.  `limit` is in microseconds of the clock, the unit of the workspace's polls; a
+// poll suspends the warp for as long as the hardware likes, which is finite.  (With suspensions of a microsecond at most, as the
+// quantized products have them, the update product of 2048 x 5632 took 83 us instead of 67.)
+__device__ __forceinline__ uint64_t now_ns()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t *status, uint64_t limit, uint32_t where)
 {
-    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, status, limit, where));
+    bool ok = true;
+    uint64_t since = 0;
+    while (true) {
+        uint32_t done;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) break;
+        if (*abort_flag) { ok = false; break; }
+        const uint64_t now = now_ns();
+        if (since == 0) since = now;
+        else if (now - since > limit * 1000) {
+            *abort_flag = 1u;
+            if (atomicCAS(status, 0u, (uint32_t)FP4Q_ERR_TIMEOUT) == 0u) status[1] = where;
+            ok = false;
+            break;
+        }
+    }
+    return __all_sync(0xFFFFFFFFu, ok);
 }
+// A ring's next slot and its phase.
+template <int N>
+struct Ring16 {
+    uint32_t slot = 0, phase = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++slot == N) { slot = 0; phase ^= 1u; }
+    }
+};
 
 // ---------------------------------------------------------------------------------------- tiles
 
@@ -267,10 +307,27 @@ __device__ __forceinline__ void store_f32(const Gemm16Params &p, int64_t row, in
     }
 }
 
+// What the epilogue of a step reads of 32 columns of a row: the upper and lower parts of A (POLY) or X (UPDATE).
+struct Fetched16 {
+    uint4 up[4], lo[4];
+};
+template <int EPI>
+__device__ __forceinline__ void fetch16(const Gemm16Params &p, int64_t at, int col, Fetched16 &f)
+{
+    if (EPI != EPI16_POLY && EPI != EPI16_UPDATE) return;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        f.lo[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (col + 8 * i >= p.pitch) continue;
+        f.up[i] = load_uint4(p.in0 + at + 8 * i);
+        if (EPI == EPI16_UPDATE || p.split) f.lo[i] = load_uint4(p.in1 + at + 8 * i);
+    }
+}
+
 // The iterates' rows are padded to whole 32 bytes: a piece of eight columns is written if it starts inside the row.  What columns behind
 // the matrix hold is never read.
 template <int EPI>
-__device__ __forceinline__ void step16(const Gemm16Params &p, const Tile16 &t, int64_t base, int row, int col, const float *v)
+__device__ __forceinline__ void step16(const Gemm16Params &p, const Tile16 &t, int64_t base, int row, int col, const Fetched16 &f, const float *v)
 {
     const int64_t at = base + (int64_t)row * p.pitch + col;
 #pragma unroll
@@ -282,7 +339,7 @@ __device__ __forceinline__ void step16(const Gemm16Params &p, const Tile16 &t, i
             for (int j = 0; j < 8; j++) w[j] = v[e + j] * p.fa;
         }
         if (EPI == EPI16_POLY) {
-            const uint4 a = load_uint4(p.in0 + at + e), b = p.split ? load_uint4(p.in1 + at + e) : make_uint4(0u, 0u, 0u, 0u);
+            const uint4 a = f.up[e / 8], b = f.lo[e / 8];
             const uint32_t up[4] = {a.x, a.y, a.z, a.w}, lo[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
             for (int j = 0; j < 4; j++) {
@@ -292,7 +349,7 @@ __device__ __forceinline__ void step16(const Gemm16Params &p, const Tile16 &t, i
             }
         }
         if (EPI == EPI16_UPDATE) {
-            const uint4 a = load_uint4(p.in0 + at + e), b = load_uint4(p.in1 + at + e);
+            const uint4 a = f.up[e / 8], b = f.lo[e / 8];
             const uint32_t up[4] = {a.x, a.y, a.z, a.w}, lo[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
             for (int j = 0; j < 4; j++) {
@@ -433,94 +490,111 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     }
     const int tiles = TILES == TILES_ROWS ? m_tiles * p.n_tiles : TILES == TILES_SYM ? p.batch * (m_tiles * (m_tiles + 1) / 2) : p.batch * m_tiles * p.n_tiles;
     const int tile0 = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+    const int passes = kSplits && p.split ? 3 : 1;   // upper x upper, upper x lower, lower x upper
+    if (p.admit) admit_successor();
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
-        uint32_t it = 0, loads = 0;
+        uint32_t loads = 0, issued = 0;
+        Ring16<kStages> ring;
         bool ok = true;
-        const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b);
+        const bool issuer = elect_one();
+        const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b), lead = CTAS == 2 ? cluster_addr(bar_full, 0) : bar_full;
         for (int tile = tile0; ok && tile < tiles; tile += step) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
-            const int k_stages = (t.k_len + kK16 - 1) / kK16, stages = kSplits && p.split ? 3 * k_stages : k_stages;
             const int a_copies = A_MN ? 2 : (t.rows + p.a_box - 1) / p.a_box;
-            const int a_copies_peer = A_MN ? 2 : (t.rows_peer + p.a_box - 1) / p.a_box;
             const uint32_t a_copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
-            for (int s = 0; s < stages; s++, it++) {
-                const uint32_t slot = it % kStages;
-                if (!warp_wait(bar_empty + 8 * slot, ((it / kStages) & 1u) ^ 1u, abort_flag, p.status, limit, 0x100u + slot)) { ok = false; break; }
-                const int pass = kSplits ? (s >= k_stages) + (s >= 2 * k_stages) : 0, k = t.k0 + (s - pass * k_stages) * kK16;
-                // A stage with rows behind its group's end lands on a barrier of its own in each CTA, where warp 2 waits for it.
-                const bool cut = TILES == TILES_CUT && t.k_len - s * kK16 < kK16;
-                if (elect_one()) {
-                    const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * slot;
-                    const bool lead_counts = CTAS == 2 && !cut;
-                    if (rank == 0 || cut)
-                        mbar_arrive_expect_tx(own_bar, (uint32_t)a_copies * a_copy_bytes + (uint32_t)C::kBBytes +
-                                                           (lead_counts ? (uint32_t)a_copies_peer * a_copy_bytes + (uint32_t)C::kBBytes : 0u));
-                    if (withhold == 0u || ++loads != withhold) {
-                        const uint32_t bar = lead_counts ? cluster_addr(own_bar, 0) : own_bar;
-                        const uint32_t a = a0 + slot * C::kABytes, b = b0 + slot * C::kBBytes;
-                        auto load = [&](uint32_t dst, const CUtensorMap *map, int x, int y, int z) {
-                            if (CTAS == 2 && lead_counts) tma_load_3d_pair(dst, map, x, y, z, bar);
-                            else tma_load_3d(dst, map, x, y, z, bar);
-                        };
-                        // TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack
-                        const CUtensorMap *mapA = kSplits && pass == 2 ? &tmA2 : &tmA, *mapB = kSplits && pass == 1 ? &tmB2 : &tmB;
-                        const int az = TILES <= TILES_CUT ? 0 : t.batch, bz = TILES == TILES_CUT ? 0 : t.batch;
-                        if (A_MN) {
+            const uint32_t box_bytes = (uint32_t)a_copies * a_copy_bytes + (uint32_t)C::kBBox;   // of this CTA
+            const uint32_t peer_bytes = CTAS == 2 ? (uint32_t)(A_MN ? 2 : (t.rows_peer + p.a_box - 1) / p.a_box) * a_copy_bytes + (uint32_t)C::kBBox : 0u;
+            // TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack
+            const int az = TILES <= TILES_CUT ? 0 : t.batch, bz = TILES == TILES_CUT ? 0 : t.batch;
+            for (int pass = 0; ok && pass < passes; pass++) {
+                const CUtensorMap *mapA = kSplits && pass == 2 ? &tmA2 : &tmA, *mapB = kSplits && pass == 1 ? &tmB2 : &tmB;
+                for (int k = 0; k < t.k_len; k += C::kK, ring.next()) {
+                    if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) { ok = false; break; }
+                    issued++;
+                    // A stage with rows behind its group's end lands on a barrier of its own in each CTA, where warp 2 waits for it.
+                    const int left = t.k_len - k;
+                    const bool cut = TILES == TILES_CUT && left < C::kK;
+                    if (issuer) {
+                        const int boxes = C::kBoxes == 1 || left > kBox16 ? C::kBoxes : 1;
+                        const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * ring.slot, bar = CTAS == 2 && !cut ? lead + 8 * ring.slot : own_bar;
+                        if (rank == 0 || cut) mbar_arrive_expect_tx(own_bar, (uint32_t)boxes * (box_bytes + (cut ? 0u : peer_bytes)));
+                        if (withhold == 0u || ++loads != withhold) {
+                            auto load = [&](uint32_t dst, const CUtensorMap *map, int x, int y, int z) {
+                                if (CTAS == 2 && !cut) tma_load_3d_pair(dst, map, x, y, z, bar);
+                                else tma_load_3d(dst, map, x, y, z, bar);
+                            };
 #pragma unroll
-                            for (int j = 0; j < 2; j++) load(a + j * 8192, mapA, t.a_row + 64 * j, k, az);
-                        } else {
-                            for (int j = 0; j < a_copies; j++) load(a + j * a_copy_bytes, mapA, k, t.a_row + j * p.a_box, az);
-                        }
-                        if (B_MN) {
+                            for (int i = 0; i < C::kBoxes; i++) {
+                                if (i >= boxes) break;
+                                const uint32_t a = a0 + ring.slot * C::kABytes + i * C::kABox, b = b0 + ring.slot * C::kBBytes + i * C::kBBox;
+                                const int at = t.k0 + k + i * kBox16;
+                                if (A_MN) {
 #pragma unroll
-                            for (int j = 0; j < C::kBRows / 64; j++) load(b + j * 8192, mapB, t.b_row + 64 * j, k, bz);
-                        } else {
-                            load(b, mapB, k, t.b_row, bz);
+                                    for (int j = 0; j < 2; j++) load(a + j * 8192, mapA, t.a_row + 64 * j, at, az);
+                                } else {
+                                    for (int j = 0; j < a_copies; j++) load(a + j * a_copy_bytes, mapA, at, t.a_row + j * p.a_box, az);
+                                }
+                                if (B_MN) {
+#pragma unroll
+                                    for (int j = 0; j < C::kBRows / 64; j++) load(b + j * 8192, mapB, t.b_row + 64 * j, at, bz);
+                                } else {
+                                    load(b, mapB, at, t.b_row, bz);
+                                }
+                            }
                         }
                     }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
         }
         // The MMAs' last reports reach this CTA's barriers while it is still there.
-        for (uint32_t s = it < kStages ? 0u : it - kStages; ok && s < it; s++)
-            ok = warp_wait(bar_empty + 8 * (s % kStages), (s / kStages) & 1u, abort_flag, p.status, limit, 0x700u + s % kStages);
+        for (uint32_t i = 0; ok && i < kStages; i++, ring.next())
+            if (issued >= kStages - i) ok = warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x700u + ring.slot);
     } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------------------------ MMA issuer
         const uint32_t idesc = instr_desc16<CTAS, BN>(p.bf16 != 0, A_MN, B_MN);
-        uint32_t it = 0, n_acc = 0;
-        bool ok = true;
+        Ring16<kStages> ring;
+        Ring16<2> acc;      // accumulators
+        bool ok = true, ready = false;   // ready: the next stage has been seen full
+        const bool issuer = elect_one();
+        const uint64_t a_desc0 = A_MN ? smem_desc_mn_sw128(smem_u32(smem_a)) : smem_desc_sw128(smem_u32(smem_a));
+        const uint64_t b_desc0 = B_MN ? smem_desc_mn_sw128(smem_u32(smem_b)) : smem_desc_sw128(smem_u32(smem_b));
         for (int tile = tile0; ok && tile < tiles; tile += step) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
-            const int k_stages = (t.k_len + kK16 - 1) / kK16, stages = kSplits && p.split ? 3 * k_stages : k_stages;
-            uint32_t acc = 0;
-            for (int s = 0; s < stages; s++, it++) {
-                const bool opens = EPI == EPI16_SUM ? s % kSumStages == 0 : s == 0;
-                const bool closes = s == stages - 1 || (EPI == EPI16_SUM && s % kSumStages == kSumStages - 1);
-                if (opens) {
-                    acc = n_acc & 1u;
-                    if (!warp_wait(bar_acc_empty + 8 * acc, ((n_acc >> 1) & 1u) ^ 1u, abort_flag, p.status, limit, 0x200u)) { ok = false; break; }
-                    n_acc++;
-                    if (CTAS == 2) fence_cluster_acquire();
-                }
-                const uint32_t slot = it % kStages;
-                if (!warp_wait(bar_full + 8 * slot, (it / kStages) & 1u, abort_flag, p.status, limit, 0x300u + slot)) { ok = false; break; }
-                const int left = t.k_len - (kSplits ? s - ((s >= k_stages) + (s >= 2 * k_stages)) * k_stages : s) * kK16;
-                if (TILES == TILES_CUT && CTAS == 2 && left < kK16) fence_cluster_acquire();
-                tcgen05_fence_after();
-                if (elect_one()) {
-                    const uint32_t a = smem_u32(smem_a) + slot * C::kABytes, b = smem_u32(smem_b) + slot * C::kBBytes;
-                    const uint64_t ad = A_MN ? smem_desc_mn_sw128(a) : smem_desc_sw128(a), bd = B_MN ? smem_desc_mn_sw128(b) : smem_desc_sw128(b);
+            uint32_t d = 0;
+            for (int pass = 0; ok && pass < passes; pass++) {
+                for (int k = 0; k < t.k_len; k += C::kK) {
+                    const int left = t.k_len - k;
+                    const bool opens = EPI == EPI16_SUM ? k % kSumElems == 0 : k == 0 && pass == 0;
+                    const bool closes = EPI == EPI16_SUM ? left <= C::kK || (k + C::kK) % kSumElems == 0 : left <= C::kK && pass == passes - 1;
+                    if (opens) {
+                        if (!warp_wait(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u)) { ok = false; break; }
+                        d = tmem + acc.slot * BN;
+                        if (CTAS == 2) fence_cluster_acquire();
+                    }
+                    if (!ready && !warp_wait(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot)) { ok = false; break; }
+                    const uint32_t slot = ring.slot;
+                    ring.next();
+                    // Looked at before this stage is issued: afterwards the look would wait for the MMAs.
+                    ready = __all_sync(0xFFFFFFFFu, mbar_test_wait(bar_full + 8 * ring.slot, ring.phase));
+                    if (TILES == TILES_CUT && CTAS == 2 && left < C::kK) fence_cluster_acquire();
+                    tcgen05_fence_after();
+                    if (issuer) {
 #pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        if (16 * j < left)
-                            tcgen05_mma_f16<CTAS>(tmem + acc * BN, ad + (uint64_t)(j * (A_MN ? 2048 : 32) >> 4), bd + (uint64_t)(j * (B_MN ? 2048 : 32) >> 4), idesc, !opens || j > 0);
-                    tcgen05_commit<CTAS>(bar_empty + 8 * slot);
-                    if (closes) tcgen05_commit<CTAS>(bar_acc_full + 8 * acc);
+                        for (int j = 0; j < 4 * C::kBoxes; j++) {
+                            constexpr int kAStep = A_MN ? 2048 : 32, kBStep = B_MN ? 2048 : 32;
+                            const uint64_t ad = a_desc0 + (uint64_t)((slot * C::kABytes + (j / 4) * C::kABox + (j % 4) * kAStep) >> 4);
+                            const uint64_t bd = b_desc0 + (uint64_t)((slot * C::kBBytes + (j / 4) * C::kBBox + (j % 4) * kBStep) >> 4);
+                            if (16 * j < left) tcgen05_mma_f16<CTAS>(d, ad, bd, idesc, !opens || j > 0);
+                        }
+                        tcgen05_commit<CTAS>(bar_empty + 8 * slot);
+                        if (closes) tcgen05_commit<CTAS>(bar_acc_full + 8 * acc.slot);
+                    }
+                    __syncwarp();
+                    if (closes) acc.next();
                 }
-                __syncwarp();
             }
         }
     } else if (warp == 2 && TILES == TILES_CUT) {
@@ -528,19 +602,20 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         // The last stage of a group holds rows of the next one, or whatever lies behind them.  Up to 15 of them meet an MMA: they are zeroed in
         // both operands (in one, an infinity in the other would make NaN).  Then, and in a pair when the other CTA has done the same, the
         // stage is full.  A slot is filled again only when the MMAs have read it, so its barriers are never a phase ahead.
-        uint32_t it = 0, phases = 0;
+        uint32_t slot = 0, phases = 0;
         for (int tile = tile0; tile < tiles; tile += step) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
-            const int stages = (t.k_len + kK16 - 1) / kK16, left = t.k_len - (stages - 1) * kK16;
-            it += stages;
-            if (stages == 0 || left == kK16) continue;
-            const uint32_t slot = (it - 1) % kStages, parity = (phases >> slot) & 1u;
+            const int whole = t.k_len / C::kK, left = t.k_len - whole * C::kK;
+            slot = (slot + whole) % kStages;
+            if (left == 0) continue;
+            const uint32_t parity = (phases >> slot) & 1u;
             phases ^= 1u << slot;
             if (!warp_wait(bar_cut + 8 * slot, parity, abort_flag, p.status, limit, 0x500u + slot)) break;
-            const int pieces = (((left + 15) & ~15) - left) * 8;
+            const int in_box = left % kBox16, pieces = (((in_box + 15) & ~15) - in_box) * 8;
+            const uint32_t box = left / kBox16;   // in_box is 0, and nothing is zeroed, where this box is not there
             for (int c = 0; c < 2 + C::kBRows / 64; c++) {
-                uint8_t *chunk = c < 2 ? smem_a + slot * C::kABytes + c * 8192 : smem_b + slot * C::kBBytes + (c - 2) * 8192;
-                for (int i = lane; i < pieces; i += 32) *reinterpret_cast<uint4 *>(chunk + left * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                uint8_t *chunk = c < 2 ? smem_a + slot * C::kABytes + box * C::kABox + c * 8192 : smem_b + slot * C::kBBytes + box * C::kBBox + (c - 2) * 8192;
+                for (int i = lane; i < pieces; i += 32) *reinterpret_cast<uint4 *>(chunk + in_box * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -553,24 +628,26 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 else mbar_arrive_release_cluster(cluster_addr(bar_peer + 8 * slot, 0));
             }
             __syncwarp();
+            slot = (slot + 1) % kStages;
         }
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ epilogue
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        uint32_t n_acc = 0;
+        Ring16<2> acc;
         for (int tile = tile0; tile < tiles; tile += step) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
             const int in = 32 * quarter + lane;
-            const int chunks = EPI == EPI16_SUM ? (t.k_len + kSumStages * kK16 - 1) / (kSumStages * kK16) : t.k_len > 0;   // accumulators of the tile
+            const int chunks = EPI == EPI16_SUM ? (t.k_len + kSumElems - 1) / kSumElems : t.k_len > 0;   // accumulators of the tile
             const uint64_t acc_limit = limit * (uint64_t)(1 + (t.k_len >> 8));
-            const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
+            const uint32_t from = tmem + half * (BN / 2) + ((uint32_t)(32 * quarter) << 16);
             const int64_t row = (TILES == TILES_CUT ? (int64_t)t.batch * p.m : 0) + t.row + in;
+            const int col0 = t.col + half * (BN / 2);
             // The accumulator may be overwritten as soon as all warps have it in registers.
-            auto release = [&](uint32_t acc) {
+            auto release = [&]() {
                 tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) {
-                    const uint32_t bar = bar_acc_empty + 8 * acc;
+                    const uint32_t bar = bar_acc_empty + 8 * acc.slot;
                     if (CTAS == 2) mbar_arrive_release_cluster(cluster_addr(bar, 0));
                     else mbar_arrive(bar);
                 }
@@ -581,52 +658,55 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
 #pragma unroll
                 for (int e = 0; e < BN / 2; e++) sum[e] = 0.f;
                 bool ok = true;
-                for (int k = 0; k < chunks; k++, n_acc++) {
-                    const uint32_t acc = n_acc & 1u;
-                    if (!warp_wait(bar_acc_full + 8 * acc, (n_acc >> 1) & 1u, abort_flag, p.status, acc_limit, 0x600u)) { ok = false; break; }
+                for (int k = 0; k < chunks; k++, acc.next()) {
+                    if (!warp_wait(bar_acc_full + 8 * acc.slot, acc.phase, abort_flag, p.status, acc_limit, 0x600u)) { ok = false; break; }
                     tcgen05_fence_after();
 #pragma unroll
                     for (int c = 0; c < BN / 32; c++) {
                         uint32_t v[16];
-                        FP4Q_TMEM_LD_X16(tmem + acc * BN + half * (BN / 2) + 16 * c + lanes, v);
+                        FP4Q_TMEM_LD_X16(from + acc.slot * BN + 16 * c, v);
                         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
                         for (int e = 0; e < 16; e++) sum[16 * c + e] += __uint_as_float(v[e]);
                     }
-                    release(acc);
+                    release();
                 }
                 if (!ok) break;
                 if (in < t.rows && (chunks > 0 || !p.accumulate)) {
 #pragma unroll
-                    for (int c = 0; c < BN / 64; c++) store_f32(p, row, t.col + half * (BN / 2) + 32 * c, sum + 32 * c);
+                    for (int c = 0; c < BN / 64; c++) store_f32(p, row, col0 + 32 * c, sum + 32 * c);
                 }
                 __syncwarp();
                 continue;
             }
-            const uint32_t acc = n_acc & 1u;
+            // What a step's epilogue reads is fetched a round ahead, the first before the accumulator is there.
+            const int64_t at = (int64_t)t.batch * p.m * p.pitch + (int64_t)(t.row + in) * p.pitch + col0;
+            Fetched16 fetched[2];
+            if (in < t.rows) fetch16<EPI>(p, at, col0, fetched[0]);
             if (chunks > 0) {
-                if (!warp_wait(bar_acc_full + 8 * acc, (n_acc >> 1) & 1u, abort_flag, p.status, acc_limit, 0x600u)) break;
-                n_acc++;
+                if (!warp_wait(bar_acc_full + 8 * acc.slot, acc.phase, abort_flag, p.status, acc_limit, 0x600u)) break;
                 tcgen05_fence_after();
             }
-#pragma unroll 1
+#pragma unroll
             for (int c = 0; c < BN / 64; c++) {
-                const int col = half * (BN / 2) + 32 * c;
                 uint32_t v[32];
+                if (c + 1 < BN / 64 && in < t.rows) fetch16<EPI>(p, at + 32 * (c + 1), col0 + 32 * (c + 1), fetched[(c + 1) & 1]);
+                __syncwarp();
                 if (chunks > 0) {
-                    FP4Q_TMEM_LD_X32(tmem + acc * BN + col + lanes, v);
+                    FP4Q_TMEM_LD_X32(from + acc.slot * BN + 32 * c, v);
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                    if (c == BN / 64 - 1) release(acc);
+                    if (c == BN / 64 - 1) release();
                 } else {
 #pragma unroll
                     for (int e = 0; e < 32; e++) v[e] = 0u;
                 }
                 if (in < t.rows) {
-                    if (EPI == EPI16_STORE) store_bf16(p, row, t.col + col, reinterpret_cast<const float *>(v));
-                    else step16<EPI>(p, t, (int64_t)t.batch * p.m * p.pitch, t.row + in, t.col + col, reinterpret_cast<const float *>(v));
+                    if (EPI == EPI16_STORE) store_bf16(p, row, col0 + 32 * c, reinterpret_cast<const float *>(v));
+                    else step16<EPI>(p, t, (int64_t)t.batch * p.m * p.pitch, t.row + in, col0 + 32 * c, fetched[c & 1], reinterpret_cast<const float *>(v));
                 }
                 __syncwarp();
             }
+            if (chunks > 0) acc.next();
         }
     }
 
@@ -668,7 +748,7 @@ inline bool make_map16(CUtensorMap *map, const Operand16 &o, int box_rows)
 {
     const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.batch};
     const cuuint64_t strides[2] = {(cuuint64_t)o.pitch * 2, (cuuint64_t)o.stride * 2};
-    const cuuint32_t box[3] = {(cuuint32_t)kK16, (cuuint32_t)box_rows, 1u};
+    const cuuint32_t box[3] = {(cuuint32_t)kBox16, (cuuint32_t)box_rows, 1u};
     return encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void *>(o.base), dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
@@ -678,11 +758,11 @@ fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand1
 {
     using C = Cfg16<CTAS, BN>;
     CUtensorMap tmA, tmB, tmA2, tmB2;
-    if (!make_map16(&tmA, a, A_MN ? kK16 : p.a_box)) return FP4Q_ERR_CUDA;
-    if (!make_map16(&tmB, b, B_MN ? kK16 : C::kBRows)) return FP4Q_ERR_CUDA;
+    if (!make_map16(&tmA, a, A_MN ? kBox16 : p.a_box)) return FP4Q_ERR_CUDA;
+    if (!make_map16(&tmB, b, B_MN ? kBox16 : C::kBRows)) return FP4Q_ERR_CUDA;
     tmA2 = tmA;
     tmB2 = tmB;
-    if (p.split && (!make_map16(&tmA2, a2, A_MN ? kK16 : p.a_box) || !make_map16(&tmB2, b2, B_MN ? kK16 : C::kBRows))) return FP4Q_ERR_CUDA;
+    if (p.split && (!make_map16(&tmA2, a2, A_MN ? kBox16 : p.a_box) || !make_map16(&tmB2, b2, B_MN ? kBox16 : C::kBRows))) return FP4Q_ERR_CUDA;
     const int dev = current_device();
     if (dev < 0) return FP4Q_ERR_CUDA;
     constexpr int kSmem = C::smem(TILES);

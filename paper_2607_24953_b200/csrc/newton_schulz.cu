@@ -299,6 +299,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     p.a_box = 128;
     p.status = static_cast<uint32_t *>(ws);
     p.split = at.split;
+    p.admit = 1;
     const Parts part_a(half_at(at.a[0]), half_at(at.a[1]), side, side, count, at.pitch_a), part_p(half_at(at.poly[0]), half_at(at.poly[1]), side, side, count, at.pitch_a);
     // Pairs where their tiles fill the GPU; else smaller tiles.
     const bool pairs = count * ceil_div(side, 256) * (ceil_div(side, 256) + 1) / 2 >= 74;
@@ -333,6 +334,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
         up.out1 = half_at(at.lo[next]);
         up.pitch = at.pitch_x;
         if (i == steps - 1) {
+            up.admit = 0;
             up.o = static_cast<__nv_bfloat16 *>(out_bf16);
             up.ld_o = ld_o;
             up.o_scale = scale / kScaleX;
