@@ -388,7 +388,7 @@ fp4q_status fp4q_gemm_fwd_static_workspace(const fp4q_tensor *X, const fp4q_tens
  * Group g owns rows row_offsets[g] .. row_offsets[g+1]-1: here the offsets need not be multiples of anything (row_alignment 0 or 1 states
  * nothing; 128 and 256 are accepted and state nothing either), row_offsets[0] may be above 0 and row_offsets[n_groups] below T.  Groups may be
  * empty.  Rows that no group owns are not read, and not written either (but see FP4Q_OUT_ZERO_REST): what lies there stays there.  Offsets
- * outside 0..T are held to it, and one that is below an earlier one counts as that one.  n_groups <= 4095 (FP4Q_ERR_UNSUPPORTED); g == NULL:
+ * outside 0..T are held to it, and one that is below an earlier one counts as that one.  n_groups <= 2047 (FP4Q_ERR_UNSUPPORTED); g == NULL:
  * one group of all rows.  w is the expert stack [w_rows = n_groups*N, K]; dW is such a stack; an empty group's dW is zero (or unchanged
  * when accumulating).
  * Any T, N and K, 0 included.  Operands are 16-byte aligned with leading dimensions in multiples of 8 elements; outputs are BF16 or FP32

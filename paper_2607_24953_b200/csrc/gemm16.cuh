@@ -9,7 +9,9 @@
 //   warp 0      TMA producer: a stage is 64 contraction elements (single CTAs: 128), boxes of 128 bytes with the 128-byte swizzle
 //   warp 1      MMA issuer (in the leader of a pair): four tcgen05.mma of 16 contraction elements per box
 //   warp 2      cut contractions: zeroes the rows of a group's last stage that lie behind the group
-//   warps 4-11  epilogue: a thread has a row of the tile; the accumulator is double-buffered in tensor memory
+//   warps 4-11  epilogue: a thread has a row of the tile; the accumulator is double-buffered in tensor memory.  Outputs leave, and what an
+//               epilogue reads comes, as boxes of 32 rows x 128 bytes through shared memory (TMA): with plain accesses a warp's 16 bytes
+//               in each of 32 rows take the load/store unit 32 cycles, which made update products of 768 x 2048 epilogue-bound
 // Every wait is bounded: when a limit is hit the CTA records FP4Q_ERR_TIMEOUT in the workspace, its roles stop and it leaves through the
 // normal exit, after its copies in flight have landed.
 #pragma once
@@ -26,7 +28,7 @@ constexpr int kRows16 = 128;         // accumulator rows per CTA
 constexpr int kBox16 = 64;           // contraction elements of a box: 128 bytes
 constexpr int kThreads16 = 384;
 constexpr int kRaster16 = 16;        // row tiles per rasterisation group: their A rows stay in L2 while the columns go by
-constexpr int kMaxGroups16 = 4095;   // boundaries and first tiles of this many groups lie in shared memory
+constexpr int kMaxGroups16 = 2047;   // boundaries and first tiles of this many groups lie in shared memory
 
 // TILES_ROWS: groups of A rows (and of output rows), a matrix B per group.  TILES_CUT: a product per group, contracted over its rows.
 // TILES_BATCH: a stack of products.  TILES_SYM: a stack of symmetric products; only tiles on and below the diagonal are computed.
@@ -42,20 +44,19 @@ template <int CTAS, int BN>
 struct Cfg16 {
     static_assert(CTAS == 1 || (CTAS == 2 && BN == 256), "tile shapes");
     static constexpr int kBRows = BN / CTAS;
-    // A stage of a pair is one box deep: 512 cycles of MMAs.  The tiles of single CTAs take a quarter or half of that, less than a round of
-    // the issuer's (the wait for the next stage, a shared-memory access, queues behind the MMAs just issued: about 600 cycles, measured
-    // with one box), so their stages are two boxes deep.
-    static constexpr int kBoxes = CTAS == 2 ? 1 : 2;
+    // 128 x 64 tiles take 128 cycles of MMAs per box, less than a round of the issuer: their stages are two boxes deep.
+    static constexpr int kBoxes = BN == 64 ? 2 : 1;
     static constexpr int kK = kBoxes * kBox16;                              // contraction elements per stage
     static constexpr int kABox = kRows16 * 128, kBBox = kBRows * 128;
     static constexpr int kABytes = kBoxes * kABox, kBBytes = kBoxes * kBBox;
-    static constexpr int kStages = CTAS == 2 ? 6 : BN == 64 ? 4 : 3;
+    static constexpr int kStages = BN == 64 ? 3 : 5;
     static constexpr int kTmemCols = 2 * BN;
     static constexpr int kOperands = kStages * (kABytes + kBBytes);
     static constexpr int kTail = 512;                                       // barriers, tensor memory's address, abort flag
     static constexpr int kTables = 2 * (kMaxGroups16 + 1) * 4;              // row groups and cut contractions only
-    static constexpr int smem(int tiles) { return 1024 + kOperands + kTail + (tiles <= TILES_CUT ? kTables : 0); }
-    static_assert(1024 + kOperands + kTail + kTables <= 227 * 1024, "shared memory budget");
+    __host__ __device__ static constexpr int staging(int epi) { return epi == EPI16_STORE || epi == EPI16_SUM ? 4096 : 8192; }   // of an epilogue warp: one box, or an upper and a lower one
+    static constexpr int smem(int tiles, int epi) { return 1024 + kOperands + 8 * staging(epi) + kTail + (tiles <= TILES_CUT ? kTables : 0); }
+    static_assert(1024 + kOperands + 8 * 4096 + kTail + kTables <= 227 * 1024 && 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024, "shared memory budget");
 };
 
 struct Gemm16Params {
@@ -72,16 +73,19 @@ struct Gemm16Params {
     void *c;
     int64_t ldc;
     int32_t accumulate, wide, zero_rest;   // zero_rest: rows that no group owns are written as zeros
+    int32_t boxed;                   // columns that leave in boxes, whole 16 bytes; the rest of a row leaves by itself
     // EPI16_GRAM, _POLY, _UPDATE
     int32_t split;                   // operands are sums of two numbers: the products upper x upper, upper x lower and lower x upper are added up
     float fa, fb, fc;                // the step's coefficients, with the iterates' scales
-    const __half *in0, *in1;         // POLY: A, upper and (split) lower parts.  UPDATE: those of X
-    __half *out0, *out1;             // GRAM: A.  POLY: P.  UPDATE: the next X.  Lower parts of A and P if split
-    int64_t pitch;                   // of in0, in1, out0, out1
     __nv_bfloat16 *o;                // UPDATE, last step: the result instead
     int64_t ld_o;
     float o_scale;
-    int32_t o_vec;
+};
+
+// Operands and their lower parts; what an epilogue reads (POLY: A, UPDATE: X) and writes, upper and lower parts, in boxes of 32 rows x 128
+// bytes; the mirrored tiles of symmetric results, in boxes of 64 rows x 64 bytes.
+struct Maps16 {
+    CUtensorMap a, b, a2, b2, in, in2, out, out2, mirror, mirror2;
 };
 
 // A tile as one CTA of it sees it.
@@ -101,6 +105,24 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
 {
     asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(leader_bar) : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t src)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
+}
+__device__ __forceinline__ void tma_reduce_add_3d(const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t src)
+{
+    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
+}
+__device__ __forceinline__ void st_shared_16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared_16(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
 }
 // Arrival on a barrier of either CTA of a pair that orders this thread's writes, to shared memory or tensor memory, before what the waiter does.
 __device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_bar)
@@ -251,7 +273,6 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&b);
 }
 __device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
-__device__ __forceinline__ uint4 load_uint4(const void *p) { return *static_cast<const uint4 *>(p); }
 __device__ __forceinline__ void store_32_bytes(void *p, const uint32_t *w)
 {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
@@ -281,7 +302,7 @@ __device__ __forceinline__ void store_bf16(const Gemm16Params &p, int64_t row, i
             if (e < left) c[e] = __float2bfloat16_rn(v[e]);
     }
 }
-__device__ __forceinline__ void store_f32(const Gemm16Params &p, int64_t row, int col, float *v)
+__device__ __forceinline__ void store_f32(const Gemm16Params &p, int64_t row, int col, const float *v)
 {
     const int left = p.n - col;
     if (left <= 0) return;
@@ -289,7 +310,9 @@ __device__ __forceinline__ void store_f32(const Gemm16Params &p, int64_t row, in
     if (left >= 32) {
 #pragma unroll
         for (int e = 0; e < 32; e += 8) {
-            float *w = v + e;
+            float w[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) w[j] = v[e + j];
             if (p.accumulate) {
                 const float4 a = *reinterpret_cast<const float4 *>(c + e), b = *reinterpret_cast<const float4 *>(c + e + 4);
                 w[0] += a.x; w[1] += a.y; w[2] += a.z; w[3] += a.w; w[4] += b.x; w[5] += b.y; w[6] += b.z; w[7] += b.w;
@@ -307,115 +330,45 @@ __device__ __forceinline__ void store_f32(const Gemm16Params &p, int64_t row, in
     }
 }
 
-// What the epilogue of a step reads of 32 columns of a row: the upper and lower parts of A (POLY) or X (UPDATE).
-struct Fetched16 {
-    uint4 up[4], lo[4];
+// An epilogue warp's box in shared memory: 32 rows of 128 bytes, 16-byte pieces swizzled as TMA does.  A lane writes and reads its own row.
+struct Box16 {
+    uint32_t row, swizzle;
+    __device__ __forceinline__ Box16(uint32_t base, int lane) : row(base + lane * 128), swizzle((uint32_t)lane & 7u) {}
+    __device__ __forceinline__ uint32_t piece(int i) const { return row + (((uint32_t)i ^ swizzle) << 4); }
+    __device__ __forceinline__ void put(const uint32_t *w) const   // 32 words
+    {
+#pragma unroll
+        for (int i = 0; i < 8; i++) st_shared_16(piece(i), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
 };
-template <int EPI>
-__device__ __forceinline__ void fetch16(const Gemm16Params &p, int64_t at, int col, Fetched16 &f)
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// The warp's stores have read its boxes.
+__device__ __forceinline__ void boxes_free(int lane)
 {
-    if (EPI != EPI16_POLY && EPI != EPI16_UPDATE) return;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        f.lo[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (col + 8 * i >= p.pitch) continue;
-        f.up[i] = load_uint4(p.in0 + at + 8 * i);
-        if (EPI == EPI16_UPDATE || p.split) f.lo[i] = load_uint4(p.in1 + at + 8 * i);
-    }
-}
-
-// The iterates' rows are padded to whole 32 bytes: a piece of eight columns is written if it starts inside the row.  What columns behind
-// the matrix hold is never read.
-template <int EPI>
-__device__ __forceinline__ void step16(const Gemm16Params &p, const Tile16 &t, int64_t base, int row, int col, const Fetched16 &f, const float *v)
-{
-    const int64_t at = base + (int64_t)row * p.pitch + col;
-#pragma unroll
-    for (int e = 0; e < 32; e += 8) {
-        if (col + e >= p.pitch) continue;
-        float w[8];
-        if (EPI == EPI16_GRAM) {
-#pragma unroll
-            for (int j = 0; j < 8; j++) w[j] = v[e + j] * p.fa;
-        }
-        if (EPI == EPI16_POLY) {
-            const uint4 a = f.up[e / 8], b = f.lo[e / 8];
-            const uint32_t up[4] = {a.x, a.y, a.z, a.w}, lo[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const float2 x = unpack_half(up[j]), y = unpack_half(lo[j]);
-                w[2 * j] = fmaf(p.fb, x.x + y.x, p.fc * v[e + 2 * j]);
-                w[2 * j + 1] = fmaf(p.fb, x.y + y.y, p.fc * v[e + 2 * j + 1]);
-            }
-        }
-        if (EPI == EPI16_UPDATE) {
-            const uint4 a = f.up[e / 8], b = f.lo[e / 8];
-            const uint32_t up[4] = {a.x, a.y, a.z, a.w}, lo[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const float2 x = unpack_half(up[j]), y = unpack_half(lo[j]);
-                w[2 * j] = fmaf(p.fa, x.x + y.x, p.fb * v[e + 2 * j]);
-                w[2 * j + 1] = fmaf(p.fa, x.y + y.y, p.fb * v[e + 2 * j + 1]);
-            }
-            if (p.o) {
-                __nv_bfloat16 *o = p.o + ((int64_t)t.batch * p.m + row) * p.ld_o + col + e;
-                if (p.o_vec && col + e + 8 <= p.n) {
-                    *reinterpret_cast<uint4 *>(o) = make_uint4(pack_bf16(w[0] * p.o_scale, w[1] * p.o_scale), pack_bf16(w[2] * p.o_scale, w[3] * p.o_scale),
-                                                               pack_bf16(w[4] * p.o_scale, w[5] * p.o_scale), pack_bf16(w[6] * p.o_scale, w[7] * p.o_scale));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; j++)
-                        if (col + e + j < p.n) o[j] = __float2bfloat16_rn(w[j] * p.o_scale);
-                }
-                continue;
-            }
-        }
-        uint32_t h[4];
-#pragma unroll
-        for (int j = 0; j < 4; j++) h[j] = pack_half(w[2 * j], w[2 * j + 1]);
-        *reinterpret_cast<uint4 *>(p.out0 + at + e) = make_uint4(h[0], h[1], h[2], h[3]);
-        uint32_t l[4];
-        if (EPI == EPI16_UPDATE || p.split) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const float2 x = unpack_half(h[j]);
-                l[j] = pack_half(w[2 * j] - x.x, w[2 * j + 1] - x.y);
-            }
-            *reinterpret_cast<uint4 *>(p.out1 + at + e) = make_uint4(l[0], l[1], l[2], l[3]);
-        }
-        if (EPI != EPI16_UPDATE && t.mirror) {
-            const __half *s = reinterpret_cast<const __half *>(h), *r = reinterpret_cast<const __half *>(l);
-#pragma unroll
-            for (int j = 0; j < 8; j++) {
-                if (col + e + j >= p.n) continue;
-                const int64_t there = base + (int64_t)(col + e + j) * p.pitch + row;
-                p.out0[there] = s[j];
-                if (p.split) p.out1[there] = r[j];
-            }
-        }
-    }
+    if (lane == 0) bulk_wait_read_all();
+    __syncwarp();
 }
 
 // ---------------------------------------------------------------------------------------- kernel
 
 template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
-__global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmA2,
-                                                               const __grid_constant__ CUtensorMap tmB2, const Gemm16Params p)
+__global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_constant__ Maps16 maps, const Gemm16Params p)
 {
     using C = Cfg16<CTAS, BN>;
-    constexpr int kStages = C::kStages;
+    constexpr int kStages = C::kStages, kStaging = C::staging(EPI);
     constexpr bool kSplits = EPI == EPI16_GRAM || EPI == EPI16_POLY || EPI == EPI16_UPDATE;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t *smem_a = smem, *smem_b = smem + kStages * C::kABytes;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + C::kOperands);
+    uint8_t *smem_boxes = smem + C::kOperands;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem_boxes + 8 * kStaging);
     // bars[0..7] full, [8..15] empty, [16..17] accumulator full, [18..19] accumulator empty, [20..27] a group's last stage has landed here,
-    // [28..35] (leader of a pair) it is ready in the other CTA
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 36);
+    // [28..35] (leader of a pair) it is ready in the other CTA, [36..43] an epilogue warp's boxes have come
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 44);
     volatile uint32_t *abort_flag = tmem_slot + 1;
     int32_t *shared_tiles = reinterpret_cast<int32_t *>(tmem_slot + 2);
-    int32_t *start = reinterpret_cast<int32_t *>(smem + C::kOperands + C::kTail), *first = start + kMaxGroups16 + 1;
-    static_assert(kStages <= 8 && 36 * 8 + 16 <= C::kTail, "barriers");
+    int32_t *start = reinterpret_cast<int32_t *>(reinterpret_cast<uint8_t *>(bars) + C::kTail), *first = start + kMaxGroups16 + 1;
+    static_assert(kStages <= 8 && 44 * 8 + 16 <= C::kTail, "barriers");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t bar_full = smem_u32(bars), bar_empty = smem_u32(bars + 8), bar_acc_full = smem_u32(bars + 16), bar_acc_empty = smem_u32(bars + 18),
@@ -424,7 +377,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
 
     if (warp == 4) {
         mbar_init(smem_u32(bars + lane), lane >= 18 && lane < 20 ? 8 * CTAS : 1);
-        if (lane < 4) mbar_init(smem_u32(bars + 32 + lane), 1);
+        if (lane < 12) mbar_init(smem_u32(bars + 32 + lane), 1);
         if (lane == 0) *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     } else if (warp == 1) {
@@ -437,8 +390,8 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         }
         tcgen05_fence_before();
     } else if (warp == 0 && lane == 0) {
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmA) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmB) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b) : "memory");
     }
     __syncthreads();
     if (CTAS == 2) { cluster_arrive(); cluster_wait(); }
@@ -509,7 +462,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             // TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack
             const int az = TILES <= TILES_CUT ? 0 : t.batch, bz = TILES == TILES_CUT ? 0 : t.batch;
             for (int pass = 0; ok && pass < passes; pass++) {
-                const CUtensorMap *mapA = kSplits && pass == 2 ? &tmA2 : &tmA, *mapB = kSplits && pass == 1 ? &tmB2 : &tmB;
+                const CUtensorMap *mapA = kSplits && pass == 2 ? &maps.a2 : &maps.a, *mapB = kSplits && pass == 1 ? &maps.b2 : &maps.b;
                 for (int k = 0; k < t.k_len; k += C::kK, ring.next()) {
                     if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) { ok = false; break; }
                     issued++;
@@ -633,15 +586,20 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ epilogue
         const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t boxes = smem_u32(smem_boxes) + (warp - 4) * kStaging, bar_box = smem_u32(bars + 36 + warp - 4);
+        const Box16 up(boxes, lane), lo(boxes + 4096, lane);
+        constexpr int kCols = BN / 2, kChunk = EPI == EPI16_SUM || kCols < 64 ? 32 : 64;   // a warp's columns, and those of a box
         Ring16<2> acc;
+        uint32_t box_phase = 0;
         for (int tile = tile0; tile < tiles; tile += step) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
             const int in = 32 * quarter + lane;
             const int chunks = EPI == EPI16_SUM ? (t.k_len + kSumElems - 1) / kSumElems : t.k_len > 0;   // accumulators of the tile
             const uint64_t acc_limit = limit * (uint64_t)(1 + (t.k_len >> 8));
-            const uint32_t from = tmem + half * (BN / 2) + ((uint32_t)(32 * quarter) << 16);
+            const uint32_t from = tmem + half * kCols + ((uint32_t)(32 * quarter) << 16);
+            const int col0 = t.col + half * kCols, row0 = t.row + 32 * quarter, rows = t.rows - 32 * quarter;   // this warp's first column and row, its rows
+            const int batch = TILES == TILES_ROWS ? 0 : t.batch;
             const int64_t row = (TILES == TILES_CUT ? (int64_t)t.batch * p.m : 0) + t.row + in;
-            const int col0 = t.col + half * (BN / 2);
             // The accumulator may be overwritten as soon as all warps have it in registers.
             auto release = [&]() {
                 tcgen05_fence_before();
@@ -653,61 +611,181 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 }
                 __syncwarp();
             };
-            if (EPI == EPI16_SUM) {
-                float sum[BN / 2];
+            // A box leaves.  Rows of a group's last box, which shares its rows with the next group, and a row's last bytes leave by themselves.
+            auto send = [&](const uint32_t *w, const float *v, int col) {
+                if (col < p.boxed && rows >= (TILES == TILES_ROWS ? 32 : 1)) {
+                    boxes_free(lane);
+                    up.put(w);
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (EPI == EPI16_SUM && p.accumulate) tma_reduce_add_3d(&maps.out, col, row0, batch, boxes);
+                        else tma_store_3d(&maps.out, col, row0, batch, boxes);
+                        bulk_commit();
+                    }
+                    if (col + kChunk > p.boxed && lane < rows) {
 #pragma unroll
-                for (int e = 0; e < BN / 2; e++) sum[e] = 0.f;
+                        for (int e = 0; e < kChunk; e++) {
+                            if (col + e < p.boxed || col + e >= p.n) continue;
+                            if (EPI == EPI16_SUM) {
+                                float *c = static_cast<float *>(p.c) + row * p.ldc + col + e;
+                                *c = p.accumulate ? *c + v[e] : v[e];
+                            } else static_cast<__nv_bfloat16 *>(p.c)[row * p.ldc + col + e] = __float2bfloat16_rn(v[e]);
+                        }
+                    }
+                } else if (lane < rows) {
+#pragma unroll
+                    for (int e = 0; e < kChunk; e += 32) {
+                        if (EPI == EPI16_SUM) store_f32(p, row, col + e, v + e);
+                        else store_bf16(p, row, col + e, v + e);
+                    }
+                }
+                __syncwarp();
+            };
+            if (EPI == EPI16_SUM) {
+                float sum[kCols];
+#pragma unroll
+                for (int e = 0; e < kCols; e++) sum[e] = 0.f;
                 bool ok = true;
                 for (int k = 0; k < chunks; k++, acc.next()) {
                     if (!warp_wait(bar_acc_full + 8 * acc.slot, acc.phase, abort_flag, p.status, acc_limit, 0x600u)) { ok = false; break; }
                     tcgen05_fence_after();
 #pragma unroll
-                    for (int c = 0; c < BN / 32; c++) {
+                    for (int c = 0; c < kCols; c += 16) {
                         uint32_t v[16];
-                        FP4Q_TMEM_LD_X16(from + acc.slot * BN + 16 * c, v);
+                        FP4Q_TMEM_LD_X16(from + acc.slot * BN + c, v);
                         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-                        for (int e = 0; e < 16; e++) sum[16 * c + e] += __uint_as_float(v[e]);
+                        for (int e = 0; e < 16; e++) sum[c + e] += __uint_as_float(v[e]);
                     }
                     release();
                 }
                 if (!ok) break;
-                if (in < t.rows && (chunks > 0 || !p.accumulate)) {
+                if (chunks > 0 || !p.accumulate) {
 #pragma unroll
-                    for (int c = 0; c < BN / 64; c++) store_f32(p, row, col0 + 32 * c, sum + 32 * c);
+                    for (int c = 0; c < kCols; c += kChunk) send(reinterpret_cast<const uint32_t *>(sum) + c, sum + c, col0 + c);
                 }
-                __syncwarp();
                 continue;
             }
-            // What a step's epilogue reads is fetched a round ahead, the first before the accumulator is there.
-            const int64_t at = (int64_t)t.batch * p.m * p.pitch + (int64_t)(t.row + in) * p.pitch + col0;
-            Fetched16 fetched[2];
-            if (in < t.rows) fetch16<EPI>(p, at, col0, fetched[0]);
+            // What a step's epilogue reads is fetched before it waits for the accumulator, and for a later chunk when the one before has left.
+            constexpr bool kReads = EPI == EPI16_POLY || EPI == EPI16_UPDATE;
+            const bool two = EPI == EPI16_UPDATE || p.split != 0;      // upper and lower parts
+            auto fetch = [&](int col) {
+                if (!kReads || rows <= 0 || col >= p.n) return;
+                boxes_free(lane);
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(bar_box, two ? 8192u : 4096u);
+                    tma_load_3d(boxes, &maps.in, col, row0, batch, bar_box);
+                    if (two) tma_load_3d(boxes + 4096, &maps.in2, col, row0, batch, bar_box);
+                }
+            };
+            fetch(col0);
             if (chunks > 0) {
                 if (!warp_wait(bar_acc_full + 8 * acc.slot, acc.phase, abort_flag, p.status, acc_limit, 0x600u)) break;
                 tcgen05_fence_after();
             }
-#pragma unroll
-            for (int c = 0; c < BN / 64; c++) {
-                uint32_t v[32];
-                if (c + 1 < BN / 64 && in < t.rows) fetch16<EPI>(p, at + 32 * (c + 1), col0 + 32 * (c + 1), fetched[(c + 1) & 1]);
-                __syncwarp();
+            bool ok = true;
+#pragma unroll 1
+            for (int c = 0; c < kCols; c += kChunk) {
+                uint32_t v[kChunk];
+                const int col = col0 + c;
                 if (chunks > 0) {
-                    FP4Q_TMEM_LD_X32(from + acc.slot * BN + 32 * c, v);
+#pragma unroll
+                    for (int e = 0; e < kChunk; e += 32) FP4Q_TMEM_LD_X32(from + acc.slot * BN + c + e, (v + e));
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                    if (c == BN / 64 - 1) release();
+                    if (c == kCols - kChunk) release();
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 32; e++) v[e] = 0u;
+                    for (int e = 0; e < kChunk; e++) v[e] = 0u;
                 }
-                if (in < t.rows) {
-                    if (EPI == EPI16_STORE) store_bf16(p, row, col0 + 32 * c, reinterpret_cast<const float *>(v));
-                    else step16<EPI>(p, t, (int64_t)t.batch * p.m * p.pitch, t.row + in, col0 + 32 * c, fetched[c & 1], reinterpret_cast<const float *>(v));
+                const float *x = reinterpret_cast<const float *>(v);
+                if (EPI == EPI16_STORE) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int e = 0; e < kChunk / 2; e++) w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
+                    if (kChunk == 64) send(w, x, col);
+                    else if (lane < rows) store_bf16(p, row, col, x);   // half a box
+                    __syncwarp();
+                    continue;
                 }
+                if (rows <= 0 || col >= p.n) continue;
+                if (kReads) {
+                    if (!warp_wait(bar_box, box_phase, abort_flag, p.status, limit, 0x800u)) { ok = false; break; }
+                    box_phase ^= 1u;
+                }
+                // The new values, upper and lower parts, replace those that were read, a piece of eight columns at a time.
+                const bool out = EPI == EPI16_UPDATE && p.o;
+                if (!kReads) boxes_free(lane);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    float w[8];
+                    const uint4 a = kReads ? ld_shared_16(up.piece(i)) : make_uint4(0u, 0u, 0u, 0u), b = kReads && two ? ld_shared_16(lo.piece(i)) : make_uint4(0u, 0u, 0u, 0u);
+                    const uint32_t au[4] = {a.x, a.y, a.z, a.w}, bu[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int j = 0; j < 4; j++) {
+                        const float2 y = unpack_half(au[j]), z = unpack_half(bu[j]);
+                        const float v0 = x[8 * i + 2 * j], v1 = x[8 * i + 2 * j + 1];
+                        w[2 * j] = EPI == EPI16_GRAM ? v0 * p.fa : fmaf(p.fb, y.x + z.x, p.fc * v0);
+                        w[2 * j + 1] = EPI == EPI16_GRAM ? v1 * p.fa : fmaf(p.fb, y.y + z.y, p.fc * v1);
+                    }
+                    uint32_t h[4], l[4];
+                    if (out) {
+#pragma unroll
+                        for (int j = 0; j < 4; j++) h[j] = pack_bf16(w[2 * j] * p.o_scale, w[2 * j + 1] * p.o_scale);
+                        if (col + 8 * i + 8 > p.boxed && lane < rows) {
+                            __nv_bfloat16 *o = p.o + ((int64_t)t.batch * p.m + t.row + in) * p.ld_o + col + 8 * i;
+#pragma unroll
+                            for (int j = 0; j < 8; j++)
+                                if (col + 8 * i + j < p.n) o[j] = __float2bfloat16_rn(w[j] * p.o_scale);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            h[j] = pack_half(w[2 * j], w[2 * j + 1]);
+                            const float2 y = unpack_half(h[j]);
+                            l[j] = pack_half(w[2 * j] - y.x, w[2 * j + 1] - y.y);
+                        }
+                        if (two) st_shared_16(lo.piece(i), l[0], l[1], l[2], l[3]);
+                    }
+                    st_shared_16(up.piece(i), h[0], h[1], h[2], h[3]);
+                }
+                fence_async_shared();
                 __syncwarp();
+                if (lane == 0 && !(out && col >= p.boxed)) {
+                    tma_store_3d(&maps.out, col, row0, batch, boxes);
+                    if (two && !out) tma_store_3d(&maps.out2, col, row0, batch, boxes + 4096);
+                    bulk_commit();
+                }
+                if (EPI != EPI16_UPDATE && t.mirror) {
+                    // The transposed box, 64 rows of 64 bytes, in place of the box itself once that has left: a column is read from all rows.
+                    uint32_t keep_up[32], keep_lo[32];
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const uint4 a = ld_shared_16(up.piece(i)), b = two ? ld_shared_16(lo.piece(i)) : make_uint4(0u, 0u, 0u, 0u);
+                        keep_up[4 * i] = a.x; keep_up[4 * i + 1] = a.y; keep_up[4 * i + 2] = a.z; keep_up[4 * i + 3] = a.w;
+                        keep_lo[4 * i] = b.x; keep_lo[4 * i + 1] = b.y; keep_lo[4 * i + 2] = b.z; keep_lo[4 * i + 3] = b.w;
+                    }
+                    boxes_free(lane);
+#pragma unroll
+                    for (int e = 0; e < 64; e++) {
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(boxes + e * 64 + lane * 2), "h"((uint16_t)(keep_up[e / 2] >> (16 * (e & 1)))) : "memory");
+                        if (two) asm volatile("st.shared.u16 [%0], %1;" ::"r"(boxes + 4096 + e * 64 + lane * 2), "h"((uint16_t)(keep_lo[e / 2] >> (16 * (e & 1)))) : "memory");
+                    }
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_3d(&maps.mirror, row0, col, batch, boxes);
+                        if (two) tma_store_3d(&maps.mirror2, row0, col, batch, boxes + 4096);
+                        bulk_commit();
+                    }
+                }
+                if (c + kChunk < kCols) fetch(col + kChunk);
             }
+            if (!ok) break;
             if (chunks > 0) acc.next();
         }
+        // The stores have read shared memory; what they write is there when the grid has completed.
+        boxes_free(lane);
     }
 
     if (TILES == TILES_ROWS && p.zero_rest && warp >= 4) {
@@ -738,34 +816,33 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
 
 // ---------------------------------------------------------------------------------------- host side
 
-// What a launch reads of an operand: a stack of `batch` matrices [rows, cols] of 16-bit elements, `pitch` elements from row to row and `stride`
-// from matrix to matrix.
+// A stack of `batch` matrices [rows, cols], `pitch` elements from row to row and `stride` from matrix to matrix.
 struct Operand16 {
     const void *base;
     int64_t cols, rows, batch, pitch, stride;
 };
-inline bool make_map16(CUtensorMap *map, const Operand16 &o, int box_rows)
+inline bool make_map16(CUtensorMap *map, const Operand16 &o, int box_cols, int box_rows, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B, bool f32 = false)
 {
     const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.batch};
-    const cuuint64_t strides[2] = {(cuuint64_t)o.pitch * 2, (cuuint64_t)o.stride * 2};
-    const cuuint32_t box[3] = {(cuuint32_t)kBox16, (cuuint32_t)box_rows, 1u};
-    return encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void *>(o.base), dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+    const cuuint64_t strides[2] = {(cuuint64_t)o.pitch * (f32 ? 4 : 2), (cuuint64_t)o.stride * (f32 ? 4 : 2)};
+    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1u};
+    return encode_tiled(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void *>(o.base), dims, strides, box, swizzle,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
-// a2, b2: the operands' lower parts (p.split).  most_tiles: no fewer than the tiles there can be.
+// maps: what lies beside the operands is the caller's.  a2, b2: the operands' lower parts (p.split).  most_tiles: no fewer than the tiles
+// there can be.
 template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
-fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand16 &a2, const Operand16 &b2, const Gemm16Params &p, int64_t most_tiles, cudaStream_t stream)
+fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand16 &a2, const Operand16 &b2, Maps16 &maps, const Gemm16Params &p, int64_t most_tiles,
+                          cudaStream_t stream)
 {
     using C = Cfg16<CTAS, BN>;
-    CUtensorMap tmA, tmB, tmA2, tmB2;
-    if (!make_map16(&tmA, a, A_MN ? kBox16 : p.a_box)) return FP4Q_ERR_CUDA;
-    if (!make_map16(&tmB, b, B_MN ? kBox16 : C::kBRows)) return FP4Q_ERR_CUDA;
-    tmA2 = tmA;
-    tmB2 = tmB;
-    if (p.split && (!make_map16(&tmA2, a2, A_MN ? kBox16 : p.a_box) || !make_map16(&tmB2, b2, B_MN ? kBox16 : C::kBRows))) return FP4Q_ERR_CUDA;
+    const int a_rows = A_MN ? kBox16 : p.a_box, b_rows = B_MN ? kBox16 : C::kBRows;
+    if (!make_map16(&maps.a, a, kBox16, a_rows) || !make_map16(&maps.b, b, kBox16, b_rows)) return FP4Q_ERR_CUDA;
+    if (p.split && (!make_map16(&maps.a2, a2, kBox16, a_rows) || !make_map16(&maps.b2, b2, kBox16, b_rows))) return FP4Q_ERR_CUDA;
     const int dev = current_device();
     if (dev < 0) return FP4Q_ERR_CUDA;
-    constexpr int kSmem = C::smem(TILES);
+    constexpr int kSmem = C::smem(TILES, EPI);
     static std::atomic<bool> attr_set[kMaxDevices];   // the attribute is a property of (kernel, device)
     if (!attr_set[dev].load(std::memory_order_relaxed)) {
         if (cudaFuncSetAttribute(gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
@@ -792,7 +869,7 @@ fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand1
         attr[1].val.clusterDim.z = 1;
         cfg.numAttrs = 2;
     }
-    return launched(cudaLaunchKernelEx(&cfg, gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES>, tmA, tmB, tmA2, tmB2, p));
+    return launched(cudaLaunchKernelEx(&cfg, gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES>, maps, p));
 }
 
 }  // namespace fp4q

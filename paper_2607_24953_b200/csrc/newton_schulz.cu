@@ -223,29 +223,55 @@ struct Parts {
         : up{u, cols, rows, count, pitch, rows * pitch}, lo{l, cols, rows, count, pitch, rows * pitch} {}
 };
 
+// Boxes of an epilogue: what it reads or writes, and mirrored.
+fp4q_status boxes16(CUtensorMap *up, CUtensorMap *lo, const Parts &x, bool two, bool mirrored = false)
+{
+    const int cols = mirrored ? 32 : 64, rows = mirrored ? 64 : 32;
+    const CUtensorMapSwizzle swizzle = mirrored ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B;
+    return make_map16(up, x.up, cols, rows, swizzle) && (!two || make_map16(lo, x.lo, cols, rows, swizzle)) ? FP4Q_OK : FP4Q_ERR_CUDA;
+}
+
 template <int CTAS, int BN>
 struct Steps {
     static constexpr int kBM = kRows16 * CTAS;
-    static fp4q_status gram(const Parts &x, bool tall, Gemm16Params p, cudaStream_t stream)
+    static int64_t symmetric_tiles(Gemm16Params &p)
     {
         static_assert(kBM == BN, "symmetric products have square tiles");
         p.m_tiles = p.n_tiles = (int32_t)ceil_div(p.n, BN);
-        const int64_t tiles = (int64_t)p.batch * p.m_tiles * (p.m_tiles + 1) / 2;
-        return tall ? launch_gemm16<CTAS, BN, true, true, EPI16_GRAM, TILES_SYM>(x.up, x.up, x.lo, x.lo, p, tiles, stream)
-                    : launch_gemm16<CTAS, BN, false, false, EPI16_GRAM, TILES_SYM>(x.up, x.up, x.lo, x.lo, p, tiles, stream);
+        return (int64_t)p.batch * p.m_tiles * (p.m_tiles + 1) / 2;
     }
-    static fp4q_status poly(const Parts &a, Gemm16Params p, cudaStream_t stream)
+    static fp4q_status gram(const Parts &x, const Parts &a, bool tall, Gemm16Params p, cudaStream_t stream)
     {
-        p.m_tiles = p.n_tiles = (int32_t)ceil_div(p.n, BN);
-        return launch_gemm16<CTAS, BN, false, false, EPI16_POLY, TILES_SYM>(a.up, a.up, a.lo, a.lo, p, (int64_t)p.batch * p.m_tiles * (p.m_tiles + 1) / 2, stream);
+        Maps16 maps = {};
+        const int64_t tiles = symmetric_tiles(p);
+        if (fp4q_status s = boxes16(&maps.out, &maps.out2, a, p.split)) return s;
+        if (fp4q_status s = boxes16(&maps.mirror, &maps.mirror2, a, p.split, true)) return s;
+        return tall ? launch_gemm16<CTAS, BN, true, true, EPI16_GRAM, TILES_SYM>(x.up, x.up, x.lo, x.lo, maps, p, tiles, stream)
+                    : launch_gemm16<CTAS, BN, false, false, EPI16_GRAM, TILES_SYM>(x.up, x.up, x.lo, x.lo, maps, p, tiles, stream);
     }
-    static fp4q_status update(const Parts &x, const Parts &poly, bool tall, Gemm16Params p, cudaStream_t stream)
+    static fp4q_status poly(const Parts &a, const Parts &poly, Gemm16Params p, cudaStream_t stream)
     {
+        Maps16 maps = {};
+        const int64_t tiles = symmetric_tiles(p);
+        if (fp4q_status s = boxes16(&maps.in, &maps.in2, a, p.split)) return s;
+        if (fp4q_status s = boxes16(&maps.out, &maps.out2, poly, p.split)) return s;
+        if (fp4q_status s = boxes16(&maps.mirror, &maps.mirror2, poly, p.split, true)) return s;
+        return launch_gemm16<CTAS, BN, false, false, EPI16_POLY, TILES_SYM>(a.up, a.up, a.lo, a.lo, maps, p, tiles, stream);
+    }
+    static fp4q_status update(const Parts &x, const Parts &poly, const Parts &next, bool tall, Gemm16Params p, cudaStream_t stream)
+    {
+        Maps16 maps = {};
         p.m_tiles = (int32_t)ceil_div(p.m, kBM);
         p.n_tiles = (int32_t)ceil_div(p.n, BN);
         const int64_t tiles = (int64_t)p.batch * p.m_tiles * p.n_tiles;
-        return tall ? launch_gemm16<CTAS, BN, false, false, EPI16_UPDATE, TILES_BATCH>(x.up, poly.up, x.lo, poly.lo, p, tiles, stream)
-                    : launch_gemm16<CTAS, BN, false, true, EPI16_UPDATE, TILES_BATCH>(poly.up, x.up, poly.lo, x.lo, p, tiles, stream);
+        if (fp4q_status s = boxes16(&maps.in, &maps.in2, x, true)) return s;
+        if (p.o) {
+            if (p.boxed > 0 && !make_map16(&maps.out, Operand16{p.o, p.boxed, p.m, p.batch, p.ld_o, p.m * p.ld_o}, 64, 32)) return FP4Q_ERR_CUDA;
+        } else if (fp4q_status s = boxes16(&maps.out, &maps.out2, next, true)) {
+            return s;
+        }
+        return tall ? launch_gemm16<CTAS, BN, false, false, EPI16_UPDATE, TILES_BATCH>(x.up, poly.up, x.lo, poly.lo, maps, p, tiles, stream)
+                    : launch_gemm16<CTAS, BN, false, true, EPI16_UPDATE, TILES_BATCH>(poly.up, x.up, poly.lo, x.lo, maps, p, tiles, stream);
     }
 };
 
@@ -301,48 +327,36 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     p.split = at.split;
     p.admit = 1;
     const Parts part_a(half_at(at.a[0]), half_at(at.a[1]), side, side, count, at.pitch_a), part_p(half_at(at.poly[0]), half_at(at.poly[1]), side, side, count, at.pitch_a);
-    // Pairs where their tiles fill the GPU; else smaller tiles.
-    const bool pairs = count * ceil_div(side, 256) * (ceil_div(side, 256) + 1) / 2 >= 74;
+    const bool pairs = side > 128;
     for (int32_t i = 0; i < steps; i++) {
         const float *c = coefficients + 3 * i;
         const int now = i & 1, next = now ^ 1;
         const Parts part_x(half_at(at.x[now]), half_at(at.lo[now]), cols, rows, count, at.pitch_x);
+        const Parts part_next(half_at(at.x[next]), half_at(at.lo[next]), cols, rows, count, at.pitch_x);
         Gemm16Params gp = p;
         gp.m = gp.n = (int32_t)side;
         gp.k = (int32_t)(tall ? rows : cols);
         gp.fa = kScaleA / (kScaleX * kScaleX);
-        gp.out0 = half_at(at.a[0]);
-        gp.out1 = half_at(at.a[1]);
-        gp.pitch = at.pitch_a;
         Gemm16Params pp = gp;
         pp.k = (int32_t)side;
-        pp.in0 = half_at(at.a[0]);
-        pp.in1 = half_at(at.a[1]);
-        pp.out0 = half_at(at.poly[0]);
-        pp.out1 = half_at(at.poly[1]);
         pp.fb = c[1];
         pp.fc = c[2] / kScaleA;
         Gemm16Params up = p;
         up.m = (int32_t)rows;
         up.n = (int32_t)cols;
         up.k = (int32_t)side;
-        up.fa = c[0];
-        up.fb = 1.0f / kScaleA;
-        up.in0 = half_at(at.x[now]);
-        up.in1 = half_at(at.lo[now]);
-        up.out0 = half_at(at.x[next]);
-        up.out1 = half_at(at.lo[next]);
-        up.pitch = at.pitch_x;
+        up.fb = c[0];
+        up.fc = 1.0f / kScaleA;
         if (i == steps - 1) {
             up.admit = 0;
             up.o = static_cast<__nv_bfloat16 *>(out_bf16);
             up.ld_o = ld_o;
             up.o_scale = scale / kScaleX;
-            up.o_vec = aligned(out_bf16, 16) && ld_o % 8 == 0;
+            up.boxed = aligned(out_bf16, 16) && ld_o % 8 == 0 ? (int32_t)(cols / 8 * 8) : 0;
         }
-        fp4q_status st = pairs ? Steps<2, 256>::gram(part_x, tall, gp, s) : Steps<1, 128>::gram(part_x, tall, gp, s);
-        if (!st) st = pairs ? Steps<2, 256>::poly(part_a, pp, s) : Steps<1, 128>::poly(part_a, pp, s);
-        if (!st) st = pairs ? Steps<2, 256>::update(part_x, part_p, tall, up, s) : Steps<1, 128>::update(part_x, part_p, tall, up, s);
+        fp4q_status st = pairs ? Steps<2, 256>::gram(part_x, part_a, tall, gp, s) : Steps<1, 128>::gram(part_x, part_a, tall, gp, s);
+        if (!st) st = pairs ? Steps<2, 256>::poly(part_a, part_p, pp, s) : Steps<1, 128>::poly(part_a, part_p, pp, s);
+        if (!st) st = pairs ? Steps<2, 256>::update(part_x, part_p, part_next, tall, up, s) : Steps<1, 128>::update(part_x, part_p, part_next, tall, up, s);
         if (st) return st;
     }
     return FP4Q_OK;

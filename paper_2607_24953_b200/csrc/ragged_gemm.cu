@@ -60,10 +60,15 @@ fp4q_status check_workspace(const void *ws, size_t ws_bytes)
 Operand16 operand16(const Matrix16 &m, int64_t rows, int64_t batch) { return Operand16{m.p, m.cols, rows, batch, m.ld, rows * m.ld}; }
 
 template <int CTAS, int BN, bool A_MN, bool B_MN, int TILES>
-fp4q_status launch_store16(const Operand16 &a, const Operand16 &b, const Gemm16Params &p, fp4q_out dt, int64_t most_tiles, cudaStream_t stream)
+fp4q_status launch_store16(const Operand16 &a, const Operand16 &b, Gemm16Params &p, fp4q_out dt, int64_t most_tiles, cudaStream_t stream)
 {
-    return out_f32(dt) ? launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_SUM, TILES>(a, b, a, b, p, most_tiles, stream)
-                       : launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_STORE, TILES>(a, b, a, b, p, most_tiles, stream);
+    Maps16 maps = {};
+    const bool f32 = out_f32(dt);
+    p.boxed = p.n / (f32 ? 4 : 8) * (f32 ? 4 : 8);   // a store of a box fills the 16 bytes in which a row ends
+    const int64_t groups = TILES == TILES_CUT ? p.batch : 1;
+    if (p.boxed > 0 && !make_map16(&maps.out, Operand16{p.c, p.boxed, p.m, groups, p.ldc, p.m * p.ldc}, f32 ? 32 : 64, 32, CU_TENSOR_MAP_SWIZZLE_128B, f32)) return FP4Q_ERR_CUDA;
+    return f32 ? launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_SUM, TILES>(a, b, a, b, maps, p, most_tiles, stream)
+               : launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_STORE, TILES>(a, b, a, b, maps, p, most_tiles, stream);
 }
 
 // Rows of groups, T in all.

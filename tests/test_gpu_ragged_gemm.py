@@ -206,7 +206,7 @@ def test_offsets_that_are_no_boundaries_touch_nothing_else(values):
 
 
 def test_many_groups():
-    e, T = 4095, 5000
+    e, T = 2047, 5000
     values = [0] + sorted(np.random.RandomState(1).randint(0, T + 1, e - 1).tolist()) + [T]
     x, w = operands("fwd", T, 16, 32, e)
     y, s = reference("fwd", x, w, groups(values, T))

@@ -31,7 +31,7 @@ def test_products():
         assert f(T=-1) == 2 and f(K=-1) == 2
         assert f(ldx=32) == 2 and f(ldw=16) == 2
         assert f(dt=2) == 4 and f(dt=0x400) == 4
-        assert f(g=groups(0)) == 2 and f(g=groups(-3)) == 2 and f(g=groups(4096)) == 4
+        assert f(g=groups(0)) == 2 and f(g=groups(-3)) == 2 and f(g=groups(2048)) == 4
         assert f(g=groups(alignment=64)) == 4 and f(g=groups(offsets=None)) == 1
         assert f(ws=None) == 5 and f(wsb=100) == 5 and f(ws=P + 16) == 3
         assert f(x=None) == 1 and f(x=P + 8) == 3
