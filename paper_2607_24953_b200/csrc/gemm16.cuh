@@ -4,8 +4,10 @@
 // newton_schulz.cu.
 //
 // Persistent kernel, one CTA per SM, 12 warps.  A CTA has 128 rows of the accumulator; pairs (cta_group::2) share a tile of 256 rows and
-// each loads half of B's columns, which is what lets 32 KB of operands feed 2 x 256 x 256 x 64 operations per stage; single CTAs have tiles of
-// 128 x 128 or 128 x 64 for problems with few tiles or short groups.
+// each loads half of B's columns, which is what lets 32 KB of operands feed 2 x 256 x 256 x 64 operations per stage (an SM gets 32 KB from L2
+// in about 0.3 us, as long as the MMAs take at the clock that full load leaves); single CTAs have tiles of 128 x 128 for problems with few
+// tiles, and of 32 x 64 for short groups (the MMAs have 128 rows all the same: those behind the first 32 are whatever lies in shared
+// memory, and nobody looks at them).
 //   warp 0      TMA producer: a stage is 64 contraction elements (single CTAs: 128), boxes of 128 bytes with the 128-byte swizzle
 //   warp 1      MMA issuer (in the leader of a pair): four tcgen05.mma of 16 contraction elements per box
 //   warp 2      cut contractions: zeroes the rows of a group's last stage that lie behind the group
@@ -44,19 +46,20 @@ template <int CTAS, int BN>
 struct Cfg16 {
     static_assert(CTAS == 1 || (CTAS == 2 && BN == 256), "tile shapes");
     static constexpr int kBRows = BN / CTAS;
-    // 128 x 64 tiles take 128 cycles of MMAs per box, less than a round of the issuer: their stages are two boxes deep.
+    // 32 x 64 tiles take 128 cycles of MMAs per box, less than a round of the issuer: their stages are two boxes deep.
     static constexpr int kBoxes = BN == 64 ? 2 : 1;
     static constexpr int kK = kBoxes * kBox16;                              // contraction elements per stage
-    static constexpr int kABox = kRows16 * 128, kBBox = kBRows * 128;
+    static constexpr int kRows = BN == 64 ? 32 : kRows16;                   // rows of a CTA's part of a tile
+    static constexpr int kABox = kRows * 128, kBBox = kBRows * 128;
     static constexpr int kABytes = kBoxes * kABox, kBBytes = kBoxes * kBBox;
-    static constexpr int kStages = BN == 64 ? 3 : 5;
+    static constexpr int kStages = BN == 64 ? 7 : 5;
     static constexpr int kTmemCols = 2 * BN;
     static constexpr int kOperands = kStages * (kABytes + kBBytes);
     static constexpr int kTail = 512;                                       // barriers, tensor memory's address, abort flag
     static constexpr int kTables = 2 * (kMaxGroups16 + 1) * 4;              // row groups and cut contractions only
     __host__ __device__ static constexpr int staging(int epi) { return epi == EPI16_STORE || epi == EPI16_SUM ? 4096 : 8192; }   // of an epilogue warp: one box, or an upper and a lower one
     static constexpr int smem(int tiles, int epi) { return 1024 + kOperands + 8 * staging(epi) + kTail + (tiles <= TILES_CUT ? kTables : 0); }
-    static_assert(1024 + kOperands + 8 * 4096 + kTail + kTables <= 227 * 1024 && 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024, "shared memory budget");
+    static_assert(1024 + kOperands + 8 * 4096 + kTail + kTables <= 227 * 1024 && (BN == 64 || 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024), "shared memory budget");
 };
 
 struct Gemm16Params {
@@ -64,7 +67,7 @@ struct Gemm16Params {
     int32_t m_tiles, n_tiles;        // TILES_ROWS: m_tiles is found on the device
     int32_t batch;                   // groups or matrices
     int32_t bf16;                    // operand type: 0 = FP16, 1 = BF16
-    int32_t a_box;                   // rows of one copy of a K-major A operand: 128, or 32 for short groups
+    int32_t a_box;                   // rows of one copy of a K-major A operand: 128; 32 or 16 in tiles of 32 rows
     const int64_t *offsets;          // TILES_ROWS, TILES_CUT: batch + 1 boundaries; NULL: one group of all rows
     int64_t total_rows;              // rows that the boundaries are held to
     uint32_t *status;
@@ -213,7 +216,7 @@ __device__ __forceinline__ int find_group16(const int32_t *first, int n, int til
 template <int TILES, int CTAS, int BN>
 __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int m_tiles, const int32_t *start, const int32_t *first, int rank)
 {
-    constexpr int kBM = kRows16 * CTAS, kBRows = Cfg16<CTAS, BN>::kBRows;
+    constexpr int kRows = Cfg16<CTAS, BN>::kRows, kBM = kRows * CTAS, kBRows = Cfg16<CTAS, BN>::kBRows;
     Tile16 t;
     int mt, nt;
     t.batch = 0;
@@ -253,10 +256,10 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
         valid = p.m - t.row;
     }
     if (TILES == TILES_CUT) { t.k0 = start[t.batch]; t.k_len = group_rows(start, t.batch); }
-    t.row += rank * kRows16;
+    t.row += rank * kRows;
     t.a_row = t.row;
-    t.rows = max(0, min(kRows16, valid - rank * kRows16));
-    t.rows_peer = CTAS == 2 ? max(0, min(kRows16, valid - (1 - rank) * kRows16)) : 0;
+    t.rows = max(0, min(kRows, valid - rank * kRows));
+    t.rows_peer = CTAS == 2 ? max(0, min(kRows, valid - (1 - rank) * kRows)) : 0;
     return t;
 }
 
@@ -420,7 +423,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             for (int g = g0; g < g1; g++) start[g] = before = max(before, start[g]);   // boundaries that fall are lifted
             __syncwarp();
             if (TILES == TILES_ROWS) {   // row tiles of all groups before a group's
-                constexpr int kBM = kRows16 * CTAS;
+                constexpr int kBM = C::kRows * CTAS;
                 const int last = min(g1, p.batch);
                 int sum = 0;
                 for (int g = g0; g < last; g++) sum += (group_rows(start, g) + kBM - 1) / kBM;
@@ -510,7 +513,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         const uint32_t idesc = instr_desc16<CTAS, BN>(p.bf16 != 0, A_MN, B_MN);
         Ring16<kStages> ring;
         Ring16<2> acc;      // accumulators
-        bool ok = true, ready = false;   // ready: the next stage has been seen full
+        bool ok = true, ready = false, acc_ready = false;   // the next stage has been seen full, the next accumulator empty
         const bool issuer = elect_one();
         const uint64_t a_desc0 = A_MN ? smem_desc_mn_sw128(smem_u32(smem_a)) : smem_desc_sw128(smem_u32(smem_a));
         const uint64_t b_desc0 = B_MN ? smem_desc_mn_sw128(smem_u32(smem_b)) : smem_desc_sw128(smem_u32(smem_b));
@@ -523,7 +526,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     const bool opens = EPI == EPI16_SUM ? k % kSumElems == 0 : k == 0 && pass == 0;
                     const bool closes = EPI == EPI16_SUM ? left <= C::kK || (k + C::kK) % kSumElems == 0 : left <= C::kK && pass == passes - 1;
                     if (opens) {
-                        if (!warp_wait(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u)) { ok = false; break; }
+                        if (!acc_ready && !warp_wait(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u)) { ok = false; break; }
                         d = tmem + acc.slot * BN;
                         if (CTAS == 2) fence_cluster_acquire();
                     }
@@ -532,6 +535,11 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     ring.next();
                     // Looked at before this stage is issued: afterwards the look would wait for the MMAs.
                     ready = __all_sync(0xFFFFFFFFu, mbar_test_wait(bar_full + 8 * ring.slot, ring.phase));
+                    const uint32_t acc_bar = 8 * acc.slot;
+                    if (closes) {
+                        acc.next();
+                        acc_ready = __all_sync(0xFFFFFFFFu, mbar_test_wait(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u));
+                    }
                     if (TILES == TILES_CUT && CTAS == 2 && left < C::kK) fence_cluster_acquire();
                     tcgen05_fence_after();
                     if (issuer) {
@@ -543,10 +551,9 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                             if (16 * j < left) tcgen05_mma_f16<CTAS>(d, ad, bd, idesc, !opens || j > 0);
                         }
                         tcgen05_commit<CTAS>(bar_empty + 8 * slot);
-                        if (closes) tcgen05_commit<CTAS>(bar_acc_full + 8 * acc.slot);
+                        if (closes) tcgen05_commit<CTAS>(bar_acc_full + acc_bar);
                     }
                     __syncwarp();
-                    if (closes) acc.next();
                 }
             }
         }
@@ -732,12 +739,6 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     if (out) {
 #pragma unroll
                         for (int j = 0; j < 4; j++) h[j] = pack_bf16(w[2 * j] * p.o_scale, w[2 * j + 1] * p.o_scale);
-                        if (col + 8 * i + 8 > p.boxed && lane < rows) {
-                            __nv_bfloat16 *o = p.o + ((int64_t)t.batch * p.m + t.row + in) * p.ld_o + col + 8 * i;
-#pragma unroll
-                            for (int j = 0; j < 8; j++)
-                                if (col + 8 * i + j < p.n) o[j] = __float2bfloat16_rn(w[j] * p.o_scale);
-                        }
                     } else {
 #pragma unroll
                         for (int j = 0; j < 4; j++) {
@@ -751,6 +752,21 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 }
                 fence_async_shared();
                 __syncwarp();
+                if (out && col + kChunk > p.boxed) {
+                    // Columns that do not leave in boxes: row by row, two columns of a row a lane.
+                    __nv_bfloat16 *o = p.o + ((int64_t)t.batch * p.m + row0) * p.ld_o + col;
+                    const int left = p.n - col, c0 = 2 * lane;
+#pragma unroll 4
+                    for (int r = 0; r < 32; r++) {
+                        if (r >= rows) break;
+                        uint32_t w;
+                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(boxes + r * 128 + ((((uint32_t)lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
+                        const __nv_bfloat162 pair = *reinterpret_cast<const __nv_bfloat162 *>(&w);
+                        if (c0 < left && col + c0 >= p.boxed) o[r * p.ld_o + c0] = pair.x;
+                        if (c0 + 1 < left && col + c0 >= p.boxed) o[r * p.ld_o + c0 + 1] = pair.y;
+                    }
+                    __syncwarp();
+                }
                 if (lane == 0 && !(out && col >= p.boxed)) {
                     tma_store_3d(&maps.out, col, row0, batch, boxes);
                     if (two && !out) tma_store_3d(&maps.out2, col, row0, batch, boxes + 4096);

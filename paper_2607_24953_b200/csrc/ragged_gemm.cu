@@ -2,6 +2,9 @@
 // variants are in gemm16.cuh; here are the arguments' checks and the choice of a variant.
 #include "gemm16.cuh"
 
+#include <algorithm>
+#include <cmath>
+
 using namespace fp4q;
 
 namespace {
@@ -71,24 +74,36 @@ fp4q_status launch_store16(const Operand16 &a, const Operand16 &b, Gemm16Params 
                : launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_STORE, TILES>(a, b, a, b, maps, p, most_tiles, stream);
 }
 
-// Rows of groups, T in all.
+// What a product of rows in tiles of rows x cols takes, in us, where `groups` groups may have rows and each fills its last tile by half: rounds of tiles
+// over the GPU's slots, per tile 2 us and its boxes, of which an SM gets 115 GB/s from L2 and all of them together 11 TB/s.
+double rows_cost(int64_t T, int64_t groups, int64_t n, int64_t k, int rows, int cols, int slots, double box_bytes, int ctas)
+{
+    const double row_tiles = std::max<double>((double)groups, (double)T / rows + 0.5 * groups), tiles = row_tiles * ceil_div(n, cols);
+    const double rate = std::min(115e3, 11e6 / (ctas * std::min<double>(tiles, slots)));   // bytes a us
+    return std::ceil(tiles / slots) * (2.0 + (double)ceil_div(k, 64) * box_bytes / rate);
+}
+
+// Rows of groups, T in all.  Pairs for groups of many rows, tiles of 32 rows for groups of few, 128 x 128 between them.
 template <bool B_MN>
 fp4q_status rows_product(const Operand16 &a, const Operand16 &b, Gemm16Params &p, fp4q_out dt, int64_t T, int64_t groups, cudaStream_t stream)
 {
     const int64_t few = T < groups ? T : groups;   // groups that have rows, at most
-    if (T >= 192 * groups) {
+    const int box = T <= 16 * few ? 16 : 32;
+    const double pairs = rows_cost(T, few, p.n, p.k, 256, 256, 74, 32768.0, 2), singles = rows_cost(T, few, p.n, p.k, 128, 128, 148, 32768.0, 1),
+                 small = rows_cost(T, few, p.n, p.k, 32, 64, 148, 8192.0 + 128.0 * box, 1);
+    const double least = std::min(pairs, std::min(singles, small));
+    p.a_box = 128;
+    if (least == pairs) {
         p.n_tiles = (int32_t)ceil_div(p.n, 256);
-        p.a_box = 128;
         return launch_store16<2, 256, false, B_MN, TILES_ROWS>(a, b, p, dt, (T / 256 + few) * p.n_tiles, stream);
     }
-    p.a_box = T <= 64 * groups ? 32 : 128;
-    const int64_t row_tiles = T / 128 + few;
-    if (row_tiles * ceil_div(p.n, 128) >= 148) {
+    if (least == singles) {
         p.n_tiles = (int32_t)ceil_div(p.n, 128);
-        return launch_store16<1, 128, false, B_MN, TILES_ROWS>(a, b, p, dt, row_tiles * p.n_tiles, stream);
+        return launch_store16<1, 128, false, B_MN, TILES_ROWS>(a, b, p, dt, (T / 128 + few) * p.n_tiles, stream);
     }
+    p.a_box = box;
     p.n_tiles = (int32_t)ceil_div(p.n, 64);
-    return launch_store16<1, 64, false, B_MN, TILES_ROWS>(a, b, p, dt, row_tiles * p.n_tiles, stream);
+    return launch_store16<1, 64, false, B_MN, TILES_ROWS>(a, b, p, dt, (T / 32 + few) * p.n_tiles, stream);
 }
 
 // which: 0 = Y = X W^T, 1 = dX = dY W.
@@ -108,7 +123,7 @@ fp4q_status rows_call(int which, const Matrix16 &x, const Matrix16 &w, void *c, 
     if (fp4q_status s = check_operand16(x)) return s;
     if (fp4q_status s = check_operand16(w)) return s;
     if (fp4q_status s = check_workspace(ws, ws_bytes)) return s;
-    if ((x.rows / 128 + groups) * ceil_div(cols, 64) > kMaxDim16) return FP4Q_ERR_UNSUPPORTED;   // tiles are counted in 32 bits
+    if ((x.rows / 32 + groups) * ceil_div(cols, 64) > kMaxDim16) return FP4Q_ERR_UNSUPPORTED;   // tiles are counted in 32 bits
     p.m = (int32_t)x.rows;
     p.n = (int32_t)cols;
     p.k = (int32_t)contraction;
