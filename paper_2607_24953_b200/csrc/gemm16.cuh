@@ -8,7 +8,7 @@
 // in about 0.3 us, as long as the MMAs take at the clock that full load leaves); single CTAs have tiles of 128 x 128 for problems with few
 // tiles, and of 32 x 64 for short groups (the MMAs have 128 rows all the same: those behind the first 32 are whatever lies in shared
 // memory, and nobody looks at them).
-//   warp 0      TMA producer: a stage is 64 contraction elements (single CTAs: 128), boxes of 128 bytes with the 128-byte swizzle
+//   warps 0, 3  TMA producers of A and B: a stage is 64 contraction elements (32 x 64 tiles: 128), boxes of 128 bytes with the 128-byte swizzle
 //   warp 1      MMA issuer (in the leader of a pair): four tcgen05.mma of 16 contraction elements per box
 //   warp 2      cut contractions: zeroes the rows of a group's last stage that lie behind the group
 //   warps 4-11  epilogue: a thread has a row of the tile; the accumulator is double-buffered in tensor memory.  Outputs leave, and what an
@@ -132,7 +132,6 @@ __device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_bar
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-__device__ __forceinline__ void fence_cluster_acquire() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 
 template <int CTAS>
 __device__ __forceinline__ void tcgen05_mma_f16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
@@ -157,23 +156,43 @@ __device__ __forceinline__ uint32_t instr_desc16(bool bf16, bool a_mn, bool b_mn
     return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(BN >> 3) << 17) |
            ((uint32_t)((kRows16 * CTAS) >> 4) << 24);
 }
-// A whole warp's bounded wait: all lanes go on or none does.  `limit` is in microseconds of the clock, the unit of the workspace's polls; a
-// poll suspends the warp for as long as the hardware likes, which is finite.  (With suspensions of a microsecond at most, as the
-// quantized products have them, the update product of 2048 x 5632 took 83 us instead of 67.)
+// A barrier's phase: CLUSTER if the other CTA of a pair arrives on it, whose writes this thread then sees.  (A fence behind the wait
+// instead waits for all that the issuer has under way: 1.2 us whenever it went on to the next accumulator.)
+template <bool CLUSTER>
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    if (CLUSTER)
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0u;
+}
+template <bool CLUSTER>
+__device__ __forceinline__ bool warp_test(uint32_t bar, uint32_t parity)   // a look at it, without suspension
+{
+    uint32_t done;
+    if (CLUSTER)
+        asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return __all_sync(0xFFFFFFFFu, done != 0u);
+}
 __device__ __forceinline__ uint64_t now_ns()
 {
     uint64_t t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
+// A whole warp's bounded wait: all lanes go on or none does.  `limit` is in microseconds of the clock, the unit of the workspace's polls; a
+// poll suspends the warp for as long as the hardware likes, which is finite.  (With suspensions of a microsecond at most, as the
+// quantized products have them, the update product of 2048 x 5632 took 83 us instead of 67.)
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t *status, uint64_t limit, uint32_t where)
 {
     bool ok = true;
     uint64_t since = 0;
-    while (true) {
-        uint32_t done;
-        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-        if (done) break;
+    while (!mbar_try<CLUSTER>(bar, parity)) {
         if (*abort_flag) { ok = false; break; }
         const uint64_t now = now_ns();
         if (since == 0) since = now;
@@ -394,7 +413,13 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         tcgen05_fence_before();
     } else if (warp == 0 && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
+        if (kSplits && p.split) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a2) : "memory");
+    } else if (warp == 3 && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b) : "memory");
+        if (kSplits && p.split) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b2) : "memory");
+    } else if (warp == 5 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.out) : "memory");
+        if (EPI == EPI16_POLY || EPI == EPI16_UPDATE) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.in) : "memory");
     }
     __syncthreads();
     if (CTAS == 2) { cluster_arrive(); cluster_wait(); }
@@ -406,13 +431,21 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     const uint64_t limit = limit_word != 0u ? limit_word : kWaitLimit;
     int m_tiles = p.m_tiles;
     if (TILES <= TILES_CUT) {
-        for (int g = threadIdx.x; g <= p.batch; g += kThreads16)
-            start[g] = !p.offsets ? (g == 0 ? 0 : (int32_t)p.total_rows) : (int32_t)max((int64_t)0, min(p.total_rows, load_global(p.offsets + g)));
-        __syncthreads();
+        // A lane of warp 4 has a run of boundaries, up to eight in registers.  Boundaries that fall are lifted; then the row tiles of all groups
+        // before a group's are counted (TILES_ROWS).
         if (warp == 4) {
-            const int per_lane = (p.batch + 32) / 32, g0 = min(lane * per_lane, p.batch + 1), g1 = min(g0 + per_lane, p.batch + 1);   // 32 runs of boundaries
-            int top = 0;
-            for (int g = g0; g < g1; g++) top = max(top, start[g]);
+            constexpr int kBM = C::kRows * CTAS, kRun = 8;
+            const int run = (p.batch + 32) / 32, g0 = min(lane * run, p.batch + 1), g1 = min(g0 + run, p.batch + 1);
+            auto boundary = [&](int g) { return !p.offsets ? (g == 0 ? 0 : (int32_t)p.total_rows) : (int32_t)max((int64_t)0, min(p.total_rows, load_global(p.offsets + g))); };
+            int b[kRun], top = 0;
+            if (run <= kRun) {
+#pragma unroll
+                for (int i = 0; i < kRun; i++) b[i] = g0 + i < g1 ? boundary(g0 + i) : 0;
+#pragma unroll
+                for (int i = 0; i < kRun; i++) top = b[i] = max(top, b[i]);
+            } else {
+                for (int g = g0; g < g1; g++) start[g] = top = max(top, boundary(g));
+            }
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const int other = __shfl_up_sync(0xFFFFFFFFu, top, d);
@@ -420,13 +453,27 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             }
             int before = __shfl_up_sync(0xFFFFFFFFu, top, 1);
             if (lane == 0) before = 0;
-            for (int g = g0; g < g1; g++) start[g] = before = max(before, start[g]);   // boundaries that fall are lifted
-            __syncwarp();
-            if (TILES == TILES_ROWS) {   // row tiles of all groups before a group's
-                constexpr int kBM = C::kRows * CTAS;
-                const int last = min(g1, p.batch);
+            if (run <= kRun) {
+#pragma unroll
+                for (int i = 0; i < kRun; i++)
+                    if (g0 + i < g1) start[g0 + i] = b[i] = max(before, b[i]);
+            } else {
+                for (int g = g0; g < g1; g++) start[g] = max(before, start[g]);
+            }
+            if (TILES == TILES_ROWS) {
+                __syncwarp();
+                const int last = min(g1, p.batch), after = g1 <= p.batch ? start[g1] : 0;   // the boundary behind the run
                 int sum = 0;
-                for (int g = g0; g < last; g++) sum += (group_rows(start, g) + kBM - 1) / kBM;
+                if (run <= kRun) {
+#pragma unroll
+                    for (int i = 0; i < kRun; i++) {
+                        const int next = i + 1 < kRun && g0 + i + 1 < g1 ? b[i + 1 < kRun ? i + 1 : 0] : after;
+                        b[i] = g0 + i < last ? (next - b[i] + kBM - 1) / kBM : 0;
+                        sum += b[i];
+                    }
+                } else {
+                    for (int g = g0; g < last; g++) sum += (group_rows(start, g) + kBM - 1) / kBM;
+                }
                 before = sum;
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
@@ -435,9 +482,17 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 }
                 if (lane == 31) *shared_tiles = before;
                 before -= sum;
-                for (int g = g0; g < last; g++) {
-                    first[g] = before;
-                    before += (group_rows(start, g) + kBM - 1) / kBM;
+                if (run <= kRun) {
+#pragma unroll
+                    for (int i = 0; i < kRun; i++) {
+                        if (g0 + i < last) first[g0 + i] = before;
+                        before += b[i];
+                    }
+                } else {
+                    for (int g = g0; g < last; g++) {
+                        first[g] = before;
+                        before += (group_rows(start, g) + kBM - 1) / kBM;
+                    }
                 }
             }
         }
@@ -449,8 +504,10 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     const int passes = kSplits && p.split ? 3 : 1;   // upper x upper, upper x lower, lower x upper
     if (p.admit) admit_successor();
 
-    if (warp == 0) {
-        // ------------------------------------------------------------------ TMA producer
+    if (warp == 0 || warp == 3) {
+        // ------------------------------------------------------------------ TMA producers: warp 0 loads A and announces the bytes, warp 3 loads B
+        // One thread that issues up to four copies a stage needs 0.55 us for it, longer than the stage's MMAs take.
+        const bool a_side = warp == 0;
         uint32_t loads = 0, issued = 0;
         Ring16<kStages> ring;
         bool ok = true;
@@ -475,8 +532,8 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     if (issuer) {
                         const int boxes = C::kBoxes == 1 || left > kBox16 ? C::kBoxes : 1;
                         const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * ring.slot, bar = CTAS == 2 && !cut ? lead + 8 * ring.slot : own_bar;
-                        if (rank == 0 || cut) mbar_arrive_expect_tx(own_bar, (uint32_t)boxes * (box_bytes + (cut ? 0u : peer_bytes)));
-                        if (withhold == 0u || ++loads != withhold) {
+                        if (a_side && (rank == 0 || cut)) mbar_arrive_expect_tx(own_bar, (uint32_t)boxes * (box_bytes + (cut ? 0u : peer_bytes)));
+                        if (withhold == 0u || !a_side || ++loads != withhold) {
                             auto load = [&](uint32_t dst, const CUtensorMap *map, int x, int y, int z) {
                                 if (CTAS == 2 && !cut) tma_load_3d_pair(dst, map, x, y, z, bar);
                                 else tma_load_3d(dst, map, x, y, z, bar);
@@ -486,13 +543,15 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                                 if (i >= boxes) break;
                                 const uint32_t a = a0 + ring.slot * C::kABytes + i * C::kABox, b = b0 + ring.slot * C::kBBytes + i * C::kBBox;
                                 const int at = t.k0 + k + i * kBox16;
-                                if (A_MN) {
+                                if (!a_side) {
+                                } else if (A_MN) {
 #pragma unroll
                                     for (int j = 0; j < 2; j++) load(a + j * 8192, mapA, t.a_row + 64 * j, at, az);
                                 } else {
                                     for (int j = 0; j < a_copies; j++) load(a + j * a_copy_bytes, mapA, at, t.a_row + j * p.a_box, az);
                                 }
-                                if (B_MN) {
+                                if (a_side) {
+                                } else if (B_MN) {
 #pragma unroll
                                     for (int j = 0; j < C::kBRows / 64; j++) load(b + j * 8192, mapB, t.b_row + 64 * j, at, bz);
                                 } else {
@@ -513,6 +572,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         const uint32_t idesc = instr_desc16<CTAS, BN>(p.bf16 != 0, A_MN, B_MN);
         Ring16<kStages> ring;
         Ring16<2> acc;      // accumulators
+        constexpr bool kPeerFills = TILES == TILES_CUT && CTAS == 2;   // the other CTA's warp 2 has part in "full"
         bool ok = true, ready = false, acc_ready = false;   // the next stage has been seen full, the next accumulator empty
         const bool issuer = elect_one();
         const uint64_t a_desc0 = A_MN ? smem_desc_mn_sw128(smem_u32(smem_a)) : smem_desc_sw128(smem_u32(smem_a));
@@ -526,21 +586,19 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     const bool opens = EPI == EPI16_SUM ? k % kSumElems == 0 : k == 0 && pass == 0;
                     const bool closes = EPI == EPI16_SUM ? left <= C::kK || (k + C::kK) % kSumElems == 0 : left <= C::kK && pass == passes - 1;
                     if (opens) {
-                        if (!acc_ready && !warp_wait(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u)) { ok = false; break; }
+                        if (!acc_ready && !warp_wait<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u)) { ok = false; break; }
                         d = tmem + acc.slot * BN;
-                        if (CTAS == 2) fence_cluster_acquire();
                     }
-                    if (!ready && !warp_wait(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot)) { ok = false; break; }
+                    if (!ready && !warp_wait<kPeerFills>(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot)) { ok = false; break; }
                     const uint32_t slot = ring.slot;
                     ring.next();
                     // Looked at before this stage is issued: afterwards the look would wait for the MMAs.
-                    ready = __all_sync(0xFFFFFFFFu, mbar_test_wait(bar_full + 8 * ring.slot, ring.phase));
+                    ready = warp_test<kPeerFills>(bar_full + 8 * ring.slot, ring.phase);
                     const uint32_t acc_bar = 8 * acc.slot;
                     if (closes) {
                         acc.next();
-                        acc_ready = __all_sync(0xFFFFFFFFu, mbar_test_wait(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u));
+                        acc_ready = warp_test<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u);
                     }
-                    if (TILES == TILES_CUT && CTAS == 2 && left < C::kK) fence_cluster_acquire();
                     tcgen05_fence_after();
                     if (issuer) {
 #pragma unroll
@@ -580,11 +638,11 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (CTAS == 2 && rank == 0) {
-                if (!warp_wait(bar_peer + 8 * slot, parity, abort_flag, p.status, limit, 0x400u + slot)) break;
-                fence_cluster_acquire();
+                if (!warp_wait<true>(bar_peer + 8 * slot, parity, abort_flag, p.status, limit, 0x400u + slot)) break;
             }
             if (lane == 0) {
-                if (rank == 0) mbar_arrive(bar_full + 8 * slot);
+                if (rank == 0 && CTAS == 2) mbar_arrive_release_cluster(cluster_addr(bar_full + 8 * slot, 0));
+                else if (rank == 0) mbar_arrive(bar_full + 8 * slot);
                 else mbar_arrive_release_cluster(cluster_addr(bar_peer + 8 * slot, 0));
             }
             __syncwarp();
