@@ -10,7 +10,7 @@
 // memory, and nobody looks at them).
 //   warps 0, 3  TMA producers of A and B: a stage is 64 contraction elements (32 x 64 tiles: 128), boxes of 128 bytes with the 128-byte swizzle
 //   warp 1      MMA issuer (in the leader of a pair): four tcgen05.mma of 16 contraction elements per box
-//   warp 2      cut contractions: zeroes the rows of a group's last stage that lie behind the group
+//   warp 2      cut contractions: deals the tiles (in the leader of a pair), zeroes the rows of a group's last stage that lie behind the group
 //   warps 4-11  epilogue: a thread has a row of the tile; the accumulator is double-buffered in tensor memory.  Outputs leave, and what an
 //               epilogue reads comes, as boxes of 32 rows x 128 bytes through shared memory (TMA): with plain accesses a warp's 16 bytes
 //               in each of 32 rows take the load/store unit 32 cycles, which made update products of 768 x 2048 epilogue-bound
@@ -30,6 +30,8 @@ constexpr int kRows16 = 128;         // accumulator rows per CTA
 constexpr int kBox16 = 64;           // contraction elements of a box: 128 bytes
 constexpr int kThreads16 = 384;
 constexpr int kRaster16 = 16;        // row tiles per rasterisation group: their A rows stay in L2 while the columns go by
+constexpr int kMaxSorted16 = 256;    // cut contractions: so many groups are taken longest first
+constexpr int kDealt16 = 4;          // cut contractions: tiles that are dealt ahead
 constexpr int kMaxGroups16 = 2047;   // boundaries and first tiles of this many groups lie in shared memory
 
 // TILES_ROWS: groups of A rows (and of output rows), a matrix B per group.  TILES_CUT: a product per group, contracted over its rows.
@@ -67,6 +69,7 @@ struct Gemm16Params {
     int32_t m_tiles, n_tiles;        // TILES_ROWS: m_tiles is found on the device
     int32_t batch;                   // groups or matrices
     int32_t bf16;                    // operand type: 0 = FP16, 1 = BF16
+    int32_t deals;                   // TILES_CUT: tiles go to whoever is free instead of in turn
     int32_t a_box;                   // rows of one copy of a K-major A operand: 128; 32 or 16 in tiles of 32 rows
     const int64_t *offsets;          // TILES_ROWS, TILES_CUT: batch + 1 boundaries; NULL: one group of all rows
     int64_t total_rows;              // rows that the boundaries are held to
@@ -274,6 +277,7 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
         t.row = mt * kBM;
         valid = p.m - t.row;
     }
+    if (TILES == TILES_CUT && p.deals && p.batch <= kMaxSorted16) t.batch = first[t.batch];
     if (TILES == TILES_CUT) { t.k0 = start[t.batch]; t.k_len = group_rows(start, t.batch); }
     t.row += rank * kRows;
     t.a_row = t.row;
@@ -385,12 +389,14 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     uint8_t *smem_boxes = smem + C::kOperands;
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem_boxes + 8 * kStaging);
     // bars[0..7] full, [8..15] empty, [16..17] accumulator full, [18..19] accumulator empty, [20..27] a group's last stage has landed here,
-    // [28..35] (leader of a pair) it is ready in the other CTA, [36..43] an epilogue warp's boxes have come
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 44);
+    // [28..35] (leader of a pair) it is ready in the other CTA, [36..43] an epilogue warp's boxes have come, [44..47] a tile is dealt,
+    // [48..51] (leader) it has been taken
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 52);
     volatile uint32_t *abort_flag = tmem_slot + 1;
     int32_t *shared_tiles = reinterpret_cast<int32_t *>(tmem_slot + 2);
     int32_t *start = reinterpret_cast<int32_t *>(reinterpret_cast<uint8_t *>(bars) + C::kTail), *first = start + kMaxGroups16 + 1;
-    static_assert(kStages <= 8 && 44 * 8 + 16 <= C::kTail, "barriers");
+    int32_t *dealt = shared_tiles + 1;   // kDealt16 tiles
+    static_assert(kStages <= 8 && 52 * 8 + 16 + 4 * kDealt16 <= C::kTail, "barriers");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t bar_full = smem_u32(bars), bar_empty = smem_u32(bars + 8), bar_acc_full = smem_u32(bars + 16), bar_acc_empty = smem_u32(bars + 18),
@@ -399,7 +405,8 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
 
     if (warp == 4) {
         mbar_init(smem_u32(bars + lane), lane >= 18 && lane < 20 ? 8 * CTAS : 1);
-        if (lane < 12) mbar_init(smem_u32(bars + 32 + lane), 1);
+        // A dealt tile is taken by both producers, the epilogue's warps, the leader's issuer and the other CTA's warp 2.
+        if (lane < 20) mbar_init(smem_u32(bars + 32 + lane), lane >= 16 ? (CTAS == 2 ? 22 : 11) : 1);
         if (lane == 0) *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     } else if (warp == 1) {
@@ -430,6 +437,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     const uint32_t limit_word = load_global(p.status + 2), withhold = blockIdx.x == 0 ? load_global(p.status + 3) : 0u;
     const uint64_t limit = limit_word != 0u ? limit_word : kWaitLimit;
     int m_tiles = p.m_tiles;
+    const bool deals = TILES == TILES_CUT && p.deals;
     if (TILES <= TILES_CUT) {
         // A lane of warp 4 has a run of boundaries, up to eight in registers.  Boundaries that fall are lifted; then the row tiles of all groups
         // before a group's are counted (TILES_ROWS).
@@ -498,9 +506,38 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         }
         __syncthreads();
         if (TILES == TILES_ROWS) m_tiles = *shared_tiles;
+        if (deals && p.batch <= kMaxSorted16) {   // first: the groups' order
+            for (int g = threadIdx.x; g < p.batch; g += kThreads16) {
+                const int len = group_rows(start, g);
+                int place = 0;
+                for (int h = 0; h < p.batch; h++) {
+                    const int other = group_rows(start, h);
+                    place += other > len || (other == len && h < g);
+                }
+                first[place] = g;
+            }
+            __syncthreads();
+        }
     }
     const int tiles = TILES == TILES_ROWS ? m_tiles * p.n_tiles : TILES == TILES_SYM ? p.batch * (m_tiles * (m_tiles + 1) / 2) : p.batch * m_tiles * p.n_tiles;
     const int tile0 = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+    // Cut contractions differ in length: the tiles are dealt to the CTAs or pairs as these fall free, longest groups first (128 groups with loads of
+    // 302 to 15157 rows: dealt round in order, the last pair would have 1.4 times the average of stages, longest first in turn 1.16
+    // times).  Which CTA has a tile changes nothing in its result.
+    Ring16<kDealt16> deal;
+    const uint32_t bar_dealt = smem_u32(bars + 44), bar_taken = smem_u32(bars + 48);
+    auto next_tile = [&](int tile) {   // the tile after `tile` of this CTA or pair (a warp's first: tile = -1); tiles or more: no more
+        if (!deals) return tile < 0 ? tile0 : tile + step;
+        if (!warp_wait<CTAS == 2>(bar_dealt + 8 * deal.slot, deal.phase, abort_flag, p.status, limit * 16, 0x900u)) return tiles;
+        const int t = dealt[deal.slot];
+        __syncwarp();
+        if (lane == 0) {
+            if (CTAS == 2) mbar_arrive_release_cluster(cluster_addr(bar_taken + 8 * deal.slot, 0));
+            else mbar_arrive(bar_taken + 8 * deal.slot);
+        }
+        deal.next();
+        return t;
+    };
     const int passes = kSplits && p.split ? 3 : 1;   // upper x upper, upper x lower, lower x upper
     if (p.admit) admit_successor();
 
@@ -513,7 +550,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         bool ok = true;
         const bool issuer = elect_one();
         const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b), lead = CTAS == 2 ? cluster_addr(bar_full, 0) : bar_full;
-        for (int tile = tile0; ok && tile < tiles; tile += step) {
+        for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
             const int a_copies = A_MN ? 2 : (t.rows + p.a_box - 1) / p.a_box;
             const uint32_t a_copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
@@ -563,6 +600,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     __syncwarp();
                 }
             }
+            if (!ok) break;
         }
         // The MMAs' last reports reach this CTA's barriers while it is still there.
         for (uint32_t i = 0; ok && i < kStages; i++, ring.next())
@@ -577,7 +615,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         const bool issuer = elect_one();
         const uint64_t a_desc0 = A_MN ? smem_desc_mn_sw128(smem_u32(smem_a)) : smem_desc_sw128(smem_u32(smem_a));
         const uint64_t b_desc0 = B_MN ? smem_desc_mn_sw128(smem_u32(smem_b)) : smem_desc_sw128(smem_u32(smem_b));
-        for (int tile = tile0; ok && tile < tiles; tile += step) {
+        for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
             uint32_t d = 0;
             for (int pass = 0; ok && pass < passes; pass++) {
@@ -614,6 +652,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     __syncwarp();
                 }
             }
+            if (!ok) break;
         }
     } else if (warp == 2 && TILES == TILES_CUT) {
         // ------------------------------------------------------------------ rows behind a group's end
@@ -621,7 +660,46 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         // both operands (in one, an infinity in the other would make NaN).  Then, and in a pair when the other CTA has done the same, the
         // stage is full.  A slot is filled again only when the MMAs have read it, so its barriers are never a phase ahead.
         uint32_t slot = 0, phases = 0;
-        for (int tile = tile0; tile < tiles; tile += step) {
+        // The leader's warp 2 deals: a number from the workspace's counter is the next tile, for both CTAs, as far ahead as there are places.
+        Ring16<kDealt16> dealing;
+        int ahead = 0, mine = 0, more = 1, hand[kDealt16];
+        auto deal_ahead = [&]() {
+            while (rank == 0 && more && ahead < kDealt16) {
+                if (!warp_wait<CTAS == 2>(bar_taken + 8 * dealing.slot, dealing.phase ^ 1u, abort_flag, p.status, limit * 16, 0xA00u)) return false;
+                int n = 0;
+                if (lane == 0) {
+                    n = (int)min(atomicAdd(p.status + 4, 1u), (uint32_t)tiles);
+                    dealt[dealing.slot] = n;
+                    if (CTAS == 2) {
+                        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(smem_u32(dealt + dealing.slot), 1)), "r"(n) : "memory");
+                        mbar_arrive_release_cluster(cluster_addr(bar_dealt + 8 * dealing.slot, 0));
+                        mbar_arrive_release_cluster(cluster_addr(bar_dealt + 8 * dealing.slot, 1));
+                    } else {
+                        mbar_arrive(bar_dealt + 8 * dealing.slot);
+                    }
+                }
+                n = __shfl_sync(0xFFFFFFFFu, n, 0);
+#pragma unroll
+                for (int i = 0; i < kDealt16; i++)
+                    if (i == (int)dealing.slot) hand[i] = n;
+                more = n < tiles;
+                ahead++;
+                dealing.next();
+            }
+            return true;
+        };
+        auto my_tile = [&](int tile) {
+            if (!deals || rank != 0) return next_tile(tile);
+            if (!deal_ahead()) return tiles;
+            int t = tiles;
+#pragma unroll
+            for (int i = 0; i < kDealt16; i++)
+                if (i == mine) t = hand[i];
+            mine = mine + 1 == kDealt16 ? 0 : mine + 1;
+            ahead--;
+            return t;
+        };
+        for (int tile = my_tile(-1); tile < tiles; tile = my_tile(tile)) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
             const int whole = t.k_len / C::kK, left = t.k_len - whole * C::kK;
             slot = (slot + whole) % kStages;
@@ -656,7 +734,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         constexpr int kCols = BN / 2, kChunk = EPI == EPI16_SUM || kCols < 64 ? 32 : 64;   // a warp's columns, and those of a box
         Ring16<2> acc;
         uint32_t box_phase = 0;
-        for (int tile = tile0; tile < tiles; tile += step) {
+        for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
             const int in = 32 * quarter + lane;
             const int chunks = EPI == EPI16_SUM ? (t.k_len + kSumElems - 1) / kSumElems : t.k_len > 0;   // accumulators of the tile
@@ -876,11 +954,18 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     // Shared memory and tensor memory stay until all roles, of both CTAs of a pair, have done with them.  Where a wait has run out, copies and
     // MMAs may still be under way: they take microseconds, a millisecond is left to them.
     __syncwarp();
-    if (*abort_flag != 0u)
+    if (*abort_flag != 0u) {
+        if (CTAS == 2 && lane == 0)   // the other CTA is told
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(smem_u32(const_cast<const uint32_t *>(abort_flag)), 1 - rank)), "r"(1u) : "memory");
         for (int i = 0; i < 64; i++) __nanosleep(16000);
+    }
     tcgen05_fence_before();
     __syncthreads();
     if (CTAS == 2) { cluster_arrive(); cluster_wait(); }
+    if (deals && threadIdx.x == 0 && rank == 0 && atomicAdd(p.status + 5, 1u) == (uint32_t)step - 1u) {   // nobody deals any more: the counters are as they were
+        p.status[4] = 0u;
+        p.status[5] = 0u;
+    }
     if (warp == 1) {
         tcgen05_fence_after();
         if (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");

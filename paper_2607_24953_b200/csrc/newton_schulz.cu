@@ -111,10 +111,16 @@ __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumPara
 {
     wait_for_predecessor();
     const int64_t row0 = (int64_t)blockIdx.y * p.rows;
-    double sum = 0.0, inv = 0.0;
+    double sum = 0.0;
+    float inv0 = 0.f, inv1 = 0.f;   // 1 / (|U| + eps), scaled, as a power of two and the rest: it may lie outside of what FP32 holds
     if (FINISH) {
         for (int i = threadIdx.x; i < (int)gridDim.x; i += kNsThreads) sum += load_global(p.partial + (int64_t)blockIdx.y * gridDim.x + i);
-        inv = (double)kScaleX / (sqrt(block_sum(sum)) + p.eps);
+        const double inv = (double)kScaleX / (sqrt(block_sum(sum)) + p.eps);
+        int e;
+        frexp(inv, &e);
+        e = max(-200, min(200, e)) / 2;
+        inv0 = ldexpf(1.f, e);
+        inv1 = (float)ldexp(inv, -e);
     }
     const uint32_t step = gridDim.x * kNsThreads;
     for (uint32_t base = blockIdx.x * kNsThreads + threadIdx.x; base < p.units; base += kNsUnroll * step) {
@@ -148,7 +154,7 @@ __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumPara
                 sum += (double)u.x * u.x + (double)u.y * u.y;
                 sum += (double)u.z * u.z + (double)u.w * u.w;
             } else {
-                const float x[4] = {(float)(u.x * inv), (float)(u.y * inv), (float)(u.z * inv), (float)(u.w * inv)};
+                const float x[4] = {u.x * inv0 * inv1, u.y * inv0 * inv1, u.z * inv0 * inv1, u.w * inv0 * inv1};
                 uint32_t up[2], lo[2];
 #pragma unroll
                 for (int e = 0; e < 2; e++) {

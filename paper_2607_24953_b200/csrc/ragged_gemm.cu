@@ -179,6 +179,7 @@ extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t
     p.offsets = g ? g->row_offsets : nullptr;
     p.total_rows = T;
     p.accumulate = accumulate != 0;
+    p.deals = groups > 1 && T >= 256 * groups;   // shorter groups: 300 rows in 64 groups 23.5 us in turn, 35.0 dealt
     p.status = static_cast<uint32_t *>(ws);
     const Operand16 a = T ? operand16(d, T, 1) : Operand16{dW, 8, 1, 1, 8, 8}, b = T ? operand16(m, T, 1) : a;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
