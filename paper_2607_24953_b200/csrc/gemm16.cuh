@@ -367,6 +367,14 @@ struct Box16 {
         for (int i = 0; i < 8; i++) st_shared_16(piece(i), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     }
 };
+__device__ __forceinline__ void load_blocks_transposed(uint32_t at, uint32_t *v)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void store_blocks(uint32_t at, const uint32_t *v)
+{
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // The warp's stores have read its boxes.
 __device__ __forceinline__ void boxes_free(int lane)
@@ -432,9 +440,17 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     if (CTAS == 2) { cluster_arrive(); cluster_wait(); }
     tcgen05_fence_after();
     const uint32_t tmem = *tmem_slot;
+    // The workspace's settings.  The products of a Newton-Schulz step run behind other kernels of the same call, which is behind whatever
+    // wrote them: those are read ahead of the wait.
+    uint32_t limit_word = 0u, withhold = 0u;
+    auto settings = [&]() {
+        limit_word = load_global(p.status + 2);
+        if (blockIdx.x == 0) withhold = load_global(p.status + 3);
+    };
+    if (kSplits) settings();
     wait_for_predecessor();   // from here on global memory is read and written
+    if (!kSplits) settings();
 
-    const uint32_t limit_word = load_global(p.status + 2), withhold = blockIdx.x == 0 ? load_global(p.status + 3) : 0u;
     const uint64_t limit = limit_word != 0u ? limit_word : kWaitLimit;
     int m_tiles = p.m_tiles;
     const bool deals = TILES == TILES_CUT && p.deals;
@@ -743,13 +759,14 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             const int col0 = t.col + half * kCols, row0 = t.row + 32 * quarter, rows = t.rows - 32 * quarter;   // this warp's first column and row, its rows
             const int batch = TILES == TILES_ROWS ? 0 : t.batch;
             const int64_t row = (TILES == TILES_CUT ? (int64_t)t.batch * p.m : 0) + t.row + in;
-            // The accumulator may be overwritten as soon as all warps have it in registers.
+            // The accumulator may be overwritten as soon as all warps have it in registers: reads of tensor memory, which the fence orders, and
+            // nothing else.  (Release at cluster scope, here and in the leader's own CTA too, held the warp up for 0.7 us.)
             auto release = [&]() {
                 tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) {
                     const uint32_t bar = bar_acc_empty + 8 * acc.slot;
-                    if (CTAS == 2) mbar_arrive_release_cluster(cluster_addr(bar, 0));
+                    if (rank != 0) mbar_arrive_cluster(cluster_addr(bar, 0));
                     else mbar_arrive(bar);
                 }
                 __syncwarp();
@@ -909,19 +926,20 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     bulk_commit();
                 }
                 if (EPI != EPI16_UPDATE && t.mirror) {
-                    // The transposed box, 64 rows of 64 bytes, in place of the box itself once that has left: a column is read from all rows.
-                    uint32_t keep_up[32], keep_lo[32];
+                    // The transposed box, 64 rows of 64 bytes, in place of the box itself once that has left.  A lane gives the addresses of its
+                    // row's pieces: four blocks of 8 x 8 at a time are read transposed, and written where they then belong.
+                    uint32_t block_up[32], block_lo[32];
 #pragma unroll
                     for (int i = 0; i < 8; i++) {
-                        const uint4 a = ld_shared_16(up.piece(i)), b = two ? ld_shared_16(lo.piece(i)) : make_uint4(0u, 0u, 0u, 0u);
-                        keep_up[4 * i] = a.x; keep_up[4 * i + 1] = a.y; keep_up[4 * i + 2] = a.z; keep_up[4 * i + 3] = a.w;
-                        keep_lo[4 * i] = b.x; keep_lo[4 * i + 1] = b.y; keep_lo[4 * i + 2] = b.z; keep_lo[4 * i + 3] = b.w;
+                        load_blocks_transposed(up.piece(i), block_up + 4 * i);
+                        if (two) load_blocks_transposed(lo.piece(i), block_lo + 4 * i);
                     }
                     boxes_free(lane);
+                    const uint32_t there = boxes + (lane & 7) * 64 + (lane >> 3) * 16;
 #pragma unroll
-                    for (int e = 0; e < 64; e++) {
-                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(boxes + e * 64 + lane * 2), "h"((uint16_t)(keep_up[e / 2] >> (16 * (e & 1)))) : "memory");
-                        if (two) asm volatile("st.shared.u16 [%0], %1;" ::"r"(boxes + 4096 + e * 64 + lane * 2), "h"((uint16_t)(keep_lo[e / 2] >> (16 * (e & 1)))) : "memory");
+                    for (int i = 0; i < 8; i++) {
+                        store_blocks(there + i * 512, block_up + 4 * i);
+                        if (two) store_blocks(there + 4096 + i * 512, block_lo + 4 * i);
                     }
                     fence_async_shared();
                     __syncwarp();
