@@ -33,7 +33,7 @@ EXPORTS = ["fp4q_quantize2d", "fp4q_gemm_fwd", "fp4q_gemm_dgrad", "fp4q_gemm_wgr
            "fp4q_mxfp8_quantize1d_t", "fp4q_mxfp8_gemm", "fp4q_gemm_fwd_quantized", "fp4q_gemm_dgrad_quantized",
            "fp4q_gemm_fwd_b16", "fp4q_gemm_dgrad_b16", "fp4q_gemm_wgrad_b16", "fp4q_quantize2d_multi",
            "fp4q_quantize2d_multi_f32", "fp4q_ragged_gemm_fwd", "fp4q_ragged_gemm_dgrad", "fp4q_ragged_gemm_wgrad",
-           "fp4q_newton_schulz", "fp4q_newton_schulz_scratch_bytes"]
+           "fp4q_ragged_gemm_wgrad_scratch_bytes", "fp4q_newton_schulz", "fp4q_newton_schulz_scratch_bytes"]
 
 
 class Fp4qError(RuntimeError):
@@ -135,7 +135,9 @@ def lib() -> ctypes.CDLL:
         L.fp4q_ragged_gemm_dgrad.restype = ci
         L.fp4q_ragged_gemm_dgrad.argtypes = [vp, i64, i64, i64, vp, i64, i64, i64, vp, i64, ci, ctypes.POINTER(_CGroups), vp, ctypes.c_size_t, vp]
         L.fp4q_ragged_gemm_wgrad.restype = ci
-        L.fp4q_ragged_gemm_wgrad.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, i64, ci, ci, ctypes.POINTER(_CGroups), vp, ctypes.c_size_t, vp]
+        L.fp4q_ragged_gemm_wgrad.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, i64, ci, ci, ctypes.POINTER(_CGroups), vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp]
+        L.fp4q_ragged_gemm_wgrad_scratch_bytes.restype = ctypes.c_size_t
+        L.fp4q_ragged_gemm_wgrad_scratch_bytes.argtypes = [i64, i64, i64, ctypes.c_int32]
         L.fp4q_newton_schulz_scratch_bytes.restype = ctypes.c_size_t
         L.fp4q_newton_schulz_scratch_bytes.argtypes = [i64, i64, i64]
         L.fp4q_newton_schulz.restype = ci
@@ -381,18 +383,24 @@ def fp4q_ragged_gemm_fwd(x: torch.Tensor, w: torch.Tensor, row_offsets=None, out
     """Y[T,N] = X W_g^T for the rows of every group g, on BF16 operands: x [T, K], w the expert stack [E*N, K], row_offsets int64 [E+1] on the
     device, any non-decreasing values (None: one group).  Rows that no group owns stay as they are in `out`; in an output that is
     allocated here they are zero."""
-    return _host().ragged_gemm(_FWD, x, w, row_offsets, out, dt, False, ws, _handle(stream))
+    return _host().ragged_gemm(_FWD, x, w, row_offsets, out, dt, False, None, ws, _handle(stream))
 
 
 def fp4q_ragged_gemm_dgrad(dY: torch.Tensor, w: torch.Tensor, row_offsets=None, out=None, dt: int = OUT_BF16, ws=None, stream=None):
     """dX[T,K] = dY W_g for the rows of every group g; groups and rows that no group owns as in fp4q_ragged_gemm_fwd."""
-    return _host().ragged_gemm(_DGRAD, dY, w, row_offsets, out, dt, False, ws, _handle(stream))
+    return _host().ragged_gemm(_DGRAD, dY, w, row_offsets, out, dt, False, None, ws, _handle(stream))
 
 
 def fp4q_ragged_gemm_wgrad(dY: torch.Tensor, x: torch.Tensor, row_offsets=None, out=None, dt: int = OUT_F32, accumulate: bool = False, ws=None,
-                           stream=None):
-    """dW[E*N, K] (+)= dY^T X over the rows of every group; an empty group's is zero."""
-    return _host().ragged_gemm(_WGRAD, dY, x, row_offsets, out, dt, accumulate, ws, _handle(stream))
+                           stream=None, scratch=None):
+    """dW[E*N, K] (+)= dY^T X over the rows of every group; an empty group's is zero.  scratch: memory for contractions in parts
+    (alloc_ragged_wgrad_scratch), allocated here if None."""
+    return _host().ragged_gemm(_WGRAD, dY, x, row_offsets, out, dt, accumulate, scratch, ws, _handle(stream))
+
+
+def alloc_ragged_wgrad_scratch(T: int, N: int, K: int, n_groups: int, device) -> torch.Tensor:
+    """Scratch memory of fp4q_ragged_gemm_wgrad for these sizes; calls that share it must not overlap on the GPU."""
+    return torch.empty(int(lib().fp4q_ragged_gemm_wgrad_scratch_bytes(T, N, K, n_groups)), dtype=torch.uint8, device=device)
 
 
 NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5

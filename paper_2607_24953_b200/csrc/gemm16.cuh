@@ -30,7 +30,7 @@ constexpr int kRows16 = 128;         // accumulator rows per CTA
 constexpr int kBox16 = 64;           // contraction elements of a box: 128 bytes
 constexpr int kThreads16 = 384;
 constexpr int kRaster16 = 16;        // row tiles per rasterisation group: their A rows stay in L2 while the columns go by
-constexpr int kMaxSorted16 = 256;    // cut contractions: so many groups are taken longest first
+constexpr int kMaxSorted16 = 256;    // cut contractions: so many groups are dealt longest first
 constexpr int kDealt16 = 4;          // cut contractions: tiles that are dealt ahead
 constexpr int kMaxGroups16 = 2047;   // boundaries and first tiles of this many groups lie in shared memory
 
@@ -58,9 +58,10 @@ struct Cfg16 {
     static constexpr int kTmemCols = 2 * BN;
     static constexpr int kOperands = kStages * (kABytes + kBBytes);
     static constexpr int kTail = 512;                                       // barriers, tensor memory's address, abort flag
-    static constexpr int kTables = 2 * (kMaxGroups16 + 1) * 4;              // row groups and cut contractions only
+    static constexpr int kTables = 3 * (kMaxGroups16 + 1) * 4 + kMaxSorted16 * 2;              // row groups and cut contractions only
     __host__ __device__ static constexpr int staging(int epi) { return epi == EPI16_STORE || epi == EPI16_SUM ? 4096 : 8192; }   // of an epilogue warp: one box, or an upper and a lower one
     static constexpr int smem(int tiles, int epi) { return 1024 + kOperands + 8 * staging(epi) + kTail + (tiles <= TILES_CUT ? kTables : 0); }
+    static constexpr int64_t kPlaceBytes = (int64_t)CTAS * kRows16 * BN * 4;   // of a part's accumulator
     static_assert(1024 + kOperands + 8 * 4096 + kTail + kTables <= 227 * 1024 && (BN == 64 || 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024), "shared memory budget");
 };
 
@@ -74,6 +75,11 @@ struct Gemm16Params {
     const int64_t *offsets;          // TILES_ROWS, TILES_CUT: batch + 1 boundaries; NULL: one group of all rows
     int64_t total_rows;              // rows that the boundaries are held to
     uint32_t *status;
+    // Contractions in parts (TILES_CUT, EPI16_GRAM): a part's accumulator goes to `partial`, and who comes last to a tile, by its counter, adds up
+    // the parts in their order.  NULL: no parts.
+    int32_t part_stages;             // stages of a part
+    float *partial;                  // [part][CTA of the tile][warp][column][row]
+    uint32_t *counters;              // of a tile's warps; 0 between kernels
     int32_t admit;                   // the next kernel may set up beside this one (it is one of the same call)
     // EPI16_STORE, EPI16_SUM
     void *c;
@@ -98,6 +104,8 @@ struct Maps16 {
 struct Tile16 {
     int32_t batch, a_row, b_row, k0, k_len;    // where the operands start along M and N, where the contraction starts and how long it is
     int32_t row, col, rows, rows_peer;         // first output row and column of this CTA's half, its valid rows and the other CTA's
+    int32_t s0, s1, k_stages;                  // its stages (a part of all), and those of one pass over the contraction
+    int32_t parts, slot0, counter;             // parts of the contraction; where the first one's accumulator goes; the tile's counter
     bool mirror;                               // TILES_SYM: below the diagonal, so the transposed tile is written too
 };
 
@@ -235,18 +243,31 @@ __device__ __forceinline__ int find_group16(const int32_t *first, int n, int til
     return lo;
 }
 
+// Parts that a contraction of `stages` stages is cut into.
+__device__ __forceinline__ int parts16(const Gemm16Params &p, int stages) { return p.partial && stages > p.part_stages ? (stages + p.part_stages - 1) / p.part_stages : 1; }
+
+// slots: TILES_CUT: places for accumulators that the groups before a group take, counted in tiles' parts.
 template <int TILES, int CTAS, int BN>
-__device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int m_tiles, const int32_t *start, const int32_t *first, int rank)
+__device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int m_tiles, int passes, const int32_t *start, const int32_t *first, const int32_t *slots,
+                                           const uint16_t *order, int rank)
 {
-    constexpr int kRows = Cfg16<CTAS, BN>::kRows, kBM = kRows * CTAS, kBRows = Cfg16<CTAS, BN>::kBRows;
+    constexpr int kRows = Cfg16<CTAS, BN>::kRows, kBM = kRows * CTAS, kBRows = Cfg16<CTAS, BN>::kBRows, kK = Cfg16<CTAS, BN>::kK;
     Tile16 t;
-    int mt, nt;
+    int mt, nt, part = 0;
     t.batch = 0;
     t.mirror = false;
+    t.k0 = 0;
+    t.k_len = p.k;
+    t.parts = 1;
+    t.slot0 = t.counter = 0;
     if (TILES == TILES_SYM) {
+        t.parts = parts16(p, passes * ((p.k + kK - 1) / kK));
+        t.counter = tile / t.parts;
+        part = tile - t.counter * t.parts;
+        t.slot0 = tile - part;
         const int per = m_tiles * (m_tiles + 1) / 2;
-        t.batch = tile / per;
-        const int r = tile - t.batch * per;
+        t.batch = t.counter / per;
+        const int r = t.counter - t.batch * per;
         mt = (int)((sqrtf(8.0f * (float)r + 1.0f) - 1.0f) * 0.5f);
         while (mt * (mt + 1) / 2 > r) mt--;
         while ((mt + 1) * (mt + 2) / 2 <= r) mt++;
@@ -254,7 +275,22 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
         t.mirror = mt != nt;
     } else {
         int r = tile;
-        if (TILES != TILES_ROWS) {
+        if (TILES == TILES_CUT) {
+            const int per = m_tiles * p.n_tiles, at = p.partial ? find_group16(first, p.batch, tile) : tile / per;
+            t.batch = order ? order[at] : at;
+            t.k0 = start[t.batch];
+            t.k_len = group_rows(start, t.batch);
+            r = tile - (p.partial ? first[at] : at * per);
+            if (p.partial) {
+                t.parts = parts16(p, (t.k_len + kK - 1) / kK);
+                const int in_group = r / t.parts;
+                part = r - in_group * t.parts;
+                t.slot0 = slots[at] + in_group * t.parts;
+                t.counter = t.slot0;   // no two tiles start in one place
+                r = in_group;
+            }
+        }
+        if (TILES == TILES_BATCH) {
             const int per = m_tiles * p.n_tiles;
             t.batch = tile / per;
             r = tile - t.batch * per;
@@ -265,8 +301,6 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
     }
     t.col = nt * BN;
     t.b_row = t.col + rank * kBRows;
-    t.k0 = 0;
-    t.k_len = p.k;
     int valid;   // rows of the whole tile
     if (TILES == TILES_ROWS) {
         t.batch = find_group16(first, p.batch, mt);
@@ -277,14 +311,18 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
         t.row = mt * kBM;
         valid = p.m - t.row;
     }
-    if (TILES == TILES_CUT && p.deals && p.batch <= kMaxSorted16) t.batch = first[t.batch];
-    if (TILES == TILES_CUT) { t.k0 = start[t.batch]; t.k_len = group_rows(start, t.batch); }
     t.row += rank * kRows;
     t.a_row = t.row;
     t.rows = max(0, min(kRows, valid - rank * kRows));
     t.rows_peer = CTAS == 2 ? max(0, min(kRows, valid - (1 - rank) * kRows)) : 0;
+    t.k_stages = (t.k_len + kK - 1) / kK;
+    t.s0 = part * p.part_stages;
+    t.s1 = t.parts == 1 ? passes * t.k_stages : min(t.s0 + p.part_stages, passes * t.k_stages);
     return t;
 }
+// A stage's pass over the contraction (operands in two parts), and where it starts in it.
+template <bool SPLITS>
+__device__ __forceinline__ int pass16(const Tile16 &t, int s) { return SPLITS ? (s >= t.k_stages) + (s >= 2 * t.k_stages) : 0; }
 
 // ---------------------------------------------------------------------------------------- epilogues: 32 columns of a thread's row
 
@@ -402,7 +440,8 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 52);
     volatile uint32_t *abort_flag = tmem_slot + 1;
     int32_t *shared_tiles = reinterpret_cast<int32_t *>(tmem_slot + 2);
-    int32_t *start = reinterpret_cast<int32_t *>(reinterpret_cast<uint8_t *>(bars) + C::kTail), *first = start + kMaxGroups16 + 1;
+    int32_t *start = reinterpret_cast<int32_t *>(reinterpret_cast<uint8_t *>(bars) + C::kTail), *first = start + kMaxGroups16 + 1, *slots = first + kMaxGroups16 + 1;
+    uint16_t *order = reinterpret_cast<uint16_t *>(slots + kMaxGroups16 + 1);
     int32_t *dealt = shared_tiles + 1;   // kDealt16 tiles
     static_assert(kStages <= 8 && 52 * 8 + 16 + 4 * kDealt16 <= C::kTail, "barriers");
 
@@ -522,7 +561,9 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         }
         __syncthreads();
         if (TILES == TILES_ROWS) m_tiles = *shared_tiles;
-        if (deals && p.batch <= kMaxSorted16) {   // first: the groups' order
+        // The groups longest first, then the parts of tiles before each.
+        if (!deals || p.batch > kMaxSorted16) order = nullptr;
+        if (TILES == TILES_CUT && order) {
             for (int g = threadIdx.x; g < p.batch; g += kThreads16) {
                 const int len = group_rows(start, g);
                 int place = 0;
@@ -530,16 +571,41 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     const int other = group_rows(start, h);
                     place += other > len || (other == len && h < g);
                 }
-                first[place] = g;
+                order[place] = (uint16_t)g;
+            }
+            __syncthreads();
+        }
+        if (TILES == TILES_CUT && p.partial) {
+            if (warp == 4) {
+                const int run = (p.batch + 31) / 32, g0 = min(lane * run, p.batch), last = min(g0 + run, p.batch), each = m_tiles * p.n_tiles;
+                int units = 0, places = 0;
+                for (int i = g0; i < last; i++) {
+                    const int parts = parts16(p, (group_rows(start, order ? order[i] : i) + C::kK - 1) / C::kK);
+                    first[i] = units;
+                    slots[i] = places;
+                    units += parts * each;
+                    if (parts > 1) places += parts * each;
+                }
+                int units_before = units, places_before = places;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int u = __shfl_up_sync(0xFFFFFFFFu, units_before, d), v = __shfl_up_sync(0xFFFFFFFFu, places_before, d);
+                    if (lane >= d) { units_before += u; places_before += v; }
+                }
+                if (lane == 31) *shared_tiles = units_before;
+                units_before -= units;
+                places_before -= places;
+                for (int i = g0; i < last; i++) { first[i] += units_before; slots[i] += places_before; }
             }
             __syncthreads();
         }
     }
-    const int tiles = TILES == TILES_ROWS ? m_tiles * p.n_tiles : TILES == TILES_SYM ? p.batch * (m_tiles * (m_tiles + 1) / 2) : p.batch * m_tiles * p.n_tiles;
+    const int passes = kSplits && p.split ? 3 : 1;   // upper x upper, upper x lower, lower x upper
+    const int tiles = TILES == TILES_ROWS ? m_tiles * p.n_tiles : TILES == TILES_CUT && p.partial ? *shared_tiles : TILES <= TILES_BATCH ? p.batch * m_tiles * p.n_tiles
+                      : p.batch * (m_tiles * (m_tiles + 1) / 2) * parts16(p, passes * ((p.k + C::kK - 1) / C::kK));   // or parts of tiles
     const int tile0 = blockIdx.x / CTAS, step = gridDim.x / CTAS;
-    // Cut contractions differ in length: the tiles are dealt to the CTAs or pairs as these fall free, longest groups first (128 groups with loads of
-    // 302 to 15157 rows: dealt round in order, the last pair would have 1.4 times the average of stages, longest first in turn 1.16
-    // times).  Which CTA has a tile changes nothing in its result.
+    // Cut contractions differ in length: the tiles are dealt to the CTAs or pairs as these fall free (128 groups with loads of 302 to 15157 rows:
+    // dealt round in turn, the last pair would have 1.4 times the average of stages).  Which CTA has a tile changes nothing in its result.
     Ring16<kDealt16> deal;
     const uint32_t bar_dealt = smem_u32(bars + 44), bar_taken = smem_u32(bars + 48);
     auto next_tile = [&](int tile) {   // the tile after `tile` of this CTA or pair (a warp's first: tile = -1); tiles or more: no more
@@ -554,7 +620,6 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         deal.next();
         return t;
     };
-    const int passes = kSplits && p.split ? 3 : 1;   // upper x upper, upper x lower, lower x upper
     if (p.admit) admit_successor();
 
     if (warp == 0 || warp == 3) {
@@ -567,54 +632,53 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         const bool issuer = elect_one();
         const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b), lead = CTAS == 2 ? cluster_addr(bar_full, 0) : bar_full;
         for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
-            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
+            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, passes, start, first, slots, order, rank);
             const int a_copies = A_MN ? 2 : (t.rows + p.a_box - 1) / p.a_box;
             const uint32_t a_copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
             const uint32_t box_bytes = (uint32_t)a_copies * a_copy_bytes + (uint32_t)C::kBBox;   // of this CTA
             const uint32_t peer_bytes = CTAS == 2 ? (uint32_t)(A_MN ? 2 : (t.rows_peer + p.a_box - 1) / p.a_box) * a_copy_bytes + (uint32_t)C::kBBox : 0u;
             // TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack
             const int az = TILES <= TILES_CUT ? 0 : t.batch, bz = TILES == TILES_CUT ? 0 : t.batch;
-            for (int pass = 0; ok && pass < passes; pass++) {
+            for (int s = t.s0; s < t.s1; s++, ring.next()) {
+                const int pass = pass16<kSplits>(t, s), k = (s - pass * t.k_stages) * C::kK;
                 const CUtensorMap *mapA = kSplits && pass == 2 ? &maps.a2 : &maps.a, *mapB = kSplits && pass == 1 ? &maps.b2 : &maps.b;
-                for (int k = 0; k < t.k_len; k += C::kK, ring.next()) {
-                    if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) { ok = false; break; }
-                    issued++;
-                    // A stage with rows behind its group's end lands on a barrier of its own in each CTA, where warp 2 waits for it.
-                    const int left = t.k_len - k;
-                    const bool cut = TILES == TILES_CUT && left < C::kK;
-                    if (issuer) {
-                        const int boxes = C::kBoxes == 1 || left > kBox16 ? C::kBoxes : 1;
-                        const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * ring.slot, bar = CTAS == 2 && !cut ? lead + 8 * ring.slot : own_bar;
-                        if (a_side && (rank == 0 || cut)) mbar_arrive_expect_tx(own_bar, (uint32_t)boxes * (box_bytes + (cut ? 0u : peer_bytes)));
-                        if (withhold == 0u || !a_side || ++loads != withhold) {
-                            auto load = [&](uint32_t dst, const CUtensorMap *map, int x, int y, int z) {
-                                if (CTAS == 2 && !cut) tma_load_3d_pair(dst, map, x, y, z, bar);
-                                else tma_load_3d(dst, map, x, y, z, bar);
-                            };
+                if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) { ok = false; break; }
+                issued++;
+                // A stage with rows behind its group's end lands on a barrier of its own in each CTA, where warp 2 waits for it.
+                const int left = t.k_len - k;
+                const bool cut = TILES == TILES_CUT && left < C::kK;
+                if (issuer) {
+                    const int boxes = C::kBoxes == 1 || left > kBox16 ? C::kBoxes : 1;
+                    const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * ring.slot, bar = CTAS == 2 && !cut ? lead + 8 * ring.slot : own_bar;
+                    if (a_side && (rank == 0 || cut)) mbar_arrive_expect_tx(own_bar, (uint32_t)boxes * (box_bytes + (cut ? 0u : peer_bytes)));
+                    if (withhold == 0u || !a_side || ++loads != withhold) {
+                        auto load = [&](uint32_t dst, const CUtensorMap *map, int x, int y, int z) {
+                            if (CTAS == 2 && !cut) tma_load_3d_pair(dst, map, x, y, z, bar);
+                            else tma_load_3d(dst, map, x, y, z, bar);
+                        };
 #pragma unroll
-                            for (int i = 0; i < C::kBoxes; i++) {
-                                if (i >= boxes) break;
-                                const uint32_t a = a0 + ring.slot * C::kABytes + i * C::kABox, b = b0 + ring.slot * C::kBBytes + i * C::kBBox;
-                                const int at = t.k0 + k + i * kBox16;
-                                if (!a_side) {
-                                } else if (A_MN) {
+                        for (int i = 0; i < C::kBoxes; i++) {
+                            if (i >= boxes) break;
+                            const uint32_t a = a0 + ring.slot * C::kABytes + i * C::kABox, b = b0 + ring.slot * C::kBBytes + i * C::kBBox;
+                            const int at = t.k0 + k + i * kBox16;
+                            if (!a_side) {
+                            } else if (A_MN) {
 #pragma unroll
-                                    for (int j = 0; j < 2; j++) load(a + j * 8192, mapA, t.a_row + 64 * j, at, az);
-                                } else {
-                                    for (int j = 0; j < a_copies; j++) load(a + j * a_copy_bytes, mapA, at, t.a_row + j * p.a_box, az);
-                                }
-                                if (a_side) {
-                                } else if (B_MN) {
+                                for (int j = 0; j < 2; j++) load(a + j * 8192, mapA, t.a_row + 64 * j, at, az);
+                            } else {
+                                for (int j = 0; j < a_copies; j++) load(a + j * a_copy_bytes, mapA, at, t.a_row + j * p.a_box, az);
+                            }
+                            if (a_side) {
+                            } else if (B_MN) {
 #pragma unroll
-                                    for (int j = 0; j < C::kBRows / 64; j++) load(b + j * 8192, mapB, t.b_row + 64 * j, at, bz);
-                                } else {
-                                    load(b, mapB, at, t.b_row, bz);
-                                }
+                                for (int j = 0; j < C::kBRows / 64; j++) load(b + j * 8192, mapB, t.b_row + 64 * j, at, bz);
+                            } else {
+                                load(b, mapB, at, t.b_row, bz);
                             }
                         }
                     }
-                    __syncwarp();
                 }
+                __syncwarp();
             }
             if (!ok) break;
         }
@@ -632,41 +696,40 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         const uint64_t a_desc0 = A_MN ? smem_desc_mn_sw128(smem_u32(smem_a)) : smem_desc_sw128(smem_u32(smem_a));
         const uint64_t b_desc0 = B_MN ? smem_desc_mn_sw128(smem_u32(smem_b)) : smem_desc_sw128(smem_u32(smem_b));
         for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
-            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
+            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, passes, start, first, slots, order, rank);
             uint32_t d = 0;
-            for (int pass = 0; ok && pass < passes; pass++) {
-                for (int k = 0; k < t.k_len; k += C::kK) {
-                    const int left = t.k_len - k;
-                    const bool opens = EPI == EPI16_SUM ? k % kSumElems == 0 : k == 0 && pass == 0;
-                    const bool closes = EPI == EPI16_SUM ? left <= C::kK || (k + C::kK) % kSumElems == 0 : left <= C::kK && pass == passes - 1;
-                    if (opens) {
-                        if (!acc_ready && !warp_wait<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u)) { ok = false; break; }
-                        d = tmem + acc.slot * BN;
-                    }
-                    if (!ready && !warp_wait<kPeerFills>(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot)) { ok = false; break; }
-                    const uint32_t slot = ring.slot;
-                    ring.next();
-                    // Looked at before this stage is issued: afterwards the look would wait for the MMAs.
-                    ready = warp_test<kPeerFills>(bar_full + 8 * ring.slot, ring.phase);
-                    const uint32_t acc_bar = 8 * acc.slot;
-                    if (closes) {
-                        acc.next();
-                        acc_ready = warp_test<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u);
-                    }
-                    tcgen05_fence_after();
-                    if (issuer) {
-#pragma unroll
-                        for (int j = 0; j < 4 * C::kBoxes; j++) {
-                            constexpr int kAStep = A_MN ? 2048 : 32, kBStep = B_MN ? 2048 : 32;
-                            const uint64_t ad = a_desc0 + (uint64_t)((slot * C::kABytes + (j / 4) * C::kABox + (j % 4) * kAStep) >> 4);
-                            const uint64_t bd = b_desc0 + (uint64_t)((slot * C::kBBytes + (j / 4) * C::kBBox + (j % 4) * kBStep) >> 4);
-                            if (16 * j < left) tcgen05_mma_f16<CTAS>(d, ad, bd, idesc, !opens || j > 0);
-                        }
-                        tcgen05_commit<CTAS>(bar_empty + 8 * slot);
-                        if (closes) tcgen05_commit<CTAS>(bar_acc_full + acc_bar);
-                    }
-                    __syncwarp();
+            for (int s = t.s0; s < t.s1; s++) {
+                const int left = t.k_len - (s - pass16<kSplits>(t, s) * t.k_stages) * C::kK, n = s - t.s0;
+                constexpr int kChunk = kSumElems / C::kK;
+                const bool opens = EPI == EPI16_SUM ? n % kChunk == 0 : n == 0;
+                const bool closes = s == t.s1 - 1 || (EPI == EPI16_SUM && n % kChunk == kChunk - 1);
+                if (opens) {
+                    if (!acc_ready && !warp_wait<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u)) { ok = false; break; }
+                    d = tmem + acc.slot * BN;
                 }
+                if (!ready && !warp_wait<kPeerFills>(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot)) { ok = false; break; }
+                const uint32_t slot = ring.slot;
+                ring.next();
+                // Looked at before this stage is issued: afterwards the look would wait for the MMAs.
+                ready = warp_test<kPeerFills>(bar_full + 8 * ring.slot, ring.phase);
+                const uint32_t acc_bar = 8 * acc.slot;
+                if (closes) {
+                    acc.next();
+                    acc_ready = warp_test<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u);
+                }
+                tcgen05_fence_after();
+                if (issuer) {
+#pragma unroll
+                    for (int j = 0; j < 4 * C::kBoxes; j++) {
+                        constexpr int kAStep = A_MN ? 2048 : 32, kBStep = B_MN ? 2048 : 32;
+                        const uint64_t ad = a_desc0 + (uint64_t)((slot * C::kABytes + (j / 4) * C::kABox + (j % 4) * kAStep) >> 4);
+                        const uint64_t bd = b_desc0 + (uint64_t)((slot * C::kBBytes + (j / 4) * C::kBBox + (j % 4) * kBStep) >> 4);
+                        if (16 * j < left) tcgen05_mma_f16<CTAS>(d, ad, bd, idesc, !opens || j > 0);
+                    }
+                    tcgen05_commit<CTAS>(bar_empty + 8 * slot);
+                    if (closes) tcgen05_commit<CTAS>(bar_acc_full + acc_bar);
+                }
+                __syncwarp();
             }
             if (!ok) break;
         }
@@ -716,10 +779,13 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             return t;
         };
         for (int tile = my_tile(-1); tile < tiles; tile = my_tile(tile)) {
-            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
-            const int whole = t.k_len / C::kK, left = t.k_len - whole * C::kK;
-            slot = (slot + whole) % kStages;
-            if (left == 0) continue;
+            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, passes, start, first, slots, order, rank);
+            const int left = t.k_len - (t.s1 - 1) * C::kK;   // rows of the last stage
+            if (t.s1 == t.s0 || left >= C::kK) {
+                slot = (slot + t.s1 - t.s0) % kStages;
+                continue;
+            }
+            slot = (slot + t.s1 - t.s0 - 1) % kStages;
             const uint32_t parity = (phases >> slot) & 1u;
             phases ^= 1u << slot;
             if (!warp_wait(bar_cut + 8 * slot, parity, abort_flag, p.status, limit, 0x500u + slot)) break;
@@ -751,9 +817,9 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         Ring16<2> acc;
         uint32_t box_phase = 0;
         for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
-            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, start, first, rank);
+            const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, passes, start, first, slots, order, rank);
             const int in = 32 * quarter + lane;
-            const int chunks = EPI == EPI16_SUM ? (t.k_len + kSumElems - 1) / kSumElems : t.k_len > 0;   // accumulators of the tile
+            const int elems = (t.s1 - t.s0) * C::kK, chunks = EPI == EPI16_SUM ? (elems + kSumElems - 1) / kSumElems : elems > 0;   // accumulators of the tile
             const uint64_t acc_limit = limit * (uint64_t)(1 + (t.k_len >> 8));
             const uint32_t from = tmem + half * kCols + ((uint32_t)(32 * quarter) << 16);
             const int col0 = t.col + half * kCols, row0 = t.row + 32 * quarter, rows = t.rows - 32 * quarter;   // this warp's first column and row, its rows
@@ -770,6 +836,37 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     else mbar_arrive(bar);
                 }
                 __syncwarp();
+            };
+            // Parts: this one's accumulator, columns c and up, goes to its place; the sum of all parts comes from there.
+            constexpr bool kParts = TILES == TILES_CUT || EPI == EPI16_GRAM;
+            const int64_t place = kParts ? ((int64_t)(t.slot0 * CTAS + rank) * 8 + (warp - 4)) * (32 * kCols) + lane : 0;
+            constexpr int64_t kPlace = (int64_t)CTAS * 8 * 32 * kCols;
+            auto put_part = [&](const float *v, int c, int n) {
+                float *to = p.partial + place + (t.s0 / p.part_stages) * kPlace + 32 * c;
+#pragma unroll
+                for (int e = 0; e < n; e++) to[32 * e] = v[e];
+            };
+            auto add_parts = [&](float *v, int c, int n) {
+                const float *from = p.partial + place + 32 * c;
+#pragma unroll
+                for (int e = 0; e < n; e++) v[e] = __ldcg(from + 32 * e);
+                for (int i = 1; i < t.parts; i++) {
+#pragma unroll
+                    for (int e = 0; e < n; e++) v[e] += __ldcg(from + i * kPlace + 32 * e);
+                }
+            };
+            auto last_part = [&]() {   // whether all the others have been put
+                __threadfence();
+                __syncwarp();
+                uint32_t before = 0;
+                if (lane == 0) {
+                    uint32_t *counter = p.counters + (t.counter * CTAS + rank) * 8 + warp - 4;
+                    before = atomicAdd(counter, 1u);
+                    if (before == (uint32_t)t.parts - 1u) *counter = 0u;
+                }
+                before = __shfl_sync(0xFFFFFFFFu, before, 0);
+                __threadfence();
+                return before == (uint32_t)t.parts - 1u;
             };
             // A box leaves.  Rows of a group's last box, which shares its rows with the next group, and a row's last bytes leave by themselves.
             auto send = [&](const uint32_t *w, const float *v, int col) {
@@ -821,6 +918,11 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     release();
                 }
                 if (!ok) break;
+                if (kParts && t.parts > 1) {
+                    put_part(sum, 0, kCols);
+                    if (!last_part()) continue;
+                    add_parts(sum, 0, kCols);
+                }
                 if (chunks > 0 || !p.accumulate) {
 #pragma unroll
                     for (int c = 0; c < kCols; c += kChunk) send(reinterpret_cast<const uint32_t *>(sum) + c, sum + c, col0 + c);
@@ -845,11 +947,25 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 tcgen05_fence_after();
             }
             bool ok = true;
+            if (kParts && t.parts > 1) {
+#pragma unroll 1
+                for (int c = 0; c < kCols; c += 32) {
+                    uint32_t v[32];
+                    FP4Q_TMEM_LD_X32(from + acc.slot * BN + c, v);
+                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                    if (c == kCols - 32) release();
+                    put_part(reinterpret_cast<const float *>(v), c, 32);
+                }
+                acc.next();
+                if (!last_part()) continue;
+            }
 #pragma unroll 1
             for (int c = 0; c < kCols; c += kChunk) {
                 uint32_t v[kChunk];
                 const int col = col0 + c;
-                if (chunks > 0) {
+                if (kParts && t.parts > 1) {
+                    add_parts(reinterpret_cast<float *>(v), c, kChunk);
+                } else if (chunks > 0) {
 #pragma unroll
                     for (int e = 0; e < kChunk; e += 32) FP4Q_TMEM_LD_X32(from + acc.slot * BN + c + e, (v + e));
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -952,7 +1068,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 if (c + kChunk < kCols) fetch(col + kChunk);
             }
             if (!ok) break;
-            if (chunks > 0) acc.next();
+            if (chunks > 0 && !(kParts && t.parts > 1)) acc.next();
         }
         // The stores have read shared memory; what they write is there when the grid has completed.
         boxes_free(lane);

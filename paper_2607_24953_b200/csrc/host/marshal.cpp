@@ -44,6 +44,7 @@ struct Entry {
     decltype(&fp4q_ragged_gemm_fwd) ragged_gemm_fwd;
     decltype(&fp4q_ragged_gemm_dgrad) ragged_gemm_dgrad;
     decltype(&fp4q_ragged_gemm_wgrad) ragged_gemm_wgrad;
+    decltype(&fp4q_ragged_gemm_wgrad_scratch_bytes) ragged_gemm_wgrad_scratch_bytes;
     decltype(&fp4q_newton_schulz) newton_schulz;
     decltype(&fp4q_newton_schulz_scratch_bytes) newton_schulz_scratch_bytes;
 } lib;
@@ -531,10 +532,10 @@ void same_device(const at::Tensor &t, const at::Tensor &like, const char *name)
     throw PyError();
 }
 
-// which (0 fwd, 1 dgrad, 2 wgrad), a (x or dY), b (w or x), row_offsets | None, out | None, dt, accumulate, ws | None, stream
+// which (0 fwd, 1 dgrad, 2 wgrad), a (x or dY), b (w or x), row_offsets | None, out | None, dt, accumulate, scratch | None, ws | None, stream
 PyObject *ragged_gemm(Args a, Py_ssize_t n)
 {
-    want(n, 9);
+    want(n, 10);
     static const char *const names[3] = {"fp4q_ragged_gemm_fwd", "fp4q_ragged_gemm_dgrad", "fp4q_ragged_gemm_wgrad"};
     static const char *const operands[3][2] = {{"x", "w"}, {"dY", "w"}, {"dY", "x"}};
     const int which = as_int(a[0]), dt = as_int(a[5]), accumulate = as_bool(a[6]) ? 1 : 0;
@@ -551,7 +552,7 @@ PyObject *ragged_gemm(Args a, Py_ssize_t n)
     if (dt != FP4Q_OUT_BF16 && dt != FP4Q_OUT_F32) value_error("dt must be OUT_BF16 or OUT_F32");
     const int64_t rows = which == 2 ? x.size(1) * groups : x.size(0), cols = which == 0 ? y.size(0) / groups : y.size(1);
     const c10::cuda::CUDAGuard device(x.device());
-    const OnStream on(a[8], &x);
+    const OnStream on(a[9], &x);
     const bool ours = a[4] == Py_None;
     const at::Tensor out = ours ? out_buffer(on, rows, cols, dt, x) : as_tensor(a[4]);
     if (ours && accumulate) { Unlock u; out.zero_(); }
@@ -561,12 +562,23 @@ PyObject *ragged_gemm(Args a, Py_ssize_t n)
             (out.numel() && out.stride(1) != 1 && cols > 1))
             value_error("out must be a 2-D tensor of the result's shape and of the type that dt names, with contiguous rows");
     }
-    const at::Tensor ws = workspace(a[7], x);
+    at::Tensor scratch;
+    if (a[7] != Py_None) {
+        scratch = as_tensor(a[7]);
+        same_device(scratch, x, "scratch");
+        if (!scratch.is_contiguous()) value_error("scratch must be contiguous");
+    } else if (which == 2) {
+        const int64_t bytes = (int64_t)lib.ragged_gemm_wgrad_scratch_bytes(x.size(0), x.size(1), y.size(1), (int32_t)groups);
+        Unlock u;
+        if (bytes) scratch = at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(x.device()));
+    }
+    const at::Tensor ws = workspace(a[8], x);
     const int64_t ld = out_pitch(out, cols);
     const fp4q_out type = (fp4q_out)(ours && which < 2 ? dt | FP4Q_OUT_ZERO_REST : dt);   // fresh memory holds anything
     const fp4q_status s =
         which == 2   ? unlocked(lib.ragged_gemm_wgrad, x.data_ptr(), x.size(0), x.size(1), pitch(x), y.data_ptr(), y.size(1), pitch(y), out.data_ptr(), ld, type, accumulate,
-                                g.ptr, ws.data_ptr(), (size_t)ws.numel(), on.handle)
+                                g.ptr, scratch.defined() ? scratch.data_ptr() : nullptr, scratch.defined() ? (size_t)scratch.nbytes() : 0, ws.data_ptr(),
+                                (size_t)ws.numel(), on.handle)
         : which == 1 ? unlocked(lib.ragged_gemm_dgrad, x.data_ptr(), x.size(0), x.size(1), pitch(x), y.data_ptr(), y.size(0), y.size(1), pitch(y), out.data_ptr(), ld, type, g.ptr,
                                 ws.data_ptr(), (size_t)ws.numel(), on.handle)
                      : unlocked(lib.ragged_gemm_fwd, x.data_ptr(), x.size(0), x.size(1), pitch(x), y.data_ptr(), y.size(0), pitch(y), out.data_ptr(), ld, type, g.ptr, ws.data_ptr(),
@@ -815,6 +827,7 @@ PyObject *init(Args a, Py_ssize_t n)
     set_entry(a[0], "fp4q_ragged_gemm_fwd", lib.ragged_gemm_fwd);
     set_entry(a[0], "fp4q_ragged_gemm_dgrad", lib.ragged_gemm_dgrad);
     set_entry(a[0], "fp4q_ragged_gemm_wgrad", lib.ragged_gemm_wgrad);
+    set_entry(a[0], "fp4q_ragged_gemm_wgrad_scratch_bytes", lib.ragged_gemm_wgrad_scratch_bytes);
     set_entry(a[0], "fp4q_newton_schulz", lib.newton_schulz);
     set_entry(a[0], "fp4q_newton_schulz_scratch_bytes", lib.newton_schulz_scratch_bytes);
     Py_XSETREF(g_qtensor, Py_NewRef(a[1]));

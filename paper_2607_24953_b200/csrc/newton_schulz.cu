@@ -23,7 +23,7 @@ using namespace fp4q;
 
 namespace {
 
-constexpr int kNsThreads = 256, kNsUnroll = 4, kNsMaxBlocks = 1024;
+constexpr int kNsThreads = 256, kNsMaxBlocks = 1024;
 constexpr float kScaleX = 1024.0f, kScaleA = 512.0f;
 constexpr int kMaxSteps = 64;
 constexpr int64_t kSplitSide = 384;
@@ -34,60 +34,55 @@ struct MomentumParams {
     int64_t ld_g, ld_m;
     int64_t rows;
     int32_t cols, g_f32, vec_g, vec_m;
-    uint32_t units_row, units;   // units of four columns in a row and in a matrix
+    uint32_t units_row, units;   // units of eight columns in a row and in a matrix
     float beta;
     int32_t nesterov;
     double eps;
     double *partial;             // [count, gridDim.x]
     __half *up, *lo;             // normalised: upper and lower parts
     int64_t pitch;
+    uint32_t *counters;          // of the products' tiles, to be zeroed
+    int32_t n_counters;
 };
 
-__device__ __forceinline__ float4 load_gradient(const MomentumParams &p, int64_t row, int col)
+struct Eight {
+    float v[8];
+};
+__device__ __forceinline__ Eight load_eight(const float *p, bool vec, int left)
 {
-    const int64_t at = row * p.ld_g + col;
-    const int left = p.cols - col;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (p.g_f32) {
-        const float *g = static_cast<const float *>(p.g) + at;
-        if (p.vec_g && left >= 4) return *reinterpret_cast<const float4 *>(g);
-        v.x = g[0];
-        if (left > 1) v.y = g[1];
-        if (left > 2) v.z = g[2];
-        if (left > 3) v.w = g[3];
-    } else {
-        const __nv_bfloat16 *g = static_cast<const __nv_bfloat16 *>(p.g) + at;
-        if (p.vec_g && left >= 4) {
-            const uint2 w = *reinterpret_cast<const uint2 *>(g);
-            return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
-        }
-        v.x = __bfloat162float(g[0]);
-        if (left > 1) v.y = __bfloat162float(g[1]);
-        if (left > 2) v.z = __bfloat162float(g[2]);
-        if (left > 3) v.w = __bfloat162float(g[3]);
+    Eight r;
+    if (vec && left >= 8) {
+        const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+        return Eight{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
     }
-    return v;
+#pragma unroll
+    for (int e = 0; e < 8; e++) r.v[e] = e < left ? p[e] : 0.f;
+    return r;
 }
-__device__ __forceinline__ float4 load_momentum(const MomentumParams &p, int64_t row, int col)
+__device__ __forceinline__ Eight load_eight(const __nv_bfloat16 *p, bool vec, int left)
 {
-    const float *m = p.m + row * p.ld_m + col;
-    const int left = p.cols - col;
-    if (p.vec_m && left >= 4) return *reinterpret_cast<const float4 *>(m);
-    return make_float4(m[0], left > 1 ? m[1] : 0.f, left > 2 ? m[2] : 0.f, left > 3 ? m[3] : 0.f);
+    Eight r;
+    if (vec && left >= 8) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(p);
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; e++) { r.v[2 * e] = __uint_as_float(u[e] << 16); r.v[2 * e + 1] = __uint_as_float(u[e] & 0xFFFF0000u); }
+        return r;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++) r.v[e] = e < left ? __bfloat162float(p[e]) : 0.f;
+    return r;
 }
-__device__ __forceinline__ void store_momentum(const MomentumParams &p, int64_t row, int col, float4 v)
+__device__ __forceinline__ void store_eight(float *p, bool vec, int left, const Eight &x)
 {
-    float *m = p.m + row * p.ld_m + col;
-    const int left = p.cols - col;
-    if (p.vec_m && left >= 4) { *reinterpret_cast<float4 *>(m) = v; return; }
-    m[0] = v.x;
-    if (left > 1) m[1] = v.y;
-    if (left > 2) m[2] = v.z;
-    if (left > 3) m[3] = v.w;
-}
-__device__ __forceinline__ float4 axpy(float a, float4 x, float4 y)
-{
-    return make_float4(fmaf(a, x.x, y.x), fmaf(a, x.y, y.y), fmaf(a, x.z, y.z), fmaf(a, x.w, y.w));
+    if (vec && left >= 8) {
+        *reinterpret_cast<float4 *>(p) = make_float4(x.v[0], x.v[1], x.v[2], x.v[3]);
+        *reinterpret_cast<float4 *>(p + 4) = make_float4(x.v[4], x.v[5], x.v[6], x.v[7]);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        if (e < left) p[e] = x.v[e];
 }
 
 // The block's sum, in an order that depends on nothing but the block's size; every thread gets it.
@@ -106,7 +101,9 @@ __device__ __forceinline__ double block_sum(double v)
 
 // FINISH = false: the momentum, and each block's share of |U|^2.  FINISH = true: the norm, and X = U / (|U| + eps) in two halves.
 // The sum of squares is held in 64 bits: gradients of 1e-25 and 1e25 have squares that FP32 does not.
-template <bool FINISH>
+// UNROLL: units of eight columns that a thread has under way: one in stacks (64 of 768 x 2048, BF16 gradients: 157 and 180 us, with two 199 and 200;
+// 1 GB each), two in a single matrix, whose blocks are fewer (11008 x 4096: 105 and 87 with one, 86 and 85 with two; 541 MB).
+template <bool FINISH, int UNROLL>
 __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumParams p)
 {
     wait_for_predecessor();
@@ -123,51 +120,56 @@ __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumPara
         inv1 = (float)ldexp(inv, -e);
     }
     const uint32_t step = gridDim.x * kNsThreads;
-    for (uint32_t base = blockIdx.x * kNsThreads + threadIdx.x; base < p.units; base += kNsUnroll * step) {
-        float4 g[kNsUnroll], m[kNsUnroll];
-        int64_t row[kNsUnroll];
-        int col[kNsUnroll];
+    for (uint32_t base = blockIdx.x * kNsThreads + threadIdx.x; base < p.units; base += UNROLL * step) {
+        Eight g[UNROLL], m[UNROLL];
+        int64_t row[UNROLL];
+        int col[UNROLL];
 #pragma unroll
-        for (int j = 0; j < kNsUnroll; j++) {
+        for (int j = 0; j < UNROLL; j++) {
             const uint32_t u = base + j * step;
             const uint32_t r = u / p.units_row;
             row[j] = u < p.units ? row0 + r : -1;
-            col[j] = (int)(u - r * p.units_row) * 4;
-            g[j] = m[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (row[j] >= 0) {
-                if (!FINISH || !p.m || p.nesterov) g[j] = load_gradient(p, row[j], col[j]);
-                if (p.m) m[j] = load_momentum(p, row[j], col[j]);
-            }
+            col[j] = (int)(u - r * p.units_row) * 8;
+            if (row[j] < 0) continue;
+            const int left = p.cols - col[j];
+            if (!FINISH || !p.m || p.nesterov)
+                g[j] = p.g_f32 ? load_eight(static_cast<const float *>(p.g) + row[j] * p.ld_g + col[j], p.vec_g, left)
+                               : load_eight(static_cast<const __nv_bfloat16 *>(p.g) + row[j] * p.ld_g + col[j], p.vec_g, left);
+            if (p.m) m[j] = load_eight(p.m + row[j] * p.ld_m + col[j], p.vec_m, left);
         }
 #pragma unroll
-        for (int j = 0; j < kNsUnroll; j++) {
+        for (int j = 0; j < UNROLL; j++) {
             if (row[j] < 0) continue;
-            float4 u = g[j];
+            Eight u = g[j];
             if (p.m) {
                 if (!FINISH) {
-                    m[j] = axpy(p.beta, m[j], g[j]);
-                    store_momentum(p, row[j], col[j], m[j]);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) m[j].v[e] = fmaf(p.beta, m[j].v[e], g[j].v[e]);
+                    store_eight(p.m + row[j] * p.ld_m + col[j], p.vec_m, p.cols - col[j], m[j]);
                 }
-                u = p.nesterov ? axpy(p.beta, m[j], g[j]) : m[j];
+#pragma unroll
+                for (int e = 0; e < 8; e++) u.v[e] = p.nesterov ? fmaf(p.beta, m[j].v[e], g[j].v[e]) : m[j].v[e];
             }
             if (!FINISH) {
-                sum += (double)u.x * u.x + (double)u.y * u.y;
-                sum += (double)u.z * u.z + (double)u.w * u.w;
-            } else {
-                const float x[4] = {u.x * inv0 * inv1, u.y * inv0 * inv1, u.z * inv0 * inv1, u.w * inv0 * inv1};
-                uint32_t up[2], lo[2];
 #pragma unroll
-                for (int e = 0; e < 2; e++) {
-                    up[e] = pack_half(x[2 * e], x[2 * e + 1]);
+                for (int e = 0; e < 8; e++) sum += (double)u.v[e] * u.v[e];
+            } else {
+                uint32_t up[4], lo[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const float x = u.v[2 * e] * inv0 * inv1, y = u.v[2 * e + 1] * inv0 * inv1;
+                    up[e] = pack_half(x, y);
                     const float2 h = unpack_half(up[e]);
-                    lo[e] = pack_half(x[2 * e] - h.x, x[2 * e + 1] - h.y);
+                    lo[e] = pack_half(x - h.x, y - h.y);
                 }
                 const int64_t at = row[j] * p.pitch + col[j];
-                *reinterpret_cast<uint2 *>(p.up + at) = make_uint2(up[0], up[1]);
-                *reinterpret_cast<uint2 *>(p.lo + at) = make_uint2(lo[0], lo[1]);
+                *reinterpret_cast<uint4 *>(p.up + at) = make_uint4(up[0], up[1], up[2], up[3]);
+                *reinterpret_cast<uint4 *>(p.lo + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
             }
         }
     }
+    if (!FINISH && blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = threadIdx.x; i < p.n_counters; i += kNsThreads) p.counters[i] = 0u;
     if (!FINISH) {
         sum = block_sum(sum);
         if (threadIdx.x == 0) p.partial[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
@@ -177,8 +179,10 @@ __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumPara
 // Where things lie in the scratch memory.
 struct Scratch {
     int64_t pitch_x, pitch_a, side;
-    bool split;
-    size_t partial, x[2], lo[2], a[2], poly[2], bytes;   // upper and lower parts; X and the next X: lower parts in one place unless they are operands
+    bool split, pairs;
+    // Few tiles with a long contraction, as A of a short side has them: parts of no less than 16 stages, as many as there are CTAs or pairs for.
+    int64_t tiles, part_stages;
+    size_t counters, accumulators, partial, x[2], lo[2], a[2], poly[2], bytes;   // upper and lower parts; X and the next X: lower parts in one place unless they are operands
     Scratch(int64_t count, int64_t rows, int64_t cols)
     {
         side = rows < cols ? rows : cols;
@@ -193,6 +197,13 @@ struct Scratch {
         lo[0] = place(x_bytes); lo[1] = split ? place(x_bytes) : lo[0];
         a[0] = place(a_bytes); a[1] = split ? place(a_bytes) : a[0];
         poly[0] = place(a_bytes); poly[1] = split ? place(a_bytes) : poly[0];
+        pairs = side > 128;
+        const int64_t edge = pairs ? 256 : 128, slots = pairs ? 74 : 148, stages = (split ? 3 : 1) * ceil_div(rows < cols ? cols : rows, kBox16);
+        tiles = count * (ceil_div(side, edge) * (ceil_div(side, edge) + 1) / 2);
+        const int64_t parts = std::min(slots / std::min(tiles, slots), stages / 16);
+        part_stages = parts >= 2 ? ceil_div(stages, parts) : 0;
+        counters = place(part_stages ? (size_t)round_up(tiles * 2 * 8 * 4, 256) : 0);
+        accumulators = place(part_stages ? (size_t)(tiles * parts * (pairs ? Cfg16<2, 256>::kPlaceBytes : Cfg16<1, 128>::kPlaceBytes)) : 0);
     }
 };
 
@@ -200,7 +211,7 @@ const int64_t kMaxSide = 1 << 20, kMaxCount = 65535;
 
 bool sizes_ok(int64_t count, int64_t rows, int64_t cols)
 {
-    return count <= kMaxCount && rows <= kMaxSide && cols <= kMaxSide && rows * ceil_div(cols, 4) < (1ll << 31) && count * rows <= 0x7FFFFFFF &&
+    return count <= kMaxCount && rows <= kMaxSide && cols <= kMaxSide && rows * ceil_div(cols, 8) < (1ll << 31) && count * rows <= 0x7FFFFFFF &&
            count * rows * round_up(cols, 16) <= (1ll << 40) && count * ceil_div(rows, 128) * ceil_div(cols, 64) <= 0x7FFFFFFF - 4096;
 }
 
@@ -249,7 +260,8 @@ struct Steps {
     static fp4q_status gram(const Parts &x, const Parts &a, bool tall, Gemm16Params p, cudaStream_t stream)
     {
         Maps16 maps = {};
-        const int64_t tiles = symmetric_tiles(p);
+        int64_t tiles = symmetric_tiles(p);
+        if (p.partial) tiles *= ceil_div((p.split ? 3 : 1) * ceil_div(p.k, kBox16), p.part_stages);
         if (fp4q_status s = boxes16(&maps.out, &maps.out2, a, p.split)) return s;
         if (fp4q_status s = boxes16(&maps.mirror, &maps.mirror2, a, p.split, true)) return s;
         return tall ? launch_gemm16<CTAS, BN, true, true, EPI16_GRAM, TILES_SYM>(x.up, x.up, x.lo, x.lo, maps, p, tiles, stream)
@@ -312,17 +324,19 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     MomentumParams q = {};
     q.g = g; q.m = momentum; q.ld_g = ld_g; q.ld_m = ld_m; q.rows = rows; q.cols = (int32_t)cols;
     q.g_f32 = g_type == FP4Q_OUT_F32;
-    q.vec_g = aligned(g, 4 * g_bytes) && ld_g % 4 == 0;
+    q.vec_g = aligned(g, 16) && ld_g * g_bytes % 16 == 0;
     q.vec_m = momentum && aligned(momentum, 16) && ld_m % 4 == 0;
-    q.units_row = (uint32_t)ceil_div(cols, 4);
+    q.units_row = (uint32_t)ceil_div(cols, 8);
     q.units = (uint32_t)(rows * q.units_row);
     q.beta = beta; q.nesterov = nesterov != 0; q.eps = eps;
     q.partial = reinterpret_cast<double *>(base + at.partial);
+    q.counters = reinterpret_cast<uint32_t *>(base + at.counters);
+    q.n_counters = at.part_stages ? (int32_t)(at.tiles * (at.pairs ? 16 : 8)) : 0;
     q.up = half_at(at.x[0]); q.lo = half_at(at.lo[0]); q.pitch = at.pitch_x;
-    const int64_t want = ceil_div(q.units, kNsThreads * kNsUnroll), share = ceil_div(16 * 148, count);
+    const int64_t want = ceil_div(q.units, kNsThreads * (count > 1 ? 1 : 2)), share = ceil_div(16 * 148, count);
     const dim3 grid((unsigned)std::min<int64_t>(std::min(want, share), kNsMaxBlocks), (unsigned)count);
-    if (fp4q_status st = launched(launch_dependent(momentum_kernel<false>, grid, kNsThreads, s, q, true))) return st;
-    if (fp4q_status st = launched(launch_dependent(momentum_kernel<true>, grid, kNsThreads, s, q, true))) return st;
+    if (fp4q_status st = launched(launch_dependent(count > 1 ? momentum_kernel<false, 1> : momentum_kernel<false, 2>, grid, kNsThreads, s, q, true))) return st;
+    if (fp4q_status st = launched(launch_dependent(count > 1 ? momentum_kernel<true, 1> : momentum_kernel<true, 2>, grid, kNsThreads, s, q, true))) return st;
 
     const bool tall = rows > cols;
     const int64_t side = at.side;
@@ -333,7 +347,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     p.split = at.split;
     p.admit = 1;
     const Parts part_a(half_at(at.a[0]), half_at(at.a[1]), side, side, count, at.pitch_a), part_p(half_at(at.poly[0]), half_at(at.poly[1]), side, side, count, at.pitch_a);
-    const bool pairs = side > 128;
+    const bool pairs = at.pairs;
     for (int32_t i = 0; i < steps; i++) {
         const float *c = coefficients + 3 * i;
         const int now = i & 1, next = now ^ 1;
@@ -344,6 +358,11 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
         gp.k = (int32_t)(tall ? rows : cols);
         gp.fa = kScaleA / (kScaleX * kScaleX);
         Gemm16Params pp = gp;
+        if (at.part_stages) {
+            gp.part_stages = (int32_t)at.part_stages;
+            gp.partial = reinterpret_cast<float *>(base + at.accumulators);
+            gp.counters = reinterpret_cast<uint32_t *>(base + at.counters);
+        }
         pp.k = (int32_t)side;
         pp.fb = c[1];
         pp.fc = c[2] / kScaleA;

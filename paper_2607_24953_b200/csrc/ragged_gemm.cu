@@ -153,8 +153,41 @@ extern "C" fp4q_status fp4q_ragged_gemm_dgrad(const void *dY, int64_t T, int64_t
     return rows_call(1, Matrix16{dY, T, N, ld_dy}, Matrix16{w, w_rows, K, ldw}, dX, ldx, dt, g, ws, ws_bytes, stream);
 }
 
+namespace {
+
+// How a weight gradient is computed: pairs or single CTAs, and the parts that long contractions are cut into: a group of most of the rows has few tiles,
+// which would otherwise leave most of the GPU idle (one group, 131072 rows, 768 x 2048).  A part is half of what a CTA or pair would have to do if all
+// had the same, and no less than 16 stages (below that joining costs what it saves).
+struct CutPlan {
+    bool pairs;
+    int64_t m_tiles, n_tiles, part_stages, places, counter_bytes;
+    size_t bytes = 0;   // 0: no parts
+    CutPlan(int64_t T, int64_t N, int64_t K, int64_t groups, bool parts)
+    {
+        pairs = N > 128 && K > 128 && (parts || groups * ceil_div(N, 256) * ceil_div(K, 256) >= 74);
+        m_tiles = ceil_div(N, pairs ? 256 : 128);
+        n_tiles = ceil_div(K, pairs ? 256 : 128);
+        const int64_t slots = pairs ? 74 : 148, each = m_tiles * n_tiles, stages = ceil_div(T, kBox16);
+        part_stages = std::max<int64_t>(16, round_up(ceil_div(each * (stages + groups / 2), 2 * slots), 8));
+        if (!parts || stages <= part_stages) return;
+        // Groups with more stages than a part: no more than this, and with so many parts.
+        const int64_t longer = std::min(groups, stages / part_stages + 1);
+        places = each * (ceil_div(stages + longer, part_stages) + longer);
+        counter_bytes = round_up(places * (pairs ? 2 : 1) * 8 * 4, 256);
+        bytes = (size_t)(counter_bytes + places * (pairs ? Cfg16<2, 256>::kPlaceBytes : Cfg16<1, 128>::kPlaceBytes));
+    }
+};
+
+}  // namespace
+
+extern "C" size_t fp4q_ragged_gemm_wgrad_scratch_bytes(int64_t T, int64_t N, int64_t K, int32_t n_groups)
+{
+    if (T <= 0 || N <= 0 || K <= 0 || n_groups <= 0 || n_groups > kMaxGroups16 || T > kMaxDim16 || N > kMaxDim16 || K > kMaxDim16) return 0;
+    return CutPlan(T, N, K, n_groups, true).bytes;
+}
+
 extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t N, int64_t ld_dy, const void *x, int64_t K, int64_t ldx, void *dW, int64_t ldw,
-                                              fp4q_out dt, int accumulate, const fp4q_groups *g, void *ws, size_t ws_bytes, void *stream)
+                                              fp4q_out dt, int accumulate, const fp4q_groups *g, void *scratch, size_t scratch_bytes, void *ws, size_t ws_bytes, void *stream)
 {
     const Matrix16 d = {dY, T, N, ld_dy}, m = {x, T, K, ldx};
     if (fp4q_status s = check_groups16(g)) return s;
@@ -169,10 +202,16 @@ extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t
     if (fp4q_status s = check_operand16(d)) return s;
     if (fp4q_status s = check_operand16(m)) return s;
     if (fp4q_status s = check_workspace(ws, ws_bytes)) return s;
-    if (groups * ceil_div(N, 128) * ceil_div(K, 128) > kMaxDim16) return FP4Q_ERR_UNSUPPORTED;
+    if (groups * ceil_div(N, 128) * ceil_div(K, 128) > kMaxDim16 / 2 || ceil_div(N, 128) * ceil_div(K, 128) * ceil_div(T, 1024) > kMaxDim16 / 4) return FP4Q_ERR_UNSUPPORTED;
+    const CutPlan plan(T, N, K, groups, scratch != nullptr);
+    if (scratch && scratch_bytes < plan.bytes) return FP4Q_ERR_WORKSPACE;
+    if (scratch && !aligned(scratch, 256)) return FP4Q_ERR_ALIGN;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
     p.m = (int32_t)N;
     p.n = (int32_t)K;
     p.k = (int32_t)T;
+    p.m_tiles = (int32_t)plan.m_tiles;
+    p.n_tiles = (int32_t)plan.n_tiles;
     p.batch = (int32_t)groups;
     p.bf16 = 1;
     p.a_box = 128;
@@ -181,14 +220,13 @@ extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t
     p.accumulate = accumulate != 0;
     p.deals = groups > 1 && T >= 256 * groups;   // shorter groups: 300 rows in 64 groups 23.5 us in turn, 35.0 dealt
     p.status = static_cast<uint32_t *>(ws);
-    const Operand16 a = T ? operand16(d, T, 1) : Operand16{dW, 8, 1, 1, 8, 8}, b = T ? operand16(m, T, 1) : a;
-    const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (groups * ceil_div(N, 256) * ceil_div(K, 256) >= 74) {
-        p.m_tiles = (int32_t)ceil_div(N, 256);
-        p.n_tiles = (int32_t)ceil_div(K, 256);
-        return launch_store16<2, 256, true, true, TILES_CUT>(a, b, p, dt, groups * p.m_tiles * p.n_tiles, s);
+    if (plan.bytes) {
+        p.part_stages = (int32_t)plan.part_stages;
+        p.counters = static_cast<uint32_t *>(scratch);
+        p.partial = reinterpret_cast<float *>(static_cast<uint8_t *>(scratch) + plan.counter_bytes);
+        if (fp4q_status st = launched(cudaMemsetAsync(scratch, 0, (size_t)plan.counter_bytes, s))) return st;
     }
-    p.m_tiles = (int32_t)ceil_div(N, 128);
-    p.n_tiles = (int32_t)ceil_div(K, 128);
-    return launch_store16<1, 128, true, true, TILES_CUT>(a, b, p, dt, groups * p.m_tiles * p.n_tiles, s);
+    const Operand16 a = T ? operand16(d, T, 1) : Operand16{dW, 8, 1, 1, 8, 8}, b = T ? operand16(m, T, 1) : a;
+    const int64_t most = groups * plan.m_tiles * plan.n_tiles + (plan.bytes ? plan.places : 0);
+    return plan.pairs ? launch_store16<2, 256, true, true, TILES_CUT>(a, b, p, dt, most, s) : launch_store16<1, 128, true, true, TILES_CUT>(a, b, p, dt, most, s);
 }

@@ -40,7 +40,7 @@ def close(got, want, limit=LIMIT):
 
 
 SIZES = [(1, 1), (1, 5), (7, 1), (16, 16), (17, 300), (300, 33), (64, 64), (129, 257), (257, 129), (128, 4096), (1003, 777), (777, 1003), (520, 2048),
-         (2048, 520), (2600, 1100), (1500, 2000)]
+         (2048, 520), (2600, 1100), (1500, 2000), (4751, 63), (20, 9000), (300, 5000)]
 
 
 @pytest.mark.parametrize("rows,cols", SIZES)
@@ -55,7 +55,7 @@ def test_one_matrix(rows, cols):
     assert b.fp4q_workspace_status(ws) == 0
 
 
-@pytest.mark.parametrize("count,rows,cols", [(3, 100, 200), (5, 200, 100), (40, 256, 512), (130, 64, 64), (1, 50, 60), (9, 768, 300)])
+@pytest.mark.parametrize("count,rows,cols", [(3, 100, 200), (5, 200, 100), (40, 256, 512), (130, 64, 64), (1, 50, 60), (9, 768, 300), (30, 40, 1500), (85, 2382, 45)])
 def test_stacks_with_and_without_momentum(count, rows, cols):
     for dtype in (torch.float32, torch.bfloat16):
         for nesterov in (True, False):

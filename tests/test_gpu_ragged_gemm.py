@@ -135,6 +135,30 @@ def test_larger_ones_with_skewed_groups(op, T, n, k, e):
             assert ((z - s).abs() <= bound(s, s, length, dt))[rows].all()
 
 
+@pytest.mark.parametrize("T,n,k,values", [(20000, 200, 300, [0, 20000]), (20000, 100, 72, [0, 7, 15000, 15001, 20000]), (9000, 512, 256, [100, 5000, 9000]),
+                                          (60000, 300, 130, [0, 59000, 59900, 60000]), (3000, 64, 64, [0, 3000])])
+def test_long_contractions_in_parts(T, n, k, values):
+    dy, x = operands("wgrad", T, n, k, len(values) - 1)
+    y, s = reference("wgrad", dy, x, groups(values, T))
+    length = max(j - i for i, j in groups(values, T))
+    scratch = b.alloc_ragged_wgrad_scratch(T, n, k, len(values) - 1, "cuda")
+    assert scratch.numel() > 0
+    for dt in (b.OUT_F32, b.OUT_BF16):
+        scratch.fill_(255)                                  # any contents
+        want = call("wgrad", dy, x, offsets(values), dt=dt, scratch=scratch)
+        assert ((want.double() - y).abs() <= bound(y, s, length, dt)).all()
+        for _ in range(3):                                  # which part comes last changes nothing
+            assert torch.equal(call("wgrad", dy, x, offsets(values), dt=dt, scratch=scratch), want)
+        assert torch.equal(call("wgrad", dy, x, offsets(values), dt=dt), want)
+    out = randn(3, y.shape[0], (k + 3) // 4 * 4 + 4)[:, :k]
+    before = out.clone()
+    call("wgrad", dy, x, offsets(values), out, b.OUT_F32, accumulate=True, scratch=scratch)
+    assert ((out.double() - before.double() - y).abs() <= bound(y + before.double(), s + before.double().abs(), length, b.OUT_F32, adds=True)).all()
+    with pytest.raises(b.Fp4qError) as err:
+        call("wgrad", dy, x, offsets(values), dt=b.OUT_F32, scratch=scratch[:256])
+    assert err.value.status == 5
+
+
 def test_no_groups_at_all_and_one_for_everything():
     a, w = operands("fwd", 300, 96, 200, 1)
     assert torch.equal(call("fwd", a, w, None), call("fwd", a, w, offsets([0, 300])))

@@ -23,7 +23,7 @@ def dgrad(x=P, T=10, N=40, ldx=40, w=P, w_rows=80, K=64, ldw=64, y=P, ldy=64, dt
 
 
 def wgrad(dy=P, T=10, N=40, ldd=40, x=P, K=64, ldx=64, dw=P, ldw=64, dt=1, accumulate=0, g=None, ws=P, wsb=256):
-    return b.lib().fp4q_ragged_gemm_wgrad(dy, T, N, ldd, x, K, ldx, dw, ldw, dt, accumulate, g or groups(), ws, wsb, None)
+    return b.lib().fp4q_ragged_gemm_wgrad(dy, T, N, ldd, x, K, ldx, dw, ldw, dt, accumulate, g or groups(), None, 0, ws, wsb, None)
 
 
 def test_products():
