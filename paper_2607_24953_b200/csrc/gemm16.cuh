@@ -8,7 +8,7 @@
 // in about 0.3 us, as long as the MMAs take at the clock that full load leaves); single CTAs have tiles of 128 x 128 for problems with few
 // tiles, and of 32 x 64 for short groups (the MMAs have 128 rows all the same: those behind the first 32 are whatever lies in shared
 // memory, and nobody looks at them).
-//   warps 0, 3  TMA producers of A and B: a stage is 64 contraction elements (32 x 64 tiles: 128), boxes of 128 bytes with the 128-byte swizzle
+//   warps 0, 3  TMA producers of A and B: a stage is 64 contraction elements (32 x 64 tiles: 256), boxes of 128 bytes with the 128-byte swizzle
 //   warp 1      MMA issuer (in the leader of a pair): four tcgen05.mma of 16 contraction elements per box
 //   warp 2      cut contractions: deals the tiles (in the leader of a pair), zeroes the rows of a group's last stage that lie behind the group
 //   warps 4-11  epilogue: a thread has a row of the tile; the accumulator is double-buffered in tensor memory.  Outputs leave, and what an
@@ -48,13 +48,13 @@ template <int CTAS, int BN>
 struct Cfg16 {
     static_assert(CTAS == 1 || (CTAS == 2 && BN == 256), "tile shapes");
     static constexpr int kBRows = BN / CTAS;
-    // 32 x 64 tiles take 128 cycles of MMAs per box, less than a round of the issuer: their stages are two boxes deep.
-    static constexpr int kBoxes = BN == 64 ? 2 : 1;
+    // 32 x 64 tiles take 128 cycles of MMAs per box, much less than a round of the issuer: their stages are four boxes deep.
+    static constexpr int kBoxes = BN == 64 ? 4 : 1;
     static constexpr int kK = kBoxes * kBox16;                              // contraction elements per stage
     static constexpr int kRows = BN == 64 ? 32 : kRows16;                   // rows of a CTA's part of a tile
     static constexpr int kABox = kRows * 128, kBBox = kBRows * 128;
     static constexpr int kABytes = kBoxes * kABox, kBBytes = kBoxes * kBBox;
-    static constexpr int kStages = BN == 64 ? 7 : 5;
+    static constexpr int kStages = BN == 64 ? 3 : 5;
     static constexpr int kTmemCols = 2 * BN;
     static constexpr int kOperands = kStages * (kABytes + kBBytes);
     static constexpr int kTail = 512;                                       // barriers, tensor memory's address, abort flag
@@ -78,7 +78,7 @@ struct Gemm16Params {
     // Contractions in parts (TILES_CUT, EPI16_GRAM): a part's accumulator goes to `partial`, and who comes last to a tile, by its counter, adds up
     // the parts in their order.  NULL: no parts.
     int32_t part_stages;             // stages of a part
-    float *partial;                  // [part][CTA of the tile][warp][column][row]
+    float *partial;                  // [part][CTA of the tile][warp][column / 4][row][column % 4]
     uint32_t *counters;              // of a tile's warps; 0 between kernels
     int32_t admit;                   // the next kernel may set up beside this one (it is one of the same call)
     // EPI16_STORE, EPI16_SUM
@@ -648,7 +648,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 const int left = t.k_len - k;
                 const bool cut = TILES == TILES_CUT && left < C::kK;
                 if (issuer) {
-                    const int boxes = C::kBoxes == 1 || left > kBox16 ? C::kBoxes : 1;
+                    const int boxes = C::kBoxes == 1 ? 1 : min(C::kBoxes, (left + kBox16 - 1) / kBox16);
                     const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * ring.slot, bar = CTAS == 2 && !cut ? lead + 8 * ring.slot : own_bar;
                     if (a_side && (rank == 0 || cut)) mbar_arrive_expect_tx(own_bar, (uint32_t)boxes * (box_bytes + (cut ? 0u : peer_bytes)));
                     if (withhold == 0u || !a_side || ++loads != withhold) {
@@ -839,20 +839,34 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             };
             // Parts: this one's accumulator, columns c and up, goes to its place; the sum of all parts comes from there.
             constexpr bool kParts = TILES == TILES_CUT || EPI == EPI16_GRAM;
-            const int64_t place = kParts ? ((int64_t)(t.slot0 * CTAS + rank) * 8 + (warp - 4)) * (32 * kCols) + lane : 0;
+            const int64_t place = kParts ? ((int64_t)(t.slot0 * CTAS + rank) * 8 + (warp - 4)) * (32 * kCols) + 4 * lane : 0;
             constexpr int64_t kPlace = (int64_t)CTAS * 8 * 32 * kCols;
             auto put_part = [&](const float *v, int c, int n) {
-                float *to = p.partial + place + (t.s0 / p.part_stages) * kPlace + 32 * c;
+                float4 *to = reinterpret_cast<float4 *>(p.partial + place + (t.s0 / p.part_stages) * kPlace + 32 * c);
 #pragma unroll
-                for (int e = 0; e < n; e++) to[32 * e] = v[e];
+                for (int e = 0; e < n; e += 4) to[8 * e] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
             };
+            // Several parts are on their way at a time; they are added in their order all the same.
             auto add_parts = [&](float *v, int c, int n) {
-                const float *from = p.partial + place + 32 * c;
+                constexpr int kBatch = EPI == EPI16_SUM ? 8 : 32, kWay = 3;   // columns, and parts of them
 #pragma unroll
-                for (int e = 0; e < n; e++) v[e] = __ldcg(from + 32 * e);
-                for (int i = 1; i < t.parts; i++) {
+                for (int e0 = 0; e0 < n; e0 += kBatch) {
+                    const float4 *from = reinterpret_cast<const float4 *>(p.partial + place + 32 * (c + e0));
 #pragma unroll
-                    for (int e = 0; e < n; e++) v[e] += __ldcg(from + i * kPlace + 32 * e);
+                    for (int e = 0; e < kBatch; e++) v[e0 + e] = 0.f;
+                    for (int i = 0; i < t.parts; i += kWay) {
+                        float4 x[kWay][kBatch / 4];
+#pragma unroll
+                        for (int w = 0; w < kWay; w++)
+#pragma unroll
+                            for (int e = 0; e < kBatch / 4; e++) x[w][e] = i + w < t.parts ? __ldcg(from + (i + w) * (kPlace / 4) + 32 * e) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int w = 0; w < kWay; w++)
+#pragma unroll
+                            for (int e = 0; e < kBatch / 4; e++) {
+                                v[e0 + 4 * e] += x[w][e].x; v[e0 + 4 * e + 1] += x[w][e].y; v[e0 + 4 * e + 2] += x[w][e].z; v[e0 + 4 * e + 3] += x[w][e].w;
+                            }
+                    }
                 }
             };
             auto last_part = [&]() {   // whether all the others have been put
@@ -919,6 +933,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 }
                 if (!ok) break;
                 if (kParts && t.parts > 1) {
+                    if (rows <= 0 || col0 >= p.n) continue;
                     put_part(sum, 0, kCols);
                     if (!last_part()) continue;
                     add_parts(sum, 0, kCols);
@@ -954,17 +969,17 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     FP4Q_TMEM_LD_X32(from + acc.slot * BN + c, v);
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
                     if (c == kCols - 32) release();
-                    put_part(reinterpret_cast<const float *>(v), c, 32);
+                    if (rows > 0 && col0 + c < p.n) put_part(reinterpret_cast<const float *>(v), c, 32);
                 }
                 acc.next();
-                if (!last_part()) continue;
+                if (rows <= 0 || col0 >= p.n || !last_part()) continue;
             }
 #pragma unroll 1
             for (int c = 0; c < kCols; c += kChunk) {
                 uint32_t v[kChunk];
                 const int col = col0 + c;
                 if (kParts && t.parts > 1) {
-                    add_parts(reinterpret_cast<float *>(v), c, kChunk);
+                    if (col < p.n) add_parts(reinterpret_cast<float *>(v), c, kChunk);
                 } else if (chunks > 0) {
 #pragma unroll
                     for (int e = 0; e < kChunk; e += 32) FP4Q_TMEM_LD_X32(from + acc.slot * BN + c + e, (v + e));

@@ -197,7 +197,7 @@ struct Scratch {
         lo[0] = place(x_bytes); lo[1] = split ? place(x_bytes) : lo[0];
         a[0] = place(a_bytes); a[1] = split ? place(a_bytes) : a[0];
         poly[0] = place(a_bytes); poly[1] = split ? place(a_bytes) : poly[0];
-        pairs = side > 128;
+        pairs = count * (ceil_div(side, 128) * (ceil_div(side, 128) + 1) / 2) > 148;
         const int64_t edge = pairs ? 256 : 128, slots = pairs ? 74 : 148, stages = (split ? 3 : 1) * ceil_div(rows < cols ? cols : rows, kBox16);
         tiles = count * (ceil_div(side, edge) * (ceil_div(side, edge) + 1) / 2);
         const int64_t parts = std::min(slots / std::min(tiles, slots), stages / 16);
@@ -347,7 +347,8 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     p.split = at.split;
     p.admit = 1;
     const Parts part_a(half_at(at.a[0]), half_at(at.a[1]), side, side, count, at.pitch_a), part_p(half_at(at.poly[0]), half_at(at.poly[1]), side, side, count, at.pitch_a);
-    const bool pairs = at.pairs;
+    // 128 x 128 tiles where one round of them does, each with half the epilogue of a pair's; else pairs.
+    const bool pairs = at.pairs, pairs_update = count * ceil_div(rows, 128) * ceil_div(cols, 128) > 148;
     for (int32_t i = 0; i < steps; i++) {
         const float *c = coefficients + 3 * i;
         const int now = i & 1, next = now ^ 1;
@@ -381,7 +382,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
         }
         fp4q_status st = pairs ? Steps<2, 256>::gram(part_x, part_a, tall, gp, s) : Steps<1, 128>::gram(part_x, part_a, tall, gp, s);
         if (!st) st = pairs ? Steps<2, 256>::poly(part_a, part_p, pp, s) : Steps<1, 128>::poly(part_a, part_p, pp, s);
-        if (!st) st = pairs ? Steps<2, 256>::update(part_x, part_p, part_next, tall, up, s) : Steps<1, 128>::update(part_x, part_p, part_next, tall, up, s);
+        if (!st) st = pairs_update ? Steps<2, 256>::update(part_x, part_p, part_next, tall, up, s) : Steps<1, 128>::update(part_x, part_p, part_next, tall, up, s);
         if (st) return st;
     }
     return FP4Q_OK;
