@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -96,6 +97,7 @@ class _RaggedLinearFn(torch.autograd.Function):
         return binding.fp4q_ragged_gemm_fwd(xb, wb, row_offsets, ws=ws).contiguous()
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         xb, wb, row_offsets = ctx.saved_tensors
         dyb, dx, dw = _rows16(dy), None, None

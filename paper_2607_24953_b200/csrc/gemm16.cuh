@@ -44,7 +44,10 @@ enum { TILES_ROWS = 0, TILES_CUT = 1, TILES_BATCH = 2, TILES_SYM = 3 };
 enum { EPI16_STORE = 0, EPI16_GRAM = 1, EPI16_POLY = 2, EPI16_UPDATE = 3, EPI16_SUM = 4 };
 constexpr int kSumElems = 512;
 
-template <int CTAS, int BN>
+// TWO: an epilogue warp of a product that writes its output as it is has two boxes, at the price of a stage.  Cut contractions, which are
+// often short beside their output, gain (300 rows in 64 groups 30 -> 27 us, 24266 in 44 groups of 306 x 4270 183-199 -> 175), rows of groups
+// lose (the expert layer's forward 363 -> 381).
+template <int CTAS, int BN, bool TWO = false>
 struct Cfg16 {
     static_assert(CTAS == 1 || (CTAS == 2 && BN == 256), "tile shapes");
     static constexpr int kBRows = BN / CTAS;
@@ -54,15 +57,15 @@ struct Cfg16 {
     static constexpr int kRows = BN == 64 ? 32 : kRows16;                   // rows of a CTA's part of a tile
     static constexpr int kABox = kRows * 128, kBBox = kBRows * 128;
     static constexpr int kABytes = kBoxes * kABox, kBBytes = kBoxes * kBBox;
-    static constexpr int kStages = BN == 64 ? 3 : 5;
+    static constexpr int kStages = BN == 64 ? 3 : TWO ? 4 : 5;
     static constexpr int kTmemCols = 2 * BN;
     static constexpr int kOperands = kStages * (kABytes + kBBytes);
     static constexpr int kTail = 512;                                       // barriers, tensor memory's address, abort flag
     static constexpr int kTables = 3 * (kMaxGroups16 + 1) * 4 + kMaxSorted16 * 2;              // row groups and cut contractions only
-    __host__ __device__ static constexpr int staging(int epi) { return epi == EPI16_STORE || epi == EPI16_SUM ? 4096 : 8192; }   // of an epilogue warp: one box, or an upper and a lower one
+    __host__ __device__ static constexpr int staging(int epi) { return !TWO && (epi == EPI16_STORE || epi == EPI16_SUM) ? 4096 : 8192; }   // of an epilogue warp: one box or two, or an upper and a lower one
     static constexpr int smem(int tiles, int epi) { return 1024 + kOperands + 8 * staging(epi) + kTail + (tiles <= TILES_CUT ? kTables : 0); }
     static constexpr int64_t kPlaceBytes = (int64_t)CTAS * kRows16 * BN * 4;   // of a part's accumulator
-    static_assert(1024 + kOperands + 8 * 4096 + kTail + kTables <= 227 * 1024 && (BN == 64 || 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024), "shared memory budget");
+    static_assert(1024 + kOperands + 8 * (TWO ? 8192 : 4096) + kTail + kTables <= 227 * 1024 && (BN == 64 || 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024), "shared memory budget");
 };
 
 struct Gemm16Params {
@@ -426,7 +429,7 @@ __device__ __forceinline__ void boxes_free(int lane)
 template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
 __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_constant__ Maps16 maps, const Gemm16Params p)
 {
-    using C = Cfg16<CTAS, BN>;
+    using C = Cfg16<CTAS, BN, TILES == TILES_CUT>;
     constexpr int kStages = C::kStages, kStaging = C::staging(EPI);
     constexpr bool kSplits = EPI == EPI16_GRAM || EPI == EPI16_POLY || EPI == EPI16_UPDATE;
     extern __shared__ uint8_t smem_raw[];
@@ -815,7 +818,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         const Box16 up(boxes, lane), lo(boxes + 4096, lane);
         constexpr int kCols = BN / 2, kChunk = EPI == EPI16_SUM || kCols < 64 ? 32 : 64;   // a warp's columns, and those of a box
         Ring16<2> acc;
-        uint32_t box_phase = 0;
+        uint32_t box_phase = 0, second = 0;
         for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, passes, start, first, slots, order, rank);
             const int in = 32 * quarter + lane;
@@ -885,15 +888,23 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             // A box leaves.  Rows of a group's last box, which shares its rows with the next group, and a row's last bytes leave by themselves.
             auto send = [&](const uint32_t *w, const float *v, int col) {
                 if (col < p.boxed && rows >= (TILES == TILES_ROWS ? 32 : 1)) {
-                    boxes_free(lane);
-                    up.put(w);
+                    if (TILES == TILES_CUT) {   // the store before the last has read the box that is next
+                        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                        __syncwarp();
+                        if (second) lo.put(w);
+                        else up.put(w);
+                    } else {
+                        boxes_free(lane);
+                        up.put(w);
+                    }
                     fence_async_shared();
                     __syncwarp();
                     if (lane == 0) {
-                        if (EPI == EPI16_SUM && p.accumulate) tma_reduce_add_3d(&maps.out, col, row0, batch, boxes);
-                        else tma_store_3d(&maps.out, col, row0, batch, boxes);
+                        if (EPI == EPI16_SUM && p.accumulate) tma_reduce_add_3d(&maps.out, col, row0, batch, boxes + second);
+                        else tma_store_3d(&maps.out, col, row0, batch, boxes + second);
                         bulk_commit();
                     }
+                    if (TILES == TILES_CUT) second ^= 4096u;
                     if (col + kChunk > p.boxed && lane < rows) {
 #pragma unroll
                         for (int e = 0; e < kChunk; e++) {
@@ -1144,7 +1155,7 @@ template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
 fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand16 &a2, const Operand16 &b2, Maps16 &maps, const Gemm16Params &p, int64_t most_tiles,
                           cudaStream_t stream)
 {
-    using C = Cfg16<CTAS, BN>;
+    using C = Cfg16<CTAS, BN, TILES == TILES_CUT>;
     const int a_rows = A_MN ? kBox16 : p.a_box, b_rows = B_MN ? kBox16 : C::kBRows;
     if (!make_map16(&maps.a, a, kBox16, a_rows) || !make_map16(&maps.b, b, kBox16, b_rows)) return FP4Q_ERR_CUDA;
     if (p.split && (!make_map16(&maps.a2, a2, kBox16, a_rows) || !make_map16(&maps.b2, b2, kBox16, b_rows))) return FP4Q_ERR_CUDA;

@@ -176,11 +176,25 @@ __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumPara
     }
 }
 
+// A's product in tiles of `edge` for `slots` CTAs or pairs: how many parts a contraction of `stages` stages is cut into, no less than 16 stages each and
+// no more than there are slots for, and an estimate of the time: rounds of stages, which get 115 GB/s an SM and 11 TB/s in all from L2, and
+// for parts their way through memory.
+struct GramPlan {
+    int64_t tiles, parts;
+    double us;
+    GramPlan(int64_t count, int64_t side, int64_t stages, int64_t edge, int64_t slots, int64_t sms)
+    {
+        tiles = count * (ceil_div(side, edge) * (ceil_div(side, edge) + 1) / 2);
+        parts = std::max<int64_t>(1, std::min(slots / std::min(tiles, slots), stages / 16));
+        const double stage = std::max(32768.0 / 115e3, 32768.0 * (double)(sms * std::min(tiles * parts, slots)) / 11e6);
+        us = (double)ceil_div(tiles * parts, slots) * ((double)stages / parts * stage + 2.0 * sms) + (parts > 1 ? 3.0 + 0.7 * parts : 0.0);
+    }
+};
+
 // Where things lie in the scratch memory.
 struct Scratch {
     int64_t pitch_x, pitch_a, side;
     bool split, pairs;
-    // Few tiles with a long contraction, as A of a short side has them: parts of no less than 16 stages, as many as there are CTAs or pairs for.
     int64_t tiles, part_stages;
     size_t counters, accumulators, partial, x[2], lo[2], a[2], poly[2], bytes;   // upper and lower parts; X and the next X: lower parts in one place unless they are operands
     Scratch(int64_t count, int64_t rows, int64_t cols)
@@ -197,10 +211,11 @@ struct Scratch {
         lo[0] = place(x_bytes); lo[1] = split ? place(x_bytes) : lo[0];
         a[0] = place(a_bytes); a[1] = split ? place(a_bytes) : a[0];
         poly[0] = place(a_bytes); poly[1] = split ? place(a_bytes) : poly[0];
-        pairs = count * (ceil_div(side, 128) * (ceil_div(side, 128) + 1) / 2) > 148;
-        const int64_t edge = pairs ? 256 : 128, slots = pairs ? 74 : 148, stages = (split ? 3 : 1) * ceil_div(rows < cols ? cols : rows, kBox16);
-        tiles = count * (ceil_div(side, edge) * (ceil_div(side, edge) + 1) / 2);
-        const int64_t parts = std::min(slots / std::min(tiles, slots), stages / 16);
+        const int64_t stages = (split ? 3 : 1) * ceil_div(rows < cols ? cols : rows, kBox16);
+        const GramPlan one(count, side, stages, 128, 148, 1), two(count, side, stages, 256, 74, 2);
+        pairs = two.us < one.us;
+        tiles = pairs ? two.tiles : one.tiles;
+        const int64_t parts = pairs ? two.parts : one.parts;
         part_stages = parts >= 2 ? ceil_div(stages, parts) : 0;
         counters = place(part_stages ? (size_t)round_up(tiles * 2 * 8 * 4, 256) : 0);
         accumulators = place(part_stages ? (size_t)(tiles * parts * (pairs ? Cfg16<2, 256>::kPlaceBytes : Cfg16<1, 128>::kPlaceBytes)) : 0);
@@ -347,8 +362,8 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     p.split = at.split;
     p.admit = 1;
     const Parts part_a(half_at(at.a[0]), half_at(at.a[1]), side, side, count, at.pitch_a), part_p(half_at(at.poly[0]), half_at(at.poly[1]), side, side, count, at.pitch_a);
-    // 128 x 128 tiles where one round of them does, each with half the epilogue of a pair's; else pairs.
-    const bool pairs = at.pairs, pairs_update = count * ceil_div(rows, 128) * ceil_div(cols, 128) > 148;
+    // P and X': 128 x 128 tiles where one round of them does, each with half the epilogue of a pair's; else pairs.
+    const bool pairs = at.pairs, pairs_poly = count * (ceil_div(side, 128) * (ceil_div(side, 128) + 1) / 2) > 148, pairs_update = count * ceil_div(rows, 128) * ceil_div(cols, 128) > 148;
     for (int32_t i = 0; i < steps; i++) {
         const float *c = coefficients + 3 * i;
         const int now = i & 1, next = now ^ 1;
@@ -381,7 +396,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
             up.boxed = aligned(out_bf16, 16) && ld_o % 8 == 0 ? (int32_t)(cols / 8 * 8) : 0;
         }
         fp4q_status st = pairs ? Steps<2, 256>::gram(part_x, part_a, tall, gp, s) : Steps<1, 128>::gram(part_x, part_a, tall, gp, s);
-        if (!st) st = pairs ? Steps<2, 256>::poly(part_a, part_p, pp, s) : Steps<1, 128>::poly(part_a, part_p, pp, s);
+        if (!st) st = pairs_poly ? Steps<2, 256>::poly(part_a, part_p, pp, s) : Steps<1, 128>::poly(part_a, part_p, pp, s);
         if (!st) st = pairs_update ? Steps<2, 256>::update(part_x, part_p, part_next, tall, up, s) : Steps<1, 128>::update(part_x, part_p, part_next, tall, up, s);
         if (st) return st;
     }
