@@ -47,25 +47,28 @@ constexpr int kSumElems = 512;
 // TWO: an epilogue warp of a product that writes its output as it is has two boxes, at the price of a stage.  Cut contractions, which are
 // often short beside their output, gain (300 rows in 64 groups 30 -> 27 us, 24266 in 44 groups of 306 x 4270 183-199 -> 175), rows of groups
 // lose (the expert layer's forward 363 -> 381).
-template <int CTAS, int BN, bool TWO = false>
+// Tiles of 64 columns have 32 rows where rows come in short groups, and 64 in stacks of matrices (STACK), where they serve those so small
+// that all their tiles run at once: the fewer bytes a CTA loads, the sooner it is done.
+template <int CTAS, int BN, bool TWO = false, bool STACK = false>
 struct Cfg16 {
     static_assert(CTAS == 1 || (CTAS == 2 && BN == 256), "tile shapes");
     static constexpr int kBRows = BN / CTAS;
-    // 32 x 64 tiles take 128 cycles of MMAs per box, much less than a round of the issuer: their stages are four boxes deep.
-    static constexpr int kBoxes = BN == 64 ? 4 : 1;
+    // 32 x 64 tiles take 128 cycles of MMAs per box, much less than a round of the issuer: their stages are four boxes deep, 64 x 64 ones' two.
+    static constexpr int kBoxes = BN == 64 ? (STACK ? 2 : 4) : 1;
     static constexpr int kK = kBoxes * kBox16;                              // contraction elements per stage
-    static constexpr int kRows = BN == 64 ? 32 : kRows16;                   // rows of a CTA's part of a tile
+    static constexpr int kRows = BN == 64 ? (STACK ? 64 : 32) : kRows16;                   // rows of a CTA's part of a tile
     static constexpr int kABox = kRows * 128, kBBox = kBRows * 128;
     static constexpr int kABytes = kBoxes * kABox, kBBytes = kBoxes * kBBox;
-    static constexpr int kStages = BN == 64 ? 3 : TWO ? 4 : 5;
+    static constexpr int kStages = BN == 64 && !STACK ? 3 : TWO ? 4 : 5;
     static constexpr int kTmemCols = 2 * BN;
     static constexpr int kOperands = kStages * (kABytes + kBBytes);
     static constexpr int kTail = 512;                                       // barriers, tensor memory's address, abort flag
     static constexpr int kTables = 3 * (kMaxGroups16 + 1) * 4 + kMaxSorted16 * 2;              // row groups and cut contractions only
     __host__ __device__ static constexpr int staging(int epi) { return !TWO && (epi == EPI16_STORE || epi == EPI16_SUM) ? 4096 : 8192; }   // of an epilogue warp: one box or two, or an upper and a lower one
     static constexpr int smem(int tiles, int epi) { return 1024 + kOperands + 8 * staging(epi) + kTail + (tiles <= TILES_CUT ? kTables : 0); }
+    static constexpr int kTileRows = kRows * CTAS;
     static constexpr int64_t kPlaceBytes = (int64_t)CTAS * kRows16 * BN * 4;   // of a part's accumulator
-    static_assert(1024 + kOperands + 8 * (TWO ? 8192 : 4096) + kTail + kTables <= 227 * 1024 && (BN == 64 || 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024), "shared memory budget");
+    static_assert(1024 + kOperands + 8 * (TWO ? 8192 : 4096) + kTail + kTables <= 227 * 1024 && ((BN == 64 && !STACK) || 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024), "shared memory budget");
 };
 
 struct Gemm16Params {
@@ -254,7 +257,8 @@ template <int TILES, int CTAS, int BN>
 __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int m_tiles, int passes, const int32_t *start, const int32_t *first, const int32_t *slots,
                                            const uint16_t *order, int rank)
 {
-    constexpr int kRows = Cfg16<CTAS, BN>::kRows, kBM = kRows * CTAS, kBRows = Cfg16<CTAS, BN>::kBRows, kK = Cfg16<CTAS, BN>::kK;
+    using C = Cfg16<CTAS, BN, TILES == TILES_CUT, (TILES >= TILES_BATCH)>;
+    constexpr int kRows = C::kRows, kBM = kRows * CTAS, kBRows = C::kBRows, kK = C::kK;
     Tile16 t;
     int mt, nt, part = 0;
     t.batch = 0;
@@ -429,7 +433,7 @@ __device__ __forceinline__ void boxes_free(int lane)
 template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
 __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_constant__ Maps16 maps, const Gemm16Params p)
 {
-    using C = Cfg16<CTAS, BN, TILES == TILES_CUT>;
+    using C = Cfg16<CTAS, BN, TILES == TILES_CUT, (TILES >= TILES_BATCH)>;
     constexpr int kStages = C::kStages, kStaging = C::staging(EPI);
     constexpr bool kSplits = EPI == EPI16_GRAM || EPI == EPI16_POLY || EPI == EPI16_UPDATE;
     extern __shared__ uint8_t smem_raw[];
@@ -636,7 +640,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b), lead = CTAS == 2 ? cluster_addr(bar_full, 0) : bar_full;
         for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, passes, start, first, slots, order, rank);
-            const int a_copies = A_MN ? 2 : (t.rows + p.a_box - 1) / p.a_box;
+            const int a_copies = A_MN ? C::kRows / 64 : (t.rows + p.a_box - 1) / p.a_box;
             const uint32_t a_copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
             const uint32_t box_bytes = (uint32_t)a_copies * a_copy_bytes + (uint32_t)C::kBBox;   // of this CTA
             const uint32_t peer_bytes = CTAS == 2 ? (uint32_t)(A_MN ? 2 : (t.rows_peer + p.a_box - 1) / p.a_box) * a_copy_bytes + (uint32_t)C::kBBox : 0u;
@@ -667,7 +671,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                             if (!a_side) {
                             } else if (A_MN) {
 #pragma unroll
-                                for (int j = 0; j < 2; j++) load(a + j * 8192, mapA, t.a_row + 64 * j, at, az);
+                                for (int j = 0; j < C::kRows / 64; j++) load(a + j * 8192, mapA, t.a_row + 64 * j, at, az);
                             } else {
                                 for (int j = 0; j < a_copies; j++) load(a + j * a_copy_bytes, mapA, at, t.a_row + j * p.a_box, az);
                             }
@@ -813,10 +817,11 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         }
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ epilogue
-        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        constexpr bool kNarrow = BN == 64 && TILES >= TILES_BATCH;   // four warps have all the columns, the others none
+        const int quarter = warp & 3, half = kNarrow ? 0 : (warp - 4) >> 2;
         const uint32_t boxes = smem_u32(smem_boxes) + (warp - 4) * kStaging, bar_box = smem_u32(bars + 36 + warp - 4);
         const Box16 up(boxes, lane), lo(boxes + 4096, lane);
-        constexpr int kCols = BN / 2, kChunk = EPI == EPI16_SUM || kCols < 64 ? 32 : 64;   // a warp's columns, and those of a box
+        constexpr int kCols = kNarrow ? BN : BN / 2, kChunk = EPI == EPI16_SUM || kCols < 64 ? 32 : 64;   // a warp's columns, and those of a box
         Ring16<2> acc;
         uint32_t box_phase = 0, second = 0;
         for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
@@ -825,7 +830,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             const int elems = (t.s1 - t.s0) * C::kK, chunks = EPI == EPI16_SUM ? (elems + kSumElems - 1) / kSumElems : elems > 0;   // accumulators of the tile
             const uint64_t acc_limit = limit * (uint64_t)(1 + (t.k_len >> 8));
             const uint32_t from = tmem + half * kCols + ((uint32_t)(32 * quarter) << 16);
-            const int col0 = t.col + half * kCols, row0 = t.row + 32 * quarter, rows = t.rows - 32 * quarter;   // this warp's first column and row, its rows
+            const int col0 = t.col + half * kCols, row0 = t.row + 32 * quarter, rows = kNarrow && warp >= 8 ? 0 : t.rows - 32 * quarter;   // this warp's first column and row, its rows
             const int batch = TILES == TILES_ROWS ? 0 : t.batch;
             const int64_t row = (TILES == TILES_CUT ? (int64_t)t.batch * p.m : 0) + t.row + in;
             // The accumulator may be overwritten as soon as all warps have it in registers: reads of tensor memory, which the fence orders, and
@@ -841,7 +846,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 __syncwarp();
             };
             // Parts: this one's accumulator, columns c and up, goes to its place; the sum of all parts comes from there.
-            constexpr bool kParts = TILES == TILES_CUT || EPI == EPI16_GRAM;
+            constexpr bool kParts = TILES == TILES_CUT || (TILES == TILES_SYM && EPI == EPI16_GRAM);
             const int64_t place = kParts ? ((int64_t)(t.slot0 * CTAS + rank) * 8 + (warp - 4)) * (32 * kCols) + 4 * lane : 0;
             constexpr int64_t kPlace = (int64_t)CTAS * 8 * 32 * kCols;
             auto put_part = [&](const float *v, int c, int n) {
@@ -1155,7 +1160,7 @@ template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
 fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand16 &a2, const Operand16 &b2, Maps16 &maps, const Gemm16Params &p, int64_t most_tiles,
                           cudaStream_t stream)
 {
-    using C = Cfg16<CTAS, BN, TILES == TILES_CUT>;
+    using C = Cfg16<CTAS, BN, TILES == TILES_CUT, (TILES >= TILES_BATCH)>;
     const int a_rows = A_MN ? kBox16 : p.a_box, b_rows = B_MN ? kBox16 : C::kBRows;
     if (!make_map16(&maps.a, a, kBox16, a_rows) || !make_map16(&maps.b, b, kBox16, b_rows)) return FP4Q_ERR_CUDA;
     if (p.split && (!make_map16(&maps.a2, a2, kBox16, a_rows) || !make_map16(&maps.b2, b2, kBox16, b_rows))) return FP4Q_ERR_CUDA;

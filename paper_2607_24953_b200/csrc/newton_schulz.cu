@@ -176,25 +176,29 @@ __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumPara
     }
 }
 
-// A's product in tiles of `edge` for `slots` CTAs or pairs: how many parts a contraction of `stages` stages is cut into, no less than 16 stages each and
-// no more than there are slots for, and an estimate of the time: rounds of stages, which get 115 GB/s an SM and 11 TB/s in all from L2, and
-// for parts their way through memory.
+// A's product in tiles of `edge` (128, or 256 for pairs), its contraction of `stages` boxes cut into parts: the number of parts with the least
+// estimated time.  A round of the CTAs' or pairs' tiles takes its boxes, which get 115 GB/s an SM and 11 TB/s in all from L2, and 2 or 4 us; parts take
+// their way through memory, where whoever comes last reads them one after the other.  (Parts for 4751 x 63: 70 -> 20 us.)
 struct GramPlan {
-    int64_t tiles, parts;
-    double us;
-    GramPlan(int64_t count, int64_t side, int64_t stages, int64_t edge, int64_t slots, int64_t sms)
+    int64_t tiles, parts = 1;
+    double us = 1e30;
+    GramPlan(int64_t count, int64_t side, int64_t stages, int64_t edge)
     {
-        tiles = count * (ceil_div(side, edge) * (ceil_div(side, edge) + 1) / 2);
-        parts = std::max<int64_t>(1, std::min(slots / std::min(tiles, slots), stages / 16));
-        const double stage = std::max(32768.0 / 115e3, 32768.0 * (double)(sms * std::min(tiles * parts, slots)) / 11e6);
-        us = (double)ceil_div(tiles * parts, slots) * ((double)stages / parts * stage + 2.0 * sms) + (parts > 1 ? 3.0 + 0.7 * parts : 0.0);
+        const int64_t across = ceil_div(side, edge), slots = edge == 256 ? 74 : 148, sms = edge == 256 ? 2 : 1;
+        tiles = count * across * (across + 1) / 2;
+        for (int64_t n = 1; n == 1 || (n <= 32 && stages / n >= 16 && tiles * n <= 4 * slots); n++) {
+            const double box = std::max(32768.0 / 115e3, 32768.0 * (double)(sms * std::min(tiles * n, slots)) / 11e6);
+            const double t = (double)ceil_div(tiles * n, slots) * ((double)ceil_div(stages, n) * box + 2.0 * sms) + (n > 1 ? 3.0 + 0.6 * (double)n : 0.0);
+            if (t < us) { us = t; parts = n; }
+        }
     }
 };
 
 // Where things lie in the scratch memory.
 struct Scratch {
     int64_t pitch_x, pitch_a, side;
-    bool split, pairs;
+    bool split;
+    int edge;                            // tiles of A's product: 64, 128 or 256 (pairs)
     int64_t tiles, part_stages;
     size_t counters, accumulators, partial, x[2], lo[2], a[2], poly[2], bytes;   // upper and lower parts; X and the next X: lower parts in one place unless they are operands
     Scratch(int64_t count, int64_t rows, int64_t cols)
@@ -212,13 +216,17 @@ struct Scratch {
         a[0] = place(a_bytes); a[1] = split ? place(a_bytes) : a[0];
         poly[0] = place(a_bytes); poly[1] = split ? place(a_bytes) : poly[0];
         const int64_t stages = (split ? 3 : 1) * ceil_div(rows < cols ? cols : rows, kBox16);
-        const GramPlan one(count, side, stages, 128, 148, 1), two(count, side, stages, 256, 74, 2);
-        pairs = two.us < one.us;
+        const GramPlan one(count, side, stages, 128), two(count, side, stages, 256);
+        const bool pairs = two.us < one.us;
+        // 64 x 64 tiles, a quarter of a microsecond a box, where all of them run at once and no parts are faster: they are all computed, and not
+        // cut (256 x 256 10 -> 7 us, 85 of 2382 x 45 41 -> 31).
+        const bool small = count * ceil_div(side, 64) * ceil_div(side, 64) <= 148 && 0.26 * (double)stages + 1.0 < std::min(one.us, two.us);
+        edge = small ? 64 : pairs ? 256 : 128;
         tiles = pairs ? two.tiles : one.tiles;
-        const int64_t parts = pairs ? two.parts : one.parts;
+        const int64_t parts = edge == 64 ? 1 : pairs ? two.parts : one.parts;
         part_stages = parts >= 2 ? ceil_div(stages, parts) : 0;
         counters = place(part_stages ? (size_t)round_up(tiles * 2 * 8 * 4, 256) : 0);
-        accumulators = place(part_stages ? (size_t)(tiles * parts * (pairs ? Cfg16<2, 256>::kPlaceBytes : Cfg16<1, 128>::kPlaceBytes)) : 0);
+        accumulators = place(part_stages ? (size_t)(tiles * parts * (edge == 256 ? Cfg16<2, 256>::kPlaceBytes : Cfg16<1, 128>::kPlaceBytes)) : 0);
     }
 };
 
@@ -265,12 +273,15 @@ fp4q_status boxes16(CUtensorMap *up, CUtensorMap *lo, const Parts &x, bool two, 
 
 template <int CTAS, int BN>
 struct Steps {
-    static constexpr int kBM = kRows16 * CTAS;
+    static constexpr int kBM = Cfg16<CTAS, BN, false, true>::kTileRows;
+    static_assert(kBM == BN, "symmetric products have square tiles");
+    // 64 x 64 tiles are all computed, which is as fast and saves the mirrored stores: they all run at once.
+    static constexpr int kSym = BN == 64 ? TILES_BATCH : TILES_SYM;
     static int64_t symmetric_tiles(Gemm16Params &p)
     {
-        static_assert(kBM == BN, "symmetric products have square tiles");
+        p.a_box = kBM / CTAS;
         p.m_tiles = p.n_tiles = (int32_t)ceil_div(p.n, BN);
-        return (int64_t)p.batch * p.m_tiles * (p.m_tiles + 1) / 2;
+        return (int64_t)p.batch * p.m_tiles * (kSym == TILES_BATCH ? 2 * p.m_tiles : p.m_tiles + 1) / 2;
     }
     static fp4q_status gram(const Parts &x, const Parts &a, bool tall, Gemm16Params p, cudaStream_t stream)
     {
@@ -279,8 +290,8 @@ struct Steps {
         if (p.partial) tiles *= ceil_div((p.split ? 3 : 1) * ceil_div(p.k, kBox16), p.part_stages);
         if (fp4q_status s = boxes16(&maps.out, &maps.out2, a, p.split)) return s;
         if (fp4q_status s = boxes16(&maps.mirror, &maps.mirror2, a, p.split, true)) return s;
-        return tall ? launch_gemm16<CTAS, BN, true, true, EPI16_GRAM, TILES_SYM>(x.up, x.up, x.lo, x.lo, maps, p, tiles, stream)
-                    : launch_gemm16<CTAS, BN, false, false, EPI16_GRAM, TILES_SYM>(x.up, x.up, x.lo, x.lo, maps, p, tiles, stream);
+        return tall ? launch_gemm16<CTAS, BN, true, true, EPI16_GRAM, kSym>(x.up, x.up, x.lo, x.lo, maps, p, tiles, stream)
+                    : launch_gemm16<CTAS, BN, false, false, EPI16_GRAM, kSym>(x.up, x.up, x.lo, x.lo, maps, p, tiles, stream);
     }
     static fp4q_status poly(const Parts &a, const Parts &poly, Gemm16Params p, cudaStream_t stream)
     {
@@ -289,11 +300,12 @@ struct Steps {
         if (fp4q_status s = boxes16(&maps.in, &maps.in2, a, p.split)) return s;
         if (fp4q_status s = boxes16(&maps.out, &maps.out2, poly, p.split)) return s;
         if (fp4q_status s = boxes16(&maps.mirror, &maps.mirror2, poly, p.split, true)) return s;
-        return launch_gemm16<CTAS, BN, false, false, EPI16_POLY, TILES_SYM>(a.up, a.up, a.lo, a.lo, maps, p, tiles, stream);
+        return launch_gemm16<CTAS, BN, false, false, EPI16_POLY, kSym>(a.up, a.up, a.lo, a.lo, maps, p, tiles, stream);
     }
     static fp4q_status update(const Parts &x, const Parts &poly, const Parts &next, bool tall, Gemm16Params p, cudaStream_t stream)
     {
         Maps16 maps = {};
+        p.a_box = kBM / CTAS;
         p.m_tiles = (int32_t)ceil_div(p.m, kBM);
         p.n_tiles = (int32_t)ceil_div(p.n, BN);
         const int64_t tiles = (int64_t)p.batch * p.m_tiles * p.n_tiles;
@@ -346,7 +358,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     q.beta = beta; q.nesterov = nesterov != 0; q.eps = eps;
     q.partial = reinterpret_cast<double *>(base + at.partial);
     q.counters = reinterpret_cast<uint32_t *>(base + at.counters);
-    q.n_counters = at.part_stages ? (int32_t)(at.tiles * (at.pairs ? 16 : 8)) : 0;
+    q.n_counters = at.part_stages ? (int32_t)(at.tiles * (at.edge == 256 ? 16 : 8)) : 0;
     q.up = half_at(at.x[0]); q.lo = half_at(at.lo[0]); q.pitch = at.pitch_x;
     const int64_t want = ceil_div(q.units, kNsThreads * (count > 1 ? 1 : 2)), share = ceil_div(16 * 148, count);
     const dim3 grid((unsigned)std::min<int64_t>(std::min(want, share), kNsMaxBlocks), (unsigned)count);
@@ -362,8 +374,11 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     p.split = at.split;
     p.admit = 1;
     const Parts part_a(half_at(at.a[0]), half_at(at.a[1]), side, side, count, at.pitch_a), part_p(half_at(at.poly[0]), half_at(at.poly[1]), side, side, count, at.pitch_a);
-    // P and X': 128 x 128 tiles where one round of them does, each with half the epilogue of a pair's; else pairs.
-    const bool pairs = at.pairs, pairs_poly = count * (ceil_div(side, 128) * (ceil_div(side, 128) + 1) / 2) > 148, pairs_update = count * ceil_div(rows, 128) * ceil_div(cols, 128) > 148;
+    // P and X': the smallest tiles of which one round does, each with less to load and a shorter epilogue; else pairs.
+    auto edge_of = [&](int64_t small, int64_t tiles64, int64_t tiles128) { return small * tiles64 <= 148 ? 64 : small * tiles128 <= 148 ? 128 : 256; };
+    const int64_t s64 = ceil_div(side, 64), s128 = ceil_div(side, 128);
+    const int edge_poly = edge_of(count, s64 * s64, s128 * (s128 + 1) / 2),
+              edge_update = edge_of(count, ceil_div(rows, 64) * ceil_div(cols, 64), ceil_div(rows, 128) * ceil_div(cols, 128));
     for (int32_t i = 0; i < steps; i++) {
         const float *c = coefficients + 3 * i;
         const int now = i & 1, next = now ^ 1;
@@ -395,9 +410,17 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
             up.o_scale = scale / kScaleX;
             up.boxed = aligned(out_bf16, 16) && ld_o % 8 == 0 ? (int32_t)(cols / 8 * 8) : 0;
         }
-        fp4q_status st = pairs ? Steps<2, 256>::gram(part_x, part_a, tall, gp, s) : Steps<1, 128>::gram(part_x, part_a, tall, gp, s);
-        if (!st) st = pairs_poly ? Steps<2, 256>::poly(part_a, part_p, pp, s) : Steps<1, 128>::poly(part_a, part_p, pp, s);
-        if (!st) st = pairs_update ? Steps<2, 256>::update(part_x, part_p, part_next, tall, up, s) : Steps<1, 128>::update(part_x, part_p, part_next, tall, up, s);
+        fp4q_status st = at.edge == 256   ? Steps<2, 256>::gram(part_x, part_a, tall, gp, s)
+                         : at.edge == 128 ? Steps<1, 128>::gram(part_x, part_a, tall, gp, s)
+                                          : Steps<1, 64>::gram(part_x, part_a, tall, gp, s);
+        if (!st)
+            st = edge_poly == 256   ? Steps<2, 256>::poly(part_a, part_p, pp, s)
+                 : edge_poly == 128 ? Steps<1, 128>::poly(part_a, part_p, pp, s)
+                                    : Steps<1, 64>::poly(part_a, part_p, pp, s);
+        if (!st)
+            st = edge_update == 256   ? Steps<2, 256>::update(part_x, part_p, part_next, tall, up, s)
+                 : edge_update == 128 ? Steps<1, 128>::update(part_x, part_p, part_next, tall, up, s)
+                                      : Steps<1, 64>::update(part_x, part_p, part_next, tall, up, s);
         if (st) return st;
     }
     return FP4Q_OK;
