@@ -44,9 +44,9 @@ enum { TILES_ROWS = 0, TILES_CUT = 1, TILES_BATCH = 2, TILES_SYM = 3 };
 enum { EPI16_STORE = 0, EPI16_GRAM = 1, EPI16_POLY = 2, EPI16_UPDATE = 3, EPI16_SUM = 4 };
 constexpr int kSumElems = 512;
 
-// TWO: an epilogue warp of a product that writes its output as it is has two boxes, at the price of a stage.  Cut contractions, which are
-// often short beside their output, gain (300 rows in 64 groups 30 -> 27 us, 24266 in 44 groups of 306 x 4270 183-199 -> 175), rows of groups
-// lose (the expert layer's forward 363 -> 381).
+// TWO: an epilogue warp of a product that writes its output as it is has two boxes, at the price of a stage.  For contractions that are short
+// beside their output (300 rows in 64 groups 30 -> 27 us, 24266 in 44 groups of 306 x 4270 183-199 -> 175); others lose (the expert layer's
+// forward 363 -> 381).
 // Tiles of 64 columns have 32 rows where rows come in short groups, and 64 in stacks of matrices (STACK), where they serve those so small
 // that all their tiles run at once: the fewer bytes a CTA loads, the sooner it is done.
 template <int CTAS, int BN, bool TWO = false, bool STACK = false>
@@ -257,7 +257,7 @@ template <int TILES, int CTAS, int BN>
 __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int m_tiles, int passes, const int32_t *start, const int32_t *first, const int32_t *slots,
                                            const uint16_t *order, int rank)
 {
-    using C = Cfg16<CTAS, BN, TILES == TILES_CUT, (TILES >= TILES_BATCH)>;
+    using C = Cfg16<CTAS, BN, false, (TILES >= TILES_BATCH)>;
     constexpr int kRows = C::kRows, kBM = kRows * CTAS, kBRows = C::kBRows, kK = C::kK;
     Tile16 t;
     int mt, nt, part = 0;
@@ -430,10 +430,10 @@ __device__ __forceinline__ void boxes_free(int lane)
 
 // ---------------------------------------------------------------------------------------- kernel
 
-template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
+template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES, bool TWO = false>
 __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_constant__ Maps16 maps, const Gemm16Params p)
 {
-    using C = Cfg16<CTAS, BN, TILES == TILES_CUT, (TILES >= TILES_BATCH)>;
+    using C = Cfg16<CTAS, BN, TWO, (TILES >= TILES_BATCH)>;
     constexpr int kStages = C::kStages, kStaging = C::staging(EPI);
     constexpr bool kSplits = EPI == EPI16_GRAM || EPI == EPI16_POLY || EPI == EPI16_UPDATE;
     extern __shared__ uint8_t smem_raw[];
@@ -631,58 +631,68 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
 
     if (warp == 0 || warp == 3) {
         // ------------------------------------------------------------------ TMA producers: warp 0 loads A and announces the bytes, warp 3 loads B
-        // One thread that issues up to four copies a stage needs 0.55 us for it, longer than the stage's MMAs take.
+        // One thread that issues up to four copies a stage needs 0.55 us for it, longer than the stage's MMAs take.  (What comes out of memory
+        // fetched into L2 some stages ahead by the same threads was 2 to 25 % slower: the copies' unit takes 65 bytes a cycle, a stage's 32 KB in
+        // as long as its MMAs take, and the fetches pass through it too.)
         const bool a_side = warp == 0;
         uint32_t loads = 0, issued = 0;
         Ring16<kStages> ring;
         bool ok = true;
         const bool issuer = elect_one();
         const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b), lead = CTAS == 2 ? cluster_addr(bar_full, 0) : bar_full;
+        // The boxes of a stage of this side, each handed to f: destination in the stage, map, coordinates.
+        auto boxes_of = [&](const Tile16 &t, int st, auto f) {
+            const int pass = pass16<kSplits>(t, st), k = (st - pass * t.k_stages) * C::kK, left = t.k_len - k;
+            const int boxes = C::kBoxes == 1 ? 1 : min(C::kBoxes, (left + kBox16 - 1) / kBox16), at0 = t.k0 + k;
+            // TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack
+            if (a_side) {
+                const CUtensorMap *map = kSplits && pass == 2 ? &maps.a2 : &maps.a;
+                const int z = TILES <= TILES_CUT ? 0 : t.batch, copies = A_MN ? C::kRows / 64 : (t.rows + p.a_box - 1) / p.a_box;
+                const uint32_t copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
+#pragma unroll
+                for (int i = 0; i < C::kBoxes; i++) {
+                    if (i >= boxes) break;
+                    for (int j = 0; j < copies; j++)
+                        if (A_MN) f(i * C::kABox + j * copy_bytes, map, t.a_row + 64 * j, at0 + i * kBox16, z);
+                        else f(i * C::kABox + j * copy_bytes, map, at0 + i * kBox16, t.a_row + j * p.a_box, z);
+                }
+            } else {
+                const CUtensorMap *map = kSplits && pass == 1 ? &maps.b2 : &maps.b;
+                const int z = TILES == TILES_CUT ? 0 : t.batch;
+#pragma unroll
+                for (int i = 0; i < C::kBoxes; i++) {
+                    if (i >= boxes) break;
+                    if (B_MN) {
+#pragma unroll
+                        for (int j = 0; j < C::kBRows / 64; j++) f(i * C::kBBox + j * 8192, map, t.b_row + 64 * j, at0 + i * kBox16, z);
+                    } else {
+                        f(i * C::kBBox, map, at0 + i * kBox16, t.b_row, z);
+                    }
+                }
+            }
+        };
         for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, passes, start, first, slots, order, rank);
             const int a_copies = A_MN ? C::kRows / 64 : (t.rows + p.a_box - 1) / p.a_box;
             const uint32_t a_copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
             const uint32_t box_bytes = (uint32_t)a_copies * a_copy_bytes + (uint32_t)C::kBBox;   // of this CTA
             const uint32_t peer_bytes = CTAS == 2 ? (uint32_t)(A_MN ? 2 : (t.rows_peer + p.a_box - 1) / p.a_box) * a_copy_bytes + (uint32_t)C::kBBox : 0u;
-            // TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack
-            const int az = TILES <= TILES_CUT ? 0 : t.batch, bz = TILES == TILES_CUT ? 0 : t.batch;
             for (int s = t.s0; s < t.s1; s++, ring.next()) {
-                const int pass = pass16<kSplits>(t, s), k = (s - pass * t.k_stages) * C::kK;
-                const CUtensorMap *mapA = kSplits && pass == 2 ? &maps.a2 : &maps.a, *mapB = kSplits && pass == 1 ? &maps.b2 : &maps.b;
                 if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) { ok = false; break; }
                 issued++;
                 // A stage with rows behind its group's end lands on a barrier of its own in each CTA, where warp 2 waits for it.
-                const int left = t.k_len - k;
+                const int left = t.k_len - (s - pass16<kSplits>(t, s) * t.k_stages) * C::kK;
                 const bool cut = TILES == TILES_CUT && left < C::kK;
                 if (issuer) {
                     const int boxes = C::kBoxes == 1 ? 1 : min(C::kBoxes, (left + kBox16 - 1) / kBox16);
                     const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * ring.slot, bar = CTAS == 2 && !cut ? lead + 8 * ring.slot : own_bar;
                     if (a_side && (rank == 0 || cut)) mbar_arrive_expect_tx(own_bar, (uint32_t)boxes * (box_bytes + (cut ? 0u : peer_bytes)));
                     if (withhold == 0u || !a_side || ++loads != withhold) {
-                        auto load = [&](uint32_t dst, const CUtensorMap *map, int x, int y, int z) {
-                            if (CTAS == 2 && !cut) tma_load_3d_pair(dst, map, x, y, z, bar);
-                            else tma_load_3d(dst, map, x, y, z, bar);
-                        };
-#pragma unroll
-                        for (int i = 0; i < C::kBoxes; i++) {
-                            if (i >= boxes) break;
-                            const uint32_t a = a0 + ring.slot * C::kABytes + i * C::kABox, b = b0 + ring.slot * C::kBBytes + i * C::kBBox;
-                            const int at = t.k0 + k + i * kBox16;
-                            if (!a_side) {
-                            } else if (A_MN) {
-#pragma unroll
-                                for (int j = 0; j < C::kRows / 64; j++) load(a + j * 8192, mapA, t.a_row + 64 * j, at, az);
-                            } else {
-                                for (int j = 0; j < a_copies; j++) load(a + j * a_copy_bytes, mapA, at, t.a_row + j * p.a_box, az);
-                            }
-                            if (a_side) {
-                            } else if (B_MN) {
-#pragma unroll
-                                for (int j = 0; j < C::kBRows / 64; j++) load(b + j * 8192, mapB, t.b_row + 64 * j, at, bz);
-                            } else {
-                                load(b, mapB, at, t.b_row, bz);
-                            }
-                        }
+                        const uint32_t to = a_side ? a0 + ring.slot * C::kABytes : b0 + ring.slot * C::kBBytes;
+                        boxes_of(t, s, [&](uint32_t offset, const CUtensorMap *map, int x, int y, int z) {
+                            if (CTAS == 2 && !cut) tma_load_3d_pair(to + offset, map, x, y, z, bar);
+                            else tma_load_3d(to + offset, map, x, y, z, bar);
+                        });
                     }
                 }
                 __syncwarp();
@@ -893,7 +903,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             // A box leaves.  Rows of a group's last box, which shares its rows with the next group, and a row's last bytes leave by themselves.
             auto send = [&](const uint32_t *w, const float *v, int col) {
                 if (col < p.boxed && rows >= (TILES == TILES_ROWS ? 32 : 1)) {
-                    if (TILES == TILES_CUT) {   // the store before the last has read the box that is next
+                    if (TWO) {   // the store before the last has read the box that is next
                         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
                         __syncwarp();
                         if (second) lo.put(w);
@@ -909,7 +919,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                         else tma_store_3d(&maps.out, col, row0, batch, boxes + second);
                         bulk_commit();
                     }
-                    if (TILES == TILES_CUT) second ^= 4096u;
+                    if (TWO) second ^= 4096u;
                     if (col + kChunk > p.boxed && lane < rows) {
 #pragma unroll
                         for (int e = 0; e < kChunk; e++) {
@@ -1156,11 +1166,11 @@ inline bool make_map16(CUtensorMap *map, const Operand16 &o, int box_cols, int b
 
 // maps: what lies beside the operands is the caller's.  a2, b2: the operands' lower parts (p.split).  most_tiles: no fewer than the tiles
 // there can be.
-template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES>
+template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES, bool TWO = false>
 fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand16 &a2, const Operand16 &b2, Maps16 &maps, const Gemm16Params &p, int64_t most_tiles,
                           cudaStream_t stream)
 {
-    using C = Cfg16<CTAS, BN, TILES == TILES_CUT, (TILES >= TILES_BATCH)>;
+    using C = Cfg16<CTAS, BN, TWO, (TILES >= TILES_BATCH)>;
     const int a_rows = A_MN ? kBox16 : p.a_box, b_rows = B_MN ? kBox16 : C::kBRows;
     if (!make_map16(&maps.a, a, kBox16, a_rows) || !make_map16(&maps.b, b, kBox16, b_rows)) return FP4Q_ERR_CUDA;
     if (p.split && (!make_map16(&maps.a2, a2, kBox16, a_rows) || !make_map16(&maps.b2, b2, kBox16, b_rows))) return FP4Q_ERR_CUDA;
@@ -1169,7 +1179,7 @@ fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand1
     constexpr int kSmem = C::smem(TILES, EPI);
     static std::atomic<bool> attr_set[kMaxDevices];   // the attribute is a property of (kernel, device)
     if (!attr_set[dev].load(std::memory_order_relaxed)) {
-        if (cudaFuncSetAttribute(gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
+        if (cudaFuncSetAttribute(gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) {
             cudaGetLastError();
             return FP4Q_ERR_CUDA;
         }
@@ -1193,7 +1203,7 @@ fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand1
         attr[1].val.clusterDim.z = 1;
         cfg.numAttrs = 2;
     }
-    return launched(cudaLaunchKernelEx(&cfg, gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES>, maps, p));
+    return launched(cudaLaunchKernelEx(&cfg, gemm16_kernel<CTAS, BN, A_MN, B_MN, EPI, TILES, TWO>, maps, p));
 }
 
 }  // namespace fp4q

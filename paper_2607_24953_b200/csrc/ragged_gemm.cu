@@ -62,7 +62,7 @@ fp4q_status check_workspace(const void *ws, size_t ws_bytes)
 }
 Operand16 operand16(const Matrix16 &m, int64_t rows, int64_t batch) { return Operand16{m.p, m.cols, rows, batch, m.ld, rows * m.ld}; }
 
-template <int CTAS, int BN, bool A_MN, bool B_MN, int TILES>
+template <int CTAS, int BN, bool A_MN, bool B_MN, int TILES, bool TWO = false>
 fp4q_status launch_store16(const Operand16 &a, const Operand16 &b, Gemm16Params &p, fp4q_out dt, int64_t most_tiles, cudaStream_t stream)
 {
     Maps16 maps = {};
@@ -70,8 +70,8 @@ fp4q_status launch_store16(const Operand16 &a, const Operand16 &b, Gemm16Params 
     p.boxed = p.n / (f32 ? 4 : 8) * (f32 ? 4 : 8);   // a store of a box fills the 16 bytes in which a row ends
     const int64_t groups = TILES == TILES_CUT ? p.batch : 1;
     if (p.boxed > 0 && !make_map16(&maps.out, Operand16{p.c, p.boxed, p.m, groups, p.ldc, p.m * p.ldc}, f32 ? 32 : 64, 32, CU_TENSOR_MAP_SWIZZLE_128B, f32)) return FP4Q_ERR_CUDA;
-    return f32 ? launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_SUM, TILES>(a, b, a, b, maps, p, most_tiles, stream)
-               : launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_STORE, TILES>(a, b, a, b, maps, p, most_tiles, stream);
+    return f32 ? launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_SUM, TILES, TWO>(a, b, a, b, maps, p, most_tiles, stream)
+               : launch_gemm16<CTAS, BN, A_MN, B_MN, EPI16_STORE, TILES, TWO>(a, b, a, b, maps, p, most_tiles, stream);
 }
 
 // What a product of rows in tiles of rows x cols takes, in us, where `groups` groups may have rows and each fills its last tile by half: rounds of tiles
@@ -228,5 +228,7 @@ extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t
     }
     const Operand16 a = T ? operand16(d, T, 1) : Operand16{dW, 8, 1, 1, 8, 8}, b = T ? operand16(m, T, 1) : a;
     const int64_t most = groups * plan.m_tiles * plan.n_tiles + (plan.bytes ? plan.places : 0);
+    if (T < 256 * groups)   // short contractions
+        return plan.pairs ? launch_store16<2, 256, true, true, TILES_CUT, true>(a, b, p, dt, most, s) : launch_store16<1, 128, true, true, TILES_CUT, true>(a, b, p, dt, most, s);
     return plan.pairs ? launch_store16<2, 256, true, true, TILES_CUT>(a, b, p, dt, most, s) : launch_store16<1, 128, true, true, TILES_CUT>(a, b, p, dt, most, s);
 }
