@@ -121,7 +121,12 @@ def _rows16(t: torch.Tensor) -> torch.Tensor:
 
 def ragged_linear(x: torch.Tensor, weight: torch.Tensor, row_offsets: torch.Tensor, ws=None) -> torch.Tensor:
     """y_t = weight[g] x_t for the rows t of group g, in BF16: the expert layer as it is without FP4, on groups of any size.  x [T, K], weight
-    [E, N, K], row_offsets int64 [E+1], non-decreasing, all on one GPU; rows that no group owns give zeros and get no gradient."""
+    [E, N, K], row_offsets int64 [E+1], non-decreasing, all on one GPU; rows that no group owns give zeros and get no gradient.  Differentiable
+    once.  A backward pass that is captured into a CUDA graph needs, as with torch's own layers, leaves that no living eager graph holds."""
+    if x.dim() != 2 or weight.dim() != 3 or x.shape[1] != weight.shape[2]:
+        raise ValueError(f"x must be [T, K] and weight [E, N, K], not {list(x.shape)} and {list(weight.shape)}")
+    if row_offsets.dim() != 1 or row_offsets.shape[0] != weight.shape[0] + 1:
+        raise ValueError(f"row_offsets must hold one offset more than weight has groups, {weight.shape[0] + 1}, not {list(row_offsets.shape)}")
     if ws is None:
         ws = binding.alloc_workspace(x.device)
     return _RaggedLinearFn.apply(x, weight, row_offsets, ws)

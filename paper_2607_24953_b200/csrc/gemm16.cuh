@@ -7,7 +7,8 @@
 // each loads half of B's columns, which is what lets 32 KB of operands feed 2 x 256 x 256 x 64 operations per stage (an SM gets 32 KB from L2
 // in about 0.3 us, as long as the MMAs take at the clock that full load leaves); single CTAs have tiles of 128 x 128 for problems with few
 // tiles, and of 32 x 64 for short groups (the MMAs have 128 rows all the same: those behind the first 32 are whatever lies in shared
-// memory, and nobody looks at them).
+// memory, and nobody looks at them), and of 64 x 64 for small stacks of matrices.  Long contractions of few tiles are cut into parts, whose
+// accumulators meet in the caller's scratch memory.
 //   warps 0, 3  TMA producers of A and B: a stage is 64 contraction elements (32 x 64 tiles: 256), boxes of 128 bytes with the 128-byte swizzle
 //   warp 1      MMA issuer (in the leader of a pair): four tcgen05.mma of 16 contraction elements per box
 //   warp 2      cut contractions: deals the tiles (in the leader of a pair), zeroes the rows of a group's last stage that lie behind the group
@@ -56,19 +57,21 @@ struct Cfg16 {
     // 32 x 64 tiles take 128 cycles of MMAs per box, much less than a round of the issuer: their stages are four boxes deep, 64 x 64 ones' two.
     static constexpr int kBoxes = BN == 64 ? (STACK ? 2 : 4) : 1;
     static constexpr int kK = kBoxes * kBox16;                              // contraction elements per stage
-    static constexpr int kRows = BN == 64 ? (STACK ? 64 : 32) : kRows16;                   // rows of a CTA's part of a tile
+    static constexpr int kRows = BN == 64 ? (STACK ? 64 : 32) : kRows16;    // rows of a CTA's part of a tile
     static constexpr int kABox = kRows * 128, kBBox = kBRows * 128;
     static constexpr int kABytes = kBoxes * kABox, kBBytes = kBoxes * kBBox;
     static constexpr int kStages = BN == 64 && !STACK ? 3 : TWO ? 4 : 5;
     static constexpr int kTmemCols = 2 * BN;
     static constexpr int kOperands = kStages * (kABytes + kBBytes);
     static constexpr int kTail = 512;                                       // barriers, tensor memory's address, abort flag
-    static constexpr int kTables = 3 * (kMaxGroups16 + 1) * 4 + kMaxSorted16 * 2;              // row groups and cut contractions only
-    __host__ __device__ static constexpr int staging(int epi) { return !TWO && (epi == EPI16_STORE || epi == EPI16_SUM) ? 4096 : 8192; }   // of an epilogue warp: one box or two, or an upper and a lower one
+    static constexpr int kTables = 3 * (kMaxGroups16 + 1) * 4 + kMaxSorted16 * 2;   // row groups and cut contractions only
+    // Of an epilogue warp: one box or two, or an upper and a lower one.
+    __host__ __device__ static constexpr int staging(int epi) { return !TWO && (epi == EPI16_STORE || epi == EPI16_SUM) ? 4096 : 8192; }
     static constexpr int smem(int tiles, int epi) { return 1024 + kOperands + 8 * staging(epi) + kTail + (tiles <= TILES_CUT ? kTables : 0); }
     static constexpr int kTileRows = kRows * CTAS;
     static constexpr int64_t kPlaceBytes = (int64_t)CTAS * kRows16 * BN * 4;   // of a part's accumulator
-    static_assert(1024 + kOperands + 8 * (TWO ? 8192 : 4096) + kTail + kTables <= 227 * 1024 && ((BN == 64 && !STACK) || 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024), "shared memory budget");
+    static_assert(1024 + kOperands + 8 * (TWO ? 8192 : 4096) + kTail + kTables <= 227 * 1024, "shared memory budget: groups");
+    static_assert((BN == 64 && !STACK) || 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024, "shared memory budget: stacks");
 };
 
 struct Gemm16Params {
@@ -77,7 +80,7 @@ struct Gemm16Params {
     int32_t batch;                   // groups or matrices
     int32_t bf16;                    // operand type: 0 = FP16, 1 = BF16
     int32_t deals;                   // TILES_CUT: tiles go to whoever is free instead of in turn
-    int32_t a_box;                   // rows of one copy of a K-major A operand: 128; 32 or 16 in tiles of 32 rows
+    int32_t a_box;                   // rows of one copy of a K-major A operand: 128, 64 in 64 x 64 tiles, 32 or 16 in tiles of 32 rows
     const int64_t *offsets;          // TILES_ROWS, TILES_CUT: batch + 1 boundaries; NULL: one group of all rows
     int64_t total_rows;              // rows that the boundaries are held to
     uint32_t *status;
@@ -752,7 +755,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         }
     } else if (warp == 2 && TILES == TILES_CUT) {
         // ------------------------------------------------------------------ rows behind a group's end
-        // The last stage of a group holds rows of the next one, or whatever lies behind them.  Up to 15 of them meet an MMA: they are zeroed in
+        // The last stage of a group holds rows of the next one, or whatever lies behind it.  Up to 15 of them meet an MMA: they are zeroed in
         // both operands (in one, an infinity in the other would make NaN).  Then, and in a pair when the other CTA has done the same, the
         // stage is full.  A slot is filled again only when the MMAs have read it, so its barriers are never a phase ahead.
         uint32_t slot = 0, phases = 0;
@@ -1118,11 +1121,11 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     if (TILES == TILES_ROWS && p.zero_rest && warp >= 4) {
         constexpr int kElem = EPI == EPI16_SUM ? 4 : 2;
         const int64_t head = start[0], rest = head + p.total_rows - start[p.batch];
-        const int pieces = p.n * kElem / 16;
+        const int64_t halves = (int64_t)p.n * kElem / 2, pieces = halves / 8;
         for (int64_t i = blockIdx.x * 8 + warp - 4; i < rest; i += gridDim.x * 8) {
             uint8_t *row = static_cast<uint8_t *>(p.c) + (i < head ? i : start[p.batch] + i - head) * p.ldc * kElem;
-            for (int e = lane; e < pieces; e += 32) reinterpret_cast<uint4 *>(row)[e] = make_uint4(0u, 0u, 0u, 0u);
-            for (int e = pieces * 8 + lane; e < p.n * kElem / 2; e += 32) reinterpret_cast<uint16_t *>(row)[e] = 0;
+            for (int64_t e = lane; e < pieces; e += 32) reinterpret_cast<uint4 *>(row)[e] = make_uint4(0u, 0u, 0u, 0u);
+            for (int64_t e = pieces * 8 + lane; e < halves; e += 32) reinterpret_cast<uint16_t *>(row)[e] = 0;
         }
     }
 

@@ -293,6 +293,23 @@ def test_captured_and_on_another_stream():
     assert all(torch.equal(c, e) for c, e in zip(captured, eager)) and b.fp4q_workspace_status(ws) == 0
 
 
+def test_captured_with_contractions_in_parts():
+    T, n, k, values = 12000, 130, 72, [0, 11000, 11000, 12000]
+    dy, x = operands("wgrad", T, n, k, 3)
+    offs, ws, scratch = offsets(values), b.alloc_workspace("cuda"), b.alloc_ragged_wgrad_scratch(T, n, k, 3, "cuda")
+    want = call("wgrad", dy, x, offs, dt=b.OUT_F32, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call("wgrad", dy, x, offs, dt=b.OUT_F32, ws=ws, scratch=scratch)
+    for _ in range(3):
+        got.zero_()
+        scratch.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and b.fp4q_workspace_status(ws) == 0
+
+
 def test_a_wait_that_runs_out_is_reported():
     for T, e in ((4000, 1), (100, 4)):                      # pairs and single CTAs, whose first one always has a tile
         values = [0] + [T * (i + 1) // e for i in range(e)]

@@ -50,6 +50,15 @@ def test_products():
 C5 = (ctypes.c_float * 15)(*[3.4445, -4.775, 2.0315] * 5)
 
 
+def test_scratch_of_weight_gradients():
+    f = b.lib().fp4q_ragged_gemm_wgrad_scratch_bytes
+    assert f(0, 64, 64, 1) == f(64, 0, 64, 1) == f(64, 64, 64, 0) == f(64, 64, 64, 2048) == f(-1, 64, 64, 1) == 0
+    assert f(300, 1024, 512, 64) == 0                       # nothing to cut
+    assert 0 < f(131072, 768, 2048, 1) < 1 << 28 and 0 < f(131072, 128, 64, 4) < 1 << 28
+    call = lambda scratch, size: b.lib().fp4q_ragged_gemm_wgrad(P, 131072, 64, 64, P, 64, 64, P, 64, 1, 0, None, scratch, size, P, 256, None)
+    assert call(P, 16) == 5 and call(P + 16, 1 << 30) == 3
+
+
 def update(g=P, dt=1, count=2, rows=30, cols=50, ldg=50, m=P, ldm=50, eps=1e-7, c=C5, steps=5, out=P, ldo=50, scratch=P, sb=1 << 30, ws=P, wsb=256):
     return b.lib().fp4q_newton_schulz(g, dt, count, rows, cols, ldg, m, ldm, 0.9, 1, c, steps, eps, 1.0, out, ldo, scratch, sb, ws, wsb, None)
 
@@ -84,3 +93,11 @@ def test_the_binding_refuses_tensors_of_other_kinds():
         b.fp4q_newton_schulz(torch.zeros(8, 16))
     with pytest.raises(TypeError):
         b.fp4q_newton_schulz([1.0, 2.0])
+
+
+def test_the_layer_refuses_shapes_that_do_not_belong_together():
+    from paper_2607_24953_b200.autograd import ragged_linear
+    x, w, offs = torch.zeros(10, 16), torch.zeros(4, 8, 16), torch.zeros(5, dtype=torch.int64)
+    for bad in [(x, w, offs[:3]), (x, w, offs[None]), (x, w[0], offs), (x[0], w, offs), (x[:, :8], w, offs)]:
+        with pytest.raises(ValueError):
+            ragged_linear(*bad)
