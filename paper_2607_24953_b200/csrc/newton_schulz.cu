@@ -11,7 +11,7 @@
 // the operand of the products.  The term a X carries directions of small singular values from step to step, multiplied by a = 3.4 each time,
 // and rounding X as a whole puts noise into those that a gradient does not have (rank 100, 768 x 2048: the update is off by 1.8e-2 with one
 // FP16 number and 1.4e-1 with a BF16 one, 7e-4 with the sum of two).  Matrices of a short side have few elements over which the roundings of
-// A, P and the products' X average out (1.5e-3 of the result at 777 x 1003, 2.0e-3 at 64 x 64, 3e-3 and more below 16) and little work:
+// A, P and the products' X average out (0.8e-3 of the result at 777 x 1003, 2.0e-3 at 64 x 64, 3e-3 and more below 16) and little work:
 // there A and P are sums of two numbers as well, and the three products are made of three each (kSplitSide).  Scales: X 2^10, A and P 2^9, so that elements of large matrices
 // stay above FP16's smallest normal number and the largest singular values that the entry point admits below its largest.
 #include "gemm16.cuh"
