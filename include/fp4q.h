@@ -420,8 +420,8 @@ fp4q_status fp4q_ragged_gemm_wgrad(const void *dy_bf16, int64_t T, int64_t N, in
  * (taken on the shorter side: for rows > cols the same polynomial is evaluated with A = X^T X).  g is BF16 or FP32 (g_type, a plain fp4q_out),
  * momentum FP32 [count*rows, ld_m], out BF16; each with its leading dimension in elements, aligned to its element.  None of the three may
  * overlap another.  coefficients is a HOST array, read during the call; steps 1 to 64.  (3.4445, -4.7750, 2.0315) five times is the usual choice.
- * Coefficients that let a singular value exceed 10, or an eigenvalue of b A + c A A 100, are refused (FP4Q_ERR_UNSUPPORTED): the
- * products' operands are FP16.  eps >= 0; a matrix U of zeros gives zeros if eps > 0.  A matrix that holds an infinity or NaN gives NaN
+ * Coefficients that let a singular value exceed 10, or an eigenvalue of b A + c A A or a I + b A + c A A 100, are refused
+ * (FP4Q_ERR_UNSUPPORTED): the products' operands are FP16.  eps >= 0; a matrix U of zeros gives zeros if eps > 0.  A matrix that holds an infinity or NaN gives NaN
  * and leaves the others as they are.  The iterate X is held in 22 bits and the sum of squares in 64-bit floating point.
  * scratch: fp4q_newton_schulz_scratch_bytes() bytes of device memory, 256-byte aligned, any contents; calls that share it must not overlap
  * on the GPU.  fp4q_newton_schulz_scratch_bytes returns 0 for sizes that the call refuses or that are empty.  Sides up to 2^20, up to

@@ -96,14 +96,14 @@ struct Gemm16Params {
     int32_t accumulate, wide, zero_rest;   // zero_rest: rows that no group owns are written as zeros
     int32_t boxed;                   // columns that leave in boxes, whole 16 bytes; the rest of a row leaves by itself
     // EPI16_GRAM, _POLY, _UPDATE
-    int32_t split;                   // operands are sums of two numbers: the products upper x upper, upper x lower and lower x upper are added up
-    float fa, fb, fc;                // the step's coefficients, with the iterates' scales
+    int32_t split;                   // 1: operands are sums of two numbers: the products upper x upper, upper x lower and lower x upper are added up
+    float fa, fb, fc;                // the step's coefficients, with the iterates' scales; POLY: fa on the diagonal
     __nv_bfloat16 *o;                // UPDATE, last step: the result instead
     int64_t ld_o;
     float o_scale;
 };
 
-// Operands and their lower parts; what an epilogue reads (POLY: A, UPDATE: X) and writes, upper and lower parts, in boxes of 32 rows x 128
+// Operands and their lower parts; what an epilogue reads (POLY: A, UPDATE: X's lower part, as in) and writes, upper and lower parts, in boxes of 32 rows x 128
 // bytes; the mirrored tiles of symmetric results, in boxes of 64 rows x 64 bytes.
 struct Maps16 {
     CUtensorMap a, b, a2, b2, in, in2, out, out2, mirror, mirror2;
@@ -113,21 +113,28 @@ struct Maps16 {
 struct Tile16 {
     int32_t batch, a_row, b_row, k0, k_len;    // where the operands start along M and N, where the contraction starts and how long it is
     int32_t row, col, rows, rows_peer;         // first output row and column of this CTA's half, its valid rows and the other CTA's
-    int32_t s0, s1, k_stages;                  // its stages (a part of all), and those of one pass over the contraction
+    int32_t s0, s1;                            // its stages (a part of all)
     int32_t parts, slot0, counter;             // parts of the contraction; where the first one's accumulator goes; the tile's counter
-    bool mirror;                               // TILES_SYM: below the diagonal, so the transposed tile is written too
+    bool mirror;                               // TILES_SYM: below the diagonal, so the transposed tile is written too; on it, A's boxes serve as B's
 };
 
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar)
+// By the lanes for which `issue` holds, without a branch (see tcgen05_mma_f16).  PAIR: the copy is counted on a barrier of the pair's leader.
+template <bool PAIR = false>
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar, bool issue = true)
 {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+    if (PAIR)
+        asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %6, 0;\n"
+                     "@q cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n}"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "r"((uint32_t)issue) : "memory");
+    else
+        asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %6, 0;\n"
+                     "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n}"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "r"((uint32_t)issue) : "memory");
 }
-// Of either CTA of a pair: the bytes are counted on the leader's barrier.
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t leader_bar)
+__device__ __forceinline__ void expect_tx_if(uint32_t bar, uint32_t bytes, bool issue)
 {
-    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(leader_bar) : "memory");
+    asm volatile("{\n .reg .pred q;\n .reg .b64 state;\n setp.ne.b32 q, %2, 0;\n @q mbarrier.arrive.expect_tx.shared::cta.b64 state, [%0], %1;\n}"
+                 ::"r"(bar), "r"(bytes), "r"((uint32_t)issue) : "memory");
 }
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t src)
 {
@@ -153,15 +160,28 @@ __device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_bar
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
+// By the lanes for which `issue` holds.  The whole warp comes here, without a branch: what an instruction takes from uniform registers stays in them
+// (a lane that branches off moves six words there for every MMA).  Descriptors: their lower words, which hold the address, and the upper one.
 template <int CTAS>
-__device__ __forceinline__ void tcgen05_mma_f16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void tcgen05_mma_f16(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool accumulate, bool issue)
 {
     if (CTAS == 2)
-        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
-                     ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+        asm volatile("{\n .reg .pred p, q;\n .reg .b64 a, b;\n setp.ne.b32 p, %5, 0;\n setp.ne.b32 q, %6, 0;\n mov.b64 a, {%1, %3};\n mov.b64 b, {%2, %3};\n"
+                     "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %4, p;\n}"
+                     ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"((uint32_t)accumulate), "r"((uint32_t)issue) : "memory");
     else
-        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                     ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+        asm volatile("{\n .reg .pred p, q;\n .reg .b64 a, b;\n setp.ne.b32 p, %5, 0;\n setp.ne.b32 q, %6, 0;\n mov.b64 a, {%1, %3};\n mov.b64 b, {%2, %3};\n"
+                     "@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n}"
+                     ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"((uint32_t)accumulate), "r"((uint32_t)issue) : "memory");
+}
+template <int CTAS>
+__device__ __forceinline__ void tcgen05_commit_if(uint32_t bar, bool issue)
+{
+    if (CTAS == 1)
+        asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar), "r"((uint32_t)issue) : "memory");
+    else   // arrives on the barrier at this offset in both CTAs of the pair
+        asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %2, 0;\n @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}"
+                     ::"r"(bar), "h"((uint16_t)3), "r"((uint32_t)issue) : "memory");
 }
 // MN-major operand tile: chunks of 64 elements x 64 contraction rows (8 KB each), a row of a chunk 128 bytes with the 128-byte swizzle;
 // eight contraction rows make 1024 bytes.
@@ -189,14 +209,14 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
     return done != 0u;
 }
 template <bool CLUSTER>
-__device__ __forceinline__ bool warp_test(uint32_t bar, uint32_t parity)   // a look at it, without suspension
+__device__ __forceinline__ bool mbar_look(uint32_t bar, uint32_t parity)   // without suspension
 {
     uint32_t done;
     if (CLUSTER)
         asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     else
         asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return __all_sync(0xFFFFFFFFu, done != 0u);
+    return done != 0u;
 }
 __device__ __forceinline__ uint64_t now_ns()
 {
@@ -325,14 +345,22 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
     t.a_row = t.row;
     t.rows = max(0, min(kRows, valid - rank * kRows));
     t.rows_peer = CTAS == 2 ? max(0, min(kRows, valid - (1 - rank) * kRows)) : 0;
-    t.k_stages = (t.k_len + kK - 1) / kK;
+    const int stages = passes * ((t.k_len + kK - 1) / kK);
     t.s0 = part * p.part_stages;
-    t.s1 = t.parts == 1 ? passes * t.k_stages : min(t.s0 + p.part_stages, passes * t.k_stages);
+    t.s1 = t.parts == 1 ? stages : min(t.s0 + p.part_stages, stages);
     return t;
 }
-// A stage's pass over the contraction (operands in two parts), and where it starts in it.
+// Operands in two numbers take two stages for a piece of the contraction, upper and lower parts: whether a stage is the second, and how much of
+// the contraction (of k_len) is left where it starts.  Three loads of each, one for every product, took a third longer (256 x 256 113 us).
 template <bool SPLITS>
-__device__ __forceinline__ int pass16(const Tile16 &t, int s) { return SPLITS ? (s >= t.k_stages) + (s >= 2 * t.k_stages) : 0; }
+__device__ __forceinline__ bool lower16(const Gemm16Params &p, int s) { return SPLITS && (s & p.split) != 0; }
+template <bool SPLITS, int K>
+__device__ __forceinline__ int left16(const Gemm16Params &p, const Tile16 &t, int s) { return t.k_len - (SPLITS ? s >> p.split : s) * K; }
+
+// On the diagonal of a symmetric product both operands are the same rows: they are loaded once.  (128 of 768 x 2048, where half of the tiles lie
+// there: P's stages 0.65 -> 0.57 us.)
+template <int TILES>
+__device__ __forceinline__ bool shares_a(const Tile16 &t) { return TILES == TILES_SYM && !t.mirror; }
 
 // ---------------------------------------------------------------------------------------- epilogues: 32 columns of a thread's row
 
@@ -610,7 +638,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             __syncthreads();
         }
     }
-    const int passes = kSplits && p.split ? 3 : 1;   // upper x upper, upper x lower, lower x upper
+    const int passes = kSplits && p.split ? 2 : 1;   // stages for a piece of the contraction
     const int tiles = TILES == TILES_ROWS ? m_tiles * p.n_tiles : TILES == TILES_CUT && p.partial ? *shared_tiles : TILES <= TILES_BATCH ? p.batch * m_tiles * p.n_tiles
                       : p.batch * (m_tiles * (m_tiles + 1) / 2) * parts16(p, passes * ((p.k + C::kK - 1) / C::kK));   // or parts of tiles
     const int tile0 = blockIdx.x / CTAS, step = gridDim.x / CTAS;
@@ -643,61 +671,60 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         bool ok = true;
         const bool issuer = elect_one();
         const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b), lead = CTAS == 2 ? cluster_addr(bar_full, 0) : bar_full;
-        // The boxes of a stage of this side, each handed to f: destination in the stage, map, coordinates.
-        auto boxes_of = [&](const Tile16 &t, int st, auto f) {
-            const int pass = pass16<kSplits>(t, st), k = (st - pass * t.k_stages) * C::kK, left = t.k_len - k;
-            const int boxes = C::kBoxes == 1 ? 1 : min(C::kBoxes, (left + kBox16 - 1) / kBox16), at0 = t.k0 + k;
-            // TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack
+        // The boxes of a stage of this side.  TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack.
+        auto load_stage = [&](const Tile16 &t, int st, int copies, uint32_t to, uint32_t bar, bool in_pair, bool issue) {
+            const int left = left16<kSplits, C::kK>(p, t, st), at0 = t.k0 + t.k_len - left;
+            auto load = [&](uint32_t offset, const CUtensorMap *map, int x, int y, int z, bool there) {
+                if (CTAS == 2 && in_pair) tma_load_3d<true>(to + offset, map, x, y, z, bar, there);
+                else tma_load_3d(to + offset, map, x, y, z, bar, there);
+            };
             if (a_side) {
-                const CUtensorMap *map = kSplits && pass == 2 ? &maps.a2 : &maps.a;
-                const int z = TILES <= TILES_CUT ? 0 : t.batch, copies = A_MN ? C::kRows / 64 : (t.rows + p.a_box - 1) / p.a_box;
+                const CUtensorMap *map = lower16<kSplits>(p, st) ? &maps.a2 : &maps.a;
+                const int z = TILES <= TILES_CUT ? 0 : t.batch;
+                constexpr int kCopies = A_MN ? C::kRows / 64 : C::kRows == 32 ? 2 : 1;
                 const uint32_t copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
 #pragma unroll
-                for (int i = 0; i < C::kBoxes; i++) {
-                    if (i >= boxes) break;
-                    for (int j = 0; j < copies; j++)
-                        if (A_MN) f(i * C::kABox + j * copy_bytes, map, t.a_row + 64 * j, at0 + i * kBox16, z);
-                        else f(i * C::kABox + j * copy_bytes, map, at0 + i * kBox16, t.a_row + j * p.a_box, z);
-                }
+                for (int i = 0; i < C::kBoxes; i++)
+#pragma unroll
+                    for (int j = 0; j < kCopies; j++) {
+                        const bool there = issue && j < copies && i * kBox16 < left;
+                        if (A_MN) load(i * C::kABox + j * copy_bytes, map, t.a_row + 64 * j, at0 + i * kBox16, z, there);
+                        else load(i * C::kABox + j * copy_bytes, map, at0 + i * kBox16, t.a_row + j * p.a_box, z, there);
+                    }
             } else {
-                const CUtensorMap *map = kSplits && pass == 1 ? &maps.b2 : &maps.b;
+                const CUtensorMap *map = lower16<kSplits>(p, st) ? &maps.b2 : &maps.b;
                 const int z = TILES == TILES_CUT ? 0 : t.batch;
 #pragma unroll
                 for (int i = 0; i < C::kBoxes; i++) {
-                    if (i >= boxes) break;
+                    const bool there = issue && i * kBox16 < left;
                     if (B_MN) {
 #pragma unroll
-                        for (int j = 0; j < C::kBRows / 64; j++) f(i * C::kBBox + j * 8192, map, t.b_row + 64 * j, at0 + i * kBox16, z);
+                        for (int j = 0; j < C::kBRows / 64; j++) load(i * C::kBBox + j * 8192, map, t.b_row + 64 * j, at0 + i * kBox16, z, there);
                     } else {
-                        f(i * C::kBBox, map, at0 + i * kBox16, t.b_row, z);
+                        load(i * C::kBBox, map, at0 + i * kBox16, t.b_row, z, there);
                     }
                 }
             }
         };
+        static_assert(TILES != TILES_SYM || (A_MN == B_MN && C::kABytes == C::kBBytes), "a symmetric product's operands lie alike");
         for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, passes, start, first, slots, order, rank);
             const int a_copies = A_MN ? C::kRows / 64 : (t.rows + p.a_box - 1) / p.a_box;
             const uint32_t a_copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
-            const uint32_t box_bytes = (uint32_t)a_copies * a_copy_bytes + (uint32_t)C::kBBox;   // of this CTA
-            const uint32_t peer_bytes = CTAS == 2 ? (uint32_t)(A_MN ? 2 : (t.rows_peer + p.a_box - 1) / p.a_box) * a_copy_bytes + (uint32_t)C::kBBox : 0u;
+            const uint32_t a_bytes = (uint32_t)a_copies * a_copy_bytes;   // of this CTA, and of the other
+            const uint32_t a_peer = CTAS == 2 ? (uint32_t)(A_MN ? C::kRows / 64 : (t.rows_peer + p.a_box - 1) / p.a_box) * a_copy_bytes : 0u;
             for (int s = t.s0; s < t.s1; s++, ring.next()) {
                 if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) { ok = false; break; }
                 issued++;
                 // A stage with rows behind its group's end lands on a barrier of its own in each CTA, where warp 2 waits for it.
-                const int left = t.k_len - (s - pass16<kSplits>(t, s) * t.k_stages) * C::kK;
-                const bool cut = TILES == TILES_CUT && left < C::kK;
-                if (issuer) {
-                    const int boxes = C::kBoxes == 1 ? 1 : min(C::kBoxes, (left + kBox16 - 1) / kBox16);
-                    const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * ring.slot, bar = CTAS == 2 && !cut ? lead + 8 * ring.slot : own_bar;
-                    if (a_side && (rank == 0 || cut)) mbar_arrive_expect_tx(own_bar, (uint32_t)boxes * (box_bytes + (cut ? 0u : peer_bytes)));
-                    if (withhold == 0u || !a_side || ++loads != withhold) {
-                        const uint32_t to = a_side ? a0 + ring.slot * C::kABytes : b0 + ring.slot * C::kBBytes;
-                        boxes_of(t, s, [&](uint32_t offset, const CUtensorMap *map, int x, int y, int z) {
-                            if (CTAS == 2 && !cut) tma_load_3d_pair(to + offset, map, x, y, z, bar);
-                            else tma_load_3d(to + offset, map, x, y, z, bar);
-                        });
-                    }
-                }
+                const int left = left16<kSplits, C::kK>(p, t, s);
+                const bool cut = TILES == TILES_CUT && left < C::kK, own_b = !shares_a<TILES>(t);
+                const uint32_t b_bytes = own_b ? (uint32_t)C::kBBox : 0u;
+                const int boxes = C::kBoxes == 1 ? 1 : min(C::kBoxes, (left + kBox16 - 1) / kBox16);
+                const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * ring.slot, bar = CTAS == 2 && !cut ? lead + 8 * ring.slot : own_bar;
+                expect_tx_if(own_bar, (uint32_t)boxes * (a_bytes + b_bytes + (CTAS == 1 || cut ? 0u : a_peer + b_bytes)), issuer && a_side && (rank == 0 || cut));
+                if ((a_side || own_b) && (withhold == 0u || !a_side || ++loads != withhold))
+                    load_stage(t, s, a_copies, a_side ? a0 + ring.slot * C::kABytes : b0 + ring.slot * C::kBBytes, bar, !cut, issuer);
                 __syncwarp();
             }
             if (!ok) break;
@@ -713,13 +740,15 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         constexpr bool kPeerFills = TILES == TILES_CUT && CTAS == 2;   // the other CTA's warp 2 has part in "full"
         bool ok = true, ready = false, acc_ready = false;   // the next stage has been seen full, the next accumulator empty
         const bool issuer = elect_one();
-        const uint64_t a_desc0 = A_MN ? smem_desc_mn_sw128(smem_u32(smem_a)) : smem_desc_sw128(smem_u32(smem_a));
-        const uint64_t b_desc0 = B_MN ? smem_desc_mn_sw128(smem_u32(smem_b)) : smem_desc_sw128(smem_u32(smem_b));
+        const uint32_t a_desc0 = (uint32_t)(A_MN ? smem_desc_mn_sw128(smem_u32(smem_a)) : smem_desc_sw128(smem_u32(smem_a)));
+        const uint32_t b_desc0 = (uint32_t)(B_MN ? smem_desc_mn_sw128(smem_u32(smem_b)) : smem_desc_sw128(smem_u32(smem_b)));
+        constexpr uint32_t desc_hi = (1024 >> 4) | (1u << 14) | (2u << 29);   // of either order
         for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, passes, start, first, slots, order, rank);
-            uint32_t d = 0;
+            const uint32_t b_desc = shares_a<TILES>(t) ? a_desc0 : b_desc0;
+            uint32_t d = 0, upper = 0;
             for (int s = t.s0; s < t.s1; s++) {
-                const int left = t.k_len - (s - pass16<kSplits>(t, s) * t.k_stages) * C::kK, n = s - t.s0;
+                const int left = left16<kSplits, C::kK>(p, t, s), n = s - t.s0;
                 constexpr int kChunk = kSumElems / C::kK;
                 const bool opens = EPI == EPI16_SUM ? n % kChunk == 0 : n == 0;
                 const bool closes = s == t.s1 - 1 || (EPI == EPI16_SUM && n % kChunk == kChunk - 1);
@@ -730,26 +759,37 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 if (!ready && !warp_wait<kPeerFills>(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot)) { ok = false; break; }
                 const uint32_t slot = ring.slot;
                 ring.next();
-                // Looked at before this stage is issued: afterwards the look would wait for the MMAs.
-                ready = warp_test<kPeerFills>(bar_full + 8 * ring.slot, ring.phase);
+                // Looked at before this stage is issued: afterwards the look would wait for the MMAs.  What it saw is asked for after them.
+                const bool full = mbar_look<kPeerFills>(bar_full + 8 * ring.slot, ring.phase);
+                bool empty = false;
                 const uint32_t acc_bar = 8 * acc.slot;
                 if (closes) {
                     acc.next();
-                    acc_ready = warp_test<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u);
+                    empty = mbar_look<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u);
                 }
                 tcgen05_fence_after();
-                if (issuer) {
+                auto product = [&](uint32_t a_slot, uint32_t b_slot, bool adds) {
 #pragma unroll
                     for (int j = 0; j < 4 * C::kBoxes; j++) {
                         constexpr int kAStep = A_MN ? 2048 : 32, kBStep = B_MN ? 2048 : 32;
-                        const uint64_t ad = a_desc0 + (uint64_t)((slot * C::kABytes + (j / 4) * C::kABox + (j % 4) * kAStep) >> 4);
-                        const uint64_t bd = b_desc0 + (uint64_t)((slot * C::kBBytes + (j / 4) * C::kBBox + (j % 4) * kBStep) >> 4);
-                        if (16 * j < left) tcgen05_mma_f16<CTAS>(d, ad, bd, idesc, !opens || j > 0);
+                        const uint32_t ad = a_desc0 + ((a_slot * C::kABytes + (j / 4) * C::kABox + (j % 4) * kAStep) >> 4);
+                        const uint32_t bd = b_desc + ((b_slot * C::kBBytes + (j / 4) * C::kBBox + (j % 4) * kBStep) >> 4);
+                        tcgen05_mma_f16<CTAS>(d, ad, bd, desc_hi, idesc, adds || j > 0, issuer && 16 * j < left);
                     }
-                    tcgen05_commit<CTAS>(bar_empty + 8 * slot);
-                    if (closes) tcgen05_commit<CTAS>(bar_acc_full + acc_bar);
+                };
+                if (lower16<kSplits>(p, s)) {   // with the upper parts, which lie in the stage before
+                    product(upper, slot, true);
+                    product(slot, upper, true);
+                    tcgen05_commit_if<CTAS>(bar_empty + 8 * upper, issuer);
+                    tcgen05_commit_if<CTAS>(bar_empty + 8 * slot, issuer);
+                } else {
+                    product(slot, slot, !opens);
+                    if (!kSplits || !p.split) tcgen05_commit_if<CTAS>(bar_empty + 8 * slot, issuer);
                 }
-                __syncwarp();
+                if (closes) tcgen05_commit_if<CTAS>(bar_acc_full + acc_bar, issuer);
+                upper = slot;
+                ready = __all_sync(0xFFFFFFFFu, full);
+                if (closes) acc_ready = __all_sync(0xFFFFFFFFu, empty);
             }
             if (!ok) break;
         }
@@ -974,15 +1014,17 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 continue;
             }
             // What a step's epilogue reads is fetched before it waits for the accumulator, and for a later chunk when the one before has left.
-            constexpr bool kReads = EPI == EPI16_POLY || EPI == EPI16_UPDATE;
+            // P has a I in it, so that the product brings a X as well; a times X's lower part is left to add, or nothing where that is an operand too.
             const bool two = EPI == EPI16_UPDATE || p.split != 0;      // upper and lower parts
+            const bool reads_up = EPI == EPI16_POLY, reads_lo = EPI == EPI16_UPDATE ? p.split == 0 : EPI == EPI16_POLY && p.split != 0;
+            const bool reads = reads_up || reads_lo;
             auto fetch = [&](int col) {
-                if (!kReads || rows <= 0 || col >= p.n) return;
+                if (!reads || rows <= 0 || col >= p.n) return;
                 boxes_free(lane);
                 if (lane == 0) {
-                    mbar_arrive_expect_tx(bar_box, two ? 8192u : 4096u);
-                    tma_load_3d(boxes, &maps.in, col, row0, batch, bar_box);
-                    if (two) tma_load_3d(boxes + 4096, &maps.in2, col, row0, batch, bar_box);
+                    mbar_arrive_expect_tx(bar_box, reads_up && reads_lo ? 8192u : 4096u);
+                    if (reads_up) tma_load_3d(boxes, &maps.in, col, row0, batch, bar_box);
+                    if (reads_lo) tma_load_3d(boxes + 4096, &maps.in2, col, row0, batch, bar_box);
                 }
             };
             fetch(col0);
@@ -1010,6 +1052,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 if (kParts && t.parts > 1) {
                     if (col < p.n) add_parts(reinterpret_cast<float *>(v), c, kChunk);
                 } else if (chunks > 0) {
+
 #pragma unroll
                     for (int e = 0; e < kChunk; e += 32) FP4Q_TMEM_LD_X32(from + acc.slot * BN + c + e, (v + e));
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -1029,17 +1072,17 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     continue;
                 }
                 if (rows <= 0 || col >= p.n) continue;
-                if (kReads) {
+                if (reads) {
                     if (!warp_wait(bar_box, box_phase, abort_flag, p.status, limit, 0x800u)) { ok = false; break; }
                     box_phase ^= 1u;
                 }
                 // The new values, upper and lower parts, replace those that were read, a piece of eight columns at a time.
                 const bool out = EPI == EPI16_UPDATE && p.o;
-                if (!kReads) boxes_free(lane);
+                if (!reads) boxes_free(lane);
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
                     float w[8];
-                    const uint4 a = kReads ? ld_shared_16(up.piece(i)) : make_uint4(0u, 0u, 0u, 0u), b = kReads && two ? ld_shared_16(lo.piece(i)) : make_uint4(0u, 0u, 0u, 0u);
+                    const uint4 a = reads_up ? ld_shared_16(up.piece(i)) : make_uint4(0u, 0u, 0u, 0u), b = reads_lo ? ld_shared_16(lo.piece(i)) : make_uint4(0u, 0u, 0u, 0u);
                     const uint32_t au[4] = {a.x, a.y, a.z, a.w}, bu[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
                     for (int j = 0; j < 4; j++) {
@@ -1062,6 +1105,19 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                         if (two) st_shared_16(lo.piece(i), l[0], l[1], l[2], l[3]);
                     }
                     st_shared_16(up.piece(i), h[0], h[1], h[2], h[3]);
+                }
+                if (EPI == EPI16_POLY) {   // a I: this row's element in the box, if it has one
+                    const uint32_t e = (uint32_t)(row0 + lane - col);
+                    if (e < 64u) {
+                        const uint32_t at = (e & 7u) * 2u;
+                        uint16_t h, l = 0;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(up.piece(e >> 3) + at) : "memory");
+                        if (two) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(l) : "r"(lo.piece(e >> 3) + at) : "memory");
+                        const float w = unpack_half(h).x + unpack_half(l).x + p.fa;
+                        const uint32_t v_up = pack_half(w, 0.f), v_lo = pack_half(w - unpack_half(v_up).x, 0.f);
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(up.piece(e >> 3) + at), "h"((uint16_t)v_up) : "memory");
+                        if (two) asm volatile("st.shared.u16 [%0], %1;" ::"r"(lo.piece(e >> 3) + at), "h"((uint16_t)v_lo) : "memory");
+                    }
                 }
                 fence_async_shared();
                 __syncwarp();

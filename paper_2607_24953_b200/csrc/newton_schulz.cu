@@ -2,13 +2,14 @@
 //
 //   X <- U / (|U| + eps);  per step, with A = X X^T on the shorter side:  X <- a X + (b A + c A A) X
 //
-// A step is three products: A = X X^T and P = b A + c A A are symmetric, so only the tiles on and below the diagonal are computed and
-// written to both places; X' = a X + P X reads X once more in its epilogue.  A matrix that is taller than wide keeps its layout: A = X^T X
-// and X' = a X + X P, with operands read across their rows.
+// A step is three products: A = X X^T and P = a I + b A + c A A are symmetric, so only the tiles on and below the diagonal are computed and
+// written to both places; X' = P X.  A matrix that is taller than wide keeps its layout: A = X^T X and X' = X P, with operands read across
+// their rows.
 //
 // Precision.  The products' operands are FP16: values of X, A and P lie in a narrow range (singular values of at most about 1.3), so the
-// three bits that FP16 has more than BF16 cost nothing.  X itself is kept as a sum of two FP16 numbers (22 bits): what is rounded is only
-// the operand of the products.  The term a X carries directions of small singular values from step to step, multiplied by a = 3.4 each time,
+// three bits that FP16 has more than BF16 cost nothing.  X itself is kept as a sum of two FP16 numbers (22 bits): A's product takes the upper
+// one, and a times the lower one is added to P's product with the upper one.  P's diagonal is off by up to 2^-11 of itself, which is a factor on
+// a row (2e-4 of the result); the rows' directions are kept.  The term a X carries directions of small singular values from step to step, multiplied by a = 3.4 each time,
 // and rounding X as a whole puts noise into those that a gradient does not have (rank 100, 768 x 2048: the update is off by 1.8e-2 with one
 // FP16 number and 1.4e-1 with a BF16 one, 7e-4 with the sum of two).  Matrices of a short side have few elements over which the roundings of
 // A, P and the products' X average out (0.8e-3 of the result at 777 x 1003, 2.0e-3 at 64 x 64, 3e-3 and more below 16) and little work:
@@ -215,7 +216,7 @@ struct Scratch {
         lo[0] = place(x_bytes); lo[1] = split ? place(x_bytes) : lo[0];
         a[0] = place(a_bytes); a[1] = split ? place(a_bytes) : a[0];
         poly[0] = place(a_bytes); poly[1] = split ? place(a_bytes) : poly[0];
-        const int64_t stages = (split ? 3 : 1) * ceil_div(rows < cols ? cols : rows, kBox16);
+        const int64_t stages = (split ? 2 : 1) * ceil_div(rows < cols ? cols : rows, kBox16);
         const GramPlan one(count, side, stages, 128), two(count, side, stages, 256);
         const bool pairs = two.us < one.us;
         // 64 x 64 tiles, a quarter of a microsecond a box, where all of them run at once and no parts are faster: they are all computed, and not
@@ -224,7 +225,7 @@ struct Scratch {
         edge = small ? 64 : pairs ? 256 : 128;
         tiles = pairs ? two.tiles : one.tiles;
         const int64_t parts = edge == 64 ? 1 : pairs ? two.parts : one.parts;
-        part_stages = parts >= 2 ? ceil_div(stages, parts) : 0;
+        part_stages = parts >= 2 ? round_up(ceil_div(stages, parts), split ? 2 : 1) : 0;
         counters = place(part_stages ? (size_t)round_up(tiles * 2 * 8 * 4, 256) : 0);
         accumulators = place(part_stages ? (size_t)(tiles * parts * (edge == 256 ? Cfg16<2, 256>::kPlaceBytes : Cfg16<1, 128>::kPlaceBytes)) : 0);
     }
@@ -238,8 +239,8 @@ bool sizes_ok(int64_t count, int64_t rows, int64_t cols)
            count * rows * round_up(cols, 16) <= (1ll << 40) && count * ceil_div(rows, 128) * ceil_div(cols, 64) <= 0x7FFFFFFF - 4096;
 }
 
-// The largest singular value that X can have after each step, from at most 1, and the largest eigenvalue of b A + c A A: the polynomials
-// are sampled.  Whether FP16 holds all that they reach.
+// The largest singular value that X can have after each step, from at most 1, and the largest eigenvalues of b A + c A A and a I + b A + c A A: the
+// polynomials are sampled.  Whether FP16 holds all that they reach.
 bool steps_fit(const float *c, int32_t steps)
 {
     double top = 1.0;
@@ -247,7 +248,7 @@ bool steps_fit(const float *c, int32_t steps)
         double next = 0.0;
         for (int i = 0; i <= 512; i++) {
             const double x = top * i / 512, q = x * x, poly = c[3 * s + 1] * q + c[3 * s + 2] * q * q, y = std::fabs(x * (c[3 * s] + poly));
-            if (!(std::fabs(poly) <= 100.0) || !(y <= 10.0)) return false;
+            if (!(std::fabs(poly) <= 100.0) || !(std::fabs(c[3 * s] + poly) <= 100.0) || !(y <= 10.0)) return false;
             if (y > next) next = y;
         }
         top = next * 1.01;   // roundings
@@ -287,7 +288,7 @@ struct Steps {
     {
         Maps16 maps = {};
         int64_t tiles = symmetric_tiles(p);
-        if (p.partial) tiles *= ceil_div((p.split ? 3 : 1) * ceil_div(p.k, kBox16), p.part_stages);
+        if (p.partial) tiles *= ceil_div((p.split ? 2 : 1) * ceil_div(p.k, kBox16), p.part_stages);
         if (fp4q_status s = boxes16(&maps.out, &maps.out2, a, p.split)) return s;
         if (fp4q_status s = boxes16(&maps.mirror, &maps.mirror2, a, p.split, true)) return s;
         return tall ? launch_gemm16<CTAS, BN, true, true, EPI16_GRAM, kSym>(x.up, x.up, x.lo, x.lo, maps, p, tiles, stream)
@@ -309,7 +310,7 @@ struct Steps {
         p.m_tiles = (int32_t)ceil_div(p.m, kBM);
         p.n_tiles = (int32_t)ceil_div(p.n, BN);
         const int64_t tiles = (int64_t)p.batch * p.m_tiles * p.n_tiles;
-        if (fp4q_status s = boxes16(&maps.in, &maps.in2, x, true)) return s;
+        if (!p.split && !make_map16(&maps.in2, x.lo, 64, 32)) return FP4Q_ERR_CUDA;
         if (p.o) {
             if (p.boxed > 0 && !make_map16(&maps.out, Operand16{p.o, p.boxed, p.m, p.batch, p.ld_o, p.m * p.ld_o}, 64, 32)) return FP4Q_ERR_CUDA;
         } else if (fp4q_status s = boxes16(&maps.out, &maps.out2, next, true)) {
@@ -395,6 +396,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
             gp.counters = reinterpret_cast<uint32_t *>(base + at.counters);
         }
         pp.k = (int32_t)side;
+        pp.fa = c[0] * kScaleA;
         pp.fb = c[1];
         pp.fc = c[2] / kScaleA;
         Gemm16Params up = p;
