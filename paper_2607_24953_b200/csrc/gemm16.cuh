@@ -61,7 +61,12 @@ struct Cfg16 {
     static constexpr int kABox = kRows * 128, kBBox = kBRows * 128;
     static constexpr int kABytes = kBoxes * kABox, kBBytes = kBoxes * kBBox;
     static constexpr int kStages = BN == 64 && !STACK ? 3 : TWO ? 4 : 5;
-    static constexpr int kTmemCols = 2 * BN;
+    // 64 x 64 tiles of operands in two numbers: a stage's two boxes are the upper and lower parts of one, and an MMA of 128 x 128 multiplies both of A,
+    // above each other, with both of B.  The tile is the sum of the four quarters of what it makes.  (An MMA of 128 x 64, with rows for nothing, takes
+    // 48 cycles, of which 32 x 64 x 16 for each of three products would have needed SMALL_US.)
+    static constexpr bool kBoth = BN == 64 && STACK;
+    static constexpr int kAccCols = kBoth ? 128 : BN;
+    static constexpr int kTmemCols = 2 * kAccCols;
     static constexpr int kOperands = kStages * (kABytes + kBBytes);
     static constexpr int kTail = 512;                                       // barriers, tensor memory's address, abort flag
     static constexpr int kTables = 3 * (kMaxGroups16 + 1) * 4 + kMaxSorted16 * 2;   // row groups and cut contractions only
@@ -189,11 +194,11 @@ __device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t addr)
 {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(8192 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-template <int CTAS, int BN>
-__device__ __forceinline__ uint32_t instr_desc16(bool bf16, bool a_mn, bool b_mn)
+template <int CTAS>
+__device__ __forceinline__ uint32_t instr_desc16(bool bf16, bool a_mn, bool b_mn, int cols)
 {
     const uint32_t type = bf16 ? 1u : 0u;
-    return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(BN >> 3) << 17) |
+    return (1u << 4) | (type << 7) | (type << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(cols >> 3) << 17) |
            ((uint32_t)((kRows16 * CTAS) >> 4) << 24);
 }
 // A barrier's phase: CLUSTER if the other CTA of a pair arrives on it, whose writes this thread then sees.  (A fence behind the wait
@@ -345,7 +350,7 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
     t.a_row = t.row;
     t.rows = max(0, min(kRows, valid - rank * kRows));
     t.rows_peer = CTAS == 2 ? max(0, min(kRows, valid - (1 - rank) * kRows)) : 0;
-    const int stages = passes * ((t.k_len + kK - 1) / kK);
+    const int stages = C::kBoth && p.split ? (t.k_len + kBox16 - 1) / kBox16 : passes * ((t.k_len + kK - 1) / kK);
     t.s0 = part * p.part_stages;
     t.s1 = t.parts == 1 ? stages : min(t.s0 + p.part_stages, stages);
     return t;
@@ -353,9 +358,12 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
 // Operands in two numbers take two stages for a piece of the contraction, upper and lower parts: whether a stage is the second, and how much of
 // the contraction (of k_len) is left where it starts.  Three loads of each, one for every product, took a third longer (256 x 256 113 us).
 template <bool SPLITS>
-__device__ __forceinline__ bool lower16(const Gemm16Params &p, int s) { return SPLITS && (s & p.split) != 0; }
-template <bool SPLITS, int K>
-__device__ __forceinline__ int left16(const Gemm16Params &p, const Tile16 &t, int s) { return t.k_len - (SPLITS ? s >> p.split : s) * K; }
+__device__ __forceinline__ bool lower16(const Gemm16Params &p, int s) { return SPLITS && (s & p.split) != 0; }   // not in 64 x 64 tiles
+template <bool SPLITS, int K, bool BOTH>
+__device__ __forceinline__ int left16(const Gemm16Params &p, const Tile16 &t, int s)
+{
+    return t.k_len - (BOTH ? s * (p.split ? kBox16 : K) : (SPLITS ? s >> p.split : s) * K);
+}
 
 // On the diagonal of a symmetric product both operands are the same rows: they are loaded once.  (128 of 768 x 2048, where half of the tiles lie
 // there: P's stages 0.65 -> 0.57 us.)
@@ -466,14 +474,15 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
 {
     using C = Cfg16<CTAS, BN, TWO, (TILES >= TILES_BATCH)>;
     constexpr int kStages = C::kStages, kStaging = C::staging(EPI);
-    constexpr bool kSplits = EPI == EPI16_GRAM || EPI == EPI16_POLY || EPI == EPI16_UPDATE;
+    constexpr bool kSplits = EPI == EPI16_GRAM || EPI == EPI16_POLY || EPI == EPI16_UPDATE, kTwoStages = kSplits && !C::kBoth;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t *smem_a = smem, *smem_b = smem + kStages * C::kABytes;
     uint8_t *smem_boxes = smem + C::kOperands;
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem_boxes + 8 * kStaging);
     // bars[0..7] full, [8..15] empty, [16..17] accumulator full, [18..19] accumulator empty, [20..27] a group's last stage has landed here,
-    // [28..35] (leader of a pair) it is ready in the other CTA, [36..43] an epilogue warp's boxes have come, [44..47] a tile is dealt,
+    // [28..35] (leader of a pair) it is ready in the other CTA, [36..43] an epilogue warp's boxes have come ([40..43]
+    // in 64 x 64 tiles: lower halves of a tile's sums have been sent, and read), [44..47] a tile is dealt,
     // [48..51] (leader) it has been taken
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 52);
     volatile uint32_t *abort_flag = tmem_slot + 1;
@@ -511,7 +520,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         if (kSplits && p.split) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b2) : "memory");
     } else if (warp == 5 && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.out) : "memory");
-        if (EPI == EPI16_POLY || EPI == EPI16_UPDATE) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.in) : "memory");
+        if (EPI == EPI16_POLY) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.in) : "memory");
     }
     __syncthreads();
     if (CTAS == 2) { cluster_arrive(); cluster_wait(); }
@@ -639,6 +648,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         }
     }
     const int passes = kSplits && p.split ? 2 : 1;   // stages for a piece of the contraction
+    const bool both = C::kBoth && p.split;
     const int tiles = TILES == TILES_ROWS ? m_tiles * p.n_tiles : TILES == TILES_CUT && p.partial ? *shared_tiles : TILES <= TILES_BATCH ? p.batch * m_tiles * p.n_tiles
                       : p.batch * (m_tiles * (m_tiles + 1) / 2) * parts16(p, passes * ((p.k + C::kK - 1) / C::kK));   // or parts of tiles
     const int tile0 = blockIdx.x / CTAS, step = gridDim.x / CTAS;
@@ -673,13 +683,13 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b), lead = CTAS == 2 ? cluster_addr(bar_full, 0) : bar_full;
         // The boxes of a stage of this side.  TILES_ROWS and TILES_CUT: the token matrices are one matrix, the weights a stack.
         auto load_stage = [&](const Tile16 &t, int st, int copies, uint32_t to, uint32_t bar, bool in_pair, bool issue) {
-            const int left = left16<kSplits, C::kK>(p, t, st), at0 = t.k0 + t.k_len - left;
+            const int left = left16<kSplits, C::kK, C::kBoth>(p, t, st), at0 = t.k0 + t.k_len - left;
             auto load = [&](uint32_t offset, const CUtensorMap *map, int x, int y, int z, bool there) {
                 if (CTAS == 2 && in_pair) tma_load_3d<true>(to + offset, map, x, y, z, bar, there);
                 else tma_load_3d(to + offset, map, x, y, z, bar, there);
             };
             if (a_side) {
-                const CUtensorMap *map = lower16<kSplits>(p, st) ? &maps.a2 : &maps.a;
+                const CUtensorMap *map = lower16<kTwoStages>(p, st) ? &maps.a2 : &maps.a;
                 const int z = TILES <= TILES_CUT ? 0 : t.batch;
                 constexpr int kCopies = A_MN ? C::kRows / 64 : C::kRows == 32 ? 2 : 1;
                 const uint32_t copy_bytes = A_MN ? 8192u : (uint32_t)p.a_box * 128u;
@@ -687,21 +697,25 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 for (int i = 0; i < C::kBoxes; i++)
 #pragma unroll
                     for (int j = 0; j < kCopies; j++) {
-                        const bool there = issue && j < copies && i * kBox16 < left;
-                        if (A_MN) load(i * C::kABox + j * copy_bytes, map, t.a_row + 64 * j, at0 + i * kBox16, z, there);
-                        else load(i * C::kABox + j * copy_bytes, map, at0 + i * kBox16, t.a_row + j * p.a_box, z, there);
+                        const bool there = issue && j < copies && (both || i * kBox16 < left);
+                        const CUtensorMap *of = both && i == 1 ? &maps.a2 : map;
+                        const int at = at0 + (both ? 0 : i * kBox16);
+                        if (A_MN) load(i * C::kABox + j * copy_bytes, of, t.a_row + 64 * j, at, z, there);
+                        else load(i * C::kABox + j * copy_bytes, of, at, t.a_row + j * p.a_box, z, there);
                     }
             } else {
-                const CUtensorMap *map = lower16<kSplits>(p, st) ? &maps.b2 : &maps.b;
+                const CUtensorMap *map = lower16<kTwoStages>(p, st) ? &maps.b2 : &maps.b;
                 const int z = TILES == TILES_CUT ? 0 : t.batch;
 #pragma unroll
                 for (int i = 0; i < C::kBoxes; i++) {
-                    const bool there = issue && i * kBox16 < left;
+                    const bool there = issue && (both || i * kBox16 < left);
+                    const CUtensorMap *of = both && i == 1 ? &maps.b2 : map;
+                    const int at = at0 + (both ? 0 : i * kBox16);
                     if (B_MN) {
 #pragma unroll
-                        for (int j = 0; j < C::kBRows / 64; j++) load(i * C::kBBox + j * 8192, map, t.b_row + 64 * j, at0 + i * kBox16, z, there);
+                        for (int j = 0; j < C::kBRows / 64; j++) load(i * C::kBBox + j * 8192, of, t.b_row + 64 * j, at, z, there);
                     } else {
-                        load(i * C::kBBox, map, at0 + i * kBox16, t.b_row, z, there);
+                        load(i * C::kBBox, of, at, t.b_row, z, there);
                     }
                 }
             }
@@ -717,10 +731,10 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) { ok = false; break; }
                 issued++;
                 // A stage with rows behind its group's end lands on a barrier of its own in each CTA, where warp 2 waits for it.
-                const int left = left16<kSplits, C::kK>(p, t, s);
+                const int left = left16<kSplits, C::kK, C::kBoth>(p, t, s);
                 const bool cut = TILES == TILES_CUT && left < C::kK, own_b = !shares_a<TILES>(t);
                 const uint32_t b_bytes = own_b ? (uint32_t)C::kBBox : 0u;
-                const int boxes = C::kBoxes == 1 ? 1 : min(C::kBoxes, (left + kBox16 - 1) / kBox16);
+                const int boxes = C::kBoxes == 1 ? 1 : both ? 2 : min(C::kBoxes, (left + kBox16 - 1) / kBox16);
                 const uint32_t own_bar = (cut ? bar_cut : bar_full) + 8 * ring.slot, bar = CTAS == 2 && !cut ? lead + 8 * ring.slot : own_bar;
                 expect_tx_if(own_bar, (uint32_t)boxes * (a_bytes + b_bytes + (CTAS == 1 || cut ? 0u : a_peer + b_bytes)), issuer && a_side && (rank == 0 || cut));
                 if ((a_side || own_b) && (withhold == 0u || !a_side || ++loads != withhold))
@@ -734,7 +748,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             if (issued >= kStages - i) ok = warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x700u + ring.slot);
     } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------------------------ MMA issuer
-        const uint32_t idesc = instr_desc16<CTAS, BN>(p.bf16 != 0, A_MN, B_MN);
+        const uint32_t idesc = instr_desc16<CTAS>(p.bf16 != 0, A_MN, B_MN, both ? C::kAccCols : BN);
         Ring16<kStages> ring;
         Ring16<2> acc;      // accumulators
         constexpr bool kPeerFills = TILES == TILES_CUT && CTAS == 2;   // the other CTA's warp 2 has part in "full"
@@ -748,13 +762,13 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             const uint32_t b_desc = shares_a<TILES>(t) ? a_desc0 : b_desc0;
             uint32_t d = 0, upper = 0;
             for (int s = t.s0; s < t.s1; s++) {
-                const int left = left16<kSplits, C::kK>(p, t, s), n = s - t.s0;
+                const int left = left16<kSplits, C::kK, C::kBoth>(p, t, s), n = s - t.s0;
                 constexpr int kChunk = kSumElems / C::kK;
                 const bool opens = EPI == EPI16_SUM ? n % kChunk == 0 : n == 0;
                 const bool closes = s == t.s1 - 1 || (EPI == EPI16_SUM && n % kChunk == kChunk - 1);
                 if (opens) {
                     if (!acc_ready && !warp_wait<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u)) { ok = false; break; }
-                    d = tmem + acc.slot * BN;
+                    d = tmem + acc.slot * C::kAccCols;
                 }
                 if (!ready && !warp_wait<kPeerFills>(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot)) { ok = false; break; }
                 const uint32_t slot = ring.slot;
@@ -774,17 +788,17 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                         constexpr int kAStep = A_MN ? 2048 : 32, kBStep = B_MN ? 2048 : 32;
                         const uint32_t ad = a_desc0 + ((a_slot * C::kABytes + (j / 4) * C::kABox + (j % 4) * kAStep) >> 4);
                         const uint32_t bd = b_desc + ((b_slot * C::kBBytes + (j / 4) * C::kBBox + (j % 4) * kBStep) >> 4);
-                        tcgen05_mma_f16<CTAS>(d, ad, bd, desc_hi, idesc, adds || j > 0, issuer && 16 * j < left);
+                        tcgen05_mma_f16<CTAS>(d, ad, bd, desc_hi, idesc, adds || j > 0, issuer && 16 * j < left && (!both || j < 4));
                     }
                 };
-                if (lower16<kSplits>(p, s)) {   // with the upper parts, which lie in the stage before
+                if (lower16<kTwoStages>(p, s)) {   // with the upper parts, which lie in the stage before
                     product(upper, slot, true);
                     product(slot, upper, true);
                     tcgen05_commit_if<CTAS>(bar_empty + 8 * upper, issuer);
                     tcgen05_commit_if<CTAS>(bar_empty + 8 * slot, issuer);
                 } else {
                     product(slot, slot, !opens);
-                    if (!kSplits || !p.split) tcgen05_commit_if<CTAS>(bar_empty + 8 * slot, issuer);
+                    if (!kTwoStages || !p.split) tcgen05_commit_if<CTAS>(bar_empty + 8 * slot, issuer);
                 }
                 if (closes) tcgen05_commit_if<CTAS>(bar_acc_full + acc_bar, issuer);
                 upper = slot;
@@ -876,7 +890,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         const Box16 up(boxes, lane), lo(boxes + 4096, lane);
         constexpr int kCols = kNarrow ? BN : BN / 2, kChunk = EPI == EPI16_SUM || kCols < 64 ? 32 : 64;   // a warp's columns, and those of a box
         Ring16<2> acc;
-        uint32_t box_phase = 0, second = 0;
+        uint32_t box_phase = 0, second = 0, half_phase = 0;
         for (int tile = next_tile(-1); tile < tiles; tile = next_tile(tile)) {
             const Tile16 t = decode16<TILES, CTAS, BN>(p, tile, m_tiles, passes, start, first, slots, order, rank);
             const int in = 32 * quarter + lane;
@@ -993,7 +1007,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
 #pragma unroll
                     for (int c = 0; c < kCols; c += 16) {
                         uint32_t v[16];
-                        FP4Q_TMEM_LD_X16(from + acc.slot * BN + c, v);
+                        FP4Q_TMEM_LD_X16(from + acc.slot * C::kAccCols + c, v);
                         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
                         for (int e = 0; e < 16; e++) sum[c + e] += __uint_as_float(v[e]);
@@ -1037,7 +1051,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
 #pragma unroll 1
                 for (int c = 0; c < kCols; c += 32) {
                     uint32_t v[32];
-                    FP4Q_TMEM_LD_X32(from + acc.slot * BN + c, v);
+                    FP4Q_TMEM_LD_X32(from + acc.slot * C::kAccCols + c, v);
                     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
                     if (c == kCols - 32) release();
                     if (rows > 0 && col0 + c < p.n) put_part(reinterpret_cast<const float *>(v), c, 32);
@@ -1052,11 +1066,41 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 if (kParts && t.parts > 1) {
                     if (col < p.n) add_parts(reinterpret_cast<float *>(v), c, kChunk);
                 } else if (chunks > 0) {
-
 #pragma unroll
-                    for (int e = 0; e < kChunk; e += 32) FP4Q_TMEM_LD_X32(from + acc.slot * BN + c + e, (v + e));
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                    if (c == kCols - kChunk) release();
+                    for (int e = 0; e < kChunk; e += 32) FP4Q_TMEM_LD_X32(from + acc.slot * C::kAccCols + c + e, (v + e));
+                    if (C::kBoth && both) {
+                        float *sum = reinterpret_cast<float *>(v);
+                        uint32_t u[kChunk];
+#pragma unroll
+                        for (int e = 0; e < kChunk; e += 32) FP4Q_TMEM_LD_X32(from + acc.slot * C::kAccCols + BN + e, (u + e));
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+                        for (int e = 0; e < kChunk; e++) sum[e] += __uint_as_float(u[e]);
+                        release();
+                        // The lower halves, of warps 6 and 7, are added to the upper ones, of warps 4 and 5, by way of their boxes.
+                        const uint32_t half_box = smem_u32(smem_boxes) + (quarter | 2) * kStaging + lane * 256;
+                        const uint32_t sent = smem_u32(bars + 40 + (quarter & 1)), read = smem_u32(bars + 42 + (quarter & 1));   // warps 8 to 11 have no boxes
+                        if (warp >= 6 && warp < 8) {
+                            if (!warp_wait(read, half_phase ^ 1u, abort_flag, p.status, limit, 0xB00u)) { ok = false; break; }
+#pragma unroll
+                            for (int i = 0; i < kChunk / 4; i++) st_shared_16(half_box + ((i ^ (lane & 7)) << 4), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(sent);
+                        } else if (warp < 6) {
+                            if (!warp_wait(sent, half_phase, abort_flag, p.status, limit, 0xC00u)) { ok = false; break; }
+#pragma unroll
+                            for (int i = 0; i < kChunk / 4; i++) {
+                                const uint4 w = ld_shared_16(half_box + ((i ^ (lane & 7)) << 4));
+                                sum[4 * i] += __uint_as_float(w.x); sum[4 * i + 1] += __uint_as_float(w.y); sum[4 * i + 2] += __uint_as_float(w.z); sum[4 * i + 3] += __uint_as_float(w.w);
+                            }
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(read);
+                        }
+                        half_phase ^= 1u;
+                    } else {
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        if (c == kCols - kChunk) release();
+                    }
                 } else {
 #pragma unroll
                     for (int e = 0; e < kChunk; e++) v[e] = 0u;
