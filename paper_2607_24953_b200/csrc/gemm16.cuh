@@ -62,8 +62,8 @@ struct Cfg16 {
     static constexpr int kABytes = kBoxes * kABox, kBBytes = kBoxes * kBBox;
     static constexpr int kStages = BN == 64 && !STACK ? 3 : TWO ? 4 : 5;
     // 64 x 64 tiles of operands in two numbers: a stage's two boxes are the upper and lower parts of one, and an MMA of 128 x 128 multiplies both of A,
-    // above each other, with both of B.  The tile is the sum of the four quarters of what it makes.  (An MMA of 128 x 64, with rows for nothing, takes
-    // 48 cycles, of which 32 x 64 x 16 for each of three products would have needed SMALL_US.)
+    // above each other, with both of B.  The tile is the sum of the four quarters of what it makes.  (Three MMAs of 128 x 64, half of their rows for
+    // nothing, instead: 384 x 384 122 us for 113, four of 128 x 1000 127 for 116, 256 x 256 99 for 101.)
     static constexpr bool kBoth = BN == 64 && STACK;
     static constexpr int kAccCols = kBoth ? 128 : BN;
     static constexpr int kTmemCols = 2 * kAccCols;
@@ -1070,12 +1070,14 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     for (int e = 0; e < kChunk; e += 32) FP4Q_TMEM_LD_X32(from + acc.slot * C::kAccCols + c + e, (v + e));
                     if (C::kBoth && both) {
                         float *sum = reinterpret_cast<float *>(v);
-                        uint32_t u[kChunk];
 #pragma unroll
-                        for (int e = 0; e < kChunk; e += 32) FP4Q_TMEM_LD_X32(from + acc.slot * C::kAccCols + BN + e, (u + e));
-                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        for (int e = 0; e < kChunk; e += 32) {
+                            uint32_t u[32];
+                            FP4Q_TMEM_LD_X32(from + acc.slot * C::kAccCols + BN + e, u);
+                            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-                        for (int e = 0; e < kChunk; e++) sum[e] += __uint_as_float(u[e]);
+                            for (int i = 0; i < 32; i++) sum[e + i] += __uint_as_float(u[i]);
+                        }
                         release();
                         // The lower halves, of warps 6 and 7, are added to the upper ones, of warps 4 and 5, by way of their boxes.
                         const uint32_t half_box = smem_u32(smem_boxes) + (quarter | 2) * kStaging + lane * 256;

@@ -219,9 +219,10 @@ struct Scratch {
         const int64_t stages = (split ? 2 : 1) * ceil_div(rows < cols ? cols : rows, kBox16);
         const GramPlan one(count, side, stages, 128), two(count, side, stages, 256);
         const bool pairs = two.us < one.us;
-        // 64 x 64 tiles, a quarter of a microsecond a box, where all of them run at once and no parts are faster: they are all computed, and not
-        // cut (256 x 256 10 -> 7 us, 85 of 2382 x 45 41 -> 31).
-        const bool small = count * ceil_div(side, 64) * ceil_div(side, 64) <= 148 && 0.26 * (double)stages + 1.0 < std::min(one.us, two.us);
+        // 64 x 64 tiles, 0.17 us a stage, where all of them run at once and no parts are faster (which take about 3 us more than estimated): they are
+        // all computed, and not cut.  All five steps, in larger tiles and in these: 256 x 256 129 and 104 us, 300 x 1500 167 and 143, 85 of 2382 x 45
+        // 370 and 311; 200 x 5000 182 and 232.
+        const bool small = count * ceil_div(side, 64) * ceil_div(side, 64) <= 148 && 0.17 * (double)stages < std::min(one.us, two.us) + 2.0;
         edge = small ? 64 : pairs ? 256 : 128;
         tiles = pairs ? two.tiles : one.tiles;
         const int64_t parts = edge == 64 ? 1 : pairs ? two.parts : one.parts;
