@@ -75,12 +75,14 @@ fp4q_status launch_store16(const Operand16 &a, const Operand16 &b, Gemm16Params 
 }
 
 // What a product of rows in tiles of rows x cols takes, in us, where `groups` groups may have rows and each fills its last tile by half: rounds of tiles
-// over the GPU's slots, per tile 2 us and its boxes, of which an SM gets 115 GB/s from L2 and all of them together 11 TB/s.
-double rows_cost(int64_t T, int64_t groups, int64_t n, int64_t k, int rows, int cols, int slots, double box_bytes, int ctas)
+// over the GPU's slots, per tile `each` us beside its boxes, of which an SM gets 115 GB/s from L2 and all of them together 15 TB/s.  (Where the rule decides,
+// the variant it takes and the next: 64 rows in one group, 4096 x 4096, 32 x 64 tiles 13.6 us and pairs 24.2; 600 in 4, 2048 x 1024, 128 x 128 tiles 9.5
+// and pairs 11.9; 1531 in 8, 1003 x 2731, 17.2 and 20.6; 1999 in 13 pairs 22.0 and 30.6; 3000 in 100, 2048 x 768, 32 x 64 60.5 and 69.)
+double rows_cost(int64_t T, int64_t groups, int64_t n, int64_t k, int rows, int cols, int slots, double box_bytes, int ctas, double each)
 {
-    const double row_tiles = std::max<double>((double)groups, (double)T / rows + 0.5 * groups), tiles = row_tiles * ceil_div(n, cols);
-    const double rate = std::min(115e3, 11e6 / (ctas * std::min<double>(tiles, slots)));   // bytes a us
-    return std::ceil(tiles / slots) * (2.0 + (double)ceil_div(k, 64) * box_bytes / rate);
+    const double row_tiles = groups == 1 ? (double)ceil_div(T, rows) : std::max<double>((double)groups, (double)T / rows + 0.5 * groups), tiles = row_tiles * ceil_div(n, cols);
+    const double rate = std::min(115e3, 15e6 / (ctas * std::min<double>(tiles, slots)));   // bytes a us
+    return std::ceil(tiles / slots) * (each + (double)ceil_div(k, 64) * box_bytes / rate);
 }
 
 // Rows of groups, T in all.  Pairs for groups of many rows, tiles of 32 rows for groups of few, 128 x 128 between them.
@@ -89,8 +91,8 @@ fp4q_status rows_product(const Operand16 &a, const Operand16 &b, Gemm16Params &p
 {
     const int64_t few = T < groups ? T : groups;   // groups that have rows, at most
     const int box = T <= 16 * few ? 16 : 32;
-    const double pairs = rows_cost(T, few, p.n, p.k, 256, 256, 74, 32768.0, 2), singles = rows_cost(T, few, p.n, p.k, 128, 128, 148, 32768.0, 1),
-                 small = rows_cost(T, few, p.n, p.k, 32, 64, 148, 8192.0 + 128.0 * box, 1);
+    const double pairs = rows_cost(T, few, p.n, p.k, 256, 256, 74, 32768.0, 2, 3.6), singles = rows_cost(T, few, p.n, p.k, 128, 128, 148, 32768.0, 1, 3.0),
+                 small = rows_cost(T, few, p.n, p.k, 32, 64, 148, 8192.0 + 128.0 * box, 1, 0.6);
     const double least = std::min(pairs, std::min(singles, small));
     p.a_box = 128;
     if (least == pairs) {
