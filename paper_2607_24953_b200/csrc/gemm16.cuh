@@ -613,9 +613,11 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         if (TILES == TILES_CUT && order) {
             for (int g = threadIdx.x; g < p.batch; g += kThreads16) {
                 const int len = group_rows(start, g);
-                int place = 0;
+                int place = 0, from = start[0];
+#pragma unroll 8
                 for (int h = 0; h < p.batch; h++) {
-                    const int other = group_rows(start, h);
+                    const int to = start[h + 1], other = to - from;
+                    from = to;
                     place += other > len || (other == len && h < g);
                 }
                 order[place] = (uint16_t)g;
@@ -923,7 +925,8 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             };
             // Several parts are on their way at a time; they are added in their order all the same.
             auto add_parts = [&](float *v, int c, int n) {
-                constexpr int kBatch = EPI == EPI16_SUM ? 8 : 32, kWay = 3;   // columns, and parts of them
+                constexpr bool kFull = EPI == EPI16_SUM && kCols > 64;               // the sums take most of the registers
+                constexpr int kBatch = kFull ? 16 : 32, kWay = kFull ? 2 : 3;   // columns, and parts of them
 #pragma unroll
                 for (int e0 = 0; e0 < n; e0 += kBatch) {
                     const float4 *from = reinterpret_cast<const float4 *>(p.partial + place + 32 * (c + e0));

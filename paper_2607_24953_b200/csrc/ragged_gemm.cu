@@ -157,20 +157,37 @@ extern "C" fp4q_status fp4q_ragged_gemm_dgrad(const void *dY, int64_t T, int64_t
 
 namespace {
 
-// How a weight gradient is computed: pairs or single CTAs, and the parts that long contractions are cut into: a group of most of the rows has few tiles,
-// which would otherwise leave most of the GPU idle (one group, 131072 rows, 768 x 2048).  A part is half of what a CTA or pair would have to do if all
-// had the same, and no less than 16 stages (below that joining costs what it saves).
+// How a weight gradient is computed: in pairs' tiles or single CTAs', and the parts that long contractions are cut into: a group of most of the rows
+// has few tiles, which would otherwise leave most of the GPU idle.  Estimated for groups of the same length: rounds of tiles or of their parts, a box
+// 0.38 us in a pair and 0.285 in a single CTA (0.32 with all of them at work), 3.3 and 1.7 us a tile, and where there are parts 3 us and 1.4 or 0.7 us
+// for each, which whoever comes last reads.  Groups longer than the others are cut at half of what a CTA or pair would have to do if all had the same.
+// (131072 rows in 4 groups, 256 x 256: 9 parts in single CTAs 39 us, 32 parts in pairs 198; 131072 in one, 768 x 2048: 3 parts in pairs 300, 14 of them
+// 411, single CTAs 544; 8192 in 2, 2048 x 2048: uncut in pairs 55, in parts of 56 stages 111, single CTAs 82.)
 struct CutPlan {
-    bool pairs;
+    bool pairs = false;
     int64_t m_tiles, n_tiles, part_stages, places, counter_bytes;
     size_t bytes = 0;   // 0: no parts
     CutPlan(int64_t T, int64_t N, int64_t K, int64_t groups, bool parts)
     {
-        pairs = N > 128 && K > 128 && (parts || groups * ceil_div(N, 256) * ceil_div(K, 256) >= 74);
+        const int64_t stages = ceil_div(T, kBox16);
+        const double mean = std::max(1.0, (double)stages / groups + (groups > 1 ? 0.5 : 0.0));   // stages of a group
+        double least = 1e30;
+        for (int two = 0; two < (N > 128 && K > 128 ? 2 : 1); two++) {
+            const int64_t edge = two ? 256 : 128, slots = two ? 74 : 148, tiles = groups * ceil_div(N, edge) * ceil_div(K, edge);
+            const int64_t most = parts ? std::min<int64_t>(64, std::max<int64_t>(1, (int64_t)mean / 16)) : 1;
+            for (int64_t n = 1; n <= most; n++) {
+                const double box = two ? 0.38 : tiles * n >= slots ? 0.32 : 0.285;
+                const double us = (double)ceil_div(tiles * n, slots) * (std::ceil(mean / n) * box + (two ? 3.3 : 1.7)) + (n > 1 ? 3.0 + (two ? 1.4 : 0.7) * (double)n : 0.0);
+                if (us >= least) continue;
+                least = us;
+                pairs = two != 0;
+                const double half = (double)tiles * mean / (2.0 * slots);
+                part_stages = round_up(std::max<int64_t>(16, (int64_t)std::ceil(n > 1 ? mean / n : std::max(half, 1.25 * mean))), 8);
+            }
+        }
         m_tiles = ceil_div(N, pairs ? 256 : 128);
         n_tiles = ceil_div(K, pairs ? 256 : 128);
-        const int64_t slots = pairs ? 74 : 148, each = m_tiles * n_tiles, stages = ceil_div(T, kBox16);
-        part_stages = std::max<int64_t>(16, round_up(ceil_div(each * (stages + groups / 2), 2 * slots), 8));
+        const int64_t each = m_tiles * n_tiles;
         if (!parts || stages <= part_stages) return;
         // Groups with more stages than a part: no more than this, and with so many parts.
         const int64_t longer = std::min(groups, stages / part_stages + 1);
@@ -220,7 +237,6 @@ extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t
     p.offsets = g ? g->row_offsets : nullptr;
     p.total_rows = T;
     p.accumulate = accumulate != 0;
-    p.deals = groups > 1 && T >= 256 * groups;   // shorter groups: 300 rows in 64 groups 23.5 us in turn, 35.0 dealt
     p.status = static_cast<uint32_t *>(ws);
     if (plan.bytes) {
         p.part_stages = (int32_t)plan.part_stages;
@@ -230,6 +246,8 @@ extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t
     }
     const Operand16 a = T ? operand16(d, T, 1) : Operand16{dW, 8, 1, 1, 8, 8}, b = T ? operand16(m, T, 1) : a;
     const int64_t most = groups * plan.m_tiles * plan.n_tiles + (plan.bytes ? plan.places : 0);
+    // Not where every tile has a CTA or pair to itself, nor for shorter groups: 300 rows in 64 groups 23.5 us in turn, 35.0 dealt.
+    p.deals = groups > 1 && T >= 256 * groups && most > (plan.pairs ? 74 : 148);
     if (T < 256 * groups)   // short contractions
         return plan.pairs ? launch_store16<2, 256, true, true, TILES_CUT, true>(a, b, p, dt, most, s) : launch_store16<1, 128, true, true, TILES_CUT, true>(a, b, p, dt, most, s);
     return plan.pairs ? launch_store16<2, 256, true, true, TILES_CUT>(a, b, p, dt, most, s) : launch_store16<1, 128, true, true, TILES_CUT>(a, b, p, dt, most, s);
