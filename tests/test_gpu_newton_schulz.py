@@ -158,6 +158,26 @@ def test_captured_and_on_another_stream():
     assert torch.equal(m1, m2) and torch.equal(m1, m3) and b.fp4q_workspace_status(ws) == 0
 
 
+@pytest.mark.parametrize("count,rows,cols", [(1, 100, 200), (1, 500, 700), (3, 1000, 300), (1, 2100, 2300)])
+def test_a_wait_that_runs_out_is_reported(count, rows, cols):
+    g, ws = randn(1, count, rows, cols), b.alloc_workspace("cuda")
+    want = b.fp4q_newton_schulz(g, ws=ws)
+    b.fp4q_workspace_set_wait_limit(ws, 2000)
+    b.fp4q_debug_withhold_load(ws, 1)
+    b.fp4q_newton_schulz(g, ws=ws)
+    assert b.fp4q_workspace_status(ws) == 7
+    b.fp4q_debug_withhold_load(ws, 0)
+    b.fp4q_workspace_set_wait_limit(ws, 0)
+    assert torch.equal(b.fp4q_newton_schulz(g, ws=ws), want) and b.fp4q_workspace_status(ws) == 0
+
+
+@pytest.mark.parametrize("count,side,other", [(1, 384, 384), (1, 385, 385), (1, 60, 3000), (2, 200, 5000), (5, 380, 1500), (1, 768, 768), (3, 640, 2000), (2, 1100, 1100)])
+def test_tiles_of_every_edge_wide_and_tall(count, side, other):
+    g = randn(1, count, side, other)
+    close(b.fp4q_newton_schulz(g), exact(g))
+    close(b.fp4q_newton_schulz(g.transpose(1, 2).contiguous()), exact(g.transpose(1, 2).contiguous()))
+
+
 def test_a_training_step_of_an_expert_layer():
     # ragged products forward and backward, the update, the new master weights into FP4 and through the framework's own product
     E, n, k, T = 4, 256, 128, 700

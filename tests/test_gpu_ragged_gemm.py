@@ -159,6 +159,31 @@ def test_long_contractions_in_parts(T, n, k, values):
     assert err.value.status == 5
 
 
+@pytest.mark.parametrize("T,n,k,values", [(16000, 1024, 1000, [0, 16000]), (20000, 600, 1500, [0, 300, 20000]), (40000, 520, 264, [0, 9000, 9000, 21000, 40000])])
+def test_parts_of_larger_tiles_and_of_few_groups(T, n, k, values):
+    dy, x = operands("wgrad", T, n, k, len(values) - 1)
+    y, s = reference("wgrad", dy, x, groups(values, T))
+    length = max(j - i for i, j in groups(values, T))
+    scratch = b.alloc_ragged_wgrad_scratch(T, n, k, len(values) - 1, "cuda")
+    assert scratch.numel() > 0
+    for dt in (b.OUT_F32, b.OUT_BF16):
+        scratch.fill_(255)
+        want = call("wgrad", dy, x, offsets(values), dt=dt, scratch=scratch)
+        assert ((want.double() - y).abs() <= bound(y, s, length, dt)).all()
+        assert torch.equal(call("wgrad", dy, x, offsets(values), dt=dt, scratch=scratch), want)
+
+
+@pytest.mark.parametrize("T,values", [(64, [0, 64]), (600, [0, 150, 300, 450, 600]), (200, [0] + [2 * i for i in range(1, 101)])])
+def test_every_shape_of_tile(T, values):
+    # few rows of one group, some of a few, two each of a hundred
+    for op in ("fwd", "dgrad"):
+        x, w = operands(op, T, 1000, 520, len(values) - 1)
+        y, s = reference(op, x, w, groups(values, T))
+        for dt in (b.OUT_BF16, b.OUT_F32):
+            got = call(op, x, w, offsets(values), dt=dt)
+            assert ((got.double() - y).abs() <= bound(y, s, 520 if op == "fwd" else 1000, dt)).all()
+
+
 def test_no_groups_at_all_and_one_for_everything():
     a, w = operands("fwd", 300, 96, 200, 1)
     assert torch.equal(call("fwd", a, w, None), call("fwd", a, w, offsets([0, 300])))
