@@ -79,9 +79,24 @@ struct Cfg16 {
     static_assert((BN == 64 && !STACK) || 1024 + kOperands + 8 * 8192 + kTail <= 227 * 1024, "shared memory budget: stacks");
 };
 
+// Division by a number that the host knows, of numbers below 2^31: with s = ceil(log2 d), n / d = n m >> (31 + s) for m = ceil(2^(31 + s) / d), since m d
+// exceeds 2^(31 + s) by less than 2^s.
+struct Divisor16 {
+    uint32_t mul, shift;   // mul = 0: by one
+    __host__ static Divisor16 of(int64_t d)
+    {
+        if (d <= 1) return Divisor16{0u, 0u};
+        uint32_t s = 1;
+        while ((1ll << s) < d) s++;
+        return Divisor16{(uint32_t)(((1ull << (31 + s)) + (uint64_t)d - 1) / (uint64_t)d), s - 1};
+    }
+    __device__ __forceinline__ int operator()(int n) const { return mul == 0u ? n : (int)(__umulhi((uint32_t)n, mul) >> shift); }
+};
+
 struct Gemm16Params {
     int32_t m, n, k;                 // output rows and columns and contraction length of one product (TILES_ROWS: m = all rows, TILES_CUT: k = all rows)
     int32_t m_tiles, n_tiles;        // TILES_ROWS: m_tiles is found on the device
+    Divisor16 by_matrix, by_band;    // tiles of a matrix or group (but TILES_ROWS), and of kRaster16 rows of tiles: set by launch_gemm16
     int32_t batch;                   // groups or matrices
     int32_t bf16;                    // operand type: 0 = FP16, 1 = BF16
     int32_t deals;                   // TILES_CUT: tiles go to whoever is free instead of in turn
@@ -166,7 +181,8 @@ __device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_bar
 }
 
 // By the lanes for which `issue` holds.  The whole warp comes here, without a branch: what an instruction takes from uniform registers stays in them
-// (a lane that branches off moves six words there for every MMA).  Descriptors: their lower words, which hold the address, and the upper one.
+// (a lane that branches off moves six words there for every MMA: 75 cycles each, now 37; and 8 rows in 8 groups
+// of 768 x 2048 11.5 us, now 9.8, 11008 x 4096 updates 3160 and 3060).  Descriptors: their lower words, which hold the address, and the upper one.
 template <int CTAS>
 __device__ __forceinline__ void tcgen05_mma_f16(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool accumulate, bool issue)
 {
@@ -266,15 +282,16 @@ struct Ring16 {
 // touched and none belongs to two groups.  first[g]: row tiles before group g (TILES_ROWS).
 __device__ __forceinline__ int32_t group_rows(const int32_t *start, int g) { return start[g + 1] - start[g]; }
 
-__device__ __forceinline__ int find_group16(const int32_t *first, int n, int tile)   // the last g with first[g] <= tile; first[0] = 0
+// The last g with first[g] <= tile, of n which do not fall, first[0] = 0: the whole warp looks, at one of every n / 32 and then at those between.  (With a search
+// by halves and divisions by variables a tile was decoded in 1200 cycles, now in 600; all steps of an update 256 x 256 103 -> 100 us, 30 of 64 x 64 84 -> 82.)
+__device__ __forceinline__ int find_group16(const int32_t *first, int n, int tile)
 {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (first[mid] <= tile) lo = mid;
-        else hi = mid;
-    }
-    return lo;
+    const int lane = threadIdx.x & 31, run = (n + 31) / 32;
+    const int at = (__popc(__ballot_sync(0xFFFFFFFFu, lane * run < n && first[lane * run] <= tile)) - 1) * run;
+    if (run == 1) return at;
+    int found = 0;
+    for (int i = lane; i - lane < run; i += 32) found += __popc(__ballot_sync(0xFFFFFFFFu, i < run && at + i < n && first[at + i] <= tile));
+    return at + found - 1;
 }
 
 // Parts that a contraction of `stages` stages is cut into.
@@ -301,7 +318,7 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
         part = tile - t.counter * t.parts;
         t.slot0 = tile - part;
         const int per = m_tiles * (m_tiles + 1) / 2;
-        t.batch = t.counter / per;
+        t.batch = p.by_matrix(t.counter);
         const int r = t.counter - t.batch * per;
         mt = (int)((sqrtf(8.0f * (float)r + 1.0f) - 1.0f) * 0.5f);
         while (mt * (mt + 1) / 2 > r) mt--;
@@ -311,7 +328,7 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
     } else {
         int r = tile;
         if (TILES == TILES_CUT) {
-            const int per = m_tiles * p.n_tiles, at = p.partial ? find_group16(first, p.batch, tile) : tile / per;
+            const int per = m_tiles * p.n_tiles, at = p.partial ? find_group16(first, p.batch, tile) : p.by_matrix(tile);
             t.batch = order ? order[at] : at;
             t.k0 = start[t.batch];
             t.k_len = group_rows(start, t.batch);
@@ -327,11 +344,11 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
         }
         if (TILES == TILES_BATCH) {
             const int per = m_tiles * p.n_tiles;
-            t.batch = tile / per;
+            t.batch = p.by_matrix(tile);
             r = tile - t.batch * per;
         }
-        const int per_group = kRaster16 * p.n_tiles, g = r / per_group, m0 = g * kRaster16, h = min(kRaster16, m_tiles - m0), rem = r - g * per_group;
-        nt = rem / h;
+        const int per_group = kRaster16 * p.n_tiles, g = p.by_band(r), m0 = g * kRaster16, h = min(kRaster16, m_tiles - m0), rem = r - g * per_group;
+        nt = h == kRaster16 ? rem / kRaster16 : rem / h;
         mt = m0 + rem - nt * h;
     }
     t.col = nt * BN;
@@ -356,7 +373,8 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
     return t;
 }
 // Operands in two numbers take two stages for a piece of the contraction, upper and lower parts: whether a stage is the second, and how much of
-// the contraction (of k_len) is left where it starts.  Three loads of each, one for every product, took a third longer (256 x 256 113 us).
+// the contraction (of k_len) is left where it starts.  (With three loads of each, one for every product, the
+// updates of 14 of 7397 x 193 took 632 us instead of 563.)
 template <bool SPLITS>
 __device__ __forceinline__ bool lower16(const Gemm16Params &p, int s) { return SPLITS && (s & p.split) != 0; }   // not in 64 x 64 tiles
 template <bool SPLITS, int K, bool BOTH>
@@ -674,7 +692,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
 
     if (warp == 0 || warp == 3) {
         // ------------------------------------------------------------------ TMA producers: warp 0 loads A and announces the bytes, warp 3 loads B
-        // One thread that issues up to four copies a stage needs 0.55 us for it, longer than the stage's MMAs take.  (What comes out of memory
+        // One thread that issued up to four copies a stage needed 0.55 us for it, longer than the stage's MMAs take.  (What comes out of memory
         // fetched into L2 some stages ahead by the same threads was 2 to 25 % slower: the copies' unit takes 65 bytes a cycle, a stage's 32 KB in
         // as long as its MMAs take, and the fetches pass through it too.)
         const bool a_side = warp == 0;
@@ -1275,9 +1293,11 @@ inline bool make_map16(CUtensorMap *map, const Operand16 &o, int box_cols, int b
 // maps: what lies beside the operands is the caller's.  a2, b2: the operands' lower parts (p.split).  most_tiles: no fewer than the tiles
 // there can be.
 template <int CTAS, int BN, bool A_MN, bool B_MN, int EPI, int TILES, bool TWO = false>
-fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand16 &a2, const Operand16 &b2, Maps16 &maps, const Gemm16Params &p, int64_t most_tiles,
+fp4q_status launch_gemm16(const Operand16 &a, const Operand16 &b, const Operand16 &a2, const Operand16 &b2, Maps16 &maps, Gemm16Params p, int64_t most_tiles,
                           cudaStream_t stream)
 {
+    p.by_matrix = Divisor16::of(TILES == TILES_SYM ? (int64_t)p.m_tiles * (p.m_tiles + 1) / 2 : (int64_t)p.m_tiles * p.n_tiles);
+    p.by_band = Divisor16::of((int64_t)kRaster16 * p.n_tiles);
     using C = Cfg16<CTAS, BN, TWO, (TILES >= TILES_BATCH)>;
     const int a_rows = A_MN ? kBox16 : p.a_box, b_rows = B_MN ? kBox16 : C::kBRows;
     if (!make_map16(&maps.a, a, kBox16, a_rows) || !make_map16(&maps.b, b, kBox16, b_rows)) return FP4Q_ERR_CUDA;
