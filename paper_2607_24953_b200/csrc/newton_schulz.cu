@@ -177,19 +177,25 @@ __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumPara
     }
 }
 
-// A's product in tiles of `edge` (128, or 256 for pairs), its contraction of `stages` boxes cut into parts: the number of parts with the least
-// estimated time.  A round of the CTAs' or pairs' tiles takes its boxes, which get 115 GB/s an SM and 11 TB/s in all from L2, and 2 or 4 us; parts take
+// Rounds of tiles of 128 x 128 in single CTAs or 256 x 256 in pairs, in us: a round takes its boxes, which get 115 GB/s an SM and 15 TB/s in all from L2, and
+// 2 or 4 us.
+double rounds_us(int64_t tiles, int64_t stages, int64_t edge)
+{
+    const int64_t slots = edge == 256 ? 74 : 148, sms = edge == 256 ? 2 : 1;
+    const double box = std::max(32768.0 / 115e3, 32768.0 * (double)(sms * std::min(tiles, slots)) / 15e6);
+    return (double)ceil_div(tiles, slots) * ((double)stages * box + 2.0 * sms);
+}
+// A's product in tiles of `edge`, its contraction of `stages` boxes cut into parts: the number of parts with the least estimated time.  Parts take
 // their way through memory, where whoever comes last reads them one after the other.  (Parts for 4751 x 63: 70 -> 20 us.)
 struct GramPlan {
     int64_t tiles, parts = 1;
     double us = 1e30;
     GramPlan(int64_t count, int64_t side, int64_t stages, int64_t edge)
     {
-        const int64_t across = ceil_div(side, edge), slots = edge == 256 ? 74 : 148, sms = edge == 256 ? 2 : 1;
+        const int64_t across = ceil_div(side, edge), slots = edge == 256 ? 74 : 148;
         tiles = count * across * (across + 1) / 2;
         for (int64_t n = 1; n == 1 || (n <= 32 && stages / n >= 16 && tiles * n <= 4 * slots); n++) {
-            const double box = std::max(32768.0 / 115e3, 32768.0 * (double)(sms * std::min(tiles * n, slots)) / 11e6);
-            const double t = (double)ceil_div(tiles * n, slots) * ((double)ceil_div(stages, n) * box + 2.0 * sms) + (n > 1 ? 3.0 + 0.6 * (double)n : 0.0);
+            const double t = rounds_us(tiles * n, ceil_div(stages, n), edge) + (n > 1 ? 3.0 + 0.6 * (double)n : 0.0);
             if (t < us) { us = t; parts = n; }
         }
     }
@@ -376,11 +382,16 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     p.split = at.split;
     p.admit = 1;
     const Parts part_a(half_at(at.a[0]), half_at(at.a[1]), side, side, count, at.pitch_a), part_p(half_at(at.poly[0]), half_at(at.poly[1]), side, side, count, at.pitch_a);
-    // P and X': the smallest tiles of which one round does, each with less to load and a shorter epilogue; else pairs.
-    auto edge_of = [&](int64_t small, int64_t tiles64, int64_t tiles128) { return small * tiles64 <= 148 ? 64 : small * tiles128 <= 148 ? 128 : 256; };
-    const int64_t s64 = ceil_div(side, 64), s128 = ceil_div(side, 128);
-    const int edge_poly = edge_of(count, s64 * s64, s128 * (s128 + 1) / 2),
-              edge_update = edge_of(count, ceil_div(rows, 64) * ceil_div(cols, 64), ceil_div(rows, 128) * ceil_div(cols, 128));
+    // P and X': 64 x 64 tiles where one round of them does, each with less to load and a shorter epilogue; else what is estimated to be faster
+    // (all steps with pairs for all that takes several rounds, and so: 200 of 128 x 128 220 and 164 us, 86 of 6358 x 29 618 and 557; 4 of 900 x 1000 197 and
+    // 201).
+    const int64_t s64 = ceil_div(side, 64), s128 = ceil_div(side, 128), s256 = ceil_div(side, 256), stages = (at.split ? 2 : 1) * s64;
+    auto edge_of = [&](int64_t tiles64, int64_t tiles128, int64_t tiles256) {
+        if (count * tiles64 <= 148) return 64;
+        return rounds_us(count * tiles128, stages, 128) <= rounds_us(count * tiles256, stages, 256) ? 128 : 256;
+    };
+    const int edge_poly = edge_of(s64 * s64, s128 * (s128 + 1) / 2, s256 * (s256 + 1) / 2),
+              edge_update = edge_of(ceil_div(rows, 64) * ceil_div(cols, 64), ceil_div(rows, 128) * ceil_div(cols, 128), ceil_div(rows, 256) * ceil_div(cols, 256));
     for (int32_t i = 0; i < steps; i++) {
         const float *c = coefficients + 3 * i;
         const int now = i & 1, next = now ^ 1;
