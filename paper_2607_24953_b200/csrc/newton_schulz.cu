@@ -8,8 +8,9 @@
 //
 // Precision.  The products' operands are FP16: values of X, A and P lie in a narrow range (singular values of at most about 1.3), so the
 // three bits that FP16 has more than BF16 cost nothing.  X itself is kept as a sum of two FP16 numbers (22 bits): A's product takes the upper
-// one, and a times the lower one is added to P's product with the upper one.  P's diagonal is off by up to 2^-11 of itself, which is a factor on
-// a row (2e-4 of the result); the rows' directions are kept.  The term a X carries directions of small singular values from step to step, multiplied by a = 3.4 each time,
+// one, and a times the lower one is added to P's product with the upper one.  P's diagonal, which has a in it, is rounded once, by up to 2^-11 of itself,
+// and carries what A's rounding makes of b A + c A A.  Where a matrix's singular values are all alike A and P are little but their diagonals, and these
+// errors do not average out.  The term a X carries directions of small singular values from step to step, multiplied by a = 3.4 each time,
 // and rounding X as a whole puts noise into those that a gradient does not have (rank 100, 768 x 2048: the update is off by 1.8e-2 with one
 // FP16 number and 1.4e-1 with a BF16 one, 7e-4 with the sum of two).  Matrices of a short side have few elements over which the roundings of
 // A, P and the products' X average out (0.8e-3 of the result at 777 x 1003, 2.0e-3 at 64 x 64, 3e-3 and more below 16) and little work:

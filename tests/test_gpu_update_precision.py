@@ -1,0 +1,49 @@
+"""Where orthogonalised updates are exact, or closer to their definition than one FP16 operand would be."""
+import math
+
+import pytest
+import torch
+
+from paper_2607_24953_b200 import binding as b
+
+pytestmark = pytest.mark.gpu
+
+
+def randn(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator("cuda").manual_seed(seed), device="cuda")
+
+
+def exact(u, coefficients=b.NEWTON_SCHULZ, eps=1e-7):
+    x = u.double()
+    x = x / (x.square().sum((-2, -1), keepdim=True).sqrt() + eps)
+    tall = x.shape[-2] > x.shape[-1]
+    x = x.mT if tall else x
+    for a, c1, c2 in coefficients:
+        q = x @ x.mT
+        x = a * x + (c1 * q + c2 * (q @ q)) @ x
+    return x.mT if tall else x
+
+
+@pytest.mark.parametrize("count,side,other", [(1, 500, 700), (5, 400, 600), (1, 1300, 1400), (12, 800, 900)])
+def test_the_polynomials_diagonal_is_rounded_once(count, side, other):
+    # One row of 256 elements +-1/16 in each matrix: X, A = e e^T and a + b A are exact in FP16 (a = 20 and b = -19.3046875 make 89/128 = 356/512), and so
+    # is the result in BF16; b A alone, 9884/512, is none of FP16's numbers.
+    g = torch.zeros(count, side, other, device="cuda")
+    for i in range(count):
+        at = torch.randperm(other, generator=torch.Generator().manual_seed(i))[:256].cuda()
+        g[i, (77 + 131 * i) % side, at] = torch.sign(randn(i, 256)) * 3.0
+    want = (torch.sign(g) * (89 / 128 / 16)).to(torch.bfloat16)
+    step = ((20.0, -19.3046875, 0.0),)
+    assert torch.equal(b.fp4q_newton_schulz(g, coefficients=step, eps=0.0), want)
+    assert torch.equal(b.fp4q_newton_schulz(g.mT.contiguous(), coefficients=step, eps=0.0), want.mT)
+
+
+@pytest.mark.parametrize("side,other", [(385, 8000), (500, 5000), (640, 640)])
+def test_products_that_are_little_but_their_diagonals(side, other):
+    # Operands in one FP16 number, rounded by 2^-11 / sqrt(3) in the mean square, independently from row to row as the diagonals differ.  Per step 9 times
+    # that for A (at most |b| + 2 |c|) and 3 for P and for X, in quadrature over five steps 6.3e-3 where all of it acts; A's error is one of the diagonal
+    # alone and meets b + 2 c A instead of |b| + 2 |c|, below 5: sqrt(5 (5^2 + 3^2 + 3^2)) 2^-11 / sqrt(3) = 4.1e-3.  The result's rounding: 2^-8 / sqrt(3).
+    g = randn(1, side, other) if side != other else torch.diag(1 + torch.rand(side, generator=torch.Generator("cuda").manual_seed(2), device="cuda"))
+    for u in (g, g.T.contiguous()):
+        want = exact(u)
+        assert (b.fp4q_newton_schulz(u).double() - want).norm() <= math.hypot(4.1e-3, 2 ** -8 / 3 ** 0.5) * want.norm()
