@@ -395,11 +395,10 @@ fp4q_status fp4q_gemm_fwd_static_workspace(const fp4q_tensor *X, const fp4q_tens
  * (dt; FP4Q_OUT_PADDED may be added and changes nothing), 16-byte aligned with rows of whole 16 bytes, and only their columns are
  * written.  accumulate != 0 adds to dW (FP32 only).  FP32 accumulation; an FP32 output is the sum, rounded to nearest, of partial
  * sums over 512 contraction elements each, so that the tensor cores' cut-off towards zero does not add up over a long contraction.
- * A group's result does not depend on the other groups' values.  ws/ws_bytes/stream and the asynchronous FP4Q_ERR_TIMEOUT as for fp4q_gemm_fwd;
- * the weight gradient also counts its tiles in the workspace, so that calls which share one and overlap give wrong results.
+ * A group's result does not depend on the other groups' values.  ws/ws_bytes/stream and the asynchronous FP4Q_ERR_TIMEOUT as for fp4q_gemm_fwd.
  * scratch (weight gradient): fp4q_ragged_gemm_wgrad_scratch_bytes() bytes of device memory (0: none is needed), 256-byte aligned, any contents,
- * in which long contractions that have few tiles are added up from parts, in a fixed order; NULL: they are not cut into parts, which is
- * slower.  Calls that share it must not overlap on the GPU.
+ * in which long contractions that have few tiles are added up from parts, in a fixed order, and what is left to do is counted; NULL: they are
+ * not cut into parts, which is slower.  Calls that share it must not overlap on the GPU.
  */
 size_t fp4q_ragged_gemm_wgrad_scratch_bytes(int64_t T, int64_t N, int64_t K, int32_t n_groups);
 fp4q_status fp4q_ragged_gemm_fwd(const void *x_bf16, int64_t T, int64_t K, int64_t ldx, const void *w_bf16, int64_t w_rows, int64_t ldw,

@@ -20,8 +20,7 @@ struct Workspace {
     uint32_t detail;         // where the kernel gave up (role/stage), for diagnostics
     uint32_t wait_limit;     // polls (of up to about 1 us) after which a bounded wait gives up; 0 = the kernels' default
     uint32_t withhold_load;  // development hook, 0 in production: n > 0 = CTA 0 leaves out its n-th stage load
-    uint32_t dealt, done;    // 16-bit products with a cut contraction: tiles dealt and CTAs or pairs that have finished; 0 between kernels
-    uint32_t pad[58];
+    uint32_t pad[60];
 };
 
 // Short launches overlap their predecessor's end: quantizers of up to kShortGrid CTAs and short products (launch_gemm_impl says

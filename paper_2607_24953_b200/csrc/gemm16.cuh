@@ -99,7 +99,7 @@ struct Gemm16Params {
     Divisor16 by_matrix, by_band;    // tiles of a matrix or group (but TILES_ROWS), and of kRaster16 rows of tiles: set by launch_gemm16
     int32_t batch;                   // groups or matrices
     int32_t bf16;                    // operand type: 0 = FP16, 1 = BF16
-    int32_t deals;                   // TILES_CUT: tiles go to whoever is free instead of in turn
+    uint32_t *deal;                  // TILES_CUT: tiles dealt, 0 when the kernel starts: they go to whoever is free; NULL: in turn
     int32_t a_box;                   // rows of one copy of a K-major A operand: 128, 64 in 64 x 64 tiles, 32 or 16 in tiles of 32 rows
     const int64_t *offsets;          // TILES_ROWS, TILES_CUT: batch + 1 boundaries; NULL: one group of all rows
     int64_t total_rows;              // rows that the boundaries are held to
@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
 
     const uint64_t limit = limit_word != 0u ? limit_word : kWaitLimit;
     int m_tiles = p.m_tiles;
-    const bool deals = TILES == TILES_CUT && p.deals;
+    const bool deals = TILES == TILES_CUT && p.deal;
     if (TILES <= TILES_CUT) {
         // A lane of warp 4 has a run of boundaries, up to eight in registers.  Boundaries that fall are lifted; then the row tiles of all groups
         // before a group's are counted (TILES_ROWS).
@@ -672,7 +672,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     const int tiles = TILES == TILES_ROWS ? m_tiles * p.n_tiles : TILES == TILES_CUT && p.partial ? *shared_tiles : TILES <= TILES_BATCH ? p.batch * m_tiles * p.n_tiles
                       : p.batch * (m_tiles * (m_tiles + 1) / 2) * parts16(p, passes * ((p.k + C::kK - 1) / C::kK));   // or parts of tiles
     const int tile0 = blockIdx.x / CTAS, step = gridDim.x / CTAS;
-    // Cut contractions differ in length: the tiles are dealt to the CTAs or pairs as these fall free (128 groups with loads of 302 to 15157 rows:
+    // Cut contractions differ in length: the tiles may be dealt to the CTAs or pairs as these fall free (128 groups with loads of 302 to 15157 rows:
     // dealt round in turn, the last pair would have 1.4 times the average of stages).  Which CTA has a tile changes nothing in its result.
     Ring16<kDealt16> deal;
     const uint32_t bar_dealt = smem_u32(bars + 44), bar_taken = smem_u32(bars + 48);
@@ -833,7 +833,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
         // both operands (in one, an infinity in the other would make NaN).  Then, and in a pair when the other CTA has done the same, the
         // stage is full.  A slot is filled again only when the MMAs have read it, so its barriers are never a phase ahead.
         uint32_t slot = 0, phases = 0;
-        // The leader's warp 2 deals: a number from the workspace's counter is the next tile, for both CTAs, as far ahead as there are places.
+        // The leader's warp 2 deals: a number from the call's counter is the next tile, for both CTAs, as far ahead as there are places.
         Ring16<kDealt16> dealing;
         int ahead = 0, mine = 0, more = 1, hand[kDealt16];
         auto deal_ahead = [&]() {
@@ -841,7 +841,7 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 if (!warp_wait<CTAS == 2>(bar_taken + 8 * dealing.slot, dealing.phase ^ 1u, abort_flag, p.status, limit * 16, 0xA00u)) return false;
                 int n = 0;
                 if (lane == 0) {
-                    n = (int)min(atomicAdd(p.status + 4, 1u), (uint32_t)tiles);
+                    n = (int)min(atomicAdd(p.deal, 1u), (uint32_t)tiles);
                     dealt[dealing.slot] = n;
                     if (CTAS == 2) {
                         asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(smem_u32(dealt + dealing.slot), 1)), "r"(n) : "memory");
@@ -1255,10 +1255,6 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
     tcgen05_fence_before();
     __syncthreads();
     if (CTAS == 2) { cluster_arrive(); cluster_wait(); }
-    if (deals && threadIdx.x == 0 && rank == 0 && atomicAdd(p.status + 5, 1u) == (uint32_t)step - 1u) {   // nobody deals any more: the counters are as they were
-        p.status[4] = 0u;
-        p.status[5] = 0u;
-    }
     if (warp == 1) {
         tcgen05_fence_after();
         if (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");

@@ -163,18 +163,24 @@ namespace {
 // for each, which whoever comes last reads.  Groups longer than the others are cut at half of what a CTA or pair would have to do if all had the same.
 // (131072 rows in 4 groups, 256 x 256: 9 parts in single CTAs 39 us, 32 parts in pairs 198; 131072 in one, 768 x 2048: 3 parts in pairs 300, 14 of them
 // 411, single CTAs 544; 8192 in 2, 2048 x 2048: uncut in pairs 55, in parts of 56 stages 111, single CTAs 82.)
+//
+// Where there are parts, groups of several lengths are dealt to whoever is free, by a counter, but not where every tile has a CTA or pair to itself
+// (65536 rows in 64 skewed groups, 1024 x 1024: 190 us dealt, 224 in turn; 32768 in 16, 2048 x 1024: 152 and 169).  Without parts a group
+// alone fills the GPU, or all are short, and tiles go in turn (8192 rows in 32, 4096 x 2048: 348 us dealt, 276 in turn; 1024 in 4, 768 x 2048: 14.6 and 12.3).  The counters of a
+// call lie in its own scratch memory, so that calls which share a workspace do not meddle with one another's tiles.
 struct CutPlan {
-    bool pairs = false;
-    int64_t m_tiles, n_tiles, part_stages, places, counter_bytes;
-    size_t bytes = 0;   // 0: no parts
-    CutPlan(int64_t T, int64_t N, int64_t K, int64_t groups, bool parts)
+    static constexpr int64_t kDealBytes = 256;
+    bool pairs = false, cut = false, deals = false;   // without scratch memory neither parts nor dealing
+    int64_t m_tiles, n_tiles, part_stages = 0, places = 0, most_tiles, counter_bytes = 0;   // counters: the tiles dealt, then those of the parts
+    size_t bytes = 0;
+    CutPlan(int64_t T, int64_t N, int64_t K, int64_t groups, bool scratch)
     {
         const int64_t stages = ceil_div(T, kBox16);
         const double mean = std::max(1.0, (double)stages / groups + (groups > 1 ? 0.5 : 0.0));   // stages of a group
         double least = 1e30;
         for (int two = 0; two < (N > 128 && K > 128 ? 2 : 1); two++) {
             const int64_t edge = two ? 256 : 128, slots = two ? 74 : 148, tiles = groups * ceil_div(N, edge) * ceil_div(K, edge);
-            const int64_t most = parts ? std::min<int64_t>(64, std::max<int64_t>(1, (int64_t)mean / 16)) : 1;
+            const int64_t most = scratch ? std::min<int64_t>(64, std::max<int64_t>(1, (int64_t)mean / 16)) : 1;
             for (int64_t n = 1; n <= most; n++) {
                 const double box = two ? 0.38 : tiles * n >= slots ? 0.32 : 0.285;
                 const double us = (double)ceil_div(tiles * n, slots) * (std::ceil(mean / n) * box + (two ? 3.3 : 1.7)) + (n > 1 ? 3.0 + (two ? 1.4 : 0.7) * (double)n : 0.0);
@@ -188,11 +194,15 @@ struct CutPlan {
         m_tiles = ceil_div(N, pairs ? 256 : 128);
         n_tiles = ceil_div(K, pairs ? 256 : 128);
         const int64_t each = m_tiles * n_tiles;
-        if (!parts || stages <= part_stages) return;
+        most_tiles = groups * each;
+        cut = scratch && stages > part_stages;
+        if (!cut) return;
         // Groups with more stages than a part: no more than this, and with so many parts.
         const int64_t longer = std::min(groups, stages / part_stages + 1);
         places = each * (ceil_div(stages + longer, part_stages) + longer);
-        counter_bytes = round_up(places * (pairs ? 2 : 1) * 8 * 4, 256);
+        most_tiles += places;
+        deals = groups > 1 && T >= 256 * groups && most_tiles > (pairs ? 74 : 148);
+        counter_bytes = kDealBytes + round_up(places * (pairs ? 2 : 1) * 8 * 4, 256);
         bytes = (size_t)(counter_bytes + places * (pairs ? Cfg16<2, 256>::kPlaceBytes : Cfg16<1, 128>::kPlaceBytes));
     }
 };
@@ -239,16 +249,15 @@ extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t
     p.accumulate = accumulate != 0;
     p.status = static_cast<uint32_t *>(ws);
     if (plan.bytes) {
+        uint8_t *counters = static_cast<uint8_t *>(scratch);
+        if (plan.deals) p.deal = reinterpret_cast<uint32_t *>(counters);
         p.part_stages = (int32_t)plan.part_stages;
-        p.counters = static_cast<uint32_t *>(scratch);
-        p.partial = reinterpret_cast<float *>(static_cast<uint8_t *>(scratch) + plan.counter_bytes);
+        p.counters = reinterpret_cast<uint32_t *>(counters + CutPlan::kDealBytes);
+        p.partial = reinterpret_cast<float *>(counters + plan.counter_bytes);
         if (fp4q_status st = launched(cudaMemsetAsync(scratch, 0, (size_t)plan.counter_bytes, s))) return st;
     }
     const Operand16 a = T ? operand16(d, T, 1) : Operand16{dW, 8, 1, 1, 8, 8}, b = T ? operand16(m, T, 1) : a;
-    const int64_t most = groups * plan.m_tiles * plan.n_tiles + (plan.bytes ? plan.places : 0);
-    // Not where every tile has a CTA or pair to itself, nor for shorter groups: 300 rows in 64 groups 23.5 us in turn, 35.0 dealt.
-    p.deals = groups > 1 && T >= 256 * groups && most > (plan.pairs ? 74 : 148);
     if (T < 256 * groups)   // short contractions
-        return plan.pairs ? launch_store16<2, 256, true, true, TILES_CUT, true>(a, b, p, dt, most, s) : launch_store16<1, 128, true, true, TILES_CUT, true>(a, b, p, dt, most, s);
-    return plan.pairs ? launch_store16<2, 256, true, true, TILES_CUT>(a, b, p, dt, most, s) : launch_store16<1, 128, true, true, TILES_CUT>(a, b, p, dt, most, s);
+        return plan.pairs ? launch_store16<2, 256, true, true, TILES_CUT, true>(a, b, p, dt, plan.most_tiles, s) : launch_store16<1, 128, true, true, TILES_CUT, true>(a, b, p, dt, plan.most_tiles, s);
+    return plan.pairs ? launch_store16<2, 256, true, true, TILES_CUT>(a, b, p, dt, plan.most_tiles, s) : launch_store16<1, 128, true, true, TILES_CUT>(a, b, p, dt, plan.most_tiles, s);
 }
