@@ -102,11 +102,15 @@ class _RaggedLinearFn(torch.autograd.Function):
         xb, wb, row_offsets = ctx.saved_tensors
         dyb, dx, dw = _rows16(dy), None, None
         if ctx.needs_input_grad[0]:
-            dx = binding.fp4q_ragged_gemm_dgrad(dyb, wb, row_offsets, ws=ctx.ws).to(ctx.x_dtype)
+            dx = binding.fp4q_ragged_gemm_dgrad(dyb, wb, row_offsets, dt=_out16(ctx.x_dtype), ws=ctx.ws).to(ctx.x_dtype)
         if ctx.needs_input_grad[1]:
-            out = binding.OUT_BF16 if ctx.w_dtype == torch.bfloat16 else binding.OUT_F32
-            dw = binding.fp4q_ragged_gemm_wgrad(dyb, xb, row_offsets, dt=out, ws=ctx.ws).to(ctx.w_dtype).reshape(ctx.shape)
+            dw = binding.fp4q_ragged_gemm_wgrad(dyb, xb, row_offsets, dt=_out16(ctx.w_dtype), ws=ctx.ws).to(ctx.w_dtype).reshape(ctx.shape)
         return dx, dw, None, None
+
+
+def _out16(dtype: torch.dtype) -> int:
+    """The type a gradient is computed in: not less than what it belongs to holds."""
+    return binding.OUT_BF16 if dtype == torch.bfloat16 else binding.OUT_F32
 
 
 def _rows16(t: torch.Tensor) -> torch.Tensor:
@@ -121,8 +125,8 @@ def _rows16(t: torch.Tensor) -> torch.Tensor:
 
 def ragged_linear(x: torch.Tensor, weight: torch.Tensor, row_offsets: torch.Tensor, ws=None) -> torch.Tensor:
     """y_t = weight[g] x_t for the rows t of group g, in BF16: the expert layer as it is without FP4, on groups of any size.  x [T, K], weight
-    [E, N, K], row_offsets int64 [E+1], non-decreasing, all on one GPU; rows that no group owns give zeros and get no gradient.  Differentiable
-    once.  A backward pass that is captured into a CUDA graph needs, as with torch's own layers, leaves that no living eager graph holds."""
+    [E, N, K], row_offsets int64 [E+1], non-decreasing, all on one GPU; rows that no group owns give zeros and get no gradient.  Gradients are
+    computed in BF16 for BF16 tensors and in FP32 for others.  Differentiable once.  A backward pass that is captured into a CUDA graph needs, as with torch's own layers, leaves that no living eager graph holds."""
     if x.dim() != 2 or weight.dim() != 3 or x.shape[1] != weight.shape[2]:
         raise ValueError(f"x must be [T, K] and weight [E, N, K], not {list(x.shape)} and {list(weight.shape)}")
     if row_offsets.dim() != 1 or row_offsets.shape[0] != weight.shape[0] + 1:
