@@ -117,7 +117,7 @@ def _rows16(t: torch.Tensor) -> torch.Tensor:
     """t in BF16 and in rows that start on 16 bytes, as the products read them; t itself where it is so."""
     t = t.to(torch.bfloat16)
     rows, cols = t.shape
-    if (cols <= 1 or t.stride(1) == 1) and t.stride(0) % 8 == 0 and t.stride(0) >= cols and t.data_ptr() % 16 == 0:
+    if t.stride(1) == 1 and t.stride(0) % 8 == 0 and t.stride(0) >= cols and t.data_ptr() % 16 == 0:
         return t
     out = torch.empty((rows, (cols + 7) // 8 * 8), dtype=torch.bfloat16, device=t.device)[:, :cols]
     return out.copy_(t)
