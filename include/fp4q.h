@@ -396,7 +396,7 @@ fp4q_status fp4q_gemm_fwd_static_workspace(const fp4q_tensor *X, const fp4q_tens
  * written.  accumulate != 0 adds to dW (FP32 only).  FP32 accumulation; an FP32 output is the sum, rounded to nearest, of partial
  * sums over 512 contraction elements each, so that the tensor cores' cut-off towards zero does not add up over a long contraction.
  * A group's result does not depend on the other groups' values.  ws/ws_bytes/stream and the asynchronous FP4Q_ERR_TIMEOUT as for fp4q_gemm_fwd.
- * scratch (weight gradient): fp4q_ragged_gemm_wgrad_scratch_bytes() bytes of device memory (0: none is needed), 256-byte aligned, any contents,
+ * scratch (weight gradient): fp4q_ragged_gemm_wgrad_scratch_bytes() bytes of device memory (0: none is needed, or the call refuses these sizes), 256-byte aligned, any contents,
  * in which long contractions that have few tiles are added up from parts, in a fixed order, and what is left to do is counted; NULL: they are
  * not cut into parts, which is slower.  Calls that share it must not overlap on the GPU.
  */

@@ -207,12 +207,19 @@ struct CutPlan {
     }
 };
 
+// Tiles, and parts of them, are counted in 32 bits.
+bool tiles_fit(int64_t T, int64_t N, int64_t K, int64_t groups)
+{
+    const int64_t each = ceil_div(N, 128) * ceil_div(K, 128);
+    return groups * each <= kMaxDim16 / 2 && each * ceil_div(T, 1024) <= kMaxDim16 / 4;
+}
+
 }  // namespace
 
 extern "C" size_t fp4q_ragged_gemm_wgrad_scratch_bytes(int64_t T, int64_t N, int64_t K, int32_t n_groups)
 {
     if (T <= 0 || N <= 0 || K <= 0 || n_groups <= 0 || n_groups > kMaxGroups16 || T > kMaxDim16 || N > kMaxDim16 || K > kMaxDim16) return 0;
-    return CutPlan(T, N, K, n_groups, true).bytes;
+    return tiles_fit(T, N, K, n_groups) ? CutPlan(T, N, K, n_groups, true).bytes : 0;
 }
 
 extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t N, int64_t ld_dy, const void *x, int64_t K, int64_t ldx, void *dW, int64_t ldw,
@@ -231,7 +238,7 @@ extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t
     if (fp4q_status s = check_operand16(d)) return s;
     if (fp4q_status s = check_operand16(m)) return s;
     if (fp4q_status s = check_workspace(ws, ws_bytes)) return s;
-    if (groups * ceil_div(N, 128) * ceil_div(K, 128) > kMaxDim16 / 2 || ceil_div(N, 128) * ceil_div(K, 128) * ceil_div(T, 1024) > kMaxDim16 / 4) return FP4Q_ERR_UNSUPPORTED;
+    if (!tiles_fit(T, N, K, groups)) return FP4Q_ERR_UNSUPPORTED;
     const CutPlan plan(T, N, K, groups, scratch != nullptr);
     if (scratch && scratch_bytes < plan.bytes) return FP4Q_ERR_WORKSPACE;
     if (scratch && !aligned(scratch, 256)) return FP4Q_ERR_ALIGN;
