@@ -592,13 +592,18 @@ const at::Tensor &as_stack(const at::Tensor &t, const char *name)
 {
     if (!t.is_cuda()) { PyErr_Format(PyExc_ValueError, "%s must live on a CUDA device (there is no CPU path)", name); throw PyError(); }
     const bool dims = t.dim() == 2 || t.dim() == 3;
-    if (!dims || (t.numel() && ((t.size(-1) > 1 && t.stride(-1) != 1) || (t.dim() == 3 && t.size(0) > 1 && t.stride(0) != t.size(1) * t.stride(1))))) {
+    if (!dims || (t.numel() && ((t.size(-1) > 1 && t.stride(-1) != 1) || (t.dim() == 3 && t.size(0) > 1 && t.size(1) > 1 && t.stride(0) != t.size(1) * t.stride(1))))) {
         PyErr_Format(PyExc_ValueError, "%s must be a matrix or a stack of matrices [count, rows, cols] with contiguous rows, one matrix behind the other", name);
         throw PyError();
     }
     return t;
 }
-int64_t stack_pitch(const at::Tensor &t) { return t.numel() && t.size(-2) * (t.dim() == 3 ? t.size(0) : 1) > 1 ? t.stride(-2) : t.size(-1); }
+// From row to row, which in a stack of single rows is from matrix to matrix.
+int64_t stack_pitch(const at::Tensor &t)
+{
+    if (t.numel() && t.size(-2) > 1) return t.stride(-2);
+    return t.numel() && t.dim() == 3 && t.size(0) > 1 ? t.stride(0) : t.size(-1);
+}
 
 // g, momentum | None, beta, nesterov, coefficients (a flat sequence of floats), eps, scale, out | None, scratch | None, ws | None, stream
 PyObject *newton_schulz(Args a, Py_ssize_t n)

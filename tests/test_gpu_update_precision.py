@@ -47,3 +47,22 @@ def test_products_that_are_little_but_their_diagonals(side, other):
     for u in (g, g.T.contiguous()):
         want = exact(u)
         assert (b.fp4q_newton_schulz(u).double() - want).norm() <= math.hypot(4.1e-3, 2 ** -8 / 3 ** 0.5) * want.norm()
+
+
+@pytest.mark.parametrize("count,cols", [(4, 50), (3, 700)])
+def test_stacks_of_single_rows_in_any_pitch(count, cols):
+    # As first rows of larger matrices, or as a padded matrix's rows: one step of (1.5, -0.5, 0) leaves a row of length 1 as it is.
+    big, m, out = randn(1, count, 6, cols + 14), torch.zeros(count, 5, cols, device="cuda"), torch.zeros(count, 3, cols + 3, dtype=torch.bfloat16, device="cuda")
+    step = ((1.5, -0.5, 0.0),)
+    rows = big[:, 0, :cols]
+    want = b.fp4q_newton_schulz(rows.contiguous().view(count, 1, cols), coefficients=step)
+    assert torch.equal(b.fp4q_newton_schulz(big[:, :1, :cols], coefficients=step), want)
+    assert torch.equal(b.fp4q_newton_schulz(rows.unsqueeze(1), coefficients=step), want)
+    o = out[:, 1:2, :cols]
+    assert b.fp4q_newton_schulz(big[:, :1, :cols], momentum=m[:, 2:3], coefficients=step, out=o) is o
+    # 2^-8 of the value for BF16, and 2^-20 for sums and products in 22 bits
+    assert ((o.double() - rows.double()[:, None] / rows.double().norm(dim=1)[:, None, None]).abs() <= (2 ** -8 + 2 ** -20) * o.double().abs() + 1e-7).all()
+    assert torch.equal(m[:, 2], rows) and not m[:, :2].any() and not m[:, 3:].any()
+    assert not out[:, 0].any() and not out[:, 2].any() and not out[:, :, cols:].any()
+    with pytest.raises(b.Fp4qError):
+        b.fp4q_newton_schulz(big[:1, :1, :cols].expand(count, 1, cols), momentum=m[:1, :1].expand(count, 1, cols))       # rows that lie in one another
