@@ -1145,7 +1145,6 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                 }
                 // The new values, upper and lower parts, replace those that were read, a piece of eight columns at a time.
                 const bool out = EPI == EPI16_UPDATE && p.o;
-                const uint32_t diagonal = (uint32_t)(row0 + lane - col);   // this row's element on the diagonal, if it is one of the box's 64
                 if (!reads) boxes_free(lane);
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
@@ -1159,10 +1158,6 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                         w[2 * j] = EPI == EPI16_GRAM ? v0 * p.fa : fmaf(p.fb, y.x + z.x, p.fc * v0);
                         w[2 * j + 1] = EPI == EPI16_GRAM ? v1 * p.fa : fmaf(p.fb, y.y + z.y, p.fc * v1);
                     }
-                    if (EPI == EPI16_POLY && (diagonal >> 3) == (uint32_t)i) {   // a I, before the only rounding: b A + c A A may nearly cancel it
-#pragma unroll
-                        for (int e = 0; e < 8; e++) w[e] += (diagonal & 7u) == (uint32_t)e ? p.fa : 0.f;
-                    }
                     uint32_t h[4], l[4];
                     if (out) {
 #pragma unroll
@@ -1174,9 +1169,24 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                             const float2 y = unpack_half(h[j]);
                             l[j] = pack_half(w[2 * j] - y.x, w[2 * j + 1] - y.y);
                         }
-                        if (two) st_shared_16(lo.piece(i), l[0], l[1], l[2], l[3]);
+                        if (two || EPI == EPI16_POLY) st_shared_16(lo.piece(i), l[0], l[1], l[2], l[3]);
                     }
                     st_shared_16(up.piece(i), h[0], h[1], h[2], h[3]);
+                }
+                if (EPI == EPI16_POLY) {   // a I: this row's element in the box, if it has one
+                    // From both parts, whether the lower one leaves or not: b A + c A A may nearly cancel a, which would magnify its rounding.  (Added to the FP32
+                    // values instead, the code of 64 columns, fetched anew by every kernel, cost 0.8 us a step.)
+                    const uint32_t e = (uint32_t)(row0 + lane - col);
+                    if (e < 64u) {
+                        const uint32_t at = (e & 7u) * 2u;
+                        uint16_t h, l;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(up.piece(e >> 3) + at) : "memory");
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(l) : "r"(lo.piece(e >> 3) + at) : "memory");
+                        const float w = unpack_half(h).x + unpack_half(l).x + p.fa;
+                        const uint32_t v_up = pack_half(w, 0.f), v_lo = pack_half(w - unpack_half(v_up).x, 0.f);
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(up.piece(e >> 3) + at), "h"((uint16_t)v_up) : "memory");
+                        if (two) asm volatile("st.shared.u16 [%0], %1;" ::"r"(lo.piece(e >> 3) + at), "h"((uint16_t)v_lo) : "memory");
+                    }
                 }
                 fence_async_shared();
                 __syncwarp();
