@@ -416,7 +416,4 @@ def fp4q_newton_schulz(g: torch.Tensor, momentum=None, beta: float = 0.95, neste
     """The orthogonalised update of weights from their gradient g, BF16 or FP32 [rows, cols] or a stack [count, rows, cols]: with a momentum (FP32,
     g's shape, updated in place) M = beta M + G and U = beta M + G (nesterov) or M, without one U = G; X = U / (|U| + eps), then one step
     X = a X + (b A + c A A) X, A = X X^T, per triple of coefficients.  Returns scale X in BF16."""
-    steps = [tuple(step) for step in coefficients]
-    if not steps or any(len(step) != 3 for step in steps):
-        raise ValueError("coefficients must be triples, one for every step")
-    return _host().newton_schulz(g, momentum, beta, nesterov, [v for step in steps for v in step], eps, scale, out, scratch, ws, _handle(stream))
+    return _host().newton_schulz(g, momentum, beta, nesterov, coefficients, eps, scale, out, scratch, ws, _handle(stream))

@@ -605,10 +605,21 @@ int64_t stack_pitch(const at::Tensor &t)
     return t.numel() && t.dim() == 3 && t.size(0) > 1 ? t.stride(0) : t.size(-1);
 }
 
-// g, momentum | None, beta, nesterov, coefficients (a flat sequence of floats), eps, scale, out | None, scratch | None, ws | None, stream
+// g, momentum | None, beta, nesterov, coefficients (triples of floats), eps, scale, out | None, scratch | None, ws | None, stream
 PyObject *newton_schulz(Args a, Py_ssize_t n)
 {
     want(n, 11);
+    Ref steps(PySequence_Tuple(a[4]));
+    std::vector<float> c;
+    for (Py_ssize_t s = 0; s < PyTuple_GET_SIZE(steps.p); s++) {
+        Ref triple(PySequence_Tuple(PyTuple_GET_ITEM(steps.p, s)));
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(triple.p); i++) {
+            c.push_back((float)PyFloat_AsDouble(PyTuple_GET_ITEM(triple.p, i)));
+            if (PyErr_Occurred()) throw PyError();
+        }
+        if (PyTuple_GET_SIZE(triple.p) != 3) value_error("coefficients must be triples, one for every step");
+    }
+    if (c.empty()) value_error("coefficients must be triples, one for every step");
     const at::Tensor &g = as_stack(as_tensor(a[0]), "g");
     if (g.scalar_type() != at::kBFloat16 && g.scalar_type() != at::kFloat) value_error("g must be BF16 or FP32");
     const bool ours = a[7] == Py_None;
@@ -621,13 +632,6 @@ PyObject *newton_schulz(Args a, Py_ssize_t n)
     const double beta = PyFloat_AsDouble(a[2]), eps = PyFloat_AsDouble(a[5]), scale = PyFloat_AsDouble(a[6]);
     if (PyErr_Occurred()) throw PyError();
     const int nesterov = as_bool(a[3]) ? 1 : 0;
-    Ref list(PySequence_Tuple(a[4]));
-    std::vector<float> c;
-    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(list.p); i++) {
-        c.push_back((float)PyFloat_AsDouble(PyTuple_GET_ITEM(list.p, i)));
-        if (PyErr_Occurred()) throw PyError();
-    }
-    if (c.empty() || c.size() % 3) value_error("coefficients must be triples, one for every step");
     const int64_t count = g.dim() == 3 ? g.size(0) : 1, rows = g.size(-2), cols = g.size(-1);
     const c10::cuda::CUDAGuard device(g.device());
     const OnStream on(a[10], &g);
