@@ -99,17 +99,20 @@ struct Gemm16Params {
     Divisor16 by_matrix, by_band;    // tiles of a matrix or group (but TILES_ROWS), and of kRaster16 rows of tiles: set by launch_gemm16
     int32_t batch;                   // groups or matrices
     int32_t bf16;                    // operand type: 0 = FP16, 1 = BF16
+    int32_t admit;                   // the next kernel may set up beside this one (it is one of the same call)
     uint32_t *deal;                  // TILES_CUT: tiles dealt, 0 when the kernel starts: they go to whoever is free; NULL: in turn
     int32_t a_box;                   // rows of one copy of a K-major A operand: 128, 64 in 64 x 64 tiles, 32 or 16 in tiles of 32 rows
-    const int64_t *offsets;          // TILES_ROWS, TILES_CUT: batch + 1 boundaries; NULL: one group of all rows
+    int32_t part_stages;             // stages of a part of a contraction in parts
+    union {
+        const int64_t *offsets;      // TILES_ROWS, TILES_CUT: batch + 1 boundaries; NULL: one group of all rows
+        const int32_t *lift;         // GRAM, UPDATE: of each matrix: its first X is scaled by this power of two more than others
+    };
     int64_t total_rows;              // rows that the boundaries are held to
     uint32_t *status;
     // Contractions in parts (TILES_CUT, EPI16_GRAM): a part's accumulator goes to `partial`, and who comes last to a tile, by its counter, adds up
     // the parts in their order.  NULL: no parts.
-    int32_t part_stages;             // stages of a part
     float *partial;                  // [part][CTA of the tile][warp][column / 4][row][column % 4]
     uint32_t *counters;              // of a tile's warps; 0 between kernels
-    int32_t admit;                   // the next kernel may set up beside this one (it is one of the same call)
     // EPI16_STORE, EPI16_SUM
     void *c;
     int64_t ldc;
@@ -117,10 +120,11 @@ struct Gemm16Params {
     int32_t boxed;                   // columns that leave in boxes, whole 16 bytes; the rest of a row leaves by itself
     // EPI16_GRAM, _POLY, _UPDATE
     int32_t split;                   // 1: operands are sums of two numbers: the products upper x upper, upper x lower and lower x upper are added up
+    float o_scale;                   // UPDATE, last step
     float fa, fb, fc;                // the step's coefficients, with the iterates' scales; POLY: fa on the diagonal
+    int32_t grown, grown_next;       // powers of two by which X may have grown since, up to this step's product and behind it
     __nv_bfloat16 *o;                // UPDATE, last step: the result instead
     int64_t ld_o;
-    float o_scale;
 };
 
 // Operands and their lower parts; what an epilogue reads (POLY: A, UPDATE: X's lower part, as in) and writes, upper and lower parts, in boxes of 32 rows x 128
@@ -266,6 +270,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     }
     return __all_sync(0xFFFFFFFFu, ok);
 }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(max(e, -126) + 127) << 23); }   // e <= 127
 // A ring's next slot and its phase.
 template <int N>
 struct Ring16 {
@@ -1053,6 +1058,13 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
             const bool two = EPI == EPI16_UPDATE || p.split != 0;      // upper and lower parts
             const bool reads_up = EPI == EPI16_POLY, reads_lo = EPI == EPI16_UPDATE ? p.split == 0 : EPI == EPI16_POLY && p.split != 0;
             const bool reads = reads_up || reads_lo;
+            // The scale that a small X has beside the usual one, now and in the next step.
+            float fa = p.fa, fb = p.fb, fc = p.fc;
+            if (EPI == EPI16_GRAM || EPI == EPI16_UPDATE) {
+                const int lift = load_global(p.lift + t.batch), now = max(0, lift - p.grown), next = p.o ? 0 : max(0, lift - p.grown_next);
+                const float by = power_of_two(EPI == EPI16_GRAM ? -2 * now : next - now);
+                fa *= by; fb *= by; fc *= by;
+            }
             auto fetch = [&](int col) {
                 if (!reads || rows <= 0 || col >= p.n) return;
                 boxes_free(lane);
@@ -1155,8 +1167,8 @@ __global__ void __launch_bounds__(kThreads16, 1) gemm16_kernel(const __grid_cons
                     for (int j = 0; j < 4; j++) {
                         const float2 y = unpack_half(au[j]), z = unpack_half(bu[j]);
                         const float v0 = x[8 * i + 2 * j], v1 = x[8 * i + 2 * j + 1];
-                        w[2 * j] = EPI == EPI16_GRAM ? v0 * p.fa : fmaf(p.fb, y.x + z.x, p.fc * v0);
-                        w[2 * j + 1] = EPI == EPI16_GRAM ? v1 * p.fa : fmaf(p.fb, y.y + z.y, p.fc * v1);
+                        w[2 * j] = EPI == EPI16_GRAM ? v0 * fa : fmaf(fb, y.x + z.x, fc * v0);
+                        w[2 * j + 1] = EPI == EPI16_GRAM ? v1 * fa : fmaf(fb, y.y + z.y, fc * v1);
                     }
                     uint32_t h[4], l[4];
                     if (out) {

@@ -15,7 +15,9 @@
 // FP16 number and 1.4e-1 with a BF16 one, 7e-4 with the sum of two).  Matrices of a short side have few elements over which the roundings of
 // A, P and the products' X average out (0.8e-3 of the result at 777 x 1003, 2.0e-3 at 64 x 64, 3e-3 and more below 16) and little work:
 // there A and P are sums of two numbers as well, and the three products are made of three each (kSplitSide).  Scales: X 2^10, A and P 2^9, so that elements of large matrices
-// stay above FP16's smallest normal number and the largest singular values that the entry point admits below its largest.
+// stay above FP16's smallest normal number and the largest singular values that the entry point admits below its largest.  A matrix whose norm is far
+// below eps keeps X small for some steps: it has a power of two more in X's scale, of which every step takes back what X may have grown by, so that X
+// is held to 22 bits, or 2^-33 of its norm, whatever that norm is.
 #include "gemm16.cuh"
 
 #include <algorithm>
@@ -26,8 +28,10 @@ using namespace fp4q;
 namespace {
 
 constexpr int kNsThreads = 256, kNsMaxBlocks = 1024;
-constexpr float kScaleX = 1024.0f, kScaleA = 512.0f;
+constexpr int kLogScaleX = 10;
+constexpr float kScaleX = 1 << kLogScaleX, kScaleA = 512.0f;
 constexpr int kMaxSteps = 64;
+constexpr int kMaxLift = 100;   // what is smaller is beyond the result's type
 constexpr int64_t kSplitSide = 384;
 
 struct MomentumParams {
@@ -41,6 +45,7 @@ struct MomentumParams {
     int32_t nesterov;
     double eps;
     double *partial;             // [count, gridDim.x]
+    int32_t *lift;               // [count]
     __half *up, *lo;             // normalised: upper and lower parts
     int64_t pitch;
     uint32_t *counters;          // of the products' tiles, to be zeroed
@@ -111,10 +116,14 @@ __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumPara
     wait_for_predecessor();
     const int64_t row0 = (int64_t)blockIdx.y * p.rows;
     double sum = 0.0;
+    int lift = 0;
     float inv0 = 0.f, inv1 = 0.f;   // 1 / (|U| + eps), scaled, as a power of two and the rest: it may lie outside of what FP32 holds
     if (FINISH) {
         for (int i = threadIdx.x; i < (int)gridDim.x; i += kNsThreads) sum += load_global(p.partial + (int64_t)blockIdx.y * gridDim.x + i);
-        const double inv = (double)kScaleX / (sqrt(block_sum(sum)) + p.eps);
+        const double norm = sqrt(block_sum(sum));
+        // A norm below eps leaves X small: it is scaled by so much more that its own norm lies between a quarter and one (from the numbers' exponents).
+        lift = max(0, min(kMaxLift, (__double2hiint(norm + p.eps) >> 20) - (__double2hiint(norm) >> 20) - 1));
+        const double inv = __hiloint2double((1023 + kLogScaleX + lift) << 20, 0) / (norm + p.eps);
         int e;
         frexp(inv, &e);
         e = max(-200, min(200, e)) / 2;
@@ -170,6 +179,7 @@ __global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumPara
             }
         }
     }
+    if (FINISH && blockIdx.x == 0 && threadIdx.x == 0) p.lift[blockIdx.y] = lift;
     if (!FINISH && blockIdx.x == 0 && blockIdx.y == 0)
         for (int i = threadIdx.x; i < p.n_counters; i += kNsThreads) p.counters[i] = 0u;
     if (!FINISH) {
@@ -208,7 +218,7 @@ struct Scratch {
     bool split;
     int edge;                            // tiles of A's product: 64, 128 or 256 (pairs)
     int64_t tiles, part_stages;
-    size_t counters, accumulators, partial, x[2], lo[2], a[2], poly[2], bytes;   // upper and lower parts; X and the next X: lower parts in one place unless they are operands
+    size_t counters, accumulators, partial, lift, x[2], lo[2], a[2], poly[2], bytes;   // upper and lower parts; X and the next X: lower parts in one place unless they are operands
     Scratch(int64_t count, int64_t rows, int64_t cols)
     {
         side = rows < cols ? rows : cols;
@@ -219,6 +229,7 @@ struct Scratch {
         partial = 0;
         bytes = (size_t)round_up(count * kNsMaxBlocks * 8, 256);
         auto place = [&](size_t n) { const size_t at = bytes; bytes += n; return at; };
+        lift = place((size_t)round_up(count * 4, 256));
         x[0] = place(x_bytes); x[1] = place(x_bytes);
         lo[0] = place(x_bytes); lo[1] = split ? place(x_bytes) : lo[0];
         a[0] = place(a_bytes); a[1] = split ? place(a_bytes) : a[0];
@@ -247,20 +258,29 @@ bool sizes_ok(int64_t count, int64_t rows, int64_t cols)
            count * rows * round_up(cols, 16) <= (1ll << 40) && count * ceil_div(rows, 128) * ceil_div(cols, 64) <= 0x7FFFFFFF - 4096;
 }
 
-// The largest singular value that X can have after each step, from at most 1, and the largest eigenvalues of b A + c A A and a I + b A + c A A: the
-// polynomials are sampled.  Whether FP16 holds all that they reach.
-bool steps_fit(const float *c, int32_t steps)
+// The largest singular value x that X can have after each step, from at most 1, and the largest eigenvalues of b A + c A A and a I + b A + c A A, with
+// q = x x: both polynomials are largest at an end of q's range or where their slope is zero.  Whether FP16 holds all that they reach.  grown[s]:
+// powers of two by which a singular value may have grown before step s.
+bool steps_fit(const float *coefficients, int32_t steps, int32_t *grown)
 {
     double top = 1.0;
+    grown[0] = 0;
     for (int32_t s = 0; s < steps; s++) {
-        double next = 0.0;
-        for (int i = 0; i <= 512; i++) {
-            const double x = top * i / 512, q = x * x, poly = c[3 * s + 1] * q + c[3 * s + 2] * q * q, y = std::fabs(x * (c[3 * s] + poly));
-            if (!(std::fabs(poly) <= 100.0) || !(std::fabs(c[3 * s] + poly) <= 100.0) || !(y <= 10.0)) return false;
-            if (y > next) next = y;
+        const double a = coefficients[3 * s], b = coefficients[3 * s + 1], c = coefficients[3 * s + 2], end = top * top;
+        const double root = std::sqrt(std::max(0.0, 9.0 * b * b - 20.0 * a * c));   // a + 3 b q + 5 c q q = 0; b + 2 c q = 0 first
+        const double at[4] = {end, c != 0.0 ? -b / (2.0 * c) : end, c != 0.0 ? (-3.0 * b + root) / (10.0 * c) : b != 0.0 ? -a / (3.0 * b) : end,
+                              c != 0.0 ? (-3.0 * b - root) / (10.0 * c) : end};
+        double next = 0.0, factor = std::fabs(a);
+        for (const double q : at) {
+            if (q < 0.0 || q > end) continue;
+            const double poly = b * q + c * q * q, all = std::fabs(a + poly), y = std::sqrt(q) * all;
+            if (!(std::fabs(poly) <= 100.0) || !(all <= 100.0) || !(y <= 10.0)) return false;
+            next = std::max(next, y);
+            factor = std::max(factor, all);
         }
-        top = next * 1.01;   // roundings
-        if (top < 1e-3) top = 1e-3;
+        if (!(factor <= 100.0)) return false;
+        grown[s + 1] = grown[s] + std::max(0, (int32_t)std::ceil(std::log2(std::max(factor, 1e-3) * 1.01)));
+        top = std::max(next * 1.01, 1e-3);   // roundings
     }
     return true;
 }
@@ -344,7 +364,8 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     if (count < 0 || rows < 0 || cols < 0 || ld_g < cols || ld_o < cols || (momentum && ld_m < cols)) return FP4Q_ERR_SHAPE;
     if (g_type != FP4Q_OUT_BF16 && g_type != FP4Q_OUT_F32) return FP4Q_ERR_UNSUPPORTED;
     if (!coefficients) return FP4Q_ERR_NULL;
-    if (steps < 1 || steps > kMaxSteps || !(eps >= 0.0f) || !steps_fit(coefficients, steps)) return FP4Q_ERR_UNSUPPORTED;
+    int32_t grown[kMaxSteps + 1];
+    if (steps < 1 || steps > kMaxSteps || !(eps >= 0.0f) || !steps_fit(coefficients, steps, grown)) return FP4Q_ERR_UNSUPPORTED;
     if (count == 0 || rows == 0 || cols == 0) return FP4Q_OK;
     if (!sizes_ok(count, rows, cols)) return FP4Q_ERR_UNSUPPORTED;
     if (!g || !out_bf16) return FP4Q_ERR_NULL;
@@ -366,6 +387,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     q.units = (uint32_t)(rows * q.units_row);
     q.beta = beta; q.nesterov = nesterov != 0; q.eps = eps;
     q.partial = reinterpret_cast<double *>(base + at.partial);
+    q.lift = reinterpret_cast<int32_t *>(base + at.lift);
     q.counters = reinterpret_cast<uint32_t *>(base + at.counters);
     q.n_counters = at.part_stages ? (int32_t)(at.tiles * (at.edge == 256 ? 16 : 8)) : 0;
     q.up = half_at(at.x[0]); q.lo = half_at(at.lo[0]); q.pitch = at.pitch_x;
@@ -381,6 +403,7 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     p.a_box = 128;
     p.status = static_cast<uint32_t *>(ws);
     p.split = at.split;
+    p.lift = q.lift;
     p.admit = 1;
     const Parts part_a(half_at(at.a[0]), half_at(at.a[1]), side, side, count, at.pitch_a), part_p(half_at(at.poly[0]), half_at(at.poly[1]), side, side, count, at.pitch_a);
     // P and X': 64 x 64 tiles where one round of them does, each with less to load and a shorter epilogue; else what is estimated to be faster
@@ -396,6 +419,8 @@ extern "C" fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_
     for (int32_t i = 0; i < steps; i++) {
         const float *c = coefficients + 3 * i;
         const int now = i & 1, next = now ^ 1;
+        p.grown = grown[i];
+        p.grown_next = grown[i + 1];
         const Parts part_x(half_at(at.x[now]), half_at(at.lo[now]), cols, rows, count, at.pitch_x);
         const Parts part_next(half_at(at.x[next]), half_at(at.lo[next]), cols, rows, count, at.pitch_x);
         Gemm16Params gp = p;

@@ -66,3 +66,20 @@ def test_stacks_of_single_rows_in_any_pitch(count, cols):
     assert not out[:, 0].any() and not out[:, 2].any() and not out[:, :, cols:].any()
     with pytest.raises(b.Fp4qError):
         b.fp4q_newton_schulz(big[:1, :1, :cols].expand(count, 1, cols), momentum=m[:1, :1].expand(count, 1, cols))       # rows that lie in one another
+
+
+@pytest.mark.parametrize("count,rows,cols", [(1, 768, 2048), (1, 200, 300), (1, 2048, 520), (6, 300, 70), (5, 900, 800), (40, 300, 400)])
+@pytest.mark.parametrize("below", [0.7, 1e-2, 1e-5, 1e-7, 1e-9, 1e-14, 1e-18])
+def test_norms_far_below_eps(count, rows, cols, below):
+    # Each matrix in its own distance from eps, one of them above it, one of zeros.  The limit is that of norms above eps: operands in FP16 in the mean
+    # square, 2^-11 / sqrt(3) sqrt(5 (3^2 + 3^2 + 4^2)), and BF16's rounding, 2^-8 / sqrt(3).
+    eps = float(torch.tensor(1e-7))
+    g = randn(1, count, rows, cols)
+    factors = [below * 0.31 ** (i % 5) for i in range(count)]
+    if count > 3:
+        factors[1], factors[2] = 1e9, 0.0
+    g *= (torch.tensor(factors, device="cuda", dtype=torch.float64) * eps / g.double().norm(dim=(1, 2))).float()[:, None, None]
+    for coefficients in (b.NEWTON_SCHULZ, ((2.0, -1.5, 0.5),) * 5, ((9.0, -9.0, 0.0), (0.5, 0.0, 0.0), (1.5, -0.5, 0.0))):
+        got, want = b.fp4q_newton_schulz(g, coefficients=coefficients, eps=eps).double(), exact(g, coefficients, eps)
+        for i in range(count):
+            assert (got[i] - want[i]).norm() <= 4.4e-3 * want[i].norm(), (i, factors[i])
