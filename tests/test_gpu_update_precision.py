@@ -83,3 +83,16 @@ def test_norms_far_below_eps(count, rows, cols, below):
         got, want = b.fp4q_newton_schulz(g, coefficients=coefficients, eps=eps).double(), exact(g, coefficients, eps)
         for i in range(count):
             assert (got[i] - want[i]).norm() <= 4.4e-3 * want[i].norm(), (i, factors[i])
+
+
+@pytest.mark.parametrize("count,rows,cols", [(1, 5, 7), (1, 16, 16), (1, 20, 20), (1, 64, 64), (1, 100, 64), (2, 64, 128), (1, 128, 120), (30, 64, 64), (130, 64, 64), (200, 128, 128),
+                                             (150, 70, 128), (150, 128, 70), (1, 17, 300), (1, 300, 33), (1, 129, 257), (40, 256, 256), (100, 256, 200), (1, 384, 384), (80, 384, 300)])
+def test_short_sides_compute_with_both_parts_of_their_operands(count, rows, cols):
+    # What is beyond BF16's rounding, half a step of the result at most.  In units of 2^-22: an operand's two parts are off by 1, the product of the lower
+    # ones, left out, is 1, the cut-off of K / 16 instructions 1 each, and the new value's two parts 1: 4 + K / 16 a product.  A's counts 2 (|b| + 2 |c|) = 18
+    # times at most, half of which cancels, P's and X's 3 each, in a result of 3: 8 a step, 5 steps.  Without one of the lower parts an operand is off by 2^11 units.
+    g = randn(rows + count, count, rows, cols)
+    got, want = b.fp4q_newton_schulz(g).double(), exact(g)
+    half = torch.ldexp(torch.full_like(got, 2.0 ** -8), torch.floor(torch.log2(got.abs().clamp_min(1e-300))))
+    beyond = ((got - want).abs() - half).clamp_min(0.0)
+    assert (beyond.norm(dim=(1, 2)) <= 40 * 2 ** -22 * (4 + max(rows, cols) / 16) * want.norm(dim=(1, 2))).all()
