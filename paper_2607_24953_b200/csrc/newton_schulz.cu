@@ -197,15 +197,18 @@ double rounds_us(int64_t tiles, int64_t stages, int64_t edge)
     return (double)ceil_div(tiles, slots) * ((double)stages * box + 2.0 * sms);
 }
 // A's product in tiles of `edge`, its contraction of `stages` boxes cut into parts: the number of parts with the least estimated time.  Parts take
-// their way through memory, where whoever comes last reads them one after the other.  (Parts for 4751 x 63: 70 -> 20 us.)
+// their way through memory, where whoever comes last reads them one after the other.  (Parts for 4751 x 63: 70 -> 20 us.)  No accumulator takes more than
+// kMostElems elements: the tensor cores cut it off towards zero, by 5e-9 of a sum of squares for each (16 x 2^20 in one: the update off by 8.5e-3).  It costs
+// stacks of some hundred short and very long matrices their 64 x 64 tiles, which are not cut (130 of 16 x 250000 22.4 -> 31.2 ms).
+constexpr int64_t kMostElems = 32768;
 struct GramPlan {
     int64_t tiles, parts = 1;
     double us = 1e30;
-    GramPlan(int64_t count, int64_t side, int64_t stages, int64_t edge)
+    GramPlan(int64_t count, int64_t side, int64_t stages, int64_t most, int64_t edge)
     {
-        const int64_t across = ceil_div(side, edge), slots = edge == 256 ? 74 : 148;
+        const int64_t across = ceil_div(side, edge), slots = edge == 256 ? 74 : 148, least = ceil_div(stages, most);
         tiles = count * across * (across + 1) / 2;
-        for (int64_t n = 1; n == 1 || (n <= 32 && stages / n >= 16 && tiles * n <= 4 * slots); n++) {
+        for (int64_t n = least; n == least || (n <= 32 && stages / n >= 16 && tiles * n <= 4 * slots); n++) {
             const double t = rounds_us(tiles * n, ceil_div(stages, n), edge) + (n > 1 ? 3.0 + 0.6 * (double)n : 0.0);
             if (t < us) { us = t; parts = n; }
         }
@@ -235,12 +238,13 @@ struct Scratch {
         a[0] = place(a_bytes); a[1] = split ? place(a_bytes) : a[0];
         poly[0] = place(a_bytes); poly[1] = split ? place(a_bytes) : poly[0];
         const int64_t stages = (split ? 2 : 1) * ceil_div(rows < cols ? cols : rows, kBox16);
-        const GramPlan one(count, side, stages, 128), two(count, side, stages, 256);
+        const int64_t most = (split ? 2 : 1) * kMostElems / kBox16;
+        const GramPlan one(count, side, stages, most, 128), two(count, side, stages, most, 256);
         const bool pairs = two.us < one.us;
         // 64 x 64 tiles, 0.17 us a stage, where all of them run at once and no parts are faster (which take about 3 us more than estimated): they are
         // all computed, and not cut.  All five steps, in larger tiles and in these: 256 x 256 129 and 104 us, 300 x 1500 167 and 143, 85 of 2382 x 45
         // 370 and 311; 200 x 5000 182 and 232.
-        const bool small = count * ceil_div(side, 64) * ceil_div(side, 64) <= 148 && 0.17 * (double)stages < std::min(one.us, two.us) + 2.0;
+        const bool small = stages <= most && count * ceil_div(side, 64) * ceil_div(side, 64) <= 148 && 0.17 * (double)stages < std::min(one.us, two.us) + 2.0;
         edge = small ? 64 : pairs ? 256 : 128;
         tiles = pairs ? two.tiles : one.tiles;
         const int64_t parts = edge == 64 ? 1 : pairs ? two.parts : one.parts;
@@ -254,8 +258,10 @@ const int64_t kMaxSide = 1 << 20, kMaxCount = 65535;
 
 bool sizes_ok(int64_t count, int64_t rows, int64_t cols)
 {
+    const int64_t side = rows < cols ? rows : cols, across = ceil_div(side, 128);   // tiles of A and parts of them are counted in 32 bits, too
     return count <= kMaxCount && rows <= kMaxSide && cols <= kMaxSide && rows * ceil_div(cols, 8) < (1ll << 31) && count * rows <= 0x7FFFFFFF &&
-           count * rows * round_up(cols, 16) <= (1ll << 40) && count * ceil_div(rows, 128) * ceil_div(cols, 64) <= 0x7FFFFFFF - 4096;
+           count * rows * round_up(cols, 16) <= (1ll << 40) && count * ceil_div(rows, 128) * ceil_div(cols, 64) <= 0x7FFFFFFF - 4096 &&
+           count * (across * (across + 1) / 2) * ceil_div(rows < cols ? cols : rows, kMostElems) <= 0x7FFFFFFF - 4096;
 }
 
 // The largest singular value x that X can have after each step, from at most 1, and the largest eigenvalues of b A + c A A and a I + b A + c A A, with

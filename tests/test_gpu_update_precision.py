@@ -96,3 +96,38 @@ def test_short_sides_compute_with_both_parts_of_their_operands(count, rows, cols
     half = torch.ldexp(torch.full_like(got, 2.0 ** -8), torch.floor(torch.log2(got.abs().clamp_min(1e-300))))
     beyond = ((got - want).abs() - half).clamp_min(0.0)
     assert (beyond.norm(dim=(1, 2)) <= 40 * 2 ** -22 * (4 + max(rows, cols) / 16) * want.norm(dim=(1, 2))).all()
+
+
+def test_more_than_2_to_the_31_elements():
+    # The last matrices of a stack, wide and tall, whose offsets pass 32 bits; BF16 gradients, without a momentum and with one.
+    for rows, cols in ((16, 1 << 20), (1 << 20, 16)):
+        count = 130
+        g = torch.empty(count, rows, cols, dtype=torch.bfloat16, device="cuda")
+        g.normal_(generator=torch.Generator("cuda").manual_seed(1))
+        out = b.fp4q_newton_schulz(g)
+        for i in (0, 63, 64, 127, 128, 129):
+            want = exact(g[i])
+            assert (out[i].double() - want).norm() <= 4.4e-3 * want.norm()
+        m = torch.ones(count, rows, cols, device="cuda")
+        b.fp4q_newton_schulz(g, momentum=m, beta=0.5, nesterov=False, out=out)
+        for i in (0, 128, 129):
+            u = 0.5 + g[i].double()
+            assert ((m[i].double() - u).abs() <= 2 ** -24 * u.abs()).all()
+            want = exact(u)
+            assert (out[i].double() - want).norm() <= 4.4e-3 * want.norm()
+        del g, m, out
+        torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("count,side,other", [(1, 24, 300_000), (3, 200, 120_000), (1, 500, 200_000), (160, 16, 70_000)])
+def test_long_sides_do_not_add_up_what_the_accumulators_cut_off(count, side, other):
+    # An instruction's cut-off is below 2^-22 of what all products add up to so far: with 32768 elements in an accumulator, 2048 instructions and a sum that
+    # grows evenly, A's diagonal is off by 1024 * 2^-22 = 2.4e-4 at most (with 300 000 elements by 2.2e-3), and counts |b + 2 c A| < 5 times a step at
+    # most: as independent steps 5 sqrt(5) 2.4e-4 = 2.7e-3 beside the limit for shorter sides, 4.4e-3 above a side of 384 and BF16's rounding below.
+    g = randn(1, count, side, other) * torch.exp(0.5 * randn(2, count, side, 1))           # rows of several lengths: their roundings are independent
+    limit = math.hypot(2.7e-3, 2 ** -8 / 3 ** 0.5 if side <= 384 else 4.4e-3)
+    for u in (g, g.mT.contiguous()):
+        got = b.fp4q_newton_schulz(u).double()
+        for i in range(0, count, 53):
+            want = exact(u[i])
+            assert (got[i] - want).norm() <= limit * want.norm()
