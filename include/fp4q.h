@@ -394,7 +394,10 @@ fp4q_status fp4q_gemm_fwd_static_workspace(const fp4q_tensor *X, const fp4q_tens
  * Any T, N and K, 0 included.  Operands are 16-byte aligned with leading dimensions in multiples of 8 elements; outputs are BF16 or FP32
  * (dt; FP4Q_OUT_PADDED may be added and changes nothing), 16-byte aligned with rows of whole 16 bytes, and only their columns are
  * written.  accumulate != 0 adds to dW (FP32 only).  FP32 accumulation; an FP32 output is the sum, rounded to nearest, of partial
- * sums over 512 contraction elements each, so that the tensor cores' cut-off towards zero does not add up over a long contraction.
+ * sums over 512 contraction elements each, so that the tensor cores' cut-off towards zero does not add up over a long contraction.  A BF16
+ * output is rounded from one accumulator, which is cut off by some 1e-9 of the result for every contraction element, 5e-9 where all products have
+ * one sign (2^-22 / 16 of the sum of absolute products at most); in weight gradients with scratch memory from the sum of accumulators over up to
+ * 131072 rows each.
  * A group's result does not depend on the other groups' values.  ws/ws_bytes/stream and the asynchronous FP4Q_ERR_TIMEOUT as for fp4q_gemm_fwd.
  * scratch (weight gradient): fp4q_ragged_gemm_wgrad_scratch_bytes() bytes of device memory (0: none is needed, or the call refuses these sizes), 256-byte aligned, any contents,
  * in which long contractions that have few tiles are added up from parts, in a fixed order, and what is left to do is counted; NULL: they are

@@ -318,9 +318,9 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
     t.parts = 1;
     t.slot0 = t.counter = 0;
     if (TILES == TILES_SYM) {
+        // The first parts of all tiles, then the second ones: tiles that share rows read them at the same time.  (Updates of 4096 x 128256 in 4 parts 31.1 -> 29.7 ms.)
         t.parts = parts16(p, passes * ((p.k + kK - 1) / kK));
         const int per = m_tiles * (m_tiles + 1) / 2;
-        // The first parts of all tiles, then the second ones: tiles that share rows read them at the same time.  (4096 x 128256, all steps 31.1 -> 29.7 ms.)
         part = t.parts == 1 ? 0 : tile / (p.batch * per);
         t.counter = tile - part * (p.batch * per);
         t.slot0 = t.counter * t.parts;
@@ -341,8 +341,16 @@ __device__ __forceinline__ Tile16 decode16(const Gemm16Params &p, int tile, int 
             r = tile - (p.partial ? first[at] : at * per);
             if (p.partial) {
                 t.parts = parts16(p, (t.k_len + kK - 1) / kK);
-                const int in_group = r / t.parts;
-                part = r - in_group * t.parts;
+                // The first parts of all the group's tiles, then the second ones, as above, unless there are more parts than tiles.  (2^20 rows in 2 groups of 1024 x
+                // 1024 2178 -> 1768 us, 32768 in 16 skewed ones of 2048 x 1024 220 -> 174; but 131072 in 100 of 256 x 256 87 -> 98.)
+                int in_group;
+                if (t.parts <= per) {
+                    part = p.by_matrix(r);
+                    in_group = r - part * per;
+                } else {
+                    in_group = r / t.parts;
+                    part = r - in_group * t.parts;
+                }
                 t.slot0 = slots[at] + in_group * t.parts;
                 t.counter = t.slot0;   // no two tiles start in one place
                 r = in_group;

@@ -162,26 +162,28 @@ namespace {
 // 0.38 us in a pair and 0.285 in a single CTA (0.32 with all of them at work), 3.3 and 1.7 us a tile, and where there are parts 3 us and 1.4 or 0.7 us
 // for each, which whoever comes last reads.  Groups longer than the others are cut at half of what a CTA or pair would have to do if all had the same.
 // (131072 rows in 4 groups, 256 x 256: 9 parts in single CTAs 39 us, 32 parts in pairs 198; 131072 in one, 768 x 2048: 3 parts in pairs 300, 14 of them
-// 411, single CTAs 544; 8192 in 2, 2048 x 2048: uncut in pairs 55, in parts of 56 stages 111, single CTAs 82.)
+// 411, single CTAs 544; 8192 in 2, 2048 x 2048: uncut in pairs 55, in parts of 56 stages 111, single CTAs 82.)  Where the output is BF16 no part is longer
+// than kMostStages: its accumulators are cut off towards zero, by 5e-9 of a sum of one sign for every row, which adds up (2^20 rows, 768 x 2048, in 3 parts:
+// 2.5e-3 too small in the mean, half a step of BF16 being 2 to 4e-3; in parts of this length 0.3e-3).
 //
 // Where there are parts, groups of several lengths are dealt to whoever is free, by a counter, but not where every tile has a CTA or pair to itself
 // (65536 rows in 64 skewed groups, 1024 x 1024: 190 us dealt, 224 in turn; 32768 in 16, 2048 x 1024: 152 and 169).  Without parts a group
 // alone fills the GPU, or all are short, and tiles go in turn (8192 rows in 32, 4096 x 2048: 348 us dealt, 276 in turn; 1024 in 4, 768 x 2048: 14.6 and 12.3).  The counters of a
 // call lie in its own scratch memory, so that calls which share a workspace do not meddle with one another's tiles.
 struct CutPlan {
-    static constexpr int64_t kDealBytes = 256;
+    static constexpr int64_t kDealBytes = 256, kMostStages = 2048;
     bool pairs = false, cut = false, deals = false;   // without scratch memory neither parts nor dealing
     int64_t m_tiles, n_tiles, part_stages = 0, places = 0, most_tiles, counter_bytes = 0;   // counters: the tiles dealt, then those of the parts
     size_t bytes = 0;
-    CutPlan(int64_t T, int64_t N, int64_t K, int64_t groups, bool scratch)
+    CutPlan(int64_t T, int64_t N, int64_t K, int64_t groups, bool scratch, bool f32)
     {
         const int64_t stages = ceil_div(T, kBox16);
         const double mean = std::max(1.0, (double)stages / groups + (groups > 1 ? 0.5 : 0.0));   // stages of a group
         double least = 1e30;
         for (int two = 0; two < (N > 128 && K > 128 ? 2 : 1); two++) {
             const int64_t edge = two ? 256 : 128, slots = two ? 74 : 148, tiles = groups * ceil_div(N, edge) * ceil_div(K, edge);
-            const int64_t most = scratch ? std::min<int64_t>(64, std::max<int64_t>(1, (int64_t)mean / 16)) : 1;
-            for (int64_t n = 1; n <= most; n++) {
+            const int64_t fewest = scratch && !f32 ? (int64_t)std::ceil(mean / kMostStages) : 1, most = scratch ? std::max(fewest > 1 ? fewest + 2 : 1, std::min<int64_t>(64, (int64_t)mean / 16)) : 1;
+            for (int64_t n = fewest; n <= most; n++) {
                 const double box = two ? 0.38 : tiles * n >= slots ? 0.32 : 0.285;
                 const double us = (double)ceil_div(tiles * n, slots) * (std::ceil(mean / n) * box + (two ? 3.3 : 1.7)) + (n > 1 ? 3.0 + (two ? 1.4 : 0.7) * (double)n : 0.0);
                 if (us >= least) continue;
@@ -191,6 +193,7 @@ struct CutPlan {
                 part_stages = round_up(std::max<int64_t>(16, (int64_t)std::ceil(n > 1 ? mean / n : std::max(half, 1.25 * mean))), 8);
             }
         }
+        if (!f32) part_stages = std::min(part_stages, kMostStages);
         m_tiles = ceil_div(N, pairs ? 256 : 128);
         n_tiles = ceil_div(K, pairs ? 256 : 128);
         const int64_t each = m_tiles * n_tiles;
@@ -219,7 +222,7 @@ bool tiles_fit(int64_t T, int64_t N, int64_t K, int64_t groups)
 extern "C" size_t fp4q_ragged_gemm_wgrad_scratch_bytes(int64_t T, int64_t N, int64_t K, int32_t n_groups)
 {
     if (T <= 0 || N <= 0 || K <= 0 || n_groups <= 0 || n_groups > kMaxGroups16 || T > kMaxDim16 || N > kMaxDim16 || K > kMaxDim16) return 0;
-    return tiles_fit(T, N, K, n_groups) ? CutPlan(T, N, K, n_groups, true).bytes : 0;
+    return tiles_fit(T, N, K, n_groups) ? std::max(CutPlan(T, N, K, n_groups, true, false).bytes, CutPlan(T, N, K, n_groups, true, true).bytes) : 0;   // of either type
 }
 
 extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t N, int64_t ld_dy, const void *x, int64_t K, int64_t ldx, void *dW, int64_t ldw,
@@ -239,7 +242,7 @@ extern "C" fp4q_status fp4q_ragged_gemm_wgrad(const void *dY, int64_t T, int64_t
     if (fp4q_status s = check_operand16(m)) return s;
     if (fp4q_status s = check_workspace(ws, ws_bytes)) return s;
     if (!tiles_fit(T, N, K, groups)) return FP4Q_ERR_UNSUPPORTED;
-    const CutPlan plan(T, N, K, groups, scratch != nullptr);
+    const CutPlan plan(T, N, K, groups, scratch != nullptr, out_f32(dt));
     if (scratch && scratch_bytes < plan.bytes) return FP4Q_ERR_WORKSPACE;
     if (scratch && !aligned(scratch, 256)) return FP4Q_ERR_ALIGN;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);

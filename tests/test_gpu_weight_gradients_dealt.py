@@ -102,3 +102,16 @@ def test_without_scratch_memory_they_go_in_turn():
     want = torch.cat([dy[i:j].double().T @ x[i:j].double() for i, j in spans])
     s = torch.cat([dy[i:j].double().abs().T @ x[i:j].double().abs() for i, j in spans])
     assert ((out.double() - want).abs() <= s * (32 * 2 ** -22 + (max(j - i for i, j in spans) // 512 + 2) * 2 ** -24)).all()
+
+
+def test_many_rows_do_not_add_up_what_bf16_accumulators_cut_off():
+    # Sums of one sign over 2^20 rows.  An accumulator takes 131072 of them at most, in 8192 instructions that cut off less than 2^-22 of a sum that grows
+    # evenly: 4096 * 2^-22 = 9.8e-4 of the result.  Rounding to BF16 is right in the mean: 2^-8 / sqrt(3) / sqrt(32768) for the columns' several sizes.
+    T, n, k = 1 << 20, 768, 2048
+    g = torch.Generator("cuda").manual_seed(1)
+    dy = torch.rand(T, n, generator=g, device="cuda").to(torch.bfloat16)
+    x = (torch.rand(T, k, generator=g, device="cuda") * (1 + torch.rand(k, generator=g, device="cuda"))).to(torch.bfloat16)
+    got = b.fp4q_ragged_gemm_wgrad(dy, x, dt=b.OUT_BF16)[:64, :512].double()
+    want = dy[:, :64].double().T @ x[:, :512].double()
+    off = (got - want) / want
+    assert off.mean().abs() <= 4096 * 2 ** -22 + 5 * 2 ** -8 / 3 ** 0.5 / 32768 ** 0.5 and off.abs().max() <= 4096 * 2 ** -22 + 2 ** -8
