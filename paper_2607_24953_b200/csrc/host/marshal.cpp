@@ -164,10 +164,22 @@ const at::Tensor &as_matrix(PyObject *o, const char *name, const char *what)
     if (x.scalar_type() != at::kBFloat16 || x.dim() != 2 || (x.numel() && x.stride(1) != 1)) value_error(what);
     return x;
 }
+// A tensor that a kernel reads or writes beside `like`: on its device.
+void same_device(const at::Tensor &t, const at::Tensor &like, const char *name)
+{
+    if (t.device() == like.device()) return;
+    PyErr_Format(PyExc_ValueError, "%s must live on the same CUDA device as the other tensors", name);
+    throw PyError();
+}
 // The caller's workspace, or one that lasts for this call: its memory is reused in the order of the call's stream.
 at::Tensor workspace(PyObject *o, const at::Tensor &like)
 {
-    if (o != Py_None) return as_tensor(o);
+    if (o != Py_None) {
+        const at::Tensor &t = as_tensor(o);
+        same_device(t, like, "ws");
+        if (!t.is_contiguous()) value_error("ws must be contiguous");
+        return t;
+    }
     Unlock u;
     return at::zeros({(int64_t)lib.workspace_bytes()}, at::TensorOptions().dtype(at::kByte).device(like.device()));
 }
@@ -522,14 +534,6 @@ PyObject *mxfp8_qk(Args a, Py_ssize_t n)
                        ws.data_ptr(), (size_t)ws.numel(), on.handle), "fp4q_mxfp8_qk");
     Ref q(out[0].defined() ? THPVariable_Wrap(out[0]) : Py_NewRef(Py_None)), k(out[1].defined() ? THPVariable_Wrap(out[1]) : Py_NewRef(Py_None));
     return PyTuple_Pack(2, q.p, k.p);
-}
-
-// A tensor that a kernel reads or writes beside `like`: on its device.
-void same_device(const at::Tensor &t, const at::Tensor &like, const char *name)
-{
-    if (t.device() == like.device()) return;
-    PyErr_Format(PyExc_ValueError, "%s must live on the same CUDA device as the other tensors", name);
-    throw PyError();
 }
 
 // which (0 fwd, 1 dgrad, 2 wgrad), a (x or dY), b (w or x), row_offsets | None, out | None, dt, accumulate, scratch | None, ws | None, stream
