@@ -12,9 +12,10 @@
 // and carries what A's rounding makes of b A + c A A.  Where a matrix's singular values are all alike A and P are little but their diagonals, and these
 // errors do not average out.  The term a X carries directions of small singular values from step to step, multiplied by a = 3.4 each time,
 // and rounding X as a whole puts noise into those that a gradient does not have (rank 100, 768 x 2048: the update is off by 1.8e-2 with one
-// FP16 number and 1.4e-1 with a BF16 one, 7e-4 with the sum of two).  Matrices of a short side have few elements over which the roundings of
-// A, P and the products' X average out (0.8e-3 of the result at 777 x 1003, 2.0e-3 at 64 x 64, 3e-3 and more below 16) and little work:
-// there A and P are sums of two numbers as well, and the three products are made of three each (kSplitSide).  Scales: X 2^10, A and P 2^9, so that elements of large matrices
+// FP16 number and 1.4e-1 with a BF16 one, 1.3e-3 with the sum of two).  Matrices of a short side have few elements over which the roundings of
+// A, P and the products' X average out and little work: there A and P are sums of two numbers as well, and the three products are made of three each
+// (kSplitSide).  Beside the result's rounding to BF16, 1.7e-3 of its norm, they are off by 5e-7; others by 1.4e-3 (777 x 1003) to 2.8e-3 (385 x 30000) on random
+// matrices, and by up to 4e-3 where all singular values are alike (orthogonal 400 x 400, an identity of 385).  Scales: X 2^10, A and P 2^9, so that elements of large matrices
 // stay above FP16's smallest normal number and the largest singular values that the entry point admits below its largest.  A matrix whose norm is far
 // below eps keeps X small for some steps: it has a power of two more in X's scale, of which every step takes back what X may have grown by, so that X
 // is held to 22 bits, or 2^-33 of its norm, whatever that norm is.
@@ -109,15 +110,16 @@ __device__ __forceinline__ double block_sum(double v)
 // FINISH = false: the momentum, and each block's share of |U|^2.  FINISH = true: the norm, and X = U / (|U| + eps) in two halves.
 // The sum of squares is held in 64 bits: gradients of 1e-25 and 1e25 have squares that FP32 does not.
 // UNROLL: units of eight columns that a thread has under way: one in stacks (64 of 768 x 2048, BF16 gradients: 157 and 180 us, with two 199 and 200;
-// 1 GB each), two in a single matrix, whose blocks are fewer (11008 x 4096: 105 and 87 with one, 86 and 85 with two; 541 MB).
+// 1 GB each), two in a single matrix, whose blocks are fewer (11008 x 4096: 105 and 87 with one, 86 and 85 with two; 541 MB).  Six blocks an SM, 40 registers, in
+// the stacks' first pass (128 of 768 x 2048 313 us; 347 with 42 registers and five blocks).
 template <bool FINISH, int UNROLL>
-__global__ void __launch_bounds__(kNsThreads) momentum_kernel(const MomentumParams p)
+__global__ void __launch_bounds__(kNsThreads, !FINISH && UNROLL == 1 ? 6 : 1) momentum_kernel(const MomentumParams p)
 {
     wait_for_predecessor();
     const int64_t row0 = (int64_t)blockIdx.y * p.rows;
     double sum = 0.0;
     int lift = 0;
-    float inv0 = 0.f, inv1 = 0.f;   // 1 / (|U| + eps), scaled, as a power of two and the rest: it may lie outside of what FP32 holds
+    float inv0 = 0.f, inv1 = 0.f;   // 1 / (|U| + eps), scaled, as a power of two and the rest, rounded by 2^-24 as one factor of the matrix: it may lie outside of what FP32 holds
     if (FINISH) {
         for (int i = threadIdx.x; i < (int)gridDim.x; i += kNsThreads) sum += load_global(p.partial + (int64_t)blockIdx.y * gridDim.x + i);
         const double norm = sqrt(block_sum(sum));
