@@ -40,8 +40,9 @@ constexpr int kMaxGroups16 = 2047;   // boundaries and first tiles of this many 
 enum { TILES_ROWS = 0, TILES_CUT = 1, TILES_BATCH = 2, TILES_SYM = 3 };
 // EPI16_STORE: BF16 output.  EPI16_SUM: FP32 output.  The others are the three products of a Newton-Schulz step (newton_schulz.cu).
 // The tensor cores cut the sum of an accumulator and 16 products off to FP32, towards zero: the error grows with the contraction, by 1e-9 of
-// the result for every element (2e-5 at 16384; 8e-5 where all products are positive).  BF16 and FP16 outputs do not show it.  FP32
-// ones are sums, to nearest and in registers, of accumulators of 512 elements each.
+// the result for every element (2e-5 at 16384; 8e-5 where all products are positive).  BF16 and FP16 outputs do not show it up to some 10^5
+// elements, and longer contractions are cut into parts (newton_schulz.cu, CutPlan in ragged_gemm.cu); forward and input gradient, whose contraction is a
+// layer's width, are not.  FP32 ones are sums, to nearest and in registers, of accumulators of 512 elements each.
 enum { EPI16_STORE = 0, EPI16_GRAM = 1, EPI16_POLY = 2, EPI16_UPDATE = 3, EPI16_SUM = 4 };
 constexpr int kSumElems = 512;
 
