@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kNsThreads, !FINISH && UNROLL == 1 ? 6 : 1) mo
         for (int i = threadIdx.x; i < (int)gridDim.x; i += kNsThreads) sum += load_global(p.partial + (int64_t)blockIdx.y * gridDim.x + i);
         const double norm = sqrt(block_sum(sum));
         // A norm below eps leaves X small: it is scaled by so much more that its own norm lies between a quarter and one (from the numbers' exponents).
-        lift = max(0, min(kMaxLift, (__double2hiint(norm + p.eps) >> 20) - (__double2hiint(norm) >> 20) - 1));
+        lift = norm > 0.0 ? max(0, min(kMaxLift, (__double2hiint(norm + p.eps) >> 20) - (__double2hiint(norm) >> 20) - 1)) : 0;
         const double inv = __hiloint2double((1023 + kLogScaleX + lift) << 20, 0) / (norm + p.eps);
         int e;
         frexp(inv, &e);

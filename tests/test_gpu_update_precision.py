@@ -131,3 +131,14 @@ def test_long_sides_do_not_add_up_what_the_accumulators_cut_off(count, side, oth
         for i in range(0, count, 53):
             want = exact(u[i])
             assert (got[i] - want).norm() <= limit * want.norm()
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 60), (500, 700)])
+def test_zeros_beside_the_smallest_eps(rows, cols):
+    for eps in (1e-45, 1e-38, 1e-30, 1e-7, 1.0):
+        g = torch.zeros(3, rows, cols, device="cuda")
+        g[1] = randn(1, rows, cols)
+        out = b.fp4q_newton_schulz(g, eps=eps)
+        assert not out[0].any() and not out[2].any()
+        want = exact(g[1], eps=float(torch.tensor(eps)))
+        assert (out[1].double() - want).norm() <= 4.4e-3 * want.norm()
