@@ -424,8 +424,8 @@ fp4q_status fp4q_ragged_gemm_wgrad(const void *dy_bf16, int64_t T, int64_t N, in
  * overlap another.  coefficients is a HOST array, read during the call; steps 1 to 64.  (3.4445, -4.7750, 2.0315) five times is the usual choice.
  * Coefficients that let a singular value exceed 10, or an eigenvalue of b A + c A A or a I + b A + c A A 100, are refused
  * (FP4Q_ERR_UNSUPPORTED): the products' operands are FP16.  eps >= 0; a matrix U of zeros gives zeros if eps > 0.  A matrix that holds an infinity or NaN gives NaN
- * and leaves the others as they are.  An element of the iterate X is held in 22 bits, or to 2^-33 of X's norm where that is more (also where |U| is far
- * below eps, down to 2^-100 of it), and the sum of squares in 64-bit floating point.  Up to a shorter side of 384 all operands have these 22 bits,
+ * and leaves the others as they are.  An element of the iterate X is held in 22 bits, or to 2^-33 of the norm that X starts with, or may have grown to,
+ * where that is more (also where |U| is far below eps, down to 2^-100 of it), and the sum of squares in 64-bit floating point.  Up to a shorter side of 384 all operands have these 22 bits,
  * and the result is off by its rounding to BF16, 1.7e-3 of its norm.  Above, the products' operands are rounded to 11 bits: 2.1e-3 to 3.2e-3 on random
  * matrices, up to 6e-3 where all singular values are alike.
  * scratch: fp4q_newton_schulz_scratch_bytes() bytes of device memory, 256-byte aligned, any contents; calls that share it must not overlap

@@ -18,7 +18,7 @@
 // matrices, and by up to 4e-3 where all singular values are alike (orthogonal 400 x 400, an identity of 385).  Scales: X 2^10, A and P 2^9, so that elements of large matrices
 // stay above FP16's smallest normal number and the largest singular values that the entry point admits below its largest.  A matrix whose norm is far
 // below eps keeps X small for some steps: it has a power of two more in X's scale, of which every step takes back what X may have grown by, so that X
-// is held to 22 bits, or 2^-33 of its norm, whatever that norm is.
+// is held to 22 bits, or 2^-33 of the norm that it starts with or may have grown to, whatever that norm is.
 #include "gemm16.cuh"
 
 #include <algorithm>
