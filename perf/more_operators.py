@@ -269,7 +269,7 @@ def run(s):
             r, c = s["case"]["rows"], s["case"]["cols"]
             return {"q": q.q[:, :c].view(torch.float8_e4m3fn), "scale": q.scale, "q_t": q.q_t[:, :r].view(torch.float8_e4m3fn), "scale_t": q.scale_t}
         if op == "clip":
-            norm = b.fp4q_clip_grad_norm(s["g"], s["max_norm"], outs=s["out"], ws=s["ws"], scratch=s["scratch"])
+            norm = b.fp4q_clip_grad_norm(s["g"], s["max_norm"], outs=s["out"], scratch=s["scratch"])
             return {"norm": norm, "g": s["out"]}
         dt = b.OUT_F32 if s["case"]["out"] == "f32" else b.OUT_BF16
         call = {"fwd": b.fp4q_fp8_gemm_fwd, "dgrad": b.fp4q_fp8_gemm_dgrad, "wgrad": b.fp4q_fp8_gemm_wgrad}[op]
