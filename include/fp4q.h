@@ -437,6 +437,129 @@ fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_t count, in
                                int64_t ld_m, float beta, int nesterov, const float *coefficients, int32_t steps, float eps, float scale,
                                void *out_bf16, int64_t ld_o, void *scratch, size_t scratch_bytes, void *ws, size_t ws_bytes, void *stream);
 
+/*
+ * 8-bit tensors with a scale for every block of 128 -- no counterpart in the paper's method: the 8-bit format that FP4 and MXFP8 layers are compared
+ * with, and the one to keep a layer in that does not stand FP4.  E4M3 codes and FP32 scales, element = code x scale.  A block is 128
+ * consecutive elements along the contraction of one row (1D, activations and gradients) or 128 x 128 elements (square, weights); blocks that the
+ * tensor's edge cuts off are shorter.
+ *   q   [rows, ld_q]: codes; scale [rows, ld_s >= ceil(cols/128)], with square blocks [ceil(rows/128), ld_s]
+ *   q_t [cols, ld_t]: codes of the transpose; 1D blocks: along the rows of the source, with scales of their own, scale_t [cols, ld_st >= ceil(rows/128)];
+ *                     square blocks: the same codes as in q, and the same scales (scale is written and read either way, scale_t is not used)
+ * q or q_t may be NULL where it is not wanted.  Payloads are 16-byte aligned in pitches of whole 16 bytes, scales are aligned to their elements.
+ */
+typedef struct {
+    int64_t rows, cols;
+    uint8_t *q;
+    int64_t ld_q;
+    float *scale;
+    int64_t ld_s;
+    uint8_t *q_t;
+    int64_t ld_t;
+    float *scale_t;
+    int64_t ld_st;
+    int32_t square;   /* 0: 1D blocks, 1: 128 x 128 */
+} fp4q_fp8_tensor;
+
+/*
+ * fp4q_fp8_quantize -- x (BF16 or FP32 (x_type, a plain fp4q_out), [rows, cols], ld_x in elements, aligned to its element) into that format, both orientations
+ * in one reading.  With M the largest magnitude of a block's finite elements, not below 2^-100: scale = M / 448, code = x * (448 / M) rounded to the
+ * nearest E4M3 number, ties to even (every operation in FP32, rounded to nearest).  Infinities and NaN become NaN.  Bytes of a payload row up to the next multiple of 16 behind its last element are written as 0.
+ */
+fp4q_status fp4q_fp8_quantize(const void *x, fp4q_out x_type, int64_t rows, int64_t cols, int64_t ld_x, const fp4q_fp8_tensor *out, void *stream);
+
+/*
+ * fp4q_fp8_gemm_fwd / _dgrad / _wgrad -- the three products of Section 3, "Application to linear layers", on such tensors:
+ *   Y[T,N] = X^ W^^T    reads X.q (1D blocks) and W.q (square)            dX[T,K] = dY^ W^    reads dY.q (1D) and W.q_t (square)
+ *   dW[N,K] (+)= dY^^T X^    reads dY.q_t and X.q_t (1D, along the tokens)
+ * Any T, N and K, 0 included (an empty contraction gives zeros).  The products of 128 contraction elements are added up by the tensor cores, the sums of these blocks,
+ * times both scales, in FP32, rounded to nearest.  Single tokens and small results split the contraction over up to 8 CTAs, whose sums are added in a fixed order.  Outputs,
+ * FP4Q_OUT_PADDED, alignment, accumulate (FP32 only), ws/ws_bytes/stream and the asynchronous FP4Q_ERR_TIMEOUT as for fp4q_gemm_fwd and
+ * fp4q_gemm_wgrad.
+ */
+fp4q_status fp4q_fp8_gemm_fwd(const fp4q_fp8_tensor *X, const fp4q_fp8_tensor *W, void *Y, int64_t ldy, fp4q_out dt, void *ws, size_t ws_bytes, void *stream);
+fp4q_status fp4q_fp8_gemm_dgrad(const fp4q_fp8_tensor *dY, const fp4q_fp8_tensor *W, void *dX, int64_t ldx, fp4q_out dt, void *ws, size_t ws_bytes, void *stream);
+fp4q_status fp4q_fp8_gemm_wgrad(const fp4q_fp8_tensor *dY, const fp4q_fp8_tensor *X, void *dW, int64_t ldw, fp4q_out dt, int accumulate, void *ws, size_t ws_bytes,
+                                void *stream);
+
+/*
+ * fp4q_rms_norm -- no counterpart in the paper: the norm in front of a projection, with the residual's addition before it and the projection's 8-bit
+ * operand behind it.  For every row of x [rows, cols]:
+ *   h = x + residual, rounded to h's type (residual == NULL: h = x, and n->h is not used);  r = 1 / sqrt(mean(h^2) + eps);  y = h r weight
+ * A residual has h's type; h may be the residual's own memory.  weight is FP32 or BF16 [cols], NULL: ones.  Of y (BF16, or FP32), q with scale, and rstd (r, [rows]) any may be
+ * NULL.  q_format: FP4Q_NORM_MXFP8 (scale: UE8M0 bytes [rows, ld_s >= ceil(cols/32)], codes and scales by the rules of fp4q_mxfp8_quantize1d) or
+ * FP4Q_NORM_FP8 (scale: FP32 [rows, ld_s >= ceil(cols/128)], by those of fp4q_fp8_quantize, 1D blocks); both are taken from y before it is rounded.
+ * q is 16-byte aligned in a pitch of whole 16 bytes (MXFP8: >= ceil32(cols)) and written up to the next multiple of 16 behind its last element (MXFP8: 32), with zeros.  The other matrices are
+ * aligned to their elements and only their columns are written.  cols up to 65536.  Sums are FP32.  Infinities and NaN go where the formulas take them.
+ */
+enum { FP4Q_NORM_MXFP8 = 1, FP4Q_NORM_FP8 = 2 };
+typedef struct {
+    const void *x;
+    int64_t ld_x;
+    fp4q_out x_type;
+    const void *residual;
+    int64_t ld_residual;
+    void *h;
+    int64_t ld_h;
+    fp4q_out h_type;        /* of h and of the residual */
+    const void *weight;
+    fp4q_out weight_type;
+    float eps;              /* >= 0 */
+    void *y;
+    int64_t ld_y;
+    fp4q_out y_type;
+    uint8_t *q;
+    int64_t ld_q;
+    void *scale;
+    int64_t ld_s;
+    int32_t q_format;
+    float *rstd;
+} fp4q_norm;
+fp4q_status fp4q_rms_norm(const fp4q_norm *n, int64_t rows, int64_t cols, void *stream);
+
+/*
+ * fp4q_rms_norm_bwd -- its gradients: with g = dy weight,
+ *   dx = r (g - h r mean(g h r)) + dh (the gradient that arrives at h by itself; NULL: none),   dweight (+)= sum over the rows of dy h r
+ * dx is the gradient of x and of the residual alike; dh and dx have h's type, and dx may be dh's own memory.  h and rstd are those of the forward pass.  dweight is FP32 [cols] or
+ * NULL; accumulate != 0 adds to it.  No rows leave dweight zero, or unchanged when accumulating.  The sum over the rows is taken in FP32 in a fixed order.  scratch: fp4q_rms_norm_bwd_scratch_bytes()
+ * bytes of device memory, 256-byte aligned, any contents, for dweight alone; calls that share it must not overlap on the GPU.
+ */
+typedef struct {
+    const void *dy;
+    int64_t ld_dy;
+    fp4q_out dy_type;
+    const void *h;
+    int64_t ld_h;
+    fp4q_out h_type;
+    const float *rstd;
+    const void *weight;
+    fp4q_out weight_type;
+    const void *dh;
+    int64_t ld_dh;
+    void *dx;
+    int64_t ld_dx;
+    float *dweight;
+    int32_t accumulate;
+} fp4q_norm_grad;
+size_t fp4q_rms_norm_bwd_scratch_bytes(int64_t rows, int64_t cols);
+fp4q_status fp4q_rms_norm_bwd(const fp4q_norm_grad *n, int64_t rows, int64_t cols, void *scratch, size_t scratch_bytes, void *stream);
+
+/*
+ * fp4q_global_norm -- no counterpart in the paper: norm = the square root of the sum of squares of all elements of n_tensors matrices (BF16 or FP32, [rows, cols], ld in
+ * elements, aligned to their elements), the gradients of a step; into the FP32 at `norm` (device memory).  Squares are added in 64 bits or, where that loses nothing, in FP32 runs of 32;
+ * the order is fixed.  `tensors` is a HOST array, read during the call; empty tensors are skipped; without any the norm is 0.
+ * fp4q_clip_by_norm -- out = g * min(1, max_norm / (norm + eps)), every tensor into its entry of `outs` (rounded once; BF16 or FP32, the same shape; not
+ * overlapping another's), or in place (outs == NULL; then tensors stay untouched where the factor is 1).  A norm of NaN gives NaN.  max_norm >= 0, eps >= 0.
+ * scratch: fp4q_global_norm_scratch_bytes() bytes of device memory, 256-byte aligned, any contents; calls that share it must not overlap on the GPU.
+ */
+typedef struct {
+    void *data;
+    int64_t rows, cols, ld;
+    fp4q_out type;
+} fp4q_span;
+size_t fp4q_global_norm_scratch_bytes(const fp4q_span *tensors, int32_t n_tensors);
+fp4q_status fp4q_global_norm(const fp4q_span *tensors, int32_t n_tensors, float *norm, void *scratch, size_t scratch_bytes, void *stream);
+fp4q_status fp4q_clip_by_norm(const fp4q_span *tensors, const fp4q_span *outs, int32_t n_tensors, const float *norm, float max_norm, float eps, void *stream);
+
 const char *fp4q_status_string(fp4q_status s);
 
 /* Library version: major*10000 + minor*100 + patch. */

@@ -136,6 +136,143 @@ def ragged_linear(x: torch.Tensor, weight: torch.Tensor, row_offsets: torch.Tens
     return _RaggedLinearFn.apply(x, weight, row_offsets, ws)
 
 
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """t as the norm and the 8-bit quantizer read it: BF16 or FP32 in contiguous rows; t itself where it is so."""
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        t = t.to(torch.bfloat16)
+    return t if t.stride(1) == 1 or t.shape[1] <= 1 else t.contiguous()
+
+
+def _cast(t, dtype):
+    return t if t is None or t.dtype == dtype else t.to(dtype)
+
+
+class _RMSNormFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        xr, rr = _rows(x), None if residual is None else _rows(residual)
+        out = binding.alloc_norm(xr, rr, y=x.dtype != torch.float32, rstd=True)
+        if out.y is None:
+            out.y = torch.empty(x.shape, dtype=torch.float32, device=x.device)
+        n = binding.fp4q_rms_norm(xr, _weight(weight), rr, eps=eps, out=out)
+        ctx.save_for_backward(xr if rr is None else n.h, n.rstd, weight)
+        ctx.types = x.dtype, None if residual is None else residual.dtype
+        y = _cast(n.y, x.dtype).contiguous()
+        return (y, None) if residual is None else (y, _cast(n.h, residual.dtype).contiguous())
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh):
+        h, rstd, weight = ctx.saved_tensors
+        dx, dw = _norm_backward(dy, dh, h, rstd, weight, ctx.needs_input_grad[1])
+        return _cast(dx, ctx.types[0]), dw, _cast(dx, ctx.types[1]) if ctx.needs_input_grad[2] else None, None
+
+
+def _weight(weight):
+    return None if weight is None else _cast(weight, torch.float32 if weight.dtype not in (torch.bfloat16, torch.float32) else weight.dtype).contiguous()
+
+
+def _norm_backward(dy, dh, h, rstd, weight, want):
+    dh = None if dh is None else _cast(_rows(dh), h.dtype)
+    dx, dw = binding.fp4q_rms_norm_bwd(_rows(dy), h, rstd, _weight(weight), dh=dh, want_dweight=want)
+    return dx, _cast(dw, weight.dtype) if want else None
+
+
+def _check_norm(x, weight, residual):
+    if weight is not None and (weight.dim() != 1 or weight.shape[0] != x.shape[-1]):
+        raise ValueError(f"weight must have one element for each of x's {x.shape[-1]} columns, not {list(weight.shape)}")
+    if residual is not None and residual.shape != x.shape:
+        raise ValueError(f"residual must have x's shape {list(x.shape)}, not {list(residual.shape)}")
+
+
+def _fold(t):
+    return t if t is None or t.dim() == 2 else t.reshape(t.shape[:-1].numel(), t.shape[-1])
+
+
+def rms_norm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-6):
+    """y = h weight / sqrt(mean(h^2) + eps) over the last dimension, with h = x or, where there is a residual, h = x + residual (in the residual's type); then (y, h) is
+    returned, h being the residual of what follows.  BF16 or FP32.  Differentiable once."""
+    _check_norm(x, weight, residual)
+    y, h = _RMSNormFn.apply(_fold(x), weight, _fold(residual), float(eps))
+    return y.reshape(x.shape) if residual is None else (y.reshape(x.shape), h.reshape(x.shape))
+
+
+class _FP8LinearFn(torch.autograd.Function):
+    """The linear layer in 8 bits with a scale for every block of 128, behind a norm or on its own (norm: weight and eps, or None)."""
+    @staticmethod
+    def forward(ctx, x, weight, norm_weight, residual, eps, ws):
+        keep_x, keep_w = ctx.needs_input_grad[1], any(ctx.needs_input_grad[i] for i in (0, 2, 3))
+        xr = _rows(x)
+        T, K = x.shape
+        h = rstd = None
+        if eps is None:
+            qx = binding.fp4q_fp8_quantize(xr, want_t=keep_x)
+        else:
+            rr = None if residual is None else _rows(residual)
+            n = binding.fp4q_rms_norm(xr, _weight(norm_weight), rr, eps=eps, y=keep_x, q=binding.Q_FP8, rstd=True)
+            qx = binding.Fp8Tensor(T, K, n.q, n.scale)
+            h, rstd = xr if rr is None else n.h, n.rstd
+            if keep_x:   # the weight gradient's operand: the norm's output along the tokens
+                t = binding.fp4q_fp8_quantize(n.y, want=False)
+                qx.q_t, qx.scale_t = t.q_t, t.scale_t
+        qw = binding.fp4q_fp8_quantize(_rows(weight), square=True, want_t=keep_w)
+        y = binding.fp4q_fp8_gemm_fwd(qx, qw, ws=ws)
+        ctx.save_for_backward(qx.q_t, qx.scale_t, qw.q_t, qw.scale, h, rstd, norm_weight)
+        ctx.sizes, ctx.ws = (T, K, weight.shape[0]), ws
+        ctx.types = x.dtype, weight.dtype, None if residual is None else residual.dtype
+        return y.contiguous(), None if residual is None else _cast(h, residual.dtype).contiguous()
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh):
+        xt, xts, wt, ws, h, rstd, norm_weight = ctx.saved_tensors
+        (T, K, N), need = ctx.sizes, ctx.needs_input_grad
+        inputs = need[0] or need[2] or need[3]
+        qd = binding.fp4q_fp8_quantize(_rows(dy), want=inputs, want_t=need[1]) if inputs or need[1] else None
+        dx = dw = dn = None
+        if need[1]:
+            dw = _cast(binding.fp4q_fp8_gemm_wgrad(qd, binding.Fp8Tensor(T, K, None, None, xt, xts), ws=ctx.ws), ctx.types[1])
+        if inputs:
+            wide = binding.OUT_F32 if rstd is None and ctx.types[0] != torch.bfloat16 else binding.OUT_BF16
+            dx = binding.fp4q_fp8_gemm_dgrad(qd, binding.Fp8Tensor(N, K, None, ws, wt, None, True), dt=wide, ws=ctx.ws)
+            if rstd is not None:
+                dx, dn = _norm_backward(dx, dh, h, rstd, norm_weight, need[2])
+        return _cast(dx, ctx.types[0]) if need[0] else None, dw, dn, _cast(dx, ctx.types[2]) if need[3] else None, None, None
+
+
+def _check_linear(x, weight):
+    if x.dim() < 1 or weight.dim() != 2 or x.shape[-1] != weight.shape[1]:
+        raise ValueError(f"x must be [..., K] and weight [N, K], not {list(x.shape)} and {list(weight.shape)}")
+
+
+def fp8_linear(x: torch.Tensor, weight: torch.Tensor, ws=None) -> torch.Tensor:
+    """y = x^ weight^^T with products in 8 bits, forward and backward: E4M3 codes with a scale for every 128 elements of a row of x and of the gradient, and for 128 x 128 of the
+    weight.  x [..., K], weight [N, K], BF16 or FP32.  y is BF16.  Straight-through; differentiable once."""
+    _check_linear(x, weight)
+    if ws is None:
+        ws = binding.alloc_workspace(x.device)
+    return _FP8LinearFn.apply(_fold(x), weight, None, None, None, ws)[0].reshape(*x.shape[:-1], weight.shape[0])
+
+
+def rms_norm_fp8_linear(x: torch.Tensor, norm_weight, weight: torch.Tensor, residual=None, eps: float = 1e-6, ws=None):
+    """fp8_linear(rms_norm(x, norm_weight, residual)), the norm writing the product's operand itself.  Several projections of one input are one with their weights above
+    each other.  Returns y or, with a residual, (y, h)."""
+    _check_linear(x, weight)
+    _check_norm(x, norm_weight, residual)
+    if ws is None:
+        ws = binding.alloc_workspace(x.device)
+    y, h = _FP8LinearFn.apply(_fold(x), weight, norm_weight, _fold(residual), float(eps), ws)
+    y = y.reshape(*x.shape[:-1], weight.shape[0])
+    return y if residual is None else (y, h.reshape(x.shape))
+
+
+def clip_grad_norm_(parameters, max_norm: float, eps: float = 1e-6) -> torch.Tensor:
+    """Scales the gradients of the parameters (one tensor, or any of them) in place so that the norm of all of them together is at most max_norm.  Returns the norm before, a number on
+    the device.  BF16 and FP32, on one device."""
+    grads = [p.grad for p in ([parameters] if isinstance(parameters, torch.Tensor) else parameters) if p.grad is not None]
+    return binding.fp4q_clip_grad_norm(grads, max_norm, eps=eps) if grads else torch.zeros(())
+
+
 class FP4Linear(torch.nn.Module):
     """Bias-free linear layer with an FP32 master weight and FP4 products.  Each backward pass draws fresh
     stochastic-rounding bits: the module counts its forward calls and uses the count as the Philox tensor id's

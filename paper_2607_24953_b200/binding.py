@@ -22,6 +22,7 @@ ROUND_NEAREST = 0
 ROUND_STOCHASTIC = 1
 OUT_BF16 = 0
 OUT_F32 = 1
+Q_NONE, Q_MXFP8, Q_FP8 = 0, 1, 2   # fp4q_rms_norm's 8-bit output: none, MXFP8, or a scale for every block of 128
 INDEX_TRANSPOSED = 1
 BLOCK_16 = 2   # fp4q_quantize2d flags: 16 x 16 or 64 x 64 blocks instead of 32 x 32 (block-size study)
 BLOCK_64 = 4
@@ -33,7 +34,9 @@ EXPORTS = ["fp4q_quantize2d", "fp4q_gemm_fwd", "fp4q_gemm_dgrad", "fp4q_gemm_wgr
            "fp4q_mxfp8_quantize1d_t", "fp4q_mxfp8_gemm", "fp4q_gemm_fwd_quantized", "fp4q_gemm_dgrad_quantized",
            "fp4q_gemm_fwd_b16", "fp4q_gemm_dgrad_b16", "fp4q_gemm_wgrad_b16", "fp4q_quantize2d_multi",
            "fp4q_quantize2d_multi_f32", "fp4q_ragged_gemm_fwd", "fp4q_ragged_gemm_dgrad", "fp4q_ragged_gemm_wgrad",
-           "fp4q_ragged_gemm_wgrad_scratch_bytes", "fp4q_newton_schulz", "fp4q_newton_schulz_scratch_bytes"]
+           "fp4q_ragged_gemm_wgrad_scratch_bytes", "fp4q_newton_schulz", "fp4q_newton_schulz_scratch_bytes",
+           "fp4q_fp8_quantize", "fp4q_fp8_gemm_fwd", "fp4q_fp8_gemm_dgrad", "fp4q_fp8_gemm_wgrad", "fp4q_rms_norm", "fp4q_rms_norm_bwd",
+           "fp4q_rms_norm_bwd_scratch_bytes", "fp4q_global_norm", "fp4q_global_norm_scratch_bytes", "fp4q_clip_by_norm"]
 
 
 class Fp4qError(RuntimeError):
@@ -56,6 +59,28 @@ class _CQuantJob(ctypes.Structure):
 
 class _CGroups(ctypes.Structure):
     _fields_ = [("n_groups", ctypes.c_int32), ("row_alignment", ctypes.c_int32), ("row_offsets", ctypes.c_void_p)]
+
+
+class _CFp8Tensor(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("q", ctypes.c_void_p), ("ld_q", ctypes.c_int64), ("scale", ctypes.c_void_p), ("ld_s", ctypes.c_int64),
+                ("q_t", ctypes.c_void_p), ("ld_t", ctypes.c_int64), ("scale_t", ctypes.c_void_p), ("ld_st", ctypes.c_int64), ("square", ctypes.c_int32)]
+
+
+class _CNorm(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("ld_x", ctypes.c_int64), ("x_type", ctypes.c_int), ("residual", ctypes.c_void_p), ("ld_residual", ctypes.c_int64),
+                ("h", ctypes.c_void_p), ("ld_h", ctypes.c_int64), ("h_type", ctypes.c_int), ("weight", ctypes.c_void_p), ("weight_type", ctypes.c_int),
+                ("eps", ctypes.c_float), ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64), ("y_type", ctypes.c_int), ("q", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
+                ("scale", ctypes.c_void_p), ("ld_s", ctypes.c_int64), ("q_format", ctypes.c_int32), ("rstd", ctypes.c_void_p)]
+
+
+class _CNormGrad(ctypes.Structure):
+    _fields_ = [("dy", ctypes.c_void_p), ("ld_dy", ctypes.c_int64), ("dy_type", ctypes.c_int), ("h", ctypes.c_void_p), ("ld_h", ctypes.c_int64), ("h_type", ctypes.c_int),
+                ("rstd", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("weight_type", ctypes.c_int), ("dh", ctypes.c_void_p), ("ld_dh", ctypes.c_int64),
+                ("dx", ctypes.c_void_p), ("ld_dx", ctypes.c_int64), ("dweight", ctypes.c_void_p), ("accumulate", ctypes.c_int32)]
+
+
+class _CSpan(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("type", ctypes.c_int)]
 
 
 _lib = None
@@ -143,6 +168,27 @@ def lib() -> ctypes.CDLL:
         L.fp4q_newton_schulz.restype = ci
         L.fp4q_newton_schulz.argtypes = [vp, ci, i64, i64, i64, i64, vp, i64, ctypes.c_float, ci, ctypes.POINTER(ctypes.c_float), ctypes.c_int32, ctypes.c_float,
                                          ctypes.c_float, vp, i64, vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp]
+        sz, fp8 = ctypes.c_size_t, ctypes.POINTER(_CFp8Tensor)
+        L.fp4q_fp8_quantize.restype = ci
+        L.fp4q_fp8_quantize.argtypes = [vp, ci, i64, i64, i64, fp8, vp]
+        for f in (L.fp4q_fp8_gemm_fwd, L.fp4q_fp8_gemm_dgrad):
+            f.restype = ci
+            f.argtypes = [fp8, fp8, vp, i64, ci, vp, sz, vp]
+        L.fp4q_fp8_gemm_wgrad.restype = ci
+        L.fp4q_fp8_gemm_wgrad.argtypes = [fp8, fp8, vp, i64, ci, ci, vp, sz, vp]
+        L.fp4q_rms_norm.restype = ci
+        L.fp4q_rms_norm.argtypes = [ctypes.POINTER(_CNorm), i64, i64, vp]
+        L.fp4q_rms_norm_bwd.restype = ci
+        L.fp4q_rms_norm_bwd.argtypes = [ctypes.POINTER(_CNormGrad), i64, i64, vp, sz, vp]
+        L.fp4q_rms_norm_bwd_scratch_bytes.restype = sz
+        L.fp4q_rms_norm_bwd_scratch_bytes.argtypes = [i64, i64]
+        spans = ctypes.POINTER(_CSpan)
+        L.fp4q_global_norm.restype = ci
+        L.fp4q_global_norm.argtypes = [spans, ctypes.c_int32, vp, vp, sz, vp]
+        L.fp4q_global_norm_scratch_bytes.restype = sz
+        L.fp4q_global_norm_scratch_bytes.argtypes = [spans, ctypes.c_int32]
+        L.fp4q_clip_by_norm.restype = ci
+        L.fp4q_clip_by_norm.argtypes = [spans, spans, ctypes.c_int32, vp, ctypes.c_float, ctypes.c_float, vp]
         _lib = L
     return _lib
 
@@ -184,6 +230,28 @@ class QTensor:
                         self.scale.data_ptr(), self.scale.stride(0))
 
 
+@dataclass
+class Fp8Tensor:
+    """An 8-bit tensor with a scale for every block of 128 (fp4q_fp8_tensor of include/fp4q.h): 1D blocks, or square ones under one set of scales."""
+    rows: int
+    cols: int
+    q: Optional[torch.Tensor]                # uint8 [rows, ld_q]: E4M3 codes
+    scale: Optional[torch.Tensor]            # FP32 [rows, ceil(cols/128)]; square: [ceil(rows/128), ceil(cols/128)]
+    q_t: Optional[torch.Tensor] = None       # uint8 [cols, ld_t]: codes of the transpose
+    scale_t: Optional[torch.Tensor] = None   # FP32 [cols, ceil(rows/128)]; square: None
+    square: bool = False
+
+
+@dataclass
+class NormOut:
+    """What fp4q_rms_norm writes; None is not written."""
+    h: Optional[torch.Tensor] = None         # x + residual, where there is a residual
+    y: Optional[torch.Tensor] = None         # BF16 or FP32 [rows, cols]
+    q: Optional[torch.Tensor] = None         # uint8 [rows, ld_q]: E4M3 codes
+    scale: Optional[torch.Tensor] = None     # MXFP8: uint8 [rows, ceil(cols/32)]; blocks of 128: FP32 [rows, ceil(cols/128)]
+    rstd: Optional[torch.Tensor] = None      # FP32 [rows]
+
+
 def _pad16(n: int) -> int:
     return (n + 15) // 16 * 16
 
@@ -215,7 +283,7 @@ def _host():
             from . import _host as module
         except ImportError as exc:
             raise ImportError("%s does not load (%s); if it was built for another Python or torch, %s" % (path, exc, hint)) from exc
-        module.init({name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in EXPORTS}, QTensor, _check)
+        module.init({name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in EXPORTS}, QTensor, _check, Fp8Tensor, NormOut)
         _native = module
     return _native
 
@@ -417,3 +485,80 @@ def fp4q_newton_schulz(g: torch.Tensor, momentum=None, beta: float = 0.95, neste
     g's shape, updated in place) M = beta M + G and U = beta M + G (nesterov) or M, without one U = G; X = U / (|U| + eps), then one step
     X = a X + (b A + c A A) X, A = X X^T, per triple of coefficients.  Returns scale X in BF16."""
     return _host().newton_schulz(g, momentum, beta, nesterov, coefficients, eps, scale, out, scratch, ws, _handle(stream))
+
+
+def alloc_fp8tensor(rows: int, cols: int, device, square: bool = False, want: bool = True, want_t: bool = True) -> Fp8Tensor:
+    """Buffers for fp4q_fp8_quantize."""
+    blocks = lambda n: (n + 127) // 128  # noqa: E731
+    scales = lambda r, c: torch.empty((r, max(blocks(c), 1)), dtype=torch.float32, device=device)  # noqa: E731
+    codes = lambda r, c: torch.empty((r, max(_pad16(c), 16)), dtype=torch.uint8, device=device)  # noqa: E731
+    return Fp8Tensor(rows, cols, codes(rows, cols) if want else None, scales(blocks(rows), cols) if square else scales(rows, cols) if want else None,
+                     codes(cols, rows) if want_t else None, scales(cols, rows) if want_t and not square else None, square)
+
+
+def fp4q_fp8_quantize(x: torch.Tensor, out: Optional[Fp8Tensor] = None, square: bool = False, want: bool = True, want_t: bool = True, stream=None) -> Fp8Tensor:
+    """x, BF16 or FP32 [rows, cols] with contiguous rows, as E4M3 codes with an FP32 scale for every 128 elements of a row (and, in the codes of the transpose, of
+    a column) or, square, for 128 x 128.  want, want_t: the row-major codes and those of the transpose."""
+    return _host().fp8_quantize(x, out, square, want, want_t, _handle(stream))
+
+
+def fp4q_fp8_gemm_fwd(X: Fp8Tensor, W: Fp8Tensor, out=None, dt: int = OUT_BF16, ws=None, stream=None) -> torch.Tensor:
+    """Y[T,N] = X^ W^^T: X in 1D blocks, W in square ones."""
+    return _host().fp8_gemm(_FWD, X, W, out, dt, False, ws, _handle(stream))
+
+
+def fp4q_fp8_gemm_dgrad(dY: Fp8Tensor, W: Fp8Tensor, out=None, dt: int = OUT_BF16, ws=None, stream=None) -> torch.Tensor:
+    """dX[T,K] = dY^ W^: reads dY.q (1D blocks) and W.q_t (square ones)."""
+    return _host().fp8_gemm(_DGRAD, dY, W, out, dt, False, ws, _handle(stream))
+
+
+def fp4q_fp8_gemm_wgrad(dY: Fp8Tensor, X: Fp8Tensor, out=None, dt: int = OUT_F32, accumulate: bool = False, ws=None, stream=None) -> torch.Tensor:
+    """dW[N,K] (+)= dY^^T X^: reads dY.q_t and X.q_t (1D blocks along the tokens)."""
+    return _host().fp8_gemm(_WGRAD, dY, X, out, dt, accumulate, ws, _handle(stream))
+
+
+def alloc_norm(x: torch.Tensor, residual=None, y: bool = True, q: int = Q_NONE, rstd: bool = False, stream=None) -> NormOut:
+    """Buffers for fp4q_rms_norm."""
+    return _host().alloc_norm(x, residual, y, q, rstd, _handle(stream))
+
+
+def fp4q_rms_norm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-6, y: bool = True, q: int = Q_NONE, rstd: bool = False, out: Optional[NormOut] = None,
+                  stream=None) -> NormOut:
+    """h = x + residual (rounded to the residual's type; without one h = x), y = h weight / sqrt(mean(h^2) + eps) over the rows of x [rows, cols].  y in BF16, and/or as 8-bit
+    operand: Q_MXFP8 for fp4q_mxfp8_qk and fp4q_mxfp8_gemm, Q_FP8 for fp4q_fp8_gemm_fwd.  rstd: 1 / sqrt(...), which fp4q_rms_norm_bwd reads.  out: buffers to fill, which
+    then say what is written; out.h may be the residual itself."""
+    return _host().rms_norm(x, weight, residual, eps, y, q, rstd, out, _handle(stream))
+
+
+def alloc_rms_norm_scratch(rows: int, cols: int, device) -> torch.Tensor:
+    """Scratch memory of fp4q_rms_norm_bwd; calls that share it must not overlap on the GPU."""
+    return torch.empty(int(lib().fp4q_rms_norm_bwd_scratch_bytes(rows, cols)), dtype=torch.uint8, device=device)
+
+
+def fp4q_rms_norm_bwd(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight=None, dh=None, out=None, dweight=None, want_dweight: bool = True,
+                      accumulate: bool = False, scratch=None, stream=None):
+    """(dx, dweight): the gradient of x and of the residual, in h's type, and that of the weight, FP32.  dh: the gradient that arrives at h by itself; accumulate: adds to
+    dweight."""
+    return _host().rms_norm_bwd(dy, h, rstd, weight, dh, out, dweight, want_dweight, accumulate, scratch, _handle(stream))
+
+
+def alloc_global_norm_scratch(tensors) -> torch.Tensor:
+    """Scratch memory of fp4q_global_norm and fp4q_clip_grad_norm for as many tensors; calls that share it must not overlap on the GPU."""
+    n = len(tensors)
+    return torch.empty(int(lib().fp4q_global_norm_scratch_bytes((_CSpan * max(n, 1))(), n)), dtype=torch.uint8, device=tensors[0].device)
+
+
+def fp4q_global_norm(tensors, norm=None, scratch=None, stream=None) -> torch.Tensor:
+    """The square root of the sum of squares of all elements of the tensors (BF16 or FP32, on one device), one FP32 number on the device."""
+    return _host().global_norm(tensors, norm, scratch, _handle(stream))
+
+
+def fp4q_clip_by_norm(tensors, norm: torch.Tensor, max_norm: float, outs=None, eps: float = 1e-6, stream=None):
+    """Every tensor times min(1, max_norm / (norm + eps)), in place or into its entry of `outs` (BF16 or FP32).  With gradients that are spread over several processes,
+    norm is the square root of the sum of their squared norms."""
+    return _host().clip_by_norm(tensors, norm, max_norm, outs, eps, _handle(stream))
+
+
+def fp4q_clip_grad_norm(tensors, max_norm: float, outs=None, eps: float = 1e-6, norm=None, scratch=None, stream=None) -> torch.Tensor:
+    """fp4q_global_norm and fp4q_clip_by_norm by one call.  Returns the norm before clipping."""
+    return _host().clip_grad_norm(tensors, max_norm, outs, eps, norm, scratch, _handle(stream))

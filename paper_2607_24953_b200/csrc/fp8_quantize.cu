@@ -1,0 +1,166 @@
+// fp4q_fp8_quantize: BF16 or FP32 -> E4M3 codes with an FP32 scale for every block of 128, both orientations in one reading.
+//
+// A CTA of 8 warps owns 128 x 128 elements: one block of every row, one of every column, one square block.  A warp has 16 rows, a lane 4 consecutive rows x 16
+// columns, so that eight lanes make a row's block and a lane's four rows a word of the transposed codes; those cross 16 KB of shared memory
+// (pieces of 16 bytes, swizzled by the column's group) and leave as 128 consecutive bytes a column.  Bound by memory: 2 or 4 bytes an element are read, 1 or 2 written.
+#include "common.cuh"
+#include "fp8_format.cuh"
+#include "row_io.cuh"
+
+using namespace fp4q;
+
+namespace {
+
+struct Fp8QuantParams {
+    int64_t rows, cols;
+    RowsOf<__nv_bfloat16> b16;   // x as what it is
+    RowsOf<float> f32;
+    fp4q_fp8_tensor out;
+    int64_t col_tiles;
+};
+
+template <typename T>
+__device__ __forceinline__ const RowsOf<T> &source(const Fp8QuantParams &p)
+{
+    if constexpr (sizeof(T) == 4) return p.f32;
+    else return p.b16;
+}
+
+template <typename T, bool SQUARE>
+__global__ void __launch_bounds__(256) fp8_quantize_kernel(const __grid_constant__ Fp8QuantParams p)
+{
+    wait_for_predecessor();
+    admit_successor();
+    __shared__ uint4 stage[128 * 8];      // 128 columns x 128 bytes
+    __shared__ float tops[8][128], factors[128];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cg = lane & 7, rg = lane >> 3;
+    const int64_t by = blockIdx.x / p.col_tiles, bx = blockIdx.x - by * p.col_tiles;
+    const int64_t row0 = by * 128 + warp * 16 + rg * 4, col0 = bx * 128 + cg * 16;
+
+    Raw16<T> x[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) x[i] = load_row16<T>(source<T>(p), row0 + i < p.rows ? row0 + i : 0, row0 + i < p.rows ? col0 : p.cols, p.cols);
+
+    float row_top[4], all = 0.f;   // infinity where there is one; NaN does not count
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        float m = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; e++) m = fmaxf(m, fabsf(x[i][e]));
+        row_top[i] = m;
+        all = fmaxf(all, m);
+    }
+    const bool careful = __syncthreads_or(is_infinite(all));   // maxima of finite elements only
+    if (careful) {
+        all = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            float m = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; e++) m = fmaxf(m, finite_size(x[i][e]));
+            row_top[i] = m;
+            all = fmaxf(all, m);
+        }
+    }
+    if (!SQUARE) {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) row_top[i] = fmaxf(row_top[i], __shfl_xor_sync(0xFFFFFFFFu, row_top[i], d));
+        if (p.out.q_t) {
+#pragma unroll
+            for (int e = 0; e < 16; e++) {
+                float m = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; i++) m = fmaxf(m, careful ? finite_size(x[i][e]) : fabsf(x[i][e]));
+                m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
+                m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+                if (rg == (e & 3)) tops[warp][16 * cg + e] = m;
+            }
+            __syncthreads();
+            if (threadIdx.x < 128) {
+                float m = tops[0][threadIdx.x];
+#pragma unroll
+                for (int w = 1; w < 8; w++) m = fmaxf(m, tops[w][threadIdx.x]);
+                factors[threadIdx.x] = fp8_factor(m);
+                if (bx * 128 + threadIdx.x < p.cols) p.out.scale_t[(bx * 128 + threadIdx.x) * p.out.ld_st + by] = fp8_scale(m);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) all = fmaxf(all, __shfl_xor_sync(0xFFFFFFFFu, all, d));
+        if (lane == 0) tops[0][warp] = all;
+        __syncthreads();
+        all = tops[0][0];
+#pragma unroll
+        for (int w = 1; w < 8; w++) all = fmaxf(all, tops[0][w]);
+        if (threadIdx.x == 0) p.out.scale[by * p.out.ld_s + bx] = fp8_scale(all);
+    }
+    const float whole = SQUARE ? fp8_factor(all) : 0.f;
+
+    if (p.out.q) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            if (row0 + i >= p.rows) break;
+            float v[16];
+#pragma unroll
+            for (int e = 0; e < 16; e++) v[e] = x[i][e];
+            if (col0 < p.cols) *reinterpret_cast<uint4 *>(p.out.q + (row0 + i) * p.out.ld_q + col0) = fp8_codes(v, SQUARE ? whole : fp8_factor(row_top[i]), careful);
+            if (!SQUARE && cg == 0) p.out.scale[(row0 + i) * p.out.ld_s + bx] = fp8_scale(row_top[i]);
+        }
+    }
+    if (!p.out.q_t) return;
+    if (!SQUARE) __syncthreads();   // factors
+    uint32_t *words = reinterpret_cast<uint32_t *>(stage);
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+        const float f = SQUARE ? whole : factors[16 * cg + e];
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) v[i] = careful && is_infinite(x[i][e]) ? nan32() : x[i][e] * f;
+        words[(16 * cg + e) * 32 + ((warp ^ cg) << 2) + rg] = cvt_rn_e4m3x4(v[3], v[2], v[1], v[0]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const int col = (threadIdx.x >> 3) + 32 * k, piece = threadIdx.x & 7;
+        const uint4 v = stage[col * 8 + (piece ^ (col >> 4))];
+        if (bx * 128 + col < p.cols && by * 128 + piece * 16 < p.rows)
+            *reinterpret_cast<uint4 *>(p.out.q_t + (bx * 128 + col) * p.out.ld_t + by * 128 + piece * 16) = v;
+    }
+}
+
+}  // namespace
+
+extern "C" fp4q_status fp4q_fp8_quantize(const void *x, fp4q_out x_type, int64_t rows, int64_t cols, int64_t ld_x, const fp4q_fp8_tensor *out, void *stream)
+{
+    if (!out) return FP4Q_ERR_NULL;
+    if (rows < 0 || cols < 0 || out->rows != rows || out->cols != cols) return FP4Q_ERR_SHAPE;
+    if (x_type != FP4Q_OUT_BF16 && x_type != FP4Q_OUT_F32) return FP4Q_ERR_UNSUPPORTED;
+    if (out->square != 0 && out->square != 1) return FP4Q_ERR_UNSUPPORTED;
+    if (rows == 0 || cols == 0) return FP4Q_OK;
+    if (!x || (!out->q && !out->q_t)) return FP4Q_ERR_NULL;
+    const bool square = out->square != 0;
+    if ((out->q || square) && !out->scale) return FP4Q_ERR_NULL;
+    if (out->q_t && !square && !out->scale_t) return FP4Q_ERR_NULL;
+    if (ld_x < cols) return FP4Q_ERR_SHAPE;
+    if (out->q && out->ld_q < cols) return FP4Q_ERR_SHAPE;
+    if ((out->q || square) && out->ld_s < ceil_div(cols, 128)) return FP4Q_ERR_SHAPE;
+    if (out->q_t && (out->ld_t < rows || (!square && out->ld_st < ceil_div(rows, 128)))) return FP4Q_ERR_SHAPE;
+    if (!aligned(x, x_type == FP4Q_OUT_F32 ? 4 : 2) || !aligned(out->q, 16) || !aligned(out->q_t, 16) || (out->q && out->ld_q % 16 != 0) || (out->q_t && out->ld_t % 16 != 0) ||
+        !aligned(out->scale, 4) || !aligned(out->scale_t, 4))
+        return FP4Q_ERR_ALIGN;
+    Fp8QuantParams p;
+    p.rows = rows;
+    p.cols = cols;
+    p.b16 = rows_of<__nv_bfloat16>(x, rows, cols, ld_x);
+    p.f32 = rows_of<float>(x, rows, cols, ld_x);
+    p.out = *out;
+    p.col_tiles = ceil_div(cols, 128);
+    const int64_t tiles = p.col_tiles * ceil_div(rows, 128);
+    if (tiles > 0x7FFFFFFF) return FP4Q_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)tiles);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (x_type == FP4Q_OUT_F32) return launched(square ? launch_dependent(fp8_quantize_kernel<float, true>, grid, 256, s, p) : launch_dependent(fp8_quantize_kernel<float, false>, grid, 256, s, p));
+    return launched(square ? launch_dependent(fp8_quantize_kernel<__nv_bfloat16, true>, grid, 256, s, p) : launch_dependent(fp8_quantize_kernel<__nv_bfloat16, false>, grid, 256, s, p));
+}

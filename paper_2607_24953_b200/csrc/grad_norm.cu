@@ -1,0 +1,341 @@
+// fp4q_global_norm and fp4q_clip_by_norm (include/fp4q.h): the norm of all gradients of a step, and their clipping.
+//
+// Every tensor is cut into units of 8 elements, those of a row on the 16-byte grid of its memory, and chunks of 1024 units, which the CTAs take in turn; the
+// tensors' descriptions travel as kernel parameters, up to 450 a launch.  Bound by memory: the norm reads everything, the clipping reads it again, last
+// chunks first, since those are still in L2, and writes it.
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+
+#include <algorithm>
+
+using namespace fp4q;
+
+namespace {
+
+constexpr int kUnit = 8, kChunkUnits = 1024;   // four units a thread
+constexpr int kNormCtas = 148 * 6;
+constexpr int kFew = 56, kMany = 450;          // tensors of a launch: parameters of up to 4 and 32 KB
+
+struct Span {
+    void *data, *out;
+    int64_t units_row, units, cols, ld, ld_out;   // units of a row and of the tensor; a tensor without gaps is one row
+    int64_t chunk0;                               // chunks of the tensors before it
+    int32_t f32, out_f32;
+};
+template <int N>
+struct SpanParams {
+    int64_t chunks;
+    int32_t n, in_place;
+    double *partial;
+    const float *norm;
+    float max_norm, eps;
+    Span span[N];
+};
+static_assert(sizeof(SpanParams<kFew>) <= 4096 && sizeof(SpanParams<kMany>) <= 32764, "a kernel's parameters");
+
+// The tensor that a chunk belongs to: the last one that begins at or before it.
+template <int N>
+__device__ __forceinline__ int span_of(const SpanParams<N> &p, int64_t chunk)
+{
+    int lo = 0, hi = p.n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p.span[mid].chunk0 <= chunk) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// A unit: element e of its row's columns k .. k + 7 (k may begin before the row).
+struct Unit {
+    int64_t row, col;
+    bool whole;   // all eight exist; they lie on 16 bytes
+};
+__device__ __forceinline__ Unit unit_of(const Span &s, int64_t u)
+{
+    Unit r;
+    r.row = 0;
+    if (s.units != s.units_row) {
+        r.row = s.units <= 0xFFFFFFFFll ? (uint32_t)u / (uint32_t)s.units_row : u / s.units_row;
+        u -= r.row * s.units_row;
+    }
+    const uintptr_t at = reinterpret_cast<uintptr_t>(s.data) + (uintptr_t)(r.row * s.ld) * (s.f32 ? 4 : 2);
+    r.col = u * kUnit - (int64_t)((at & 15u) >> (s.f32 ? 2 : 1));
+    r.whole = r.col >= 0 && r.col + kUnit <= s.cols;
+    return r;
+}
+__device__ __forceinline__ void load_unit(const Span &s, const Unit &u, bool exists, uint32_t (&w)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++) w[i] = 0u;
+    if (!exists) return;
+    const int64_t at = u.row * s.ld + u.col;
+    if (u.whole) {
+        const uint4 *src = s.f32 ? reinterpret_cast<const uint4 *>(static_cast<const float *>(s.data) + at) : reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(s.data) + at);
+        const uint4 a = load_global(src);
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+        if (s.f32) {
+            const uint4 b = load_global(src + 1);
+            w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < kUnit; e++) {
+        if (u.col + e < 0 || u.col + e >= s.cols) continue;
+        if (s.f32) w[e] = load_global(static_cast<const uint32_t *>(s.data) + at + e);
+        else w[e >> 1] |= (uint32_t)load_global(static_cast<const uint16_t *>(s.data) + at + e) << (16 * (e & 1));
+    }
+}
+__device__ __forceinline__ float element(const Span &s, const uint32_t (&w)[8], int e)
+{
+    return s.f32 ? __uint_as_float(w[e]) : __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+}
+
+template <int N>
+__global__ void __launch_bounds__(256) sum_squares_kernel(const __grid_constant__ SpanParams<N> p)
+{
+    wait_for_predecessor();
+    admit_successor();
+    __shared__ double sums[8];
+    double total = 0.0;
+    for (int64_t chunk = blockIdx.x; chunk < p.chunks; chunk += gridDim.x) {
+        const Span &s = p.span[span_of(p, chunk)];
+        const int64_t u0 = (chunk - s.chunk0) * kChunkUnits + threadIdx.x;
+        uint32_t w[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int64_t u = u0 + 256 * k;
+            load_unit(s, unit_of(s, u), u < s.units, w[k]);
+        }
+        float run = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+            for (int e = 0; e < kUnit; e++) {
+                const float v = element(s, w[k], e);
+                run = fmaf(v, v, run);
+            }
+        // A run that is normal has lost no square that counts; another one, with squares out of FP32's range, is added up in 64 bits.
+        if (run > 1e-30f && run < 1e38f) total += (double)run;
+        else
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+#pragma unroll
+                for (int e = 0; e < kUnit; e++) {
+                    const double v = (double)element(s, w[k], e);
+                    total = fma(v, v, total);
+                }
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, d);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = total;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    total = 0.0;
+#pragma unroll
+    for (int k = 0; k < 8; k++) total += sums[k];
+    p.partial[blockIdx.x] = total;
+}
+
+struct RootParams {
+    const double *partial;
+    int64_t n;
+    float *norm;
+};
+__global__ void __launch_bounds__(256) root_kernel(const __grid_constant__ RootParams p)
+{
+    wait_for_predecessor();
+    admit_successor();
+    __shared__ double sums[8];
+    double total = 0.0;
+    for (int64_t i = threadIdx.x; i < p.n; i += 256) total += load_global(p.partial + i);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, d);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = total;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    total = 0.0;
+#pragma unroll
+    for (int k = 0; k < 8; k++) total += sums[k];
+    *p.norm = (float)sqrt(total);
+}
+
+template <int N>
+__global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ SpanParams<N> p)
+{
+    wait_for_predecessor();
+    admit_successor();
+    const float ratio = __fdiv_rn(p.max_norm, load_global(p.norm) + p.eps), factor = ratio > 1.f ? 1.f : ratio;
+    if (p.in_place && factor == 1.f) return;
+    for (int64_t back = blockIdx.x; back < p.chunks; back += gridDim.x) {
+        const int64_t chunk = p.chunks - 1 - back;
+        const Span &s = p.span[span_of(p, chunk)];
+        const int64_t u0 = (chunk - s.chunk0) * kChunkUnits + threadIdx.x;
+        uint32_t w[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int64_t u = u0 + 256 * k;
+            load_unit(s, unit_of(s, u), u < s.units, w[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int64_t u = u0 + 256 * k;
+            if (u >= s.units) continue;
+            const Unit at = unit_of(s, u);
+            float v[kUnit];
+#pragma unroll
+            for (int e = 0; e < kUnit; e++) v[e] = element(s, w[k], e) * factor;
+            const int64_t to = at.row * s.ld_out + at.col;
+            if (s.out_f32) {
+                float *o = static_cast<float *>(s.out) + to;
+                if (at.whole && (reinterpret_cast<uintptr_t>(o) & 15u) == 0u) {
+                    reinterpret_cast<float4 *>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                    reinterpret_cast<float4 *>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kUnit; e++)
+                        if (at.col + e >= 0 && at.col + e < s.cols) o[e] = v[e];
+                }
+            } else {
+                __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(s.out) + to;
+                if (at.whole && (reinterpret_cast<uintptr_t>(o) & 15u) == 0u) {
+                    uint32_t b[4];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const __nv_bfloat162 pair = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+                        b[e] = *reinterpret_cast<const uint32_t *>(&pair);
+                    }
+                    *reinterpret_cast<uint4 *>(o) = make_uint4(b[0], b[1], b[2], b[3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kUnit; e++)
+                        if (at.col + e >= 0 && at.col + e < s.cols) o[e] = __float2bfloat16_rn(v[e]);
+                }
+            }
+        }
+    }
+}
+
+fp4q_status check_span(const fp4q_span &t)
+{
+    if (t.rows < 0 || t.cols < 0) return FP4Q_ERR_SHAPE;
+    if (t.type != FP4Q_OUT_BF16 && t.type != FP4Q_OUT_F32) return FP4Q_ERR_UNSUPPORTED;
+    if (t.rows == 0 || t.cols == 0) return FP4Q_OK;
+    if (!t.data) return FP4Q_ERR_NULL;
+    if (t.rows > 1 && t.ld < t.cols) return FP4Q_ERR_SHAPE;
+    return aligned(t.data, t.type == FP4Q_OUT_F32 ? 4 : 2) ? FP4Q_OK : FP4Q_ERR_ALIGN;
+}
+fp4q_status check_spans(const fp4q_span *t, int32_t n)
+{
+    if (n < 0) return FP4Q_ERR_SHAPE;
+    if (n > 0 && !t) return FP4Q_ERR_NULL;
+    for (int32_t i = 0; i < n; i++)
+        if (fp4q_status s = check_span(t[i])) return s;
+    return FP4Q_OK;
+}
+
+// As the kernels take it.  o: the tensor that the result goes to.
+Span span_for(const fp4q_span &t, const fp4q_span &o)
+{
+    Span s = {};
+    s.data = t.data;
+    s.out = o.data;
+    s.f32 = t.type == FP4Q_OUT_F32;
+    s.out_f32 = o.type == FP4Q_OUT_F32;
+    const bool gaps = t.rows > 1 && (t.ld != t.cols || o.ld != o.cols);
+    const int64_t rows = gaps ? t.rows : 1, size = s.f32 ? 4 : 2;
+    s.cols = gaps ? t.cols : t.rows * t.cols;
+    s.ld = t.ld;
+    s.ld_out = o.ld;
+    // A row off the grid has one unit more.
+    const bool off = !aligned(t.data, 16) || (rows > 1 && t.ld * size % 16 != 0);
+    s.units_row = (s.cols + kUnit - 1 + (off ? 16 / size - 1 : 0)) / kUnit;
+    s.units = rows * s.units_row;
+    return s;
+}
+
+// The tensors from `at` on that are not empty, as many as there is room for; at: the first that is left.
+template <int N>
+int64_t take_spans(const fp4q_span *t, const fp4q_span *o, int32_t n, int32_t &at, SpanParams<N> &p)
+{
+    for (; at < n && p.n < N; at++) {
+        if (t[at].rows == 0 || t[at].cols == 0) continue;
+        Span &s = p.span[p.n++] = span_for(t[at], o[at]);
+        s.chunk0 = p.chunks;
+        p.chunks += ceil_div(s.units, kChunkUnits);
+    }
+    return std::min<int64_t>(kNormCtas, p.chunks);
+}
+
+}  // namespace
+
+extern "C" size_t fp4q_global_norm_scratch_bytes(const fp4q_span *tensors, int32_t n_tensors)
+{
+    if (n_tensors <= 0 || !tensors) return 256;
+    return (size_t)round_up(ceil_div(n_tensors, kMany) * kNormCtas * 8, 256);
+}
+
+extern "C" fp4q_status fp4q_global_norm(const fp4q_span *tensors, int32_t n_tensors, float *norm, void *scratch, size_t scratch_bytes, void *stream)
+{
+    if (fp4q_status s = check_spans(tensors, n_tensors)) return s;
+    if (!norm) return FP4Q_ERR_NULL;
+    if (!aligned(norm, 4)) return FP4Q_ERR_ALIGN;
+    if (!scratch || scratch_bytes < fp4q_global_norm_scratch_bytes(tensors, n_tensors)) return FP4Q_ERR_WORKSPACE;
+    if (!aligned(scratch, 256)) return FP4Q_ERR_ALIGN;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    double *partial = static_cast<double *>(scratch);
+    int64_t parts = 0;
+    fp4q_status st = FP4Q_OK;
+    auto launch = [&](auto &p, auto kernel, int32_t &at) {
+        p.partial = partial + parts;
+        const int64_t ctas = take_spans(tensors, tensors, n_tensors, at, p);
+        parts += ctas;
+        if (ctas) st = launched(launch_dependent(kernel, dim3((unsigned)ctas), 256, s, p));
+    };
+    for (int32_t at = 0; at < n_tensors && !st;) {
+        if (n_tensors - at <= kFew) {
+            SpanParams<kFew> p = {};
+            launch(p, sum_squares_kernel<kFew>, at);
+        } else {
+            SpanParams<kMany> p = {};
+            launch(p, sum_squares_kernel<kMany>, at);
+        }
+    }
+    if (st) return st;
+    const RootParams r = {partial, parts, norm};
+    return launched(launch_dependent(root_kernel, dim3(1), 256, s, r));
+}
+
+extern "C" fp4q_status fp4q_clip_by_norm(const fp4q_span *tensors, const fp4q_span *outs, int32_t n_tensors, const float *norm, float max_norm, float eps, void *stream)
+{
+    if (fp4q_status s = check_spans(tensors, n_tensors)) return s;
+    if (outs) {
+        if (fp4q_status s = check_spans(outs, n_tensors)) return s;
+        for (int32_t i = 0; i < n_tensors; i++)
+            if (outs[i].rows != tensors[i].rows || outs[i].cols != tensors[i].cols) return FP4Q_ERR_SHAPE;
+    }
+    if (!norm) return FP4Q_ERR_NULL;
+    if (!aligned(norm, 4)) return FP4Q_ERR_ALIGN;
+    if (!(max_norm >= 0.f) || !(eps >= 0.f)) return FP4Q_ERR_UNSUPPORTED;
+    fp4q_status st = FP4Q_OK;
+    auto launch = [&](auto &p, auto kernel, int32_t &at) {
+        p.norm = norm;
+        p.max_norm = max_norm;
+        p.eps = eps;
+        p.in_place = !outs;
+        const int64_t ctas = take_spans(tensors, outs ? outs : tensors, n_tensors, at, p);
+        if (ctas) st = launched(launch_dependent(kernel, dim3((unsigned)ctas), 256, static_cast<cudaStream_t>(stream), p));
+    };
+    for (int32_t at = 0; at < n_tensors && !st;) {
+        if (n_tensors - at <= kFew) {
+            SpanParams<kFew> p = {};
+            launch(p, scale_kernel<kFew>, at);
+        } else {
+            SpanParams<kMany> p = {};
+            launch(p, scale_kernel<kMany>, at);
+        }
+    }
+    return st;
+}

@@ -47,10 +47,20 @@ struct Entry {
     decltype(&fp4q_ragged_gemm_wgrad_scratch_bytes) ragged_gemm_wgrad_scratch_bytes;
     decltype(&fp4q_newton_schulz) newton_schulz;
     decltype(&fp4q_newton_schulz_scratch_bytes) newton_schulz_scratch_bytes;
+    decltype(&fp4q_fp8_quantize) fp8_quantize;
+    decltype(&fp4q_fp8_gemm_fwd) fp8_gemm_fwd, fp8_gemm_dgrad;
+    decltype(&fp4q_fp8_gemm_wgrad) fp8_gemm_wgrad;
+    decltype(&fp4q_rms_norm) rms_norm;
+    decltype(&fp4q_rms_norm_bwd) rms_norm_bwd;
+    decltype(&fp4q_rms_norm_bwd_scratch_bytes) rms_norm_bwd_scratch_bytes;
+    decltype(&fp4q_global_norm) global_norm;
+    decltype(&fp4q_global_norm_scratch_bytes) global_norm_scratch_bytes;
+    decltype(&fp4q_clip_by_norm) clip_by_norm;
 } lib;
 
 PyObject *g_qtensor = nullptr, *g_fail = nullptr;   // binding.QTensor; binding._check
-PyObject *s_rows, *s_cols, *s_q_rm, *s_q_t, *s_scale, *s_granularity;
+PyObject *g_fp8 = nullptr, *g_norm = nullptr;       // binding.Fp8Tensor, binding.NormOut
+PyObject *s_rows, *s_cols, *s_q_rm, *s_q_t, *s_scale, *s_granularity, *s_q, *s_scale_t, *s_square, *s_h, *s_y, *s_rstd;
 
 // A Python exception is set: unwinds to the entry point, which returns NULL.
 struct PyError {};
@@ -665,6 +675,463 @@ PyObject *newton_schulz(Args a, Py_ssize_t n)
     return ours ? THPVariable_Wrap(out) : Py_NewRef(a[7]);
 }
 
+// ---- 8-bit tensors with a scale for every block of 128, the norm, the gradients' norm and clipping
+
+double as_double(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw PyError();
+    return v;
+}
+[[noreturn]] void bad_argument(const char *name, const char *what)
+{
+    PyErr_Format(PyExc_ValueError, "%s must be %s", name, what);
+    throw PyError();
+}
+void on_cuda(const at::Tensor &t, const char *name)
+{
+    if (!t.is_cuda()) { PyErr_Format(PyExc_ValueError, "%s must live on a CUDA device (there is no CPU path)", name); throw PyError(); }
+}
+bool bf16_or_f32(const at::Tensor &t) { return t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kFloat; }
+fp4q_out type_of(const at::Tensor &t) { return t.scalar_type() == at::kFloat ? FP4Q_OUT_F32 : FP4Q_OUT_BF16; }
+// A matrix of either type with contiguous rows; rows, cols: its shape, if not -1.
+const at::Tensor &either_matrix(const at::Tensor &t, const char *name, int64_t rows = -1, int64_t cols = -1)
+{
+    on_cuda(t, name);
+    if (!bf16_or_f32(t) || t.dim() != 2 || (t.numel() && t.size(1) > 1 && t.stride(1) != 1)) bad_argument(name, "a 2-D BF16 or FP32 tensor with contiguous rows");
+    if ((rows >= 0 && t.size(0) != rows) || (cols >= 0 && t.size(1) != cols)) bad_argument(name, "of the other tensors' shape");
+    return t;
+}
+int64_t pitch_of(const at::Tensor &t) { return t.numel() && t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.size(1), 1); }
+at::Tensor attribute(PyObject *o, PyObject *name)
+{
+    Ref v(PyObject_GetAttr(o, name));
+    return v.p == Py_None ? at::Tensor() : as_tensor(v.p);
+}
+int64_t number(PyObject *o, PyObject *name)
+{
+    Ref v(PyObject_GetAttr(o, name));
+    return as_i64(v.p);
+}
+at::Tensor maybe(PyObject *o) { return o == Py_None ? at::Tensor() : as_tensor(o); }
+PyObject *wrap(const at::Tensor &t) { return t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None); }
+
+// Part of an 8-bit tensor or of a norm's output: at least [rows, cols] of one type, contiguous rows, on `like`'s device.
+void check_part(const at::Tensor &t, const char *name, at::ScalarType type, int64_t rows, int64_t cols, const at::Tensor &like)
+{
+    if (!t.defined()) return;
+    on_cuda(t, name);
+    same_device(t, like, name);
+    const bool kind = t.scalar_type() == type || (type == at::kByte && t.scalar_type() == at::kFloat8_e4m3fn);
+    if (!kind || t.dim() != 2 || t.size(0) != rows || t.size(1) < cols || (t.numel() && t.size(1) > 1 && t.stride(1) != 1)) {
+        PyErr_Format(PyExc_ValueError, "%s must be a tensor of %lld rows of at least %lld elements of its type, with contiguous rows", name, (long long)rows, (long long)cols);
+        throw PyError();
+    }
+}
+struct Fp8View {
+    fp4q_fp8_tensor t = {};
+    at::Tensor q, scale, q_t, scale_t;
+};
+Fp8View fp8_view(PyObject *o, const at::Tensor *like)
+{
+    Fp8View v;
+    v.t.rows = number(o, s_rows);
+    v.t.cols = number(o, s_cols);
+    Ref square(PyObject_GetAttr(o, s_square));
+    v.t.square = as_bool(square.p);
+    v.q = attribute(o, s_q); v.scale = attribute(o, s_scale); v.q_t = attribute(o, s_q_t); v.scale_t = attribute(o, s_scale_t);
+    const int64_t r = v.t.rows, c = v.t.cols, br = ceil_to(r, 128), bc = ceil_to(c, 128);
+    if (r < 0 || c < 0) value_error("rows and cols must not be negative");
+    const at::Tensor &first = v.q.defined() ? v.q : v.q_t;
+    if (!first.defined()) value_error("an Fp8Tensor must have q or q_t");
+    on_cuda(first, "q");
+    const at::Tensor &device = like ? *like : first;
+    check_part(v.q, "q", at::kByte, r, c, device);
+    check_part(v.scale, "scale", at::kFloat, v.t.square ? br : r, bc, device);
+    check_part(v.q_t, "q_t", at::kByte, c, r, device);
+    check_part(v.scale_t, "scale_t", at::kFloat, c, br, device);
+    auto put = [](const at::Tensor &t, auto *&p, int64_t &ld) {
+        if (!t.defined()) return;
+        p = static_cast<std::remove_reference_t<decltype(p)>>(t.data_ptr());
+        ld = pitch_of(t);
+    };
+    put(v.q, v.t.q, v.t.ld_q); put(v.scale, v.t.scale, v.t.ld_s); put(v.q_t, v.t.q_t, v.t.ld_t); put(v.scale_t, v.t.scale_t, v.t.ld_st);
+    // One row, or rows of which each is one pitch: whole 16 bytes.
+    if (v.t.rows == 1 && v.q.defined()) v.t.ld_q = pad16(v.t.ld_q);
+    if (v.t.cols == 1 && v.q_t.defined()) v.t.ld_t = pad16(v.t.ld_t);
+    return v;
+}
+// Codes that are written: `bytes` of every row, which reach behind the last row's elements.
+void check_room(const at::Tensor &t, const char *name, int64_t ld, int64_t bytes)
+{
+    if (!t.defined() || t.numel() == 0) return;
+    if ((int64_t)t.storage().nbytes() - t.storage_offset() < (t.size(0) - 1) * ld + bytes) bad_argument(name, "in rows of whole 16 bytes (MXFP8: 32), the last one included");
+}
+const at::Tensor &payload(const Fp8View &v) { return v.q.defined() ? v.q : v.q_t; }
+
+// x, out | None, square, want, want_t, stream
+PyObject *fp8_quantize(Args a, Py_ssize_t n)
+{
+    want(n, 6);
+    const at::Tensor &x = either_matrix(as_tensor(a[0]), "x");
+    const c10::cuda::CUDAGuard device(x.device());
+    const OnStream on(a[5], &x);
+    const int64_t rows = x.size(0), cols = x.size(1);
+    Ref out(Py_NewRef(a[1]));
+    if (a[1] == Py_None) {
+        const bool square = as_bool(a[2]), want_q = as_bool(a[3]), want_t = as_bool(a[4]);
+        at::Tensor q, scale, q_t, scale_t;
+        if (want_q) q = empty2(rows, std::max<int64_t>(pad16(cols), 16), at::kByte, x);
+        if (want_q || square) scale = empty2(square ? ceil_to(rows, 128) : rows, std::max<int64_t>(ceil_to(cols, 128), 1), at::kFloat, x);
+        if (want_t) q_t = empty2(cols, std::max<int64_t>(pad16(rows), 16), at::kByte, x);
+        if (want_t && !square) scale_t = empty2(cols, std::max<int64_t>(ceil_to(rows, 128), 1), at::kFloat, x);
+        for (const at::Tensor *t : {&q, &scale, &q_t, &scale_t}) on.returned(*t);
+        Ref r(PyLong_FromLongLong(rows)), c(PyLong_FromLongLong(cols)), w0(wrap(q)), w1(wrap(scale)), w2(wrap(q_t)), w3(wrap(scale_t)), sq(PyBool_FromLong(square));
+        PyObject *args[7] = {r.p, c.p, w0.p, w1.p, w2.p, w3.p, sq.p};
+        PyObject *made = PyObject_Vectorcall(g_fp8, args, 7, nullptr);
+        if (!made) throw PyError();
+        Py_SETREF(out.p, made);
+        if (!want_q && !want_t) value_error("one of want and want_t must be true");
+    }
+    const Fp8View v = fp8_view(out.p, &x);
+    if (a[1] != Py_None && (v.t.square != 0) != as_bool(a[2])) value_error("out must have the blocks that the call asks for");
+    check_room(v.q, "q", v.t.ld_q, pad16(cols));
+    check_room(v.q_t, "q_t", v.t.ld_t, pad16(rows));
+    check(unlocked(lib.fp8_quantize, x.data_ptr(), type_of(x), rows, cols, pitch_of(x), &v.t, on.handle), "fp4q_fp8_quantize");
+    return Py_NewRef(out.p);
+}
+
+// which (0 forward, 1 input gradient, 2 weight gradient), operands, out | None, dt, accumulate, ws | None, stream
+PyObject *fp8_gemm(Args a, Py_ssize_t n)
+{
+    want(n, 8);
+    static const char *const names[3] = {"fp4q_fp8_gemm_fwd", "fp4q_fp8_gemm_dgrad", "fp4q_fp8_gemm_wgrad"};
+    const int which = as_int(a[0]), dt = as_int(a[4]);
+    const Fp8View x = fp8_view(a[1], nullptr), y = fp8_view(a[2], &payload(x));
+    const at::Tensor &like = payload(x);
+    const c10::cuda::CUDAGuard device(like.device());
+    const OnStream on(a[7], &like);
+    const int64_t rows = which == 2 ? x.t.cols : x.t.rows, cols = which == 0 ? y.t.rows : y.t.cols;
+    const int accumulate = as_bool(a[5]) ? 1 : 0;
+    const bool ours = a[3] == Py_None;
+    if (dt != FP4Q_OUT_BF16 && dt != FP4Q_OUT_F32) value_error("dt must be OUT_BF16 or OUT_F32");
+    const at::Tensor out = ours ? out_buffer(on, rows, cols, dt, like) : as_tensor(a[3]);
+    if (ours && accumulate) { Unlock u; out.zero_(); }
+    if (!ours) {
+        on_cuda(out, "out");
+        same_device(out, like, "out");
+        if (out.scalar_type() != (dt == FP4Q_OUT_BF16 ? at::kBFloat16 : at::kFloat) || out.dim() != 2 || out.size(0) != rows || out.size(1) != cols ||
+            (out.numel() && out.stride(1) != 1 && cols > 1))
+            value_error("out must be a 2-D tensor of the result's shape and of the type that dt names, with contiguous rows");
+    }
+    const at::Tensor ws = workspace(a[6], like);
+    const int64_t ld = out_pitch(out, cols);
+    const fp4q_out type = out_type(dt, ours);
+    const fp4q_status s = which == 2 ? unlocked(lib.fp8_gemm_wgrad, &x.t, &y.t, out.data_ptr(), ld, type, accumulate, ws.data_ptr(), (size_t)ws.numel(), on.handle)
+                                     : unlocked(which == 1 ? lib.fp8_gemm_dgrad : lib.fp8_gemm_fwd, &x.t, &y.t, out.data_ptr(), ld, type, ws.data_ptr(), (size_t)ws.numel(), on.handle);
+    check(s, names[which]);
+    return ours ? THPVariable_Wrap(out) : Py_NewRef(a[3]);
+}
+
+// The norm's weight: [cols], or none.
+void check_weight(const at::Tensor &w, int64_t cols, const at::Tensor &like)
+{
+    if (!w.defined()) return;
+    on_cuda(w, "weight");
+    same_device(w, like, "weight");
+    if (!bf16_or_f32(w) || w.dim() != 1 || w.size(0) != cols || !w.is_contiguous()) value_error("weight must be a contiguous BF16 or FP32 tensor with an element for every column");
+}
+// A row of `cols` in a buffer of whole 16 bytes.
+at::Tensor padded(const OnStream &on, int64_t rows, int64_t cols, at::ScalarType type, const at::Tensor &like)
+{
+    return out_buffer(on, rows, cols, type == at::kFloat ? FP4Q_OUT_F32 : FP4Q_OUT_BF16, like);
+}
+PyObject *new_norm(const OnStream &on, const at::Tensor &x, const at::Tensor &residual, bool want_y, int format, bool want_rstd)
+{
+    const int64_t rows = x.size(0), cols = x.size(1);
+    if (format != 0 && format != FP4Q_NORM_MXFP8 && format != FP4Q_NORM_FP8) value_error("q must be Q_NONE, Q_MXFP8 or Q_FP8");
+    at::Tensor h, y, q, scale, rstd;
+    if (residual.defined()) h = padded(on, rows, cols, residual.scalar_type(), x);
+    if (want_y) y = padded(on, rows, cols, at::kBFloat16, x);
+    if (format) {
+        const int64_t b = format == FP4Q_NORM_MXFP8 ? 32 : 128;
+        q = on.returned(empty2(rows, std::max<int64_t>(format == FP4Q_NORM_MXFP8 ? ceil_to(cols, 32) * 32 : pad16(cols), 16), at::kByte, x));
+        scale = on.returned(empty2(rows, std::max<int64_t>(ceil_to(cols, b), 1), format == FP4Q_NORM_MXFP8 ? at::kByte : at::kFloat, x));
+    }
+    if (want_rstd) {
+        Unlock u;
+        rstd = on.returned(at::empty({rows}, at::TensorOptions().dtype(at::kFloat).device(x.device())));
+    }
+    Ref w0(wrap(h)), w1(wrap(y)), w2(wrap(q)), w3(wrap(scale)), w4(wrap(rstd));
+    PyObject *args[5] = {w0.p, w1.p, w2.p, w3.p, w4.p};
+    PyObject *made = PyObject_Vectorcall(g_norm, args, 5, nullptr);
+    if (!made) throw PyError();
+    return made;
+}
+const at::Tensor &norm_input(PyObject *o) { return either_matrix(as_tensor(o), "x"); }
+at::Tensor norm_residual(PyObject *o, const at::Tensor &x)
+{
+    const at::Tensor r = maybe(o);
+    if (r.defined()) {
+        either_matrix(r, "residual", x.size(0), x.size(1));
+        same_device(r, x, "residual");
+    }
+    return r;
+}
+// x, residual | None, y, q, rstd, stream
+PyObject *alloc_norm(Args a, Py_ssize_t n)
+{
+    want(n, 6);
+    const at::Tensor &x = norm_input(a[0]);
+    const c10::cuda::CUDAGuard device(x.device());
+    const OnStream on(a[5], &x);
+    return new_norm(on, x, norm_residual(a[1], x), as_bool(a[2]), as_int(a[3]), as_bool(a[4]));
+}
+// x, weight | None, residual | None, eps, y, q, rstd, out | None, stream
+PyObject *rms_norm(Args a, Py_ssize_t n)
+{
+    want(n, 9);
+    const at::Tensor &x = norm_input(a[0]);
+    const c10::cuda::CUDAGuard device(x.device());
+    const OnStream on(a[8], &x);
+    const at::Tensor w = maybe(a[1]), residual = norm_residual(a[2], x);
+    const int64_t rows = x.size(0), cols = x.size(1);
+    check_weight(w, cols, x);
+    Ref out(a[7] == Py_None ? new_norm(on, x, residual, as_bool(a[4]), as_int(a[5]), as_bool(a[6])) : Py_NewRef(a[7]));
+    const at::Tensor h = attribute(out.p, s_h), y = attribute(out.p, s_y), q = attribute(out.p, s_q), scale = attribute(out.p, s_scale), rstd = attribute(out.p, s_rstd);
+    fp4q_norm p = {};
+    p.x = x.data_ptr(); p.ld_x = pitch_of(x); p.x_type = type_of(x);
+    if (residual.defined()) {
+        if (!h.defined()) value_error("out.h must take the sum where there is a residual");
+        check_part(h, "out.h", residual.scalar_type(), rows, cols, x);
+        if (h.size(1) != cols) bad_argument("out.h", "of x's shape");
+        p.residual = residual.data_ptr(); p.ld_residual = pitch_of(residual); p.h_type = type_of(residual);
+        p.h = h.data_ptr(); p.ld_h = pitch_of(h);
+    }
+    if (w.defined()) { p.weight = w.data_ptr(); p.weight_type = type_of(w); }
+    p.eps = (float)as_double(a[3]);
+    if (y.defined()) {
+        either_matrix(y, "out.y", rows, cols);
+        same_device(y, x, "out.y");
+        p.y = y.data_ptr(); p.ld_y = pitch_of(y); p.y_type = type_of(y);
+    }
+    if (q.defined()) {
+        if (!scale.defined()) value_error("out.scale must be there where out.q is");
+        const bool mx = scale.scalar_type() == at::kByte;
+        check_part(q, "out.q", at::kByte, rows, mx ? ceil_to(cols, 32) * 32 : cols, x);
+        check_part(scale, "out.scale", mx ? at::kByte : at::kFloat, rows, ceil_to(cols, mx ? 32 : 128), x);
+        p.q = static_cast<uint8_t *>(q.data_ptr()); p.ld_q = rows == 1 ? pad16(pitch_of(q)) : pitch_of(q);
+        check_room(q, "out.q", p.ld_q, mx ? ceil_to(cols, 32) * 32 : pad16(cols));
+        p.scale = scale.data_ptr(); p.ld_s = pitch_of(scale);
+        p.q_format = mx ? FP4Q_NORM_MXFP8 : FP4Q_NORM_FP8;
+    }
+    if (rstd.defined()) {
+        on_cuda(rstd, "out.rstd");
+        same_device(rstd, x, "out.rstd");
+        if (rstd.scalar_type() != at::kFloat || rstd.dim() != 1 || rstd.size(0) != rows || !rstd.is_contiguous()) bad_argument("out.rstd", "a contiguous FP32 tensor with an element for every row");
+        p.rstd = static_cast<float *>(rstd.data_ptr());
+    }
+    check(unlocked(lib.rms_norm, &p, rows, cols, on.handle), "fp4q_rms_norm");
+    return Py_NewRef(out.p);
+}
+
+// dy, h, rstd, weight | None, dh | None, out | None, dweight | None, want_dweight, accumulate, scratch | None, stream
+PyObject *rms_norm_bwd(Args a, Py_ssize_t n)
+{
+    want(n, 11);
+    const at::Tensor &h = either_matrix(as_tensor(a[1]), "h");
+    const int64_t rows = h.size(0), cols = h.size(1);
+    const at::Tensor &dy = either_matrix(as_tensor(a[0]), "dy", rows, cols), &rstd = as_tensor(a[2]);
+    const c10::cuda::CUDAGuard device(h.device());
+    const OnStream on(a[10], &h);
+    same_device(dy, h, "dy");
+    on_cuda(rstd, "rstd");
+    same_device(rstd, h, "rstd");
+    if (rstd.scalar_type() != at::kFloat || rstd.dim() != 1 || rstd.size(0) != rows || !rstd.is_contiguous()) bad_argument("rstd", "a contiguous FP32 tensor with an element for every row");
+    const at::Tensor w = maybe(a[3]), dh = maybe(a[4]);
+    check_weight(w, cols, h);
+    auto like_h = [&](const at::Tensor &t, const char *name) {
+        either_matrix(t, name, rows, cols);
+        same_device(t, h, name);
+        if (t.scalar_type() != h.scalar_type()) bad_argument(name, "of h's type");
+    };
+    if (dh.defined()) like_h(dh, "dh");
+    at::Tensor dx = maybe(a[5]), dw = maybe(a[6]);
+    const bool accumulate = as_bool(a[8]);
+    if (dx.defined()) like_h(dx, "out");
+    else dx = padded(on, rows, cols, h.scalar_type(), h);
+    if (dw.defined()) {
+        on_cuda(dw, "dweight");
+        same_device(dw, h, "dweight");
+        if (dw.scalar_type() != at::kFloat || dw.dim() != 1 || dw.size(0) != cols || !dw.is_contiguous()) bad_argument("dweight", "a contiguous FP32 tensor with an element for every column");
+    } else if (as_bool(a[7])) {
+        Unlock u;
+        const auto options = at::TensorOptions().dtype(at::kFloat).device(h.device());
+        dw = on.returned(accumulate ? at::zeros({cols}, options) : at::empty({cols}, options));
+    }
+    at::Tensor scratch = maybe(a[9]);
+    if (scratch.defined()) {
+        on_cuda(scratch, "scratch");
+        same_device(scratch, h, "scratch");
+        if (!scratch.is_contiguous()) value_error("scratch must be contiguous");
+    } else if (dw.defined()) {
+        Unlock u;
+        scratch = at::empty({(int64_t)lib.rms_norm_bwd_scratch_bytes(rows, cols)}, at::TensorOptions().dtype(at::kByte).device(h.device()));
+    }
+    fp4q_norm_grad p = {};
+    p.dy = dy.data_ptr(); p.ld_dy = pitch_of(dy); p.dy_type = type_of(dy);
+    p.h = h.data_ptr(); p.ld_h = pitch_of(h); p.h_type = type_of(h);
+    p.rstd = static_cast<const float *>(rstd.data_ptr());
+    if (w.defined()) { p.weight = w.data_ptr(); p.weight_type = type_of(w); }
+    if (dh.defined()) { p.dh = dh.data_ptr(); p.ld_dh = pitch_of(dh); }
+    p.dx = dx.data_ptr(); p.ld_dx = pitch_of(dx);
+    if (dw.defined()) { p.dweight = static_cast<float *>(dw.data_ptr()); p.accumulate = accumulate; }
+    check(unlocked(lib.rms_norm_bwd, &p, rows, cols, scratch.defined() ? scratch.data_ptr() : nullptr, scratch.defined() ? (size_t)scratch.nbytes() : 0, on.handle), "fp4q_rms_norm_bwd");
+    Ref o(a[5] == Py_None ? wrap(dx) : Py_NewRef(a[5])), d(a[6] == Py_None ? wrap(dw) : Py_NewRef(a[6]));
+    return PyTuple_Pack(2, o.p, d.p);
+}
+
+// A tensor as the gradients' norm takes it: without gaps, in whatever order, or a matrix or stack with contiguous rows.
+fp4q_span span_of(const at::Tensor &t, const char *name)
+{
+    on_cuda(t, name);
+    if (!bf16_or_f32(t)) bad_argument(name, "BF16 or FP32");
+    fp4q_span s = {t.data_ptr(), 1, t.numel(), t.numel(), type_of(t)};
+    if (t.is_non_overlapping_and_dense() || t.numel() == 0) return s;
+    const at::Tensor &m = as_stack(t, name);
+    s.cols = m.size(-1);
+    s.rows = m.numel() / s.cols;
+    s.ld = stack_pitch(m);
+    if (s.rows > 1 && s.ld < s.cols) bad_argument(name, "without elements that share memory");
+    return s;
+}
+struct Spans {
+    std::vector<at::Tensor> kept;
+    std::vector<fp4q_span> spans;
+    Spans(PyObject *list, const char *name)
+    {
+        Ref t(PySequence_Tuple(list));
+        const Py_ssize_t n = PyTuple_GET_SIZE(t.p);
+        for (Py_ssize_t i = 0; i < n; i++) {
+            char text[48];
+            snprintf(text, sizeof text, "%s[%zd]", name, i);
+            kept.push_back(as_tensor(PyTuple_GET_ITEM(t.p, i)));
+            spans.push_back(span_of(kept.back(), text));
+            if (i > 0) same_device(kept.back(), kept.front(), text);
+        }
+    }
+    int32_t n() const { return (int32_t)spans.size(); }
+    // What is written: no tensor twice.
+    void distinct() const
+    {
+        std::vector<const void *> p;
+        for (const fp4q_span &s : spans)
+            if (s.rows * s.cols > 0) p.push_back(s.data);
+        std::sort(p.begin(), p.end());
+        if (std::adjacent_find(p.begin(), p.end()) != p.end()) value_error("a tensor that is written must not be in the list twice");
+    }
+};
+struct ClipOuts {
+    std::optional<Spans> outs;
+    ClipOuts(PyObject *o, Spans &in)
+    {
+        if (o == Py_None) {
+            in.distinct();
+            return;
+        }
+        outs.emplace(o, "outs");
+        if (outs->n() != in.n()) value_error("outs must have an entry for every tensor");
+        for (int32_t i = 0; i < in.n(); i++) {
+            const at::Tensor &t = in.kept[i], &u = outs->kept[i];
+            same_device(u, t, "outs");
+            if (u.sizes() != t.sizes()) value_error("an entry of outs must have its tensor's shape");
+            fp4q_span &a = in.spans[i], &b = outs->spans[i];
+            if (a.rows == b.rows && t.strides() == u.strides()) continue;
+            // One is without gaps and the other is not, or their orders differ: both row by row.
+            const at::Tensor &x = as_stack(t, "a tensor whose strides are not those of its entry of outs"), &y = as_stack(u, "an entry of outs whose strides are not its tensor's");
+            a.cols = b.cols = x.size(-1);
+            a.rows = b.rows = x.size(-1) ? x.numel() / x.size(-1) : 0;
+            a.ld = stack_pitch(x);
+            b.ld = stack_pitch(y);
+        }
+        outs->distinct();
+    }
+    const fp4q_span *data() const { return outs ? outs->spans.data() : nullptr; }
+};
+at::Tensor norm_scratch(PyObject *o, const Spans &s, const at::Tensor &like)
+{
+    if (o != Py_None) {
+        const at::Tensor &t = as_tensor(o);
+        on_cuda(t, "scratch");
+        same_device(t, like, "scratch");
+        if (!t.is_contiguous()) value_error("scratch must be contiguous");
+        return t;
+    }
+    Unlock u;
+    return at::empty({(int64_t)lib.global_norm_scratch_bytes(s.spans.data(), s.n())}, at::TensorOptions().dtype(at::kByte).device(like.device()));
+}
+at::Tensor norm_scalar(PyObject *o, const OnStream &on, const at::Tensor &like)
+{
+    if (o != Py_None) {
+        const at::Tensor &t = as_tensor(o);
+        on_cuda(t, "norm");
+        same_device(t, like, "norm");
+        if (t.scalar_type() != at::kFloat || t.numel() != 1) bad_argument("norm", "one FP32 number");
+        return t;
+    }
+    Unlock u;
+    return on.returned(at::empty({}, at::TensorOptions().dtype(at::kFloat).device(like.device())));
+}
+const at::Tensor &first_of(const Spans &s)
+{
+    if (s.kept.empty()) value_error("the list must have a tensor");
+    return s.kept.front();
+}
+// tensors, norm | None, scratch | None, stream
+PyObject *global_norm(Args a, Py_ssize_t n)
+{
+    want(n, 4);
+    const Spans s(a[0], "tensors");
+    const at::Tensor &like = first_of(s);
+    const c10::cuda::CUDAGuard device(like.device());
+    const OnStream on(a[3], &like);
+    const at::Tensor norm = norm_scalar(a[1], on, like), scratch = norm_scratch(a[2], s, like);
+    check(unlocked(lib.global_norm, s.spans.data(), s.n(), static_cast<float *>(norm.data_ptr()), scratch.data_ptr(), (size_t)scratch.nbytes(), on.handle), "fp4q_global_norm");
+    return a[1] == Py_None ? wrap(norm) : Py_NewRef(a[1]);
+}
+// tensors, norm, max_norm, outs | None, eps, stream
+PyObject *clip_by_norm(Args a, Py_ssize_t n)
+{
+    want(n, 6);
+    Spans s(a[0], "tensors");
+    const at::Tensor &like = first_of(s);
+    const c10::cuda::CUDAGuard device(like.device());
+    const OnStream on(a[5], &like);
+    const at::Tensor norm = as_tensor(a[1]);
+    norm_scalar(a[1], on, like);
+    const ClipOuts outs(a[3], s);
+    check(unlocked(lib.clip_by_norm, s.spans.data(), outs.data(), s.n(), static_cast<const float *>(norm.data_ptr()), (float)as_double(a[2]), (float)as_double(a[4]), on.handle), "fp4q_clip_by_norm");
+    return Py_NewRef(a[3] == Py_None ? a[0] : a[3]);
+}
+// tensors, max_norm, outs | None, eps, norm | None, scratch | None, stream
+PyObject *clip_grad_norm(Args a, Py_ssize_t n)
+{
+    want(n, 7);
+    Spans s(a[0], "tensors");
+    const at::Tensor &like = first_of(s);
+    const c10::cuda::CUDAGuard device(like.device());
+    const OnStream on(a[6], &like);
+    const std::vector<fp4q_span> as_read = s.spans;
+    const ClipOuts outs(a[2], s);
+    const float max_norm = (float)as_double(a[1]), eps = (float)as_double(a[3]);
+    if (!(max_norm >= 0.f) || !(eps >= 0.f)) check(FP4Q_ERR_UNSUPPORTED, "fp4q_clip_by_norm");   // before anything is enqueued
+    const at::Tensor norm = norm_scalar(a[4], on, like), scratch = norm_scratch(a[5], s, like);
+    float *to = static_cast<float *>(norm.data_ptr());
+    check(unlocked(lib.global_norm, as_read.data(), s.n(), to, scratch.data_ptr(), (size_t)scratch.nbytes(), on.handle), "fp4q_global_norm");
+    check(unlocked(lib.clip_by_norm, s.spans.data(), outs.data(), s.n(), (const float *)to, max_norm, eps, on.handle), "fp4q_clip_by_norm");
+    return a[4] == Py_None ? wrap(norm) : Py_NewRef(a[4]);
+}
+
 // ---- the straight-through layer of autograd.py as one native autograd node
 //
 // The layer's kernels run 20 to 90 us forward and backward at the sizes where layers are small; through a Python autograd
@@ -813,10 +1280,10 @@ void set_entry(PyObject *addresses, const char *name, F &slot)
     if (PyErr_Occurred()) throw PyError();
 }
 
-// {name: address of the C entry point}, QTensor, _check
+// {name: address of the C entry point}, QTensor, _check, Fp8Tensor, NormOut
 PyObject *init(Args a, Py_ssize_t n)
 {
-    want(n, 3);
+    want(n, 5);
     set_entry(a[0], "fp4q_quantize2d", lib.quantize2d);
     set_entry(a[0], "fp4q_quantize2d_multi", lib.quantize2d_multi);
     set_entry(a[0], "fp4q_quantize2d_multi_f32", lib.quantize2d_multi_f32);
@@ -843,8 +1310,20 @@ PyObject *init(Args a, Py_ssize_t n)
     set_entry(a[0], "fp4q_ragged_gemm_wgrad_scratch_bytes", lib.ragged_gemm_wgrad_scratch_bytes);
     set_entry(a[0], "fp4q_newton_schulz", lib.newton_schulz);
     set_entry(a[0], "fp4q_newton_schulz_scratch_bytes", lib.newton_schulz_scratch_bytes);
+    set_entry(a[0], "fp4q_fp8_quantize", lib.fp8_quantize);
+    set_entry(a[0], "fp4q_fp8_gemm_fwd", lib.fp8_gemm_fwd);
+    set_entry(a[0], "fp4q_fp8_gemm_dgrad", lib.fp8_gemm_dgrad);
+    set_entry(a[0], "fp4q_fp8_gemm_wgrad", lib.fp8_gemm_wgrad);
+    set_entry(a[0], "fp4q_rms_norm", lib.rms_norm);
+    set_entry(a[0], "fp4q_rms_norm_bwd", lib.rms_norm_bwd);
+    set_entry(a[0], "fp4q_rms_norm_bwd_scratch_bytes", lib.rms_norm_bwd_scratch_bytes);
+    set_entry(a[0], "fp4q_global_norm", lib.global_norm);
+    set_entry(a[0], "fp4q_global_norm_scratch_bytes", lib.global_norm_scratch_bytes);
+    set_entry(a[0], "fp4q_clip_by_norm", lib.clip_by_norm);
     Py_XSETREF(g_qtensor, Py_NewRef(a[1]));
     Py_XSETREF(g_fail, Py_NewRef(a[2]));
+    Py_XSETREF(g_fp8, Py_NewRef(a[3]));
+    Py_XSETREF(g_norm, Py_NewRef(a[4]));
     return Py_NewRef(Py_None);
 }
 
@@ -879,6 +1358,14 @@ PyMethodDef methods[] = {METHOD("init", init),
                          METHOD("linear", linear),
                          METHOD("ragged_gemm", ragged_gemm),
                          METHOD("newton_schulz", newton_schulz),
+                         METHOD("fp8_quantize", fp8_quantize),
+                         METHOD("fp8_gemm", fp8_gemm),
+                         METHOD("alloc_norm", alloc_norm),
+                         METHOD("rms_norm", rms_norm),
+                         METHOD("rms_norm_bwd", rms_norm_bwd),
+                         METHOD("global_norm", global_norm),
+                         METHOD("clip_by_norm", clip_by_norm),
+                         METHOD("clip_grad_norm", clip_grad_norm),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", "argument marshalling of binding.py", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -892,5 +1379,11 @@ PyMODINIT_FUNC PyInit__host(void)
     s_q_t = PyUnicode_InternFromString("q_t");
     s_scale = PyUnicode_InternFromString("scale");
     s_granularity = PyUnicode_InternFromString("scale_granularity");
+    s_q = PyUnicode_InternFromString("q");
+    s_scale_t = PyUnicode_InternFromString("scale_t");
+    s_square = PyUnicode_InternFromString("square");
+    s_h = PyUnicode_InternFromString("h");
+    s_y = PyUnicode_InternFromString("y");
+    s_rstd = PyUnicode_InternFromString("rstd");
     return PyModule_Create(&module);
 }
