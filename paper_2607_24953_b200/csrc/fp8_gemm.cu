@@ -27,7 +27,8 @@ struct Scales8 {
 
 struct Gemm8Params {
     int32_t m, n, blocks;            // rows of A and B, blocks of the contraction
-    int32_t n_tiles, split;          // split: CTAs of a cluster, which share a tile's contraction
+    int32_t m_tiles, n_tiles, split; // split: CTAs of a cluster, which share a tile's contraction
+    int32_t boxed;                   // columns that leave in boxes, whole 16 bytes; the rest of a row leaves by itself
     Scales8 sa, sb;
     void *c;                         // row-major, [m, n] or, with SCALE_COLS, its transpose: [n, m]
     int64_t ldc;
@@ -78,8 +79,9 @@ __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b)
     return r;
 }
 
-// 16 columns of an accumulator's row; the values are there after landed().
+// Columns of an accumulator's row; the values are there after landed().
 __device__ __forceinline__ void load_acc(uint32_t from, uint32_t (&v)[16]) { FP4Q_TMEM_LD_X16(from, v); }
+__device__ __forceinline__ void load_acc(uint32_t from, uint32_t (&v)[32]) { FP4Q_TMEM_LD_X32(from, v); }
 __device__ __forceinline__ void landed(uint32_t (&v)[16])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -87,21 +89,32 @@ __device__ __forceinline__ void landed(uint32_t (&v)[16])
                    "+r"(v[14]), "+r"(v[15])
                  :: "memory");
 }
-
-// sum += a block's product times its scales, for COLS columns of a thread's row.  row_scale: of the row; cols: of the columns, in shared memory.
-template <int MODE, int COLS>
-__device__ __forceinline__ void add_block(uint64_t (&sum)[COLS / 2], uint32_t from, float row_scale, const float *cols)
+__device__ __forceinline__ void landed(uint32_t (&v)[32])
 {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]),
+                   "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]),
+                   "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
+                 :: "memory");
+}
+
+// sum += a block's product times its scales, for COLS columns of a thread's row.  row_scale: of the row; cols: of the columns, in shared memory.  read: called when the accumulator
+// has been read.
+template <int MODE, int COLS, typename F>
+__device__ __forceinline__ void add_block(uint64_t (&sum)[COLS / 2], uint32_t from, float row_scale, const float *cols, F read)
+{
+    constexpr int kStep = COLS < 32 ? 16 : 32;
     const uint64_t s = pair32(row_scale, row_scale);
-    uint32_t v[2][16];
+    uint32_t v[2][kStep];
     load_acc(from, v[0]);
 #pragma unroll
-    for (int c = 0; c < COLS; c += 16) {
-        uint32_t(&x)[16] = v[(c / 16) & 1];
+    for (int c = 0; c < COLS; c += kStep) {
+        uint32_t(&x)[kStep] = v[(c / kStep) & 1];
         landed(x);
-        if (c + 16 < COLS) load_acc(from + c + 16, v[(c / 16 + 1) & 1]);
+        if (c + kStep < COLS) load_acc(from + c + kStep, v[(c / kStep + 1) & 1]);
+        else read();
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
+        for (int e = 0; e < kStep; e += 4) {
             const uint64_t lo = pair32(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), hi = pair32(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
             uint64_t &a = sum[(c + e) / 2], &b = sum[(c + e) / 2 + 1];
             if (MODE == SCALE_ROWS) {
@@ -169,6 +182,57 @@ __device__ __forceinline__ void store_one(const Gemm8Params &p, int64_t row, int
         *c = p.accumulate ? *c + v : v;
     } else {
         static_cast<__nv_bfloat16 *>(p.c)[row * p.ldc + col] = __float2bfloat16_rn(v);
+    }
+}
+
+// A box of 32 rows x 128 bytes, COLS columns from col on, leaves an epilogue warp.  w: the lane's row of it, value(e): its elements.
+template <int COLS, typename F>
+__device__ __forceinline__ void send_box(const Gemm8Params &p, const CUtensorMap *map, const Box16 &box, uint32_t box_at, const uint32_t *w, int row0, int col, int lane, F value)
+{
+    if (row0 >= p.m || col >= p.n) return;
+    if (col < p.boxed) {
+        boxes_free(lane);
+        box.put(w);
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) {
+            if (p.accumulate) tma_reduce_add_2d(map, col, row0, box_at);
+            else tma_store_2d(map, col, row0, box_at);
+            bulk_commit();
+        }
+    }
+    if (col + COLS > p.boxed && p.boxed < p.n && row0 + lane < p.m) {
+#pragma unroll
+        for (int e = 0; e < COLS; e++)
+            if (col + e >= p.boxed && col + e < p.n) store_one(p, row0 + lane, col + e, value(e));
+    }
+    __syncwarp();
+}
+
+// The scales of AHEAD blocks from b on, for ROWS rows from m0 on and COLS columns from n0 on: those of rows already times the one of the columns, and the other way round.  All of
+// a warp's loads are on their way before the first is written.
+template <int MODE, int AHEAD, int ROWS, int COLS>
+__device__ __forceinline__ void load_scales(const Gemm8Params &p, int m0, int n0, int b, int b1, float *to)
+{
+    constexpr int kR = (ROWS + 31) / 32, kC = (COLS + 31) / 32;
+    const int lane = threadIdx.x & 31;
+    float other[AHEAD], r[AHEAD][kR ? kR : 1], c[AHEAD][kC ? kC : 1];
+#pragma unroll
+    for (int i = 0; i < AHEAD; i++) {
+        const bool there = b + i < b1;
+        other[i] = !there || MODE == SCALE_BOTH ? 1.f : MODE == SCALE_ROWS ? p.sb.at(n0, b + i) : p.sa.at(m0, b + i);
+#pragma unroll
+        for (int j = 0; j < kR; j++) r[i][j] = there && m0 + lane + 32 * j < p.m ? p.sa.at(m0 + lane + 32 * j, b + i) : 0.f;
+#pragma unroll
+        for (int j = 0; j < kC; j++) c[i][j] = there && lane + 32 * j < COLS && n0 + lane + 32 * j < p.n ? p.sb.at(n0 + lane + 32 * j, b + i) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; i++) {
+#pragma unroll
+        for (int j = 0; j < kR; j++) to[i * ROWS + lane + 32 * j] = r[i][j] * other[i];
+#pragma unroll
+        for (int j = 0; j < kC; j++)
+            if (lane + 32 * j < COLS) to[AHEAD * ROWS + i * COLS + lane + 32 * j] = c[i][j] * other[i];
     }
 }
 
@@ -268,15 +332,7 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
         for (int b = b0; b < b1; b += C::kAhead, set.next()) {
             if (!warp_wait(bar_sc_empty + 8 * set.slot, set.phase ^ 1u, abort_flag, p.status, limit, 0x400u)) break;
             float *to = scales + set.slot * C::kScales;
-#pragma unroll
-            for (int i = 0; i < C::kAhead; i++) {
-                const bool there = b + i < b1;
-                const float other = !there || MODE == SCALE_BOTH ? 1.f : MODE == SCALE_ROWS ? p.sb.at(n0, b + i) : p.sa.at(m0, b + i);
-#pragma unroll
-                for (int j = lane; j < C::kRowScales; j += 32) to[i * C::kRowScales + j] = there && m0 + j < p.m ? p.sa.at(m0 + j, b + i) * other : 0.f;
-#pragma unroll
-                for (int j = lane; j < C::kColScales; j += 32) to[C::kAhead * C::kRowScales + i * C::kColScales + j] = there && n0 + j < p.n ? p.sb.at(n0 + j, b + i) * other : 0.f;
-            }
+            load_scales<MODE, C::kAhead, C::kRowScales, C::kColScales>(p, m0, n0, b, b1, to);
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_sc_full + 8 * set.slot);
         }
@@ -293,10 +349,12 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
             tcgen05_fence_after();
             const float *from = scales + set.slot * C::kScales;
             const float row = C::kRowScales ? from[i * C::kRowScales + 32 * quarter + lane] : 1.f;
-            add_block<MODE, C::kCols>(sum, tmem + acc.slot * BN + half * C::kCols + ((uint32_t)(32 * quarter) << 16), row, from + C::kAhead * C::kRowScales + i * C::kColScales + half * C::kCols);
-            tcgen05_fence_before();
+            add_block<MODE, C::kCols>(sum, tmem + acc.slot * BN + half * C::kCols + ((uint32_t)(32 * quarter) << 16), row, from + C::kAhead * C::kRowScales + i * C::kColScales + half * C::kCols, [&] {
+                tcgen05_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_acc_empty + 8 * acc.slot);
+            });
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar_acc_empty + 8 * acc.slot);
             if (i == C::kAhead - 1 || b == b1 - 1) {
                 if (lane == 0) mbar_arrive(bar_sc_empty + 8 * set.slot);
                 set.next();
@@ -367,6 +425,232 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
     }
 }
 
+// ---------------------------------------------------------------------------------------- persistent: many tiles
+
+// Single CTAs with tiles of 128 x 128, or pairs (cta_group::2) with tiles of 256 x 256 of which each CTA has 128 rows and loads half of B's: 32 KB of operands then feed
+// 2 x 128 x 256 x 128 operations, in 512 cycles of the tensor core, which is what L2 delivers.  Warps: 0, 3 TMA producers of A and B, 1 MMA issuer, 2 scales, 4 and up epilogue, each with 32 rows x half
+// of the columns: with 128 sums a thread they need more registers than 12 warps' share, which the others give.
+template <int CTAS, int MODE>
+struct CfgP {
+    static constexpr int kBN = 128 * CTAS, kThreads = 384;
+    static constexpr int kCols = 64 * CTAS;
+    static constexpr int kABytes = 128 * kBlock8, kBBytes = 128 * kBlock8, kStageBytes = kABytes + kBBytes;   // of a CTA
+    static constexpr int kStages = 5;
+    static constexpr int kOperands = kStages * kStageBytes;
+    static constexpr int kAccs = 4 / CTAS, kTmemCols = 512;
+    static constexpr int kColScales = MODE == SCALE_BOTH ? kBN : 0;        // else one for each block of 128 columns
+    static constexpr int kAhead = 4, kScales = kAhead * (128 + kBN);
+    static constexpr int kStaging = 4096;                                  // of an epilogue warp: a box of 32 rows x 128 bytes
+    static constexpr int kSmem = 1024 + kOperands + 8 * kStaging + 2 * kScales * 4 + 512;
+    static constexpr int kFewRegs = 72, kManyRegs = 216;
+    static_assert(128 * kFewRegs + 256 * kManyRegs <= 384 * 168, "registers: what the epilogue takes is what the other warps give");
+    static_assert(kSmem <= 227 * 1024, "shared memory budget");
+};
+struct MapsP {
+    CUtensorMap a, b, out;
+};
+
+template <int CTAS, int MODE>
+__global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ MapsP maps, const Gemm8Params p)
+{
+    using C = CfgP<CTAS, MODE>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t *smem_a = smem, *smem_b = smem + C::kStages * C::kABytes, *smem_boxes = smem + C::kOperands;
+    float *scales = reinterpret_cast<float *>(smem_boxes + 8 * C::kStaging);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(scales + 2 * C::kScales);
+    // [0..7] full, [8..15] empty, [16..19] accumulator full, [20..23] accumulator empty, [24..25] scales full, [26..27] scales empty
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + 28);
+    volatile uint32_t *abort_flag = tmem_slot + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t bar_full = smem_u32(bars), bar_empty = smem_u32(bars + 8), bar_acc_full = smem_u32(bars + 16), bar_acc_empty = smem_u32(bars + 20),
+                   bar_sc_full = smem_u32(bars + 24), bar_sc_empty = smem_u32(bars + 26);
+    const int rank = CTAS == 2 ? (int)cluster_ctarank() : 0;
+
+    if (warp == 0) {
+        if (lane < 28) mbar_init(smem_u32(bars + lane), lane >= 20 && lane < 24 ? 8 * CTAS : lane >= 26 ? 8 : 1);
+        if (lane == 0) *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    } else if (warp == 1) {
+        if (CTAS == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+        tcgen05_fence_before();
+    } else if (warp == 2 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.out) : "memory");
+    }
+    __syncthreads();
+    if (CTAS == 2) { cluster_arrive(); cluster_wait(); }
+    tcgen05_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    wait_for_predecessor();   // from here on global memory is read and written
+
+    const uint32_t limit_word = load_global(p.status + 2), withhold = blockIdx.x == 0 ? load_global(p.status + 3) : 0u;
+    const uint64_t limit = limit_word != 0u ? limit_word : kWaitLimit;
+    const int tiles = p.m_tiles * p.n_tiles, step = gridDim.x / CTAS, blocks = p.blocks;
+    // Bands of kRaster16 rows of tiles, whose A rows stay in L2 while the columns go by.
+    auto place = [&](int tile, int &m0, int &n0) {
+        const int per_band = kRaster16 * p.n_tiles, band = tile / per_band, top = band * kRaster16, h = min(kRaster16, p.m_tiles - top), rem = tile - band * per_band;
+        n0 = rem / h * C::kBN;
+        m0 = (top + rem % h) * (128 * CTAS) + rank * 128;
+    };
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kFewRegs));
+        if (warp == 0 || warp == 3) {
+            const bool issuer = elect_one(), a_side = warp == 0;
+            const uint32_t to0 = smem_u32(a_side ? smem_a : smem_b), lead = CTAS == 2 ? cluster_addr(bar_full, 0) : bar_full;
+            Ring16<C::kStages> ring;
+            uint32_t loads = 0, issued = 0;
+            bool ok = true;
+            for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step) {
+                int m0, n0;
+                place(tile, m0, n0);
+                const int row = a_side ? m0 : n0 + (CTAS == 2 ? rank * 128 : 0);
+                for (int b = 0; b < blocks; b++, ring.next()) {
+                    if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) { ok = false; break; }
+                    issued++;
+                    expect_tx_if(bar_full + 8 * ring.slot, C::kStageBytes * CTAS, issuer && a_side && rank == 0);
+                    if (issuer && (withhold == 0u || !a_side || ++loads != withhold)) {
+                        const uint32_t to = to0 + ring.slot * C::kABytes;
+                        if (CTAS == 2) tma_load_2d_pair(to, a_side ? &maps.a : &maps.b, b * kBlock8, row, lead + 8 * ring.slot);
+                        else tma_load_2d(to, a_side ? &maps.a : &maps.b, b * kBlock8, row, lead + 8 * ring.slot);
+                    }
+                    __syncwarp();
+                }
+            }
+            // The MMAs' last reports reach this CTA's barriers while it is still there.
+            for (uint32_t i = 0; ok && i < C::kStages; i++, ring.next())
+                if (issued >= C::kStages - i) ok = warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x700u + ring.slot);
+        } else if (warp == 1 && rank == 0) {
+            const bool issuer = elect_one();
+            const uint32_t idesc = instr_desc8<CTAS>(C::kBN), a_desc = (uint32_t)smem_desc_sw128(smem_u32(smem_a)), b_desc = (uint32_t)smem_desc_sw128(smem_u32(smem_b));
+            constexpr uint32_t desc_hi = (1024 >> 4) | (1u << 14) | (2u << 29);
+            Ring16<C::kStages> ring;
+            Ring16<C::kAccs> acc;
+            bool ok = true;
+            for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step)
+                for (int b = 0; b < blocks; b++, ring.next(), acc.next()) {
+                    ok = warp_wait<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u) &&
+                         warp_wait(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot);
+                    if (!ok) break;
+                    tcgen05_fence_after();
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        tcgen05_mma_f8<CTAS>(tmem + acc.slot * C::kBN, a_desc + ((ring.slot * C::kABytes + 32 * j) >> 4), b_desc + ((ring.slot * C::kBBytes + 32 * j) >> 4), desc_hi, idesc, j > 0,
+                                             issuer);
+                    tcgen05_commit_if<CTAS>(bar_acc_full + 8 * acc.slot, issuer);
+                    tcgen05_commit_if<CTAS>(bar_empty + 8 * ring.slot, issuer);
+                }
+        } else if (warp == 2) {
+            Ring16<2> set;
+            bool ok = true;
+            for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step) {
+                int m0, n0;
+                place(tile, m0, n0);
+                for (int b = 0; b < blocks; b += C::kAhead, set.next()) {
+                    ok = warp_wait(bar_sc_empty + 8 * set.slot, set.phase ^ 1u, abort_flag, p.status, limit, 0x400u);
+                    if (!ok) break;
+                    float *to = scales + set.slot * C::kScales;
+                    load_scales<SCALE_BOTH, C::kAhead, 128, C::kColScales>(p, m0, n0, b, blocks, to);
+                    if (MODE == SCALE_ROWS && lane < C::kAhead * CTAS) {   // lane: a block of columns and one of the contraction
+                        const int i = lane / CTAS, j = lane % CTAS;
+                        to[C::kAhead * 128 + lane] = b + i < blocks && n0 + 128 * j < p.n ? p.sb.at(n0 + 128 * j, b + i) : 0.f;
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_sc_full + 8 * set.slot);
+                }
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kManyRegs));
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t box_at = smem_u32(smem_boxes) + (warp - 4) * C::kStaging, lead_empty = CTAS == 2 ? cluster_addr(bar_acc_empty, 0) : bar_acc_empty;
+        const Box16 box(box_at, lane);
+        Ring16<C::kAccs> acc;
+        Ring16<2> set;
+        bool ok = true;
+        for (int tile = blockIdx.x / CTAS; tile < tiles; tile += step) {
+            int m0, n0;
+            place(tile, m0, n0);
+            uint64_t sum[C::kCols / 2];
+#pragma unroll
+            for (int i = 0; i < C::kCols / 2; i++) sum[i] = 0;
+            for (int b = 0; b < blocks; b++, acc.next()) {
+                const int i = b % C::kAhead;
+                ok = (i != 0 || warp_wait(bar_sc_full + 8 * set.slot, set.phase, abort_flag, p.status, limit, 0x500u)) &&
+                     warp_wait(bar_acc_full + 8 * acc.slot, acc.phase, abort_flag, p.status, limit, 0x600u);
+                if (!ok) break;
+                tcgen05_fence_after();
+                const float *from = scales + set.slot * C::kScales;
+                float row = from[i * 128 + 32 * quarter + lane];
+                if (MODE == SCALE_ROWS) row *= from[C::kAhead * 128 + i * CTAS + (CTAS == 2 ? half : 0)];
+                add_block<MODE, C::kCols>(sum, tmem + acc.slot * C::kBN + half * C::kCols + ((uint32_t)(32 * quarter) << 16), row, from + C::kAhead * 128 + i * C::kColScales + half * C::kCols, [&] {
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (rank != 0) mbar_arrive_cluster(lead_empty + 8 * acc.slot);
+                        else mbar_arrive(bar_acc_empty + 8 * acc.slot);
+                    }
+                });
+                __syncwarp();
+                if (i == C::kAhead - 1 || b == blocks - 1) {
+                    if (lane == 0) mbar_arrive(bar_sc_empty + 8 * set.slot);
+                    set.next();
+                }
+            }
+            if (!ok) break;
+            // Boxes of 32 rows x 128 bytes; a row's last bytes that are no whole 16 by themselves.
+            const int row0 = m0 + 32 * quarter, col0 = n0 + half * C::kCols;
+            if (p.f32) {
+#pragma unroll
+                for (int c = 0; c < C::kCols; c += 32) {
+                    float v[32];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) unpair32(sum[(c + e) / 2], v[e], v[e + 1]);
+                    send_box<32>(p, &maps.out, box, box_at, reinterpret_cast<const uint32_t *>(v), row0, col0 + c, lane, [&](int e) { return v[e]; });
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < C::kCols; c += 64) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int e = 0; e < 32; e++) {
+                        float x, y;
+                        unpair32(sum[c / 2 + e], x, y);
+                        w[e] = pack_bf16(x, y);
+                    }
+                    send_box<64>(p, &maps.out, box, box_at, w, row0, col0 + c, lane, [&](int e) { return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16); });
+                }
+            }
+        }
+        boxes_free(lane);   // the stores have read shared memory; what they write is there when the grid has completed
+    }
+    // Shared memory and tensor memory stay until all roles, of both CTAs of a pair, have done with them.  Where a wait has run out, copies and MMAs may still be under
+    // way: they take microseconds, a millisecond is left to them.
+    __syncwarp();
+    if (*abort_flag != 0u) {
+        if (CTAS == 2 && lane == 0)   // the other CTA is told
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(smem_u32(const_cast<const uint32_t *>(abort_flag)), 1 - rank)), "r"(1u) : "memory");
+        for (int i = 0; i < 64; i++) __nanosleep(16000);
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (CTAS == 2) { cluster_arrive(); cluster_wait(); }
+    if (warp == 1) {
+        tcgen05_fence_after();
+        if (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
+    }
+}
+
 // ---------------------------------------------------------------------------------------- host side
 
 const int64_t kMaxDim8 = 0x7FFFFFFF - 4096;
@@ -427,6 +711,45 @@ fp4q_status launch_tiles(const Operand8 &a, const Operand8 &b, Gemm8Params p, in
     return launched(cudaLaunchKernelEx(&cfg, gemm8_tile_kernel<BN, MODE>, maps, p));
 }
 
+template <int CTAS, int MODE>
+fp4q_status launch_persistent(const Operand8 &a, const Operand8 &b, Gemm8Params p, cudaStream_t stream)
+{
+    using C = CfgP<CTAS, MODE>;
+    MapsP maps;
+    if (!make_map8(&maps.a, a, 128) || !make_map8(&maps.b, b, 128)) return FP4Q_ERR_CUDA;
+    const int64_t bytes = p.f32 ? 4 : 2;
+    {
+        const cuuint64_t dims[2] = {(cuuint64_t)p.boxed, (cuuint64_t)p.m};
+        const cuuint64_t strides[1] = {(cuuint64_t)(p.ldc * bytes)};
+        const cuuint32_t box[2] = {(cuuint32_t)(128 / bytes), 32u};
+        if (!encode_tiled(&maps.out, p.f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, p.c, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B))
+            return FP4Q_ERR_CUDA;
+    }
+    const int dev = current_device();
+    static std::atomic<bool> set[kMaxDevices];
+    if (dev < 0 || !allow_smem(gemm8_kernel<CTAS, MODE>, C::kSmem, set, dev)) return FP4Q_ERR_CUDA;
+    p.m_tiles = (int32_t)ceil_div(p.m, 128 * CTAS);
+    p.n_tiles = (int32_t)ceil_div(p.n, C::kBN);
+    const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles, slots = sm_count(dev) / CTAS;
+    if (tiles > 0x3FFFFFFF) return FP4Q_ERR_UNSUPPORTED;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    cfg.gridDim = dim3((unsigned)(CTAS * std::min(tiles, slots)));
+    cfg.blockDim = dim3(C::kThreads);
+    cfg.dynamicSmemBytes = C::kSmem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CTAS;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = CTAS == 2 ? 2 : 1;
+    return launched(cudaLaunchKernelEx(&cfg, gemm8_kernel<CTAS, MODE>, maps, p));
+}
+
 // CTAs that share a tile's contraction: as many as fill the GPU's places, with two blocks each at least.
 int split_of(int64_t tiles, int64_t places, int64_t blocks)
 {
@@ -447,8 +770,11 @@ fp4q_status product8(const Operand8 &a, const Operand8 &b, Gemm8Params p, bool b
         const int bn = a.rows <= 16 ? 16 : a.rows <= 32 ? 32 : 64, split = split_of(ceil_div(b.rows, 128), 296, p.blocks);
         return bn == 16 ? launch_tiles<16, SCALE_COLS>(b, a, p, split, stream) : bn == 32 ? launch_tiles<32, SCALE_COLS>(b, a, p, split, stream) : launch_tiles<64, SCALE_COLS>(b, a, p, split, stream);
     }
-    const int split = split_of(ceil_div(a.rows, 128) * ceil_div(b.rows, 128), 148, p.blocks);
-    return both ? launch_tiles<128, SCALE_BOTH>(a, b, p, split, stream) : launch_tiles<128, SCALE_ROWS>(a, b, p, split, stream);
+    const int64_t tiles = ceil_div(a.rows, 128) * ceil_div(b.rows, 128);
+    const int split = split_of(tiles, 148, p.blocks);
+    if (p.boxed == 0 || tiles <= 148) return both ? launch_tiles<128, SCALE_BOTH>(a, b, p, split, stream) : launch_tiles<128, SCALE_ROWS>(a, b, p, split, stream);
+    if (ceil_div(a.rows, 256) * ceil_div(b.rows, 256) >= 74) return both ? launch_persistent<2, SCALE_BOTH>(a, b, p, stream) : launch_persistent<2, SCALE_ROWS>(a, b, p, stream);
+    return both ? launch_persistent<1, SCALE_BOTH>(a, b, p, stream) : launch_persistent<1, SCALE_ROWS>(a, b, p, stream);
 }
 
 // Row-major codes (transposed: of the transpose), which may be missing from a tensor that has none of these elements.
@@ -498,6 +824,8 @@ fp4q_status call8(int which, const fp4q_fp8_tensor *x, const fp4q_fp8_tensor *y,
     p.accumulate = accumulate != 0;
     p.wide = aligned(c, 32) && ldc * bytes % 32 == 0;
     p.status = static_cast<uint32_t *>(ws);
+    const int64_t per16 = 16 / bytes;
+    p.boxed = (int32_t)(((int)dt & (int)FP4Q_OUT_PADDED) ? round_up(b.rows, per16) : b.rows / per16 * per16);
     if (a.cols == 0) {   // an empty contraction: maps of something that exists, and no block of it
         a.q = b.q = static_cast<const uint8_t *>(c);
         a.ld = b.ld = 16;
