@@ -22,7 +22,14 @@ struct Scales8 {
     const float *p;
     int64_t row, block;
     int32_t shift;
+    int32_t fours;                   // four blocks of a row lie in 16 aligned bytes
     __device__ __forceinline__ float at(int r, int b) const { return load_global(p + (int64_t)(r >> shift) * row + b * block); }
+    // Blocks b .. b + 3 of row r, those below `end`; b is a multiple of four.
+    __device__ __forceinline__ float4 four(int r, int b, int end) const
+    {
+        if (fours && b + 4 <= end) return load_global(reinterpret_cast<const float4 *>(p + (int64_t)(r >> shift) * row + b));
+        return make_float4(at(r, b), b + 1 < end ? at(r, b + 1) : 0.f, b + 2 < end ? at(r, b + 2) : 0.f, b + 3 < end ? at(r, b + 3) : 0.f);
+    }
 };
 
 struct Gemm8Params {
@@ -58,30 +65,8 @@ __device__ __forceinline__ uint32_t instr_desc8(int cols)
     return (1u << 4) | ((uint32_t)(cols >> 3) << 17) | ((uint32_t)((128 * CTAS) >> 4) << 24);
 }
 
-// Two FP32 in a register pair.
-__device__ __forceinline__ uint64_t pair32(float a, float b)
-{
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpair32(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 // Columns of an accumulator's row; the values are there after landed().
 __device__ __forceinline__ void load_acc(uint32_t from, uint32_t (&v)[16]) { FP4Q_TMEM_LD_X16(from, v); }
-__device__ __forceinline__ void load_acc(uint32_t from, uint32_t (&v)[32]) { FP4Q_TMEM_LD_X32(from, v); }
 __device__ __forceinline__ void landed(uint32_t (&v)[16])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -89,47 +74,32 @@ __device__ __forceinline__ void landed(uint32_t (&v)[16])
                    "+r"(v[14]), "+r"(v[15])
                  :: "memory");
 }
-__device__ __forceinline__ void landed(uint32_t (&v)[32])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]),
-                   "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]),
-                   "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])
-                 :: "memory");
-}
 
 // sum += a block's product times its scales, for COLS columns of a thread's row.  row_scale: of the row; cols: of the columns, in shared memory.  read: called when the accumulator
-// has been read.
+// has been read.  (Additions in pairs, fma.rn.f32x2, would halve the instructions, but every value is then moved into an aligned pair first: 8192 x 4096 x 4096 194 us for 147.)
 template <int MODE, int COLS, typename F>
-__device__ __forceinline__ void add_block(uint64_t (&sum)[COLS / 2], uint32_t from, float row_scale, const float *cols, F read)
+__device__ __forceinline__ void add_block(float (&sum)[COLS], uint32_t from, float row_scale, const float *cols, F read)
 {
-    constexpr int kStep = COLS < 32 ? 16 : 32;
-    const uint64_t s = pair32(row_scale, row_scale);
-    uint32_t v[2][kStep];
-    load_acc(from, v[0]);
 #pragma unroll
-    for (int c = 0; c < COLS; c += kStep) {
-        uint32_t(&x)[kStep] = v[(c / kStep) & 1];
+    for (int c = 0; c < COLS; c += 16) {
+        uint32_t x[16];
+        load_acc(from + c, x);
         landed(x);
-        if (c + kStep < COLS) load_acc(from + c + kStep, v[(c / kStep + 1) & 1]);
-        else read();
+        if (c + 16 == COLS) read();
 #pragma unroll
-        for (int e = 0; e < kStep; e += 4) {
-            const uint64_t lo = pair32(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), hi = pair32(__uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
-            uint64_t &a = sum[(c + e) / 2], &b = sum[(c + e) / 2 + 1];
-            if (MODE == SCALE_ROWS) {
-                a = fma_pair(lo, s, a);
-                b = fma_pair(hi, s, b);
-            } else {
-                const float4 f = *reinterpret_cast<const float4 *>(cols + c + e);
-                const uint64_t f0 = pair32(f.x, f.y), f1 = pair32(f.z, f.w);
-                if (MODE == SCALE_COLS) {
-                    a = fma_pair(lo, f0, a);
-                    b = fma_pair(hi, f1, b);
-                } else {
-                    a = fma_pair(mul_pair(lo, f0), s, a);
-                    b = fma_pair(mul_pair(hi, f1), s, b);
-                }
+        for (int e = 0; e < 16; e += 4) {
+            float f[4];
+            if (MODE != SCALE_ROWS) {
+                const float4 g = *reinterpret_cast<const float4 *>(cols + c + e);
+                f[0] = g.x; f[1] = g.y; f[2] = g.z; f[3] = g.w;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const float v = __uint_as_float(x[e + j]);
+                float &to = sum[c + e + j];
+                if (MODE == SCALE_ROWS) to = fmaf(v, row_scale, to);
+                else if (MODE == SCALE_COLS) to = fmaf(v, f[j], to);
+                else to = fmaf(v * f[j], row_scale, to);
             }
         }
     }
@@ -295,7 +265,7 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
     const int tile = blockIdx.x / p.split, m0 = tile / p.n_tiles * 128, n0 = tile % p.n_tiles * BN;
     const int b0 = (int)((int64_t)p.blocks * rank / p.split), b1 = (int)((int64_t)p.blocks * (rank + 1) / p.split);   // this CTA's blocks
     constexpr int kSums = C::kCols;
-    uint64_t sum[kSums / 2];
+    float sum[kSums];
 
     if (warp == 0) {
         const bool issuer = elect_one();
@@ -339,7 +309,7 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
     } else if (warp >= 4) {
         const int quarter = warp & 3, half = (warp - 4) >> 2;
 #pragma unroll
-        for (int i = 0; i < kSums / 2; i++) sum[i] = 0;
+        for (int i = 0; i < kSums; i++) sum[i] = 0.f;
         Ring16<C::kAccs> acc;
         Ring16<2> set;
         for (int b = b0; b < b1; b++, acc.next()) {
@@ -367,7 +337,7 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
                 for (int c = 0; c < C::kCols; c += 16) {
                     float v[16];
 #pragma unroll
-                    for (int e = 0; e < 16; e += 2) unpair32(sum[(c + e) / 2], v[e], v[e + 1]);
+                    for (int e = 0; e < 16; e++) v[e] = sum[c + e];
                     const int col = n0 + half * C::kCols + c;
                     if (MODE != SCALE_COLS) store_row16(p, m0 + in, col, p.n, v);
                     else
@@ -380,12 +350,7 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
             // All MMAs of this CTA are done, so its operands' place is free.
             float *mine = reinterpret_cast<float *>(smem) + in;
 #pragma unroll
-            for (int c = 0; c < C::kCols; c += 2) {
-                float x, y;
-                unpair32(sum[c / 2], x, y);
-                mine[(half * C::kCols + c) * C::kPitch] = x;
-                mine[(half * C::kCols + c + 1) * C::kPitch] = y;
-            }
+            for (int c = 0; c < C::kCols; c++) mine[(half * C::kCols + c) * C::kPitch] = sum[c];
         }
     }
     __syncwarp();
@@ -427,9 +392,18 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
 
 // ---------------------------------------------------------------------------------------- persistent: many tiles
 
+// A wait that mostly need not wait: one look, which is sooner done than a suspending poll.  (64 looks before it are slower: 8192 x 4096 x 4096 138 -> 146 us.)
+__device__ __forceinline__ bool seen_or_wait(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t *status, uint64_t limit, uint32_t where)
+{
+    return __all_sync(0xFFFFFFFFu, mbar_look<false>(bar, parity)) || warp_wait(bar, parity, abort_flag, status, limit, where);
+}
+
 // Single CTAs with tiles of 128 x 128, or pairs (cta_group::2) with tiles of 256 x 256 of which each CTA has 128 rows and loads half of B's: 32 KB of operands then feed
-// 2 x 128 x 256 x 128 operations, in 512 cycles of the tensor core, which is what L2 delivers.  Warps: 0, 3 TMA producers of A and B, 1 MMA issuer, 2 scales, 4 and up epilogue, each with 32 rows x half
-// of the columns: with 128 sums a thread they need more registers than 12 warps' share, which the others give.
+// 2 x 128 x 256 x 128 operations, in 512 cycles of the tensor core, which is what L2 delivers at best.  Warps: 0 TMA producer, 1 MMA issuer, 2 scales, 3 caller, 4 and up epilogue, each
+// with 32 rows x half of the columns: with 128 sums a thread they need more registers than 12 warps' share, which the others give.
+// What counts is how soon an accumulator is read and handed back, since a pair has two and a block's MMAs take 512 cycles.  Waiting for an mbarrier takes a warp some 300 cycles even where it has completed, and the
+// polls of eight of them hold up everything else that goes through shared memory: only the caller polls, and lets the epilogue go through named barriers, one for each half of its
+// warps and accumulator.
 template <int CTAS, int MODE>
 struct CfgP {
     static constexpr int kBN = 128 * CTAS, kThreads = 384;
@@ -438,11 +412,12 @@ struct CfgP {
     static constexpr int kStages = 5;
     static constexpr int kOperands = kStages * kStageBytes;
     static constexpr int kAccs = 4 / CTAS, kTmemCols = 512;
+    static constexpr int kCalled = 128 + 32;                               // threads of a named barrier: half of the epilogue, and the caller
     static constexpr int kColScales = MODE == SCALE_BOTH ? kBN : 0;        // else one for each block of 128 columns
     static constexpr int kAhead = 4, kScales = kAhead * (128 + kBN);
     static constexpr int kStaging = 4096;                                  // of an epilogue warp: a box of 32 rows x 128 bytes
     static constexpr int kSmem = 1024 + kOperands + 8 * kStaging + 2 * kScales * 4 + 512;
-    static constexpr int kFewRegs = 72, kManyRegs = 216;
+    static constexpr int kFewRegs = 88, kManyRegs = 208;
     static_assert(128 * kFewRegs + 256 * kManyRegs <= 384 * 168, "registers: what the epilogue takes is what the other warps give");
     static_assert(kSmem <= 227 * 1024, "shared memory budget");
 };
@@ -504,24 +479,30 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kFewRegs));
-        if (warp == 0 || warp == 3) {
-            const bool issuer = elect_one(), a_side = warp == 0;
-            const uint32_t to0 = smem_u32(a_side ? smem_a : smem_b), lead = CTAS == 2 ? cluster_addr(bar_full, 0) : bar_full;
+        if (warp == 0) {
+            const bool issuer = elect_one();
+            const uint32_t a0 = smem_u32(smem_a), b0 = smem_u32(smem_b), lead = CTAS == 2 ? cluster_addr(bar_full, 0) : bar_full;
             Ring16<C::kStages> ring;
             uint32_t loads = 0, issued = 0;
             bool ok = true;
             for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step) {
                 int m0, n0;
                 place(tile, m0, n0);
-                const int row = a_side ? m0 : n0 + (CTAS == 2 ? rank * 128 : 0);
+                if (CTAS == 2) n0 += rank * 128;
                 for (int b = 0; b < blocks; b++, ring.next()) {
                     if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) { ok = false; break; }
                     issued++;
-                    expect_tx_if(bar_full + 8 * ring.slot, C::kStageBytes * CTAS, issuer && a_side && rank == 0);
-                    if (issuer && (withhold == 0u || !a_side || ++loads != withhold)) {
-                        const uint32_t to = to0 + ring.slot * C::kABytes;
-                        if (CTAS == 2) tma_load_2d_pair(to, a_side ? &maps.a : &maps.b, b * kBlock8, row, lead + 8 * ring.slot);
-                        else tma_load_2d(to, a_side ? &maps.a : &maps.b, b * kBlock8, row, lead + 8 * ring.slot);
+                    const uint32_t bar = lead + 8 * ring.slot, at = ring.slot * C::kABytes;
+                    expect_tx_if(bar_full + 8 * ring.slot, C::kStageBytes * CTAS, issuer && rank == 0);
+                    if (issuer) {
+                        const bool with_a = withhold == 0u || ++loads != withhold;
+                        if (CTAS == 2) {
+                            if (with_a) tma_load_2d_pair(a0 + at, &maps.a, b * kBlock8, m0, bar);
+                            tma_load_2d_pair(b0 + at, &maps.b, b * kBlock8, n0, bar);
+                        } else {
+                            if (with_a) tma_load_2d(a0 + at, &maps.a, b * kBlock8, m0, bar);
+                            tma_load_2d(b0 + at, &maps.b, b * kBlock8, n0, bar);
+                        }
                     }
                     __syncwarp();
                 }
@@ -538,8 +519,8 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
             bool ok = true;
             for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step)
                 for (int b = 0; b < blocks; b++, ring.next(), acc.next()) {
-                    ok = warp_wait<CTAS == 2>(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u) &&
-                         warp_wait(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot);
+                    ok = seen_or_wait(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot) &&
+                         seen_or_wait(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u);
                     if (!ok) break;
                     tcgen05_fence_after();
 #pragma unroll
@@ -550,24 +531,55 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
                     tcgen05_commit_if<CTAS>(bar_empty + 8 * ring.slot, issuer);
                 }
         } else if (warp == 2) {
+            // The scales of four blocks at a time, loaded while the set before waits for its place.
+            constexpr int kR = 4, kC = C::kColScales / 32;
             Ring16<2> set;
             bool ok = true;
             for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step) {
                 int m0, n0;
                 place(tile, m0, n0);
                 for (int b = 0; b < blocks; b += C::kAhead, set.next()) {
+                    float4 r[kR], c[kC ? kC : 1];
+                    const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int j = 0; j < kR; j++) r[j] = m0 + lane + 32 * j < p.m ? p.sa.four(m0 + lane + 32 * j, b, blocks) : none;
+#pragma unroll
+                    for (int j = 0; j < kC; j++) c[j] = n0 + lane + 32 * j < p.n ? p.sb.four(n0 + lane + 32 * j, b, blocks) : none;
+                    float one = 0.f;   // lane: a block of the contraction and one of the columns
+                    if (MODE == SCALE_ROWS && lane < C::kAhead * CTAS && b + lane / CTAS < blocks && n0 + 128 * (lane % CTAS) < p.n) one = p.sb.at(n0 + 128 * (lane % CTAS), b + lane / CTAS);
                     ok = warp_wait(bar_sc_empty + 8 * set.slot, set.phase ^ 1u, abort_flag, p.status, limit, 0x400u);
                     if (!ok) break;
                     float *to = scales + set.slot * C::kScales;
-                    load_scales<SCALE_BOTH, C::kAhead, 128, C::kColScales>(p, m0, n0, b, blocks, to);
-                    if (MODE == SCALE_ROWS && lane < C::kAhead * CTAS) {   // lane: a block of columns and one of the contraction
-                        const int i = lane / CTAS, j = lane % CTAS;
-                        to[C::kAhead * 128 + lane] = b + i < blocks && n0 + 128 * j < p.n ? p.sb.at(n0 + 128 * j, b + i) : 0.f;
+#pragma unroll
+                    for (int j = 0; j < kR; j++) {
+                        float *at = to + lane + 32 * j;
+                        at[0] = r[j].x; at[128] = r[j].y; at[256] = r[j].z; at[384] = r[j].w;
                     }
+#pragma unroll
+                    for (int j = 0; j < kC; j++) {
+                        float *at = to + C::kAhead * 128 + lane + 32 * j;
+                        at[0] = c[j].x; at[C::kColScales] = c[j].y; at[2 * C::kColScales] = c[j].z; at[3 * C::kColScales] = c[j].w;
+                    }
+                    if (MODE == SCALE_ROWS && lane < C::kAhead * CTAS) to[C::kAhead * 128 + lane] = one;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar_sc_full + 8 * set.slot);
                 }
             }
+        } else if (warp == 3) {
+            Ring16<C::kAccs> acc;
+            Ring16<2> set;
+            bool ok = true;
+            for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step)
+                for (int b = 0; ok && b < blocks; b++, acc.next()) {
+                    if (b % C::kAhead == 0) {
+                        ok = warp_wait(bar_sc_full + 8 * set.slot, set.phase, abort_flag, p.status, limit, 0x500u);
+                        set.next();
+                    }
+                    ok = ok && warp_wait(bar_acc_full + 8 * acc.slot, acc.phase, abort_flag, p.status, limit, 0x600u);
+                    // Where a wait has run out, the abort flag is set: the epilogue is called all the same, and leaves.
+                    asm volatile("bar.arrive %0, %1;" ::"r"(1 + acc.slot), "n"(C::kCalled) : "memory");
+                    asm volatile("bar.arrive %0, %1;" ::"r"(1 + C::kAccs + acc.slot), "n"(C::kCalled) : "memory");
+                }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kManyRegs));
@@ -580,16 +592,20 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
         for (int tile = blockIdx.x / CTAS; tile < tiles; tile += step) {
             int m0, n0;
             place(tile, m0, n0);
-            uint64_t sum[C::kCols / 2];
+            float sum[C::kCols];
 #pragma unroll
-            for (int i = 0; i < C::kCols / 2; i++) sum[i] = 0;
+            for (int i = 0; i < C::kCols; i++) sum[i] = 0.f;
             for (int b = 0; b < blocks; b++, acc.next()) {
                 const int i = b % C::kAhead;
-                ok = (i != 0 || warp_wait(bar_sc_full + 8 * set.slot, set.phase, abort_flag, p.status, limit, 0x500u)) &&
-                     warp_wait(bar_acc_full + 8 * acc.slot, acc.phase, abort_flag, p.status, limit, 0x600u);
-                if (!ok) break;
-                tcgen05_fence_after();
                 const float *from = scales + set.slot * C::kScales;
+                asm volatile("bar.sync %0, %1;" ::"r"(1 + half * C::kAccs + acc.slot), "n"(C::kCalled) : "memory");
+                ok = __all_sync(0xFFFFFFFFu, *abort_flag == 0u);
+                if (!ok) {   // whoever of this half did not see it yet waits at the next barrier, and sees it behind that
+                    acc.next();
+                    asm volatile("bar.arrive %0, %1;" ::"r"(1 + half * C::kAccs + acc.slot), "n"(C::kCalled) : "memory");
+                    break;
+                }
+                tcgen05_fence_after();
                 float row = from[i * 128 + 32 * quarter + lane];
                 if (MODE == SCALE_ROWS) row *= from[C::kAhead * 128 + i * CTAS + (CTAS == 2 ? half : 0)];
                 add_block<MODE, C::kCols>(sum, tmem + acc.slot * C::kBN + half * C::kCols + ((uint32_t)(32 * quarter) << 16), row, from + C::kAhead * 128 + i * C::kColScales + half * C::kCols, [&] {
@@ -614,7 +630,7 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
                 for (int c = 0; c < C::kCols; c += 32) {
                     float v[32];
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) unpair32(sum[(c + e) / 2], v[e], v[e + 1]);
+                    for (int e = 0; e < 32; e++) v[e] = sum[c + e];
                     send_box<32>(p, &maps.out, box, box_at, reinterpret_cast<const uint32_t *>(v), row0, col0 + c, lane, [&](int e) { return v[e]; });
                 }
             } else {
@@ -622,11 +638,7 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
                 for (int c = 0; c < C::kCols; c += 64) {
                     uint32_t w[32];
 #pragma unroll
-                    for (int e = 0; e < 32; e++) {
-                        float x, y;
-                        unpair32(sum[c / 2 + e], x, y);
-                        w[e] = pack_bf16(x, y);
-                    }
+                    for (int e = 0; e < 32; e++) w[e] = pack_bf16(sum[c + 2 * e], sum[c + 2 * e + 1]);
                     send_box<64>(p, &maps.out, box, box_at, w, row0, col0 + c, lane, [&](int e) { return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16); });
                 }
             }
@@ -793,6 +805,7 @@ fp4q_status operand8(const fp4q_fp8_tensor &t, bool transposed, bool square, Ope
     o.scales.row = transposed && square ? 1 : ld;
     o.scales.block = transposed && square ? ld : 1;
     o.scales.shift = square ? 7 : 0;
+    o.scales.fours = o.scales.block == 1 && o.scales.row % 4 == 0 && aligned(o.scales.p, 16);
     if (o.rows == 0 || o.cols == 0) return FP4Q_OK;
     if (!o.q || !o.scales.p) return FP4Q_ERR_NULL;
     if (o.ld < o.cols || ld < ceil_div(square ? t.cols : o.cols, kBlock8)) return FP4Q_ERR_SHAPE;
