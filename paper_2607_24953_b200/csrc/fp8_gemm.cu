@@ -75,33 +75,37 @@ __device__ __forceinline__ void landed(uint32_t (&v)[16])
                  :: "memory");
 }
 
-// sum += a block's product times its scales, for COLS columns of a thread's row.  row_scale: of the row; cols: of the columns, in shared memory.  read: called when the accumulator
-// has been read.  (Additions in pairs, fma.rn.f32x2, would halve the instructions, but every value is then moved into an aligned pair first: 8192 x 4096 x 4096 194 us for 147.)
+__device__ __forceinline__ void load_scales_16(uint32_t at, float (&f)[16])   // in shared memory, on 16 bytes; stays behind the barrier before it
+{
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f[e]), "=f"(f[e + 1]), "=f"(f[e + 2]), "=f"(f[e + 3]) : "r"(at + 4 * e));
+}
+__device__ __forceinline__ float load_scale(uint32_t at)
+{
+    float f;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(at));
+    return f;
+}
+
+// sum += a block's product times its scales, for COLS columns of a thread's row.  row: the row's scale; cols: where those of the columns lie in shared memory.  read: called when the
+// accumulator has been read.  The scales are put together while the accumulator's values are on their way.  (Additions in pairs, fma.rn.f32x2, would halve the instructions, but
+// every value is then moved into an aligned pair first: 8192 x 4096 x 4096 194 us for 147.)
 template <int MODE, int COLS, typename F>
-__device__ __forceinline__ void add_block(float (&sum)[COLS], uint32_t from, float row_scale, const float *cols, F read)
+__device__ __forceinline__ void add_block(float (&sum)[COLS], uint32_t from, float row, uint32_t cols, F read)
 {
 #pragma unroll
     for (int c = 0; c < COLS; c += 16) {
         uint32_t x[16];
+        float f[16];
         load_acc(from + c, x);
+        if (MODE != SCALE_ROWS) load_scales_16(cols + 4 * c, f);
+        if (MODE == SCALE_BOTH)
+#pragma unroll
+            for (int e = 0; e < 16; e++) f[e] *= row;
         landed(x);
         if (c + 16 == COLS) read();
 #pragma unroll
-        for (int e = 0; e < 16; e += 4) {
-            float f[4];
-            if (MODE != SCALE_ROWS) {
-                const float4 g = *reinterpret_cast<const float4 *>(cols + c + e);
-                f[0] = g.x; f[1] = g.y; f[2] = g.z; f[3] = g.w;
-            }
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                const float v = __uint_as_float(x[e + j]);
-                float &to = sum[c + e + j];
-                if (MODE == SCALE_ROWS) to = fmaf(v, row_scale, to);
-                else if (MODE == SCALE_COLS) to = fmaf(v, f[j], to);
-                else to = fmaf(v * f[j], row_scale, to);
-            }
-        }
+        for (int e = 0; e < 16; e++) sum[c + e] = fmaf(__uint_as_float(x[e]), MODE == SCALE_ROWS ? row : f[e], sum[c + e]);
     }
 }
 
@@ -317,9 +321,9 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
             if (i == 0 && !warp_wait(bar_sc_full + 8 * set.slot, set.phase, abort_flag, p.status, limit, 0x500u)) break;
             if (!warp_wait(bar_acc_full + 8 * acc.slot, acc.phase, abort_flag, p.status, limit, 0x600u)) break;
             tcgen05_fence_after();
-            const float *from = scales + set.slot * C::kScales;
-            const float row = C::kRowScales ? from[i * C::kRowScales + 32 * quarter + lane] : 1.f;
-            add_block<MODE, C::kCols>(sum, tmem + acc.slot * BN + half * C::kCols + ((uint32_t)(32 * quarter) << 16), row, from + C::kAhead * C::kRowScales + i * C::kColScales + half * C::kCols, [&] {
+            const uint32_t from = smem_u32(scales + set.slot * C::kScales);
+            const float row = C::kRowScales ? load_scale(from + 4 * (i * C::kRowScales + 32 * quarter + lane)) : 1.f;
+            add_block<MODE, C::kCols>(sum, tmem + acc.slot * BN + half * C::kCols + ((uint32_t)(32 * quarter) << 16), row, from + 4 * (C::kAhead * C::kRowScales + i * C::kColScales + half * C::kCols), [&] {
                 tcgen05_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_acc_empty + 8 * acc.slot);
@@ -597,7 +601,7 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
             for (int i = 0; i < C::kCols; i++) sum[i] = 0.f;
             for (int b = 0; b < blocks; b++, acc.next()) {
                 const int i = b % C::kAhead;
-                const float *from = scales + set.slot * C::kScales;
+                const uint32_t from = smem_u32(scales + set.slot * C::kScales);
                 asm volatile("bar.sync %0, %1;" ::"r"(1 + half * C::kAccs + acc.slot), "n"(C::kCalled) : "memory");
                 ok = __all_sync(0xFFFFFFFFu, *abort_flag == 0u);
                 if (!ok) {   // whoever of this half did not see it yet waits at the next barrier, and sees it behind that
@@ -606,9 +610,9 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
                     break;
                 }
                 tcgen05_fence_after();
-                float row = from[i * 128 + 32 * quarter + lane];
-                if (MODE == SCALE_ROWS) row *= from[C::kAhead * 128 + i * CTAS + (CTAS == 2 ? half : 0)];
-                add_block<MODE, C::kCols>(sum, tmem + acc.slot * C::kBN + half * C::kCols + ((uint32_t)(32 * quarter) << 16), row, from + C::kAhead * 128 + i * C::kColScales + half * C::kCols, [&] {
+                float row = load_scale(from + 4 * (i * 128 + 32 * quarter + lane));
+                if (MODE == SCALE_ROWS) row *= load_scale(from + 4 * (C::kAhead * 128 + i * CTAS + (CTAS == 2 ? half : 0)));
+                add_block<MODE, C::kCols>(sum, tmem + acc.slot * C::kBN + half * C::kCols + ((uint32_t)(32 * quarter) << 16), row, from + 4 * (C::kAhead * 128 + i * C::kColScales + half * C::kCols), [&] {
                     tcgen05_fence_before();
                     __syncwarp();
                     if (lane == 0) {
