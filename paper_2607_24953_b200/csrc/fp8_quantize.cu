@@ -26,13 +26,51 @@ __device__ __forceinline__ const RowsOf<T> &source(const Fp8QuantParams &p)
     else return p.b16;
 }
 
+// Magnitudes: packed pairs of BF16, or FP32.  Infinity where there is one; NaN does not count.
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b)
+{
+    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&m);
+}
+__device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
+__device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
+
+// Maxima of a lane's four rows and, over these, of its columns.
+template <typename T>
+__device__ __forceinline__ void maxima(const Raw16<T> (&x)[4], float (&rows)[4], uint32_t (&cols)[Raw16<T>::kWords])
+{
+#pragma unroll
+    for (int k = 0; k < Raw16<T>::kWords; k++) cols[k] = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        uint32_t pair = 0u;
+        float m = 0.f;
+#pragma unroll
+        for (int k = 0; k < Raw16<T>::kWords; k++) {
+            if constexpr (sizeof(T) == 2) {
+                const uint32_t a = x[i].w[k] & 0x7FFF7FFFu;
+                pair = max_pair(pair, a);
+                cols[k] = max_pair(cols[k], a);
+            } else {
+                const float a = fabsf(x[i][k]);
+                m = fmaxf(m, a);
+                cols[k] = __float_as_uint(fmaxf(__uint_as_float(cols[k]), a));
+            }
+        }
+        rows[i] = sizeof(T) == 2 ? fmaxf(low(pair), high(pair)) : m;
+    }
+}
+
 template <typename T, bool SQUARE>
-__global__ void __launch_bounds__(256) fp8_quantize_kernel(const __grid_constant__ Fp8QuantParams p)
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) fp8_quantize_kernel(const __grid_constant__ Fp8QuantParams p)
 {
     wait_for_predecessor();
     admit_successor();
     __shared__ uint4 stage[128 * 8];      // 128 columns x 128 bytes
-    __shared__ float tops[8][128], factors[128];
+    __shared__ float tops[8][128];
+    __shared__ __align__(16) float factors[128];
+    constexpr bool kPairs = sizeof(T) == 2;
+    constexpr int W = Raw16<T>::kWords;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cg = lane & 7, rg = lane >> 3;
     const int64_t by = blockIdx.x / p.col_tiles, bx = blockIdx.x - by * p.col_tiles;
     const int64_t row0 = by * 128 + warp * 16 + rg * 4, col0 = bx * 128 + cg * 16;
@@ -41,41 +79,57 @@ __global__ void __launch_bounds__(256) fp8_quantize_kernel(const __grid_constant
 #pragma unroll
     for (int i = 0; i < 4; i++) x[i] = load_row16<T>(source<T>(p), row0 + i < p.rows ? row0 + i : 0, row0 + i < p.rows ? col0 : p.cols, p.cols);
 
-    float row_top[4], all = 0.f;   // infinity where there is one; NaN does not count
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        float m = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; e++) m = fmaxf(m, fabsf(x[i][e]));
-        row_top[i] = m;
-        all = fmaxf(all, m);
-    }
-    const bool careful = __syncthreads_or(is_infinite(all));   // maxima of finite elements only
+    float row_top[4];
+    uint32_t col_top[W];
+    maxima(x, row_top, col_top);
+    float all = fmaxf(fmaxf(row_top[0], row_top[1]), fmaxf(row_top[2], row_top[3]));
+    const bool careful = __syncthreads_or(is_infinite(all));   // maxima of finite elements only; infinities become NaN, which they are from here on
     if (careful) {
-        all = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            float m = 0.f;
-#pragma unroll
-            for (int e = 0; e < 16; e++) m = fmaxf(m, finite_size(x[i][e]));
-            row_top[i] = m;
-            all = fmaxf(all, m);
-        }
-    }
-    if (!SQUARE) {
 #pragma unroll
         for (int i = 0; i < 4; i++)
 #pragma unroll
-            for (int d = 1; d < 8; d <<= 1) row_top[i] = fmaxf(row_top[i], __shfl_xor_sync(0xFFFFFFFFu, row_top[i], d));
+            for (int k = 0; k < W; k++) {
+                uint32_t &w = x[i].w[k];
+                if constexpr (kPairs) {
+                    if ((w & 0x7FFFu) == 0x7F80u) w |= 0x7FFFu;
+                    if ((w & 0x7FFF0000u) == 0x7F800000u) w |= 0x7FFF0000u;
+                } else {
+                    if ((w & 0x7FFFFFFFu) == 0x7F800000u) w |= 0x7FFFFFFFu;
+                }
+            }
+        maxima(x, row_top, col_top);
+        all = fmaxf(fmaxf(row_top[0], row_top[1]), fmaxf(row_top[2], row_top[3]));
+    }
+    float row_factor = 0.f;   // of row cg & 3 of the lane's rows, or of the square block
+    if (!SQUARE) {
+        if (p.out.q) {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int d = 1; d < 8; d <<= 1) row_top[i] = fmaxf(row_top[i], __shfl_xor_sync(0xFFFFFFFFu, row_top[i], d));
+            const int i = cg & 3;
+            const float m = i == 0 ? row_top[0] : i == 1 ? row_top[1] : i == 2 ? row_top[2] : row_top[3];
+            row_factor = fp8_factor(m);
+            if (cg < 4 && row0 + i < p.rows) p.out.scale[(row0 + i) * p.out.ld_s + bx] = fp8_scale(m);
+        }
         if (p.out.q_t) {
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                float m = 0.f;
+            for (int k = 0; k < W; k++) {
+                uint32_t m = col_top[k];
 #pragma unroll
-                for (int i = 0; i < 4; i++) m = fmaxf(m, careful ? finite_size(x[i][e]) : fabsf(x[i][e]));
-                m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
-                m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-                if (rg == (e & 3)) tops[warp][16 * cg + e] = m;
+                for (int d = 8; d < 32; d <<= 1) {
+                    const uint32_t o = __shfl_xor_sync(0xFFFFFFFFu, m, d);
+                    if constexpr (kPairs) m = max_pair(m, o);
+                    else m = __float_as_uint(fmaxf(__uint_as_float(m), __uint_as_float(o)));
+                }
+                if (rg == (k & 3)) {
+                    if constexpr (kPairs) {
+                        tops[warp][16 * cg + 2 * k] = low(m);
+                        tops[warp][16 * cg + 2 * k + 1] = high(m);
+                    } else {
+                        tops[warp][16 * cg + k] = __uint_as_float(m);
+                    }
+                }
             }
             __syncthreads();
             if (threadIdx.x < 128) {
@@ -95,30 +149,32 @@ __global__ void __launch_bounds__(256) fp8_quantize_kernel(const __grid_constant
 #pragma unroll
         for (int w = 1; w < 8; w++) all = fmaxf(all, tops[0][w]);
         if (threadIdx.x == 0) p.out.scale[by * p.out.ld_s + bx] = fp8_scale(all);
+        row_factor = fp8_factor(all);
     }
-    const float whole = SQUARE ? fp8_factor(all) : 0.f;
 
     if (p.out.q) {
 #pragma unroll
         for (int i = 0; i < 4; i++) {
-            if (row0 + i >= p.rows) break;
+            const float f = SQUARE ? row_factor : __shfl_sync(0xFFFFFFFFu, row_factor, i, 4);
             float v[16];
 #pragma unroll
             for (int e = 0; e < 16; e++) v[e] = x[i][e];
-            if (col0 < p.cols) *reinterpret_cast<uint4 *>(p.out.q + (row0 + i) * p.out.ld_q + col0) = fp8_codes(v, SQUARE ? whole : fp8_factor(row_top[i]), careful);
-            if (!SQUARE && cg == 0) p.out.scale[(row0 + i) * p.out.ld_s + bx] = fp8_scale(row_top[i]);
+            const uint4 codes = fp8_codes(v, f, false);
+            if (row0 + i < p.rows && col0 < p.cols) *reinterpret_cast<uint4 *>(p.out.q + (row0 + i) * p.out.ld_q + col0) = codes;
         }
     }
     if (!p.out.q_t) return;
     if (!SQUARE) __syncthreads();   // factors
     uint32_t *words = reinterpret_cast<uint32_t *>(stage);
 #pragma unroll
-    for (int e = 0; e < 16; e++) {
-        const float f = SQUARE ? whole : factors[16 * cg + e];
-        float v[4];
+    for (int e0 = 0; e0 < 16; e0 += 4) {
+        float4 f = make_float4(row_factor, row_factor, row_factor, row_factor);
+        if (!SQUARE) f = *reinterpret_cast<const float4 *>(factors + 16 * cg + e0);
+        const float fs[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-        for (int i = 0; i < 4; i++) v[i] = careful && is_infinite(x[i][e]) ? nan32() : x[i][e] * f;
-        words[(16 * cg + e) * 32 + ((warp ^ cg) << 2) + rg] = cvt_rn_e4m3x4(v[3], v[2], v[1], v[0]);
+        for (int j = 0; j < 4; j++)
+            words[(16 * cg + e0 + j) * 32 + ((warp ^ cg) << 2) + rg] =
+                cvt_rn_e4m3x4(x[3][e0 + j] * fs[j], x[2][e0 + j] * fs[j], x[1][e0 + j] * fs[j], x[0][e0 + j] * fs[j]);
     }
     __syncthreads();
 #pragma unroll

@@ -6,6 +6,7 @@
 #include <cuda_bf16.h>
 
 #include "common.cuh"
+#include "row_io.cuh"
 
 #include <algorithm>
 
@@ -93,6 +94,36 @@ __device__ __forceinline__ float element(const Span &s, const uint32_t (&w)[8], 
     return s.f32 ? __uint_as_float(w[e]) : __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
 }
 
+// A chunk all of whose units are whole and lie behind one another: its first element, else NULL.
+__device__ __forceinline__ const void *solid_chunk(const Span &s, int64_t u0)
+{
+    const uintptr_t skip = (reinterpret_cast<uintptr_t>(s.data) & 15u) >> (s.f32 ? 2 : 1);
+    const int64_t col = u0 * kUnit - (int64_t)skip;
+    if (s.units != s.units_row || col < 0 || col + kChunkUnits * kUnit > s.cols) return nullptr;
+    return static_cast<const uint8_t *>(s.data) + col * (s.f32 ? 4 : 2);
+}
+__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// A run of 32 squares.  One that is normal has lost no square that counts; another one, with squares out of FP32's range, is added up in 64 bits.
+template <typename F>
+__device__ __forceinline__ double sum_run(F value)
+{
+    float run = 0.f;
+#pragma unroll
+    for (int e = 0; e < 32; e++) run = fmaf(value(e), value(e), run);
+    double total = (double)run;
+    if (!(run > 1e-30f && run < 1e38f)) {
+        total = 0.0;
+#pragma unroll
+        for (int e = 0; e < 32; e++) {
+            const double v = (double)value(e);
+            total = fma(v, v, total);
+        }
+    }
+    return total;
+}
+
 template <int N>
 __global__ void __launch_bounds__(256) sum_squares_kernel(const __grid_constant__ SpanParams<N> p)
 {
@@ -103,30 +134,28 @@ __global__ void __launch_bounds__(256) sum_squares_kernel(const __grid_constant_
     for (int64_t chunk = blockIdx.x; chunk < p.chunks; chunk += gridDim.x) {
         const Span &s = p.span[span_of(p, chunk)];
         const int64_t u0 = (chunk - s.chunk0) * kChunkUnits + threadIdx.x;
+        const uint4 *solid = static_cast<const uint4 *>(solid_chunk(s, u0 - threadIdx.x));
+        if (solid) {
+            uint4 v[8];
+            const int n = s.f32 ? 8 : 4;
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                if (k < n) v[k] = load_global(solid + 256 * k + threadIdx.x);
+            if (s.f32) total += sum_run([&](int e) { return __uint_as_float(e % 4 == 0 ? v[e / 4].x : e % 4 == 1 ? v[e / 4].y : e % 4 == 2 ? v[e / 4].z : v[e / 4].w); });
+            else
+                total += sum_run([&](int e) {
+                    const uint32_t w = e / 2 % 4 == 0 ? v[e / 8].x : e / 2 % 4 == 1 ? v[e / 8].y : e / 2 % 4 == 2 ? v[e / 8].z : v[e / 8].w;
+                    return e % 2 ? high(w) : low(w);
+                });
+            continue;
+        }
         uint32_t w[4][8];
 #pragma unroll
         for (int k = 0; k < 4; k++) {
             const int64_t u = u0 + 256 * k;
             load_unit(s, unit_of(s, u), u < s.units, w[k]);
         }
-        float run = 0.f;
-#pragma unroll
-        for (int k = 0; k < 4; k++)
-#pragma unroll
-            for (int e = 0; e < kUnit; e++) {
-                const float v = element(s, w[k], e);
-                run = fmaf(v, v, run);
-            }
-        // A run that is normal has lost no square that counts; another one, with squares out of FP32's range, is added up in 64 bits.
-        if (run > 1e-30f && run < 1e38f) total += (double)run;
-        else
-#pragma unroll
-            for (int k = 0; k < 4; k++)
-#pragma unroll
-                for (int e = 0; e < kUnit; e++) {
-                    const double v = (double)element(s, w[k], e);
-                    total = fma(v, v, total);
-                }
+        total += sum_run([&](int e) { return element(s, w[e / 8], e % 8); });
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, d);
@@ -173,6 +202,34 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Span
         const int64_t chunk = p.chunks - 1 - back;
         const Span &s = p.span[span_of(p, chunk)];
         const int64_t u0 = (chunk - s.chunk0) * kChunkUnits + threadIdx.x;
+        const uint4 *solid = static_cast<const uint4 *>(solid_chunk(s, u0 - threadIdx.x));
+        const int64_t start = solid ? (reinterpret_cast<uintptr_t>(solid) - reinterpret_cast<uintptr_t>(s.data)) >> (s.f32 ? 2 : 1) : 0;
+        uint8_t *to = static_cast<uint8_t *>(s.out) + start * (s.out_f32 ? 4 : 2);
+        if (solid && (reinterpret_cast<uintptr_t>(to) & 15u) == 0u) {
+            uint4 v[8];
+            const int n = s.f32 ? 8 : 4;
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                if (k < n) v[k] = load_global(solid + 256 * k + threadIdx.x);
+#pragma unroll
+            for (int k = 0; k < 8; k++) {
+                if (k >= n) break;
+                const int at = 256 * k + threadIdx.x;
+                const uint32_t *w = reinterpret_cast<const uint32_t *>(&v[k]);
+                if (s.f32) {
+                    const float a = __uint_as_float(w[0]) * factor, b = __uint_as_float(w[1]) * factor, c = __uint_as_float(w[2]) * factor, d = __uint_as_float(w[3]) * factor;
+                    if (s.out_f32) reinterpret_cast<float4 *>(to)[at] = make_float4(a, b, c, d);
+                    else reinterpret_cast<uint2 *>(to)[at] = make_uint2(pack_pair(a, b), pack_pair(c, d));
+                } else if (s.out_f32) {
+                    reinterpret_cast<float4 *>(to)[2 * at] = make_float4(low(w[0]) * factor, high(w[0]) * factor, low(w[1]) * factor, high(w[1]) * factor);
+                    reinterpret_cast<float4 *>(to)[2 * at + 1] = make_float4(low(w[2]) * factor, high(w[2]) * factor, low(w[3]) * factor, high(w[3]) * factor);
+                } else {
+                    reinterpret_cast<uint4 *>(to)[at] = make_uint4(pack_pair(low(w[0]) * factor, high(w[0]) * factor), pack_pair(low(w[1]) * factor, high(w[1]) * factor),
+                                                                   pack_pair(low(w[2]) * factor, high(w[2]) * factor), pack_pair(low(w[3]) * factor, high(w[3]) * factor));
+                }
+            }
+            continue;
+        }
         uint32_t w[4][8];
 #pragma unroll
         for (int k = 0; k < 4; k++) {
@@ -187,9 +244,9 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Span
             float v[kUnit];
 #pragma unroll
             for (int e = 0; e < kUnit; e++) v[e] = element(s, w[k], e) * factor;
-            const int64_t to = at.row * s.ld_out + at.col;
+            const int64_t where = at.row * s.ld_out + at.col;
             if (s.out_f32) {
-                float *o = static_cast<float *>(s.out) + to;
+                float *o = static_cast<float *>(s.out) + where;
                 if (at.whole && (reinterpret_cast<uintptr_t>(o) & 15u) == 0u) {
                     reinterpret_cast<float4 *>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
                     reinterpret_cast<float4 *>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
@@ -199,14 +256,11 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Span
                         if (at.col + e >= 0 && at.col + e < s.cols) o[e] = v[e];
                 }
             } else {
-                __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(s.out) + to;
+                __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(s.out) + where;
                 if (at.whole && (reinterpret_cast<uintptr_t>(o) & 15u) == 0u) {
                     uint32_t b[4];
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const __nv_bfloat162 pair = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
-                        b[e] = *reinterpret_cast<const uint32_t *>(&pair);
-                    }
+                    for (int e = 0; e < 4; e++) b[e] = pack_pair(v[2 * e], v[2 * e + 1]);
                     *reinterpret_cast<uint4 *>(o) = make_uint4(b[0], b[1], b[2], b[3]);
                 } else {
 #pragma unroll

@@ -76,7 +76,7 @@ __device__ __forceinline__ float team_sum(float v, int team, float (*red)[32], i
 struct NormParams {
     int64_t rows, cols;
     int32_t team, format;
-    float eps;
+    float eps, inv_cols;
     const void *residual;
     RowsOf<__nv_bfloat16> xb, rb, hb, yb;
     RowsOf<float> xf, rf, hf, yf;
@@ -95,8 +95,48 @@ __device__ __forceinline__ const RowsOf<T> &either(const RowsOf<__nv_bfloat16> &
     else return b;
 }
 
+// Codes and scale of 16 elements where a block holds infinities (or, MXFP8, NaN): maxima of finite elements only.  Out of line; whole warps come here.
+__device__ __noinline__ uint4 careful_codes(const float *y, int lanes, bool mx, float *scale)
+{
+    float v[16], top = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+        v[e] = y[e];
+        top = fmaxf(top, finite_size(v[e]));
+    }
+    for (int d = lanes >> 1; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    if (!mx) {
+        *scale = fp8_scale(top);
+        return fp8_codes(v, fp8_factor(top), true);
+    }
+#pragma unroll
+    for (int e = 0; e < 16; e++) v[e] = v[e] == v[e] ? v[e] : 0.f;   // as the MXFP8 quantizers: NaN becomes 0, infinities the largest number
+    const int code = mx_scale_code(top);
+    *scale = __int_as_float(code);
+    return fp8_codes(v, inv_scale(code), false);
+}
+
+// A stream of BF16 on BF16 is added two elements at a time: the FP32 sum of two BF16 numbers is exact, or so far from a tie that it is rounded like the exact one.
+template <typename TX, typename TH>
+__device__ __forceinline__ void add_rows(const Raw16<TX> &x, Raw16<TH> &r)
+{
+    if constexpr (sizeof(TX) == 2 && sizeof(TH) == 2) {
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            const __nv_bfloat162 s = __hadd2(*reinterpret_cast<const __nv_bfloat162 *>(&x.w[k]), *reinterpret_cast<const __nv_bfloat162 *>(&r.w[k]));
+            r.w[k] = *reinterpret_cast<const uint32_t *>(&s);
+        }
+    } else {
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; e++) v[e] = x[e] + r[e];
+        r.set(v);
+    }
+}
+
+// Without a residual TX is TH.
 template <typename TX, typename TH, int CHUNKS>
-__global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(const __grid_constant__ NormParams p)
+__global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512, CHUNKS == 1 ? 2 : 1) rms_norm_kernel(const __grid_constant__ NormParams p)
 {
     wait_for_predecessor();
     admit_successor();
@@ -107,44 +147,38 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(cons
     const int64_t i = exists ? row : 0, cols = p.cols, n = exists ? cols : 0;
     auto col_of = [&](int c) { return ((int64_t)c * team + in) * 16; };
 
-    float h[CHUNKS][16];
+    Raw16<TH> h[CHUNKS];   // as it is rounded: what the backward pass reads
     float squares = 0.f;
-    {
+    if (p.residual) {
         Raw16<TX> x[CHUNKS];
-        Raw16<TH> r[CHUNKS];
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
             x[c] = load_row16<TX>(either<TX>(p.xb, p.xf), i, col_of(c), n);
-            if (p.residual) r[c] = load_row16<TH>(either<TH>(p.rb, p.rf), i, col_of(c), n);
+            h[c] = load_row16<TH>(either<TH>(p.rb, p.rf), i, col_of(c), n);
         }
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            if (p.residual) {
-                float v[16];
-#pragma unroll
-                for (int e = 0; e < 16; e++) v[e] = x[c][e] + r[c][e];
-                r[c].set(v);
-                store_row16<TH>(either<TH>(p.hb, p.hf), i, col_of(c), cols, r[c], lanes, exists);
-#pragma unroll
-                for (int e = 0; e < 16; e++) h[c][e] = r[c][e];   // as it was rounded: what the backward pass reads
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; e++) h[c][e] = x[c][e];
-            }
-#pragma unroll
-            for (int e = 0; e < 16; e++) squares = fmaf(h[c][e], h[c][e], squares);
+            add_rows<TX, TH>(x[c], h[c]);
+            store_row16<TH>(either<TH>(p.hb, p.hf), i, col_of(c), cols, h[c], lanes, exists);
         }
+    } else {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; c++) h[c] = load_row16<TH>(either<TH>(p.xb, p.xf), i, col_of(c), n);
     }
-    const float mean = __fdiv_rn(team_sum(squares, team, red, 0), (float)cols), rstd = __frcp_rn(__fsqrt_rn(mean + p.eps));
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) squares = fmaf(h[c][e], h[c][e], squares);
+    const float mean = team_sum(squares, team, red, 0) * p.inv_cols, rstd = __frcp_rn(__fsqrt_rn(mean + p.eps));
     if (p.rstd && exists && in == 0) p.rstd[row] = rstd;
 
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
         const int64_t col = col_of(c);
-        float w[16], v[16];
-        p.weight.load(col, cols, w);
+        float v[16];
+        p.weight.load(col, cols, v);
 #pragma unroll
-        for (int e = 0; e < 16; e++) v[e] = __fmul_rn(__fmul_rn(h[c][e], rstd), w[e]);
+        for (int e = 0; e < 16; e++) v[e] = __fmul_rn(__fmul_rn(h[c][e], rstd), v[e]);
         if (p.yb.p && !p.y_f32) {
             Raw16<__nv_bfloat16> y;
             y.set(v);
@@ -155,39 +189,38 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(cons
             store_row16<float>(p.yf, i, col, cols, y, lanes, exists);
         }
         if (p.format == 0) continue;
-        float top = 0.f;   // infinity where there is one; NaN does not count
-        if (col < n) {
-#pragma unroll
-            for (int e = 0; e < 16; e++) top = fmaxf(top, col + e < cols ? fabsf(v[e]) : 0.f);
-        }
-        const bool careful = __any_sync(0xFFFFFFFFu, is_infinite(top));
-        if (careful && col < n) {
-            top = 0.f;
-#pragma unroll
-            for (int e = 0; e < 16; e++) top = fmaxf(top, col + e < cols ? finite_size(v[e]) : 0.f);
-        }
-        if (col + 16 > cols) {   // what is behind the row's end: its codes are 0
+        if (!exists || col + 16 > cols) {   // what is behind the row's end: its codes are 0
 #pragma unroll
             for (int e = 0; e < 16; e++)
-                if (col + e >= cols) v[e] = 0.f;
+                if (!exists || col + e >= cols) v[e] = 0.f;
         }
-        if (p.format == FP4Q_NORM_FP8) {
-            for (int d = min(team, 8) >> 1; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-            const uint4 codes = fp8_codes(v, fp8_factor(top), careful);
-            if (exists && col < cols) {
-                *reinterpret_cast<uint4 *>(p.q + row * p.ld_q + col) = codes;
-                if (col % 128 == 0) static_cast<float *>(p.scale)[row * p.ld_s + col / 128] = fp8_scale(top);
-            }
-        } else {
-            if (team > 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            const int code = mx_scale_code(top);
+        float top = 0.f;   // infinity where there is one; NaN does not count
 #pragma unroll
-            for (int e = 0; e < 16; e++) v[e] = v[e] == v[e] ? v[e] : 0.f;   // as the MXFP8 quantizers: NaN becomes 0, infinities the largest number
-            const uint4 codes = fp8_codes(v, inv_scale(code), false);
-            if (exists && col < (cols + 31) / 32 * 32) {
-                *reinterpret_cast<uint4 *>(p.q + row * p.ld_q + col) = codes;
-                if (col % 32 == 0) static_cast<uint8_t *>(p.scale)[row * p.ld_s + col / 32] = (uint8_t)code;
-            }
+        for (int e = 0; e < 16; e++) top = fmaxf(top, fabsf(v[e]));
+        const bool mx = p.format == FP4Q_NORM_MXFP8;
+        bool odd = is_infinite(top);
+        if (mx) {
+#pragma unroll
+            for (int e = 0; e < 16; e++) odd |= v[e] != v[e];
+        }
+        const int block = mx ? min(team, 2) : min(team, 8);   // lanes of a block
+        float scale;
+        uint4 codes;
+        if (__any_sync(0xFFFFFFFFu, odd)) {
+            codes = careful_codes(v, block, mx, &scale);
+        } else {
+            for (int d = block >> 1; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+            const int code = mx ? mx_scale_code(top) : 0;
+            scale = mx ? __int_as_float(code) : top;
+            codes = fp8_codes(v, mx ? inv_scale(code) : fp8_factor(top), false);
+            if (!mx && col % 128 == 0) scale = fp8_scale(top);
+        }
+        if (!exists || col >= (mx ? (cols + 31) / 32 * 32 : cols)) continue;
+        *reinterpret_cast<uint4 *>(p.q + row * p.ld_q + col) = codes;
+        if (mx) {
+            if (col % 32 == 0) static_cast<uint8_t *>(p.scale)[row * p.ld_s + col / 32] = (uint8_t)__float_as_int(scale);
+        } else if (col % 128 == 0) {
+            static_cast<float *>(p.scale)[row * p.ld_s + col / 128] = scale;
         }
     }
 }
@@ -200,6 +233,7 @@ constexpr int64_t kGradFused = 8192;    // columns up to which that is the kerne
 struct GradParams {
     int64_t rows, cols;
     int32_t team;
+    float inv_cols;
     const void *dh;
     RowsOf<__nv_bfloat16> dyb, hb, dhb, dxb;
     RowsOf<float> dyf, hf, dhf, dxf;
@@ -208,7 +242,8 @@ struct GradParams {
     float *partial;          // [CTA][cols]: sums over its rows; NULL: none
 };
 
-// Rows blockIdx.x, blockIdx.x + gridDim.x, ... of teams.  The operations of dx are spelled out, so that it is the same with SUMS and without.
+// Rows blockIdx.x, blockIdx.x + gridDim.x, ... of teams.  The operations of dx are spelled out, so that it is the same with SUMS and without.  With SUMS a CTA has many rows: the next
+// one's elements are on their way while this one's are worked on.
 template <typename TY, typename TH, int CHUNKS, bool SUMS>
 __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(const __grid_constant__ GradParams p)
 {
@@ -228,20 +263,36 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(
             for (int e = 0; e < 16; e++) dw[c][e] = 0.f;
         }
     }
-    int which = 0;
-    for (int64_t first = (int64_t)blockIdx.x * teams; first < p.rows; first += (int64_t)gridDim.x * teams, which ^= 1) {
-        const int64_t row = first + threadIdx.x / team;
-        const bool exists = row < p.rows;
-        const int64_t i = exists ? row : 0, n = exists ? cols : 0;
+    struct Row {
         Raw16<TY> dy[CHUNKS];
         Raw16<TH> h[CHUNKS], dh[CHUNKS];
+        float r;
+    };
+    auto load = [&](Row &to, int64_t row) {
+        const int64_t i = row < p.rows ? row : 0, n = row < p.rows ? cols : 0;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            dy[c] = load_row16<TY>(either<TY>(p.dyb, p.dyf), i, col_of(c), n);
-            h[c] = load_row16<TH>(either<TH>(p.hb, p.hf), i, col_of(c), n);
-            if (p.dh) dh[c] = load_row16<TH>(either<TH>(p.dhb, p.dhf), i, col_of(c), n);
+            to.dy[c] = load_row16<TY>(either<TY>(p.dyb, p.dyf), i, col_of(c), n);
+            to.h[c] = load_row16<TH>(either<TH>(p.hb, p.hf), i, col_of(c), n);
+            if (p.dh) to.dh[c] = load_row16<TH>(either<TH>(p.dhb, p.dhf), i, col_of(c), n);
         }
-        const float r = load_global(p.rstd + i);
+        to.r = n ? load_global(p.rstd + i) : 0.f;
+    };
+    int which = 0;
+    const int64_t mine = (int64_t)blockIdx.x * teams, step = (int64_t)gridDim.x * teams;
+    const int at = threadIdx.x / team;
+    Row next;
+    if (SUMS && mine < p.rows) load(next, mine + at);
+    for (int64_t first = mine; first < p.rows; first += step, which ^= 1) {
+        const int64_t row = first + at;
+        const bool exists = row < p.rows;
+        Row now;
+        if (SUMS) {
+            now = next;
+            if (first + step < p.rows) load(next, row + step);
+        } else {
+            load(now, row);
+        }
         float dot = 0.f;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
@@ -249,25 +300,25 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(
             if (!SUMS) p.weight.load(col_of(c), cols, wc);
 #pragma unroll
             for (int e = 0; e < 16; e++) {
-                const float x = __fmul_rn(h[c][e], r);
-                dot = fmaf(__fmul_rn(dy[c][e], SUMS ? w[SUMS ? c : 0][e] : wc[e]), x, dot);
-                if (SUMS && exists) dw[SUMS ? c : 0][e] = fmaf(dy[c][e], x, dw[SUMS ? c : 0][e]);
+                const float x = __fmul_rn(now.h[c][e], now.r);
+                dot = fmaf(__fmul_rn(now.dy[c][e], SUMS ? w[SUMS ? c : 0][e] : wc[e]), x, dot);
+                if (SUMS) dw[SUMS ? c : 0][e] = fmaf(now.dy[c][e], x, dw[SUMS ? c : 0][e]);   // rows that do not exist are zeros
             }
         }
-        const float mean = __fdiv_rn(team_sum(dot, team, red, which), (float)cols);
+        const float mean = team_sum(dot, team, red, which) * p.inv_cols;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
             float wc[16], v[16];
             if (!SUMS) p.weight.load(col_of(c), cols, wc);
 #pragma unroll
             for (int e = 0; e < 16; e++) {
-                const float g = __fmul_rn(dy[c][e], SUMS ? w[SUMS ? c : 0][e] : wc[e]);
-                v[e] = __fmul_rn(r, fmaf(-__fmul_rn(h[c][e], r), mean, g));
-                if (p.dh) v[e] = __fadd_rn(v[e], dh[c][e]);
+                const float g = __fmul_rn(now.dy[c][e], SUMS ? w[SUMS ? c : 0][e] : wc[e]);
+                v[e] = __fmul_rn(now.r, fmaf(-__fmul_rn(now.h[c][e], now.r), mean, g));
+                if (p.dh) v[e] = __fadd_rn(v[e], now.dh[c][e]);
             }
             Raw16<TH> dx;
             dx.set(v);
-            store_row16<TH>(either<TH>(p.dxb, p.dxf), i, col_of(c), cols, dx, lanes, exists);
+            store_row16<TH>(either<TH>(p.dxb, p.dxf), exists ? row : 0, col_of(c), cols, dx, lanes, exists);
         }
     }
     if (!SUMS) return;
@@ -432,6 +483,7 @@ extern "C" fp4q_status fp4q_rms_norm(const fp4q_norm *n, int64_t rows, int64_t c
     p.team = d.team;
     p.format = n->q ? n->q_format : 0;
     p.eps = n->eps;
+    p.inv_cols = 1.f / (float)cols;
     p.residual = n->residual;
     p.xb = rows_of<__nv_bfloat16>(n->x, rows, cols, n->ld_x);
     p.xf = rows_of<float>(n->x, rows, cols, n->ld_x);
@@ -451,7 +503,7 @@ extern "C" fp4q_status fp4q_rms_norm(const fp4q_norm *n, int64_t rows, int64_t c
     p.ld_s = n->ld_s;
     p.rstd = n->rstd;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const bool x32 = n->x_type == FP4Q_OUT_F32, h32 = n->residual && n->h_type == FP4Q_OUT_F32;
+    const bool x32 = n->x_type == FP4Q_OUT_F32, h32 = n->residual ? n->h_type == FP4Q_OUT_F32 : x32;
     if (x32) return h32 ? launch_norm<float, float>(p, d, s) : launch_norm<float, __nv_bfloat16>(p, d, s);
     return h32 ? launch_norm<__nv_bfloat16, float>(p, d, s) : launch_norm<__nv_bfloat16, __nv_bfloat16>(p, d, s);
 }
@@ -487,6 +539,7 @@ extern "C" fp4q_status fp4q_rms_norm_bwd(const fp4q_norm_grad *n, int64_t rows, 
     GradParams p = {};
     p.rows = rows;
     p.cols = cols;
+    p.inv_cols = 1.f / (float)cols;
     p.dh = n->dh;
     p.dyb = rows_of<__nv_bfloat16>(n->dy, rows, cols, n->ld_dy);
     p.dyf = rows_of<float>(n->dy, rows, cols, n->ld_dy);
