@@ -75,9 +75,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) fp8_quantize_kern
     const int64_t by = blockIdx.x / p.col_tiles, bx = blockIdx.x - by * p.col_tiles;
     const int64_t row0 = by * 128 + warp * 16 + rg * 4, col0 = bx * 128 + cg * 16;
 
+    const int n = columns16(col0, p.cols);
     Raw16<T> x[4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) x[i] = load_row16<T>(source<T>(p), row0 + i < p.rows ? row0 + i : 0, row0 + i < p.rows ? col0 : p.cols, p.cols);
+    for (int i = 0; i < 4; i++) x[i] = load_row16<T>(source<T>(p), row0 + i < p.rows ? row0 + i : 0, col0, row0 + i < p.rows ? n : 0);
 
     float row_top[4];
     uint32_t col_top[W];

@@ -20,17 +20,18 @@ struct WeightOf {
     int32_t bf16;
     RowsOf<float> f;
     RowsOf<__nv_bfloat16> b;
-    __device__ __forceinline__ void load(int64_t c0, int64_t cols, float (&w)[16]) const
+    template <bool FAST = false>
+    __device__ __forceinline__ void load(int64_t c0, int n, float (&w)[16]) const
     {
         if (!p) {
 #pragma unroll
             for (int e = 0; e < 16; e++) w[e] = 1.f;
         } else if (bf16) {
-            const Raw16<__nv_bfloat16> r = load_row16<__nv_bfloat16>(b, 0, c0, cols);
+            const Raw16<__nv_bfloat16> r = load_row16<__nv_bfloat16, FAST>(b, 0, c0, n);
 #pragma unroll
             for (int e = 0; e < 16; e++) w[e] = r[e];
         } else {
-            const Raw16<float> r = load_row16<float>(f, 0, c0, cols);
+            const Raw16<float> r = load_row16<float, FAST>(f, 0, c0, n);
 #pragma unroll
             for (int e = 0; e < 16; e++) w[e] = r[e];
         }
@@ -95,24 +96,21 @@ __device__ __forceinline__ const RowsOf<T> &either(const RowsOf<__nv_bfloat16> &
     else return b;
 }
 
-// Codes and scale of 16 elements where a block holds infinities (or, MXFP8, NaN): maxima of finite elements only.  Out of line; whole warps come here.
-__device__ __noinline__ uint4 careful_codes(const float *y, int lanes, bool mx, float *scale)
+// Codes and scale of 16 elements where a block holds infinities (or, MXFP8, NaN): maxima of finite elements only.  Whole warps come here.
+__device__ __forceinline__ uint4 careful_codes(float (&v)[16], int lanes, bool mx, float &scale)
 {
-    float v[16], top = 0.f;
+    float top = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; e++) {
-        v[e] = y[e];
-        top = fmaxf(top, finite_size(v[e]));
-    }
+    for (int e = 0; e < 16; e++) top = fmaxf(top, finite_size(v[e]));
     for (int d = lanes >> 1; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
     if (!mx) {
-        *scale = fp8_scale(top);
+        scale = fp8_scale(top);
         return fp8_codes(v, fp8_factor(top), true);
     }
 #pragma unroll
     for (int e = 0; e < 16; e++) v[e] = v[e] == v[e] ? v[e] : 0.f;   // as the MXFP8 quantizers: NaN becomes 0, infinities the largest number
     const int code = mx_scale_code(top);
-    *scale = __int_as_float(code);
+    scale = __int_as_float(code);
     return fp8_codes(v, inv_scale(code), false);
 }
 
@@ -134,18 +132,38 @@ __device__ __forceinline__ void add_rows(const Raw16<TX> &x, Raw16<TH> &r)
     }
 }
 
-// Without a residual TX is TH.
-template <typename TX, typename TH, int CHUNKS>
-__global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512, CHUNKS == 1 ? 2 : 1) rms_norm_kernel(const __grid_constant__ NormParams p)
+// Where a thread works: its row, and its place in the team.
+struct Place {
+    int64_t row;
+    int in;
+    __device__ __forceinline__ Place(int team)
+    {
+        in = threadIdx.x;
+        row = blockIdx.x;
+        if (team <= 32) {   // a power of two
+            const int bits = __ffs(team) - 1;
+            in = threadIdx.x & (team - 1);
+            row = (int64_t)blockIdx.x * (blockDim.x >> bits) + (threadIdx.x >> bits);
+        }
+    }
+};
+
+// Without a residual TX is TH.  FAST: all matrices' rows begin on 16 bytes, and cols is a multiple of 16.
+template <typename TX, typename TH, int CHUNKS, bool FAST>
+__global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(const __grid_constant__ NormParams p)
 {
     wait_for_predecessor();
     admit_successor();
     __shared__ float red[2][32];
-    const int team = p.team, in = (int)threadIdx.x % team, lanes = min(team, 32);
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / team) + threadIdx.x / team;
+    const int team = p.team, lanes = min(team, 32);
+    const Place at(team);
+    const int64_t row = at.row, cols = p.cols;
     const bool exists = row < p.rows;
-    const int64_t i = exists ? row : 0, cols = p.cols, n = exists ? cols : 0;
-    auto col_of = [&](int c) { return ((int64_t)c * team + in) * 16; };
+    const int64_t i = exists ? row : 0;
+    auto col_of = [&](int c) { return ((int64_t)c * team + at.in) * 16; };
+    int n[CHUNKS];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++) n[c] = exists ? columns16(col_of(c), cols) : 0;
 
     Raw16<TH> h[CHUNKS];   // as it is rounded: what the backward pass reads
     float squares = 0.f;
@@ -153,46 +171,46 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512, CHUNKS == 1 ? 2 : 1)
         Raw16<TX> x[CHUNKS];
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            x[c] = load_row16<TX>(either<TX>(p.xb, p.xf), i, col_of(c), n);
-            h[c] = load_row16<TH>(either<TH>(p.rb, p.rf), i, col_of(c), n);
+            x[c] = load_row16<TX, FAST>(either<TX>(p.xb, p.xf), i, col_of(c), n[c]);
+            h[c] = load_row16<TH, FAST>(either<TH>(p.rb, p.rf), i, col_of(c), n[c]);
         }
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
             add_rows<TX, TH>(x[c], h[c]);
-            store_row16<TH>(either<TH>(p.hb, p.hf), i, col_of(c), cols, h[c], lanes, exists);
+            store_row16<TH, FAST>(either<TH>(p.hb, p.hf), i, col_of(c), n[c], h[c], lanes);
         }
     } else {
 #pragma unroll
-        for (int c = 0; c < CHUNKS; c++) h[c] = load_row16<TH>(either<TH>(p.xb, p.xf), i, col_of(c), n);
+        for (int c = 0; c < CHUNKS; c++) h[c] = load_row16<TH, FAST>(either<TH>(p.xb, p.xf), i, col_of(c), n[c]);
     }
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++)
 #pragma unroll
         for (int e = 0; e < 16; e++) squares = fmaf(h[c][e], h[c][e], squares);
     const float mean = team_sum(squares, team, red, 0) * p.inv_cols, rstd = __frcp_rn(__fsqrt_rn(mean + p.eps));
-    if (p.rstd && exists && in == 0) p.rstd[row] = rstd;
+    if (p.rstd && exists && at.in == 0) p.rstd[row] = rstd;
 
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
-        const int64_t col = col_of(c);
+        const int col = (int)col_of(c);
         float v[16];
-        p.weight.load(col, cols, v);
+        p.weight.load<FAST>(col, n[c], v);
 #pragma unroll
         for (int e = 0; e < 16; e++) v[e] = __fmul_rn(__fmul_rn(h[c][e], rstd), v[e]);
         if (p.yb.p && !p.y_f32) {
             Raw16<__nv_bfloat16> y;
             y.set(v);
-            store_row16<__nv_bfloat16>(p.yb, i, col, cols, y, lanes, exists);
+            store_row16<__nv_bfloat16, FAST>(p.yb, i, col, n[c], y, lanes);
         } else if (p.yf.p) {
             Raw16<float> y;
             y.set(v);
-            store_row16<float>(p.yf, i, col, cols, y, lanes, exists);
+            store_row16<float, FAST>(p.yf, i, col, n[c], y, lanes);
         }
         if (p.format == 0) continue;
-        if (!exists || col + 16 > cols) {   // what is behind the row's end: its codes are 0
+        if (n[c] < 16) {   // what is behind the row's end: its codes are 0
 #pragma unroll
             for (int e = 0; e < 16; e++)
-                if (!exists || col + e >= cols) v[e] = 0.f;
+                if (e >= n[c]) v[e] = 0.f;
         }
         float top = 0.f;   // infinity where there is one; NaN does not count
 #pragma unroll
@@ -207,7 +225,7 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512, CHUNKS == 1 ? 2 : 1)
         float scale;
         uint4 codes;
         if (__any_sync(0xFFFFFFFFu, odd)) {
-            codes = careful_codes(v, block, mx, &scale);
+            codes = careful_codes(v, block, mx, scale);
         } else {
             for (int d = block >> 1; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
             const int code = mx ? mx_scale_code(top) : 0;
@@ -215,7 +233,7 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512, CHUNKS == 1 ? 2 : 1)
             codes = fp8_codes(v, mx ? inv_scale(code) : fp8_factor(top), false);
             if (!mx && col % 128 == 0) scale = fp8_scale(top);
         }
-        if (!exists || col >= (mx ? (cols + 31) / 32 * 32 : cols)) continue;
+        if (!exists || (FAST && !mx ? n[c] == 0 : col >= (mx ? ((int)cols + 31) / 32 * 32 : (int)cols))) continue;
         *reinterpret_cast<uint4 *>(p.q + row * p.ld_q + col) = codes;
         if (mx) {
             if (col % 32 == 0) static_cast<uint8_t *>(p.scale)[row * p.ld_s + col / 32] = (uint8_t)__float_as_int(scale);
@@ -244,21 +262,25 @@ struct GradParams {
 
 // Rows blockIdx.x, blockIdx.x + gridDim.x, ... of teams.  The operations of dx are spelled out, so that it is the same with SUMS and without.  With SUMS a CTA has many rows: the next
 // one's elements are on their way while this one's are worked on.
-template <typename TY, typename TH, int CHUNKS, bool SUMS>
+template <typename TY, typename TH, int CHUNKS, bool SUMS, bool FAST>
 __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(const __grid_constant__ GradParams p)
 {
     wait_for_predecessor();
     admit_successor();
     __shared__ float red[2][32];
     __shared__ float sums[SUMS ? 4096 : 1];   // of the teams of a CTA of 256 threads
-    const int team = p.team, in = (int)threadIdx.x % team, lanes = min(team, 32), teams = blockDim.x / team;
+    const int team = p.team, lanes = min(team, 32), bits = team <= 32 ? __ffs(team) - 1 : 0, teams = team <= 32 ? blockDim.x >> bits : 1;
+    const int in = team <= 32 ? threadIdx.x & (team - 1) : threadIdx.x, at = team <= 32 ? threadIdx.x >> bits : 0;
     const int64_t cols = p.cols;
     auto col_of = [&](int c) { return ((int64_t)c * team + in) * 16; };
+    int n[CHUNKS];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; c++) n[c] = columns16(col_of(c), cols);
     float dw[SUMS ? CHUNKS : 1][16], w[SUMS ? CHUNKS : 1][16];
     if (SUMS) {
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            p.weight.load(col_of(c), cols, w[c]);
+            p.weight.load<FAST>(col_of(c), n[c], w[c]);
 #pragma unroll
             for (int e = 0; e < 16; e++) dw[c][e] = 0.f;
         }
@@ -269,18 +291,19 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(
         float r;
     };
     auto load = [&](Row &to, int64_t row) {
-        const int64_t i = row < p.rows ? row : 0, n = row < p.rows ? cols : 0;
+        const bool exists = row < p.rows;
+        const int64_t i = exists ? row : 0;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            to.dy[c] = load_row16<TY>(either<TY>(p.dyb, p.dyf), i, col_of(c), n);
-            to.h[c] = load_row16<TH>(either<TH>(p.hb, p.hf), i, col_of(c), n);
-            if (p.dh) to.dh[c] = load_row16<TH>(either<TH>(p.dhb, p.dhf), i, col_of(c), n);
+            const int m = exists ? n[c] : 0;
+            to.dy[c] = load_row16<TY, FAST>(either<TY>(p.dyb, p.dyf), i, col_of(c), m);
+            to.h[c] = load_row16<TH, FAST>(either<TH>(p.hb, p.hf), i, col_of(c), m);
+            if (p.dh) to.dh[c] = load_row16<TH, FAST>(either<TH>(p.dhb, p.dhf), i, col_of(c), m);
         }
-        to.r = n ? load_global(p.rstd + i) : 0.f;
+        to.r = exists ? load_global(p.rstd + i) : 0.f;
     };
     int which = 0;
     const int64_t mine = (int64_t)blockIdx.x * teams, step = (int64_t)gridDim.x * teams;
-    const int at = threadIdx.x / team;
     Row next;
     if (SUMS && mine < p.rows) load(next, mine + at);
     for (int64_t first = mine; first < p.rows; first += step, which ^= 1) {
@@ -297,7 +320,7 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
             float wc[16];
-            if (!SUMS) p.weight.load(col_of(c), cols, wc);
+            if (!SUMS) p.weight.load<FAST>(col_of(c), n[c], wc);
 #pragma unroll
             for (int e = 0; e < 16; e++) {
                 const float x = __fmul_rn(now.h[c][e], now.r);
@@ -309,7 +332,7 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
             float wc[16], v[16];
-            if (!SUMS) p.weight.load(col_of(c), cols, wc);
+            if (!SUMS) p.weight.load<FAST>(col_of(c), n[c], wc);
 #pragma unroll
             for (int e = 0; e < 16; e++) {
                 const float g = __fmul_rn(now.dy[c][e], SUMS ? w[SUMS ? c : 0][e] : wc[e]);
@@ -318,7 +341,7 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(
             }
             Raw16<TH> dx;
             dx.set(v);
-            store_row16<TH>(either<TH>(p.dxb, p.dxf), exists ? row : 0, col_of(c), cols, dx, lanes, exists);
+            store_row16<TH, FAST>(either<TH>(p.dxb, p.dxf), exists ? row : 0, col_of(c), exists ? n[c] : 0, dx, lanes);
         }
     }
     if (!SUMS) return;
@@ -350,12 +373,13 @@ __global__ void __launch_bounds__(256) rms_norm_dweight_kernel(const __grid_cons
     __shared__ float sums[8 * 512];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t col = (int64_t)blockIdx.x * 512 + lane * 16;
+    const int n = columns16(col, p.cols);
     float dw[16];
 #pragma unroll
     for (int e = 0; e < 16; e++) dw[e] = 0.f;
     for (int64_t i = (int64_t)blockIdx.y * 8 + warp; i < p.rows; i += (int64_t)gridDim.y * 8) {
-        const Raw16<TY> dy = load_row16<TY>(either<TY>(p.dyb, p.dyf), i, col, p.cols);
-        const Raw16<TH> h = load_row16<TH>(either<TH>(p.hb, p.hf), i, col, p.cols);
+        const Raw16<TY> dy = load_row16<TY>(either<TY>(p.dyb, p.dyf), i, col, n);
+        const Raw16<TH> h = load_row16<TH>(either<TH>(p.hb, p.hf), i, col, n);
         const float r = load_global(p.rstd + i);
 #pragma unroll
         for (int e = 0; e < 16; e++) dw[e] = fmaf(dy[e], h[e] * r, dw[e]);
@@ -410,20 +434,20 @@ fp4q_status check_matrix(const void *p, int64_t ld, fp4q_out type, int64_t cols)
 constexpr int64_t kMostCols = 65536;
 
 template <typename TX, typename TH>
-fp4q_status launch_norm(const NormParams &p, const Deal &d, cudaStream_t s)
+fp4q_status launch_norm(const NormParams &p, const Deal &d, bool fast, cudaStream_t s)
 {
     const int64_t ctas = ceil_div(p.rows, d.threads / d.team);
     if (ctas > 0x7FFFFFFF) return FP4Q_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)ctas);
-    return launched(d.chunks == 1   ? launch_dependent(rms_norm_kernel<TX, TH, 1>, grid, d.threads, s, p)
-                    : d.chunks == 2 ? launch_dependent(rms_norm_kernel<TX, TH, 2>, grid, d.threads, s, p)
-                                    : launch_dependent(rms_norm_kernel<TX, TH, 4>, grid, d.threads, s, p));
+    return launched(d.chunks == 1   ? fast ? launch_dependent(rms_norm_kernel<TX, TH, 1, true>, grid, d.threads, s, p) : launch_dependent(rms_norm_kernel<TX, TH, 1, false>, grid, d.threads, s, p)
+                    : d.chunks == 2 ? launch_dependent(rms_norm_kernel<TX, TH, 2, false>, grid, d.threads, s, p)
+                                    : launch_dependent(rms_norm_kernel<TX, TH, 4, false>, grid, d.threads, s, p));
 }
 
 int64_t grad_ctas(int64_t rows, int teams) { return std::max<int64_t>(1, std::min<int64_t>(kGradCtas, ceil_div(rows, teams))); }
 
 template <typename TY, typename TH>
-fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scratch, cudaStream_t s)
+fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scratch, bool fast, cudaStream_t s)
 {
     const Deal d(ceil_div(p.cols, 16));
     p.team = d.team;
@@ -432,13 +456,14 @@ fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scra
     p.partial = dweight ? static_cast<float *>(scratch) : nullptr;
     int64_t parts = grad_ctas(p.rows, teams);
     if (fused) {
-        if (fp4q_status st = launched(launch_dependent(rms_norm_bwd_kernel<TY, TH, 1, true>, dim3((unsigned)parts), d.threads, s, p))) return st;
+        if (fp4q_status st = launched(fast ? launch_dependent(rms_norm_bwd_kernel<TY, TH, 1, true, true>, dim3((unsigned)parts), d.threads, s, p)
+                                              : launch_dependent(rms_norm_bwd_kernel<TY, TH, 1, true, false>, dim3((unsigned)parts), d.threads, s, p))) return st;
     } else if (p.rows > 0) {
         const int64_t ctas = ceil_div(p.rows, teams);
         const dim3 grid((unsigned)std::min<int64_t>(ctas, 0x7FFFFFFF));
-        if (fp4q_status st = launched(d.chunks == 1   ? launch_dependent(rms_norm_bwd_kernel<TY, TH, 1, false>, grid, d.threads, s, p)
-                                      : d.chunks == 2 ? launch_dependent(rms_norm_bwd_kernel<TY, TH, 2, false>, grid, d.threads, s, p)
-                                                      : launch_dependent(rms_norm_bwd_kernel<TY, TH, 4, false>, grid, d.threads, s, p)))
+        if (fp4q_status st = launched(d.chunks == 1   ? launch_dependent(rms_norm_bwd_kernel<TY, TH, 1, false, false>, grid, d.threads, s, p)
+                                      : d.chunks == 2 ? launch_dependent(rms_norm_bwd_kernel<TY, TH, 2, false, false>, grid, d.threads, s, p)
+                                                      : launch_dependent(rms_norm_bwd_kernel<TY, TH, 4, false, false>, grid, d.threads, s, p)))
             return st;
     }
     if (!dweight) return FP4Q_OK;
@@ -504,8 +529,10 @@ extern "C" fp4q_status fp4q_rms_norm(const fp4q_norm *n, int64_t rows, int64_t c
     p.rstd = n->rstd;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool x32 = n->x_type == FP4Q_OUT_F32, h32 = n->residual ? n->h_type == FP4Q_OUT_F32 : x32;
-    if (x32) return h32 ? launch_norm<float, float>(p, d, s) : launch_norm<float, __nv_bfloat16>(p, d, s);
-    return h32 ? launch_norm<__nv_bfloat16, float>(p, d, s) : launch_norm<__nv_bfloat16, __nv_bfloat16>(p, d, s);
+    const bool fast = cols % 16 == 0 && on_grid(n->x, n->ld_x, rows, size_of(n->x_type)) && (!n->residual || (on_grid(n->residual, n->ld_residual, rows, size_of(n->h_type)) && on_grid(n->h, n->ld_h, rows, size_of(n->h_type)))) &&
+                      aligned(n->weight, 16) && (!n->y || on_grid(n->y, n->ld_y, rows, size_of(n->y_type)));
+    if (x32) return h32 ? launch_norm<float, float>(p, d, fast, s) : launch_norm<float, __nv_bfloat16>(p, d, fast, s);
+    return h32 ? launch_norm<__nv_bfloat16, float>(p, d, fast, s) : launch_norm<__nv_bfloat16, __nv_bfloat16>(p, d, fast, s);
 }
 
 extern "C" size_t fp4q_rms_norm_bwd_scratch_bytes(int64_t rows, int64_t cols)
@@ -553,6 +580,9 @@ extern "C" fp4q_status fp4q_rms_norm_bwd(const fp4q_norm_grad *n, int64_t rows, 
     p.weight = weight_of(n->weight, n->weight_type, cols);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool y32 = n->dy_type == FP4Q_OUT_F32, h32 = n->h_type == FP4Q_OUT_F32;
-    if (y32) return h32 ? launch_grad<float, float>(p, n->dweight, n->accumulate, scratch, s) : launch_grad<float, __nv_bfloat16>(p, n->dweight, n->accumulate, scratch, s);
-    return h32 ? launch_grad<__nv_bfloat16, float>(p, n->dweight, n->accumulate, scratch, s) : launch_grad<__nv_bfloat16, __nv_bfloat16>(p, n->dweight, n->accumulate, scratch, s);
+    const size_t hs = size_of(n->h_type);
+    const bool fast = cols % 16 == 0 && on_grid(n->dy, n->ld_dy, rows, size_of(n->dy_type)) && on_grid(n->h, n->ld_h, rows, hs) && on_grid(n->dh, n->ld_dh, rows, hs) &&
+                      on_grid(n->dx, n->ld_dx, rows, hs) && aligned(n->weight, 16);
+    if (y32) return h32 ? launch_grad<float, float>(p, n->dweight, n->accumulate, scratch, fast, s) : launch_grad<float, __nv_bfloat16>(p, n->dweight, n->accumulate, scratch, fast, s);
+    return h32 ? launch_grad<__nv_bfloat16, float>(p, n->dweight, n->accumulate, scratch, fast, s) : launch_grad<__nv_bfloat16, __nv_bfloat16>(p, n->dweight, n->accumulate, scratch, fast, s);
 }

@@ -25,6 +25,9 @@ inline RowsOf<T> rows_of(const void *p, int64_t rows, int64_t cols, int64_t ld)
     return r;
 }
 
+// Whether rows of `size` bytes an element begin on 16 bytes.
+inline bool on_grid(const void *p, int64_t ld, int64_t rows, size_t size) { return !p || (aligned(p, 16) && (rows <= 1 || ld * (int64_t)size % 16 == 0)); }
+
 __device__ __forceinline__ uint32_t pack_pair(float lo, float hi)
 {
     const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
@@ -70,14 +73,25 @@ __device__ __forceinline__ void drop_bytes(uint32_t (&w)[N], uint32_t off)
         for (int i = 0; i < KEEP; i++) w[i] = __funnelshift_r(w[i], w[i + 1 < N ? i + 1 : i], 16);
 }
 
-// Columns c0 .. c0 + 15 of row i; zeros from column `cols` on.
-template <typename T>
-__device__ __forceinline__ Raw16<T> load_row16(const RowsOf<T> &m, int64_t i, int64_t c0, int64_t cols)
+// How many of the columns c0 .. c0 + 15 exist.
+__device__ __forceinline__ int columns16(int64_t c0, int64_t cols) { return c0 >= cols ? 0 : cols - c0 < 16 ? (int)(cols - c0) : 16; }
+
+// Columns c0 .. c0 + 15 of row i, of which the first n exist; zeros behind them.  FAST: rows begin on 16 bytes, and n is 0 or 16.
+template <typename T, bool FAST = false>
+__device__ __forceinline__ Raw16<T> load_row16(const RowsOf<T> &m, int64_t i, int64_t c0, int n)
 {
     constexpr int W = Raw16<T>::kWords, P = W / 4;
     Raw16<T> r;
-    const int n = c0 >= cols ? 0 : cols - c0 < 16 ? (int)(cols - c0) : 16;
     const T *src = m.p + i * m.ld + c0;
+    if constexpr (FAST) {
+#pragma unroll
+        for (int k = 0; k < P; k++) {
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (n) v = load_global(reinterpret_cast<const uint4 *>(src) + k);
+            r.w[4 * k] = v.x; r.w[4 * k + 1] = v.y; r.w[4 * k + 2] = v.z; r.w[4 * k + 3] = v.w;
+        }
+        return r;
+    }
     const uintptr_t at = reinterpret_cast<uintptr_t>(src);
     const uint32_t off = (uint32_t)at & 15u;
     if (n == 16 && off == 0u) {
@@ -119,15 +133,20 @@ __device__ __forceinline__ Raw16<T> load_row16(const RowsOf<T> &m, int64_t i, in
     return r;
 }
 
-// The same columns written, of those that exist.  All lanes of the warp come here; lanes next to one another in a run of `team` (a power of two up to 32) have neighbouring
+// The same columns written, the first n.  All lanes of the warp come here; lanes next to one another in a run of `team` (a power of two up to 32) have neighbouring
 // columns of one row.  Rows off the 16-byte grid: a lane writes the pieces that begin in it and, with its neighbour's last elements, the one before; where the
 // neighbour has none, or not all, of its elements, each writes its own one by one.
-template <typename T>
-__device__ __forceinline__ void store_row16(const RowsOf<T> &m, int64_t i, int64_t c0, int64_t cols, const Raw16<T> &r, int team, bool exists)
+template <typename T, bool FAST = false>
+__device__ __forceinline__ void store_row16(const RowsOf<T> &m, int64_t i, int64_t c0, int n, const Raw16<T> &r, int team)
 {
     constexpr int W = Raw16<T>::kWords, P = W / 4, S = (int)sizeof(T);
-    const int n = !exists || c0 >= cols ? 0 : cols - c0 < 16 ? (int)(cols - c0) : 16;
     T *dst = m.p + i * m.ld + c0;
+    if constexpr (FAST) {
+        if (n)
+#pragma unroll
+            for (int k = 0; k < P; k++) reinterpret_cast<uint4 *>(dst)[k] = make_uint4(r.w[4 * k], r.w[4 * k + 1], r.w[4 * k + 2], r.w[4 * k + 3]);
+        return;
+    }
     const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(dst) & 15u;
     const bool full = n == 16;
     if (__all_sync(0xFFFFFFFFu, n == 0 || (full && off == 0u))) {
