@@ -132,23 +132,23 @@ __device__ __forceinline__ void add_rows(const Raw16<TX> &x, Raw16<TH> &r)
     }
 }
 
-// Where a thread works: its row, and its place in the team.
+// Where a thread works: the teams of its CTA, its own, and its place in that.
 struct Place {
-    int64_t row;
-    int in;
-    __device__ __forceinline__ Place(int team)
+    int teams = 1, team = 0, in;
+    __device__ __forceinline__ explicit Place(int size)
     {
         in = threadIdx.x;
-        row = blockIdx.x;
-        if (team <= 32) {   // a power of two
-            const int bits = __ffs(team) - 1;
-            in = threadIdx.x & (team - 1);
-            row = (int64_t)blockIdx.x * (blockDim.x >> bits) + (threadIdx.x >> bits);
+        if (size <= 32) {   // a power of two
+            const int bits = __ffs(size) - 1;
+            teams = blockDim.x >> bits;
+            team = threadIdx.x >> bits;
+            in = threadIdx.x & (size - 1);
         }
     }
 };
 
-// Without a residual TX is TH.  FAST: all matrices' rows begin on 16 bytes, and cols is a multiple of 16.
+// Rows blockIdx.x, blockIdx.x + gridDim.x, ... of teams.  Up to 8192 columns (one chunk a thread) the weight stays in registers and the next row is on its way while this one is worked
+// on.  Without a residual TX is TH.  FAST: all matrices' rows begin on 16 bytes, and cols is a multiple of 16.
 template <typename TX, typename TH, int CHUNKS, bool FAST>
 __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(const __grid_constant__ NormParams p)
 {
@@ -157,88 +157,107 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(cons
     __shared__ float red[2][32];
     const int team = p.team, lanes = min(team, 32);
     const Place at(team);
-    const int64_t row = at.row, cols = p.cols;
-    const bool exists = row < p.rows;
-    const int64_t i = exists ? row : 0;
+    const int64_t cols = p.cols, step = (int64_t)gridDim.x * at.teams;
+    constexpr bool kAhead = CHUNKS == 1;
     auto col_of = [&](int c) { return ((int64_t)c * team + at.in) * 16; };
-    int n[CHUNKS];
-#pragma unroll
-    for (int c = 0; c < CHUNKS; c++) n[c] = exists ? columns16(col_of(c), cols) : 0;
-
-    Raw16<TH> h[CHUNKS];   // as it is rounded: what the backward pass reads
-    float squares = 0.f;
-    if (p.residual) {
-        Raw16<TX> x[CHUNKS];
-#pragma unroll
-        for (int c = 0; c < CHUNKS; c++) {
-            x[c] = load_row16<TX, FAST>(either<TX>(p.xb, p.xf), i, col_of(c), n[c]);
-            h[c] = load_row16<TH, FAST>(either<TH>(p.rb, p.rf), i, col_of(c), n[c]);
-        }
-#pragma unroll
-        for (int c = 0; c < CHUNKS; c++) {
-            add_rows<TX, TH>(x[c], h[c]);
-            store_row16<TH, FAST>(either<TH>(p.hb, p.hf), i, col_of(c), n[c], h[c], lanes);
-        }
-    } else {
-#pragma unroll
-        for (int c = 0; c < CHUNKS; c++) h[c] = load_row16<TH, FAST>(either<TH>(p.xb, p.xf), i, col_of(c), n[c]);
-    }
-#pragma unroll
-    for (int c = 0; c < CHUNKS; c++)
-#pragma unroll
-        for (int e = 0; e < 16; e++) squares = fmaf(h[c][e], h[c][e], squares);
-    const float mean = team_sum(squares, team, red, 0) * p.inv_cols, rstd = __frcp_rn(__fsqrt_rn(mean + p.eps));
-    if (p.rstd && exists && at.in == 0) p.rstd[row] = rstd;
-
+    int all[CHUNKS];   // columns that exist
+    float w[kAhead ? CHUNKS : 1][16];
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
-        const int col = (int)col_of(c);
-        float v[16];
-        p.weight.load<FAST>(col, n[c], v);
+        all[c] = columns16(col_of(c), cols);
+        if (kAhead) p.weight.load<FAST>(col_of(c), all[c], w[kAhead ? c : 0]);
+    }
+    Raw16<TX> x[CHUNKS];
+    Raw16<TH> r[CHUNKS];
+    auto load = [&](int64_t row) {
+        const int64_t i = row < p.rows ? row : 0;
 #pragma unroll
-        for (int e = 0; e < 16; e++) v[e] = __fmul_rn(__fmul_rn(h[c][e], rstd), v[e]);
-        if (p.yb.p && !p.y_f32) {
-            Raw16<__nv_bfloat16> y;
-            y.set(v);
-            store_row16<__nv_bfloat16, FAST>(p.yb, i, col, n[c], y, lanes);
-        } else if (p.yf.p) {
-            Raw16<float> y;
-            y.set(v);
-            store_row16<float, FAST>(p.yf, i, col, n[c], y, lanes);
+        for (int c = 0; c < CHUNKS; c++) {
+            const int m = row < p.rows ? all[c] : 0;
+            if (p.residual) {
+                x[c] = load_row16<TX, FAST>(either<TX>(p.xb, p.xf), i, col_of(c), m);
+                r[c] = load_row16<TH, FAST>(either<TH>(p.rb, p.rf), i, col_of(c), m);
+            } else {
+                r[c] = load_row16<TH, FAST>(either<TH>(p.xb, p.xf), i, col_of(c), m);
+            }
         }
-        if (p.format == 0) continue;
-        if (n[c] < 16) {   // what is behind the row's end: its codes are 0
+    };
+    int64_t first = (int64_t)blockIdx.x * at.teams;
+    if (kAhead) load(first + at.team);
+    for (int which = 0; first < p.rows; first += step, which ^= 1) {
+        const int64_t row = first + at.team;
+        if (!kAhead) load(row);
+        const bool exists = row < p.rows;
+        const int64_t i = exists ? row : 0;
+        int n[CHUNKS];
+        Raw16<TH> h[CHUNKS];   // as it is rounded: what the backward pass reads
 #pragma unroll
-            for (int e = 0; e < 16; e++)
-                if (e >= n[c]) v[e] = 0.f;
+        for (int c = 0; c < CHUNKS; c++) {
+            n[c] = exists ? all[c] : 0;
+            h[c] = r[c];
+            if (p.residual) add_rows<TX, TH>(x[c], h[c]);
         }
-        float top = 0.f;   // infinity where there is one; NaN does not count
+        if (kAhead && first + step < p.rows) load(row + step);
+        float squares = 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; e++) top = fmaxf(top, fabsf(v[e]));
-        const bool mx = p.format == FP4Q_NORM_MXFP8;
-        bool odd = is_infinite(top);
-        if (mx) {
+        for (int c = 0; c < CHUNKS; c++) {
+            if (p.residual) store_row16<TH, FAST>(either<TH>(p.hb, p.hf), i, col_of(c), n[c], h[c], lanes);
 #pragma unroll
-            for (int e = 0; e < 16; e++) odd |= v[e] != v[e];
+            for (int e = 0; e < 16; e++) squares = fmaf(h[c][e], h[c][e], squares);
         }
-        const int block = mx ? min(team, 2) : min(team, 8);   // lanes of a block
-        float scale;
-        uint4 codes;
-        if (__any_sync(0xFFFFFFFFu, odd)) {
-            codes = careful_codes(v, block, mx, scale);
-        } else {
-            for (int d = block >> 1; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-            const int code = mx ? mx_scale_code(top) : 0;
-            scale = mx ? __int_as_float(code) : top;
-            codes = fp8_codes(v, mx ? inv_scale(code) : fp8_factor(top), false);
-            if (!mx && col % 128 == 0) scale = fp8_scale(top);
-        }
-        if (!exists || (FAST && !mx ? n[c] == 0 : col >= (mx ? ((int)cols + 31) / 32 * 32 : (int)cols))) continue;
-        *reinterpret_cast<uint4 *>(p.q + row * p.ld_q + col) = codes;
-        if (mx) {
-            if (col % 32 == 0) static_cast<uint8_t *>(p.scale)[row * p.ld_s + col / 32] = (uint8_t)__float_as_int(scale);
-        } else if (col % 128 == 0) {
-            static_cast<float *>(p.scale)[row * p.ld_s + col / 128] = scale;
+        const float mean = team_sum(squares, team, red, which) * p.inv_cols, rstd = __frcp_rn(__fsqrt_rn(mean + p.eps));
+        if (p.rstd && exists && at.in == 0) p.rstd[row] = rstd;
+
+#pragma unroll
+        for (int c = 0; c < CHUNKS; c++) {
+            const int col = (int)col_of(c);
+            float v[16];
+            if (!kAhead) p.weight.load<FAST>(col, n[c], w[0]);
+#pragma unroll
+            for (int e = 0; e < 16; e++) v[e] = __fmul_rn(__fmul_rn(h[c][e], rstd), w[kAhead ? c : 0][e]);
+            if (p.yb.p && !p.y_f32) {
+                Raw16<__nv_bfloat16> y;
+                y.set(v);
+                store_row16<__nv_bfloat16, FAST>(p.yb, i, col, n[c], y, lanes);
+            } else if (p.yf.p) {
+                Raw16<float> y;
+                y.set(v);
+                store_row16<float, FAST>(p.yf, i, col, n[c], y, lanes);
+            }
+            if (p.format == 0) continue;
+            if (n[c] < 16) {   // what is behind the row's end: its codes are 0
+#pragma unroll
+                for (int e = 0; e < 16; e++)
+                    if (e >= n[c]) v[e] = 0.f;
+            }
+            float top = 0.f;   // infinity where there is one; NaN does not count
+#pragma unroll
+            for (int e = 0; e < 16; e++) top = fmaxf(top, fabsf(v[e]));
+            const bool mx = p.format == FP4Q_NORM_MXFP8;
+            bool odd = is_infinite(top);
+            if (mx) {
+#pragma unroll
+                for (int e = 0; e < 16; e++) odd |= v[e] != v[e];
+            }
+            const int block = mx ? min(team, 2) : min(team, 8);   // lanes of a block
+            float scale;
+            uint4 codes;
+            if (__any_sync(0xFFFFFFFFu, odd)) {
+                codes = careful_codes(v, block, mx, scale);
+            } else {
+                for (int d = block >> 1; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+                const int code = mx ? mx_scale_code(top) : 0;
+                scale = mx ? __int_as_float(code) : top;
+                codes = fp8_codes(v, mx ? inv_scale(code) : fp8_factor(top), false);
+                if (!mx && col % 128 == 0) scale = fp8_scale(top);
+            }
+            if (!exists || (FAST && !mx ? n[c] == 0 : col >= (mx ? ((int)cols + 31) / 32 * 32 : (int)cols))) continue;
+            *reinterpret_cast<uint4 *>(p.q + row * p.ld_q + col) = codes;
+            if (mx) {
+                if (col % 32 == 0) static_cast<uint8_t *>(p.scale)[row * p.ld_s + col / 32] = (uint8_t)__float_as_int(scale);
+            } else if (col % 128 == 0) {
+                static_cast<float *>(p.scale)[row * p.ld_s + col / 128] = scale;
+            }
         }
     }
 }
@@ -269,10 +288,11 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(
     admit_successor();
     __shared__ float red[2][32];
     __shared__ float sums[SUMS ? 4096 : 1];   // of the teams of a CTA of 256 threads
-    const int team = p.team, lanes = min(team, 32), bits = team <= 32 ? __ffs(team) - 1 : 0, teams = team <= 32 ? blockDim.x >> bits : 1;
-    const int in = team <= 32 ? threadIdx.x & (team - 1) : threadIdx.x, at = team <= 32 ? threadIdx.x >> bits : 0;
+    const int team = p.team, lanes = min(team, 32);
+    const Place at(team);
+    const int teams = at.teams;
     const int64_t cols = p.cols;
-    auto col_of = [&](int c) { return ((int64_t)c * team + in) * 16; };
+    auto col_of = [&](int c) { return ((int64_t)c * team + at.in) * 16; };
     int n[CHUNKS];
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) n[c] = columns16(col_of(c), cols);
@@ -305,9 +325,9 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(
     int which = 0;
     const int64_t mine = (int64_t)blockIdx.x * teams, step = (int64_t)gridDim.x * teams;
     Row next;
-    if (SUMS && mine < p.rows) load(next, mine + at);
+    if (SUMS && mine < p.rows) load(next, mine + at.team);
     for (int64_t first = mine; first < p.rows; first += step, which ^= 1) {
-        const int64_t row = first + at;
+        const int64_t row = first + at.team;
         const bool exists = row < p.rows;
         Row now;
         if (SUMS) {
@@ -432,13 +452,13 @@ fp4q_status check_matrix(const void *p, int64_t ld, fp4q_out type, int64_t cols)
     return aligned(p, size_of(type)) ? FP4Q_OK : FP4Q_ERR_ALIGN;
 }
 constexpr int64_t kMostCols = 65536;
+constexpr int kNormThreads = 148 * 2 * 256;   // of a grid whose CTAs take rows in turn: all of them run at once (16384 x 4096 104 us; 4 x 256 an SM 105, one row each 165)
 
 template <typename TX, typename TH>
 fp4q_status launch_norm(const NormParams &p, const Deal &d, bool fast, cudaStream_t s)
 {
     const int64_t ctas = ceil_div(p.rows, d.threads / d.team);
-    if (ctas > 0x7FFFFFFF) return FP4Q_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)ctas);
+    const dim3 grid((unsigned)std::min<int64_t>(ctas, kNormThreads / d.threads));
     return launched(d.chunks == 1   ? fast ? launch_dependent(rms_norm_kernel<TX, TH, 1, true>, grid, d.threads, s, p) : launch_dependent(rms_norm_kernel<TX, TH, 1, false>, grid, d.threads, s, p)
                     : d.chunks == 2 ? launch_dependent(rms_norm_kernel<TX, TH, 2, false>, grid, d.threads, s, p)
                                     : launch_dependent(rms_norm_kernel<TX, TH, 4, false>, grid, d.threads, s, p));
