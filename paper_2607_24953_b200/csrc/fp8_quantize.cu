@@ -37,16 +37,16 @@ __device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pai
 
 // Maxima of a lane's four rows and, over these, of its columns.
 template <typename T>
-__device__ __forceinline__ void maxima(const Raw16<T> (&x)[4], float (&rows)[4], uint32_t (&cols)[Raw16<T>::kWords])
+__device__ __forceinline__ void maxima(const Raw<T> (&x)[4], float (&rows)[4], uint32_t (&cols)[Raw<T>::kWords])
 {
 #pragma unroll
-    for (int k = 0; k < Raw16<T>::kWords; k++) cols[k] = 0u;
+    for (int k = 0; k < Raw<T>::kWords; k++) cols[k] = 0u;
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         uint32_t pair = 0u;
         float m = 0.f;
 #pragma unroll
-        for (int k = 0; k < Raw16<T>::kWords; k++) {
+        for (int k = 0; k < Raw<T>::kWords; k++) {
             if constexpr (sizeof(T) == 2) {
                 const uint32_t a = x[i].w[k] & 0x7FFF7FFFu;
                 pair = max_pair(pair, a);
@@ -61,7 +61,8 @@ __device__ __forceinline__ void maxima(const Raw16<T> (&x)[4], float (&rows)[4],
     }
 }
 
-template <typename T, bool SQUARE>
+// GRID: rows begin on 16 bytes.
+template <typename T, bool SQUARE, bool GRID>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) fp8_quantize_kernel(const __grid_constant__ Fp8QuantParams p)
 {
     wait_for_predecessor();
@@ -70,15 +71,20 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) fp8_quantize_kern
     __shared__ float tops[8][128];
     __shared__ __align__(16) float factors[128];
     constexpr bool kPairs = sizeof(T) == 2;
-    constexpr int W = Raw16<T>::kWords;
+    constexpr int W = Raw<T>::kWords;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cg = lane & 7, rg = lane >> 3;
     const int64_t by = blockIdx.x / p.col_tiles, bx = blockIdx.x - by * p.col_tiles;
     const int64_t row0 = by * 128 + warp * 16 + rg * 4, col0 = bx * 128 + cg * 16;
 
-    const int n = columns16(col0, p.cols);
-    Raw16<T> x[4];
+    const int n = columns_at(col0, p.cols);
+    Raw<T> x[4];
+    {
+        Pieces<T, GRID> on_way[4];
 #pragma unroll
-    for (int i = 0; i < 4; i++) x[i] = load_row16<T>(source<T>(p), row0 + i < p.rows ? row0 + i : 0, col0, row0 + i < p.rows ? n : 0);
+        for (int i = 0; i < 4; i++) on_way[i].fetch(source<T>(p), row0 + i < p.rows ? row0 + i : 0, col0, row0 + i < p.rows ? n : 0);
+#pragma unroll
+        for (int i = 0; i < 4; i++) x[i] = on_way[i].land(source<T>(p), row0 + i < p.rows ? row0 + i : 0, col0, row0 + i < p.rows ? n : 0);
+    }
 
     float row_top[4];
     uint32_t col_top[W];
@@ -187,6 +193,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) fp8_quantize_kern
     }
 }
 
+template <typename T, bool SQUARE>
+fp4q_status launch(const Fp8QuantParams &p, bool grid16, dim3 grid, cudaStream_t s)
+{
+    return launched(grid16 ? launch_dependent(fp8_quantize_kernel<T, SQUARE, true>, grid, 256, s, p) : launch_dependent(fp8_quantize_kernel<T, SQUARE, false>, grid, 256, s, p));
+}
+
 }  // namespace
 
 extern "C" fp4q_status fp4q_fp8_quantize(const void *x, fp4q_out x_type, int64_t rows, int64_t cols, int64_t ld_x, const fp4q_fp8_tensor *out, void *stream)
@@ -210,14 +222,15 @@ extern "C" fp4q_status fp4q_fp8_quantize(const void *x, fp4q_out x_type, int64_t
     Fp8QuantParams p;
     p.rows = rows;
     p.cols = cols;
-    p.b16 = rows_of<__nv_bfloat16>(x, rows, cols, ld_x);
-    p.f32 = rows_of<float>(x, rows, cols, ld_x);
+    p.b16 = rows_of<__nv_bfloat16>(x, ld_x);
+    p.f32 = rows_of<float>(x, ld_x);
     p.out = *out;
     p.col_tiles = ceil_div(cols, 128);
     const int64_t tiles = p.col_tiles * ceil_div(rows, 128);
     if (tiles > 0x7FFFFFFF) return FP4Q_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)tiles);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (x_type == FP4Q_OUT_F32) return launched(square ? launch_dependent(fp8_quantize_kernel<float, true>, grid, 256, s, p) : launch_dependent(fp8_quantize_kernel<float, false>, grid, 256, s, p));
-    return launched(square ? launch_dependent(fp8_quantize_kernel<__nv_bfloat16, true>, grid, 256, s, p) : launch_dependent(fp8_quantize_kernel<__nv_bfloat16, false>, grid, 256, s, p));
+    const bool grid16 = on_grid(x, ld_x, rows, x_type == FP4Q_OUT_F32 ? 4 : 2);
+    if (x_type == FP4Q_OUT_F32) return square ? launch<float, true>(p, grid16, grid, s) : launch<float, false>(p, grid16, grid, s);
+    return square ? launch<__nv_bfloat16, true>(p, grid16, grid, s) : launch<__nv_bfloat16, false>(p, grid16, grid, s);
 }

@@ -9,31 +9,32 @@
 #include "row_io.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 using namespace fp4q;
 
 namespace {
 
-// The FP32 or BF16 weight, 16 of its elements.
+// The FP32 or BF16 weight, and E of its elements.
 struct WeightOf {
     const void *p;
     int32_t bf16;
     RowsOf<float> f;
     RowsOf<__nv_bfloat16> b;
-    template <bool FAST = false>
-    __device__ __forceinline__ void load(int64_t c0, int n, float (&w)[16]) const
+    template <bool GRID, int E>
+    __device__ __forceinline__ void load(int64_t c0, int n, float (&w)[E]) const
     {
         if (!p) {
 #pragma unroll
-            for (int e = 0; e < 16; e++) w[e] = 1.f;
+            for (int e = 0; e < E; e++) w[e] = 1.f;
         } else if (bf16) {
-            const Raw16<__nv_bfloat16> r = load_row16<__nv_bfloat16, FAST>(b, 0, c0, n);
+            const Raw<__nv_bfloat16, E> r = load_row<__nv_bfloat16, GRID, E>(b, 0, c0, n);
 #pragma unroll
-            for (int e = 0; e < 16; e++) w[e] = r[e];
+            for (int e = 0; e < E; e++) w[e] = r[e];
         } else {
-            const Raw16<float> r = load_row16<float, FAST>(f, 0, c0, n);
+            const Raw<float, E> r = load_row<float, GRID, E>(f, 0, c0, n);
 #pragma unroll
-            for (int e = 0; e < 16; e++) w[e] = r[e];
+            for (int e = 0; e < E; e++) w[e] = r[e];
         }
     }
 };
@@ -42,33 +43,53 @@ WeightOf weight_of(const void *p, fp4q_out type, int64_t cols)
     WeightOf w;
     w.p = p;
     w.bf16 = type == FP4Q_OUT_BF16;
-    w.f = rows_of<float>(p, 1, cols, cols);
-    w.b = rows_of<__nv_bfloat16>(p, 1, cols, cols);
+    w.f = rows_of<float>(p, cols);
+    w.b = rows_of<__nv_bfloat16>(p, cols);
     return w;
 }
 
-// How a row is dealt to threads: `team` of them (a power of two up to 32, else whole warps and all of the CTA's), `chunks` times 16 columns each.
+// How a row is dealt to threads: `team` of them (a power of two up to 32, else whole warps), `chunks` times 16 columns each, backward 8.  A CTA has one team or, of small ones, several.
 struct Deal {
     int team, threads, chunks;
-    explicit Deal(int64_t segments)
+    // segments: of a lane's columns, 16 or, backward, 8
+    Deal(int64_t segments, bool backward)
     {
-        chunks = segments <= 512 ? 1 : segments <= 1024 ? 2 : 4;
+        chunks = segments <= 512 ? 1 : segments <= 1024 ? 2 : !backward || segments <= 2048 ? 4 : 16;
         const int64_t t = ceil_div(segments, chunks);
         team = 1;
         while (team < t && team < 32) team *= 2;
         if (t > 32) team = (int)round_up(t, 32);
-        threads = team > 32 ? team : 256;
+        threads = team > 32 ? team * (int)std::max<int64_t>(1, 256 / team) : 256;
     }
 };
 
-// Sum over a team.  red: two rows of 32 floats; a team of several warps is the CTA and passes one barrier.
-__device__ __forceinline__ float team_sum(float v, int team, float (*red)[32], int which)
+// Where a thread works: the teams of its CTA, its own, and its place in that.
+struct Place {
+    int teams, team, in;
+    __device__ __forceinline__ explicit Place(int size)
+    {
+        if (size <= 32) {   // a power of two
+            const int bits = __ffs(size) - 1;
+            teams = blockDim.x >> bits;
+            team = threadIdx.x >> bits;
+            in = threadIdx.x & (size - 1);
+        } else {
+            teams = (int)blockDim.x / size;
+            team = teams == 1 ? 0 : (int)threadIdx.x / size;
+            in = threadIdx.x - team * size;
+        }
+    }
+};
+
+// Sum over a team.  red: two rows of 32 floats; with teams of several warps the CTA passes one barrier.
+__device__ __forceinline__ float team_sum(float v, int size, const Place &at, float (*red)[32], int which)
 {
-    for (int d = min(team, 32) >> 1; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-    if (team <= 32) return v;
-    if ((threadIdx.x & 31) == 0) red[which][threadIdx.x >> 5] = v;
+    for (int d = min(size, 32) >> 1; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    if (size <= 32) return v;
+    const int lane = threadIdx.x & 31, warps = size >> 5;
+    if (lane == 0) red[which][threadIdx.x >> 5] = v;
     __syncthreads();
-    v = (threadIdx.x & 31) < (team >> 5) ? red[which][threadIdx.x & 31] : 0.f;
+    v = lane < warps ? red[which][at.team * warps + lane] : 0.f;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
     return v;
@@ -116,7 +137,7 @@ __device__ __forceinline__ uint4 careful_codes(float (&v)[16], int lanes, bool m
 
 // A stream of BF16 on BF16 is added two elements at a time: the FP32 sum of two BF16 numbers is exact, or so far from a tie that it is rounded like the exact one.
 template <typename TX, typename TH>
-__device__ __forceinline__ void add_rows(const Raw16<TX> &x, Raw16<TH> &r)
+__device__ __forceinline__ void add_rows(const Raw<TX> &x, Raw<TH> &r)
 {
     if constexpr (sizeof(TX) == 2 && sizeof(TH) == 2) {
 #pragma unroll
@@ -132,24 +153,9 @@ __device__ __forceinline__ void add_rows(const Raw16<TX> &x, Raw16<TH> &r)
     }
 }
 
-// Where a thread works: the teams of its CTA, its own, and its place in that.
-struct Place {
-    int teams = 1, team = 0, in;
-    __device__ __forceinline__ explicit Place(int size)
-    {
-        in = threadIdx.x;
-        if (size <= 32) {   // a power of two
-            const int bits = __ffs(size) - 1;
-            teams = blockDim.x >> bits;
-            team = threadIdx.x >> bits;
-            in = threadIdx.x & (size - 1);
-        }
-    }
-};
-
 // Rows blockIdx.x, blockIdx.x + gridDim.x, ... of teams.  Up to 8192 columns (one chunk a thread) the weight stays in registers and the next row is on its way while this one is worked
-// on.  Without a residual TX is TH.  FAST: all matrices' rows begin on 16 bytes, and cols is a multiple of 16.
-template <typename TX, typename TH, int CHUNKS, bool FAST>
+// on.  Without a residual TX is TH.  GRID_IN, GRID_OUT: the rows of all that is read, or written, begin on 16 bytes.
+template <typename TX, typename TH, int CHUNKS, bool GRID_IN, bool GRID_OUT>
 __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(const __grid_constant__ NormParams p)
 {
     wait_for_predecessor();
@@ -164,21 +170,22 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(cons
     float w[kAhead ? CHUNKS : 1][16];
 #pragma unroll
     for (int c = 0; c < CHUNKS; c++) {
-        all[c] = columns16(col_of(c), cols);
-        if (kAhead) p.weight.load<FAST>(col_of(c), all[c], w[kAhead ? c : 0]);
+        all[c] = columns_at(col_of(c), cols);
+        if (kAhead) p.weight.load<GRID_IN, 16>(col_of(c), all[c], w[kAhead ? c : 0]);
     }
-    Raw16<TX> x[CHUNKS];
-    Raw16<TH> r[CHUNKS];
+    constexpr bool kSame = sizeof(TX) == sizeof(TH);
+    Pieces<TX, GRID_IN> x[CHUNKS];
+    Pieces<TH, GRID_IN> r[CHUNKS];
     auto load = [&](int64_t row) {
         const int64_t i = row < p.rows ? row : 0;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
             const int m = row < p.rows ? all[c] : 0;
             if (p.residual) {
-                x[c] = load_row16<TX, FAST>(either<TX>(p.xb, p.xf), i, col_of(c), m);
-                r[c] = load_row16<TH, FAST>(either<TH>(p.rb, p.rf), i, col_of(c), m);
-            } else {
-                r[c] = load_row16<TH, FAST>(either<TH>(p.xb, p.xf), i, col_of(c), m);
+                r[c].fetch(either<TH>(p.rb, p.rf), i, col_of(c), m);
+                x[c].fetch(either<TX>(p.xb, p.xf), i, col_of(c), m);
+            } else if (kSame) {
+                x[c].fetch(either<TX>(p.xb, p.xf), i, col_of(c), m);
             }
         }
     };
@@ -190,39 +197,44 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(cons
         const bool exists = row < p.rows;
         const int64_t i = exists ? row : 0;
         int n[CHUNKS];
-        Raw16<TH> h[CHUNKS];   // as it is rounded: what the backward pass reads
+        Raw<TH> h[CHUNKS];   // as it is rounded: what the backward pass reads
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
             n[c] = exists ? all[c] : 0;
-            h[c] = r[c];
-            if (p.residual) add_rows<TX, TH>(x[c], h[c]);
+            const Raw<TX> in = x[c].land(either<TX>(p.xb, p.xf), i, col_of(c), n[c]);
+            if (p.residual) {
+                h[c] = r[c].land(either<TH>(p.rb, p.rf), i, col_of(c), n[c]);
+                add_rows<TX, TH>(in, h[c]);
+            } else if constexpr (kSame) {
+                h[c] = in;
+            }
         }
         if (kAhead && first + step < p.rows) load(row + step);
         float squares = 0.f;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            if (p.residual) store_row16<TH, FAST>(either<TH>(p.hb, p.hf), i, col_of(c), n[c], h[c], lanes);
+            if (p.residual) store_row<TH, GRID_OUT>(either<TH>(p.hb, p.hf), i, col_of(c), n[c], h[c], lanes);
 #pragma unroll
             for (int e = 0; e < 16; e++) squares = fmaf(h[c][e], h[c][e], squares);
         }
-        const float mean = team_sum(squares, team, red, which) * p.inv_cols, rstd = __frcp_rn(__fsqrt_rn(mean + p.eps));
+        const float mean = team_sum(squares, team, at, red, which) * p.inv_cols, rstd = __frcp_rn(__fsqrt_rn(mean + p.eps));
         if (p.rstd && exists && at.in == 0) p.rstd[row] = rstd;
 
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
             const int col = (int)col_of(c);
             float v[16];
-            if (!kAhead) p.weight.load<FAST>(col, n[c], w[0]);
+            if (!kAhead) p.weight.load<GRID_IN, 16>(col, n[c], w[0]);
 #pragma unroll
             for (int e = 0; e < 16; e++) v[e] = __fmul_rn(__fmul_rn(h[c][e], rstd), w[kAhead ? c : 0][e]);
             if (p.yb.p && !p.y_f32) {
-                Raw16<__nv_bfloat16> y;
+                Raw<__nv_bfloat16> y;
                 y.set(v);
-                store_row16<__nv_bfloat16, FAST>(p.yb, i, col, n[c], y, lanes);
+                store_row<__nv_bfloat16, GRID_OUT>(p.yb, i, col, n[c], y, lanes);
             } else if (p.yf.p) {
-                Raw16<float> y;
+                Raw<float> y;
                 y.set(v);
-                store_row16<float, FAST>(p.yf, i, col, n[c], y, lanes);
+                store_row<float, GRID_OUT>(p.yf, i, col, n[c], y, lanes);
             }
             if (p.format == 0) continue;
             if (n[c] < 16) {   // what is behind the row's end: its codes are 0
@@ -251,7 +263,7 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(cons
                 codes = fp8_codes(v, mx ? inv_scale(code) : fp8_factor(top), false);
                 if (!mx && col % 128 == 0) scale = fp8_scale(top);
             }
-            if (!exists || (FAST && !mx ? n[c] == 0 : col >= (mx ? ((int)cols + 31) / 32 * 32 : (int)cols))) continue;
+            if (!exists || col >= (mx ? ((int)cols + 31) / 32 * 32 : (int)cols)) continue;
             *reinterpret_cast<uint4 *>(p.q + row * p.ld_q + col) = codes;
             if (mx) {
                 if (col % 32 == 0) static_cast<uint8_t *>(p.scale)[row * p.ld_s + col / 32] = (uint8_t)__float_as_int(scale);
@@ -264,8 +276,11 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_kernel(cons
 
 // ---------------------------------------------------------------------------------------- backward
 
-constexpr int kGradCtas = 296;          // of the kernel that sums over rows: two an SM
+constexpr int kGradCtas = 592;          // most CTAs of a kernel that sums over rows: four an SM
 constexpr int64_t kGradFused = 8192;    // columns up to which that is the kernel of dx too
+
+// From a CTA's sums to the next one's: whole 32 bytes.
+__host__ __device__ constexpr int64_t partial_pitch(int64_t cols) { return (cols + 7) / 8 * 8; }
 
 struct GradParams {
     int64_t rows, cols;
@@ -276,38 +291,38 @@ struct GradParams {
     RowsOf<float> dyf, hf, dhf, dxf;
     const float *rstd;
     WeightOf weight;
-    float *partial;          // [CTA][cols]: sums over its rows; NULL: none
+    float *partial;          // [CTA][partial_pitch]: sums over its rows; NULL: none
 };
 
-// Rows blockIdx.x, blockIdx.x + gridDim.x, ... of teams.  The operations of dx are spelled out, so that it is the same with SUMS and without.  With SUMS a CTA has many rows: the next
-// one's elements are on their way while this one's are worked on.
-template <typename TY, typename TH, int CHUNKS, bool SUMS, bool FAST>
-__global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(const __grid_constant__ GradParams p)
+// Rows blockIdx.x, blockIdx.x + gridDim.x, ... of teams, 8 columns a lane and chunk.  Up to 8192 columns the weight and the sums over rows stay in registers, and the next row is on its way
+// while this one is worked on.  The operations of dx are spelled out, so that it is the same whatever else is computed.
+template <typename TY, typename TH, int CHUNKS, bool GRID_IN, bool GRID_OUT>
+__global__ void __launch_bounds__(512, CHUNKS == 1 && sizeof(TH) == 2 ? 2 : 1) rms_norm_bwd_kernel(const __grid_constant__ GradParams p)
 {
     wait_for_predecessor();
     admit_successor();
+    constexpr int E = 8;
+    constexpr bool kHold = CHUNKS <= 2;
     __shared__ float red[2][32];
-    __shared__ float sums[SUMS ? 4096 : 1];   // of the teams of a CTA of 256 threads
+    __shared__ float sums[kHold ? 256 * E : 1];   // of the teams of a CTA of 256 threads
     const int team = p.team, lanes = min(team, 32);
     const Place at(team);
-    const int teams = at.teams;
     const int64_t cols = p.cols;
-    auto col_of = [&](int c) { return ((int64_t)c * team + at.in) * 16; };
+    auto col_of = [&](int c) { return ((int64_t)c * team + at.in) * E; };
     int n[CHUNKS];
+    float dw[kHold ? CHUNKS : 1][E], w[kHold ? CHUNKS : 1][E];
 #pragma unroll
-    for (int c = 0; c < CHUNKS; c++) n[c] = columns16(col_of(c), cols);
-    float dw[SUMS ? CHUNKS : 1][16], w[SUMS ? CHUNKS : 1][16];
-    if (SUMS) {
+    for (int c = 0; c < CHUNKS; c++) {
+        n[c] = columns_at<E>(col_of(c), cols);
+        if (kHold) {
+            p.weight.load<GRID_IN, E>(col_of(c), n[c], w[kHold ? c : 0]);
 #pragma unroll
-        for (int c = 0; c < CHUNKS; c++) {
-            p.weight.load<FAST>(col_of(c), n[c], w[c]);
-#pragma unroll
-            for (int e = 0; e < 16; e++) dw[c][e] = 0.f;
+            for (int e = 0; e < E; e++) dw[kHold ? c : 0][e] = 0.f;
         }
     }
     struct Row {
-        Raw16<TY> dy[CHUNKS];
-        Raw16<TH> h[CHUNKS], dh[CHUNKS];
+        Pieces<TY, GRID_IN, E> dy[CHUNKS];
+        Pieces<TH, GRID_IN, E> h[CHUNKS], dh[CHUNKS];
         float r;
     };
     auto load = [&](Row &to, int64_t row) {
@@ -316,70 +331,78 @@ __global__ void __launch_bounds__(CHUNKS == 4 ? 1024 : 512) rms_norm_bwd_kernel(
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
             const int m = exists ? n[c] : 0;
-            to.dy[c] = load_row16<TY, FAST>(either<TY>(p.dyb, p.dyf), i, col_of(c), m);
-            to.h[c] = load_row16<TH, FAST>(either<TH>(p.hb, p.hf), i, col_of(c), m);
-            if (p.dh) to.dh[c] = load_row16<TH, FAST>(either<TH>(p.dhb, p.dhf), i, col_of(c), m);
+            to.dy[c].fetch(either<TY>(p.dyb, p.dyf), i, col_of(c), m);
+            to.h[c].fetch(either<TH>(p.hb, p.hf), i, col_of(c), m);
+            if (p.dh) to.dh[c].fetch(either<TH>(p.dhb, p.dhf), i, col_of(c), m);
         }
         to.r = exists ? load_global(p.rstd + i) : 0.f;
     };
-    int which = 0;
-    const int64_t mine = (int64_t)blockIdx.x * teams, step = (int64_t)gridDim.x * teams;
+    int64_t first = (int64_t)blockIdx.x * at.teams;
+    const int64_t step = (int64_t)gridDim.x * at.teams;
     Row next;
-    if (SUMS && mine < p.rows) load(next, mine + at.team);
-    for (int64_t first = mine; first < p.rows; first += step, which ^= 1) {
+    if (kHold && first < p.rows) load(next, first + at.team);
+    for (int which = 0; first < p.rows; first += step, which ^= 1) {
         const int64_t row = first + at.team;
         const bool exists = row < p.rows;
-        Row now;
-        if (SUMS) {
-            now = next;
-            if (first + step < p.rows) load(next, row + step);
-        } else {
-            load(now, row);
+        const int64_t i = exists ? row : 0;
+        if (!kHold) load(next, row);
+        Raw<TY, E> dy[CHUNKS];
+        Raw<TH, E> h[CHUNKS], dh[CHUNKS];
+        const float r = next.r;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; c++) {
+            const int m = exists ? n[c] : 0;
+            dy[c] = next.dy[c].land(either<TY>(p.dyb, p.dyf), i, col_of(c), m);
+            h[c] = next.h[c].land(either<TH>(p.hb, p.hf), i, col_of(c), m);
+            if (p.dh) dh[c] = next.dh[c].land(either<TH>(p.dhb, p.dhf), i, col_of(c), m);
         }
+        if (kHold && first + step < p.rows) load(next, row + step);
         float dot = 0.f;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            float wc[16];
-            if (!SUMS) p.weight.load<FAST>(col_of(c), n[c], wc);
+            const int k = kHold ? c : 0;
+            if (!kHold) p.weight.load<GRID_IN, E>(col_of(c), n[c], w[0]);
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                const float x = __fmul_rn(now.h[c][e], now.r);
-                dot = fmaf(__fmul_rn(now.dy[c][e], SUMS ? w[SUMS ? c : 0][e] : wc[e]), x, dot);
-                if (SUMS) dw[SUMS ? c : 0][e] = fmaf(now.dy[c][e], x, dw[SUMS ? c : 0][e]);   // rows that do not exist are zeros
+            for (int e = 0; e < E; e++) {
+                const float x = __fmul_rn(h[c][e], r);
+                dot = fmaf(__fmul_rn(dy[c][e], w[k][e]), x, dot);
+                if (kHold) dw[k][e] = fmaf(dy[c][e], x, dw[k][e]);   // rows that do not exist are zeros
             }
         }
-        const float mean = team_sum(dot, team, red, which) * p.inv_cols;
+        const float mean = team_sum(dot, team, at, red, which) * p.inv_cols;
 #pragma unroll
         for (int c = 0; c < CHUNKS; c++) {
-            float wc[16], v[16];
-            if (!SUMS) p.weight.load<FAST>(col_of(c), n[c], wc);
+            const int k = kHold ? c : 0;
+            float v[E];
+            if (!kHold) p.weight.load<GRID_IN, E>(col_of(c), n[c], w[0]);
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                const float g = __fmul_rn(now.dy[c][e], SUMS ? w[SUMS ? c : 0][e] : wc[e]);
-                v[e] = __fmul_rn(now.r, fmaf(-__fmul_rn(now.h[c][e], now.r), mean, g));
-                if (p.dh) v[e] = __fadd_rn(v[e], now.dh[c][e]);
+            for (int e = 0; e < E; e++) {
+                v[e] = __fmul_rn(r, fmaf(-__fmul_rn(h[c][e], r), mean, __fmul_rn(dy[c][e], w[k][e])));
+                if (p.dh) v[e] = __fadd_rn(v[e], dh[c][e]);
             }
-            Raw16<TH> dx;
+            Raw<TH, E> dx;
             dx.set(v);
-            store_row16<TH, FAST>(either<TH>(p.dxb, p.dxf), exists ? row : 0, col_of(c), exists ? n[c] : 0, dx, lanes);
+            store_row<TH, GRID_OUT, E>(either<TH>(p.dxb, p.dxf), i, col_of(c), exists ? n[c] : 0, dx, lanes);
         }
     }
-    if (!SUMS) return;
-    float *to = p.partial + (int64_t)blockIdx.x * cols;
-    if (teams == 1) {
+    if (!kHold || !p.partial) return;
+    float *to = p.partial + (int64_t)blockIdx.x * partial_pitch(cols);
+    if (at.teams == 1) {
 #pragma unroll
-        for (int c = 0; c < CHUNKS; c++)
-#pragma unroll
-            for (int e = 0; e < 16; e++)
-                if (col_of(c) + e < cols) to[col_of(c) + e] = dw[SUMS ? c : 0][e];
+        for (int c = 0; c < CHUNKS; c++) {
+            const float *d = dw[kHold ? c : 0];
+            if (n[c] == 0) continue;   // columns that do not exist, up to the pitch, are zeros
+            reinterpret_cast<float4 *>(to + col_of(c))[0] = make_float4(d[0], d[1], d[2], d[3]);
+            reinterpret_cast<float4 *>(to + col_of(c))[1] = make_float4(d[4], d[5], d[6], d[7]);
+        }
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 16; e++) sums[threadIdx.x * 16 + e] = dw[0][e];
+    for (int e = 0; e < E; e++) sums[threadIdx.x * E + e] = dw[0][e];
     __syncthreads();
     for (int c = threadIdx.x; c < cols; c += blockDim.x) {
         float v = 0.f;
-        for (int k = 0; k < teams; k++) v += sums[(k * team + (c >> 4)) * 16 + (c & 15)];
+        for (int k = 0; k < at.teams; k++) v += sums[(k * team + c / E) * E + c % E];
         to[c] = v;
     }
 }
@@ -393,13 +416,13 @@ __global__ void __launch_bounds__(256) rms_norm_dweight_kernel(const __grid_cons
     __shared__ float sums[8 * 512];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t col = (int64_t)blockIdx.x * 512 + lane * 16;
-    const int n = columns16(col, p.cols);
+    const int n = columns_at(col, p.cols);
     float dw[16];
 #pragma unroll
     for (int e = 0; e < 16; e++) dw[e] = 0.f;
     for (int64_t i = (int64_t)blockIdx.y * 8 + warp; i < p.rows; i += (int64_t)gridDim.y * 8) {
-        const Raw16<TY> dy = load_row16<TY>(either<TY>(p.dyb, p.dyf), i, col, n);
-        const Raw16<TH> h = load_row16<TH>(either<TH>(p.hb, p.hf), i, col, n);
+        const Raw<TY> dy = load_row<TY>(either<TY>(p.dyb, p.dyf), i, col, n);
+        const Raw<TH> h = load_row<TH>(either<TH>(p.hb, p.hf), i, col, n);
         const float r = load_global(p.rstd + i);
 #pragma unroll
         for (int e = 0; e < 16; e++) dw[e] = fmaf(dy[e], h[e] * r, dw[e]);
@@ -411,35 +434,35 @@ __global__ void __launch_bounds__(256) rms_norm_dweight_kernel(const __grid_cons
         float v = 0.f;
 #pragma unroll
         for (int k = 0; k < 8; k++) v += sums[k * 512 + c];
-        if ((int64_t)blockIdx.x * 512 + c < p.cols) p.partial[(int64_t)blockIdx.y * p.cols + (int64_t)blockIdx.x * 512 + c] = v;
+        if ((int64_t)blockIdx.x * 512 + c < p.cols) p.partial[(int64_t)blockIdx.y * partial_pitch(p.cols) + (int64_t)blockIdx.x * 512 + c] = v;
     }
 }
 
-// dweight (+)= the sum of `parts` rows of partial sums, 32 columns a CTA.
+// dweight (+)= the sum of `parts` rows of partial sums, 32 columns a CTA of 32 warps, which take the rows in turn.
 struct SumParams {
     const float *partial;
     int64_t cols;
     int32_t parts, accumulate;
     float *dweight;
 };
-__global__ void __launch_bounds__(256) column_sum_kernel(const __grid_constant__ SumParams p)
+__global__ void __launch_bounds__(1024) column_sum_kernel(const __grid_constant__ SumParams p)
 {
     wait_for_predecessor();
     admit_successor();
-    __shared__ float sums[8][32];
+    __shared__ float sums[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t col = (int64_t)blockIdx.x * 32 + lane;
     float v = 0.f;
     if (col < p.cols)
 #pragma unroll 8
-        for (int k = warp; k < p.parts; k += 8) v += load_global(p.partial + (int64_t)k * p.cols + col);
+        for (int k = warp; k < p.parts; k += 32) v += load_global(p.partial + (int64_t)k * partial_pitch(p.cols) + col);
     sums[warp][lane] = v;
     __syncthreads();
-    if (warp != 0 || col >= p.cols) return;
-    v = 0.f;
+    v = sums[lane][warp];   // a warp has a column
 #pragma unroll
-    for (int k = 0; k < 8; k++) v += sums[k][lane];
-    p.dweight[col] = p.accumulate ? p.dweight[col] + v : v;
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    const int64_t mine = (int64_t)blockIdx.x * 32 + warp;
+    if (lane == 0 && mine < p.cols) p.dweight[mine] = p.accumulate ? p.dweight[mine] + v : v;
 }
 
 bool plain_type(fp4q_out t) { return t == FP4Q_OUT_BF16 || t == FP4Q_OUT_F32; }
@@ -452,47 +475,68 @@ fp4q_status check_matrix(const void *p, int64_t ld, fp4q_out type, int64_t cols)
     return aligned(p, size_of(type)) ? FP4Q_OK : FP4Q_ERR_ALIGN;
 }
 constexpr int64_t kMostCols = 65536;
-constexpr int kNormThreads = 148 * 2 * 256;   // of a grid whose CTAs take rows in turn: all of them run at once (16384 x 4096 104 us; 4 x 256 an SM 105, one row each 165)
 
-template <typename TX, typename TH>
-fp4q_status launch_norm(const NormParams &p, const Deal &d, bool fast, cudaStream_t s)
+// CTAs that an SM has room for, by their registers.  A grid of as many whose CTAs take rows in turn leaves no CTA for later (16384 x 4096: three an SM 102 us, two 128, a row each 165).
+template <typename P>
+int resident(void (*kernel)(const P), int threads, std::atomic<int> &known)
 {
-    const int64_t ctas = ceil_div(p.rows, d.threads / d.team);
-    const dim3 grid((unsigned)std::min<int64_t>(ctas, kNormThreads / d.threads));
-    return launched(d.chunks == 1   ? fast ? launch_dependent(rms_norm_kernel<TX, TH, 1, true>, grid, d.threads, s, p) : launch_dependent(rms_norm_kernel<TX, TH, 1, false>, grid, d.threads, s, p)
-                    : d.chunks == 2 ? launch_dependent(rms_norm_kernel<TX, TH, 2, false>, grid, d.threads, s, p)
-                                    : launch_dependent(rms_norm_kernel<TX, TH, 4, false>, grid, d.threads, s, p));
+    int regs = known.load(std::memory_order_relaxed);
+    if (regs == 0) {
+        cudaFuncAttributes a;
+        if (cudaFuncGetAttributes(&a, reinterpret_cast<const void *>(kernel)) != cudaSuccess) {
+            cudaGetLastError();
+            return 1;
+        }
+        regs = (a.numRegs + 7) / 8 * 8;
+        known.store(regs, std::memory_order_relaxed);
+    }
+    const int warps = 4 * std::min(16, 16384 / (regs * 32));   // of four schedulers
+    return std::max(1, warps / (threads / 32));
 }
 
-int64_t grad_ctas(int64_t rows, int teams) { return std::max<int64_t>(1, std::min<int64_t>(kGradCtas, ceil_div(rows, teams))); }
+// in, out: the rows of all that is read, or written, begin on 16 bytes.
+template <typename TX, typename TH>
+fp4q_status launch_norm(const NormParams &p, const Deal &d, bool in, bool out, cudaStream_t s)
+{
+    auto launch = [&](auto kernel, std::atomic<int> &known) {
+        const int64_t ctas = ceil_div(p.rows, d.threads / d.team);
+        const dim3 grid((unsigned)std::min<int64_t>(ctas, 148 * resident(kernel, d.threads, known)));
+        return launched(launch_dependent(kernel, grid, d.threads, s, p));
+    };
+    static std::atomic<int> known[5];
+    if (d.chunks == 1) return in && out ? launch(rms_norm_kernel<TX, TH, 1, true, true>, known[0]) : out ? launch(rms_norm_kernel<TX, TH, 1, false, true>, known[1]) : launch(rms_norm_kernel<TX, TH, 1, false, false>, known[2]);
+    return d.chunks == 2 ? launch(rms_norm_kernel<TX, TH, 2, false, false>, known[3]) : launch(rms_norm_kernel<TX, TH, 4, false, false>, known[4]);
+}
 
 template <typename TY, typename TH>
-fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scratch, bool fast, cudaStream_t s)
+fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scratch, bool in, bool out, cudaStream_t s)
 {
-    const Deal d(ceil_div(p.cols, 16));
+    const Deal d(ceil_div(p.cols, 8), true);
     p.team = d.team;
-    const int teams = d.threads / d.team;
     const bool fused = dweight && p.cols <= kGradFused;
     p.partial = dweight ? static_cast<float *>(scratch) : nullptr;
-    int64_t parts = grad_ctas(p.rows, teams);
-    if (fused) {
-        if (fp4q_status st = launched(fast ? launch_dependent(rms_norm_bwd_kernel<TY, TH, 1, true, true>, dim3((unsigned)parts), d.threads, s, p)
-                                              : launch_dependent(rms_norm_bwd_kernel<TY, TH, 1, true, false>, dim3((unsigned)parts), d.threads, s, p))) return st;
-    } else if (p.rows > 0) {
-        const int64_t ctas = ceil_div(p.rows, teams);
-        const dim3 grid((unsigned)std::min<int64_t>(ctas, 0x7FFFFFFF));
-        if (fp4q_status st = launched(d.chunks == 1   ? launch_dependent(rms_norm_bwd_kernel<TY, TH, 1, false, false>, grid, d.threads, s, p)
-                                      : d.chunks == 2 ? launch_dependent(rms_norm_bwd_kernel<TY, TH, 2, false, false>, grid, d.threads, s, p)
-                                                      : launch_dependent(rms_norm_bwd_kernel<TY, TH, 4, false, false>, grid, d.threads, s, p)))
-            return st;
+    int64_t parts = 1;
+    auto launch = [&](auto kernel, std::atomic<int> &known) {
+        parts = std::max<int64_t>(1, std::min({(int64_t)kGradCtas, ceil_div(p.rows, d.threads / d.team), (int64_t)148 * resident(kernel, d.threads, known)}));
+        return launched(launch_dependent(kernel, dim3((unsigned)parts), d.threads, s, p));
+    };
+    static std::atomic<int> known[7];
+    if (fused || p.rows > 0) {
+        const fp4q_status st = d.chunks == 1   ? in && out ? launch(rms_norm_bwd_kernel<TY, TH, 1, true, true>, known[0])
+                                                 : in      ? launch(rms_norm_bwd_kernel<TY, TH, 1, true, false>, known[1])
+                                                           : launch(rms_norm_bwd_kernel<TY, TH, 1, false, false>, known[2])
+                               : d.chunks == 2 ? in && out ? launch(rms_norm_bwd_kernel<TY, TH, 2, true, true>, known[3]) : launch(rms_norm_bwd_kernel<TY, TH, 2, false, false>, known[4])
+                               : d.chunks == 4 ? launch(rms_norm_bwd_kernel<TY, TH, 4, false, false>, known[5])
+                                               : launch(rms_norm_bwd_kernel<TY, TH, 16, false, false>, known[6]);
+        if (st) return st;
     }
     if (!dweight) return FP4Q_OK;
     if (!fused) {
-        parts = std::max<int64_t>(1, std::min<int64_t>(kGradCtas, ceil_div(p.rows, 8)));
+        parts = std::max<int64_t>(1, std::min<int64_t>(kGradCtas / 2, ceil_div(p.rows, 8)));
         if (fp4q_status st = launched(launch_dependent(rms_norm_dweight_kernel<TY, TH>, dim3((unsigned)ceil_div(p.cols, 512), (unsigned)parts), 256, s, p))) return st;
     }
     const SumParams q = {p.partial, p.cols, (int32_t)parts, accumulate != 0, dweight};
-    return launched(launch_dependent(column_sum_kernel, dim3((unsigned)ceil_div(p.cols, 32)), 256, s, q));
+    return launched(launch_dependent(column_sum_kernel, dim3((unsigned)ceil_div(p.cols, 32)), 1024, s, q));
 }
 
 }  // namespace
@@ -521,7 +565,7 @@ extern "C" fp4q_status fp4q_rms_norm(const fp4q_norm *n, int64_t rows, int64_t c
         if (!aligned(n->q, 16) || n->ld_q % 16 != 0 || (!mx && !aligned(n->scale, 4))) return FP4Q_ERR_ALIGN;
     }
     if (!aligned(n->rstd, 4)) return FP4Q_ERR_ALIGN;
-    const Deal d(ceil_div(mx ? round_up(cols, 32) : cols, 16));
+    const Deal d(ceil_div(mx ? round_up(cols, 32) : cols, 16), false);
     NormParams p = {};
     p.rows = rows;
     p.cols = cols;
@@ -530,16 +574,16 @@ extern "C" fp4q_status fp4q_rms_norm(const fp4q_norm *n, int64_t rows, int64_t c
     p.eps = n->eps;
     p.inv_cols = 1.f / (float)cols;
     p.residual = n->residual;
-    p.xb = rows_of<__nv_bfloat16>(n->x, rows, cols, n->ld_x);
-    p.xf = rows_of<float>(n->x, rows, cols, n->ld_x);
+    p.xb = rows_of<__nv_bfloat16>(n->x, n->ld_x);
+    p.xf = rows_of<float>(n->x, n->ld_x);
     if (n->residual) {
-        p.rb = rows_of<__nv_bfloat16>(n->residual, rows, cols, n->ld_residual);
-        p.rf = rows_of<float>(n->residual, rows, cols, n->ld_residual);
-        p.hb = rows_of<__nv_bfloat16>(n->h, rows, cols, n->ld_h);
-        p.hf = rows_of<float>(n->h, rows, cols, n->ld_h);
+        p.rb = rows_of<__nv_bfloat16>(n->residual, n->ld_residual);
+        p.rf = rows_of<float>(n->residual, n->ld_residual);
+        p.hb = rows_of<__nv_bfloat16>(n->h, n->ld_h);
+        p.hf = rows_of<float>(n->h, n->ld_h);
     }
-    p.yb = rows_of<__nv_bfloat16>(n->y, rows, cols, n->ld_y);
-    p.yf = rows_of<float>(n->y, rows, cols, n->ld_y);
+    p.yb = rows_of<__nv_bfloat16>(n->y, n->ld_y);
+    p.yf = rows_of<float>(n->y, n->ld_y);
     p.y_f32 = n->y_type == FP4Q_OUT_F32;
     p.weight = weight_of(n->weight, n->weight_type, cols);
     p.q = n->q;
@@ -549,16 +593,17 @@ extern "C" fp4q_status fp4q_rms_norm(const fp4q_norm *n, int64_t rows, int64_t c
     p.rstd = n->rstd;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool x32 = n->x_type == FP4Q_OUT_F32, h32 = n->residual ? n->h_type == FP4Q_OUT_F32 : x32;
-    const bool fast = cols % 16 == 0 && on_grid(n->x, n->ld_x, rows, size_of(n->x_type)) && (!n->residual || (on_grid(n->residual, n->ld_residual, rows, size_of(n->h_type)) && on_grid(n->h, n->ld_h, rows, size_of(n->h_type)))) &&
-                      aligned(n->weight, 16) && (!n->y || on_grid(n->y, n->ld_y, rows, size_of(n->y_type)));
-    if (x32) return h32 ? launch_norm<float, float>(p, d, fast, s) : launch_norm<float, __nv_bfloat16>(p, d, fast, s);
-    return h32 ? launch_norm<__nv_bfloat16, float>(p, d, fast, s) : launch_norm<__nv_bfloat16, __nv_bfloat16>(p, d, fast, s);
+    const size_t xs = size_of(n->x_type), hs = size_of(n->h_type);
+    const bool in = on_grid(n->x, n->ld_x, rows, xs) && on_grid(n->residual, n->ld_residual, rows, hs) && aligned(n->weight, 16);
+    const bool out = (!n->residual || on_grid(n->h, n->ld_h, rows, hs)) && on_grid(n->y, n->ld_y, rows, size_of(n->y_type));
+    if (x32) return h32 ? launch_norm<float, float>(p, d, in, out, s) : launch_norm<float, __nv_bfloat16>(p, d, in, out, s);
+    return h32 ? launch_norm<__nv_bfloat16, float>(p, d, in, out, s) : launch_norm<__nv_bfloat16, __nv_bfloat16>(p, d, in, out, s);
 }
 
 extern "C" size_t fp4q_rms_norm_bwd_scratch_bytes(int64_t rows, int64_t cols)
 {
     if (rows < 0 || cols <= 0 || cols > kMostCols) return 0;
-    return (size_t)round_up(std::max<int64_t>(1, std::min<int64_t>(kGradCtas, rows)) * cols * 4, 256);
+    return (size_t)round_up(std::max<int64_t>(1, std::min<int64_t>(kGradCtas, rows)) * partial_pitch(cols) * 4, 256);
 }
 
 extern "C" fp4q_status fp4q_rms_norm_bwd(const fp4q_norm_grad *n, int64_t rows, int64_t cols, void *scratch, size_t scratch_bytes, void *stream)
@@ -588,21 +633,22 @@ extern "C" fp4q_status fp4q_rms_norm_bwd(const fp4q_norm_grad *n, int64_t rows, 
     p.cols = cols;
     p.inv_cols = 1.f / (float)cols;
     p.dh = n->dh;
-    p.dyb = rows_of<__nv_bfloat16>(n->dy, rows, cols, n->ld_dy);
-    p.dyf = rows_of<float>(n->dy, rows, cols, n->ld_dy);
-    p.hb = rows_of<__nv_bfloat16>(n->h, rows, cols, n->ld_h);
-    p.hf = rows_of<float>(n->h, rows, cols, n->ld_h);
-    p.dhb = rows_of<__nv_bfloat16>(n->dh, rows, cols, n->ld_dh);
-    p.dhf = rows_of<float>(n->dh, rows, cols, n->ld_dh);
-    p.dxb = rows_of<__nv_bfloat16>(n->dx, rows, cols, n->ld_dx);
-    p.dxf = rows_of<float>(n->dx, rows, cols, n->ld_dx);
+    p.dyb = rows_of<__nv_bfloat16>(n->dy, n->ld_dy);
+    p.dyf = rows_of<float>(n->dy, n->ld_dy);
+    p.hb = rows_of<__nv_bfloat16>(n->h, n->ld_h);
+    p.hf = rows_of<float>(n->h, n->ld_h);
+    p.dhb = rows_of<__nv_bfloat16>(n->dh, n->ld_dh);
+    p.dhf = rows_of<float>(n->dh, n->ld_dh);
+    p.dxb = rows_of<__nv_bfloat16>(n->dx, n->ld_dx);
+    p.dxf = rows_of<float>(n->dx, n->ld_dx);
     p.rstd = n->rstd;
     p.weight = weight_of(n->weight, n->weight_type, cols);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool y32 = n->dy_type == FP4Q_OUT_F32, h32 = n->h_type == FP4Q_OUT_F32;
     const size_t hs = size_of(n->h_type);
-    const bool fast = cols % 16 == 0 && on_grid(n->dy, n->ld_dy, rows, size_of(n->dy_type)) && on_grid(n->h, n->ld_h, rows, hs) && on_grid(n->dh, n->ld_dh, rows, hs) &&
-                      on_grid(n->dx, n->ld_dx, rows, hs) && aligned(n->weight, 16);
-    if (y32) return h32 ? launch_grad<float, float>(p, n->dweight, n->accumulate, scratch, fast, s) : launch_grad<float, __nv_bfloat16>(p, n->dweight, n->accumulate, scratch, fast, s);
-    return h32 ? launch_grad<__nv_bfloat16, float>(p, n->dweight, n->accumulate, scratch, fast, s) : launch_grad<__nv_bfloat16, __nv_bfloat16>(p, n->dweight, n->accumulate, scratch, fast, s);
+    const bool in = on_grid(n->dy, n->ld_dy, rows, size_of(n->dy_type)) && on_grid(n->h, n->ld_h, rows, hs) && on_grid(n->dh, n->ld_dh, rows, hs) && aligned(n->weight, 16);
+    const bool out = on_grid(n->dx, n->ld_dx, rows, hs);
+    if (y32) return h32 ? launch_grad<float, float>(p, n->dweight, n->accumulate, scratch, in, out, s) : launch_grad<float, __nv_bfloat16>(p, n->dweight, n->accumulate, scratch, in, out, s);
+    return h32 ? launch_grad<__nv_bfloat16, float>(p, n->dweight, n->accumulate, scratch, in, out, s)
+               : launch_grad<__nv_bfloat16, __nv_bfloat16>(p, n->dweight, n->accumulate, scratch, in, out, s);
 }
