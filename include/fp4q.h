@@ -549,6 +549,7 @@ fp4q_status fp4q_rms_norm_bwd(const fp4q_norm_grad *n, int64_t rows, int64_t col
  * the order is fixed.  `tensors` is a HOST array, read during the call; empty tensors are skipped; without any the norm is 0.
  * fp4q_clip_by_norm -- out = g * min(1, max_norm / (norm + eps)), every tensor into its entry of `outs` (rounded once; BF16 or FP32, the same shape; not
  * overlapping another's), or in place (outs == NULL; then tensors stay untouched where the factor is 1).  A norm of NaN gives NaN.  max_norm >= 0, eps >= 0.
+ * fp4q_clip_grad_norm -- both, one launch less.
  * scratch: fp4q_global_norm_scratch_bytes() bytes of device memory, 256-byte aligned, any contents; calls that share it must not overlap on the GPU.
  */
 typedef struct {
@@ -559,6 +560,8 @@ typedef struct {
 size_t fp4q_global_norm_scratch_bytes(const fp4q_span *tensors, int32_t n_tensors);
 fp4q_status fp4q_global_norm(const fp4q_span *tensors, int32_t n_tensors, float *norm, void *scratch, size_t scratch_bytes, void *stream);
 fp4q_status fp4q_clip_by_norm(const fp4q_span *tensors, const fp4q_span *outs, int32_t n_tensors, const float *norm, float max_norm, float eps, void *stream);
+fp4q_status fp4q_clip_grad_norm(const fp4q_span *tensors, const fp4q_span *outs, int32_t n_tensors, float max_norm, float eps, float *norm, void *scratch, size_t scratch_bytes,
+                                void *stream);
 
 const char *fp4q_status_string(fp4q_status s);
 

@@ -36,7 +36,7 @@ EXPORTS = ["fp4q_quantize2d", "fp4q_gemm_fwd", "fp4q_gemm_dgrad", "fp4q_gemm_wgr
            "fp4q_quantize2d_multi_f32", "fp4q_ragged_gemm_fwd", "fp4q_ragged_gemm_dgrad", "fp4q_ragged_gemm_wgrad",
            "fp4q_ragged_gemm_wgrad_scratch_bytes", "fp4q_newton_schulz", "fp4q_newton_schulz_scratch_bytes",
            "fp4q_fp8_quantize", "fp4q_fp8_gemm_fwd", "fp4q_fp8_gemm_dgrad", "fp4q_fp8_gemm_wgrad", "fp4q_rms_norm", "fp4q_rms_norm_bwd",
-           "fp4q_rms_norm_bwd_scratch_bytes", "fp4q_global_norm", "fp4q_global_norm_scratch_bytes", "fp4q_clip_by_norm"]
+           "fp4q_rms_norm_bwd_scratch_bytes", "fp4q_global_norm", "fp4q_global_norm_scratch_bytes", "fp4q_clip_by_norm", "fp4q_clip_grad_norm"]
 
 
 class Fp4qError(RuntimeError):
@@ -189,6 +189,8 @@ def lib() -> ctypes.CDLL:
         L.fp4q_global_norm_scratch_bytes.argtypes = [spans, ctypes.c_int32]
         L.fp4q_clip_by_norm.restype = ci
         L.fp4q_clip_by_norm.argtypes = [spans, spans, ctypes.c_int32, vp, ctypes.c_float, ctypes.c_float, vp]
+        L.fp4q_clip_grad_norm.restype = ci
+        L.fp4q_clip_grad_norm.argtypes = [spans, spans, ctypes.c_int32, ctypes.c_float, ctypes.c_float, vp, vp, sz, vp]
         _lib = L
     return _lib
 

@@ -159,6 +159,26 @@ __device__ __forceinline__ void store_one(const Gemm8Params &p, int64_t row, int
     }
 }
 
+// Columns col .. col + 3 of a row, of which those below n exist; col is a multiple of four.
+__device__ __forceinline__ void store_four(const Gemm8Params &p, int64_t row, int col, int n, float4 v)
+{
+    if (col + 4 > n) {
+        const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (col + e < n) store_one(p, row, col + e, w[e]);
+    } else if (p.f32) {
+        float4 *c = reinterpret_cast<float4 *>(static_cast<float *>(p.c) + row * p.ldc + col);
+        if (p.accumulate) {
+            const float4 o = *c;
+            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+        }
+        *c = v;
+    } else {
+        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.c) + row * p.ldc + col) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+    }
+}
+
 // A box of 32 rows x 128 bytes, COLS columns from col on, leaves an epilogue warp.  w: the lane's row of it, value(e): its elements.
 template <int COLS, typename F>
 __device__ __forceinline__ void send_box(const Gemm8Params &p, const CUtensorMap *map, const Box16 &box, uint32_t box_at, const uint32_t *w, int row0, int col, int lane, F value)
@@ -224,9 +244,11 @@ struct Cfg8 {
     static constexpr int kAccs = BN == 128 ? 2 : 4, kTmemCols = kAccs * BN < 32 ? 32 : kAccs * BN;
     static constexpr int kRowScales = MODE == SCALE_COLS ? 0 : 128, kColScales = MODE == SCALE_ROWS ? 0 : BN;
     static constexpr int kAhead = 4, kScales = kAhead * (kRowScales + kColScales);   // of four blocks; there are two such sets
-    static constexpr int kPitch = 129;                                     // of the CTA's sums where the cluster adds them up, in the operands' place
+    // Where the cluster adds up its CTAs' sums they lie in the operands' place: lines along what is consecutive in the output (SCALE_COLS: the tile's 128 rows), 4 more a line than
+    // it has, so that neither side's accesses meet in a bank.
+    static constexpr int kLine = MODE == SCALE_COLS ? 128 : BN, kLines = MODE == SCALE_COLS ? BN : 128, kPitch = kLine + 4;
     static constexpr int kSmem = 1024 + kOperands + 2 * kScales * 4 + 256;
-    static_assert(kPitch * BN * 4 <= kOperands && kSmem <= 227 * 1024, "shared memory budget");
+    static_assert(kPitch * kLines * 4 <= kOperands && kSmem <= 227 * 1024, "shared memory budget");
 };
 
 template <int BN, int MODE>
@@ -352,9 +374,14 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
             }
         } else {
             // All MMAs of this CTA are done, so its operands' place is free.
-            float *mine = reinterpret_cast<float *>(smem) + in;
+            float *mine = reinterpret_cast<float *>(smem);
+            if (MODE == SCALE_COLS) {
 #pragma unroll
-            for (int c = 0; c < C::kCols; c++) mine[(half * C::kCols + c) * C::kPitch] = sum[c];
+                for (int c = 0; c < C::kCols; c++) mine[(half * C::kCols + c) * C::kPitch + in] = sum[c];
+            } else {
+#pragma unroll
+                for (int c = 0; c < C::kCols; c += 4) *reinterpret_cast<float4 *>(mine + in * C::kPitch + half * C::kCols + c) = make_float4(sum[c], sum[c + 1], sum[c + 2], sum[c + 3]);
+            }
         }
     }
     __syncwarp();
@@ -363,20 +390,24 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
         cluster_wait();
         // This CTA's share of the tile: the sums of all CTAs, in their order.
         if (*abort_flag == 0u) {
-            const uint32_t base = smem_u32(smem);
-            constexpr int kTile = 128 * BN;
-            const int e0 = (int)((int64_t)kTile * rank / p.split), e1 = (int)((int64_t)kTile * (rank + 1) / p.split);
+            constexpr int kFours = C::kLine / 4 * C::kLines;
+            const int e0 = (int)((int64_t)kFours * rank / p.split), e1 = (int)((int64_t)kFours * (rank + 1) / p.split);
             for (int e = e0 + threadIdx.x; e < e1; e += C::kThreads) {
-                const int row = MODE == SCALE_COLS ? e % 128 : e / BN, col = MODE == SCALE_COLS ? e / 128 : e % BN;
-                if (m0 + row >= p.m || n0 + col >= p.n) continue;
-                float v = 0.f;
-                for (int r = 0; r < p.split; r++) {
-                    float x;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(cluster_addr(base + (col * C::kPitch + row) * 4, r)) : "memory");
-                    v += x;
-                }
-                if (MODE == SCALE_COLS) store_one(p, n0 + col, m0 + row, v);
-                else store_one(p, m0 + row, n0 + col, v);
+                const int line = e / (C::kLine / 4), at = e % (C::kLine / 4) * 4;
+                const int64_t row = MODE == SCALE_COLS ? n0 + line : m0 + line;      // of the output
+                const int col = MODE == SCALE_COLS ? m0 + at : n0 + at, rows = MODE == SCALE_COLS ? p.n : p.m, cols = MODE == SCALE_COLS ? p.m : p.n;
+                if (row >= rows || col >= cols) continue;
+                const uint32_t from = smem_u32(smem) + (line * C::kPitch + at) * 4;
+                float4 x[8];   // on their way together
+#pragma unroll
+                for (int r = 0; r < 8; r++)
+                    if (r < p.split)
+                        asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[r].x), "=f"(x[r].y), "=f"(x[r].z), "=f"(x[r].w) : "r"(cluster_addr(from, r)) : "memory");
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int r = 0; r < 8; r++)
+                    if (r < p.split) { v.x += x[r].x; v.y += x[r].y; v.z += x[r].z; v.w += x[r].w; }
+                store_four(p, row, col, cols, v);
             }
         }
         __syncwarp();
@@ -766,13 +797,29 @@ fp4q_status launch_persistent(const Operand8 &a, const Operand8 &b, Gemm8Params 
     return launched(cudaLaunchKernelEx(&cfg, gemm8_kernel<CTAS, MODE>, maps, p));
 }
 
-// CTAs that share a tile's contraction: as many as fill the GPU's places, with two blocks each at least.
-int split_of(int64_t tiles, int64_t places, int64_t blocks)
-{
-    return (int)std::max<int64_t>(1, std::min<int64_t>({8, places / tiles, blocks / 2}));
-}
+// How a product is computed, by estimated time.  Rounds of tiles: a block takes 0.365 us in a single CTA's tile of the persistent kernel (0.51 where both operands' scales differ inside a tile), 0.55 (0.87) in a
+// pair's, four times as large, and a tile 1.3 or 2.2 us beside its blocks; 0.40 (0.60) and 2 us in a tile of a CTA to itself, whose contraction a cluster may share for about 3 us.
+// (4096 x 4096 x 4096: pairs 70 us, single CTAs 82; 2731 x 1003 for 1999 rows 13 and 12.5; 512 x 4096 x 4096 19 and 12.5; 128 x 4096 x 4096 in clusters of four 9, single CTAs 12.5;
+// a weight gradient of 256 x 256 over 16384 rows in clusters of eight 15, single CTAs 72.)
+struct Plan8 {
+    int pairs = 0, split = 1;   // pairs: 2, single CTAs: 1, clusters of `split` CTAs with a tile: 0
+    Plan8(int64_t m, int64_t n, int64_t blocks, bool both, bool boxes)
+    {
+        const double each = both ? 0.60 : 0.40;
+        double least = 1e30;
+        auto consider = [&](double us, int p, int s) {
+            if (us < least) { least = us; pairs = p; split = s; }
+        };
+        const int64_t tiles = ceil_div(m, 128) * ceil_div(n, 128);
+        for (int64_t s = 1; s <= 8 && (s == 1 || s * 2 <= blocks); s++)
+            consider((double)ceil_div(tiles * s, 148) * ((double)ceil_div(blocks, s) * each + 2.0) + (s > 1 ? 2.5 + 0.15 * (double)s : 0.0), 0, (int)s);
+        if (!boxes) return;
+        consider((double)ceil_div(tiles, 148) * ((double)blocks * (both ? 0.51 : 0.365) + 1.3), 1, 1);
+        consider((double)ceil_div(ceil_div(m, 256) * ceil_div(n, 256), 74) * ((double)blocks * (both ? 0.87 : 0.55) + 2.2), 2, 1);
+    }
+};
 
-// mode: SCALE_ROWS: C[m, n] with A in 1D blocks and B in square ones; SCALE_BOTH: both in 1D blocks.
+// SCALE_ROWS: C[m, n] with A in 1D blocks and B in square ones; both: both in 1D blocks.
 fp4q_status product8(const Operand8 &a, const Operand8 &b, Gemm8Params p, bool both, cudaStream_t stream)
 {
     p.m = (int32_t)a.rows;
@@ -780,17 +827,17 @@ fp4q_status product8(const Operand8 &a, const Operand8 &b, Gemm8Params p, bool b
     p.blocks = (int32_t)ceil_div(a.cols, kBlock8);
     p.sa = a.scales;
     p.sb = b.scales;
-    if (!both && a.rows <= 64) {   // few tokens: B's rows become the tile's 128 rows
+    if (!both && a.rows <= 64) {   // few tokens: B's rows become the tile's 128 rows, of which an SM has room for two tiles; B is read at memory's pace when all SMs read
         std::swap(p.m, p.n);
         std::swap(p.sa, p.sb);
-        const int bn = a.rows <= 16 ? 16 : a.rows <= 32 ? 32 : 64, split = split_of(ceil_div(b.rows, 128), 296, p.blocks);
-        return bn == 16 ? launch_tiles<16, SCALE_COLS>(b, a, p, split, stream) : bn == 32 ? launch_tiles<32, SCALE_COLS>(b, a, p, split, stream) : launch_tiles<64, SCALE_COLS>(b, a, p, split, stream);
+        const int64_t tiles = ceil_div(b.rows, 128);
+        const int split = (int)std::max<int64_t>(1, std::min<int64_t>({8, tiles <= 64 ? ceil_div(160, tiles) : 296 / tiles, p.blocks / 2}));
+        return a.rows <= 16 ? launch_tiles<16, SCALE_COLS>(b, a, p, split, stream) : a.rows <= 32 ? launch_tiles<32, SCALE_COLS>(b, a, p, split, stream) : launch_tiles<64, SCALE_COLS>(b, a, p, split, stream);
     }
-    const int64_t tiles = ceil_div(a.rows, 128) * ceil_div(b.rows, 128);
-    const int split = split_of(tiles, 148, p.blocks);
-    if (p.boxed == 0 || tiles <= 148) return both ? launch_tiles<128, SCALE_BOTH>(a, b, p, split, stream) : launch_tiles<128, SCALE_ROWS>(a, b, p, split, stream);
-    if (ceil_div(a.rows, 256) * ceil_div(b.rows, 256) >= 74) return both ? launch_persistent<2, SCALE_BOTH>(a, b, p, stream) : launch_persistent<2, SCALE_ROWS>(a, b, p, stream);
-    return both ? launch_persistent<1, SCALE_BOTH>(a, b, p, stream) : launch_persistent<1, SCALE_ROWS>(a, b, p, stream);
+    const Plan8 plan(a.rows, b.rows, p.blocks, both, p.boxed > 0);
+    if (plan.pairs == 2) return both ? launch_persistent<2, SCALE_BOTH>(a, b, p, stream) : launch_persistent<2, SCALE_ROWS>(a, b, p, stream);
+    if (plan.pairs == 1) return both ? launch_persistent<1, SCALE_BOTH>(a, b, p, stream) : launch_persistent<1, SCALE_ROWS>(a, b, p, stream);
+    return both ? launch_tiles<128, SCALE_BOTH>(a, b, p, plan.split, stream) : launch_tiles<128, SCALE_ROWS>(a, b, p, plan.split, stream);
 }
 
 // Row-major codes (transposed: of the transpose), which may be missing from a tensor that has none of these elements.

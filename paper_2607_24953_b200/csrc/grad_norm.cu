@@ -29,7 +29,8 @@ struct SpanParams {
     int64_t chunks;
     int32_t n, in_place;
     double *partial;
-    const float *norm;
+    int64_t parts;          // scaling: sums that the norm is the root of, and where it goes; 0: the norm is there
+    float *norm;
     float max_norm, eps;
     Span span[N];
 };
@@ -168,6 +169,21 @@ __global__ void __launch_bounds__(256) sum_squares_kernel(const __grid_constant_
     p.partial[blockIdx.x] = total;
 }
 
+// The root of the sum of the CTAs' sums, the same in every CTA of 256 threads that comes here.
+__device__ __forceinline__ float root_of(const double *partial, int64_t n, double *shared)
+{
+    double total = 0.0;
+    for (int64_t i = threadIdx.x; i < n; i += 256) total += load_global(partial + i);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, d);
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = total;
+    __syncthreads();
+    total = 0.0;
+#pragma unroll
+    for (int k = 0; k < 8; k++) total += shared[k];
+    return (float)sqrt(total);
+}
+
 struct RootParams {
     const double *partial;
     int64_t n;
@@ -178,17 +194,8 @@ __global__ void __launch_bounds__(256) root_kernel(const __grid_constant__ RootP
     wait_for_predecessor();
     admit_successor();
     __shared__ double sums[8];
-    double total = 0.0;
-    for (int64_t i = threadIdx.x; i < p.n; i += 256) total += load_global(p.partial + i);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, d);
-    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = total;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    total = 0.0;
-#pragma unroll
-    for (int k = 0; k < 8; k++) total += sums[k];
-    *p.norm = (float)sqrt(total);
+    const float norm = root_of(p.partial, p.n, sums);
+    if (threadIdx.x == 0) *p.norm = norm;
 }
 
 template <int N>
@@ -196,7 +203,10 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Span
 {
     wait_for_predecessor();
     admit_successor();
-    const float ratio = __fdiv_rn(p.max_norm, load_global(p.norm) + p.eps), factor = ratio > 1.f ? 1.f : ratio;
+    __shared__ double sums[8];
+    const float norm = p.parts ? root_of(p.partial, p.parts, sums) : load_global(p.norm);
+    if (p.parts && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
+    const float ratio = __fdiv_rn(p.max_norm, norm + p.eps), factor = ratio > 1.f ? 1.f : ratio;
     if (p.in_place && factor == 1.f) return;
     for (int64_t back = blockIdx.x; back < p.chunks; back += gridDim.x) {
         const int64_t chunk = p.chunks - 1 - back;
@@ -323,6 +333,71 @@ int64_t take_spans(const fp4q_span *t, const fp4q_span *o, int32_t n, int32_t &a
     return std::min<int64_t>(kNormCtas, p.chunks);
 }
 
+// The tensors' sums of squares, one for every CTA; parts: how many.
+fp4q_status launch_sums(const fp4q_span *tensors, int32_t n, double *partial, int64_t &parts, cudaStream_t s)
+{
+    fp4q_status st = FP4Q_OK;
+    parts = 0;
+    auto launch = [&](auto &p, auto kernel, int32_t &at) {
+        p.partial = partial + parts;
+        const int64_t ctas = take_spans(tensors, tensors, n, at, p);
+        parts += ctas;
+        if (ctas) st = launched(launch_dependent(kernel, dim3((unsigned)ctas), 256, s, p));
+    };
+    for (int32_t at = 0; at < n && !st;) {
+        if (n - at <= kFew) {
+            SpanParams<kFew> p = {};
+            launch(p, sum_squares_kernel<kFew>, at);
+        } else {
+            SpanParams<kMany> p = {};
+            launch(p, sum_squares_kernel<kMany>, at);
+        }
+    }
+    return st;
+}
+// parts: the norm is still to be taken from so many sums (and nothing may have overwritten them when the last launch has begun); 0: it is there.
+fp4q_status launch_scaling(const fp4q_span *tensors, const fp4q_span *outs, int32_t n, float *norm, double *partial, int64_t parts, float max_norm, float eps, cudaStream_t s)
+{
+    fp4q_status st = FP4Q_OK;
+    auto launch = [&](auto &p, auto kernel, int32_t &at) {
+        p.norm = norm;
+        p.partial = partial;
+        p.parts = parts;
+        p.max_norm = max_norm;
+        p.eps = eps;
+        p.in_place = !outs;
+        const int64_t ctas = take_spans(tensors, outs ? outs : tensors, n, at, p);
+        if (ctas) st = launched(launch_dependent(kernel, dim3((unsigned)ctas), 256, s, p));
+    };
+    for (int32_t at = 0; at < n && !st;) {
+        if (n - at <= kFew) {
+            SpanParams<kFew> p = {};
+            launch(p, scale_kernel<kFew>, at);
+        } else {
+            SpanParams<kMany> p = {};
+            launch(p, scale_kernel<kMany>, at);
+        }
+    }
+    return st;
+}
+fp4q_status check_norm(const float *norm, const fp4q_span *tensors, int32_t n, void *scratch, size_t scratch_bytes)
+{
+    if (!norm) return FP4Q_ERR_NULL;
+    if (!aligned(norm, 4)) return FP4Q_ERR_ALIGN;
+    if (!scratch || scratch_bytes < fp4q_global_norm_scratch_bytes(tensors, n)) return FP4Q_ERR_WORKSPACE;
+    return aligned(scratch, 256) ? FP4Q_OK : FP4Q_ERR_ALIGN;
+}
+fp4q_status check_clip(const fp4q_span *tensors, const fp4q_span *outs, int32_t n, float max_norm, float eps)
+{
+    if (fp4q_status s = check_spans(tensors, n)) return s;
+    if (outs) {
+        if (fp4q_status s = check_spans(outs, n)) return s;
+        for (int32_t i = 0; i < n; i++)
+            if (outs[i].rows != tensors[i].rows || outs[i].cols != tensors[i].cols) return FP4Q_ERR_SHAPE;
+    }
+    return max_norm >= 0.f && eps >= 0.f ? FP4Q_OK : FP4Q_ERR_UNSUPPORTED;
+}
+
 }  // namespace
 
 extern "C" size_t fp4q_global_norm_scratch_bytes(const fp4q_span *tensors, int32_t n_tensors)
@@ -334,62 +409,35 @@ extern "C" size_t fp4q_global_norm_scratch_bytes(const fp4q_span *tensors, int32
 extern "C" fp4q_status fp4q_global_norm(const fp4q_span *tensors, int32_t n_tensors, float *norm, void *scratch, size_t scratch_bytes, void *stream)
 {
     if (fp4q_status s = check_spans(tensors, n_tensors)) return s;
-    if (!norm) return FP4Q_ERR_NULL;
-    if (!aligned(norm, 4)) return FP4Q_ERR_ALIGN;
-    if (!scratch || scratch_bytes < fp4q_global_norm_scratch_bytes(tensors, n_tensors)) return FP4Q_ERR_WORKSPACE;
-    if (!aligned(scratch, 256)) return FP4Q_ERR_ALIGN;
+    if (fp4q_status s = check_norm(norm, tensors, n_tensors, scratch, scratch_bytes)) return s;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     double *partial = static_cast<double *>(scratch);
-    int64_t parts = 0;
-    fp4q_status st = FP4Q_OK;
-    auto launch = [&](auto &p, auto kernel, int32_t &at) {
-        p.partial = partial + parts;
-        const int64_t ctas = take_spans(tensors, tensors, n_tensors, at, p);
-        parts += ctas;
-        if (ctas) st = launched(launch_dependent(kernel, dim3((unsigned)ctas), 256, s, p));
-    };
-    for (int32_t at = 0; at < n_tensors && !st;) {
-        if (n_tensors - at <= kFew) {
-            SpanParams<kFew> p = {};
-            launch(p, sum_squares_kernel<kFew>, at);
-        } else {
-            SpanParams<kMany> p = {};
-            launch(p, sum_squares_kernel<kMany>, at);
-        }
-    }
-    if (st) return st;
+    int64_t parts;
+    if (fp4q_status st = launch_sums(tensors, n_tensors, partial, parts, s)) return st;
     const RootParams r = {partial, parts, norm};
     return launched(launch_dependent(root_kernel, dim3(1), 256, s, r));
 }
 
 extern "C" fp4q_status fp4q_clip_by_norm(const fp4q_span *tensors, const fp4q_span *outs, int32_t n_tensors, const float *norm, float max_norm, float eps, void *stream)
 {
-    if (fp4q_status s = check_spans(tensors, n_tensors)) return s;
-    if (outs) {
-        if (fp4q_status s = check_spans(outs, n_tensors)) return s;
-        for (int32_t i = 0; i < n_tensors; i++)
-            if (outs[i].rows != tensors[i].rows || outs[i].cols != tensors[i].cols) return FP4Q_ERR_SHAPE;
-    }
+    if (fp4q_status s = check_clip(tensors, outs, n_tensors, max_norm, eps)) return s;
     if (!norm) return FP4Q_ERR_NULL;
     if (!aligned(norm, 4)) return FP4Q_ERR_ALIGN;
-    if (!(max_norm >= 0.f) || !(eps >= 0.f)) return FP4Q_ERR_UNSUPPORTED;
-    fp4q_status st = FP4Q_OK;
-    auto launch = [&](auto &p, auto kernel, int32_t &at) {
-        p.norm = norm;
-        p.max_norm = max_norm;
-        p.eps = eps;
-        p.in_place = !outs;
-        const int64_t ctas = take_spans(tensors, outs ? outs : tensors, n_tensors, at, p);
-        if (ctas) st = launched(launch_dependent(kernel, dim3((unsigned)ctas), 256, static_cast<cudaStream_t>(stream), p));
-    };
-    for (int32_t at = 0; at < n_tensors && !st;) {
-        if (n_tensors - at <= kFew) {
-            SpanParams<kFew> p = {};
-            launch(p, scale_kernel<kFew>, at);
-        } else {
-            SpanParams<kMany> p = {};
-            launch(p, scale_kernel<kMany>, at);
-        }
+    return launch_scaling(tensors, outs, n_tensors, const_cast<float *>(norm), nullptr, 0, max_norm, eps, static_cast<cudaStream_t>(stream));   // which only reads it
+}
+
+extern "C" fp4q_status fp4q_clip_grad_norm(const fp4q_span *tensors, const fp4q_span *outs, int32_t n_tensors, float max_norm, float eps, float *norm, void *scratch, size_t scratch_bytes,
+                                           void *stream)
+{
+    if (fp4q_status s = check_clip(tensors, outs, n_tensors, max_norm, eps)) return s;
+    if (fp4q_status s = check_norm(norm, tensors, n_tensors, scratch, scratch_bytes)) return s;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    double *partial = static_cast<double *>(scratch);
+    int64_t parts;
+    if (fp4q_status st = launch_sums(tensors, n_tensors, partial, parts, s)) return st;
+    if (parts == 0) {   // no elements
+        const RootParams r = {partial, 0, norm};
+        return launched(launch_dependent(root_kernel, dim3(1), 256, s, r));
     }
-    return st;
+    return launch_scaling(tensors, outs, n_tensors, norm, partial, parts, max_norm, eps, s);
 }

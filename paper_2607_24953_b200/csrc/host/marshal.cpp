@@ -56,6 +56,7 @@ struct Entry {
     decltype(&fp4q_global_norm) global_norm;
     decltype(&fp4q_global_norm_scratch_bytes) global_norm_scratch_bytes;
     decltype(&fp4q_clip_by_norm) clip_by_norm;
+    decltype(&fp4q_clip_grad_norm) clip_grad_norm;
 } lib;
 
 PyObject *g_qtensor = nullptr, *g_fail = nullptr;   // binding.QTensor; binding._check
@@ -1121,14 +1122,10 @@ PyObject *clip_grad_norm(Args a, Py_ssize_t n)
     const at::Tensor &like = first_of(s);
     const c10::cuda::CUDAGuard device(like.device());
     const OnStream on(a[6], &like);
-    const std::vector<fp4q_span> as_read = s.spans;
     const ClipOuts outs(a[2], s);
-    const float max_norm = (float)as_double(a[1]), eps = (float)as_double(a[3]);
-    if (!(max_norm >= 0.f) || !(eps >= 0.f)) check(FP4Q_ERR_UNSUPPORTED, "fp4q_clip_by_norm");   // before anything is enqueued
     const at::Tensor norm = norm_scalar(a[4], on, like), scratch = norm_scratch(a[5], s, like);
-    float *to = static_cast<float *>(norm.data_ptr());
-    check(unlocked(lib.global_norm, as_read.data(), s.n(), to, scratch.data_ptr(), (size_t)scratch.nbytes(), on.handle), "fp4q_global_norm");
-    check(unlocked(lib.clip_by_norm, s.spans.data(), outs.data(), s.n(), (const float *)to, max_norm, eps, on.handle), "fp4q_clip_by_norm");
+    check(unlocked(lib.clip_grad_norm, s.spans.data(), outs.data(), s.n(), (float)as_double(a[1]), (float)as_double(a[3]), static_cast<float *>(norm.data_ptr()), scratch.data_ptr(),
+                   (size_t)scratch.nbytes(), on.handle), "fp4q_clip_grad_norm");
     return a[4] == Py_None ? wrap(norm) : Py_NewRef(a[4]);
 }
 
@@ -1320,6 +1317,7 @@ PyObject *init(Args a, Py_ssize_t n)
     set_entry(a[0], "fp4q_global_norm", lib.global_norm);
     set_entry(a[0], "fp4q_global_norm_scratch_bytes", lib.global_norm_scratch_bytes);
     set_entry(a[0], "fp4q_clip_by_norm", lib.clip_by_norm);
+    set_entry(a[0], "fp4q_clip_grad_norm", lib.clip_grad_norm);
     Py_XSETREF(g_qtensor, Py_NewRef(a[1]));
     Py_XSETREF(g_fail, Py_NewRef(a[2]));
     Py_XSETREF(g_fp8, Py_NewRef(a[3]));
