@@ -248,6 +248,7 @@ struct Cfg8 {
     // it has, so that neither side's accesses meet in a bank.
     static constexpr int kLine = MODE == SCALE_COLS ? 128 : BN, kLines = MODE == SCALE_COLS ? BN : 128, kPitch = kLine + 4;
     static constexpr int kSmem = 1024 + kOperands + 2 * kScales * 4 + 256;
+    static_assert(kStages <= 8, "barriers");
     static_assert(kPitch * kLines * 4 <= kOperands && kSmem <= 227 * 1024, "shared memory budget");
 };
 
@@ -454,7 +455,7 @@ struct CfgP {
     static constexpr int kSmem = 1024 + kOperands + 8 * kStaging + 2 * kScales * 4 + 512;
     static constexpr int kFewRegs = 88, kManyRegs = 208;
     static_assert(128 * kFewRegs + 256 * kManyRegs <= 384 * 168, "registers: what the epilogue takes is what the other warps give");
-    static_assert(kSmem <= 227 * 1024, "shared memory budget");
+    static_assert(kSmem <= 227 * 1024 && kStages <= 8, "shared memory budget, barriers");
 };
 struct MapsP {
     CUtensorMap a, b, out;

@@ -63,7 +63,7 @@ __device__ __forceinline__ void maxima(const Raw<T> (&x)[4], float (&rows)[4], u
 
 // GRID: rows begin on 16 bytes.
 template <typename T, bool SQUARE, bool GRID>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) fp8_quantize_kernel(const __grid_constant__ Fp8QuantParams p)
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) fp8_quantize_kernel(const __grid_constant__ Fp8QuantParams p)
 {
     wait_for_predecessor();
     admit_successor();
@@ -90,8 +90,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) fp8_quantize_kern
     uint32_t col_top[W];
     maxima(x, row_top, col_top);
     float all = fmaxf(fmaxf(row_top[0], row_top[1]), fmaxf(row_top[2], row_top[3]));
-    const bool careful = __syncthreads_or(is_infinite(all));   // maxima of finite elements only; infinities become NaN, which they are from here on
-    if (careful) {
+    if (__any_sync(0xFFFFFFFFu, is_infinite(all))) {   // maxima of finite elements only; infinities become NaN, which they are from here on
 #pragma unroll
         for (int i = 0; i < 4; i++)
 #pragma unroll
