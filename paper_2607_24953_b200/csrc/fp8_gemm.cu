@@ -729,6 +729,48 @@ bool allow_smem(K kernel, int bytes, std::atomic<bool> (&set)[kMaxDevices], int 
     return true;
 }
 
+// What launches a tile kernel in clusters of `split`; attr: two of them.
+template <int BN, int MODE>
+cudaLaunchConfig_t tile_config(int64_t ctas, int split, cudaLaunchAttribute *attr, cudaStream_t stream)
+{
+    using C = Cfg8<BN, MODE>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(C::kThreads);
+    cfg.dynamicSmemBytes = C::kSmem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)split;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = split > 1 ? 2 : 1;
+    return cfg;
+}
+
+// Clusters of `split` CTAs of the 128 x 128 tile kernel that run at once: they do not cross the GPU's partitions, so fewer CTAs of large ones do (16 clusters of eight ran one behind the other: 200 x 1024 x
+// 2816 13.8 us, in clusters of six 8.3).
+template <int MODE>
+int clusters_at_once(int split, int dev)
+{
+    static std::atomic<int> known[kMaxDevices][9];
+    int n = known[dev][split].load(std::memory_order_relaxed);
+    if (n == 0) {
+        cudaLaunchAttribute attr[2];
+        cudaLaunchConfig_t cfg = tile_config<128, MODE>(split, split, attr, nullptr);
+        n = sm_count(dev) / split;
+        int found = 0;
+        if (split > 1) {
+            if (cudaOccupancyMaxActiveClusters(&found, gemm8_tile_kernel<128, MODE>, &cfg) == cudaSuccess && found > 0) n = found;
+            else cudaGetLastError();
+        }
+        known[dev][split].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
 template <int BN, int MODE>
 fp4q_status launch_tiles(const Operand8 &a, const Operand8 &b, Gemm8Params p, int split, cudaStream_t stream)
 {
@@ -742,20 +784,8 @@ fp4q_status launch_tiles(const Operand8 &a, const Operand8 &b, Gemm8Params p, in
     p.split = split;
     const int64_t ctas = ceil_div(p.m, 128) * p.n_tiles * split;
     if (ctas > 0x7FFFFFFF) return FP4Q_ERR_UNSUPPORTED;
-    cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
-    cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(C::kThreads);
-    cfg.dynamicSmemBytes = C::kSmem;
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)split;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.numAttrs = split > 1 ? 2 : 1;
+    const cudaLaunchConfig_t cfg = tile_config<BN, MODE>(ctas, split, attr, stream);
     return launched(cudaLaunchKernelEx(&cfg, gemm8_tile_kernel<BN, MODE>, maps, p));
 }
 
@@ -804,7 +834,7 @@ fp4q_status launch_persistent(const Operand8 &a, const Operand8 &b, Gemm8Params 
 // a weight gradient of 256 x 256 over 16384 rows in clusters of eight 15, single CTAs 72.)
 struct Plan8 {
     int pairs = 0, split = 1;   // pairs: 2, single CTAs: 1, clusters of `split` CTAs with a tile: 0
-    Plan8(int64_t m, int64_t n, int64_t blocks, bool both, bool boxes)
+    Plan8(int64_t m, int64_t n, int64_t blocks, bool both, bool boxes, int dev)
     {
         const double each = both ? 0.60 : 0.40;
         double least = 1e30;
@@ -813,7 +843,8 @@ struct Plan8 {
         };
         const int64_t tiles = ceil_div(m, 128) * ceil_div(n, 128);
         for (int64_t s = 1; s <= 8 && (s == 1 || s * 2 <= blocks); s++)
-            consider((double)ceil_div(tiles * s, 148) * ((double)ceil_div(blocks, s) * each + 2.0) + (s > 1 ? 2.5 + 0.15 * (double)s : 0.0), 0, (int)s);
+            consider((double)ceil_div(tiles, both ? clusters_at_once<SCALE_BOTH>((int)s, dev) : clusters_at_once<SCALE_ROWS>((int)s, dev)) * ((double)ceil_div(blocks, s) * each + 2.0) +
+                         (s > 1 ? 2.5 + 0.15 * (double)s : 0.0), 0, (int)s);
         if (!boxes) return;
         consider((double)ceil_div(tiles, 148) * ((double)blocks * (both ? 0.51 : 0.365) + 1.3), 1, 1);
         consider((double)ceil_div(ceil_div(m, 256) * ceil_div(n, 256), 74) * ((double)blocks * (both ? 0.87 : 0.55) + 2.2), 2, 1);
@@ -835,7 +866,13 @@ fp4q_status product8(const Operand8 &a, const Operand8 &b, Gemm8Params p, bool b
         const int split = (int)std::max<int64_t>(1, std::min<int64_t>({8, tiles <= 64 ? ceil_div(160, tiles) : 296 / tiles, p.blocks / 2}));
         return a.rows <= 16 ? launch_tiles<16, SCALE_COLS>(b, a, p, split, stream) : a.rows <= 32 ? launch_tiles<32, SCALE_COLS>(b, a, p, split, stream) : launch_tiles<64, SCALE_COLS>(b, a, p, split, stream);
     }
-    const Plan8 plan(a.rows, b.rows, p.blocks, both, p.boxed > 0);
+    const int dev = current_device();
+    if (dev < 0) return FP4Q_ERR_CUDA;
+    // Before the kernels' clusters are asked for, their shared memory is allowed.
+    static std::atomic<bool> rows_set[kMaxDevices], both_set[kMaxDevices];
+    if (!(both ? allow_smem(gemm8_tile_kernel<128, SCALE_BOTH>, Cfg8<128, SCALE_BOTH>::kSmem, both_set, dev) : allow_smem(gemm8_tile_kernel<128, SCALE_ROWS>, Cfg8<128, SCALE_ROWS>::kSmem, rows_set, dev)))
+        return FP4Q_ERR_CUDA;
+    const Plan8 plan(a.rows, b.rows, p.blocks, both, p.boxed > 0, dev);
     if (plan.pairs == 2) return both ? launch_persistent<2, SCALE_BOTH>(a, b, p, stream) : launch_persistent<2, SCALE_ROWS>(a, b, p, stream);
     if (plan.pairs == 1) return both ? launch_persistent<1, SCALE_BOTH>(a, b, p, stream) : launch_persistent<1, SCALE_ROWS>(a, b, p, stream);
     return both ? launch_tiles<128, SCALE_BOTH>(a, b, p, plan.split, stream) : launch_tiles<128, SCALE_ROWS>(a, b, p, plan.split, stream);
