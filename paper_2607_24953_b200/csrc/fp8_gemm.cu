@@ -101,7 +101,8 @@ __device__ __forceinline__ void add_block(float (&sum)[COLS], uint32_t from, flo
         if (MODE != SCALE_ROWS) load_scales_16(cols + 4 * c, f);
         if (MODE == SCALE_BOTH)
 #pragma unroll
-            for (int e = 0; e < 16; e++) f[e] *= row;
+            for (int e = 0; e < 16; e += 2)   // in pairs, as they were loaded
+                asm("{\n .reg .b64 a, b;\n mov.b64 a, {%0, %1};\n mov.b64 b, {%2, %2};\n mul.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}" : "+f"(f[e]), "+f"(f[e + 1]) : "f"(row));
         landed(x);
         if (c + 16 == COLS) read();
 #pragma unroll
@@ -179,14 +180,16 @@ __device__ __forceinline__ void store_four(const Gemm8Params &p, int64_t row, in
     }
 }
 
-// A box of 32 rows x 128 bytes, COLS columns from col on, leaves an epilogue warp.  w: the lane's row of it, value(e): its elements.
+// A box of 32 rows x 128 bytes, COLS columns from col on, leaves an epilogue warp, which has two of them in turn at box_at.  w: the lane's row of it, value(e): its elements.
 template <int COLS, typename F>
-__device__ __forceinline__ void send_box(const Gemm8Params &p, const CUtensorMap *map, const Box16 &box, uint32_t box_at, const uint32_t *w, int row0, int col, int lane, F value)
+__device__ __forceinline__ void send_box(const Gemm8Params &p, const CUtensorMap *map, uint32_t &box_at, const uint32_t *w, int row0, int col, int lane, F value)
 {
     if (row0 >= p.m || col >= p.n) return;
     if (col < p.boxed) {
-        boxes_free(lane);
-        box.put(w);
+        // The store before the last has read its box.
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        __syncwarp();
+        Box16(box_at, lane).put(w);
         fence_async_shared();
         __syncwarp();
         if (lane == 0) {
@@ -194,6 +197,7 @@ __device__ __forceinline__ void send_box(const Gemm8Params &p, const CUtensorMap
             else tma_store_2d(map, col, row0, box_at);
             bulk_commit();
         }
+        box_at ^= 4096u;
     }
     if (col + COLS > p.boxed && p.boxed < p.n && row0 + lane < p.m) {
 #pragma unroll
@@ -445,13 +449,14 @@ struct CfgP {
     static constexpr int kBN = 128 * CTAS, kThreads = 384;
     static constexpr int kCols = 64 * CTAS;
     static constexpr int kABytes = 128 * kBlock8, kBBytes = 128 * kBlock8, kStageBytes = kABytes + kBBytes;   // of a CTA
-    static constexpr int kStages = 5;
+    // Two boxes an epilogue warp at the price of a stage: 8192 x 8192 x 1024 89.6 -> 84.8 us, 16384 x 11008 x 4096 688 -> 679.
+    static constexpr int kStages = 4, kBoxes = 2;
     static constexpr int kOperands = kStages * kStageBytes;
     static constexpr int kAccs = 4 / CTAS, kTmemCols = 512;
     static constexpr int kCalled = 128 + 32;                               // threads of a named barrier: half of the epilogue, and the caller
     static constexpr int kColScales = MODE == SCALE_BOTH ? kBN : 0;        // else one for each block of 128 columns
     static constexpr int kAhead = 4, kScales = kAhead * (128 + kBN);
-    static constexpr int kStaging = 4096;                                  // of an epilogue warp: a box of 32 rows x 128 bytes
+    static constexpr int kStaging = 4096 * kBoxes;                         // of an epilogue warp: boxes of 32 rows x 128 bytes, on multiples of their size
     static constexpr int kSmem = 1024 + kOperands + 8 * kStaging + 2 * kScales * 4 + 512;
     static constexpr int kFewRegs = 88, kManyRegs = 208;
     static_assert(128 * kFewRegs + 256 * kManyRegs <= 384 * 168, "registers: what the epilogue takes is what the other warps give");
@@ -620,8 +625,8 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kManyRegs));
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        const uint32_t box_at = smem_u32(smem_boxes) + (warp - 4) * C::kStaging, lead_empty = CTAS == 2 ? cluster_addr(bar_acc_empty, 0) : bar_acc_empty;
-        const Box16 box(box_at, lane);
+        const uint32_t lead_empty = CTAS == 2 ? cluster_addr(bar_acc_empty, 0) : bar_acc_empty;
+        uint32_t box_at = smem_u32(smem_boxes) + (warp - 4) * C::kStaging;
         Ring16<C::kAccs> acc;
         Ring16<2> set;
         bool ok = true;
@@ -667,7 +672,7 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
                     float v[32];
 #pragma unroll
                     for (int e = 0; e < 32; e++) v[e] = sum[c + e];
-                    send_box<32>(p, &maps.out, box, box_at, reinterpret_cast<const uint32_t *>(v), row0, col0 + c, lane, [&](int e) { return v[e]; });
+                    send_box<32>(p, &maps.out, box_at, reinterpret_cast<const uint32_t *>(v), row0, col0 + c, lane, [&](int e) { return v[e]; });
                 }
             } else {
 #pragma unroll
@@ -675,7 +680,7 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
                     uint32_t w[32];
 #pragma unroll
                     for (int e = 0; e < 32; e++) w[e] = pack_bf16(sum[c + 2 * e], sum[c + 2 * e + 1]);
-                    send_box<64>(p, &maps.out, box, box_at, w, row0, col0 + c, lane, [&](int e) { return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16); });
+                    send_box<64>(p, &maps.out, box_at, w, row0, col0 + c, lane, [&](int e) { return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16); });
                 }
             }
         }
