@@ -445,7 +445,8 @@ fp4q_status fp4q_newton_schulz(const void *g, fp4q_out g_type, int64_t count, in
  *   q   [rows, ld_q]: codes; scale [rows, ld_s >= ceil(cols/128)], with square blocks [ceil(rows/128), ld_s]
  *   q_t [cols, ld_t]: codes of the transpose; 1D blocks: along the rows of the source, with scales of their own, scale_t [cols, ld_st >= ceil(rows/128)];
  *                     square blocks: the same codes as in q, and the same scales (scale is written and read either way, scale_t is not used)
- * q or q_t may be NULL where it is not wanted.  Payloads are 16-byte aligned in pitches of whole 16 bytes, scales are aligned to their elements.
+ * q or q_t may be NULL where it is not wanted.  Payloads are 16-byte aligned in pitches of whole 16 bytes, scales are aligned to their elements (fastest where four of a row lie on 16 bytes).
+ * The quantizer and the norm below read rows that start anywhere in aligned pieces of 16 bytes, and so may read, but not use, up to 15 bytes beside a row.
  */
 typedef struct {
     int64_t rows, cols;

@@ -156,6 +156,7 @@ class _RMSNormFn(torch.autograd.Function):
             out.y = torch.empty(x.shape, dtype=torch.float32, device=x.device)
         n = binding.fp4q_rms_norm(xr, _weight(weight), rr, eps=eps, out=out)
         ctx.save_for_backward(xr if rr is None else n.h, n.rstd, weight)
+        ctx.set_materialize_grads(False)
         ctx.types = x.dtype, None if residual is None else residual.dtype
         y = _cast(n.y, x.dtype).contiguous()
         return (y, None) if residual is None else (y, _cast(n.h, residual.dtype).contiguous())
@@ -164,6 +165,7 @@ class _RMSNormFn(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy, dh):
         h, rstd, weight = ctx.saved_tensors
+        dy = torch.zeros_like(h) if dy is None else dy
         dx, dw = _norm_backward(dy, dh, h, rstd, weight, ctx.needs_input_grad[1])
         return _cast(dx, ctx.types[0]), dw, _cast(dx, ctx.types[1]) if ctx.needs_input_grad[2] else None, None
 
@@ -218,7 +220,8 @@ class _FP8LinearFn(torch.autograd.Function):
         qw = binding.fp4q_fp8_quantize(_rows(weight), square=True, want_t=keep_w)
         y = binding.fp4q_fp8_gemm_fwd(qx, qw, ws=ws)
         ctx.save_for_backward(qx.q_t, qx.scale_t, qw.q_t, qw.scale, h, rstd, norm_weight)
-        ctx.sizes, ctx.ws = (T, K, weight.shape[0]), ws
+        ctx.set_materialize_grads(False)
+        ctx.sizes, ctx.ws, ctx.device = (T, K, weight.shape[0]), ws, x.device
         ctx.types = x.dtype, weight.dtype, None if residual is None else residual.dtype
         return y.contiguous(), None if residual is None else _cast(h, residual.dtype).contiguous()
 
@@ -228,6 +231,7 @@ class _FP8LinearFn(torch.autograd.Function):
         xt, xts, wt, ws, h, rstd, norm_weight = ctx.saved_tensors
         (T, K, N), need = ctx.sizes, ctx.needs_input_grad
         inputs = need[0] or need[2] or need[3]
+        dy = torch.zeros((T, N), dtype=torch.bfloat16, device=ctx.device) if dy is None else dy
         qd = binding.fp4q_fp8_quantize(_rows(dy), want=inputs, want_t=need[1]) if inputs or need[1] else None
         dx = dw = dn = None
         if need[1]:

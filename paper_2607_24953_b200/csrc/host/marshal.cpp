@@ -1047,7 +1047,7 @@ struct ClipOuts {
             same_device(u, t, "outs");
             if (u.sizes() != t.sizes()) value_error("an entry of outs must have its tensor's shape");
             fp4q_span &a = in.spans[i], &b = outs->spans[i];
-            if (a.rows == b.rows && t.strides() == u.strides()) continue;
+            if (a.rows == b.rows && (t.strides() == u.strides() || t.numel() <= 1 || (t.is_contiguous() && u.is_contiguous()))) continue;
             // One is without gaps and the other is not, or their orders differ: both row by row.
             const at::Tensor &x = as_stack(t, "a tensor whose strides are not those of its entry of outs"), &y = as_stack(u, "an entry of outs whose strides are not its tensor's");
             a.cols = b.cols = x.size(-1);

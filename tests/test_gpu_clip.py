@@ -72,6 +72,12 @@ def test_strides_and_alignments(dtype):
     check(views[:2], 0.05, shifted)
 
 
+def test_single_elements_of_any_strides():
+    flat = randn(1, 64)
+    one, row = flat[::8][:1], flat.view(8, 8)[:1]
+    check([one, row], 0.1, [torch.empty(1, device="cuda"), torch.empty(1, 8, device="cuda")])
+
+
 def test_numbers_whose_squares_leave_fp32():
     for scale in (1e-30, 1e-22, 1e25, 3e37):
         ts = [randn(1, 5000) * scale, randn(2, 3) * scale]

@@ -202,7 +202,7 @@ def test_results_do_not_depend_on_the_run():
 
 
 def test_a_wait_that_runs_out_is_reported():
-    for t in (4, 200, 2048):
+    for t in (4, 200, 1024, 2048):                             # a kernel each
         X, W, _ = operands(t, 2048, 2048)
         ws = b.alloc_workspace("cuda")
         want = b.fp4q_fp8_gemm_fwd(X, W, ws=ws)
@@ -213,3 +213,40 @@ def test_a_wait_that_runs_out_is_reported():
         b.fp4q_debug_withhold_load(ws, 0)
         b.fp4q_workspace_set_wait_limit(ws, 0)
         assert torch.equal(b.fp4q_fp8_gemm_fwd(X, W, ws=ws), want) and b.fp4q_workspace_status(ws) == 0
+
+
+def test_sizes_at_which_the_plan_changes():
+    # Clusters of every size, single CTAs' and pairs' tiles, with edges.
+    ws = b.alloc_workspace("cuda")
+    for t, n, k in ((70, 100, 2000), (129, 257, 1500), (200, 1003, 2731), (260, 900, 640), (500, 2000, 300), (1025, 1500, 260), (2100, 3000, 130)):
+        check_all(t, n, k, b.OUT_F32, ws)
+
+
+def test_rows_behind_32_bits():
+    # More than 2^31 elements between the first row of a matrix and its last: codes in a buffer of long rows, of which the product reads and the quantizer writes a few columns.
+    x = randn(1, 3, 256).to(torch.bfloat16)
+    far = torch.empty(3 << 30, dtype=torch.uint8, device="cuda")
+    q = far.as_strided((3, 256), ((1 << 30) + (1 << 28), 1))
+    t = b.fp4q_fp8_quantize(x, want_t=False)
+    out = b.Fp8Tensor(3, 256, q, torch.empty(3, 2, device="cuda"))
+    b.fp4q_fp8_quantize(x, out=out)
+    assert torch.equal(out.q, t.q) and torch.equal(out.scale, t.scale)
+    W = b.fp4q_fp8_quantize(randn(2, 300, 256), square=True)
+    assert torch.equal(b.fp4q_fp8_gemm_fwd(out, W), b.fp4q_fp8_gemm_fwd(t, W))
+
+
+def test_refusals():
+    x = randn(1, 40, 100).to(torch.bfloat16)
+    X, W = b.fp4q_fp8_quantize(x), b.fp4q_fp8_quantize(randn(2, 60, 100), square=True)
+    for bad in (lambda: b.fp4q_fp8_quantize(x.half()), lambda: b.fp4q_fp8_quantize(x.T), lambda: b.fp4q_fp8_quantize(x[0]), lambda: b.fp4q_fp8_quantize(x, want=False, want_t=False),
+                lambda: b.fp4q_fp8_quantize(x, out=X, square=True), lambda: b.fp4q_fp8_quantize(x, out=b.Fp8Tensor(40, 100, X.q[:, :96], X.scale)),
+                lambda: b.fp4q_fp8_quantize(x[:1], out=b.Fp8Tensor(1, 100, torch.empty(1, 100, dtype=torch.uint8, device="cuda"), X.scale[:1])),   # no room behind its last element
+                lambda: b.fp4q_fp8_quantize(x, out=b.Fp8Tensor(40, 100, X.q, X.scale.double())), lambda: b.fp4q_fp8_gemm_fwd(X, W, dt=7), lambda: b.fp4q_fp8_gemm_fwd(b.Fp8Tensor(40, 100, None, None), W),
+                lambda: b.fp4q_fp8_gemm_fwd(X, W, out=torch.empty(40, 60, device="cuda")), lambda: b.fp4q_fp8_gemm_fwd(b.Fp8Tensor(41, 100, X.q, X.scale), W),
+                lambda: b.fp4q_fp8_gemm_fwd(b.Fp8Tensor(40, 100, X.q, X.scale.view(torch.uint8)), W)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: b.fp4q_fp8_gemm_fwd(W, X), lambda: b.fp4q_fp8_gemm_fwd(X, X), lambda: b.fp4q_fp8_gemm_dgrad(X, b.Fp8Tensor(100, 60, W.q_t, W.scale.T.contiguous(), None, None, True)),
+                lambda: b.fp4q_fp8_gemm_fwd(X, W, ws=torch.zeros(8, dtype=torch.uint8, device="cuda")), lambda: b.fp4q_fp8_quantize(x, out=b.Fp8Tensor(41, 100, torch.empty(41, 112, dtype=torch.uint8, device="cuda"), torch.empty(41, 1, device="cuda")))):
+        with pytest.raises(b.Fp4qError):
+            bad()

@@ -89,6 +89,18 @@ def test_only_the_gradients_that_are_wanted():
             assert (t.grad is not None) == bool(need >> i & 1)
 
 
+def test_outputs_that_nobody_uses_get_no_gradient():
+    x, r, (g, w) = randn(1, 30, 64).to(BF16).requires_grad_(), randn(2, 30, 64).to(BF16).requires_grad_(), params(48, 64)
+    for f in (lambda: autograd.rms_norm(x, g, r), lambda: autograd.rms_norm_fp8_linear(x, g, w, r)):
+        both = []
+        for use in (0, 1):
+            x.grad = r.grad = None
+            f()[use].sum().backward()
+            both.append((x.grad, r.grad))
+        assert torch.equal(both[0][0], both[0][1])
+        assert (both[1][0] == 1).all() and (both[1][1] == 1).all()      # the stream's own gradient alone
+
+
 class Block:
     """Two projections behind norms on one residual stream, a step's gradients clipped and turned into updates."""
 

@@ -207,3 +207,30 @@ def test_gradients_against_differences():
         slope = (loss(h.double() + step * v, w.double() + step * u) - loss(h.double() - step * v, w.double() - step * u)) / (2 * step)
         got = (dx.double() * v).sum() + (dw.double() * u).sum()
         assert abs(float(slope - got)) <= 1e-4 * float((dx.double() * v).abs().sum() + (dw.double() * u).abs().sum())
+
+
+def test_refusals():
+    x, w = randn(1, 8, 64).to(BF16), randn(2, 64)
+    rstd = torch.ones(8, device="cuda")
+    for bad in (lambda: b.fp4q_rms_norm(x.half()), lambda: b.fp4q_rms_norm(x.T), lambda: b.fp4q_rms_norm(x[0]), lambda: b.fp4q_rms_norm(x, w[:63]), lambda: b.fp4q_rms_norm(x, w.double()),
+                lambda: b.fp4q_rms_norm(x, w, x[:4]), lambda: b.fp4q_rms_norm(x, w, x.cpu()), lambda: b.fp4q_rms_norm(x, q=5), lambda: b.fp4q_rms_norm(x, w, x, out=b.NormOut(y=x.clone())),
+                lambda: b.fp4q_rms_norm(x, w, x, out=b.NormOut(h=x.float())), lambda: b.fp4q_rms_norm(x, out=b.NormOut(q=torch.empty(8, 64, dtype=torch.uint8, device="cuda"))),
+                lambda: b.fp4q_rms_norm(x, out=b.NormOut(rstd=rstd[:7])), lambda: b.fp4q_rms_norm(x, out=b.NormOut(y=x[:, :63])),
+                lambda: b.fp4q_rms_norm_bwd(x[:4], x, rstd), lambda: b.fp4q_rms_norm_bwd(x, x, rstd[:3]), lambda: b.fp4q_rms_norm_bwd(x, x, rstd, w, dh=x.float()),
+                lambda: b.fp4q_rms_norm_bwd(x, x, rstd, w, out=x.float()), lambda: b.fp4q_rms_norm_bwd(x, x, rstd, w, dweight=w[:5])):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: b.fp4q_rms_norm(x, eps=-1.0), lambda: b.fp4q_rms_norm(torch.empty(1, 65537, device="cuda")), lambda: b.fp4q_rms_norm_bwd(x, x, rstd, w, scratch=torch.empty(16, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(b.Fp4qError):
+            bad()
+
+
+def test_rows_behind_32_bits():
+    far = torch.empty(3 << 30, dtype=BF16, device="cuda")
+    x = far.as_strided((3, 400), ((1 << 30) + (1 << 28) + 1, 1))
+    x.copy_(randn(1, 3, 400))
+    near, w = x.clone(), randn(2, 400)
+    a, c = b.fp4q_rms_norm(x, w, q=b.Q_FP8, rstd=True), b.fp4q_rms_norm(near, w, q=b.Q_FP8, rstd=True)
+    assert torch.equal(a.y, c.y) and torch.equal(a.q[:, :400], c.q[:, :400])
+    dx = b.fp4q_rms_norm_bwd(near, x, a.rstd, w, out=x)[0]
+    assert torch.equal(dx, b.fp4q_rms_norm_bwd(near, near, a.rstd, w)[0])
