@@ -46,6 +46,19 @@ struct Maps8 {
     CUtensorMap a, b;
 };
 
+// By the lanes for which `issue` holds, without a branch (see tcgen05_mma_f16).  PAIR: the copy is counted on a barrier of the pair's leader.
+template <bool PAIR>
+__device__ __forceinline__ void tma_load_if(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar, bool issue)
+{
+    if (PAIR)
+        asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %5, 0;\n"
+                     "@q cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n}"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "r"((uint32_t)issue) : "memory");
+    else
+        asm volatile("{\n .reg .pred q;\n setp.ne.b32 q, %5, 0;\n"
+                     "@q cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n}"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "r"((uint32_t)issue) : "memory");
+}
 template <int CTAS>
 __device__ __forceinline__ void tcgen05_mma_f8(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, bool accumulate, bool issue)
 {
@@ -307,9 +320,8 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
             if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) break;
             const uint32_t bar = bar_full + 8 * ring.slot;
             expect_tx_if(bar, C::kStageBytes, issuer);
-            if (issuer && (withhold == 0u || ++loads != withhold)) tma_load_2d(a0 + ring.slot * C::kABytes, &maps.a, b * kBlock8, m0, bar);
-            if (issuer) tma_load_2d(bb0 + ring.slot * C::kBBytes, &maps.b, b * kBlock8, n0, bar);
-            __syncwarp();
+            tma_load_if<false>(a0 + ring.slot * C::kABytes, &maps.a, b * kBlock8, m0, bar, issuer && (withhold == 0u || ++loads != withhold));
+            tma_load_if<false>(bb0 + ring.slot * C::kBBytes, &maps.b, b * kBlock8, n0, bar, issuer);
         }
     } else if (warp == 1) {
         const bool issuer = elect_one();
@@ -535,17 +547,8 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
                     issued++;
                     const uint32_t bar = lead + 8 * ring.slot, at = ring.slot * C::kABytes;
                     expect_tx_if(bar_full + 8 * ring.slot, C::kStageBytes * CTAS, issuer && rank == 0);
-                    if (issuer) {
-                        const bool with_a = withhold == 0u || ++loads != withhold;
-                        if (CTAS == 2) {
-                            if (with_a) tma_load_2d_pair(a0 + at, &maps.a, b * kBlock8, m0, bar);
-                            tma_load_2d_pair(b0 + at, &maps.b, b * kBlock8, n0, bar);
-                        } else {
-                            if (with_a) tma_load_2d(a0 + at, &maps.a, b * kBlock8, m0, bar);
-                            tma_load_2d(b0 + at, &maps.b, b * kBlock8, n0, bar);
-                        }
-                    }
-                    __syncwarp();
+                    tma_load_if<CTAS == 2>(a0 + at, &maps.a, b * kBlock8, m0, bar, issuer && (withhold == 0u || ++loads != withhold));
+                    tma_load_if<CTAS == 2>(b0 + at, &maps.b, b * kBlock8, n0, bar, issuer);
                 }
             }
             // The MMAs' last reports reach this CTA's barriers while it is still there.
