@@ -1013,12 +1013,20 @@ struct Spans {
     {
         Ref t(PySequence_Tuple(list));
         const Py_ssize_t n = PyTuple_GET_SIZE(t.p);
+        kept.reserve((size_t)n);
+        spans.reserve((size_t)n);
         for (Py_ssize_t i = 0; i < n; i++) {
+            kept.push_back(as_tensor(PyTuple_GET_ITEM(t.p, i)));
+            const at::Tensor &k = kept.back();
+            // An entry is named where it is refused: most are not.
+            if (k.is_cuda() && bf16_or_f32(k) && k.device() == kept.front().device() && k.is_non_overlapping_and_dense()) {
+                spans.push_back(fp4q_span{k.data_ptr(), 1, k.numel(), k.numel(), type_of(k)});
+                continue;
+            }
             char text[48];
             snprintf(text, sizeof text, "%s[%zd]", name, i);
-            kept.push_back(as_tensor(PyTuple_GET_ITEM(t.p, i)));
-            spans.push_back(span_of(kept.back(), text));
-            if (i > 0) same_device(kept.back(), kept.front(), text);
+            spans.push_back(span_of(k, text));
+            same_device(k, kept.front(), text);
         }
     }
     int32_t n() const { return (int32_t)spans.size(); }
