@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 using namespace fp4q;
 
@@ -296,8 +297,8 @@ struct GradParams {
 
 // Rows blockIdx.x, blockIdx.x + gridDim.x, ... of teams, 8 columns a lane and chunk.  Up to 8192 columns the weight and the sums over rows stay in registers, and the next row is on its way
 // while this one is worked on.  The operations of dx are spelled out, so that it is the same whatever else is computed.
-template <typename TY, typename TH, int CHUNKS, bool GRID_IN, bool GRID_OUT>
-__global__ void __launch_bounds__(512, CHUNKS == 1 && sizeof(TH) == 2 ? 2 : 1) rms_norm_bwd_kernel(const __grid_constant__ GradParams p)
+template <typename TY, typename TH, int CHUNKS, bool GRID_IN, bool GRID_OUT, int MOST = 512>
+__global__ void __launch_bounds__(MOST, CHUNKS == 1 && (sizeof(TH) == 2 || MOST < 512) ? 2 : 1) rms_norm_bwd_kernel(const __grid_constant__ GradParams p)
 {
     wait_for_predecessor();
     admit_successor();
@@ -520,14 +521,24 @@ fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scra
         parts = std::max<int64_t>(1, std::min({(int64_t)kGradCtas, ceil_div(p.rows, d.threads / d.team), (int64_t)148 * resident(kernel, d.threads, known)}));
         return launched(launch_dependent(kernel, dim3((unsigned)parts), d.threads, s, p));
     };
-    static std::atomic<int> known[7];
+    static std::atomic<int> known[10];
     if (fused || p.rows > 0) {
-        const fp4q_status st = d.chunks == 1   ? in && out ? launch(rms_norm_bwd_kernel<TY, TH, 1, true, true>, known[0])
-                                                 : in      ? launch(rms_norm_bwd_kernel<TY, TH, 1, true, false>, known[1])
-                                                           : launch(rms_norm_bwd_kernel<TY, TH, 1, false, false>, known[2])
-                               : d.chunks == 2 ? in && out ? launch(rms_norm_bwd_kernel<TY, TH, 2, true, true>, known[3]) : launch(rms_norm_bwd_kernel<TY, TH, 2, false, false>, known[4])
-                               : d.chunks == 4 ? launch(rms_norm_bwd_kernel<TY, TH, 4, false, false>, known[5])
-                                               : launch(rms_norm_bwd_kernel<TY, TH, 16, false, false>, known[6]);
+        fp4q_status st;
+        auto one = [&](auto most, int at) {   // one chunk a thread
+            constexpr int kMost = decltype(most)::value;
+            return in && out ? launch(rms_norm_bwd_kernel<TY, TH, 1, true, true, kMost>, known[at])
+                   : in      ? launch(rms_norm_bwd_kernel<TY, TH, 1, true, false, kMost>, known[at + 1])
+                             : launch(rms_norm_bwd_kernel<TY, TH, 1, false, false, kMost>, known[at + 2]);
+        };
+        if (d.chunks == 1) {
+            if constexpr (sizeof(TH) == 4)   // two CTAs an SM on an FP32 stream too, where they have no more threads (1999 x 2731 23.6 -> 20.6 us)
+                st = d.threads <= 384 ? one(std::integral_constant<int, 384>(), 5) : one(std::integral_constant<int, 512>(), 0);
+            else st = one(std::integral_constant<int, 512>(), 0);
+        } else {
+            st = d.chunks == 2 ? in && out ? launch(rms_norm_bwd_kernel<TY, TH, 2, true, true>, known[3]) : launch(rms_norm_bwd_kernel<TY, TH, 2, false, false>, known[4])
+                 : d.chunks == 4 ? launch(rms_norm_bwd_kernel<TY, TH, 4, false, false>, known[8])
+                                 : launch(rms_norm_bwd_kernel<TY, TH, 16, false, false>, known[9]);
+        }
         if (st) return st;
     }
     if (!dweight) return FP4Q_OK;
