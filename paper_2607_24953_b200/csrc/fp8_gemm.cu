@@ -5,7 +5,7 @@
 // own in tensor memory; the epilogue's warps take it from there, times its scales, into sums in registers, while the next block's MMAs run into
 // another accumulator.  The accumulator that the tensor cores cut off towards zero is thus never longer than 128 elements; the sums are rounded to nearest.
 // Bound by that path of the accumulators, 1100 cycles a block of a pair's tile where its MMAs take 512: 16384 x 11008 x 4096 797 us (1.85 PFLOP/s; 690 in a short run), the weight gradient of 4096 x 4096 over
-// 16384 rows 466.  One token: bound by the weight's bytes, 4096 x 11008 12.3 us.
+// 16384 rows 451.  One token: bound by the weight's bytes, 4096 x 11008 12.3 us.
 #include "gemm16.cuh"
 
 #include <algorithm>
@@ -37,6 +37,7 @@ struct Scales8 {
 struct Gemm8Params {
     int32_t m, n, blocks;            // rows of A and B, blocks of the contraction
     int32_t m_tiles, n_tiles, split; // split: CTAs of a cluster, which share a tile's contraction
+    int32_t whole, pieces;           // persistent: tiles that are computed as one, and pieces in all; the tiles behind these are two pieces each, of half of the columns
     int32_t boxed;                   // columns that leave in boxes, whole 16 bytes; the rest of a row leaves by itself
     Scales8 sa, sb;
     void *c;                         // row-major, [m, n] or, with SCALE_COLS, its transpose: [n, m]
@@ -477,8 +478,74 @@ struct CfgP {
     static_assert(kSmem <= 227 * 1024 && kStages <= 8, "shared memory budget, barriers");
 };
 struct MapsP {
-    CUtensorMap a, b, out;
+    CUtensorMap a, b, b_half, out;
 };
+
+// What an epilogue warp of the persistent kernel works with.
+template <int ACCS>
+struct Epilogue8 {
+    uint32_t tmem, scales, lead_empty, acc_empty, sc_empty, box_at;
+    volatile uint32_t *abort_flag;
+    int quarter, half, lane, rank;
+    Ring16<ACCS> acc;
+    Ring16<2> set;
+};
+
+// A warp's part of a tile, 32 rows x COLS columns.  false: a wait of another warp has run out.
+template <int CTAS, int MODE, int COLS>
+__device__ __forceinline__ bool tile_out(const Gemm8Params &p, const MapsP &maps, Epilogue8<CfgP<CTAS, MODE>::kAccs> &w, int m0, int n0)
+{
+    using C = CfgP<CTAS, MODE>;
+    float sum[COLS];
+#pragma unroll
+    for (int i = 0; i < COLS; i++) sum[i] = 0.f;
+    for (int b = 0; b < p.blocks; b++, w.acc.next()) {
+        const int i = b % C::kAhead;
+        const uint32_t from = w.scales + w.set.slot * C::kScales * 4;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + w.half * C::kAccs + w.acc.slot), "n"(C::kCalled) : "memory");
+        if (!__all_sync(0xFFFFFFFFu, *w.abort_flag == 0u)) {   // whoever of this half did not see it yet waits at the next barrier, and sees it behind that
+            w.acc.next();
+            asm volatile("bar.arrive %0, %1;" ::"r"(1 + w.half * C::kAccs + w.acc.slot), "n"(C::kCalled) : "memory");
+            return false;
+        }
+        tcgen05_fence_after();
+        float row = load_scale(from + 4 * (i * 128 + 32 * w.quarter + w.lane));
+        if (MODE == SCALE_ROWS) row *= load_scale(from + 4 * (C::kAhead * 128 + i * CTAS + w.half * COLS / 128));
+        add_block<MODE, COLS>(sum, w.tmem + w.acc.slot * C::kBN + w.half * COLS + ((uint32_t)(32 * w.quarter) << 16), row, from + 4 * (C::kAhead * 128 + i * C::kColScales + w.half * COLS), [&] {
+            tcgen05_fence_before();
+            __syncwarp();
+            if (w.lane == 0) {
+                if (w.rank != 0) mbar_arrive_cluster(w.lead_empty + 8 * w.acc.slot);
+                else mbar_arrive(w.acc_empty + 8 * w.acc.slot);
+            }
+        });
+        __syncwarp();
+        if (i == C::kAhead - 1 || b == p.blocks - 1) {
+            if (w.lane == 0) mbar_arrive(w.sc_empty + 8 * w.set.slot);
+            w.set.next();
+        }
+    }
+    // Boxes of 32 rows x 128 bytes; a row's last bytes that are no whole 16 by themselves.
+    const int row0 = m0 + 32 * w.quarter, col0 = n0 + w.half * COLS, lane = w.lane;
+    if (p.f32) {
+#pragma unroll
+        for (int c = 0; c < COLS; c += 32) {
+            float v[32];
+#pragma unroll
+            for (int e = 0; e < 32; e++) v[e] = sum[c + e];
+            send_box<32>(p, &maps.out, w.box_at, reinterpret_cast<const uint32_t *>(v), row0, col0 + c, lane, [&](int e) { return v[e]; });
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < COLS; c += 64) {
+            uint32_t v[32];
+#pragma unroll
+            for (int e = 0; e < 32; e++) v[e] = pack_bf16(sum[c + 2 * e], sum[c + 2 * e + 1]);
+            send_box<64>(p, &maps.out, w.box_at, v, row0, col0 + c, lane, [&](int e) { return __uint_as_float((e & 1) ? v[e >> 1] & 0xFFFF0000u : v[e >> 1] << 16); });
+        }
+    }
+    return true;
+}
 
 template <int CTAS, int MODE>
 __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ MapsP maps, const Gemm8Params p)
@@ -524,11 +591,12 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
 
     const uint32_t limit_word = load_global(p.status + 2), withhold = blockIdx.x == 0 ? load_global(p.status + 3) : 0u;
     const uint64_t limit = limit_word != 0u ? limit_word : kWaitLimit;
-    const int tiles = p.m_tiles * p.n_tiles, step = gridDim.x / CTAS, blocks = p.blocks;
+    const int step = gridDim.x / CTAS, blocks = p.blocks;
     // Bands of kRaster16 rows of tiles, whose A rows stay in L2 while the columns go by.
-    auto place = [&](int tile, int &m0, int &n0) {
+    auto place = [&](int piece, int &m0, int &n0) {
+        const int second = CTAS == 2 ? max(piece - p.whole, 0) : 0, tile = piece - second + second / 2;
         const int per_band = kRaster16 * p.n_tiles, band = tile / per_band, top = band * kRaster16, h = min(kRaster16, p.m_tiles - top), rem = tile - band * per_band;
-        n0 = rem / h * C::kBN;
+        n0 = rem / h * C::kBN + second % 2 * (C::kBN / 2);
         m0 = (top + rem % h) * (128 * CTAS) + rank * 128;
     };
 
@@ -540,17 +608,20 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
             Ring16<C::kStages> ring;
             uint32_t loads = 0, issued = 0;
             bool ok = true;
-            for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step) {
+            for (int tile = blockIdx.x / CTAS; ok && tile < p.pieces; tile += step) {
                 int m0, n0;
                 place(tile, m0, n0);
-                if (CTAS == 2) n0 += rank * 128;
+                const bool part = CTAS == 2 && tile >= p.whole;
+                const CUtensorMap *const map_b = part ? &maps.b_half : &maps.b;
+                const uint32_t bytes = part ? (C::kABytes + C::kBBytes / 2) * CTAS : C::kStageBytes * CTAS;
+                if (CTAS == 2) n0 += rank * (part ? 64 : 128);
                 for (int b = 0; b < blocks; b++, ring.next()) {
                     if (!warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x100u + ring.slot)) { ok = false; break; }
                     issued++;
                     const uint32_t bar = lead + 8 * ring.slot, at = ring.slot * C::kABytes;
-                    expect_tx_if(bar_full + 8 * ring.slot, C::kStageBytes * CTAS, issuer && rank == 0);
+                    expect_tx_if(bar_full + 8 * ring.slot, bytes, issuer && rank == 0);
                     tma_load_if<CTAS == 2>(a0 + at, &maps.a, b * kBlock8, m0, bar, issuer && (withhold == 0u || ++loads != withhold));
-                    tma_load_if<CTAS == 2>(b0 + at, &maps.b, b * kBlock8, n0, bar, issuer);
+                    tma_load_if<CTAS == 2>(b0 + at, map_b, b * kBlock8, n0, bar, issuer);
                 }
             }
             // The MMAs' last reports reach this CTA's barriers while it is still there.
@@ -558,12 +629,13 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
                 if (issued >= C::kStages - i) ok = warp_wait(bar_empty + 8 * ring.slot, ring.phase ^ 1u, abort_flag, p.status, limit, 0x700u + ring.slot);
         } else if (warp == 1 && rank == 0) {
             const bool issuer = elect_one();
-            const uint32_t idesc = instr_desc8<CTAS>(C::kBN), a_desc = (uint32_t)smem_desc_sw128(smem_u32(smem_a)), b_desc = (uint32_t)smem_desc_sw128(smem_u32(smem_b));
+            const uint32_t a_desc = (uint32_t)smem_desc_sw128(smem_u32(smem_a)), b_desc = (uint32_t)smem_desc_sw128(smem_u32(smem_b));
             constexpr uint32_t desc_hi = (1024 >> 4) | (1u << 14) | (2u << 29);
             Ring16<C::kStages> ring;
             Ring16<C::kAccs> acc;
             bool ok = true;
-            for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step)
+            for (int tile = blockIdx.x / CTAS; ok && tile < p.pieces; tile += step) {
+                const uint32_t idesc = instr_desc8<CTAS>(CTAS == 1 || tile < p.whole ? C::kBN : C::kBN / 2);
                 for (int b = 0; b < blocks; b++, ring.next(), acc.next()) {
                     ok = seen_or_wait(bar_full + 8 * ring.slot, ring.phase, abort_flag, p.status, limit, 0x300u + ring.slot) &&
                          seen_or_wait(bar_acc_empty + 8 * acc.slot, acc.phase ^ 1u, abort_flag, p.status, limit, 0x200u);
@@ -576,12 +648,13 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
                     tcgen05_commit_if<CTAS>(bar_acc_full + 8 * acc.slot, issuer);
                     tcgen05_commit_if<CTAS>(bar_empty + 8 * ring.slot, issuer);
                 }
+            }
         } else if (warp == 2) {
             // The scales of four blocks at a time, loaded while the set before waits for its place.
             constexpr int kR = 4, kC = C::kColScales / 32;
             Ring16<2> set;
             bool ok = true;
-            for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step) {
+            for (int tile = blockIdx.x / CTAS; ok && tile < p.pieces; tile += step) {
                 int m0, n0;
                 place(tile, m0, n0);
                 for (int b = 0; b < blocks; b += C::kAhead, set.next()) {
@@ -615,7 +688,7 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
             Ring16<C::kAccs> acc;
             Ring16<2> set;
             bool ok = true;
-            for (int tile = blockIdx.x / CTAS; ok && tile < tiles; tile += step)
+            for (int tile = blockIdx.x / CTAS; ok && tile < p.pieces; tile += step)
                 for (int b = 0; ok && b < blocks; b++, acc.next()) {
                     if (b % C::kAhead == 0) {
                         ok = warp_wait(bar_sc_full + 8 * set.slot, set.phase, abort_flag, p.status, limit, 0x500u);
@@ -630,64 +703,15 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kManyRegs));
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        const uint32_t lead_empty = CTAS == 2 ? cluster_addr(bar_acc_empty, 0) : bar_acc_empty;
-        uint32_t box_at = smem_u32(smem_boxes) + (warp - 4) * C::kStaging;
-        Ring16<C::kAccs> acc;
-        Ring16<2> set;
-        bool ok = true;
-        for (int tile = blockIdx.x / CTAS; tile < tiles; tile += step) {
+        Epilogue8<C::kAccs> e = {tmem, smem_u32(scales), CTAS == 2 ? cluster_addr(bar_acc_empty, 0) : bar_acc_empty, bar_acc_empty, bar_sc_empty, smem_u32(smem_boxes) + (warp - 4) * C::kStaging, abort_flag,
+                                 quarter, half, lane, rank};
+        for (int tile = blockIdx.x / CTAS; tile < p.pieces; tile += step) {
             int m0, n0;
             place(tile, m0, n0);
-            float sum[C::kCols];
-#pragma unroll
-            for (int i = 0; i < C::kCols; i++) sum[i] = 0.f;
-            for (int b = 0; b < blocks; b++, acc.next()) {
-                const int i = b % C::kAhead;
-                const uint32_t from = smem_u32(scales + set.slot * C::kScales);
-                asm volatile("bar.sync %0, %1;" ::"r"(1 + half * C::kAccs + acc.slot), "n"(C::kCalled) : "memory");
-                ok = __all_sync(0xFFFFFFFFu, *abort_flag == 0u);
-                if (!ok) {   // whoever of this half did not see it yet waits at the next barrier, and sees it behind that
-                    acc.next();
-                    asm volatile("bar.arrive %0, %1;" ::"r"(1 + half * C::kAccs + acc.slot), "n"(C::kCalled) : "memory");
-                    break;
-                }
-                tcgen05_fence_after();
-                float row = load_scale(from + 4 * (i * 128 + 32 * quarter + lane));
-                if (MODE == SCALE_ROWS) row *= load_scale(from + 4 * (C::kAhead * 128 + i * CTAS + (CTAS == 2 ? half : 0)));
-                add_block<MODE, C::kCols>(sum, tmem + acc.slot * C::kBN + half * C::kCols + ((uint32_t)(32 * quarter) << 16), row, from + 4 * (C::kAhead * 128 + i * C::kColScales + half * C::kCols), [&] {
-                    tcgen05_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (rank != 0) mbar_arrive_cluster(lead_empty + 8 * acc.slot);
-                        else mbar_arrive(bar_acc_empty + 8 * acc.slot);
-                    }
-                });
-                __syncwarp();
-                if (i == C::kAhead - 1 || b == blocks - 1) {
-                    if (lane == 0) mbar_arrive(bar_sc_empty + 8 * set.slot);
-                    set.next();
-                }
-            }
+            bool ok;
+            if (CTAS == 1 || tile < p.whole) ok = tile_out<CTAS, MODE, C::kCols>(p, maps, e, m0, n0);
+            else ok = tile_out<CTAS, MODE, 64>(p, maps, e, m0, n0);
             if (!ok) break;
-            // Boxes of 32 rows x 128 bytes; a row's last bytes that are no whole 16 by themselves.
-            const int row0 = m0 + 32 * quarter, col0 = n0 + half * C::kCols;
-            if (p.f32) {
-#pragma unroll
-                for (int c = 0; c < C::kCols; c += 32) {
-                    float v[32];
-#pragma unroll
-                    for (int e = 0; e < 32; e++) v[e] = sum[c + e];
-                    send_box<32>(p, &maps.out, box_at, reinterpret_cast<const uint32_t *>(v), row0, col0 + c, lane, [&](int e) { return v[e]; });
-                }
-            } else {
-#pragma unroll
-                for (int c = 0; c < C::kCols; c += 64) {
-                    uint32_t w[32];
-#pragma unroll
-                    for (int e = 0; e < 32; e++) w[e] = pack_bf16(sum[c + 2 * e], sum[c + 2 * e + 1]);
-                    send_box<64>(p, &maps.out, box_at, w, row0, col0 + c, lane, [&](int e) { return __uint_as_float((e & 1) ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16); });
-                }
-            }
         }
         boxes_free(lane);   // the stores have read shared memory; what they write is there when the grid has completed
     }
@@ -821,9 +845,15 @@ fp4q_status launch_persistent(const Operand8 &a, const Operand8 &b, Gemm8Params 
     p.n_tiles = (int32_t)ceil_div(p.n, C::kBN);
     const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles, slots = sm_count(dev) / CTAS;
     if (tiles > 0x3FFFFFFF) return FP4Q_ERR_UNSUPPORTED;
+    // A last round for which half of the pairs suffice is computed in halves of tiles, whose blocks take 0.7 of a whole one's time: weight gradient of 4096 x 4096 over 16384 rows 486 -> 458 us, 4096 x 4096 x 4096
+    // 78 -> 75.  (Halves of a single CTA's tiles take as long as the whole.)
+    const int64_t last = tiles % slots;
+    p.whole = (int32_t)(CTAS == 2 && 2 * last <= slots ? tiles - last : tiles);
+    p.pieces = (int32_t)(2 * tiles - p.whole);
+    if (p.whole != tiles && !make_map8(&maps.b_half, b, 64)) return FP4Q_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
-    cfg.gridDim = dim3((unsigned)(CTAS * std::min(tiles, slots)));
+    cfg.gridDim = dim3((unsigned)(CTAS * std::min<int64_t>(p.pieces, slots)));
     cfg.blockDim = dim3(C::kThreads);
     cfg.dynamicSmemBytes = C::kSmem;
     cfg.stream = stream;
@@ -840,7 +870,7 @@ fp4q_status launch_persistent(const Operand8 &a, const Operand8 &b, Gemm8Params 
 
 // How a product is computed, by estimated time.  Rounds of tiles: a block takes 0.365 us in a single CTA's tile of the persistent kernel (0.51 where both operands' scales differ inside a tile), 0.55 (0.87) in a
 // pair's, four times as large, and a tile 1.3 or 2.2 us beside its blocks; 0.40 (0.60) and 2 us in a tile of a CTA to itself, whose contraction a cluster may share for about 3 us.
-// (4096 x 4096 x 4096: pairs 70 us, single CTAs 82; 2731 x 1003 for 1999 rows 13 and 12.5; 512 x 4096 x 4096 19 and 12.5; 128 x 4096 x 4096 in clusters of four 9, single CTAs 12.5;
+// (4096 x 4096 x 4096: pairs 70 us, single CTAs 82; 1999 x 2731 over 1003 16.4 and 17.6; 512 x 4096 x 4096 19 and 12.5; 128 x 4096 x 4096 in clusters of four 9, single CTAs 12.5;
 // a weight gradient of 256 x 256 over 16384 rows in clusters of eight 15, single CTAs 72.)
 struct Plan8 {
     int pairs = 0, split = 1;   // pairs: 2, single CTAs: 1, clusters of `split` CTAs with a tile: 0
@@ -857,7 +887,8 @@ struct Plan8 {
                          (s > 1 ? 2.5 + 0.15 * (double)s : 0.0), 0, (int)s);
         if (!boxes) return;
         consider((double)ceil_div(tiles, 148) * ((double)blocks * (both ? 0.51 : 0.365) + 1.3), 1, 1);
-        consider((double)ceil_div(ceil_div(m, 256) * ceil_div(n, 256), 74) * ((double)blocks * (both ? 0.87 : 0.55) + 2.2), 2, 1);
+        const int64_t large = ceil_div(m, 256) * ceil_div(n, 256), last = large % 74;
+        consider(((double)(large / 74) + (last == 0 ? 0.0 : last <= 37 ? 0.7 : 1.0)) * ((double)blocks * (both ? 0.87 : 0.55) + 2.2), 2, 1);
     }
 };
 

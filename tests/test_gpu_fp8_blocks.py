@@ -222,6 +222,13 @@ def test_sizes_at_which_the_plan_changes():
         check_all(t, n, k, b.OUT_F32, ws)
 
 
+@pytest.mark.parametrize("dt", [b.OUT_BF16, b.OUT_F32])
+@pytest.mark.parametrize("t,n,k", [(2300, 2148, 1111), (1100, 2300, 2148), (2100, 1200, 2400), (1500, 5000, 1030)])
+def test_last_rounds_of_half_tiles(t, n, k, dt):
+    # A few tiles of 256 x 256 more than there are pairs of CTAs; the first two with columns of which the last tile's second half has none.
+    check_all(t, n, k, dt, b.alloc_workspace("cuda"))
+
+
 def test_rows_behind_32_bits():
     # More than 2^31 elements between the first row of a matrix and its last: codes in a buffer of long rows, of which the product reads and the quantizer writes a few columns.
     x = randn(1, 3, 256).to(torch.bfloat16)
