@@ -5,7 +5,7 @@
 // own in tensor memory; the epilogue's warps take it from there, times its scales, into sums in registers, while the next block's MMAs run into
 // another accumulator.  The accumulator that the tensor cores cut off towards zero is thus never longer than 128 elements; the sums are rounded to nearest.
 // Bound by that path of the accumulators, 1100 cycles a block of a pair's tile where its MMAs take 512: 16384 x 11008 x 4096 797 us (1.85 PFLOP/s; 690 in a short run), the weight gradient of 4096 x 4096 over
-// 16384 rows 451.  One token: bound by the weight's bytes, 4096 x 11008 12.3 us.
+// 16384 rows 400.  One token: bound by the weight's bytes, 4096 x 11008 12.3 us.
 #include "gemm16.cuh"
 
 #include <algorithm>
@@ -473,7 +473,7 @@ struct CfgP {
     static constexpr int kAhead = 4, kScales = kAhead * (128 + kBN);
     static constexpr int kStaging = 4096 * kBoxes;                         // of an epilogue warp: boxes of 32 rows x 128 bytes, on multiples of their size
     static constexpr int kSmem = 1024 + kOperands + 8 * kStaging + 2 * kScales * 4 + 512;
-    static constexpr int kFewRegs = 88, kManyRegs = 208;
+    static constexpr int kFewRegs = 104, kManyRegs = 200;                  // 88 are too few for the scales' warp with both: 438 -> 421 us
     static_assert(128 * kFewRegs + 256 * kManyRegs <= 384 * 168, "registers: what the epilogue takes is what the other warps give");
     static_assert(kSmem <= 227 * 1024 && kStages <= 8, "shared memory budget, barriers");
 };
@@ -499,18 +499,29 @@ __device__ __forceinline__ bool tile_out(const Gemm8Params &p, const MapsP &maps
     float sum[COLS];
 #pragma unroll
     for (int i = 0; i < COLS; i++) sum[i] = 0.f;
+    float row = 0.f;
     for (int b = 0; b < p.blocks; b++, w.acc.next()) {
         const int i = b % C::kAhead;
         const uint32_t from = w.scales + w.set.slot * C::kScales * 4;
         asm volatile("bar.sync %0, %1;" ::"r"(1 + w.half * C::kAccs + w.acc.slot), "n"(C::kCalled) : "memory");
-        if (!__all_sync(0xFFFFFFFFu, *w.abort_flag == 0u)) {   // whoever of this half did not see it yet waits at the next barrier, and sees it behind that
-            w.acc.next();
+        const uint32_t aborted = *w.abort_flag;
+        auto goes_on = [&] {
+            if (__all_sync(0xFFFFFFFFu, aborted == 0u)) return true;
+            w.acc.next();   // whoever of this half did not see it yet waits at the next barrier, and sees it behind that
             asm volatile("bar.arrive %0, %1;" ::"r"(1 + w.half * C::kAccs + w.acc.slot), "n"(C::kCalled) : "memory");
             return false;
-        }
+        };
+        auto row_scale = [&](int i) {
+            const float f = load_scale(from + 4 * (i * 128 + 32 * w.quarter + w.lane));
+            return MODE == SCALE_ROWS ? f * load_scale(from + 4 * (C::kAhead * 128 + i * CTAS + w.half * COLS / 128)) : f;
+        };
+        // Where the columns' scales make the additions the longest part, nothing is waited for ahead of them: the flag is looked at behind them, and the next block's scale is loaded
+        // beside them.  Weight gradient of 4096 x 4096 over 16384 rows 412 -> 362 us for the two together, nothing for either alone; with one scale for all columns slower, 682 -> 691.
+        if (MODE == SCALE_ROWS && !goes_on()) return false;
         tcgen05_fence_after();
-        float row = load_scale(from + 4 * (i * 128 + 32 * w.quarter + w.lane));
-        if (MODE == SCALE_ROWS) row *= load_scale(from + 4 * (C::kAhead * 128 + i * CTAS + w.half * COLS / 128));
+        float next = 0.f;
+        if (MODE == SCALE_ROWS || i == 0) row = row_scale(i);
+        if (MODE == SCALE_BOTH) next = row_scale(min(i + 1, C::kAhead - 1));
         add_block<MODE, COLS>(sum, w.tmem + w.acc.slot * C::kBN + w.half * COLS + ((uint32_t)(32 * w.quarter) << 16), row, from + 4 * (C::kAhead * 128 + i * C::kColScales + w.half * COLS), [&] {
             tcgen05_fence_before();
             __syncwarp();
@@ -519,6 +530,10 @@ __device__ __forceinline__ bool tile_out(const Gemm8Params &p, const MapsP &maps
                 else mbar_arrive(w.acc_empty + 8 * w.acc.slot);
             }
         });
+        if (MODE == SCALE_BOTH) {
+            row = next;
+            if (!goes_on()) return false;
+        }
         __syncwarp();
         if (i == C::kAhead - 1 || b == p.blocks - 1) {
             if (w.lane == 0) mbar_arrive(w.sc_empty + 8 * w.set.slot);
@@ -845,8 +860,8 @@ fp4q_status launch_persistent(const Operand8 &a, const Operand8 &b, Gemm8Params 
     p.n_tiles = (int32_t)ceil_div(p.n, C::kBN);
     const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles, slots = sm_count(dev) / CTAS;
     if (tiles > 0x3FFFFFFF) return FP4Q_ERR_UNSUPPORTED;
-    // A last round for which half of the pairs suffice is computed in halves of tiles, whose blocks take 0.7 of a whole one's time: weight gradient of 4096 x 4096 over 16384 rows 486 -> 458 us, 4096 x 4096 x 4096
-    // 78 -> 75.  (Halves of a single CTA's tiles take as long as the whole.)
+    // A last round for which half of the pairs suffice is computed in halves of tiles, whose blocks take 0.7 of a whole one's time: weight gradient of 4096 x 4096 over 16384 rows 486 -> 458 us (before its
+    // additions were faster), 4096 x 4096 x 4096 78 -> 75.  (Halves of a single CTA's tiles take as long as the whole.)
     const int64_t last = tiles % slots;
     p.whole = (int32_t)(CTAS == 2 && 2 * last <= slots ? tiles - last : tiles);
     p.pieces = (int32_t)(2 * tiles - p.whole);
@@ -868,15 +883,15 @@ fp4q_status launch_persistent(const Operand8 &a, const Operand8 &b, Gemm8Params 
     return launched(cudaLaunchKernelEx(&cfg, gemm8_kernel<CTAS, MODE>, maps, p));
 }
 
-// How a product is computed, by estimated time.  Rounds of tiles: a block takes 0.365 us in a single CTA's tile of the persistent kernel (0.51 where both operands' scales differ inside a tile), 0.55 (0.87) in a
-// pair's, four times as large, and a tile 1.3 or 2.2 us beside its blocks; 0.40 (0.60) and 2 us in a tile of a CTA to itself, whose contraction a cluster may share for about 3 us.
+// How a product is computed, by estimated time.  Rounds of tiles: a block takes 0.365 us in a single CTA's tile of the persistent kernel (0.47 where both operands' scales differ inside a tile), 0.55 (0.71) in a
+// pair's, four times as large, and a tile 1.3 or 2.2 us beside its blocks; 0.40 (0.58) and 2 us in a tile of a CTA to itself, whose contraction a cluster may share for about 3 us.
 // (4096 x 4096 x 4096: pairs 70 us, single CTAs 82; 1999 x 2731 over 1003 16.4 and 17.6; 512 x 4096 x 4096 19 and 12.5; 128 x 4096 x 4096 in clusters of four 9, single CTAs 12.5;
 // a weight gradient of 256 x 256 over 16384 rows in clusters of eight 15, single CTAs 72.)
 struct Plan8 {
     int pairs = 0, split = 1;   // pairs: 2, single CTAs: 1, clusters of `split` CTAs with a tile: 0
     Plan8(int64_t m, int64_t n, int64_t blocks, bool both, bool boxes, int dev)
     {
-        const double each = both ? 0.60 : 0.40;
+        const double each = both ? 0.58 : 0.40;
         double least = 1e30;
         auto consider = [&](double us, int p, int s) {
             if (us < least) { least = us; pairs = p; split = s; }
@@ -886,9 +901,9 @@ struct Plan8 {
             consider((double)ceil_div(tiles, both ? clusters_at_once<SCALE_BOTH>((int)s, dev) : clusters_at_once<SCALE_ROWS>((int)s, dev)) * ((double)ceil_div(blocks, s) * each + 2.0) +
                          (s > 1 ? 2.5 + 0.15 * (double)s : 0.0), 0, (int)s);
         if (!boxes) return;
-        consider((double)ceil_div(tiles, 148) * ((double)blocks * (both ? 0.51 : 0.365) + 1.3), 1, 1);
+        consider((double)ceil_div(tiles, 148) * ((double)blocks * (both ? 0.47 : 0.365) + 1.3), 1, 1);
         const int64_t large = ceil_div(m, 256) * ceil_div(n, 256), last = large % 74;
-        consider(((double)(large / 74) + (last == 0 ? 0.0 : last <= 37 ? 0.7 : 1.0)) * ((double)blocks * (both ? 0.87 : 0.55) + 2.2), 2, 1);
+        consider(((double)(large / 74) + (last == 0 ? 0.0 : last <= 37 ? 0.7 : 1.0)) * ((double)blocks * (both ? 0.71 : 0.55) + 2.2), 2, 1);
     }
 };
 
