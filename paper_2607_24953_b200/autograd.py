@@ -137,10 +137,11 @@ def ragged_linear(x: torch.Tensor, weight: torch.Tensor, row_offsets: torch.Tens
 
 
 def _rows(t: torch.Tensor) -> torch.Tensor:
-    """t as the norm and the 8-bit quantizer read it: BF16 or FP32 in contiguous rows; t itself where it is so."""
+    """t as the norm and the 8-bit quantizer read it: BF16 or FP32 in contiguous rows that do not share memory (those of expanded tensors do); t itself where it is so."""
     if t.dtype not in (torch.bfloat16, torch.float32):
         t = t.to(torch.bfloat16)
-    return t if t.stride(1) == 1 or t.shape[1] <= 1 else t.contiguous()
+    rows, cols = t.shape
+    return t if (t.stride(1) == 1 or cols <= 1) and (t.stride(0) >= cols or rows <= 1) else t.contiguous()
 
 
 def _cast(t, dtype):
