@@ -212,7 +212,10 @@ class _FP8LinearFn(torch.autograd.Function):
             qx = binding.fp4q_fp8_quantize(xr, want_t=keep_x)
         else:
             rr = None if residual is None else _rows(residual)
-            n = binding.fp4q_rms_norm(xr, _weight(norm_weight), rr, eps=eps, y=keep_x, q=binding.Q_FP8, rstd=True)
+            out = binding.alloc_norm(xr, rr, y=keep_x and x.dtype == torch.bfloat16, q=binding.Q_FP8, rstd=True)
+            if keep_x and out.y is None:
+                out.y = torch.empty((T, K), dtype=torch.float32, device=x.device)
+            n = binding.fp4q_rms_norm(xr, _weight(norm_weight), rr, eps=eps, out=out)
             qx = binding.Fp8Tensor(T, K, n.q, n.scale)
             h, rstd = xr if rr is None else n.h, n.rstd
             if keep_x:   # the weight gradient's operand: the norm's output along the tokens
@@ -238,8 +241,7 @@ class _FP8LinearFn(torch.autograd.Function):
         if need[1]:
             dw = _cast(binding.fp4q_fp8_gemm_wgrad(qd, binding.Fp8Tensor(T, K, None, None, xt, xts), ws=ctx.ws), ctx.types[1])
         if inputs:
-            wide = binding.OUT_F32 if rstd is None and ctx.types[0] != torch.bfloat16 else binding.OUT_BF16
-            dx = binding.fp4q_fp8_gemm_dgrad(qd, binding.Fp8Tensor(N, K, None, ws, wt, None, True), dt=wide, ws=ctx.ws)
+            dx = binding.fp4q_fp8_gemm_dgrad(qd, binding.Fp8Tensor(N, K, None, ws, wt, None, True), dt=_out16(ctx.types[0]), ws=ctx.ws)
             if rstd is not None:
                 dx, dn = _norm_backward(dx, dh, h, rstd, norm_weight, need[2])
         return _cast(dx, ctx.types[0]) if need[0] else None, dw, dn, _cast(dx, ctx.types[2]) if need[3] else None, None, None
@@ -260,8 +262,9 @@ def fp8_linear(x: torch.Tensor, weight: torch.Tensor, ws=None) -> torch.Tensor:
 
 
 def rms_norm_fp8_linear(x: torch.Tensor, norm_weight, weight: torch.Tensor, residual=None, eps: float = 1e-6, ws=None):
-    """fp8_linear(rms_norm(x, norm_weight, residual)), the norm writing the product's operand itself.  Several projections of one input are one with their weights above
-    each other.  Returns y or, with a residual, (y, h)."""
+    """fp8_linear(rms_norm(x, norm_weight, residual)), the norm writing the product's operand itself: from its output before that is rounded to BF16, where x is BF16 (the weight gradient's
+    operand and the gradient between the two are BF16 then); where x is FP32 all of it is FP32, and the result that of the two calls.  Several projections of one input are one with
+    their weights above each other.  Returns y or, with a residual, (y, h)."""
     _check_linear(x, weight)
     _check_norm(x, norm_weight, residual)
     if ws is None:
