@@ -520,7 +520,7 @@ fp4q_status fp4q_rms_norm(const fp4q_norm *n, int64_t rows, int64_t cols, void *
 /*
  * fp4q_rms_norm_bwd -- its gradients: with g = dy weight,
  *   dx = r (g - h r mean(g h r)) + dh (the gradient that arrives at h by itself; NULL: none),   dweight (+)= sum over the rows of dy h r
- * dx is the gradient of x and of the residual alike; dh and dx have h's type, and dx may be dh's own memory.  h and rstd are those of the forward pass.  dweight is FP32 [cols] or
+ * dx is the gradient of x and of the residual alike; dh and dx have h's type, and dx may be the memory of dh, of h or, if that has h's type, of dy, in the same pitch; otherwise it overlaps nothing that is read.  h and rstd are those of the forward pass.  dweight is FP32 [cols] or
  * NULL; accumulate != 0 adds to it.  No rows leave dweight zero, or unchanged when accumulating.  The sum over the rows is taken in FP32 in a fixed order.  scratch: fp4q_rms_norm_bwd_scratch_bytes()
  * bytes of device memory, 256-byte aligned, any contents, for dweight alone; calls that share it must not overlap on the GPU.
  */

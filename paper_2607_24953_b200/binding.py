@@ -540,7 +540,7 @@ def alloc_rms_norm_scratch(rows: int, cols: int, device) -> torch.Tensor:
 def fp4q_rms_norm_bwd(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight=None, dh=None, out=None, dweight=None, want_dweight: bool = True,
                       accumulate: bool = False, scratch=None, stream=None):
     """(dx, dweight): the gradient of x and of the residual, in h's type, and that of the weight, FP32.  dh: the gradient that arrives at h by itself; accumulate: adds to
-    dweight."""
+    dweight.  out may be dh, h or, where it has h's type, dy."""
     return _host().rms_norm_bwd(dy, h, rstd, weight, dh, out, dweight, want_dweight, accumulate, scratch, _handle(stream))
 
 

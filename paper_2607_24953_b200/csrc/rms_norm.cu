@@ -518,10 +518,15 @@ fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scra
     p.partial = dweight ? static_cast<float *>(scratch) : nullptr;
     int64_t parts = 1;
     auto launch = [&](auto kernel, std::atomic<int> &known) {
-        parts = std::max<int64_t>(1, std::min({(int64_t)kGradCtas, ceil_div(p.rows, d.threads / d.team), (int64_t)148 * resident(kernel, d.threads, known)}));
-        return launched(launch_dependent(kernel, dim3((unsigned)parts), d.threads, s, p));
+        const int64_t ctas = std::max<int64_t>(1, std::min({(int64_t)kGradCtas, ceil_div(p.rows, d.threads / d.team), (int64_t)148 * resident(kernel, d.threads, known)}));
+        if (fused) parts = ctas;
+        return launched(launch_dependent(kernel, dim3((unsigned)ctas), d.threads, s, p));
     };
     static std::atomic<int> known[10];
+    if (dweight && !fused) {   // before dx, which may overwrite what this reads
+        parts = std::max<int64_t>(1, std::min<int64_t>(kGradCtas / 2, ceil_div(p.rows, 8)));
+        if (fp4q_status st = launched(launch_dependent(rms_norm_dweight_kernel<TY, TH>, dim3((unsigned)ceil_div(p.cols, 512), (unsigned)parts), 256, s, p))) return st;
+    }
     if (fused || p.rows > 0) {
         fp4q_status st;
         auto one = [&](auto most, int at) {   // one chunk a thread
@@ -542,10 +547,6 @@ fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scra
         if (st) return st;
     }
     if (!dweight) return FP4Q_OK;
-    if (!fused) {
-        parts = std::max<int64_t>(1, std::min<int64_t>(kGradCtas / 2, ceil_div(p.rows, 8)));
-        if (fp4q_status st = launched(launch_dependent(rms_norm_dweight_kernel<TY, TH>, dim3((unsigned)ceil_div(p.cols, 512), (unsigned)parts), 256, s, p))) return st;
-    }
     const SumParams q = {p.partial, p.cols, (int32_t)parts, accumulate != 0, dweight};
     return launched(launch_dependent(column_sum_kernel, dim3((unsigned)ceil_div(p.cols, 32)), 1024, s, q));
 }
