@@ -136,10 +136,18 @@ def ragged_linear(x: torch.Tensor, weight: torch.Tensor, row_offsets: torch.Tens
     return _RaggedLinearFn.apply(x, weight, row_offsets, ws)
 
 
+def _wide(t: torch.Tensor) -> torch.Tensor:
+    """t as the norm and the 8-bit quantizer read its elements: BF16 or FP32 as they are, other floating-point types in FP32, which holds those of 16 and 8 bits exactly."""
+    if t.dtype in (torch.bfloat16, torch.float32):
+        return t
+    if not t.dtype.is_floating_point:
+        raise ValueError(f"tensors must hold floating-point numbers, not {t.dtype}")
+    return t.to(torch.float32)
+
+
 def _rows(t: torch.Tensor) -> torch.Tensor:
-    """t as the norm and the 8-bit quantizer read it: BF16 or FP32 in contiguous rows that do not share memory (those of expanded tensors do); t itself where it is so."""
-    if t.dtype not in (torch.bfloat16, torch.float32):
-        t = t.to(torch.bfloat16)
+    """The same in contiguous rows that do not share memory (those of expanded tensors do); t itself where it is so."""
+    t = _wide(t)
     rows, cols = t.shape
     return t if (t.stride(1) == 1 or cols <= 1) and (t.stride(0) >= cols or rows <= 1) else t.contiguous()
 
@@ -152,7 +160,7 @@ class _RMSNormFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, residual, eps):
         xr, rr = _rows(x), None if residual is None else _rows(residual)
-        out = binding.alloc_norm(xr, rr, y=x.dtype != torch.float32, rstd=True)
+        out = binding.alloc_norm(xr, rr, y=x.dtype == torch.bfloat16, rstd=True)
         if out.y is None:
             out.y = torch.empty(x.shape, dtype=torch.float32, device=x.device)
         n = binding.fp4q_rms_norm(xr, _weight(weight), rr, eps=eps, out=out)
@@ -172,7 +180,7 @@ class _RMSNormFn(torch.autograd.Function):
 
 
 def _weight(weight):
-    return None if weight is None else _cast(weight, torch.float32 if weight.dtype not in (torch.bfloat16, torch.float32) else weight.dtype).contiguous()
+    return None if weight is None else _wide(weight).contiguous()
 
 
 def _norm_backward(dy, dh, h, rstd, weight, want):
@@ -194,7 +202,8 @@ def _fold(t):
 
 def rms_norm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-6):
     """y = h weight / sqrt(mean(h^2) + eps) over the last dimension, with h = x or, where there is a residual, h = x + residual (in the residual's type); then (y, h) is
-    returned, h being the residual of what follows.  BF16 or FP32.  Differentiable once."""
+    returned, h being the residual of what follows.  BF16 or FP32; tensors of other floating-point types are taken in FP32, and what is returned for them is rounded to their type at the
+    end.  Differentiable once."""
     _check_norm(x, weight, residual)
     y, h = _RMSNormFn.apply(_fold(x), weight, _fold(residual), float(eps))
     return y.reshape(x.shape) if residual is None else (y.reshape(x.shape), h.reshape(x.shape))
@@ -254,7 +263,7 @@ def _check_linear(x, weight):
 
 def fp8_linear(x: torch.Tensor, weight: torch.Tensor, ws=None) -> torch.Tensor:
     """y = x^ weight^^T with products in 8 bits, forward and backward: E4M3 codes with a scale for every 128 elements of a row of x and of the gradient, and for 128 x 128 of the
-    weight.  x [..., K], weight [N, K], BF16 or FP32.  y is BF16.  Straight-through; differentiable once."""
+    weight.  x [..., K], weight [N, K], BF16 or FP32 (other floating-point types are taken in FP32).  y is BF16.  Straight-through; differentiable once."""
     _check_linear(x, weight)
     if ws is None:
         ws = binding.alloc_workspace(x.device)

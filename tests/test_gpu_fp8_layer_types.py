@@ -32,3 +32,25 @@ def test_on_fp32_one_call_is_the_two_calls(rows, k, n, stream):
         both.append(outs + list(torch.autograd.grad(outs, leaves, grads)))
     for p, q in zip(*both):
         assert p.dtype == q.dtype and torch.equal(p, q)
+
+
+def run(f, leaves, grads):
+    leaves = [t.detach().requires_grad_() for t in leaves]
+    out = f(*leaves)
+    outs = list(out) if isinstance(out, tuple) else [out]
+    return outs, torch.autograd.grad(outs, leaves, grads[:len(outs)])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64])
+def test_other_types_are_computed_in_fp32(dtype):
+    x, r, g, w = randn(1, 50, 76).to(dtype), randn(2, 50, 76).to(dtype), (1 + 0.2 * randn(3, 76)).to(dtype), (randn(4, 40, 76) * 0.05).to(dtype)
+    dy, dz, dh = randn(5, 50, 76).to(dtype), randn(6, 50, 40).to(BF16), randn(7, 50, 76).to(dtype)
+    cases = [(autograd.rms_norm, [x, g], [dy]), (autograd.rms_norm, [x, g, r], [dy, dh]), (autograd.fp8_linear, [x, w], [dz]), (autograd.rms_norm_fp8_linear, [x, g, w], [dz]),
+             (autograd.rms_norm_fp8_linear, [x, g, w, r], [dz, dh])]
+    for f, leaves, grads in cases:
+        outs, got = run(f, leaves, grads)
+        wide, want = run(f, [t.float() for t in leaves], [t if t.dtype == BF16 else t.float() for t in grads])
+        for p, q in zip(outs, wide):
+            assert p.dtype == (BF16 if q.dtype == BF16 else dtype) and torch.equal(p, q.to(p.dtype))
+        for p, q in zip(got, want):
+            assert p.dtype == dtype and torch.equal(p, q.to(dtype))
