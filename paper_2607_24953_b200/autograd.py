@@ -156,19 +156,31 @@ def _cast(t, dtype):
     return t if t is None or t.dtype == dtype else t.to(dtype)
 
 
+def _norm(x, weight, residual, eps, q=binding.Q_NONE, y=True):
+    """fp4q_rms_norm with y in x's type and h and, without q, y contiguous: layers return them, and where the call's own buffers have padding behind their rows (which the kernel does
+    not need) they would be copied."""
+    rows, cols = x.shape
+    whole = cols % 8 == 0
+    if whole and (x.dtype == torch.bfloat16 or not y):
+        return binding.fp4q_rms_norm(x, weight, residual, eps=eps, y=y, q=q, rstd=True)
+    out = binding.alloc_norm(x, residual if whole else None, y=False, q=q, rstd=True)
+    if residual is not None and not whole:
+        out.h = torch.empty((rows, cols), dtype=residual.dtype, device=x.device)
+    if y:
+        out.y = torch.empty((rows, cols if q == binding.Q_NONE else (cols + 7) // 8 * 8), dtype=x.dtype, device=x.device)[:, :cols]
+    return binding.fp4q_rms_norm(x, weight, residual, eps=eps, out=out)
+
+
 class _RMSNormFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, residual, eps):
         xr, rr = _rows(x), None if residual is None else _rows(residual)
-        out = binding.alloc_norm(xr, rr, y=x.dtype == torch.bfloat16, rstd=True)
-        if out.y is None:
-            out.y = torch.empty(x.shape, dtype=torch.float32, device=x.device)
-        n = binding.fp4q_rms_norm(xr, _weight(weight), rr, eps=eps, out=out)
+        n = _norm(xr, _weight(weight), rr, eps)
         ctx.save_for_backward(xr if rr is None else n.h, n.rstd, weight)
         ctx.set_materialize_grads(False)
         ctx.types = x.dtype, None if residual is None else residual.dtype
-        y = _cast(n.y, x.dtype).contiguous()
-        return (y, None) if residual is None else (y, _cast(n.h, residual.dtype).contiguous())
+        y = _cast(n.y, x.dtype)
+        return (y, None) if residual is None else (y, _cast(n.h, residual.dtype))
 
     @staticmethod
     @once_differentiable
@@ -221,10 +233,7 @@ class _FP8LinearFn(torch.autograd.Function):
             qx = binding.fp4q_fp8_quantize(xr, want_t=keep_x)
         else:
             rr = None if residual is None else _rows(residual)
-            out = binding.alloc_norm(xr, rr, y=keep_x and x.dtype == torch.bfloat16, q=binding.Q_FP8, rstd=True)
-            if keep_x and out.y is None:
-                out.y = torch.empty((T, K), dtype=torch.float32, device=x.device)
-            n = binding.fp4q_rms_norm(xr, _weight(norm_weight), rr, eps=eps, out=out)
+            n = _norm(xr, _weight(norm_weight), rr, eps, binding.Q_FP8, keep_x)
             qx = binding.Fp8Tensor(T, K, n.q, n.scale)
             h, rstd = xr if rr is None else n.h, n.rstd
             if keep_x:   # the weight gradient's operand: the norm's output along the tokens
@@ -236,7 +245,7 @@ class _FP8LinearFn(torch.autograd.Function):
         ctx.set_materialize_grads(False)
         ctx.sizes, ctx.ws, ctx.device = (T, K, weight.shape[0]), ws, x.device
         ctx.types = x.dtype, weight.dtype, None if residual is None else residual.dtype
-        return y.contiguous(), None if residual is None else _cast(h, residual.dtype).contiguous()
+        return y.contiguous(), None if residual is None else _cast(h, residual.dtype)
 
     @staticmethod
     @once_differentiable
