@@ -224,8 +224,9 @@ def rms_norm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-6):
 class _FP8LinearFn(torch.autograd.Function):
     """The linear layer in 8 bits with a scale for every block of 128, behind a norm or on its own (norm: weight and eps, or None)."""
     @staticmethod
-    def forward(ctx, x, weight, norm_weight, residual, eps, ws):
-        keep_x, keep_w = ctx.needs_input_grad[1], any(ctx.needs_input_grad[i] for i in (0, 2, 3))
+    def forward(ctx, x, weight, norm_weight, residual, eps, ws, keep):
+        # keep: a backward pass may follow (needs_input_grad holds where gradients are switched off, too)
+        keep_x, keep_w = keep and ctx.needs_input_grad[1], keep and any(ctx.needs_input_grad[i] for i in (0, 2, 3))
         xr = _rows(x)
         T, K = x.shape
         h = rstd = None
@@ -262,7 +263,7 @@ class _FP8LinearFn(torch.autograd.Function):
             dx = binding.fp4q_fp8_gemm_dgrad(qd, binding.Fp8Tensor(N, K, None, ws, wt, None, True), dt=_out16(ctx.types[0]), ws=ctx.ws)
             if rstd is not None:
                 dx, dn = _norm_backward(dx, dh, h, rstd, norm_weight, need[2])
-        return _cast(dx, ctx.types[0]) if need[0] else None, dw, dn, _cast(dx, ctx.types[2]) if need[3] else None, None, None
+        return _cast(dx, ctx.types[0]) if need[0] else None, dw, dn, _cast(dx, ctx.types[2]) if need[3] else None, None, None, None
 
 
 def _check_linear(x, weight):
@@ -276,7 +277,7 @@ def fp8_linear(x: torch.Tensor, weight: torch.Tensor, ws=None) -> torch.Tensor:
     _check_linear(x, weight)
     if ws is None:
         ws = binding.alloc_workspace(x.device)
-    return _FP8LinearFn.apply(_fold(x), weight, None, None, None, ws)[0].reshape(*x.shape[:-1], weight.shape[0])
+    return _FP8LinearFn.apply(_fold(x), weight, None, None, None, ws, torch.is_grad_enabled())[0].reshape(*x.shape[:-1], weight.shape[0])
 
 
 def rms_norm_fp8_linear(x: torch.Tensor, norm_weight, weight: torch.Tensor, residual=None, eps: float = 1e-6, ws=None):
@@ -287,7 +288,7 @@ def rms_norm_fp8_linear(x: torch.Tensor, norm_weight, weight: torch.Tensor, resi
     _check_norm(x, norm_weight, residual)
     if ws is None:
         ws = binding.alloc_workspace(x.device)
-    y, h = _FP8LinearFn.apply(_fold(x), weight, norm_weight, _fold(residual), float(eps), ws)
+    y, h = _FP8LinearFn.apply(_fold(x), weight, norm_weight, _fold(residual), float(eps), ws, torch.is_grad_enabled())
     y = y.reshape(*x.shape[:-1], weight.shape[0])
     return y if residual is None else (y, h.reshape(x.shape))
 

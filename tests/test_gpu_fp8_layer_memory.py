@@ -41,3 +41,16 @@ def test_the_stream_is_not_copied(rows, cols):
     assert y.is_contiguous() and h.is_contiguous()
     codes = rows * (cols + 16) + 64 * (cols + 16)
     assert most <= h.numel() * 4 + codes + 2 * y.numel() * 2 + 8 * (2 << 20)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_nothing_is_kept_for_a_backward_pass_where_gradients_are_off(dtype):
+    rows, cols, n = 4096, 2048, 512
+    x, g, w = randn(1, rows, cols).to(dtype).requires_grad_(), (1 + 0.2 * randn(3, cols)).requires_grad_(), (randn(4, n, cols) * 0.05).requires_grad_()
+    for f in (lambda: autograd.fp8_linear(x, w), lambda: autograd.rms_norm_fp8_linear(x, g, w)):
+        want = f().detach()
+        with torch.no_grad():
+            most, y = peak(f)
+        assert torch.equal(y, want)
+        # codes and scales of x and of the weight, the output, 1 / root of every row
+        assert most <= (rows + n) * cols + rows * (cols // 128) * 4 + y.numel() * 2 + 6 * (2 << 20)
