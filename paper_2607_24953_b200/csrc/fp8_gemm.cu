@@ -196,7 +196,7 @@ __device__ __forceinline__ void store_four(const Gemm8Params &p, int64_t row, in
     }
 }
 
-// A box of 32 rows x 128 bytes, COLS columns from col on, leaves an epilogue warp, which has two of them in turn at box_at.  w: the lane's row of it, value(e): its elements.
+// A box of 32 rows x 128 bytes, COLS columns from col on, leaves an epilogue warp, which has two of them in turn at box_at, side by side on 8 KB.  w: the lane's row of it, value(e): its elements.
 template <int COLS, typename F>
 __device__ __forceinline__ void send_box(const Gemm8Params &p, const CUtensorMap *map, uint32_t &box_at, const uint32_t *w, int row0, int col, int lane, F value)
 {
@@ -471,10 +471,11 @@ struct CfgP {
     static constexpr int kCalled = 128 + 32;                               // threads of a named barrier: half of the epilogue, and the caller
     static constexpr int kColScales = MODE == SCALE_BOTH ? kBN : 0;        // else one for each block of 128 columns
     static constexpr int kAhead = 4, kScales = kAhead * (128 + kBN);
-    static constexpr int kStaging = 4096 * kBoxes;                         // of an epilogue warp: boxes of 32 rows x 128 bytes, on multiples of their size
-    static constexpr int kSmem = 1024 + kOperands + 8 * kStaging + 2 * kScales * 4 + 512;
+    static constexpr int kStaging = 4096 * kBoxes, kAlign = kStaging;      // of an epilogue warp: boxes of 32 rows x 128 bytes, on a multiple of both boxes' size, wherever shared memory begins
+    static constexpr int kSmem = kAlign + kOperands + 8 * kStaging + 2 * kScales * 4 + 512;
     static constexpr int kFewRegs = 104, kManyRegs = 200;                  // 88 are too few for the scales' warp with both: 438 -> 421 us
     static_assert(128 * kFewRegs + 256 * kManyRegs <= 384 * 168, "registers: what the epilogue takes is what the other warps give");
+    static_assert(kBoxes == 2 && kAlign % 1024 == 0 && kOperands % kAlign == 0, "one box from the other: bit 12 of its address");
     static_assert(kSmem <= 227 * 1024 && kStages <= 8, "shared memory budget, barriers");
 };
 struct MapsP {
@@ -567,7 +568,7 @@ __global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ M
 {
     using C = CfgP<CTAS, MODE>;
     extern __shared__ uint8_t smem_raw[];
-    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + C::kAlign - 1) & ~(uintptr_t)(C::kAlign - 1));
     uint8_t *smem_a = smem, *smem_b = smem + C::kStages * C::kABytes, *smem_boxes = smem + C::kOperands;
     float *scales = reinterpret_cast<float *>(smem_boxes + 8 * C::kStaging);
     uint64_t *bars = reinterpret_cast<uint64_t *>(scales + 2 * C::kScales);
