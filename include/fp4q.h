@@ -473,7 +473,8 @@ fp4q_status fp4q_fp8_quantize(const void *x, fp4q_out x_type, int64_t rows, int6
  *   Y[T,N] = X^ W^^T    reads X.q (1D blocks) and W.q (square)            dX[T,K] = dY^ W^    reads dY.q (1D) and W.q_t (square)
  *   dW[N,K] (+)= dY^^T X^    reads dY.q_t and X.q_t (1D, along the tokens)
  * Any T, N and K, 0 included (an empty contraction gives zeros).  The products of 128 contraction elements are added up by the tensor cores, the sums of these blocks,
- * times both scales, in FP32, rounded to nearest.  Single tokens and small results split the contraction over up to 8 CTAs, whose sums are added in a fixed order.  Outputs,
+ * times both scales, in FP32, rounded to nearest.  Two scales whose product is not in FP32's range multiply the sum all the same (slowly where it is above); where it is below the normal
+ * range, a block's share of a result is off by 2^-125 at most.  Single tokens and small results split the contraction over up to 8 CTAs, whose sums are added in a fixed order.  Outputs,
  * FP4Q_OUT_PADDED, alignment, accumulate (FP32 only), ws/ws_bytes/stream and the asynchronous FP4Q_ERR_TIMEOUT as for fp4q_gemm_fwd and
  * fp4q_gemm_wgrad.
  */

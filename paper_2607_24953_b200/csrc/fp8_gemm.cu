@@ -6,7 +6,10 @@
 // another accumulator.  The accumulator that the tensor cores cut off towards zero is thus never longer than 128 elements; the sums are rounded to nearest.
 // Bound by that path of the accumulators, 1100 cycles a block of a pair's tile where its MMAs take 512: 16384 x 11008 x 4096 797 us (1.85 PFLOP/s; 690 in a short run), the weight gradient of 4096 x 4096 over
 // 16384 rows 400.  One token: bound by the weight's bytes, 4096 x 11008 12.3 us.
+#include "fp8_format.cuh"
 #include "gemm16.cuh"
+
+#include <cuda_fp8.h>
 
 #include <algorithm>
 
@@ -44,6 +47,8 @@ struct Gemm8Params {
     int64_t ldc;
     int32_t f32, accumulate, wide;
     uint32_t *status;
+    const uint8_t *qa, *qb;          // codes, for sums that are not finite: rows of A and B, k of each
+    int64_t lda, ldb, k;
 };
 struct Maps8 {
     CUtensorMap a, b;
@@ -124,6 +129,89 @@ __device__ __forceinline__ void add_block(float (&sum)[COLS], uint32_t from, flo
 #pragma unroll
         for (int e = 0; e < 16; e++) sum[c + e] = fmaf(__uint_as_float(x[e]), MODE == SCALE_ROWS ? row : f[e], sum[c + e]);
     }
+}
+
+// Scales are FP32 numbers, and the product of two need not be one.  Above FP32's range it is infinite, and the sum it enters infinite or, where the block's product is 0, NaN: sums that
+// are not finite are looked at before they leave, and computed again, from the codes, if scales are why.  (The loops over blocks know nothing of it: a look at every set of scales there, with
+// a way out, cost 5 to 20 %; this 0 to 2.)  Below the normal range a product of scales keeps fewer bits, which moves a block's share of a sum by |x| 2^-150 < 2^-125 at most.
+
+// sum + x a b, with nothing on the way out of FP32's range that is in it at the end; |x| is 0 or from 2^-18 to 2^25.
+__device__ __forceinline__ float add_scaled(float sum, float x, float a, float b)
+{
+    const float f = a * b;
+    if (!is_infinite(f)) return fmaf(x, f, sum);
+    return fmaf((x * 0x1p64f) * ((a * 0x1p-64f) * (b * 0x1p-64f)), 0x1p64f, sum);   // neither is below 1
+}
+// + the product of 16 codes of each operand.
+__device__ __forceinline__ float add_codes(float x, const uint4 &a, const uint4 &b)
+{
+    const uint32_t u[4] = {a.x, a.y, a.z, a.w}, v[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+        const auto value = [](uint32_t w, int at) { return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)(w >> at), __NV_E4M3))); };
+        x = fmaf(value(u[i / 4], 8 * (i % 4)), value(v[i / 4], 8 * (i % 4)), x);
+    }
+    return x;
+}
+// Codes k .. k + 15 of a row, which begins on 16 bytes, those below n.
+__device__ __forceinline__ uint4 codes_at(const uint8_t *row, int64_t k, int64_t n)
+{
+    if (k + 16 <= n) return load_global(reinterpret_cast<const uint4 *>(row + k));
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    for (int i = 0; k + i < n; i++) w[i / 4] |= (uint32_t)load_global(row + k + i) << (8 * (i % 4));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The sum of row m of A and row n of B, which was not finite.
+__device__ __noinline__ float careful_sum(const Gemm8Params &p, int m, int n, float was)
+{
+    bool scales = false;
+    for (int b = 0; b < p.blocks; b++) scales |= is_infinite(p.sa.at(m, b) * p.sb.at(n, b));
+    if (!scales) return was;
+    float sum = 0.f;
+    const uint8_t *a = p.qa + m * p.lda, *w = p.qb + n * p.ldb;
+    for (int b = 0; b < p.blocks; b++) {
+        const int64_t end = min((int64_t)(b + 1) * kBlock8, p.k);
+        float x = 0.f;
+        for (int64_t k = (int64_t)b * kBlock8; k < end; k += 16) x = add_codes(x, codes_at(a, k, end), codes_at(w, k, end));
+        sum = add_scaled(sum, x, p.sa.at(m, b), p.sb.at(n, b));
+    }
+    return sum;
+}
+__device__ __noinline__ void careful_sums(const Gemm8Params &p, int m, int n, int count, float *sums)   // columns n .. n + count - 1
+{
+    if (m >= p.m) return;
+    float top = 0.f;   // a product of finite scales is infinite if both are above 1
+    for (int b = 0; b < p.blocks; b++) top = fmaxf(top, fabsf(p.sa.at(m, b)));
+    if (!(top > 1.f)) return;
+    for (int e = 0; e < count && n + e < p.n; e++)
+        if (!(fabsf(sums[e]) <= 0x1.fffffep127f)) sums[e] = careful_sum(p, m, n + e, sums[e]);
+}
+// Four sums next to one another in the output: along B's rows or, transposed, A's.
+__device__ __noinline__ float4 careful_four(const Gemm8Params &p, int m, int n, bool transposed, float4 v)
+{
+    if (transposed) {
+        careful_sums(p, m, n, 1, &v.x);
+        careful_sums(p, m + 1, n, 1, &v.y);
+        careful_sums(p, m + 2, n, 1, &v.z);
+        careful_sums(p, m + 3, n, 1, &v.w);
+    } else {
+        careful_sums(p, m, n, 4, &v.x);
+    }
+    return v;
+}
+template <int COLS>
+__device__ __forceinline__ void check_sums(const Gemm8Params &p, int m, int n, float (&sum)[COLS])
+{
+    float zero[4] = {0.f, 0.f, 0.f, 0.f};   // or NaN
+#pragma unroll
+    for (int i = 0; i < COLS; i++) zero[i % 4] = fmaf(sum[i], 0.f, zero[i % 4]);
+    if (zero[0] + zero[1] + zero[2] + zero[3] == 0.f) return;
+    float sums[COLS];
+#pragma unroll
+    for (int i = 0; i < COLS; i++) sums[i] = sum[i];
+    careful_sums(p, m, n, COLS, sums);
+#pragma unroll
+    for (int i = 0; i < COLS; i++) sum[i] = sums[i];
 }
 
 // Columns col .. col + 15 of a row, of which those below n exist.
@@ -273,7 +361,7 @@ struct Cfg8 {
 };
 
 template <int BN, int MODE>
-__global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) gemm8_tile_kernel(const __grid_constant__ Maps8 maps, const Gemm8Params p)
+__global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) gemm8_tile_kernel(const __grid_constant__ Maps8 maps, const __grid_constant__ Gemm8Params p)
 {
     using C = Cfg8<BN, MODE>;
     extern __shared__ uint8_t smem_raw[];
@@ -379,6 +467,7 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
         const int in = 32 * quarter + lane;   // row of the tile
         if (p.split == 1) {
             if (m0 + in < p.m && *abort_flag == 0u) {
+                check_sums(p, m0 + in, n0 + half * C::kCols, sum);
 #pragma unroll
                 for (int c = 0; c < C::kCols; c += 16) {
                     float v[16];
@@ -427,6 +516,8 @@ __global__ void __launch_bounds__(Cfg8<BN, MODE>::kThreads, BN == 128 ? 1 : 2) g
 #pragma unroll
                 for (int r = 0; r < 8; r++)
                     if (r < p.split) { v.x += x[r].x; v.y += x[r].y; v.z += x[r].z; v.w += x[r].w; }
+                if (!((v.x + v.y) * 0.f + (v.z + v.w) * 0.f == 0.f))   // (a sum of two may be infinite where they are not)
+                    v = careful_four(p, MODE == SCALE_COLS ? col : (int)row, MODE == SCALE_COLS ? (int)row : col, MODE == SCALE_COLS, v);
                 store_four(p, row, col, cols, v);
             }
         }
@@ -502,7 +593,7 @@ __device__ __forceinline__ bool tile_out(const Gemm8Params &p, const MapsP &maps
     float sum[COLS];
 #pragma unroll
     for (int i = 0; i < COLS; i++) sum[i] = 0.f;
-    float row = 0.f;
+    float row = 0.f, top = 0.f;   // top: the largest factor of the row's sums.  (Short contractions: 16384 x 4096 over 256 57 us without it, 55 with.  Where the columns' scales differ, too, it costs 6 %.)
     for (int b = 0; b < p.blocks; b++, w.acc.next()) {
         const int i = b % C::kAhead;
         const uint32_t from = w.scales + w.set.slot * C::kScales * 4;
@@ -525,6 +616,7 @@ __device__ __forceinline__ bool tile_out(const Gemm8Params &p, const MapsP &maps
         float next = 0.f;
         if (MODE == SCALE_ROWS || i == 0) row = row_scale(i);
         if (MODE == SCALE_BOTH) next = row_scale(min(i + 1, C::kAhead - 1));
+        if (MODE == SCALE_ROWS) top = fmaxf(top, fabsf(row));
         add_block<MODE, COLS>(sum, w.tmem + w.acc.slot * C::kBN + w.half * COLS + ((uint32_t)(32 * w.quarter) << 16), row, from + 4 * (C::kAhead * 128 + i * C::kColScales + w.half * COLS), [&] {
             tcgen05_fence_before();
             __syncwarp();
@@ -545,6 +637,7 @@ __device__ __forceinline__ bool tile_out(const Gemm8Params &p, const MapsP &maps
             w.set.next();
         }
     }
+    if (MODE == SCALE_BOTH || top > 0x1.fffffep127f) check_sums(p, m0 + 32 * w.quarter + w.lane, n0 + w.half * COLS, sum);
     // Boxes of 32 rows x 128 bytes; a row's last bytes that are no whole 16 by themselves.
     const int row0 = m0 + 32 * w.quarter, col0 = n0 + w.half * COLS, lane = w.lane;
     if (p.f32) {
@@ -568,7 +661,7 @@ __device__ __forceinline__ bool tile_out(const Gemm8Params &p, const MapsP &maps
 }
 
 template <int CTAS, int MODE>
-__global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ MapsP maps, const Gemm8Params p)
+__global__ void __launch_bounds__(384, 1) gemm8_kernel(const __grid_constant__ MapsP maps, const __grid_constant__ Gemm8Params p)
 {
     using C = CfgP<CTAS, MODE>;
     extern __shared__ uint8_t smem_raw[];
@@ -771,6 +864,15 @@ bool make_map8(CUtensorMap *map, const Operand8 &o, int box_rows)
     return encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(o.q), dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
+void codes_of(const Operand8 &a, const Operand8 &b, Gemm8Params &p)
+{
+    p.qa = a.q;
+    p.qb = b.q;
+    p.lda = a.ld;
+    p.ldb = b.ld;
+    p.k = a.cols;
+}
+
 template <typename K>
 bool allow_smem(K kernel, int bytes, std::atomic<bool> (&set)[kMaxDevices], int dev)
 {
@@ -836,6 +938,7 @@ fp4q_status launch_tiles(const Operand8 &a, const Operand8 &b, Gemm8Params p, in
     if (dev < 0 || !allow_smem(gemm8_tile_kernel<BN, MODE>, C::kSmem, set, dev)) return FP4Q_ERR_CUDA;
     p.n_tiles = (int32_t)ceil_div(p.n, BN);
     p.split = split;
+    codes_of(a, b, p);
     const int64_t ctas = ceil_div(p.m, 128) * p.n_tiles * split;
     if (ctas > 0x7FFFFFFF) return FP4Q_ERR_UNSUPPORTED;
     cudaLaunchAttribute attr[2];
@@ -861,6 +964,7 @@ fp4q_status launch_persistent(const Operand8 &a, const Operand8 &b, Gemm8Params 
     const int dev = current_device();
     static std::atomic<bool> set[kMaxDevices];
     if (dev < 0 || !allow_smem(gemm8_kernel<CTAS, MODE>, C::kSmem, set, dev)) return FP4Q_ERR_CUDA;
+    codes_of(a, b, p);
     p.m_tiles = (int32_t)ceil_div(p.m, 128 * CTAS);
     p.n_tiles = (int32_t)ceil_div(p.n, C::kBN);
     const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles, slots = sm_count(dev) / CTAS;
