@@ -523,9 +523,14 @@ fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scra
         return launched(launch_dependent(kernel, dim3((unsigned)ctas), d.threads, s, p));
     };
     static std::atomic<int> known[10];
+    auto join = [&] {
+        const SumParams q = {p.partial, p.cols, (int32_t)parts, accumulate != 0, dweight};
+        return launched(launch_dependent(column_sum_kernel, dim3((unsigned)ceil_div(p.cols, 32)), 1024, s, q));
+    };
     if (dweight && !fused) {   // before dx, which may overwrite what this reads
         parts = std::max<int64_t>(1, std::min<int64_t>(kGradCtas / 2, ceil_div(p.rows, 8)));
         if (fp4q_status st = launched(launch_dependent(rms_norm_dweight_kernel<TY, TH>, dim3((unsigned)ceil_div(p.cols, 512), (unsigned)parts), 256, s, p))) return st;
+        if (fp4q_status st = join()) return st;
     }
     if (fused || p.rows > 0) {
         fp4q_status st;
@@ -546,9 +551,7 @@ fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scra
         }
         if (st) return st;
     }
-    if (!dweight) return FP4Q_OK;
-    const SumParams q = {p.partial, p.cols, (int32_t)parts, accumulate != 0, dweight};
-    return launched(launch_dependent(column_sum_kernel, dim3((unsigned)ceil_div(p.cols, 32)), 1024, s, q));
+    return fused ? join() : FP4Q_OK;
 }
 
 }  // namespace
