@@ -1010,9 +1010,10 @@ struct Plan8 {
             consider((double)ceil_div(tiles, both ? clusters_at_once<SCALE_BOTH>((int)s, dev) : clusters_at_once<SCALE_ROWS>((int)s, dev)) * ((double)ceil_div(blocks, s) * each + 2.0) +
                          (s > 1 ? 2.5 + 0.15 * (double)s : 0.0), 0, (int)s);
         if (!boxes) return;
-        consider((double)ceil_div(tiles, 148) * ((double)blocks * (both ? 0.47 : 0.365) + 1.3), 1, 1);
-        const int64_t large = ceil_div(m, 256) * ceil_div(n, 256), last = large % 74;
-        consider(((double)(large / 74) + (last == 0 ? 0.0 : last <= 37 ? 0.7 : 1.0)) * ((double)blocks * (both ? 0.71 : 0.55) + 2.2), 2, 1);
+        const int64_t sms = sm_count(dev), slots = sms / 2;
+        consider((double)ceil_div(tiles, sms) * ((double)blocks * (both ? 0.47 : 0.365) + 1.3), 1, 1);
+        const int64_t large = ceil_div(m, 256) * ceil_div(n, 256), last = large % slots;
+        consider(((double)(large / slots) + (last == 0 ? 0.0 : 2 * last <= slots ? 0.7 : 1.0)) * ((double)blocks * (both ? 0.71 : 0.55) + 2.2), 2, 1);
     }
 };
 

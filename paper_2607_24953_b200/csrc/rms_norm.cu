@@ -7,6 +7,7 @@
 #include "common.cuh"
 #include "fp8_format.cuh"
 #include "row_io.cuh"
+#include "tensor_map.cuh"
 
 #include <algorithm>
 #include <atomic>
@@ -499,9 +500,12 @@ int resident(void (*kernel)(const P), int threads, std::atomic<int> &known)
 template <typename TX, typename TH>
 fp4q_status launch_norm(const NormParams &p, const Deal &d, bool in, bool out, cudaStream_t s)
 {
+    const int dev = current_device();
+    if (dev < 0) return FP4Q_ERR_CUDA;
+    const int64_t sms = sm_count(dev);
     auto launch = [&](auto kernel, std::atomic<int> &known) {
         const int64_t ctas = ceil_div(p.rows, d.threads / d.team);
-        const dim3 grid((unsigned)std::min<int64_t>(ctas, 148 * resident(kernel, d.threads, known)));
+        const dim3 grid((unsigned)std::min<int64_t>(ctas, sms * resident(kernel, d.threads, known)));
         return launched(launch_dependent(kernel, grid, d.threads, s, p));
     };
     static std::atomic<int> known[5];
@@ -516,9 +520,12 @@ fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scra
     p.team = d.team;
     const bool fused = dweight && p.cols <= kGradFused;
     p.partial = dweight ? static_cast<float *>(scratch) : nullptr;
+    const int dev = current_device();
+    if (dev < 0) return FP4Q_ERR_CUDA;
+    const int64_t sms = sm_count(dev);
     int64_t parts = 1;
     auto launch = [&](auto kernel, std::atomic<int> &known) {
-        const int64_t ctas = std::max<int64_t>(1, std::min({(int64_t)kGradCtas, ceil_div(p.rows, d.threads / d.team), (int64_t)148 * resident(kernel, d.threads, known)}));
+        const int64_t ctas = std::max<int64_t>(1, std::min({(int64_t)kGradCtas, ceil_div(p.rows, d.threads / d.team), sms * resident(kernel, d.threads, known)}));
         if (fused) parts = ctas;
         return launched(launch_dependent(kernel, dim3((unsigned)ctas), d.threads, s, p));
     };
