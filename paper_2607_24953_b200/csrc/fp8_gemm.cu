@@ -1025,15 +1025,20 @@ fp4q_status product8(const Operand8 &a, const Operand8 &b, Gemm8Params p, bool b
     p.blocks = (int32_t)ceil_div(a.cols, kBlock8);
     p.sa = a.scales;
     p.sb = b.scales;
+    const int dev = current_device();
+    if (dev < 0) return FP4Q_ERR_CUDA;
     if (!both && a.rows <= 64) {   // few tokens: B's rows become the tile's 128 rows, of which an SM has room for two tiles; B is read at memory's pace when all SMs read
         std::swap(p.m, p.n);
         std::swap(p.sa, p.sb);
-        const int64_t tiles = ceil_div(b.rows, 128);
-        const int split = (int)std::max<int64_t>(1, std::min<int64_t>({8, tiles <= 64 ? ceil_div(160, tiles) : 296 / tiles, p.blocks / 2}));
+        const int64_t tiles = ceil_div(b.rows, 128), sms = sm_count(dev);
+        // CTAs of a tile: one an SM for few tiles, as far as clusters reach all SMs, two an SM for more, which clusters of over four leave idle.  One token, contractions of 4096 and 11008: 24 tiles
+        // by 5 5.8 and 9.0 us, by 7 6.5 and 9.3; 32 by 4 6.2 and 10.1, by 5 6.8 and 10.4; 40 by 4 7.4 and 11.9, by 7 10.5 and 15.3; 64 by 3 8.7 and 15.2, by 4 8.2 and 13.4, by 5 11.6 and
+        // 19.0; 148 by 2 11.6 and 36.1, by 1 12.2 and 37.1.
+        int64_t each = tiles <= 32 ? 7 * sms / 8 / tiles : std::min<int64_t>(4, 2 * sms / tiles);
+        if (each == 7) each = 6;   // 17 tiles by 7 6.2 and 8.9 us, by 6 5.6 and 8.2
+        const int split = (int)std::max<int64_t>(1, std::min<int64_t>({8, each, p.blocks / 2}));
         return a.rows <= 16 ? launch_tiles<16, SCALE_COLS>(b, a, p, split, stream) : a.rows <= 32 ? launch_tiles<32, SCALE_COLS>(b, a, p, split, stream) : launch_tiles<64, SCALE_COLS>(b, a, p, split, stream);
     }
-    const int dev = current_device();
-    if (dev < 0) return FP4Q_ERR_CUDA;
     // Before the kernels' clusters are asked for, their shared memory is allowed.
     static std::atomic<bool> rows_set[kMaxDevices], both_set[kMaxDevices];
     if (!(both ? allow_smem(gemm8_tile_kernel<128, SCALE_BOTH>, Cfg8<128, SCALE_BOTH>::kSmem, both_set, dev) : allow_smem(gemm8_tile_kernel<128, SCALE_ROWS>, Cfg8<128, SCALE_ROWS>::kSmem, rows_set, dev)))
