@@ -548,8 +548,11 @@ fp4q_status launch_grad(GradParams p, float *dweight, int accumulate, void *scra
                              : launch(rms_norm_bwd_kernel<TY, TH, 1, false, false, kMost>, known[at + 2]);
         };
         if (d.chunks == 1) {
-            if constexpr (sizeof(TH) == 4)   // two CTAs an SM on an FP32 stream too, where they have no more threads (1999 x 2731 23.6 -> 20.6 us)
-                st = d.threads <= 384 ? one(std::integral_constant<int, 384>(), 5) : one(std::integral_constant<int, 512>(), 0);
+            // On an FP32 stream registers for 384 threads let two CTAs of 256 to 384 threads run on an SM where those for 512 leave room for one, and three of 256 instead of two.  The more CTAs,
+            // the more sums there are to join: few elements in CTAs of 256 are better off without.  8192 x 3000 51 us for 67, 1999 x 2731 18.0 for 20.9, 300 x 2731 7.3 for 8.6; 256 threads: 8192 x
+            // 2048 35 for 38, 16384 x 1000 37 for 40, but 1999 x 2048 12.9 for 12.5, 1999 x 512 7.8 for 6.7, 8192 x 512 12.7 for 12.1.
+            if constexpr (sizeof(TH) == 4)
+                st = d.threads <= 384 && (d.threads > 256 || p.rows * p.cols >= 1 << 23) ? one(std::integral_constant<int, 384>(), 5) : one(std::integral_constant<int, 512>(), 0);
             else st = one(std::integral_constant<int, 512>(), 0);
         } else {
             st = d.chunks == 2 ? in && out ? launch(rms_norm_bwd_kernel<TY, TH, 2, true, true>, known[3]) : launch(rms_norm_bwd_kernel<TY, TH, 2, false, false>, known[4])
