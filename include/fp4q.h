@@ -550,7 +550,7 @@ fp4q_status fp4q_rms_norm_bwd(const fp4q_norm_grad *n, int64_t rows, int64_t col
  * elements, aligned to their elements), the gradients of a step; into the FP32 at `norm` (device memory).  Squares are added in 64 bits or, where that loses nothing, in FP32 runs of 32;
  * the order is fixed.  `tensors` is a HOST array, read during the call; empty tensors are skipped; without any the norm is 0.
  * fp4q_clip_by_norm -- out = g * min(1, max_norm / (norm + eps)), every tensor into its entry of `outs` (rounded once; BF16 or FP32, the same shape; not
- * overlapping another's), or in place (outs == NULL; then tensors stay untouched where the factor is 1).  A norm of NaN gives NaN.  max_norm >= 0, eps >= 0.
+ * overlapping another's), or in place (outs == NULL; then tensors stay untouched where the factor is 1).  A norm of NaN gives NaN; where norm + eps is 0 the factor is 1.  max_norm >= 0, eps >= 0.
  * fp4q_clip_grad_norm -- both, one launch less.
  * scratch: fp4q_global_norm_scratch_bytes() bytes of device memory, 256-byte aligned, any contents; calls that share it must not overlap on the GPU.
  */

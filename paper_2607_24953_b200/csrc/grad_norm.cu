@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(256) scale_kernel(const __grid_constant__ Span
     __shared__ double sums[8];
     const float norm = p.parts ? root_of(p.partial, p.parts, sums) : load_global(p.norm);
     if (p.parts && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
-    const float ratio = __fdiv_rn(p.max_norm, norm + p.eps), factor = ratio > 1.f ? 1.f : ratio;
+    const float bound = norm + p.eps, ratio = __fdiv_rn(p.max_norm, bound), factor = ratio > 1.f || bound == 0.f ? 1.f : ratio;   // zeros stay zeros
     if (p.in_place && factor == 1.f) return;
     for (int64_t back = blockIdx.x; back < p.chunks; back += gridDim.x) {
         const int64_t chunk = p.chunks - 1 - back;
