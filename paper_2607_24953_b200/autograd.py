@@ -296,8 +296,11 @@ def rms_norm_fp8_linear(x: torch.Tensor, norm_weight, weight: torch.Tensor, resi
 def clip_grad_norm_(parameters, max_norm: float, eps: float = 1e-6) -> torch.Tensor:
     """Scales the gradients of the parameters (one tensor, or any of them) in place so that the norm of all of them together is at most max_norm.  Returns the norm before, a number on
     the device.  BF16 and FP32, on one device."""
-    grads = [p.grad for p in ([parameters] if isinstance(parameters, torch.Tensor) else parameters) if p.grad is not None]
-    return binding.fp4q_clip_grad_norm(grads, max_norm, eps=eps) if grads else torch.zeros(())
+    parameters = [parameters] if isinstance(parameters, torch.Tensor) else list(parameters)
+    grads = [p.grad for p in parameters if p.grad is not None]
+    if not grads:
+        return torch.zeros((), device=parameters[0].device if parameters else None)
+    return binding.fp4q_clip_grad_norm(grads, max_norm, eps=eps)
 
 
 class FP4Linear(torch.nn.Module):

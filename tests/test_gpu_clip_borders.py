@@ -17,3 +17,10 @@ def test_zeros_stay_zeros_without_an_eps(max_norm, dtype):
     assert float(b.fp4q_clip_grad_norm(g, max_norm, eps=0.0)) == 0 and not any(t.any() for t in g)
     b.fp4q_clip_by_norm(g, torch.zeros((), device="cuda"), max_norm, eps=0.0)
     assert not any(t.any() for t in g)
+
+
+def test_the_norm_of_no_gradients_is_on_the_parameters_device():
+    p = torch.nn.Parameter(torch.ones(5, device="cuda"))
+    for norm in (autograd.clip_grad_norm_([p], 1.0), autograd.clip_grad_norm_(p, 1.0), autograd.clip_grad_norm_(iter([p, p]), 1.0)):
+        assert norm.device == p.device and norm.dtype == F32 and norm.shape == () and float(norm) == 0
+    assert autograd.clip_grad_norm_([], 1.0) == 0
