@@ -4,8 +4,8 @@
 // A stage of the operand ring is one block: rows of 128 bytes.  Four tcgen05.mma (kind::f8f6f4, 32 elements each) make the block's product in an accumulator of its
 // own in tensor memory; the epilogue's warps take it from there, times its scales, into sums in registers, while the next block's MMAs run into
 // another accumulator.  The accumulator that the tensor cores cut off towards zero is thus never longer than 128 elements; the sums are rounded to nearest.
-// Bound by that path of the accumulators, 1100 cycles a block of a pair's tile where its MMAs take 512: 16384 x 11008 x 4096 797 us (1.85 PFLOP/s; 690 in a short run), the weight gradient of 4096 x 4096 over
-// 16384 rows 400.  One token: bound by the weight's bytes, 4096 x 11008 12.3 us.
+// Bound by that path of the accumulators, 1100 cycles a block of a pair's tile where its MMAs take 512: 16384 x 11008 x 4096 800 us (1.85 PFLOP/s; 690 in a short run), the weight gradient of 4096 x 4096 over
+// 16384 rows 411.  One token: bound by the weight's bytes, 4096 x 11008 12.3 us.
 #include "fp8_format.cuh"
 #include "gemm16.cuh"
 

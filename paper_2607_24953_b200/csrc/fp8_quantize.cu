@@ -3,7 +3,7 @@
 // A CTA of 8 warps owns 128 x 128 elements: one block of every row, one of every column, one square block.  A warp has 16 rows, a lane 4 consecutive rows x 16
 // columns, so that eight lanes make a row's block and a lane's four rows a word of the transposed codes; those cross 16 KB of shared memory
 // (pieces of 16 bytes, swizzled by the column's group) and leave as 128 consecutive bytes a column.  Bound by memory, 2 or 4 bytes an element read and 1 or 2 written, and nearly as much by its instructions:
-// 16384 x 4096 BF16, both orientations, 54 us, 5.1 TB/s; FP32 in square blocks 64 us, 6.3 TB/s.  BF16 with four CTAs an SM (64 registers) 52 us in a row, with three 56.
+// 16384 x 4096 BF16, both orientations, 55 us, 5.0 TB/s; FP32 in square blocks 64 us, 6.3 TB/s.  BF16 with four CTAs an SM (64 registers) 52 us in a row, with three 56.
 #include "common.cuh"
 #include "fp8_format.cuh"
 #include "row_io.cuh"

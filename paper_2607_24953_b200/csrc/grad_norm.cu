@@ -2,7 +2,7 @@
 //
 // Every tensor is cut into units of 8 elements, those of a row on the 16-byte grid of its memory, and chunks of 1024 units, which the CTAs take in turn; the
 // tensors' descriptions travel as kernel parameters, up to 450 a launch.  Bound by memory: the norm reads everything, the clipping reads it again, last
-// chunks first, since those are still in L2, and writes it.  202 M FP32 elements into BF16 309 us: 124 for the norm (6.5 TB/s), 181 for the scaling (6.7).
+// chunks first, since those are still in L2, and writes it.  202 M FP32 elements into BF16 312 us: 124 for the norm (6.5 TB/s), 181 for the scaling (6.7).
 #include <cuda_bf16.h>
 
 #include "common.cuh"

@@ -3,7 +3,7 @@
 //
 // A row belongs to a team of threads, each with 16 consecutive columns at a time (one 32-byte piece of BF16), which stay in registers from the row's
 // only reading on: the sum of squares goes through shuffles and, for teams of several warps, shared memory; blocks of 32 or 128 elements are 2 or 8 lanes, so
-// their maxima need shuffles alone.  Bound by memory: 16384 x 4096, BF16, with a residual, BF16 and 8-bit outputs 606 MB in 98 us, 6.2 TB/s; its backward pass 537 MB in 97 us.
+// their maxima need shuffles alone.  Bound by memory: 16384 x 4096, BF16, with a residual, BF16 and 8-bit outputs 606 MB in 101 us, 6.0 TB/s; its backward pass 537 MB in 100 us.
 #include "common.cuh"
 #include "fp8_format.cuh"
 #include "row_io.cuh"
