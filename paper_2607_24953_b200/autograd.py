@@ -166,8 +166,10 @@ def _norm(x, weight, residual, eps, q=binding.Q_NONE, y=True):
     out = binding.alloc_norm(x, residual if whole else None, y=False, q=q, rstd=True)
     if residual is not None and not whole:
         out.h = torch.empty((rows, cols), dtype=residual.dtype, device=x.device)
-    if y:
-        out.y = torch.empty((rows, cols if q == binding.Q_NONE else (cols + 7) // 8 * 8), dtype=x.dtype, device=x.device)[:, :cols]
+    if y and (whole or q == binding.Q_NONE):   # no view: what a layer returns may be changed in place
+        out.y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    elif y:
+        out.y = torch.empty((rows, (cols + 7) // 8 * 8), dtype=x.dtype, device=x.device)[:, :cols]
     return binding.fp4q_rms_norm(x, weight, residual, eps=eps, out=out)
 
 

@@ -54,3 +54,17 @@ def test_nothing_is_kept_for_a_backward_pass_where_gradients_are_off(dtype):
         assert torch.equal(y, want)
         # codes and scales of x and of the weight, the output, 1 / root of every row
         assert most <= (rows + n) * cols + rows * (cols // 128) * 4 + y.numel() * 2 + 6 * (2 << 20)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("cols", [64, 70, 75, 9001])
+def test_outputs_may_be_changed_in_place(cols, dtype):
+    x, r, g, w = randn(1, 30, cols).to(dtype).requires_grad_(), randn(2, 30, cols).to(dtype).requires_grad_(), (1 + 0.2 * randn(3, cols)).requires_grad_(), (randn(4, 20, cols) * 0.05).requires_grad_()
+    for f in (lambda: autograd.rms_norm(x, g), lambda: autograd.rms_norm(x, g, r)[0], lambda: autograd.fp8_linear(x, w), lambda: autograd.rms_norm_fp8_linear(x, g, w), lambda: autograd.rms_norm_fp8_linear(x, g, w, r)[0]):
+        x.grad = None
+        y = f()
+        y.mul_(2)
+        y.sum().backward()
+        got, x.grad = x.grad, None
+        (f() * 2).sum().backward()
+        assert torch.equal(got, x.grad)
