@@ -275,7 +275,8 @@ def _check_linear(x, weight):
 
 def fp8_linear(x: torch.Tensor, weight: torch.Tensor, ws=None) -> torch.Tensor:
     """y = x^ weight^^T with products in 8 bits, forward and backward: E4M3 codes with a scale for every 128 elements of a row of x and of the gradient, and for 128 x 128 of the
-    weight.  x [..., K], weight [N, K], BF16 or FP32 (other floating-point types are taken in FP32).  y is BF16.  Straight-through; differentiable once."""
+    weight.  x [..., K], weight [N, K], BF16 or FP32 (other floating-point types are taken in FP32).  y is BF16.  Straight-through; differentiable once.
+    A backward pass that is captured into a CUDA graph needs, as ragged_linear's, leaves that no living eager graph holds."""
     _check_linear(x, weight)
     if ws is None:
         ws = binding.alloc_workspace(x.device)
